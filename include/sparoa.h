@@ -385,6 +385,151 @@ sparoa_status sparoa_attention(sparoa_ctx *ctx, const void *qkv, int64_t N, int6
                                int32_t heads, int32_t head_dim, void *y,
                                const sparoa_occupancy *y_occ);
 
+/* ------------------------------------------------------------------------ */
+/* Operators of a decoder that serves from a paged key/value cache            */
+/*                                                                            */
+/* The paper's operators end at encoders (Sec. 3.2: LN, MHSA); these three are */
+/* what a transformer that answers token by token needs beside sparoa_gemm.    */
+/* ------------------------------------------------------------------------ */
+
+typedef enum { SPAROA_NORM_NONE = 0, SPAROA_NORM_RMS = 1, SPAROA_NORM_LAYER = 2 } sparoa_norm_kind;
+
+/* A norm over a row v of C values, computed in fp32:
+ *   RMS    v / sqrt(mean(v^2) + eps)
+ *   LAYER  (v - mean(v)) / sqrt(biased variance + eps)
+ * then * weight + bias (each device fp32 [C], 16-byte aligned, or NULL). */
+typedef struct {
+    int32_t kind;            /* sparoa_norm_kind                             */
+    float eps;
+    const float *weight;
+    const float *bias;
+} sparoa_norm_spec;
+
+/*
+ * The residual step between two blocks, in one pass over memory:
+ *   r = x + scale * gate[row / rows_per_gate] * N_post(h),   y = N_pre(r)
+ * over [R, C].  y is computed from r in fp32, before r is rounded to its type.
+ *   x     residual stream, `res_dtype` (SPAROA_BF16 or SPAROA_F32); NULL: zero
+ *   h     bf16 output of the block before; NULL: r = x (then post and gate must
+ *         be absent)
+ *   post, pre  norms (NULL: none; y is then r)
+ *   gate  device fp32 [ceil(R / rows_per_gate)][C]; rows_per_gate 0: one row
+ *         [C] for all; NULL: 1
+ *   r     residual stream after the step, `res_dtype` (nullable); may be x
+ *   y     bf16 input of the next block (nullable); may be h
+ *   y_occ occupancy of y to write (nullable; needs y)
+ * Tensors are contiguous and 16-byte aligned; but for r = x and y = h outputs
+ * overlap nothing.  C % 8 == 0, C <= 16384.
+ * Errors: INVALID_ARG, UNSUPPORTED (C > 16384), CUDA. */
+sparoa_status sparoa_add_norm(sparoa_ctx *ctx, const void *x, const void *h, int64_t R, int64_t C,
+                              int32_t res_dtype, const sparoa_norm_spec *post, const float *gate,
+                              int64_t rows_per_gate, float scale, const sparoa_norm_spec *pre,
+                              void *r, void *y, const sparoa_occupancy *y_occ);
+
+/* Keys and values of cached tokens: bf16 pools
+ * [pages][kv_heads][page_size][head_dim], 16-byte aligned, caller-owned.  The
+ * places that no token was written to may hold anything; what was written has
+ * to be finite. */
+typedef struct {
+    void *k, *v;
+    int64_t pages;           /* in each pool; pages * kv_heads * page_size < 2^31 */
+    int32_t page_size;       /* tokens: 16, 32, 64 or 128                     */
+    int32_t kv_heads;
+    int32_t head_dim;        /* 64 or 128                                     */
+    int32_t reserved;
+} sparoa_kv_cache;
+
+/* New tokens of `batch` sequences, and where their cached tokens are.  The lists
+ * are on the device, so that a captured graph follows them.
+ * Sequence b has n = q_start[b+1] - q_start[b] new tokens in rows q_start[b]
+ * onwards of the call's tensors, and kv_len[b] tokens in the cache, the new ones
+ * (its last n) included.  Its positions [i page_size, (i+1) page_size) are in page
+ * table[b table_stride + i]; entries that no position below kv_len[b] needs are not
+ * read.  Rows that belong to no sequence are left as they are. */
+typedef struct {
+    const int32_t *q_start;  /* [batch + 1], not decreasing                   */
+    const int32_t *kv_len;   /* [batch]                                       */
+    const int32_t *table;    /* [batch][table_stride]                         */
+    int64_t table_stride;    /* >= max_pages                                  */
+    int32_t batch;           /* 1 to 1024                                     */
+    int32_t max_pages;       /* entries of a row of the table                 */
+    int32_t max_q;           /* new tokens of a sequence at most: chooses the
+                                kernel; any value gives right results          */
+    int32_t reserved;
+} sparoa_paged_batch;
+
+typedef enum { SPAROA_ROPE_HALF = 0, SPAROA_ROPE_INTERLEAVED = 1 } sparoa_rope_layout;
+
+typedef enum {
+    SPAROA_ROPE_SCALE_NONE = 0,
+    SPAROA_ROPE_SCALE_LINEAR = 1, /* every frequency / factor                  */
+    SPAROA_ROPE_SCALE_BASE = 2,   /* base * factor^(rot / (rot - 2))           */
+    SPAROA_ROPE_SCALE_PARTS = 3   /* by the turns that a pair makes over
+                                     `context` positions: `high` or more keep
+                                     their frequency, `low` or fewer take
+                                     frequency / factor, a ramp between        */
+} sparoa_rope_scaling;
+
+/* Rotary positions: pair i of the first `rot` values of a head turns by
+ * position * f_i, and both values are multiplied by `scale`.  HALF pairs value i
+ * with i + rot / 2, INTERLEAVED 2 i with 2 i + 1. */
+typedef struct {
+    int32_t rot;             /* a multiple of 16, 0 to head_dim              */
+    int32_t layout;          /* sparoa_rope_layout                            */
+    const uint64_t *turns;   /* device [rot / 2], from sparoa_rope_turns       */
+    float scale;             /* of cos and sin (1: plain rotation)             */
+    int32_t reserved;
+} sparoa_rope;
+
+/* Frequencies f_i = base^(-2 i / rot), scaled as asked, as the fraction of a turn
+ * per position in units of 2^-64: position * turns[i] modulo 2^64 is the angle of
+ * any position without rounding.  Host-only; `turns` is a host array [rot / 2].
+ * factor, context, low and high are read where the scaling uses them.
+ * Errors: INVALID_ARG. */
+sparoa_status sparoa_rope_turns(int32_t rot, double base, int32_t scaling, double factor,
+                                double context, double low, double high, uint64_t *turns);
+
+/*
+ * From the rows of a QKV projection to queries and cache, in one pass: per new
+ * token, its `heads` query heads and the cache's kv_heads key heads are rotated,
+ * queries go to q_out, keys and values to the token's place in the cache.
+ *   qkv   bf16 [T][ld_qkv >= (heads + 2 kv_heads) head_dim], q | k | v per row
+ *   q_out bf16 [T][ld_q >= heads head_dim]; may be qkv itself with ld_q = ld_qkv
+ *   positions  device int32 [T]: angles go by these (NULL: by the token's place in
+ *         its sequence); the place in the cache always goes by kv_len
+ * Row lengths are multiples of 8 values, pointers 16-byte aligned.  A new token
+ * before its sequence's first position (n > kv_len) is rotated but not cached.
+ * An entry of the table outside [0, pages), or a position past the table's row, is
+ * not written to and is reported as INVALID_ARG by the next call that synchronises.
+ * Errors: INVALID_ARG, UNSUPPORTED (head_dim, page_size, batch), CUDA. */
+sparoa_status sparoa_rope_append(sparoa_ctx *ctx, const void *qkv, int64_t ld_qkv, int64_t T,
+                                 int32_t heads, const sparoa_rope *rope, const int32_t *positions,
+                                 const sparoa_kv_cache *cache, const sparoa_paged_batch *batch,
+                                 void *q_out, int64_t ld_q);
+
+/*
+ * Attention of the new tokens over the cache (their own keys and values included:
+ * append first): per query head, with key head h / (heads / kv_heads),
+ *   y = softmax(scale Q K^T) V
+ * in tensor cores with fp32 scores, softmax statistics and accumulation; for the
+ * P V products the probabilities are two bf16 parts (16 bits) each.  The token at position p sees
+ * the keys j < kv_len with j <= p (causal) and j > p - window (window > 0).  A row
+ * that sees no key is zero.
+ *   q     bf16 [T][ld_q >= heads head_dim], ld_q % 8 == 0, 16-byte aligned
+ *   y     bf16 [T][heads head_dim], 16-byte aligned
+ *   lse   device fp32 [T][heads] (nullable): log of the sum of exp(scale q k) over
+ *         the keys that a row sees (-infinity for none)
+ *   y_occ occupancy of y to write (nullable); rows of no sequence count as they are
+ * Splits long sequences over the GPU; partial results live in a workspace that the
+ * context keeps for each stream it is used on.  A table entry outside [0, pages), or
+ * a length past the table's row, is reported as INVALID_ARG by the next call that
+ * synchronises, and the affected rows hold anything.
+ * Errors: INVALID_ARG, UNSUPPORTED (head_dim, page_size, batch), CUDA, OOM, TIMEOUT. */
+sparoa_status sparoa_paged_attention(sparoa_ctx *ctx, const void *q, int64_t ld_q, int64_t T,
+                                     int32_t heads, float scale, int32_t causal, int32_t window,
+                                     const sparoa_kv_cache *cache, const sparoa_paged_batch *batch,
+                                     void *y, float *lse, const sparoa_occupancy *y_occ);
+
 /*
  * Run a topologically ordered operator list (Sec. 4.1 layer execution order;
  * Sec. 5.1 operator-by-operator execution) on one GPU.  The input x is bf16

@@ -2,6 +2,7 @@
 // Declarations and documentation: include/sparoa.h.
 #include <cuda_runtime.h>
 
+#include <cmath>
 #include <cstdarg>
 #include <cstdio>
 #include <cstring>
@@ -74,17 +75,30 @@ struct DevBuf {
   size_t bytes = 0;
 };
 
+// Paged attention's scratch, one for each stream that a context is used on: calls on
+// two streams may run at once.
+struct PagedSlot {
+  cudaStream_t stream = nullptr;
+  bool taken = false;
+  DevBuf ws;
+};
+constexpr int kPagedSlots = 16;
+constexpr size_t kSmallBytes = 256;  // d_err(), d_path(), d_count()
+constexpr size_t kPagedCntBytes = sizeof(unsigned) * kPagedSlots * kPagedCounters;
+
 }  // namespace
 
 struct sparoa_ctx {
   int device = 0;
   cudaStream_t stream = nullptr;
   std::string last_error;
-  DevBuf small;       // u32 error flag, i32 path slot, padding
+  DevBuf small;       // u32 error flag, i32 path slot, padding; paged attention's counters
   DevBuf occ;         // occupancy of inputs measured inside a call
   DevBuf pad_x, pad_w;
   DevBuf arena;       // sparoa_run_graph activations, occupancies, paths
   DevBuf splitk;      // split-K arrival counters (kept zero) + fp32 partial tiles
+  PagedSlot paged[kPagedSlots];
+  int paged_next = 0;  // the slot given to a new stream once all are taken
   std::vector<sparoa_occupancy> graph_occ;
   int overlap = 1;    // programmatic dependent launch between consecutive kernels
   int64_t wait_limit = 0;  // SM cycles before a kernel's bounded wait gives up (0: default)
@@ -95,6 +109,9 @@ struct sparoa_ctx {
   int32_t* d_path() const { return reinterpret_cast<int32_t*>(reinterpret_cast<char*>(small.p) + 16); }
   // Eq. 1 count of an FC input that the fused small-FC kernel measures itself
   uint64_t* d_count() const { return reinterpret_cast<uint64_t*>(reinterpret_cast<char*>(small.p) + 32); }
+  unsigned* d_paged_cnt(int slot) const {
+    return reinterpret_cast<unsigned*>(reinterpret_cast<char*>(small.p) + kSmallBytes) + slot * kPagedCounters;
+  }
 };
 
 namespace {
@@ -415,6 +432,9 @@ sparoa_status read_device_error(sparoa_ctx* ctx) {
   if (err) {
     SP_CUDA(cudaMemsetAsync(ctx->d_err(), 0, 4, ctx->stream));
     SP_CUDA(cudaStreamSynchronize(ctx->stream));
+    if (err == kErrBadIndex)
+      return fail(ctx, SPAROA_ERR_INVALID_ARG,
+                  "a page table entry, a length or a first row on the device is out of its tensor's bounds");
     return fail(ctx, SPAROA_ERR_TIMEOUT, "a kernel's bounded wait ran out (code 0x%x)", err);
   }
   return SPAROA_OK;
@@ -626,13 +646,13 @@ sparoa_status sparoa_create(sparoa_ctx** out, int device, void* stream) {
   sparoa_ctx* ctx = new sparoa_ctx();
   ctx->device = device;
   ctx->stream = static_cast<cudaStream_t>(stream);
-  if (cudaMalloc(&ctx->small.p, 256) != cudaSuccess) {
+  if (cudaMalloc(&ctx->small.p, kSmallBytes + kPagedCntBytes) != cudaSuccess) {
     cudaGetLastError();
     delete ctx;
     return SPAROA_ERR_OOM;
   }
-  ctx->small.bytes = 256;
-  if (cudaMemset(ctx->small.p, 0, 256) != cudaSuccess) {
+  ctx->small.bytes = kSmallBytes + kPagedCntBytes;
+  if (cudaMemset(ctx->small.p, 0, ctx->small.bytes) != cudaSuccess) {
     cudaFree(ctx->small.p);
     delete ctx;
     return SPAROA_ERR_CUDA;
@@ -677,6 +697,8 @@ sparoa_status sparoa_destroy(sparoa_ctx* ctx) {
   if (ctx->aux) cudaStreamSynchronize(ctx->aux);
   for (DevBuf* b : {&ctx->small, &ctx->occ, &ctx->pad_x, &ctx->pad_w, &ctx->arena, &ctx->splitk})
     if (b->p) cudaFree(b->p);
+  for (PagedSlot& p : ctx->paged)
+    if (p.ws.p) cudaFree(p.ws.p);
   if (ctx->ev_fork) cudaEventDestroy(ctx->ev_fork);
   if (ctx->ev_join) cudaEventDestroy(ctx->ev_join);
   if (ctx->aux) cudaStreamDestroy(ctx->aux);
@@ -1236,6 +1258,251 @@ sparoa_status sparoa_bn_act(sparoa_ctx* ctx, const void* x, int64_t R, int64_t C
   if (y_occ) o = to_dev(*y_occ);
   SP_CUDA(launch_bn_act(static_cast<const __nv_bfloat16*>(x), R, (int)C, to_dev(ep),
                         static_cast<__nv_bfloat16*>(y), o, y_occ ? 1 : 0, ctx->stream));
+  return SPAROA_OK;
+}
+
+// ---------------------------------------------------------------------------
+// decoder operators
+// ---------------------------------------------------------------------------
+namespace {
+
+sparoa_status check_norm(sparoa_ctx* ctx, const sparoa_norm_spec* n, const char* what) {
+  if (!n) return SPAROA_OK;
+  if (n->kind < 0 || n->kind > 2) return fail(ctx, SPAROA_ERR_INVALID_ARG, "add_norm: %s: bad kind", what);
+  if (n->kind == 0) return SPAROA_OK;
+  if (!(n->eps >= 0.f)) return fail(ctx, SPAROA_ERR_INVALID_ARG, "add_norm: %s: eps", what);
+  if (!aligned16(n->weight) || !aligned16(n->bias))
+    return fail(ctx, SPAROA_ERR_INVALID_ARG, "add_norm: %s: misaligned parameter", what);
+  return SPAROA_OK;
+}
+
+NormDev to_dev(const sparoa_norm_spec* n) {
+  NormDev d;
+  if (!n || n->kind == 0) return d;
+  d.kind = n->kind;
+  d.eps = n->eps;
+  d.weight = n->weight;
+  d.bias = n->bias;
+  return d;
+}
+
+// The cache and the batch of sequences, checked for what the host can see.
+sparoa_status check_paged(sparoa_ctx* ctx, const sparoa_kv_cache* c, const sparoa_paged_batch* b, int64_t T,
+                          int32_t heads, const char* what) {
+  if (!c || !b) return fail(ctx, SPAROA_ERR_INVALID_ARG, "%s: no cache or batch", what);
+  if (c->head_dim != 64 && c->head_dim != 128)
+    return fail(ctx, SPAROA_ERR_UNSUPPORTED, "%s: head_dim 64 or 128 only", what);
+  if (c->page_size != 16 && c->page_size != 32 && c->page_size != 64 && c->page_size != 128)
+    return fail(ctx, SPAROA_ERR_UNSUPPORTED, "%s: pages of 16, 32, 64 or 128 tokens only", what);
+  if (c->kv_heads <= 0 || c->pages <= 0 || c->pages > (int64_t)0x7FFFFFFF / c->page_size / c->kv_heads)
+    return fail(ctx, SPAROA_ERR_INVALID_ARG, "%s: bad cache size", what);
+  if (!c->k || !c->v || !aligned16(c->k) || !aligned16(c->v))
+    return fail(ctx, SPAROA_ERR_INVALID_ARG, "%s: NULL or misaligned cache", what);
+  if (heads <= 0 || heads > 65536 || heads % c->kv_heads)
+    return fail(ctx, SPAROA_ERR_INVALID_ARG, "%s: heads must be a multiple of kv_heads", what);
+  if (b->batch <= 0) return fail(ctx, SPAROA_ERR_INVALID_ARG, "%s: empty batch", what);
+  if (b->batch > kPagedMaxBatch)
+    return fail(ctx, SPAROA_ERR_UNSUPPORTED, "%s: at most %d sequences", what, kPagedMaxBatch);
+  if (!b->q_start || !b->kv_len || (b->max_pages > 0 && !b->table))
+    return fail(ctx, SPAROA_ERR_INVALID_ARG, "%s: NULL list", what);
+  if (b->max_pages < 0 || b->max_pages > 0x7FFFFFFF / c->page_size || b->table_stride < b->max_pages || b->max_q < 0)
+    return fail(ctx, SPAROA_ERR_INVALID_ARG, "%s: bad table", what);
+  if (T < 0 || T > 0x7FFFFFFF) return fail(ctx, SPAROA_ERR_INVALID_ARG, "%s: bad number of tokens", what);
+  return SPAROA_OK;
+}
+
+int log2_of(int v) {
+  int l = 0;
+  while ((1 << l) < v) ++l;
+  return l;
+}
+
+// The scratch of the context's current stream.  A stream's first call may be under
+// capture: its buffer is then allocated in the relaxed mode (no work is enqueued).
+sparoa_status paged_slot(sparoa_ctx* ctx, int* out) {
+  for (int i = 0; i < kPagedSlots; ++i)
+    if (ctx->paged[i].taken && ctx->paged[i].stream == ctx->stream) {
+      *out = i;
+      return SPAROA_OK;
+    }
+  int i = 0;
+  while (i < kPagedSlots && ctx->paged[i].taken) ++i;
+  if (i == kPagedSlots) {
+    cudaStreamCaptureStatus cap = cudaStreamCaptureStatusNone;
+    SP_CUDA(cudaStreamIsCapturing(ctx->stream, &cap));
+    if (cap != cudaStreamCaptureStatusNone)
+      return fail(ctx, SPAROA_ERR_UNSUPPORTED, "paged_attention: capture on more than %d streams of a context", kPagedSlots);
+    SP_CUDA(cudaDeviceSynchronize());  // the slot's last calls may be running
+    i = ctx->paged_next;
+    ctx->paged_next = (i + 1) % kPagedSlots;
+  }
+  if (!ctx->paged[i].ws.p) {
+    cudaStreamCaptureMode mode = cudaStreamCaptureModeRelaxed;
+    SP_CUDA(cudaThreadExchangeStreamCaptureMode(&mode));
+    const sparoa_status st = ensure(ctx, ctx->paged[i].ws, paged_ws_bytes());
+    cudaThreadExchangeStreamCaptureMode(&mode);
+    SP_TRY(st);
+  }
+  ctx->paged[i].taken = true;
+  ctx->paged[i].stream = ctx->stream;
+  *out = i;
+  return SPAROA_OK;
+}
+
+}  // namespace
+
+sparoa_status sparoa_add_norm(sparoa_ctx* ctx, const void* x, const void* h, int64_t R, int64_t C, int32_t res_dtype,
+                              const sparoa_norm_spec* post, const float* gate, int64_t rows_per_gate, float scale,
+                              const sparoa_norm_spec* pre, void* r, void* y, const sparoa_occupancy* y_occ) {
+  if (!ctx) return SPAROA_ERR_INVALID_ARG;
+  if (R < 0 || C <= 0 || C % 8) return fail(ctx, SPAROA_ERR_INVALID_ARG, "add_norm: bad shape");
+  if (C > 16384) return fail(ctx, SPAROA_ERR_UNSUPPORTED, "add_norm: C <= 16384 only");
+  if (res_dtype != SPAROA_BF16 && res_dtype != SPAROA_F32)
+    return fail(ctx, SPAROA_ERR_INVALID_ARG, "add_norm: res_dtype");
+  if (R > 0 && ((!x && !h) || (!r && !y))) return fail(ctx, SPAROA_ERR_INVALID_ARG, "add_norm: no input or no output");
+  if (!h && ((post && post->kind != SPAROA_NORM_NONE) || gate))
+    return fail(ctx, SPAROA_ERR_INVALID_ARG, "add_norm: a norm or gate of no block output");
+  if (!aligned16(x) || !aligned16(h) || !aligned16(r) || !aligned16(y) || !aligned16(gate))
+    return fail(ctx, SPAROA_ERR_INVALID_ARG, "add_norm: misaligned");
+  if (rows_per_gate < 0) return fail(ctx, SPAROA_ERR_INVALID_ARG, "add_norm: rows_per_gate");
+  if (!y && y_occ) return fail(ctx, SPAROA_ERR_INVALID_ARG, "add_norm: y_occ without y");
+  SP_TRY(check_norm(ctx, post, "post"));
+  SP_TRY(check_norm(ctx, pre, "pre"));
+  SP_TRY(check_occ(ctx, y_occ, R, C, "add_norm y_occ"));
+  DeviceGuard g(ctx->device, ctx->overlap);
+  AddNormArgs a;
+  a.x = x;
+  a.h = static_cast<const __nv_bfloat16*>(h);
+  a.R = R;
+  a.C = (int)C;
+  a.res_f32 = res_dtype == SPAROA_F32;
+  a.post = to_dev(post);
+  a.pre = to_dev(pre);
+  a.gate = gate;
+  a.per = rows_per_gate;
+  a.scale = scale;
+  a.r = r;
+  a.y = static_cast<__nv_bfloat16*>(y);
+  SP_CUDA(launch_add_norm(a, ctx->stream));
+  if (y_occ) SP_TRY(run_stats(ctx, y, R, C, *y_occ));
+  return SPAROA_OK;
+}
+
+sparoa_status sparoa_rope_turns(int32_t rot, double base, int32_t scaling, double factor, double context, double low,
+                                double high, uint64_t* turns) {
+  if (rot < 0 || rot % 16 || (rot > 0 && !turns)) return SPAROA_ERR_INVALID_ARG;
+  if (!(base > 1.0) || !std::isfinite(base) || scaling < 0 || scaling > 3) return SPAROA_ERR_INVALID_ARG;
+  if (scaling != SPAROA_ROPE_SCALE_NONE && (!(factor >= 1.0) || !std::isfinite(factor))) return SPAROA_ERR_INVALID_ARG;
+  if (scaling == SPAROA_ROPE_SCALE_PARTS &&
+      (!(context > 0.0) || !std::isfinite(context) || !(high > low) || !std::isfinite(high) || !std::isfinite(low)))
+    return SPAROA_ERR_INVALID_ARG;
+  const double two_pi = 6.283185307179586476925286766559;
+  if (scaling == SPAROA_ROPE_SCALE_BASE) base *= std::pow(factor, rot / (rot - 2.0));
+  for (int i = 0; i < rot / 2; ++i) {
+    double f = std::pow(base, -2.0 * i / rot);
+    if (scaling == SPAROA_ROPE_SCALE_LINEAR) f /= factor;
+    if (scaling == SPAROA_ROPE_SCALE_PARTS) {
+      const double made = context * f / two_pi;
+      double keep = (made - low) / (high - low);
+      keep = keep < 0.0 ? 0.0 : (keep > 1.0 ? 1.0 : keep);
+      f *= keep + (1.0 - keep) / factor;
+    }
+    turns[i] = (uint64_t)std::ldexp(f / two_pi, 64);  // (f <= 1: below 2^62)
+  }
+  return SPAROA_OK;
+}
+
+sparoa_status sparoa_rope_append(sparoa_ctx* ctx, const void* qkv, int64_t ld_qkv, int64_t T, int32_t heads,
+                                 const sparoa_rope* rope, const int32_t* positions, const sparoa_kv_cache* cache,
+                                 const sparoa_paged_batch* batch, void* q_out, int64_t ld_q) {
+  if (!ctx) return SPAROA_ERR_INVALID_ARG;
+  SP_TRY(check_paged(ctx, cache, batch, T, heads, "rope_append"));
+  const int64_t D = cache->head_dim;
+  if (!rope || rope->rot < 0 || rope->rot % 16 || rope->rot > D || rope->layout < 0 || rope->layout > 1 ||
+      (rope->rot > 0 && !rope->turns) || !std::isfinite(rope->scale))
+    return fail(ctx, SPAROA_ERR_INVALID_ARG, "rope_append: bad rope");
+  if (ld_qkv < (heads + 2ll * cache->kv_heads) * D || ld_q < heads * D || ld_qkv % 8 || ld_q % 8)
+    return fail(ctx, SPAROA_ERR_INVALID_ARG, "rope_append: bad row length");
+  if (T > 0 && (!qkv || !q_out || !aligned16(qkv) || !aligned16(q_out)))
+    return fail(ctx, SPAROA_ERR_INVALID_ARG, "rope_append: NULL or misaligned tensor");
+  DeviceGuard g(ctx->device, ctx->overlap);
+  RopeArgs a;
+  a.qkv = static_cast<const __nv_bfloat16*>(qkv);
+  a.ld_qkv = ld_qkv;
+  a.T = T;
+  a.heads = heads;
+  a.kv_heads = cache->kv_heads;
+  a.D = (int)D;
+  a.rot = rope->rot;
+  a.interleaved = rope->layout == SPAROA_ROPE_INTERLEAVED;
+  a.turns = rope->turns;
+  a.scale = rope->scale;
+  a.positions = positions;
+  a.q_start = batch->q_start;
+  a.kv_len = batch->kv_len;
+  a.table = batch->table;
+  a.table_stride = batch->table_stride;
+  a.batch = batch->batch;
+  a.max_pages = batch->max_pages;
+  a.page_log2 = log2_of(cache->page_size);
+  a.pages = cache->pages;
+  a.k = static_cast<__nv_bfloat16*>(cache->k);
+  a.v = static_cast<__nv_bfloat16*>(cache->v);
+  a.q_out = static_cast<__nv_bfloat16*>(q_out);
+  a.ld_q = ld_q;
+  a.err = ctx->d_err();
+  SP_CUDA(launch_rope_append(a, ctx->stream));
+  return SPAROA_OK;
+}
+
+sparoa_status sparoa_paged_attention(sparoa_ctx* ctx, const void* q, int64_t ld_q, int64_t T, int32_t heads, float scale,
+                                     int32_t causal, int32_t window, const sparoa_kv_cache* cache,
+                                     const sparoa_paged_batch* batch, void* y, float* lse,
+                                     const sparoa_occupancy* y_occ) {
+  if (!ctx) return SPAROA_ERR_INVALID_ARG;
+  SP_TRY(check_paged(ctx, cache, batch, T, heads, "paged_attention"));
+  const int64_t D = cache->head_dim;
+  if (!(scale > 0.f) || !std::isfinite(scale)) return fail(ctx, SPAROA_ERR_INVALID_ARG, "paged_attention: scale");
+  if (window < 0) return fail(ctx, SPAROA_ERR_INVALID_ARG, "paged_attention: window");
+  if (ld_q < heads * D || ld_q % 8) return fail(ctx, SPAROA_ERR_INVALID_ARG, "paged_attention: bad row length");
+  if (T > 0 && (!q || !y || !aligned16(q) || !aligned16(y)))
+    return fail(ctx, SPAROA_ERR_INVALID_ARG, "paged_attention: NULL or misaligned tensor");
+  SP_TRY(check_occ(ctx, y_occ, T, heads * D, "paged_attention y_occ"));
+  DeviceGuard g(ctx->device, ctx->overlap);
+  if (T > 0) {
+    int slot = 0;
+    SP_TRY(paged_slot(ctx, &slot));
+    PagedArgs a;
+    a.q = static_cast<const __nv_bfloat16*>(q);
+    a.ld_q = ld_q;
+    a.T = T;
+    a.heads = heads;
+    a.kv_heads = cache->kv_heads;
+    a.group = heads / cache->kv_heads;
+    a.D = (int)D;
+    a.scale = scale;
+    a.causal = causal != 0;
+    a.window = window;
+    a.k = static_cast<const __nv_bfloat16*>(cache->k);
+    a.v = static_cast<const __nv_bfloat16*>(cache->v);
+    a.pages = cache->pages;
+    a.page_log2 = log2_of(cache->page_size);
+    a.q_start = batch->q_start;
+    a.kv_len = batch->kv_len;
+    a.table = batch->table;
+    a.table_stride = batch->table_stride;
+    a.batch = batch->batch;
+    a.max_pages = batch->max_pages;
+    a.max_q = batch->max_q;
+    a.y = static_cast<__nv_bfloat16*>(y);
+    a.lse = lse;
+    a.ws = static_cast<float*>(ctx->paged[slot].ws.p);
+    a.cnt = ctx->d_paged_cnt(slot);
+    a.err = ctx->d_err();
+    a.wait_limit = ctx->wait_limit;
+    SP_CUDA(launch_paged_attention(a, ctx->stream));
+  }
+  if (y_occ) SP_TRY(run_stats(ctx, y, T, heads * D, *y_occ));
   return SPAROA_OK;
 }
 

@@ -1,0 +1,206 @@
+// Work plan of attention over a paged cache, shared by its kernels.
+//
+// An item is one tile of RT query rows of one sequence and key head (row r of a
+// sequence: token r / group, query head key_head * group + r % group).  Its keys are
+// walked in units of 128.  The units of all items, in the order (sequence, key head,
+// tile), form one line that the CTAs cut into equal shares: every CTA loads as many
+// keys as any other, however ragged the batch, and at most its first and last item
+// are shared with other CTAs.  Lengths are on the device, so every CTA makes the plan
+// itself (a load per sequence and a scan; about a microsecond).
+#pragma once
+
+#include "sparoa_kernels.h"
+
+namespace sparoa {
+
+constexpr int kUnitKeys = 128;
+
+// The batch in shared memory: first row, new tokens, cached tokens and units per key
+// head of each sequence.
+struct PagedPlan {
+  int q0[kPagedMaxBatch], n[kPagedMaxBatch], len[kPagedMaxBatch];
+  unsigned long long units[kPagedMaxBatch];
+  unsigned long long total;
+};
+
+// Keys [lo, hi) that some row of tile t may see; hi <= lo: none.  units >= 1, so that
+// rows without keys are still written.
+struct TileKeys {
+  int lo, hi, blk0, units;
+};
+
+template <int RT>
+__device__ __forceinline__ int tiles_of(int n, int group) {
+  return (int)(((long long)n * group + RT - 1) / RT);
+}
+
+template <int RT>
+__device__ __forceinline__ TileKeys tile_keys(const PagedArgs& a, int n, int len, int t) {
+  TileKeys k;
+  const int rows = n * a.group;
+  const int first = t * RT / a.group;
+  const int last = (min(rows, (t + 1) * RT) - 1) / a.group;
+  k.hi = a.causal ? max(0, min(len, len - n + last + 1)) : len;
+  k.lo = a.window > 0 ? max(0, len - n + first - a.window + 1) : 0;
+  k.blk0 = k.lo / kUnitKeys;
+  k.units = max(1, (k.hi + kUnitKeys - 1) / kUnitKeys - k.blk0);
+  return k;
+}
+
+// Fills the plan (all threads of the CTA; ends with a block barrier).  What the lists
+// say is brought into the tensors' bounds; where it is not there already, the error
+// bit is set.
+template <int RT>
+__device__ __forceinline__ void make_plan(const PagedArgs& a, PagedPlan& p) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+  if (threadIdx.x == 0) p.total = 0ull;
+  __syncthreads();
+  bool many = false;
+  const long long room = (long long)a.max_pages << a.page_log2;
+  unsigned long long sum = 0ull;
+  for (int b = threadIdx.x; b < a.batch; b += blockDim.x) {
+    long long q0 = a.q_start[b], n = (long long)a.q_start[b + 1] - q0, len = a.kv_len[b];
+    const bool bad = q0 < 0 || n < 0 || q0 + n > a.T || n * a.group > 0x3FFFFFFF || len < 0 || len > room;
+    if (bad) {
+      atomicOr(a.err, kErrBadIndex);
+      n = q0 < 0 || n < 0 || q0 + n > a.T || n * a.group > 0x3FFFFFFF ? 0 : n;
+      len = len < 0 ? 0 : min(len, room);
+    }
+    const int tiles = tiles_of<RT>((int)n, a.group);
+    p.q0[b] = (int)q0;
+    p.n[b] = (int)n;
+    p.len[b] = (int)len;
+    p.units[b] = tiles == 1 ? (unsigned long long)tile_keys<RT>(a, (int)n, (int)len, 0).units : 0ull;
+    many |= tiles > 1;
+    sum += p.units[b] * a.kv_heads;
+  }
+  if (__syncthreads_or(many)) {
+    for (int b = warp; b < a.batch; b += warps) {
+      const int n = p.n[b], len = p.len[b], tiles = tiles_of<RT>(n, a.group);
+      if (tiles <= 1) continue;
+      unsigned long long u = 0ull;
+      for (int t = lane; t < tiles; t += 32) u += (unsigned long long)tile_keys<RT>(a, n, len, t).units;
+#pragma unroll
+      for (int d = 16; d > 0; d >>= 1) u += __shfl_xor_sync(0xffffffffu, u, d);
+      if (lane == 0) {
+        p.units[b] = u;
+        sum += u * a.kv_heads;
+      }
+    }
+  }
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+  if (lane == 0 && sum) atomicAdd(&p.total, sum);
+  __syncthreads();
+}
+
+// One place in the line of units, the same in all lanes of a warp.
+template <int RT>
+struct PagedCursor {
+  int b, h, t, tiles, blk;   // blk: unit within the item
+  int q0, n, len;
+  TileKeys k;
+
+  __device__ __forceinline__ void load_seq(const PagedArgs& a, const PagedPlan& p) {
+    q0 = p.q0[b];
+    n = p.n[b];
+    len = p.len[b];
+    tiles = tiles_of<RT>(n, a.group);
+  }
+  // to unit u < p.total (a converged warp)
+  __device__ __forceinline__ void seek(const PagedArgs& a, const PagedPlan& p, unsigned long long u) {
+    const int lane = threadIdx.x & 31;
+    unsigned long long before = 0ull;  // units of the sequences before b0
+    int b0 = 0;
+    for (;; b0 += 32) {
+      const unsigned long long mine = b0 + lane < a.batch ? p.units[b0 + lane] * a.kv_heads : 0ull;
+      unsigned long long incl = mine;
+#pragma unroll
+      for (int d = 1; d < 32; d <<= 1) {
+        const unsigned long long o = __shfl_up_sync(0xffffffffu, incl, d);
+        if (lane >= d) incl += o;
+      }
+      const unsigned hit = __ballot_sync(0xffffffffu, before + incl > u);
+      if (hit || b0 + 32 >= a.batch) {
+        const int l = hit ? __ffs(hit) - 1 : 31;
+        b = b0 + l;
+        before += __shfl_sync(0xffffffffu, incl - mine, l);
+        break;
+      }
+      before += __shfl_sync(0xffffffffu, incl, 31);
+    }
+    load_seq(a, p);
+    const unsigned long long per = p.units[b];
+    unsigned long long rem = u - before;
+    h = (int)(rem / per);
+    rem -= h * per;
+    for (int t0 = 0;; t0 += 32) {
+      const unsigned mine = t0 + lane < tiles ? (unsigned)tile_keys<RT>(a, n, len, t0 + lane).units : 0u;
+      unsigned incl = mine;
+#pragma unroll
+      for (int d = 1; d < 32; d <<= 1) {
+        const unsigned o = __shfl_up_sync(0xffffffffu, incl, d);
+        if (lane >= d) incl += o;
+      }
+      const unsigned hit = __ballot_sync(0xffffffffu, incl > rem);
+      if (hit || t0 + 32 >= tiles) {
+        const int l = hit ? __ffs(hit) - 1 : 31;
+        t = t0 + l;
+        rem -= __shfl_sync(0xffffffffu, incl - mine, l);
+        break;
+      }
+      rem -= __shfl_sync(0xffffffffu, incl, 31);
+    }
+    blk = (int)rem;
+    k = tile_keys<RT>(a, n, len, t);
+  }
+  // to the next unit (not past the last)
+  __device__ __forceinline__ void next(const PagedArgs& a, const PagedPlan& p) {
+    if (++blk < k.units) return;
+    blk = 0;
+    if (++t == tiles) {
+      t = 0;
+      if (++h == a.kv_heads) {
+        h = 0;
+        do ++b; while (b < a.batch && p.units[b] == 0ull);
+        if (b >= a.batch) {  // past the end: stay on a valid place
+          b = a.batch - 1;
+          return;
+        }
+        load_seq(a, p);
+      }
+    }
+    k = tile_keys<RT>(a, n, len, t);
+  }
+};
+
+// The line's cut: CTA c of `ctas` has units [c total / ctas, (c + 1) total / ctas).
+__device__ __forceinline__ unsigned long long cut_start(unsigned long long total, unsigned ctas, unsigned c) {
+  return total * c / ctas;
+}
+// the CTA that has unit u
+__device__ __forceinline__ unsigned cut_owner(unsigned long long total, unsigned ctas, unsigned long long u) {
+  return (unsigned)(((u + 1) * ctas - 1) / total);
+}
+
+// Page of key `key` of sequence b, brought into the pool's bounds.
+__device__ __forceinline__ int page_of(const PagedArgs& a, int b, int key) {
+  return a.table[b * a.table_stride + (key >> a.page_log2)];
+}
+__device__ __forceinline__ int page_checked(const PagedArgs& a, int page) {
+  if (page >= 0 && page < a.pages) return page;
+  atomicOr(a.err, kErrBadIndex);
+  return 0;
+}
+// Row of the pool [pages * kv_heads * page_size][D] that holds key `key` of key head h.
+__device__ __forceinline__ int pool_row(const PagedArgs& a, int page, int h, int key) {
+  return (int)(((long long)page * a.kv_heads + h) << a.page_log2) + (key & ((1 << a.page_log2) - 1));
+}
+
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+}  // namespace sparoa

@@ -25,6 +25,7 @@ enum ErrBits : uint32_t {
   kErrTimeoutFull = 1u,
   kErrTimeoutEmpty = 2u,
   kErrTimeoutAcc = 4u,
+  kErrBadIndex = 8u,  // an index list on the device points outside its tensor
 };
 
 // Occupancy outputs of a [R, C] bf16 tensor (mirrors sparoa_occupancy).

@@ -218,6 +218,77 @@ cudaError_t launch_select(const __nv_bfloat16* x, int N, int T, int D, int index
                           cudaStream_t s);
 
 // ----------------------------------------------------------------------------
+// Decoder operators (k_decoder.cu, k_paged.cu)
+// ----------------------------------------------------------------------------
+struct NormDev {
+  int kind = 0;  // 0 none, 1 RMS, 2 layer
+  float eps = 0.f;
+  const float* weight = nullptr;  // [C] or null
+  const float* bias = nullptr;
+};
+struct AddNormArgs {
+  const void* x = nullptr;            // [R, C] or null, bf16 or fp32
+  const __nv_bfloat16* h = nullptr;   // [R, C] or null
+  int64_t R = 0;
+  int C = 0;                          // % 8 == 0, <= 16384
+  int res_f32 = 0;
+  NormDev post, pre;
+  const float* gate = nullptr;        // [R / per][C], or [C] with per = 0
+  int64_t per = 0;
+  float scale = 1.f;
+  void* r = nullptr;                  // nullable, the type of x
+  __nv_bfloat16* y = nullptr;         // nullable
+};
+cudaError_t launch_add_norm(const AddNormArgs& a, cudaStream_t s);
+
+constexpr int kRopeThreads = 128;
+struct RopeArgs {
+  const __nv_bfloat16* qkv = nullptr;
+  int64_t ld_qkv = 0, T = 0;
+  int heads = 0, kv_heads = 0, D = 0;
+  int rot = 0, interleaved = 0;
+  const uint64_t* turns = nullptr;
+  float scale = 1.f;
+  const int32_t* positions = nullptr;
+  const int32_t* q_start = nullptr;
+  const int32_t* kv_len = nullptr;
+  const int32_t* table = nullptr;
+  int64_t table_stride = 0;
+  int batch = 0, max_pages = 0, page_log2 = 0;
+  int64_t pages = 0;
+  __nv_bfloat16 *k = nullptr, *v = nullptr, *q_out = nullptr;
+  int64_t ld_q = 0;
+  uint32_t* err = nullptr;
+};
+cudaError_t launch_rope_append(const RopeArgs& a, cudaStream_t s);
+
+struct PagedArgs {
+  const __nv_bfloat16* q = nullptr;
+  int64_t ld_q = 0, T = 0;
+  int heads = 0, kv_heads = 0, group = 0, D = 0;
+  float scale = 1.f;
+  int causal = 0, window = 0;
+  const __nv_bfloat16 *k = nullptr, *v = nullptr;  // pools [pages][kv_heads][page][D]
+  int64_t pages = 0;
+  int page_log2 = 0;
+  const int32_t* q_start = nullptr;
+  const int32_t* kv_len = nullptr;
+  const int32_t* table = nullptr;
+  int64_t table_stride = 0;
+  int batch = 0, max_pages = 0, max_q = 0;
+  __nv_bfloat16* y = nullptr;  // [T][heads * D]
+  float* lse = nullptr;        // [T][heads] or null
+  float* ws = nullptr;         // partial results: paged_ws_bytes() bytes
+  unsigned* cnt = nullptr;     // kPagedCounters arrival counters, zero between calls
+  uint32_t* err = nullptr;
+  long long wait_limit = 0;
+};
+constexpr int kPagedMaxBatch = 1024;
+constexpr int kPagedCounters = 512;
+size_t paged_ws_bytes();
+cudaError_t launch_paged_attention(const PagedArgs& a, cudaStream_t s);
+
+// ----------------------------------------------------------------------------
 // Memory-bound kernels (128-row x 64-channel tiles, occupancy fused)
 // ----------------------------------------------------------------------------
 // Eq. 1 statistics and bitmaps of x viewed as [R, C].  The row bitmaps are

@@ -26,6 +26,9 @@ PATH_NONE, PATH_DENSE, PATH_SKIP, PATH_DEPTHWISE = 0, 1, 2, 3
 ACT_NONE, ACT_RELU, ACT_RELU6, ACT_GELU = 0, 1, 2, 3
 OP_CONV2D, OP_FC, OP_MAXPOOL, OP_AVGPOOL, OP_BN_ACT = 1, 2, 3, 4, 5
 OP_LAYERNORM, OP_ATTENTION, OP_TOKENS, OP_SELECT = 6, 7, 8, 9
+NORM_NONE, NORM_RMS, NORM_LAYER = 0, 1, 2
+ROPE_HALF, ROPE_INTERLEAVED = 0, 1
+ROPE_SCALE_NONE, ROPE_SCALE_LINEAR, ROPE_SCALE_BASE, ROPE_SCALE_PARTS = 0, 1, 2, 3
 
 _P = ctypes.c_void_p
 _I64 = ctypes.c_int64
@@ -64,6 +67,24 @@ class Op(ctypes.Structure):
                 ("act", _I32), ("reserved", _I32), ("weight", _P), ("weight_kn", _P), ("bias", _P),
                 ("bn", _P), ("bn_eps", ctypes.c_float), ("reserved2", ctypes.c_float),
                 ("thr", Thresholds)]
+
+
+class NormSpec(ctypes.Structure):
+    _fields_ = [("kind", _I32), ("eps", ctypes.c_float), ("weight", _P), ("bias", _P)]
+
+
+class KvCacheDesc(ctypes.Structure):
+    _fields_ = [("k", _P), ("v", _P), ("pages", _I64), ("page_size", _I32), ("kv_heads", _I32),
+                ("head_dim", _I32), ("reserved", _I32)]
+
+
+class PagedBatchDesc(ctypes.Structure):
+    _fields_ = [("q_start", _P), ("kv_len", _P), ("table", _P), ("table_stride", _I64), ("batch", _I32),
+                ("max_pages", _I32), ("max_q", _I32), ("reserved", _I32)]
+
+
+class RopeDesc(ctypes.Structure):
+    _fields_ = [("rot", _I32), ("layout", _I32), ("turns", _P), ("scale", ctypes.c_float), ("reserved", _I32)]
 
 
 class Record(ctypes.Structure):
@@ -109,6 +130,14 @@ _sig("sparoa_avgpool_global", [_P, _P, _I64, _I64, _I64, _I64, _P, ctypes.POINTE
 _sig("sparoa_bn_act", [_P, _P, _I64, _I64, ctypes.POINTER(Epilogue), _P, ctypes.POINTER(Occupancy)])
 _sig("sparoa_layernorm", [_P, _P, _I64, _I64, _P, ctypes.c_float, _P, ctypes.POINTER(Occupancy)])
 _sig("sparoa_attention", [_P, _P, _I64, _I64, _I32, _I32, _P, ctypes.POINTER(Occupancy)])
+_sig("sparoa_add_norm", [_P, _P, _P, _I64, _I64, _I32, ctypes.POINTER(NormSpec), _P, _I64, ctypes.c_float,
+                         ctypes.POINTER(NormSpec), _P, _P, ctypes.POINTER(Occupancy)])
+_sig("sparoa_rope_turns", [_I32, ctypes.c_double, _I32, ctypes.c_double, ctypes.c_double, ctypes.c_double,
+                           ctypes.c_double, _P])
+_sig("sparoa_rope_append", [_P, _P, _I64, _I64, _I32, ctypes.POINTER(RopeDesc), _P, ctypes.POINTER(KvCacheDesc),
+                            ctypes.POINTER(PagedBatchDesc), _P, _I64])
+_sig("sparoa_paged_attention", [_P, _P, _I64, _I64, _I32, ctypes.c_float, _I32, _I32, ctypes.POINTER(KvCacheDesc),
+                                ctypes.POINTER(PagedBatchDesc), _P, _P, ctypes.POINTER(Occupancy)])
 _sig("sparoa_run_graph", [_P, ctypes.POINTER(Op), _I32, _P, _I64, _I64, _I64, _I64, _P,
                           ctypes.c_uint64, ctypes.POINTER(Record)])
 _sig("sparoa_gemm_noalloc", [_P, _P, _I64, _I64, _P, _P, _I64, ctypes.POINTER(Epilogue),
@@ -121,6 +150,7 @@ EXPORTED = ["sparoa_create", "sparoa_destroy", "sparoa_set_stream", "sparoa_set_
             "sparoa_occupancy_init", "sparoa_op_stats", "sparoa_gemm", "sparoa_conv2d",
             "sparoa_maxpool2d", "sparoa_avgpool_global", "sparoa_bn_act", "sparoa_run_graph",
             "sparoa_graph_workspace", "sparoa_gemm_split", "sparoa_layernorm", "sparoa_attention",
+            "sparoa_add_norm", "sparoa_rope_turns", "sparoa_rope_append", "sparoa_paged_attention",
             "sparoa_gemm_noalloc"]
 
 
@@ -143,6 +173,7 @@ def _ptr(t):
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
     (lambda device: torch.cuda.current_stream(device).cuda_stream)
 _set_stream = _lib.sparoa_set_stream
+_byref = ctypes.byref
 
 
 def _rows(shape):
@@ -211,9 +242,6 @@ class Context:
         """Error-path tests: 1 = withhold the first accumulator signal
         (timeout), 2 = fail the next workspace allocation, 0 = off."""
         self._check(_lib.sparoa_set_fault(self.h, int(code)))
-
-
-_byref = ctypes.byref
 
 
 class OccupancyBuffer:
@@ -350,6 +378,175 @@ def sparoa_attention(ctx: Context, qkv, y, heads, y_occ=None):
     ctx._bind()
     ctx._check(_lib.sparoa_attention(ctx.h, _ptr(qkv), N, T, int(heads), D // int(heads), _ptr(y),
                                      _occ(y_occ)))
+
+
+# ---------------------------------------------------------------------------
+# decoder operators: residual norm, rotary positions into a paged cache, attention over it
+# ---------------------------------------------------------------------------
+def _want(cond, what):
+    if not cond:
+        raise SparoaError(ERR_INVALID_ARG, what)
+
+
+def _want_rows(t, dtypes, what):
+    """t is a CUDA tensor of one of `dtypes` with contiguous storage."""
+    _want(t.is_cuda and t.dtype in dtypes and t.is_contiguous(), f"{what}: contiguous CUDA tensor of {dtypes} wanted")
+
+
+_BF16S = (torch.bfloat16,)
+_FP32S = (torch.float32,)
+_I32S = (torch.int32,)
+
+
+class Norm:
+    """A norm of sparoa_add_norm; keeps its parameters alive."""
+
+    def __init__(self, kind, weight=None, bias=None, eps=1e-6):
+        for t in (weight, bias):
+            if t is not None:
+                _want_rows(t, _FP32S, "norm parameter")
+        self.weight, self.bias = weight, bias
+        self.size = {t.numel() for t in (weight, bias) if t is not None}
+        self.desc = NormSpec({"none": NORM_NONE, "rms": NORM_RMS, "layer": NORM_LAYER}[kind], float(eps),
+                             _ptr(weight), _ptr(bias))
+        self.ref = _byref(self.desc)
+
+
+def norm(kind, weight=None, bias=None, eps=1e-6) -> Norm:
+    """kind "none", "rms" or "layer"; weight and bias fp32 [C] or None."""
+    return Norm(kind, weight, bias, eps)
+
+
+def sparoa_add_norm(ctx: Context, x, h, r=None, y=None, post: Norm | None = None, gate=None, rows_per_gate=0,
+                    scale=1.0, pre: Norm | None = None, y_occ=None):
+    """r = x + scale gate N_post(h), y = N_pre(r) over the last dimension; x and r bf16 or
+    fp32, h and y bf16; any of x, h (not both) and r, y may be None."""
+    lead = x if x is not None else h
+    _want(lead is not None, "add_norm: x or h")
+    C = lead.shape[-1]
+    R = _rows(lead.shape)
+    stream = x if x is not None else r
+    res = F32 if stream is not None and stream.dtype == torch.float32 else BF16
+    for t, dts in ((x, (torch.float32,) if res else _BF16S), (r, (torch.float32,) if res else _BF16S), (h, _BF16S),
+                   (y, _BF16S)):
+        if t is not None:
+            _want_rows(t, dts, "add_norm")
+            _want(t.numel() == R * C, "add_norm: tensors of different sizes")
+    for n in (post, pre):
+        _want(n is None or n.size <= {C}, "add_norm: norm parameters of another length")
+    rows_per_gate = int(rows_per_gate)
+    if gate is not None:
+        _want_rows(gate, _FP32S, "add_norm gate")
+        _want(rows_per_gate >= 0 and gate.numel() >= (C if not rows_per_gate else -(-R // rows_per_gate) * C),
+              "add_norm: gate rows")
+    ctx._bind()
+    ctx._check(_lib.sparoa_add_norm(ctx.h, _ptr(x), _ptr(h), R, C, res, None if post is None else post.ref, _ptr(gate),
+                                    rows_per_gate, float(scale), None if pre is None else pre.ref, _ptr(r), _ptr(y),
+                                    _occ(y_occ)))
+
+
+class KVCache:
+    """Key and value pools [pages, kv_heads, page_size, head_dim] (bf16, contiguous)."""
+
+    def __init__(self, k, v):
+        _want(k.dim() == 4 and k.shape == v.shape, "KVCache: pools [pages, kv_heads, page_size, head_dim]")
+        for t in (k, v):
+            _want_rows(t, _BF16S, "KVCache")
+        self.k, self.v = k, v
+        self.pages, self.kv_heads, self.page_size, self.head_dim = k.shape
+        self.desc = KvCacheDesc(_ptr(k), _ptr(v), self.pages, self.page_size, self.kv_heads, self.head_dim, 0)
+        self.ref = _byref(self.desc)
+
+    @staticmethod
+    def empty(pages, kv_heads, page_size, head_dim, device="cuda"):
+        k, v = (torch.empty(pages, kv_heads, page_size, head_dim, dtype=torch.bfloat16, device=device) for _ in range(2))
+        return KVCache(k, v)
+
+
+class PagedBatch:
+    """New tokens of a batch of sequences: q_start int32 [batch + 1], kv_len int32 [batch],
+    table int32 [batch, max_pages] (rows may be strided), max_q the largest number of new tokens."""
+
+    def __init__(self, q_start, kv_len, table, max_q):
+        for t in (q_start, kv_len):
+            _want_rows(t, _I32S, "PagedBatch")
+        _want(table.is_cuda and table.dtype == torch.int32 and table.dim() == 2, "PagedBatch: table int32 [batch, pages]")
+        B = kv_len.numel()
+        _want(table.shape[0] == B and q_start.numel() == B + 1, "PagedBatch: lists of different batches")
+        _want(table.shape[1] <= 1 or table.stride(1) == 1, "PagedBatch: strided table entries")
+        self.q_start, self.kv_len, self.table, self.max_q = q_start, kv_len, table, int(max_q)
+        self.desc = PagedBatchDesc(_ptr(q_start), _ptr(kv_len), _ptr(table),
+                                   table.stride(0) if B > 1 else max(table.stride(0), table.shape[1]),
+                                   B, table.shape[1], self.max_q, 0)
+        self.ref = _byref(self.desc)
+
+
+def sparoa_rope_turns(rot, base=10000.0, scaling="none", factor=1.0, context=0.0, low=1.0, high=32.0) -> np.ndarray:
+    """Turns per position of each rotated pair, in units of 2^-64 (uint64 [rot / 2], host)."""
+    kinds = {"none": ROPE_SCALE_NONE, "linear": ROPE_SCALE_LINEAR, "base": ROPE_SCALE_BASE, "parts": ROPE_SCALE_PARTS}
+    out = np.zeros(max(int(rot), 0) // 2, dtype=np.uint64)
+    st = _lib.sparoa_rope_turns(int(rot), float(base), kinds[scaling], float(factor), float(context), float(low),
+                                float(high), out.ctypes.data if out.size else None)
+    if st != OK:
+        raise SparoaError(st, "sparoa_rope_turns")
+    return out
+
+
+class Rope:
+    """Rotary positions: `rot` leading values of a head, layout "half" or "interleaved",
+    frequencies as sparoa_rope_turns, cos and sin times `scale`."""
+
+    def __init__(self, rot, layout="half", base=10000.0, scaling="none", factor=1.0, context=0.0, low=1.0, high=32.0,
+                 scale=1.0, device="cuda"):
+        turns = sparoa_rope_turns(rot, base, scaling, factor, context, low, high)
+        self.turns = torch.from_numpy(turns.view(np.int64)).to(device)
+        self.desc = RopeDesc(int(rot), {"half": ROPE_HALF, "interleaved": ROPE_INTERLEAVED}[layout],
+                             _ptr(self.turns) if rot else None, float(scale), 0)
+        self.ref = _byref(self.desc)
+
+
+def _token_rows(t, T, width, what):
+    """Row length in elements of t [T, ...] whose rows hold `width` adjacent bf16 values."""
+    _want(t.is_cuda and t.dtype == torch.bfloat16 and t.dim() in (2, 3) and t.shape[0] == T, f"{what}: bf16 rows of {T} tokens")
+    inner = t.shape[1] if t.dim() == 2 else t.shape[1] * t.shape[2]
+    flat = t.shape[-1] <= 1 or t.stride(-1) == 1
+    flat = flat and (t.dim() == 2 or t.shape[1] <= 1 or t.stride(1) == t.shape[2])
+    _want(inner == width and flat, f"{what}: {width} adjacent values a row")
+    return t.stride(0) if T > 1 else max(t.stride(0), width)
+
+
+def sparoa_rope_append(ctx: Context, qkv, q_out, cache: KVCache, batch: PagedBatch, rope: Rope, positions=None):
+    """Rotate the new tokens' queries (to q_out [T, heads, head_dim]) and keys (to the cache, with the
+    values) from qkv [T, (heads + 2 kv_heads) head_dim]; rows may be strided."""
+    T = qkv.shape[0]
+    width = q_out.numel() // T if T else q_out.shape[-1] * (q_out.shape[1] if q_out.dim() == 3 else 1)
+    heads = width // cache.head_dim
+    ld = _token_rows(qkv, T, width + 2 * cache.kv_heads * cache.head_dim, "rope_append qkv")
+    ldq = _token_rows(q_out, T, heads * cache.head_dim, "rope_append q_out")
+    if positions is not None:
+        _want_rows(positions, _I32S, "rope_append positions")
+        _want(positions.numel() == T, "rope_append: a position per token")
+    ctx._bind()
+    ctx._check(_lib.sparoa_rope_append(ctx.h, _ptr(qkv), ld, T, heads, rope.ref, _ptr(positions), cache.ref, batch.ref,
+                                       _ptr(q_out), ldq))
+
+
+def sparoa_paged_attention(ctx: Context, q, y, cache: KVCache, batch: PagedBatch, scale=None, causal=True, window=0,
+                           lse=None, y_occ=None):
+    """y = softmax(scale q K^T) V of the new tokens over their cached sequences; q [T, heads, head_dim]
+    (rows may be strided), y the same (contiguous), lse fp32 [T, heads] or None."""
+    T, D = q.shape[0], cache.head_dim
+    heads = y.numel() // (T * D) if T else max(1, y.shape[-1] * (y.shape[1] if y.dim() == 3 else 1) // D)
+    ld = _token_rows(q, T, heads * D, "paged_attention q")
+    _want_rows(y, _BF16S, "paged_attention y")
+    _want(y.numel() == T * heads * D, "paged_attention: y")
+    if lse is not None:
+        _want_rows(lse, _FP32S, "paged_attention lse")
+        _want(lse.numel() == T * heads, "paged_attention: lse")
+    ctx._bind()
+    ctx._check(_lib.sparoa_paged_attention(ctx.h, _ptr(q), ld, T, heads, D ** -0.5 if scale is None else float(scale),
+                                           1 if causal else 0, int(window), cache.ref, batch.ref, _ptr(y), _ptr(lse),
+                                           _occ(y_occ)))
 
 
 def sparoa_gemm_noalloc(x, W, y, W_kn=None, bias=None, bn=None, eps=1e-5, act=ACT_NONE,
