@@ -512,7 +512,8 @@ sparoa_status sparoa_rope_append(sparoa_ctx *ctx, const void *qkv, int64_t ld_qk
  * append first): per query head, with key head h / (heads / kv_heads),
  *   y = softmax(scale Q K^T) V
  * in tensor cores with fp32 scores, softmax statistics and accumulation; for the
- * P V products the probabilities are two bf16 parts (16 bits) each.  The token at position p sees
+ * P V products the probabilities are rounded to bf16, or to two bf16 parts each
+ * (16 bits) for a sequence of at most 128 rows per key head (n heads / kv_heads).  The token at position p sees
  * the keys j < kv_len with j <= p (causal) and j > p - window (window > 0).  A row
  * that sees no key is zero.
  *   q     bf16 [T][ld_q >= heads head_dim], ld_q % 8 == 0, 16-byte aligned

@@ -1500,6 +1500,7 @@ sparoa_status sparoa_paged_attention(sparoa_ctx* ctx, const void* q, int64_t ld_
     a.cnt = ctx->d_paged_cnt(slot);
     a.err = ctx->d_err();
     a.wait_limit = ctx->wait_limit;
+    a.fault = ctx->fault == 1;
     SP_CUDA(launch_paged_attention(a, ctx->stream));
   }
   if (y_occ) SP_TRY(run_stats(ctx, y, T, heads * D, *y_occ));

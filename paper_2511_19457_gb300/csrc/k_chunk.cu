@@ -1,0 +1,571 @@
+// Attention of chunks of new tokens over a paged key/value cache on tcgen05.
+#include "paged.cuh"
+
+namespace sparoa {
+
+namespace {
+
+// ---------------------------------------------------------------------------
+// An item is 256 query rows: two tiles of 128, whose scores and sums live in tensor
+// memory side by side: S (128 x 128 fp32, later overwritten by the weights P in
+// bf16) and O (128 x D fp32) of each.  Ten warps: two groups of four for the softmax
+// of a tile (a thread per row), one that issues the MMAs, one that loads K and V by
+// TMA, page by page, into a ring.
+//
+// Bound by the tensor cores and, as much, by the exponentials: 256 x 128 scores of a
+// unit are 2 x 2 x 128 x 128 x D MACs (1024 cycles at D = 128) and 32768 exponentials
+// (1024 cycles at 32 a cycle).  So the two tiles alternate: while the softmax works on
+// one, the tensor cores multiply for the other.
+//   S = Q K^T     both operands in shared memory, K-major, 128-byte swizzle
+//   O += P V      P from tensor memory, V from shared memory as it lies ([key][D], the
+//                 MN-major form of the B operand)
+// An item of one tile is bound by the bytes of K and V, so there the weights are two
+// bf16 parts (the second in the columns of S that the first leaves free).
+// MMAs of one thread run in the order of their issue, so S of the next unit may be
+// issued behind the product that still reads P from the same columns, and S complete
+// means that the O before it is.
+//
+// The softmax keeps a reference m of each row instead of the exact maximum: O and the
+// sum are only rescaled where the maximum has outgrown m by more than 2^8 in weight
+// (the weights, their sum and O hold that easily), which after a row's first units is
+// rare.  The end's O / sum is the same number.
+constexpr int kRows = 256;     // rows of an item
+constexpr int kTileRows = 128;
+constexpr int kSoftWarps = 8;
+constexpr int kMmaWarp = 8, kLoadWarp = 9;
+constexpr int kThreads = 320;
+constexpr float kSlackLog2 = 8.f;
+
+template <int D>
+struct Cfg {
+  static constexpr int kHalves = D / 64;               // 64-column halves of a tile
+  static constexpr int kHalf = kTileRows * 128;         // bytes of one
+  static constexpr int kTile = kHalves * kHalf;         // a tile of Q, or the K or V of a unit
+  static constexpr int kStages = D == 128 ? 4 : 8;
+  static constexpr int kSmem = (2 + kStages) * kTile + 1024;
+  static constexpr int kSlotFloats = kRows * (D + 2);   // a partial result: sums [D / 4][256][4], maxima, sums of weights
+  static constexpr uint32_t kCols = D == 128 ? 512 : 512;  // S, S, O, O: 256 + 2 D columns, a power of two
+  static constexpr uint32_t kO = 256;                   // first column of O
+};
+
+struct JoinItem {
+  int c0, c1, late;  // CTAs that share the item; late: its first part is CTA c0's second
+  int q0, t, h, rows, valid;
+};
+
+__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t ad, uint64_t bd, uint32_t idesc, uint32_t acc) {
+  tc_mma_bf16(d, ad, bd, idesc, acc);
+}
+// A from tensor memory (a lane per row, two values a column)
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t bd, uint32_t idesc, uint32_t acc) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
+      "r"(a), "l"(bd), "r"(idesc), "r"(acc));
+}
+// MN-major operand in 128-byte swizzle: rows of K (keys) of 64 values, groups of 8 rows
+// 1024 bytes apart (stride offset), the next 64 values kHalf bytes on (leading offset).
+__device__ __forceinline__ uint64_t smem_desc_mn(uint32_t addr, uint32_t half) {
+  uint64_t d = 0;
+  d |= (uint64_t)((addr >> 4) & 0x3FFF);
+  d |= (uint64_t)(half >> 4) << 16;
+  d |= (uint64_t)(1024 >> 4) << 32;
+  d |= (uint64_t)1 << 46;
+  d |= (uint64_t)2 << 61;
+  return d;
+}
+
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0],"
+      " {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(taddr),
+      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+      "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+      : "memory");
+}
+__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0],"
+      " {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,"
+      "%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};" ::"r"(taddr),
+      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+      "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]),
+      "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]),
+      "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
+      : "memory");
+}
+
+struct Bars {
+  unsigned long long full[8], empty[8];      // ring
+  unsigned long long s[2], p[2], q[2], o[2], o_free[2];  // per tile
+  unsigned long long drain;
+};
+
+// What a share of an item is: units [blk, blk + count) of the cursor's item.
+__device__ __forceinline__ int share(const PagedCursor<kRows>& c, unsigned long long u, unsigned long long u1) {
+  const unsigned long long left = u1 - u, rest = (unsigned long long)(c.k.units - c.blk);
+  return (int)(left < rest ? left : rest);
+}
+
+template <int D>
+__global__ void __launch_bounds__(kThreads, 1)
+    paged_chunk_kernel(const __grid_constant__ CUtensorMap tk, const __grid_constant__ CUtensorMap tv,
+                       const __grid_constant__ PagedArgs a) {
+  using C = Cfg<D>;
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ PagedPlan plan;
+  __shared__ __align__(8) Bars bars;
+  __shared__ uint32_t s_tmem;
+  __shared__ int s_abort;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const uint32_t sq = (smem_u32(smem_raw) + 1023u) & ~1023u, ring = sq + 2 * C::kTile;
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < C::kStages; ++i) {
+      mbar_init(smem_u32(&bars.full[i]), 1u);
+      mbar_init(smem_u32(&bars.empty[i]), 1u);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(smem_u32(&bars.s[i]), 1u);
+      mbar_init(smem_u32(&bars.p[i]), 4u);
+      mbar_init(smem_u32(&bars.q[i]), 4u);
+      mbar_init(smem_u32(&bars.o[i]), 1u);
+      mbar_init(smem_u32(&bars.o_free[i]), 4u);
+    }
+    mbar_init(smem_u32(&bars.drain), 1u);
+    fence_mbar_init();
+    s_abort = 0;
+    prefetch_tmap(&tk);
+    prefetch_tmap(&tv);
+  }
+  if (warp == kMmaWarp) tmem_alloc(smem_u32(&s_tmem), C::kCols);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = s_tmem;
+  pdl_wait();
+  pdl_trigger();
+  make_plan<kRows>(a, plan);
+  const unsigned long long total = plan.total;
+  const unsigned ctas = (unsigned)min((unsigned long long)gridDim.x, total);
+  JoinItem* join = reinterpret_cast<JoinItem*>(a.ws + (size_t)2 * gridDim.x * C::kSlotFloats);
+  const bool works = blockIdx.x < ctas;
+  const unsigned long long u0 = works ? cut_start(total, ctas, blockIdx.x) : 0ull;
+  const unsigned long long u1 = works ? cut_start(total, ctas, blockIdx.x + 1) : 0ull;
+  const long long limit = a.wait_limit ? a.wait_limit : kWaitLimitCycles;
+  PagedCursor<kRows> c;
+  if (works) {
+    c.seek(a, plan, u0);
+    if (threadIdx.x == 0) {
+      // an item cut at this CTA's start is joined later; the first of its cuts speaks for it
+      const unsigned long long i0 = u0 - c.blk;
+      JoinItem j;
+      j.c0 = (int)cut_owner(total, ctas, i0);
+      j.c1 = (int)cut_owner(total, ctas, i0 + c.k.units - 1);
+      j.late = i0 > cut_start(total, ctas, j.c0);
+      j.q0 = c.q0;
+      j.t = c.t;
+      j.h = c.h;
+      j.rows = min(kRows, c.n * a.group - c.t * kRows);
+      j.valid = c.blk > 0 && j.c0 + 1 == (int)blockIdx.x;
+      join[blockIdx.x] = j;
+    }
+  } else if (threadIdx.x == 0) {
+    join[blockIdx.x].valid = 0;
+  }
+  auto wait = [&](const unsigned long long& bar, unsigned parity, uint32_t bit) {
+    return mbar_wait_warp(smem_u32(&bar), parity, a.err, &s_abort, bit, limit);
+  };
+  auto next_item = [&](PagedCursor<kRows>& k, unsigned long long& u) {
+    u += share(k, u, u1);
+    if (u < u1) {
+      k.blk = k.k.units - 1;
+      k.next(a, plan);
+    }
+  };
+
+  if (warp == kLoadWarp && works) {
+    // ---- K and V of every unit, in the order of their use: K0 V0 K1 V1 ...
+    const int pages = kUnitKeys >> a.page_log2;        // of a whole unit
+    const int pg = lane / C::kHalves, half = lane % C::kHalves;
+    const uint32_t box = 128u << a.page_log2;          // bytes: page_size rows of 128
+    unsigned n = 0;                                    // stages filled
+    auto entry = [&](const PagedCursor<kRows>& k) {
+      const int key = (k.k.blk0 + k.blk) * kUnitKeys + (pg << a.page_log2);
+      return pg < pages && key < k.k.hi ? page_of(a, k.b, key) : -1;
+    };
+    int page = entry(c);
+    bool ok = true;
+    for (unsigned long long u = u0; u < u1 && ok; ++u) {
+      const int key0 = (c.k.blk0 + c.blk) * kUnitKeys;
+      const int live = max(0, min(c.k.hi, key0 + kUnitKeys) - key0);
+      const int need = (live + (1 << a.page_log2) - 1) >> a.page_log2;
+      const bool mine = pg < need;
+      const int row = mine ? pool_row(a, page_checked(a, page), c.h, 0) : 0;
+      if (u + 1 < u1) {
+        c.next(a, plan);
+        page = entry(c);  // on its way while this unit waits for room
+      }
+#pragma unroll
+      for (int kv = 0; kv < 2; ++kv) {
+        const unsigned st = n % C::kStages;
+        ok = wait(bars.empty[st], ((n / C::kStages) & 1u) ^ 1u, kErrTimeoutEmpty);
+        if (!ok) break;
+        const uint32_t bar = smem_u32(&bars.full[st]);
+        if (lane == 0) mbar_arrive_expect_tx(bar, (uint32_t)(need * C::kHalves) * box);
+        __syncwarp();
+        if (mine)
+          tma_load_2d(ring + st * C::kTile + half * C::kHalf + pg * box, kv ? &tv : &tk, bar, half * 64, row);
+        ++n;
+      }
+    }
+    // after a timeout: wait for the copies in flight into memory that is given back
+    if (*(volatile int*)&s_abort)
+      for (unsigned i = n > (unsigned)C::kStages ? n - C::kStages : 0u; i < n; ++i)
+        mbar_drain(smem_u32(&bars.full[i % C::kStages]), (i / C::kStages) & 1u, limit);
+  } else if (warp == kMmaWarp && works) {
+    // ---- the MMAs
+    const bool leader = elect_one();
+    constexpr uint32_t id_s = idesc_bf16_f32(kTileRows, kUnitKeys);
+    constexpr uint32_t id_o = idesc_bf16_f32(kTileRows, D) | (1u << 16);  // B is MN-major
+    unsigned n = 0, sp[2] = {0, 0}, items[2] = {0, 0};
+    bool ok = true;
+    auto qk = [&](int tile, unsigned st) {
+      if (leader) {
+        const uint32_t qa = sq + tile * C::kTile, ka = ring + st * C::kTile;
+#pragma unroll
+        for (int kk = 0; kk < D / 16; ++kk) {
+          const uint32_t at = (kk >> 2) * C::kHalf + (kk & 3) * 32;
+          mma_ss(tmem + tile * 128, smem_desc_kmajor<64>(qa + at), smem_desc_kmajor<64>(ka + at), id_s, kk > 0);
+        }
+        if (!a.fault) tc_commit(smem_u32(&bars.s[tile]));
+      }
+      __syncwarp();
+    };
+    auto pv = [&](int tile, unsigned st, int steps, bool first, bool last, bool fine) {
+      if (leader) {
+        const uint32_t va = ring + st * C::kTile;
+        for (int kk = 0; kk < steps; ++kk)
+          mma_ts(tmem + C::kO + tile * D, tmem + tile * 128 + kk * 8, smem_desc_mn(va + kk * 2048, C::kHalf), id_o,
+                 !(first && kk == 0));
+        if (fine)
+          for (int kk = 0; kk < steps; ++kk)
+            mma_ts(tmem + C::kO, tmem + 64 + kk * 8, smem_desc_mn(va + kk * 2048, C::kHalf), id_o, 1u);
+        if (last) tc_commit(smem_u32(&bars.o[tile]));
+      }
+      __syncwarp();
+    };
+    auto free_stage = [&](unsigned st) {
+      if (leader) tc_commit(smem_u32(&bars.empty[st]));
+      __syncwarp();
+    };
+    auto full = [&](unsigned i) { return wait(bars.full[i % C::kStages], (i / C::kStages) & 1u, kErrTimeoutFull); };
+    for (unsigned long long u = u0; u < u1 && ok;) {
+      const int count = share(c, u, u1);
+      const bool two = c.n * a.group - c.t * kRows > kTileRows;
+      const int tiles = two ? 2 : 1;
+      for (int i = 0; i < tiles && ok; ++i) ok = wait(bars.q[i], items[i] & 1u, kErrTimeoutFull);
+      unsigned kst = n++;
+      if (!ok || !(ok = full(kst))) break;
+      tc_fence_after();
+      for (int i = 0; i < tiles; ++i) qk(i, kst % C::kStages);
+      free_stage(kst % C::kStages);
+      for (int j = 0; j < count && ok; ++j) {
+        const bool last = j + 1 == count;
+        const unsigned vst = n++;
+        if (!(ok = full(vst))) break;
+        const int key0 = (c.k.blk0 + c.blk + j) * kUnitKeys;
+        const int live = max(0, min(c.k.hi, key0 + kUnitKeys) - key0), steps = (live + 15) >> 4;
+        if (key0 + steps * 16 > c.len) {
+          // values past the sequence's end may be anything, and 0 * NaN is NaN: zero them
+          const int from = max(0, c.len - key0), nz = steps * 16 - from;
+          for (int i = lane; i < nz * C::kHalves * 8; i += 32) {
+            const int r = from + i / (C::kHalves * 8), ch = i % (C::kHalves * 8);
+            sts_u4(ring + (vst % C::kStages) * C::kTile + (ch >> 3) * C::kHalf + r * 128 + (ch & 7) * 16,
+                   make_uint4(0u, 0u, 0u, 0u));
+          }
+          fence_proxy_async_smem();
+          __syncwarp();
+        }
+        for (int i = 0; i < tiles && ok; ++i) {
+          if (j == 0) ok = wait(bars.o_free[i], (items[i] & 1u) ^ 1u, kErrTimeoutAcc);
+          ok = ok && wait(bars.p[i], sp[i] & 1u, kErrTimeoutAcc);
+          if (!ok) break;
+          ++sp[i];
+          tc_fence_after();
+          pv(i, vst % C::kStages, steps, j == 0, last, !two);
+          if (!last && i == 0) {
+            kst = n++;
+            if (!(ok = full(kst))) break;
+            tc_fence_after();
+          }
+          if (i == tiles - 1) free_stage(vst % C::kStages);
+          if (!last) qk(i, kst % C::kStages);
+        }
+        if (ok && !last) free_stage(kst % C::kStages);
+      }
+      for (int i = 0; i < tiles; ++i) ++items[i];
+      next_item(c, u);
+    }
+    if (*(volatile int*)&s_abort) {  // the MMAs issued so far end before tensor memory is given back
+      if (leader) tc_commit(smem_u32(&bars.drain));
+      __syncwarp();
+      mbar_drain(smem_u32(&bars.drain), 0u, limit);
+    }
+  } else if (warp < kSoftWarps && works) {
+    // ---- softmax: a thread per row of a tile
+    const int tile = warp >> 2, r = threadIdx.x & 127;
+    const uint32_t lanes = (uint32_t)(warp & 3) << 21;  // the warp's 32 lanes of tensor memory
+    const uint32_t ts = tmem + lanes + tile * 128, to = tmem + lanes + C::kO + tile * D;
+    const float sl2 = a.scale * 1.4426950408889634f, slack = kSlackLog2 / sl2;
+    auto active = [&](const PagedCursor<kRows>& k) { return k.n * a.group - k.t * kRows > tile * kTileRows; };
+    // the rows of Q of an item, zero past its last row
+    auto load_q = [&](const PagedCursor<kRows>& k) {
+      const int row = k.t * kRows + tile * kTileRows + r;
+      const bool live = row < k.n * a.group;
+      const int tok = live ? row / a.group : 0, head = k.h * a.group + (live ? row % a.group : 0);
+      const __nv_bfloat16* p = a.q + (int64_t)(k.q0 + tok) * a.ld_q + head * D;
+      const uint32_t dst = sq + tile * C::kTile;
+#pragma unroll
+      for (int i = 0; i < D / 8; ++i)
+        cp_async_16(dst + (i >> 3) * C::kHalf + swz_offset<64>(r, i & 7), p + i * 8, live ? 16u : 0u);
+      cp_async_commit();
+    };
+    auto q_ready = [&]() {
+      cp_async_wait<0>();
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&bars.q[tile]));
+    };
+    PagedCursor<kRows> qc = c;  // the next item whose Q is loaded
+    unsigned long long uq = u0, u = u0;
+    auto next_active = [&](PagedCursor<kRows>& k, unsigned long long& at) {
+      do next_item(k, at); while (at < u1 && !active(k));
+    };
+    if (!active(qc)) next_active(qc, uq);
+    c = qc;
+    u = uq;
+    if (uq < u1) {
+      load_q(qc);
+      q_ready();
+    }
+    unsigned sn = 0, items = 0;
+    bool ok = true;
+    while (u < u1 && ok) {
+      const int count = share(c, u, u1);
+      const bool fine = c.n * a.group - c.t * kRows <= kTileRows;  // one tile
+      const int row = c.t * kRows + tile * kTileRows + r;
+      const bool live = row < c.n * a.group;
+      const int tok = live ? row / a.group : 0, head = c.h * a.group + (live ? row % a.group : 0);
+      const int pos = c.len - c.n + tok;
+      // keys [low, lim) that the row sees; a row past the item's last one never asks for masks
+      const int lim = !live ? 0x7FFFFFFF : (a.causal ? min(c.len, pos + 1) : c.len);
+      const int low = live && a.window > 0 ? max(0, pos - a.window + 1) : 0;
+      float m = -INFINITY, l = 0.f;
+      for (int j = 0; j < count; ++j) {
+        const int key0 = (c.k.blk0 + c.blk + j) * kUnitKeys;
+        if (!(ok = wait(bars.s[tile], sn & 1u, kErrTimeoutAcc))) break;
+        ++sn;
+        tc_fence_after();
+        uint32_t s[4][32];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) tmem_ld32_nowait(ts + i * 32, s[i]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) tmem_wait_ld32(s[i]);
+        if (!__all_sync(0xffffffffu, key0 >= low && key0 + kUnitKeys <= lim)) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int k = 0; k < 32; ++k) {
+              const int key = key0 + i * 32 + k;
+              if (key < low || key >= lim) s[i][k] = 0xFF800000u;  // -infinity
+            }
+        }
+        float mx = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int k = 0; k < 32; k += 2)
+            mx = fmaxf(mx, fmaxf(__uint_as_float(s[i][k]), __uint_as_float(s[i][k + 1])));
+        const bool grows = mx > m + slack;
+        if (j == 0) {
+          m = mx;
+        } else if (__any_sync(0xffffffffu, grows)) {
+          // S of this unit is complete, so the product before it is: O stands still
+          const float f = !grows ? 1.f : (m == -INFINITY ? 0.f : ex2((m - mx) * sl2));
+          if (grows) m = mx;
+          l *= f;
+#pragma unroll
+          for (int i = 0; i < D / 32; ++i) {
+            uint32_t o[32];
+            tmem_ld32_nowait(to + i * 32, o);
+            tmem_wait_ld32(o);
+#pragma unroll
+            for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * f);
+            tmem_st32(to + i * 32, o);
+          }
+        }
+        const float nz = m == -INFINITY ? 0.f : -m * sl2;
+        const f2_t sc = f2(sl2, sl2), off = f2(nz, nz);
+        f2_t sum = f2(0.f, 0.f);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          uint32_t p[16];
+#pragma unroll
+          for (int k = 0; k < 16; ++k) {
+            float x, y;
+            f2_split(ffma2(f2(__uint_as_float(s[i][2 * k]), __uint_as_float(s[i][2 * k + 1])), sc, off), x, y);
+            x = ex2(x);
+            y = ex2(y);
+            sum = fadd2(sum, f2(x, y));
+            s[i][2 * k] = __float_as_uint(x);
+            s[i][2 * k + 1] = __float_as_uint(y);
+            asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(p[k]) : "f"(y), "f"(x));
+          }
+          tmem_st16(ts + i * 16, p);  // (columns of scores that are in registers already)
+          if (fine) {
+#pragma unroll
+            for (int k = 0; k < 16; ++k) {
+              const float lo = __uint_as_float(s[i][2 * k]) - __uint_as_float(p[k] << 16);
+              const float up = __uint_as_float(s[i][2 * k + 1]) - __uint_as_float(p[k] & 0xFFFF0000u);
+              asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(p[k]) : "f"(up), "f"(lo));
+            }
+            tmem_st16(ts + 64 + i * 16, p);
+          }
+        }
+        float x, y;
+        f2_split(sum, x, y);
+        l += x + y;
+        tmem_wait_st();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&bars.p[tile]));
+      }
+      if (!ok) break;
+      // every product with this item's Q is done: the next item's rows
+      next_active(qc, uq);
+      if (uq < u1) load_q(qc);
+      ok = wait(bars.o[tile], items & 1u, kErrTimeoutAcc);
+      ++items;
+      if (uq < u1) q_ready();
+      if (!ok) break;
+      tc_fence_after();
+      const unsigned long long i0 = u - c.blk;
+      if (c.blk > 0 || count < c.k.units) {
+        // a part of the item: sums, maximum and sum of weights as they are
+        float* slot = a.ws + (size_t)(2 * blockIdx.x + (i0 > u0 ? 1 : 0)) * C::kSlotFloats;
+        const int at = tile * kTileRows + r;
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i) {
+          uint32_t o[32];
+          tmem_ld32_nowait(to + i * 32, o);
+          tmem_wait_ld32(o);
+#pragma unroll
+          for (int k = 0; k < 32; k += 4)
+            *reinterpret_cast<uint4*>(slot + (size_t)((i * 32 + k) / 4 * kRows + at) * 4) =
+                make_uint4(o[k], o[k + 1], o[k + 2], o[k + 3]);
+        }
+        slot[kRows * D + at] = m;
+        slot[kRows * D + kRows + at] = l;
+      } else {
+        const float inv = l > 0.f ? 1.f / l : 0.f;
+        const int64_t at = (int64_t)(c.q0 + tok) * a.heads + head;
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i) {
+          uint32_t o[32];
+          tmem_ld32_nowait(to + i * 32, o);
+          tmem_wait_ld32(o);
+          if (live) {
+#pragma unroll
+            for (int k = 0; k < 32; k += 8) {
+              float f[8];
+#pragma unroll
+              for (int e = 0; e < 8; ++e) f[e] = l > 0.f ? __uint_as_float(o[k + e]) * inv : 0.f;
+              *reinterpret_cast<uint4*>(a.y + at * D + i * 32 + k) = pack8(f);
+            }
+          }
+        }
+        if (live && a.lse) a.lse[at] = l > 0.f ? fmaf(m, a.scale, logf(l)) : -INFINITY;
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&bars.o_free[tile]));
+      c = qc;
+      u = uq;
+    }
+    cp_async_wait<0>();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  if (warp == kMmaWarp) tmem_dealloc(tmem, C::kCols);
+}
+
+// Joins the parts of the items that several CTAs shared, in the order of their keys:
+// a block per cut and 32 rows.
+constexpr int kJoinThreads = 128;
+template <int D>
+__global__ void __launch_bounds__(kJoinThreads)
+    paged_join_kernel(const __grid_constant__ PagedArgs a, int grid) {
+  using C = Cfg<D>;
+  pdl_wait();
+  pdl_trigger();
+  const JoinItem j = reinterpret_cast<const JoinItem*>(a.ws + (size_t)2 * grid * C::kSlotFloats)[blockIdx.x];
+  const int r = blockIdx.y * 32 + (threadIdx.x & 31);
+  if (!j.valid || r >= j.rows) return;
+  auto slot = [&](int c) { return a.ws + (size_t)(2 * c + (c == j.c0 && j.late ? 1 : 0)) * C::kSlotFloats; };
+  const float sl2 = a.scale * 1.4426950408889634f;
+  float mx = -INFINITY, l = 0.f;
+  for (int c = j.c0; c <= j.c1; ++c) mx = fmaxf(mx, slot(c)[kRows * D + r]);
+  auto weight = [&](int c) {
+    const float m = slot(c)[kRows * D + r];
+    return m == -INFINITY ? 0.f : ex2((m - mx) * sl2);
+  };
+  for (int c = j.c0; c <= j.c1; ++c) l += weight(c) * slot(c)[kRows * D + kRows + r];
+  const float inv = l > 0.f ? 1.f / l : 0.f;
+  const int row = j.t * kRows + r;
+  const int64_t at = (int64_t)(j.q0 + row / a.group) * a.heads + j.h * a.group + row % a.group;
+  for (int g = threadIdx.x >> 5; g < D / 8; g += kJoinThreads / 32) {
+    float f[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    for (int c = j.c0; c <= j.c1; ++c) {
+      const float w = weight(c) * inv;
+      const float4 p = *reinterpret_cast<const float4*>(slot(c) + (size_t)((2 * g) * kRows + r) * 4);
+      const float4 q = *reinterpret_cast<const float4*>(slot(c) + (size_t)((2 * g + 1) * kRows + r) * 4);
+      f[0] = fmaf(w, p.x, f[0]); f[1] = fmaf(w, p.y, f[1]); f[2] = fmaf(w, p.z, f[2]); f[3] = fmaf(w, p.w, f[3]);
+      f[4] = fmaf(w, q.x, f[4]); f[5] = fmaf(w, q.y, f[5]); f[6] = fmaf(w, q.z, f[6]); f[7] = fmaf(w, q.w, f[7]);
+    }
+    *reinterpret_cast<uint4*>(a.y + at * D + g * 8) = pack8(f);
+  }
+  if (a.lse && threadIdx.x < 32) a.lse[at] = l > 0.f ? fmaf(mx, a.scale, logf(l)) : -INFINITY;
+}
+
+int grid_of() {
+  const int sms = device_sm_count();
+  return sms < kPagedCounters ? sms : kPagedCounters;
+}
+
+template <int D>
+cudaError_t launch_chunk(const PagedArgs& a, cudaStream_t s) {
+  CUtensorMap tk, tv;
+  const uint64_t rows = (uint64_t)a.pages * a.kv_heads << a.page_log2;
+  if (!make_tmap_2d(&tk, a.k, rows, D, 64, 1u << a.page_log2) || !make_tmap_2d(&tv, a.v, rows, D, 64, 1u << a.page_log2))
+    return cudaErrorInvalidValue;
+  cudaError_t e = smem_optin(reinterpret_cast<const void*>(paged_chunk_kernel<D>), Cfg<D>::kSmem);
+  if (e != cudaSuccess) return e;
+  const int grid = grid_of();
+  e = launch_kernel(paged_chunk_kernel<D>, dim3(grid), dim3(kThreads), Cfg<D>::kSmem, s, tk, tv, a);
+  if (e != cudaSuccess) return e;
+  return launch_kernel(paged_join_kernel<D>, dim3(grid, kRows / 32), dim3(kJoinThreads), 0, s, a, grid);
+}
+
+}  // namespace
+
+size_t paged_chunk_ws_bytes() {
+  return ((size_t)2 * Cfg<128>::kSlotFloats * sizeof(float) + sizeof(JoinItem)) * grid_of();
+}
+
+cudaError_t launch_paged_chunk(const PagedArgs& a, cudaStream_t s) {
+  return a.D == 128 ? launch_chunk<128>(a, s) : launch_chunk<64>(a, s);
+}
+
+}  // namespace sparoa

@@ -394,9 +394,13 @@ cudaError_t launch_small(const PagedArgs& a, cudaStream_t s) {
 
 }  // namespace
 
-size_t paged_ws_bytes() { return (size_t)2 * kPagedCounters * kSlotFloats<128> * sizeof(float); }
+size_t paged_ws_bytes() {
+  const size_t small = (size_t)2 * kPagedCounters * kSlotFloats<128> * sizeof(float), chunk = paged_chunk_ws_bytes();
+  return small > chunk ? small : chunk;
+}
 
 cudaError_t launch_paged_attention(const PagedArgs& a, cudaStream_t s) {
+  if ((int64_t)a.max_q * a.group > kRows) return launch_paged_chunk(a, s);
   return a.D == 128 ? launch_small<128>(a, s) : launch_small<64>(a, s);
 }
 

@@ -218,7 +218,7 @@ cudaError_t launch_select(const __nv_bfloat16* x, int N, int T, int D, int index
                           cudaStream_t s);
 
 // ----------------------------------------------------------------------------
-// Decoder operators (k_decoder.cu, k_paged.cu)
+// Decoder operators (k_decoder.cu, k_paged.cu, k_chunk.cu)
 // ----------------------------------------------------------------------------
 struct NormDev {
   int kind = 0;  // 0 none, 1 RMS, 2 layer
@@ -282,11 +282,15 @@ struct PagedArgs {
   unsigned* cnt = nullptr;     // kPagedCounters arrival counters, zero between calls
   uint32_t* err = nullptr;
   long long wait_limit = 0;
+  int fault = 0;               // error-path tests: 1 withholds the chunk kernel's signals of its scores
 };
 constexpr int kPagedMaxBatch = 1024;
 constexpr int kPagedCounters = 512;
 size_t paged_ws_bytes();
 cudaError_t launch_paged_attention(const PagedArgs& a, cudaStream_t s);
+// the kernel for chunks of tokens (k_chunk.cu)
+size_t paged_chunk_ws_bytes();
+cudaError_t launch_paged_chunk(const PagedArgs& a, cudaStream_t s);
 
 // ----------------------------------------------------------------------------
 // Memory-bound kernels (128-row x 64-channel tiles, occupancy fused)

@@ -6,6 +6,7 @@ terms add at most C 2^-24 of the terms' sizes, far below that; for values that a
 their row (cancellation) an absolute part of 1e-5 of the row's largest is allowed.  Attention of few
 rows keeps 16 bits of its probabilities (2^-16 of sum p |v|), and fp32 scores (D 2^-24 of sum |q k|, at
 most 1e-4 here) move the probabilities by 1e-4: 2^-9 + 2^-12 of sum p |v| is allowed for both.
+Attention of chunks rounds them to one bf16: 2^-8 + 2^-12 of sum p |v|.
 The log of the sum moves with the scores: 2e-4."""
 import math
 
@@ -222,7 +223,8 @@ def _attn64(q, k, v, table, new, kv, page, scale, causal, window):
     return y, lse, size
 
 
-def _check_attn(sp, ctx, new, kv, H, KH, D, page, causal=True, window=0, seed=0, max_q=None, strided=False, scale=None):
+def _check_attn(sp, ctx, new, kv, H, KH, D, page, causal=True, window=0, seed=0, max_q=None, strided=False, scale=None,
+                p_round=2.0 ** -9):
     cache, batch, k, v, table = _batch(sp, new, kv, page, KH, D, seed)
     if max_q is not None:
         batch.desc.max_q = max_q
@@ -244,7 +246,7 @@ def _check_attn(sp, ctx, new, kv, H, KH, D, page, causal=True, window=0, seed=0,
     got = lse.double().cpu()
     assert torch.equal(torch.isinf(got), empty) and not torch.isnan(got).any(), what
     assert ((got - wl)[~empty].abs() <= 2e-4).all(), what
-    _close(y, want, what, extra=(2.0 ** -9 + 2.0 ** -12) * size)
+    _close(y, want, what, extra=(p_round + 2.0 ** -12) * size)
     assert (y.cpu()[empty] == 0).all(), what
     return y, lse
 
@@ -270,6 +272,92 @@ def test_attention_masks(sp, ctx, causal, window, D):
 def test_attention_strides_and_scale(sp, ctx):
     _check_attn(sp, ctx, [4, 1], [50, 300], 8, 4, 64, 16, strided=True, scale=0.03)
     _check_attn(sp, ctx, [1, 2], [500, 300], 4, 2, 128, 64, strided=True, scale=1.5)
+
+
+CHUNKS = [([17], [17]), ([64], [64]), ([65], [65]), ([33], [500]), ([128], [128]), ([129], [129]), ([300], [300]), ([20], [3000]),
+          ([100, 1, 40], [100, 700, 333]), ([16, 1], [16, 257]), ([40, 3], [100, 1000]), ([30, 0, 1, 200], [10, 0, 0, 1025]),
+          ([257, 20], [2000, 20])]
+
+
+@pytest.mark.parametrize("new,kv", CHUNKS)
+@pytest.mark.parametrize("H,KH,D,page", [(2, 2, 64, 16), (8, 2, 128, 64), (3, 1, 64, 32), (6, 2, 128, 128), (20, 1, 128, 16)])
+def test_attention_chunks(sp, ctx, new, kv, H, KH, D, page):
+    _check_attn(sp, ctx, new, kv, H, KH, D, page, seed=len(new) + kv[0], p_round=2.0 ** -8)
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("window", [0, 1, 5, 128, 1000])
+@pytest.mark.parametrize("D", [64, 128])
+def test_attention_chunk_masks(sp, ctx, causal, window, D):
+    _check_attn(sp, ctx, [70, 1, 7, 150], [400, 129, 7, 1300], 4, 2, D, 32, causal=causal, window=window, seed=window,
+                p_round=2.0 ** -8)
+
+
+def test_attention_chunk_strides_and_scale(sp, ctx):
+    _check_attn(sp, ctx, [40, 1], [50, 300], 8, 4, 64, 16, strided=True, scale=0.03, p_round=2.0 ** -8)
+    _check_attn(sp, ctx, [1, 90], [500, 300], 4, 2, 128, 64, strided=True, scale=1.5, p_round=2.0 ** -8)
+    _check_attn(sp, ctx, [50], [600], 4, 2, 64, 16, scale=20.0, p_round=2.0 ** -8)  # weights below the smallest float
+
+
+def test_attention_growing_scores(sp, ctx):
+    """Every key outweighs all before it by far, and the other way round: the rows' maxima move at
+    every unit, or never again."""
+    D, n, L, page = 64, 40, 1500, 16
+    for sign in (1.0, -1.0):
+        cache, batch, k, v, table = _batch(sp, [n], [L], page, 1, D, 5)
+        u = torch.ones(D) / D ** 0.5
+        for j in range(L):
+            k[int(table[0, j // page]), 0, j % page] = (sign * u * j * 0.5).to(torch.bfloat16)
+        cache.k.copy_(k)
+        q = (torch.randn(n, 2, D, generator=_g(1)) * 0.1 + u).to(torch.bfloat16)
+        y = torch.empty(n, 2, D, dtype=torch.bfloat16, device="cuda")
+        sp.sparoa_paged_attention(ctx, q.cuda(), y, cache, batch, scale=1.0, causal=False)
+        ctx.sync()
+        want, _, size = _attn64(q, k, v, table, [n], [L], page, 1.0, False, 0)
+        # scores of up to 800 in fp32: 64 2^-24 * 800 move the weights by 3e-3
+        _close(y, want, f"growing {sign}", extra=(2.0 ** -8 + 4e-3) * size)
+
+
+def test_attention_any_max_q(sp, ctx):
+    """max_q chooses a kernel, not the result."""
+    for mq in (0, 1, 1000):
+        _check_attn(sp, ctx, [30, 1, 9], [77, 400, 9], 8, 2, 128, 32, max_q=mq, p_round=2.0 ** -8)
+        _check_attn(sp, ctx, [30, 1, 9], [77, 400, 9], 6, 6, 64, 16, max_q=mq, p_round=2.0 ** -8)
+        _check_attn(sp, ctx, [700], [700], 4, 1, 64, 16, max_q=mq, p_round=2.0 ** -8)
+
+
+def test_attention_chunk_split_is_repeatable(sp, ctx):
+    """Few tiles over a long context: their units are shared by many CTAs."""
+    cache, batch, *_ = _batch(sp, [20], [40000], 64, 2, 128, 3)
+    q = torch.randn(20, 8, 128, generator=_g(4)).to(torch.bfloat16).cuda()
+    ys = [torch.empty(20, 8, 128, dtype=torch.bfloat16, device="cuda") for _ in range(10)]
+    for y in ys:
+        sp.sparoa_paged_attention(ctx, q, y, cache, batch)
+    ctx.sync()
+    assert all(torch.equal(ys[0], y) for y in ys[1:])
+    _check_attn(sp, ctx, [20], [40000], 8, 2, 128, 64, p_round=2.0 ** -8)
+
+
+def test_attention_chunk_timeout(sp):
+    """A wait that runs out: an error, and the context is usable afterwards."""
+    c = sp.Context(0)
+    cache, batch, *_ = _batch(sp, [64], [3000], 16, 2, 128, 8)
+    q = torch.randn(64, 8, 128, generator=_g(1)).to(torch.bfloat16).cuda()
+    y, z = torch.empty_like(q), torch.empty_like(q)
+    sp.sparoa_paged_attention(c, q, y, cache, batch)
+    c.sync()
+    c.set_fault(1)
+    c.set_wait_limit(2000000)
+    sp.sparoa_paged_attention(c, q, z, cache, batch)
+    with pytest.raises(sp.SparoaError) as e:
+        c.sync()
+    assert e.value.status == sp.ERR_TIMEOUT
+    c.set_fault(0)
+    c.set_wait_limit(0)
+    sp.sparoa_paged_attention(c, q, z, cache, batch)
+    c.sync()
+    assert torch.equal(y, z)
+    c.close()
 
 
 def test_attention_split_is_repeatable(sp, ctx):
