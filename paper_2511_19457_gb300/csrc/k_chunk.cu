@@ -33,7 +33,7 @@ constexpr int kRows = 256;     // rows of an item
 constexpr int kTileRows = 128;
 constexpr int kSoftWarps = 8;
 constexpr int kMmaWarp = 8, kLoadWarp = 9;
-constexpr int kThreads = 320;
+constexpr int kThreads = 384;  // 12 warps: the last two only fill the third group of four
 constexpr float kSlackLog2 = 8.f;
 
 template <int D>
@@ -96,16 +96,390 @@ __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32
       : "memory");
 }
 
+// Registers: all groups of four warps start with 168 a thread (the launch's 64512 / 384);
+// the softmax groups, whose threads hold a row of scores, take what the third gives up.
+constexpr int kManyRegs = 208, kFewRegs = 88;
+static_assert(2 * kManyRegs + kFewRegs == 3 * 168, "registers of the launch");
+template <int N>
+__device__ __forceinline__ void reg_inc() {
+  asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N));
+}
+template <int N>
+__device__ __forceinline__ void reg_dec() {
+  asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N));
+}
+
 struct Bars {
   unsigned long long full[8], empty[8];      // ring
   unsigned long long s[2], p[2], q[2], o[2], o_free[2];  // per tile
   unsigned long long drain;
 };
 
-// What a share of an item is: units [blk, blk + count) of the cursor's item.
-__device__ __forceinline__ int share(const PagedCursor<kRows>& c, unsigned long long u, unsigned long long u1) {
-  const unsigned long long left = u1 - u, rest = (unsigned long long)(c.k.units - c.blk);
-  return (int)(left < rest ? left : rest);
+// What the roles of a CTA share.
+struct Shared {
+  PagedPlan plan;
+  Bars bars;
+  PagedCursor<kRows> at[12];    // a warp's place, in memory: the softmax threads need their registers
+  PagedCursor<kRows> next[8];   // the softmax warps': the item whose Q is loaded next
+  uint32_t tmem;
+  int abort;
+};
+
+struct Role {
+  const PagedArgs& a;
+  Shared& sh;
+  uint32_t sq, ring;   // Q tiles, K and V stages
+  int units;           // of this CTA
+  long long limit;
+
+  __device__ __forceinline__ bool wait(unsigned long long& bar, unsigned parity, uint32_t bit) const {
+    return mbar_wait_warp(smem_u32(&bar), parity, a.err, &sh.abort, bit, limit);
+  }
+  __device__ __forceinline__ bool aborted() const { return *(volatile int*)&sh.abort != 0; }
+  // units of the place's item that are this CTA's, with `left` units to go
+  static __device__ __forceinline__ int share(const PagedCursor<kRows>& c, int left) { return min(left, c.k.units - c.blk); }
+  // to the next item's first unit (a converged warp; left > 0 afterwards, or c stays)
+  __device__ __forceinline__ void next_item(PagedCursor<kRows>& c, int& left) const {
+    left -= share(c, left);
+    __syncwarp();
+    if (left > 0 && (threadIdx.x & 31) == 0) {
+      c.blk = c.k.units - 1;
+      c.next(a, sh.plan);
+    }
+    __syncwarp();
+  }
+};
+
+// K and V of every unit, in the order of their use: K0 V0 K1 V1 ...
+template <int D>
+__device__ __forceinline__ void load_role(const Role& r, const CUtensorMap* tk, const CUtensorMap* tv) {
+  using C = Cfg<D>;
+  const PagedArgs& a = r.a;
+  const int lane = threadIdx.x & 31;
+  PagedCursor<kRows> c = r.sh.at[threadIdx.x >> 5];
+  const int pages = kUnitKeys >> a.page_log2;        // of a whole unit
+  const int pg = lane / C::kHalves, half = lane % C::kHalves;
+  const uint32_t box = 128u << a.page_log2;          // bytes: page_size rows of 128
+  unsigned n = 0;                                    // stages filled
+  auto entry = [&]() {
+    const int key = (c.k.blk0 + c.blk) * kUnitKeys + (pg << a.page_log2);
+    return pg < pages && key < c.k.hi ? page_of(a, c.b, key) : -1;
+  };
+  int page = entry();
+  bool ok = true;
+  for (int left = r.units; left > 0 && ok; --left) {
+    const int key0 = (c.k.blk0 + c.blk) * kUnitKeys;
+    const int live = max(0, min(c.k.hi, key0 + kUnitKeys) - key0);
+    const int need = (live + (1 << a.page_log2) - 1) >> a.page_log2;
+    const bool mine = pg < need;
+    const int row = mine ? pool_row(a, page_checked(a, page), c.h, 0) : 0;
+    if (left > 1) {
+      c.next(a, r.sh.plan);
+      page = entry();  // on its way while this unit waits for room
+    }
+#pragma unroll
+    for (int kv = 0; kv < 2; ++kv) {
+      const unsigned st = n % C::kStages;
+      ok = r.wait(r.sh.bars.empty[st], ((n / C::kStages) & 1u) ^ 1u, kErrTimeoutEmpty);
+      if (!ok) break;
+      const uint32_t bar = smem_u32(&r.sh.bars.full[st]);
+      if (lane == 0) mbar_arrive_expect_tx(bar, (uint32_t)(need * C::kHalves) * box);
+      __syncwarp();
+      if (mine) tma_load_2d(r.ring + st * C::kTile + half * C::kHalf + pg * box, kv ? tv : tk, bar, half * 64, row);
+      ++n;
+    }
+  }
+  // after a timeout: wait for the copies in flight into memory that is given back
+  if (r.aborted())
+    for (unsigned i = n > (unsigned)C::kStages ? n - C::kStages : 0u; i < n; ++i)
+      mbar_drain(smem_u32(&r.sh.bars.full[i % C::kStages]), (i / C::kStages) & 1u, r.limit);
+}
+
+// The MMAs.
+template <int D>
+__device__ __forceinline__ void mma_role(const Role& r, uint32_t tmem) {
+  using C = Cfg<D>;
+  const PagedArgs& a = r.a;
+  Bars& bars = r.sh.bars;
+  const int lane = threadIdx.x & 31;
+  PagedCursor<kRows>& c = r.sh.at[threadIdx.x >> 5];
+  const bool leader = elect_one();
+  constexpr uint32_t id_s = idesc_bf16_f32(kTileRows, kUnitKeys);
+  constexpr uint32_t id_o = idesc_bf16_f32(kTileRows, D) | (1u << 16);  // B is MN-major
+  unsigned n = 0, sp[2] = {0, 0}, items[2] = {0, 0};
+  bool ok = true;
+  auto qk = [&](int tile, unsigned st) {
+    if (leader) {
+      const uint64_t qd = smem_desc_kmajor<64>(r.sq + tile * C::kTile), kd = smem_desc_kmajor<64>(r.ring + st * C::kTile);
+#pragma unroll
+      for (int kk = 0; kk < D / 16; ++kk) {
+        const uint32_t at = ((kk >> 2) * C::kHalf + (kk & 3) * 32) >> 4;
+        mma_ss(tmem + tile * 128, qd + at, kd + at, id_s, kk > 0);
+      }
+      if (!a.fault) tc_commit(smem_u32(&bars.s[tile]));
+    }
+    __syncwarp();
+  };
+  auto pv = [&](int tile, unsigned st, int steps, bool first, bool last, bool fine) {
+    if (leader) {
+      const uint64_t vd = smem_desc_mn(r.ring + st * C::kTile, C::kHalf);
+      const uint32_t d = tmem + C::kO + tile * D, p = tmem + tile * 128;
+      if (steps == 8) {
+#pragma unroll
+        for (int kk = 0; kk < 8; ++kk) mma_ts(d, p + kk * 8, vd + kk * 128, id_o, !(first && kk == 0));
+      } else {
+        for (int kk = 0; kk < steps; ++kk) mma_ts(d, p + kk * 8, vd + kk * 128, id_o, !(first && kk == 0));
+      }
+      if (fine)
+        for (int kk = 0; kk < steps; ++kk) mma_ts(d, p + 64 + kk * 8, vd + kk * 128, id_o, 1u);
+      if (last) tc_commit(smem_u32(&bars.o[tile]));
+    }
+    __syncwarp();
+  };
+  auto free_stage = [&](unsigned st) {
+    if (leader) tc_commit(smem_u32(&bars.empty[st]));
+    __syncwarp();
+  };
+  auto full = [&](unsigned i) { return r.wait(bars.full[i % C::kStages], (i / C::kStages) & 1u, kErrTimeoutFull); };
+  for (int left = r.units; left > 0 && ok;) {
+    const int count = Role::share(c, left), first_key = (c.k.blk0 + c.blk) * kUnitKeys, hi = c.k.hi, len = c.len;
+    const bool two = c.n * a.group - c.t * kRows > kTileRows;
+    const int tiles = two ? 2 : 1;
+    for (int i = 0; i < tiles && ok; ++i) ok = r.wait(bars.q[i], items[i] & 1u, kErrTimeoutFull);
+    unsigned kst = n++;
+    if (!ok || !(ok = full(kst))) break;
+    tc_fence_after();
+    for (int i = 0; i < tiles; ++i) qk(i, kst % C::kStages);
+    free_stage(kst % C::kStages);
+    for (int j = 0; j < count && ok; ++j) {
+      const bool last = j + 1 == count;
+      const unsigned vst = n++;
+      if (!(ok = full(vst))) break;
+      const int key0 = first_key + j * kUnitKeys;
+      const int steps = (max(0, min(hi, key0 + kUnitKeys) - key0) + 15) >> 4;
+      if (key0 + steps * 16 > len) {
+        // values past the sequence's end may be anything, and 0 * NaN is NaN: zero them
+        const int from = max(0, len - key0), nz = steps * 16 - from;
+        for (int i = lane; i < nz * C::kHalves * 8; i += 32) {
+          const int row = from + i / (C::kHalves * 8), ch = i % (C::kHalves * 8);
+          sts_u4(r.ring + (vst % C::kStages) * C::kTile + (ch >> 3) * C::kHalf + row * 128 + (ch & 7) * 16,
+                 make_uint4(0u, 0u, 0u, 0u));
+        }
+        fence_proxy_async_smem();
+        __syncwarp();
+      }
+      for (int i = 0; i < tiles; ++i) {
+        if (j == 0) ok = r.wait(bars.o_free[i], (items[i] & 1u) ^ 1u, kErrTimeoutAcc);
+        ok = ok && r.wait(bars.p[i], sp[i] & 1u, kErrTimeoutAcc);
+        if (!ok) break;
+        ++sp[i];
+        tc_fence_after();
+        pv(i, vst % C::kStages, steps, j == 0, last, !two);
+        if (!last && i == 0) {
+          kst = n++;
+          if (!(ok = full(kst))) break;
+          tc_fence_after();
+        }
+        if (i == tiles - 1) free_stage(vst % C::kStages);
+        if (!last) qk(i, kst % C::kStages);
+      }
+      if (ok && !last) free_stage(kst % C::kStages);
+    }
+    for (int i = 0; i < tiles; ++i) ++items[i];
+    r.next_item(c, left);
+  }
+  if (r.aborted()) {  // the MMAs issued so far end before tensor memory is given back
+    if (leader) tc_commit(smem_u32(&bars.drain));
+    __syncwarp();
+    mbar_drain(smem_u32(&bars.drain), 0u, r.limit);
+  }
+}
+
+// The softmax: a thread per row of a tile.
+template <int D>
+__device__ __forceinline__ void softmax_role(const Role& r, uint32_t tmem) {
+  using C = Cfg<D>;
+  const PagedArgs& a = r.a;
+  Bars& bars = r.sh.bars;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, tile = warp >> 2, row = threadIdx.x & 127;
+  const uint32_t lanes = (uint32_t)(warp & 3) << 21;  // the warp's 32 lanes of tensor memory
+  const uint32_t ts = tmem + lanes + tile * 128, to = tmem + lanes + C::kO + tile * D;
+  const float sl2 = a.scale * 1.4426950408889634f, slack = kSlackLog2 / sl2;
+  PagedCursor<kRows>& c = r.sh.at[warp];
+  PagedCursor<kRows>& qc = r.sh.next[warp];
+  auto rows_of = [&](const PagedCursor<kRows>& k) { return k.n * a.group - k.t * kRows - tile * kTileRows; };
+  auto next_active = [&](PagedCursor<kRows>& k, int& left) {
+    do r.next_item(k, left); while (left > 0 && rows_of(k) <= 0);
+  };
+  // the rows of Q of an item, zero past its last row
+  auto load_q = [&]() {
+    const bool live = row < rows_of(qc);
+    const int at = live ? qc.t * kRows + tile * kTileRows + row : 0, tok = at / a.group, head = qc.h * a.group + at % a.group;
+    const __nv_bfloat16* p = a.q + (int64_t)(qc.q0 + tok) * a.ld_q + head * D;
+    const uint32_t dst = r.sq + tile * C::kTile;
+#pragma unroll
+    for (int i = 0; i < D / 8; ++i)
+      cp_async_16(dst + (i >> 3) * C::kHalf + swz_offset<64>(row, i & 7), p + i * 8, live ? 16u : 0u);
+    cp_async_commit();
+  };
+  auto q_ready = [&]() {
+    cp_async_wait<0>();
+    fence_proxy_async_smem();
+    __syncwarp();
+    if (lane == 0) mbar_arrive(smem_u32(&bars.q[tile]));
+  };
+  int left = r.units, qleft = r.units;
+  if (rows_of(c) <= 0) {
+    next_active(c, left);
+    next_active(qc, qleft);
+  }
+  if (left > 0) {
+    load_q();
+    q_ready();
+  }
+  unsigned sn = 0, items = 0;
+  bool ok = true;
+  while (left > 0) {
+    const int count = Role::share(c, left), first_key = (c.k.blk0 + c.blk) * kUnitKeys;
+    const int rows = rows_of(c);
+    const bool fine = tile == 0 && rows <= kTileRows;  // an item of one tile
+    const bool live = row < rows;
+    // keys [low, lim) that the row sees; a row past the item's last one never asks for masks
+    int lim = 0x7FFFFFFF, low = 0;
+    if (live) {
+      const int pos = c.len - c.n + (c.t * kRows + tile * kTileRows + row) / a.group;
+      lim = a.causal ? min(c.len, pos + 1) : c.len;
+      low = a.window > 0 ? max(0, pos - a.window + 1) : 0;
+    }
+    float m = -INFINITY, l = 0.f;
+    for (int j = 0; j < count; ++j) {
+      const int key0 = first_key + j * kUnitKeys;
+      if (!(ok = r.wait(bars.s[tile], sn & 1u, kErrTimeoutAcc))) break;
+      ++sn;
+      tc_fence_after();
+      uint32_t s[4][32];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) tmem_ld32_nowait(ts + i * 32, s[i]);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) tmem_wait_ld32(s[i]);
+      if (!__all_sync(0xffffffffu, key0 >= low && key0 + kUnitKeys <= lim)) {
+        const int from = low - key0, to_ = lim - key0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int k = 0; k < 32; ++k)
+            if (i * 32 + k < from || i * 32 + k >= to_) s[i][k] = 0xFF800000u;  // -infinity
+      }
+      float mx = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int k = 0; k < 32; k += 2)
+          mx = fmaxf(mx, fmaxf(__uint_as_float(s[i][k]), __uint_as_float(s[i][k + 1])));
+      const bool grows = mx > m + slack;
+      if (j == 0) {
+        m = mx;
+      } else if (__any_sync(0xffffffffu, grows)) {
+        // S of this unit is complete, so the product before it is: O stands still
+        const float f = !grows ? 1.f : (m == -INFINITY ? 0.f : ex2((m - mx) * sl2));
+        if (grows) m = mx;
+        l *= f;
+#pragma unroll 1
+        for (int i = 0; i < D / 16; ++i) {
+          float o[16];
+          uint32_t q[16];
+          tmem_ld16(to + i * 16, o);
+#pragma unroll
+          for (int k = 0; k < 16; ++k) q[k] = __float_as_uint(o[k] * f);
+          tmem_st16(to + i * 16, q);
+        }
+      }
+      const float nz = m == -INFINITY ? 0.f : -m * sl2;
+      const f2_t sc = f2(sl2, sl2), off = f2(nz, nz);
+      f2_t sum = f2(0.f, 0.f);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        uint32_t p[16];
+#pragma unroll
+        for (int k = 0; k < 16; ++k) {
+          float x, y;
+          f2_split(ffma2(f2(__uint_as_float(s[i][2 * k]), __uint_as_float(s[i][2 * k + 1])), sc, off), x, y);
+          x = ex2(x);
+          y = ex2(y);
+          sum = fadd2(sum, f2(x, y));
+          s[i][2 * k] = __float_as_uint(x);
+          s[i][2 * k + 1] = __float_as_uint(y);
+          asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(p[k]) : "f"(y), "f"(x));
+        }
+        tmem_st16(ts + i * 16, p);  // (columns of scores that are in registers already)
+        if (fine) {
+#pragma unroll
+          for (int k = 0; k < 16; ++k) {
+            const float lo = __uint_as_float(s[i][2 * k]) - __uint_as_float(p[k] << 16);
+            const float up = __uint_as_float(s[i][2 * k + 1]) - __uint_as_float(p[k] & 0xFFFF0000u);
+            asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(p[k]) : "f"(up), "f"(lo));
+          }
+          tmem_st16(ts + 64 + i * 16, p);
+        }
+      }
+      float x, y;
+      f2_split(sum, x, y);
+      l += x + y;
+      tmem_wait_st();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&bars.p[tile]));
+    }
+    if (!ok) break;
+    // every product with this item's Q is done: the next item's rows
+    next_active(qc, qleft);
+    if (qleft > 0) load_q();
+    ok = r.wait(bars.o[tile], items & 1u, kErrTimeoutAcc);
+    ++items;
+    if (qleft > 0) q_ready();
+    if (!ok) break;
+    tc_fence_after();
+    if (c.blk > 0 || count < c.k.units) {
+      // a part of the item: sums, maximum and sum of weights as they are
+      float* slot = a.ws + (size_t)(2 * blockIdx.x + (left < r.units ? 1 : 0)) * C::kSlotFloats;
+      const int at = tile * kTileRows + row;
+#pragma unroll 1
+      for (int i = 0; i < D / 16; ++i) {
+        float o[16];
+        tmem_ld16(to + i * 16, o);
+#pragma unroll
+        for (int k = 0; k < 16; k += 4)
+          *reinterpret_cast<float4*>(slot + (size_t)((i * 16 + k) / 4 * kRows + at) * 4) =
+              make_float4(o[k], o[k + 1], o[k + 2], o[k + 3]);
+      }
+      slot[kRows * D + at] = m;
+      slot[kRows * D + kRows + at] = l;
+    } else {
+      const float inv = l > 0.f ? 1.f / l : 0.f;
+      const int of = c.t * kRows + tile * kTileRows + (live ? row : 0);
+      const int64_t at = (int64_t)(c.q0 + of / a.group) * a.heads + c.h * a.group + of % a.group;
+#pragma unroll 1
+      for (int i = 0; i < D / 16; ++i) {
+        float o[16];
+        tmem_ld16(to + i * 16, o);
+        if (live) {
+#pragma unroll
+          for (int k = 0; k < 16; k += 8) {
+            float f[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) f[e] = l > 0.f ? o[k + e] * inv : 0.f;
+            *reinterpret_cast<uint4*>(a.y + at * D + i * 16 + k) = pack8(f);
+          }
+        }
+      }
+      if (live && a.lse) a.lse[at] = l > 0.f ? fmaf(m, a.scale, logf(l)) : -INFINITY;
+    }
+    tc_fence_before();
+    __syncwarp();
+    if (lane == 0) mbar_arrive(smem_u32(&bars.o_free[tile]));
+    next_active(c, left);
+  }
+  cp_async_wait<0>();
 }
 
 template <int D>
@@ -114,13 +488,10 @@ __global__ void __launch_bounds__(kThreads, 1)
                        const __grid_constant__ PagedArgs a) {
   using C = Cfg<D>;
   extern __shared__ uint8_t smem_raw[];
-  __shared__ PagedPlan plan;
-  __shared__ __align__(8) Bars bars;
-  __shared__ uint32_t s_tmem;
-  __shared__ int s_abort;
+  __shared__ __align__(8) Shared sh;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const uint32_t sq = (smem_u32(smem_raw) + 1023u) & ~1023u, ring = sq + 2 * C::kTile;
   if (threadIdx.x == 0) {
+    Bars& bars = sh.bars;
     for (int i = 0; i < C::kStages; ++i) {
       mbar_init(smem_u32(&bars.full[i]), 1u);
       mbar_init(smem_u32(&bars.empty[i]), 1u);
@@ -134,28 +505,30 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     mbar_init(smem_u32(&bars.drain), 1u);
     fence_mbar_init();
-    s_abort = 0;
+    sh.abort = 0;
     prefetch_tmap(&tk);
     prefetch_tmap(&tv);
   }
-  if (warp == kMmaWarp) tmem_alloc(smem_u32(&s_tmem), C::kCols);
+  if (warp == kMmaWarp) tmem_alloc(smem_u32(&sh.tmem), C::kCols);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const uint32_t tmem = s_tmem;
   pdl_wait();
   pdl_trigger();
-  make_plan<kRows>(a, plan);
-  const unsigned long long total = plan.total;
+  make_plan<kRows>(a, sh.plan);
+  const unsigned long long total = sh.plan.total;
   const unsigned ctas = (unsigned)min((unsigned long long)gridDim.x, total);
   JoinItem* join = reinterpret_cast<JoinItem*>(a.ws + (size_t)2 * gridDim.x * C::kSlotFloats);
-  const bool works = blockIdx.x < ctas;
-  const unsigned long long u0 = works ? cut_start(total, ctas, blockIdx.x) : 0ull;
-  const unsigned long long u1 = works ? cut_start(total, ctas, blockIdx.x + 1) : 0ull;
-  const long long limit = a.wait_limit ? a.wait_limit : kWaitLimitCycles;
-  PagedCursor<kRows> c;
-  if (works) {
-    c.seek(a, plan, u0);
+  int units = 0;
+  if (blockIdx.x < ctas) {
+    const unsigned long long u0 = cut_start(total, ctas, blockIdx.x);
+    units = (int)(cut_start(total, ctas, blockIdx.x + 1) - u0);
+    PagedCursor<kRows> c;
+    c.seek(a, sh.plan, u0);
+    if (lane == 0) {
+      sh.at[warp] = c;
+      if (warp < kSoftWarps) sh.next[warp] = c;
+    }
     if (threadIdx.x == 0) {
       // an item cut at this CTA's start is joined later; the first of its cuts speaks for it
       const unsigned long long i0 = u0 - c.blk;
@@ -173,332 +546,21 @@ __global__ void __launch_bounds__(kThreads, 1)
   } else if (threadIdx.x == 0) {
     join[blockIdx.x].valid = 0;
   }
-  auto wait = [&](const unsigned long long& bar, unsigned parity, uint32_t bit) {
-    return mbar_wait_warp(smem_u32(&bar), parity, a.err, &s_abort, bit, limit);
-  };
-  auto next_item = [&](PagedCursor<kRows>& k, unsigned long long& u) {
-    u += share(k, u, u1);
-    if (u < u1) {
-      k.blk = k.k.units - 1;
-      k.next(a, plan);
-    }
-  };
-
-  if (warp == kLoadWarp && works) {
-    // ---- K and V of every unit, in the order of their use: K0 V0 K1 V1 ...
-    const int pages = kUnitKeys >> a.page_log2;        // of a whole unit
-    const int pg = lane / C::kHalves, half = lane % C::kHalves;
-    const uint32_t box = 128u << a.page_log2;          // bytes: page_size rows of 128
-    unsigned n = 0;                                    // stages filled
-    auto entry = [&](const PagedCursor<kRows>& k) {
-      const int key = (k.k.blk0 + k.blk) * kUnitKeys + (pg << a.page_log2);
-      return pg < pages && key < k.k.hi ? page_of(a, k.b, key) : -1;
-    };
-    int page = entry(c);
-    bool ok = true;
-    for (unsigned long long u = u0; u < u1 && ok; ++u) {
-      const int key0 = (c.k.blk0 + c.blk) * kUnitKeys;
-      const int live = max(0, min(c.k.hi, key0 + kUnitKeys) - key0);
-      const int need = (live + (1 << a.page_log2) - 1) >> a.page_log2;
-      const bool mine = pg < need;
-      const int row = mine ? pool_row(a, page_checked(a, page), c.h, 0) : 0;
-      if (u + 1 < u1) {
-        c.next(a, plan);
-        page = entry(c);  // on its way while this unit waits for room
-      }
-#pragma unroll
-      for (int kv = 0; kv < 2; ++kv) {
-        const unsigned st = n % C::kStages;
-        ok = wait(bars.empty[st], ((n / C::kStages) & 1u) ^ 1u, kErrTimeoutEmpty);
-        if (!ok) break;
-        const uint32_t bar = smem_u32(&bars.full[st]);
-        if (lane == 0) mbar_arrive_expect_tx(bar, (uint32_t)(need * C::kHalves) * box);
-        __syncwarp();
-        if (mine)
-          tma_load_2d(ring + st * C::kTile + half * C::kHalf + pg * box, kv ? &tv : &tk, bar, half * 64, row);
-        ++n;
-      }
-    }
-    // after a timeout: wait for the copies in flight into memory that is given back
-    if (*(volatile int*)&s_abort)
-      for (unsigned i = n > (unsigned)C::kStages ? n - C::kStages : 0u; i < n; ++i)
-        mbar_drain(smem_u32(&bars.full[i % C::kStages]), (i / C::kStages) & 1u, limit);
-  } else if (warp == kMmaWarp && works) {
-    // ---- the MMAs
-    const bool leader = elect_one();
-    constexpr uint32_t id_s = idesc_bf16_f32(kTileRows, kUnitKeys);
-    constexpr uint32_t id_o = idesc_bf16_f32(kTileRows, D) | (1u << 16);  // B is MN-major
-    unsigned n = 0, sp[2] = {0, 0}, items[2] = {0, 0};
-    bool ok = true;
-    auto qk = [&](int tile, unsigned st) {
-      if (leader) {
-        const uint32_t qa = sq + tile * C::kTile, ka = ring + st * C::kTile;
-#pragma unroll
-        for (int kk = 0; kk < D / 16; ++kk) {
-          const uint32_t at = (kk >> 2) * C::kHalf + (kk & 3) * 32;
-          mma_ss(tmem + tile * 128, smem_desc_kmajor<64>(qa + at), smem_desc_kmajor<64>(ka + at), id_s, kk > 0);
-        }
-        if (!a.fault) tc_commit(smem_u32(&bars.s[tile]));
-      }
-      __syncwarp();
-    };
-    auto pv = [&](int tile, unsigned st, int steps, bool first, bool last, bool fine) {
-      if (leader) {
-        const uint32_t va = ring + st * C::kTile;
-        for (int kk = 0; kk < steps; ++kk)
-          mma_ts(tmem + C::kO + tile * D, tmem + tile * 128 + kk * 8, smem_desc_mn(va + kk * 2048, C::kHalf), id_o,
-                 !(first && kk == 0));
-        if (fine)
-          for (int kk = 0; kk < steps; ++kk)
-            mma_ts(tmem + C::kO, tmem + 64 + kk * 8, smem_desc_mn(va + kk * 2048, C::kHalf), id_o, 1u);
-        if (last) tc_commit(smem_u32(&bars.o[tile]));
-      }
-      __syncwarp();
-    };
-    auto free_stage = [&](unsigned st) {
-      if (leader) tc_commit(smem_u32(&bars.empty[st]));
-      __syncwarp();
-    };
-    auto full = [&](unsigned i) { return wait(bars.full[i % C::kStages], (i / C::kStages) & 1u, kErrTimeoutFull); };
-    for (unsigned long long u = u0; u < u1 && ok;) {
-      const int count = share(c, u, u1);
-      const bool two = c.n * a.group - c.t * kRows > kTileRows;
-      const int tiles = two ? 2 : 1;
-      for (int i = 0; i < tiles && ok; ++i) ok = wait(bars.q[i], items[i] & 1u, kErrTimeoutFull);
-      unsigned kst = n++;
-      if (!ok || !(ok = full(kst))) break;
-      tc_fence_after();
-      for (int i = 0; i < tiles; ++i) qk(i, kst % C::kStages);
-      free_stage(kst % C::kStages);
-      for (int j = 0; j < count && ok; ++j) {
-        const bool last = j + 1 == count;
-        const unsigned vst = n++;
-        if (!(ok = full(vst))) break;
-        const int key0 = (c.k.blk0 + c.blk + j) * kUnitKeys;
-        const int live = max(0, min(c.k.hi, key0 + kUnitKeys) - key0), steps = (live + 15) >> 4;
-        if (key0 + steps * 16 > c.len) {
-          // values past the sequence's end may be anything, and 0 * NaN is NaN: zero them
-          const int from = max(0, c.len - key0), nz = steps * 16 - from;
-          for (int i = lane; i < nz * C::kHalves * 8; i += 32) {
-            const int r = from + i / (C::kHalves * 8), ch = i % (C::kHalves * 8);
-            sts_u4(ring + (vst % C::kStages) * C::kTile + (ch >> 3) * C::kHalf + r * 128 + (ch & 7) * 16,
-                   make_uint4(0u, 0u, 0u, 0u));
-          }
-          fence_proxy_async_smem();
-          __syncwarp();
-        }
-        for (int i = 0; i < tiles && ok; ++i) {
-          if (j == 0) ok = wait(bars.o_free[i], (items[i] & 1u) ^ 1u, kErrTimeoutAcc);
-          ok = ok && wait(bars.p[i], sp[i] & 1u, kErrTimeoutAcc);
-          if (!ok) break;
-          ++sp[i];
-          tc_fence_after();
-          pv(i, vst % C::kStages, steps, j == 0, last, !two);
-          if (!last && i == 0) {
-            kst = n++;
-            if (!(ok = full(kst))) break;
-            tc_fence_after();
-          }
-          if (i == tiles - 1) free_stage(vst % C::kStages);
-          if (!last) qk(i, kst % C::kStages);
-        }
-        if (ok && !last) free_stage(kst % C::kStages);
-      }
-      for (int i = 0; i < tiles; ++i) ++items[i];
-      next_item(c, u);
-    }
-    if (*(volatile int*)&s_abort) {  // the MMAs issued so far end before tensor memory is given back
-      if (leader) tc_commit(smem_u32(&bars.drain));
-      __syncwarp();
-      mbar_drain(smem_u32(&bars.drain), 0u, limit);
-    }
-  } else if (warp < kSoftWarps && works) {
-    // ---- softmax: a thread per row of a tile
-    const int tile = warp >> 2, r = threadIdx.x & 127;
-    const uint32_t lanes = (uint32_t)(warp & 3) << 21;  // the warp's 32 lanes of tensor memory
-    const uint32_t ts = tmem + lanes + tile * 128, to = tmem + lanes + C::kO + tile * D;
-    const float sl2 = a.scale * 1.4426950408889634f, slack = kSlackLog2 / sl2;
-    auto active = [&](const PagedCursor<kRows>& k) { return k.n * a.group - k.t * kRows > tile * kTileRows; };
-    // the rows of Q of an item, zero past its last row
-    auto load_q = [&](const PagedCursor<kRows>& k) {
-      const int row = k.t * kRows + tile * kTileRows + r;
-      const bool live = row < k.n * a.group;
-      const int tok = live ? row / a.group : 0, head = k.h * a.group + (live ? row % a.group : 0);
-      const __nv_bfloat16* p = a.q + (int64_t)(k.q0 + tok) * a.ld_q + head * D;
-      const uint32_t dst = sq + tile * C::kTile;
-#pragma unroll
-      for (int i = 0; i < D / 8; ++i)
-        cp_async_16(dst + (i >> 3) * C::kHalf + swz_offset<64>(r, i & 7), p + i * 8, live ? 16u : 0u);
-      cp_async_commit();
-    };
-    auto q_ready = [&]() {
-      cp_async_wait<0>();
-      fence_proxy_async_smem();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(smem_u32(&bars.q[tile]));
-    };
-    PagedCursor<kRows> qc = c;  // the next item whose Q is loaded
-    unsigned long long uq = u0, u = u0;
-    auto next_active = [&](PagedCursor<kRows>& k, unsigned long long& at) {
-      do next_item(k, at); while (at < u1 && !active(k));
-    };
-    if (!active(qc)) next_active(qc, uq);
-    c = qc;
-    u = uq;
-    if (uq < u1) {
-      load_q(qc);
-      q_ready();
-    }
-    unsigned sn = 0, items = 0;
-    bool ok = true;
-    while (u < u1 && ok) {
-      const int count = share(c, u, u1);
-      const bool fine = c.n * a.group - c.t * kRows <= kTileRows;  // one tile
-      const int row = c.t * kRows + tile * kTileRows + r;
-      const bool live = row < c.n * a.group;
-      const int tok = live ? row / a.group : 0, head = c.h * a.group + (live ? row % a.group : 0);
-      const int pos = c.len - c.n + tok;
-      // keys [low, lim) that the row sees; a row past the item's last one never asks for masks
-      const int lim = !live ? 0x7FFFFFFF : (a.causal ? min(c.len, pos + 1) : c.len);
-      const int low = live && a.window > 0 ? max(0, pos - a.window + 1) : 0;
-      float m = -INFINITY, l = 0.f;
-      for (int j = 0; j < count; ++j) {
-        const int key0 = (c.k.blk0 + c.blk + j) * kUnitKeys;
-        if (!(ok = wait(bars.s[tile], sn & 1u, kErrTimeoutAcc))) break;
-        ++sn;
-        tc_fence_after();
-        uint32_t s[4][32];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) tmem_ld32_nowait(ts + i * 32, s[i]);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) tmem_wait_ld32(s[i]);
-        if (!__all_sync(0xffffffffu, key0 >= low && key0 + kUnitKeys <= lim)) {
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int k = 0; k < 32; ++k) {
-              const int key = key0 + i * 32 + k;
-              if (key < low || key >= lim) s[i][k] = 0xFF800000u;  // -infinity
-            }
-        }
-        float mx = -INFINITY;
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-          for (int k = 0; k < 32; k += 2)
-            mx = fmaxf(mx, fmaxf(__uint_as_float(s[i][k]), __uint_as_float(s[i][k + 1])));
-        const bool grows = mx > m + slack;
-        if (j == 0) {
-          m = mx;
-        } else if (__any_sync(0xffffffffu, grows)) {
-          // S of this unit is complete, so the product before it is: O stands still
-          const float f = !grows ? 1.f : (m == -INFINITY ? 0.f : ex2((m - mx) * sl2));
-          if (grows) m = mx;
-          l *= f;
-#pragma unroll
-          for (int i = 0; i < D / 32; ++i) {
-            uint32_t o[32];
-            tmem_ld32_nowait(to + i * 32, o);
-            tmem_wait_ld32(o);
-#pragma unroll
-            for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * f);
-            tmem_st32(to + i * 32, o);
-          }
-        }
-        const float nz = m == -INFINITY ? 0.f : -m * sl2;
-        const f2_t sc = f2(sl2, sl2), off = f2(nz, nz);
-        f2_t sum = f2(0.f, 0.f);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          uint32_t p[16];
-#pragma unroll
-          for (int k = 0; k < 16; ++k) {
-            float x, y;
-            f2_split(ffma2(f2(__uint_as_float(s[i][2 * k]), __uint_as_float(s[i][2 * k + 1])), sc, off), x, y);
-            x = ex2(x);
-            y = ex2(y);
-            sum = fadd2(sum, f2(x, y));
-            s[i][2 * k] = __float_as_uint(x);
-            s[i][2 * k + 1] = __float_as_uint(y);
-            asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(p[k]) : "f"(y), "f"(x));
-          }
-          tmem_st16(ts + i * 16, p);  // (columns of scores that are in registers already)
-          if (fine) {
-#pragma unroll
-            for (int k = 0; k < 16; ++k) {
-              const float lo = __uint_as_float(s[i][2 * k]) - __uint_as_float(p[k] << 16);
-              const float up = __uint_as_float(s[i][2 * k + 1]) - __uint_as_float(p[k] & 0xFFFF0000u);
-              asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(p[k]) : "f"(up), "f"(lo));
-            }
-            tmem_st16(ts + 64 + i * 16, p);
-          }
-        }
-        float x, y;
-        f2_split(sum, x, y);
-        l += x + y;
-        tmem_wait_st();
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(smem_u32(&bars.p[tile]));
-      }
-      if (!ok) break;
-      // every product with this item's Q is done: the next item's rows
-      next_active(qc, uq);
-      if (uq < u1) load_q(qc);
-      ok = wait(bars.o[tile], items & 1u, kErrTimeoutAcc);
-      ++items;
-      if (uq < u1) q_ready();
-      if (!ok) break;
-      tc_fence_after();
-      const unsigned long long i0 = u - c.blk;
-      if (c.blk > 0 || count < c.k.units) {
-        // a part of the item: sums, maximum and sum of weights as they are
-        float* slot = a.ws + (size_t)(2 * blockIdx.x + (i0 > u0 ? 1 : 0)) * C::kSlotFloats;
-        const int at = tile * kTileRows + r;
-#pragma unroll
-        for (int i = 0; i < D / 32; ++i) {
-          uint32_t o[32];
-          tmem_ld32_nowait(to + i * 32, o);
-          tmem_wait_ld32(o);
-#pragma unroll
-          for (int k = 0; k < 32; k += 4)
-            *reinterpret_cast<uint4*>(slot + (size_t)((i * 32 + k) / 4 * kRows + at) * 4) =
-                make_uint4(o[k], o[k + 1], o[k + 2], o[k + 3]);
-        }
-        slot[kRows * D + at] = m;
-        slot[kRows * D + kRows + at] = l;
-      } else {
-        const float inv = l > 0.f ? 1.f / l : 0.f;
-        const int64_t at = (int64_t)(c.q0 + tok) * a.heads + head;
-#pragma unroll
-        for (int i = 0; i < D / 32; ++i) {
-          uint32_t o[32];
-          tmem_ld32_nowait(to + i * 32, o);
-          tmem_wait_ld32(o);
-          if (live) {
-#pragma unroll
-            for (int k = 0; k < 32; k += 8) {
-              float f[8];
-#pragma unroll
-              for (int e = 0; e < 8; ++e) f[e] = l > 0.f ? __uint_as_float(o[k + e]) * inv : 0.f;
-              *reinterpret_cast<uint4*>(a.y + at * D + i * 32 + k) = pack8(f);
-            }
-          }
-        }
-        if (live && a.lse) a.lse[at] = l > 0.f ? fmaf(m, a.scale, logf(l)) : -INFINITY;
-      }
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(smem_u32(&bars.o_free[tile]));
-      c = qc;
-      u = uq;
-    }
-    cp_async_wait<0>();
+  __syncwarp();
+  const uint32_t sq = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  const Role r{a, sh, sq, sq + 2 * C::kTile, units, a.wait_limit ? a.wait_limit : kWaitLimitCycles};
+  if (warp < kSoftWarps) {
+    reg_inc<kManyRegs>();
+    if (units > 0) softmax_role<D>(r, sh.tmem);
+  } else {
+    reg_dec<kFewRegs>();
+    if (units > 0 && warp == kMmaWarp) mma_role<D>(r, sh.tmem);
+    if (units > 0 && warp == kLoadWarp) load_role<D>(r, &tk, &tv);
   }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  if (warp == kMmaWarp) tmem_dealloc(tmem, C::kCols);
+  if (warp == kMmaWarp) tmem_dealloc(sh.tmem, C::kCols);
 }
 
 // Joins the parts of the items that several CTAs shared, in the order of their keys:
