@@ -370,12 +370,18 @@ __device__ __forceinline__ void softmax_role(const Role& r, uint32_t tmem) {
           for (int k = 0; k < 32; ++k)
             if (i * 32 + k < from || i * 32 + k >= to_) s[i][k] = 0xFF800000u;  // -infinity
       }
-      float mx = -INFINITY;
+      // (several maxima and sums side by side: one chain of 64 steps each is as long as all
+      // of the row's exponentials)
+      float mx4[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
+      for (int i = 0; i < 4; ++i) {
+        mx4[i] = __uint_as_float(s[i][0]);
 #pragma unroll
-        for (int k = 0; k < 32; k += 2)
-          mx = fmaxf(mx, fmaxf(__uint_as_float(s[i][k]), __uint_as_float(s[i][k + 1])));
+        for (int k = 1; k < 31; k += 2)
+          mx4[i] = fmaxf(mx4[i], fmaxf(__uint_as_float(s[i][k]), __uint_as_float(s[i][k + 1])));
+        mx4[i] = fmaxf(mx4[i], __uint_as_float(s[i][31]));
+      }
+      const float mx = fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3]));
       const bool grows = mx > m + slack;
       if (j == 0) {
         m = mx;
@@ -396,34 +402,40 @@ __device__ __forceinline__ void softmax_role(const Role& r, uint32_t tmem) {
       }
       const float nz = m == -INFINITY ? 0.f : -m * sl2;
       const f2_t sc = f2(sl2, sl2), off = f2(nz, nz);
-      f2_t sum = f2(0.f, 0.f);
+      f2_t sum[4];
+      auto weigh = [&](auto two_parts) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        uint32_t p[16];
-#pragma unroll
-        for (int k = 0; k < 16; ++k) {
-          float x, y;
-          f2_split(ffma2(f2(__uint_as_float(s[i][2 * k]), __uint_as_float(s[i][2 * k + 1])), sc, off), x, y);
-          x = ex2(x);
-          y = ex2(y);
-          sum = fadd2(sum, f2(x, y));
-          s[i][2 * k] = __float_as_uint(x);
-          s[i][2 * k + 1] = __float_as_uint(y);
-          asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(p[k]) : "f"(y), "f"(x));
-        }
-        tmem_st16(ts + i * 16, p);  // (columns of scores that are in registers already)
-        if (fine) {
+        for (int i = 0; i < 4; ++i) {
+          uint32_t p[16];
 #pragma unroll
           for (int k = 0; k < 16; ++k) {
-            const float lo = __uint_as_float(s[i][2 * k]) - __uint_as_float(p[k] << 16);
-            const float up = __uint_as_float(s[i][2 * k + 1]) - __uint_as_float(p[k] & 0xFFFF0000u);
-            asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(p[k]) : "f"(up), "f"(lo));
+            float x, y;
+            f2_split(ffma2(f2(__uint_as_float(s[i][2 * k]), __uint_as_float(s[i][2 * k + 1])), sc, off), x, y);
+            x = ex2(x);
+            y = ex2(y);
+            sum[k & 3] = i == 0 && k < 4 ? f2(x, y) : fadd2(sum[k & 3], f2(x, y));
+            s[i][2 * k] = __float_as_uint(x);
+            s[i][2 * k + 1] = __float_as_uint(y);
+            asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(p[k]) : "f"(y), "f"(x));
           }
-          tmem_st16(ts + 64 + i * 16, p);
+          tmem_st16(ts + i * 16, p);  // (columns of scores that are in registers already)
+          if constexpr (decltype(two_parts)::value) {
+#pragma unroll
+            for (int k = 0; k < 16; ++k) {
+              const float lo = __uint_as_float(s[i][2 * k]) - __uint_as_float(p[k] << 16);
+              const float up = __uint_as_float(s[i][2 * k + 1]) - __uint_as_float(p[k] & 0xFFFF0000u);
+              asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(p[k]) : "f"(up), "f"(lo));
+            }
+            tmem_st16(ts + 64 + i * 16, p);
+          }
         }
-      }
+      };
+      if (fine)
+        weigh(BoolConst<true>());
+      else
+        weigh(BoolConst<false>());
       float x, y;
-      f2_split(sum, x, y);
+      f2_split(fadd2(fadd2(sum[0], sum[1]), fadd2(sum[2], sum[3])), x, y);
       l += x + y;
       tmem_wait_st();
       tc_fence_before();
