@@ -1479,6 +1479,11 @@ sparoa_status sparoa_paged_attention(sparoa_ctx* ctx, const void* q, int64_t ld_
     a.heads = heads;
     a.kv_heads = cache->kv_heads;
     a.group = heads / cache->kv_heads;
+    if (a.group > 1) {
+      const int s = log2_of(a.group);  // 2^s >= group
+      a.group_mul = (uint32_t)(((uint64_t)1 << (31 + s)) / a.group + 1);
+      a.group_shift = (uint32_t)(s - 1);
+    }
     a.D = (int)D;
     a.scale = scale;
     a.causal = causal != 0;

@@ -35,6 +35,8 @@ constexpr int kSoftWarps = 8;
 constexpr int kMmaWarp = 8, kLoadWarp = 9;
 constexpr int kThreads = 384;  // 12 warps: the last two only fill the third group of four
 constexpr float kSlackLog2 = 8.f;
+constexpr int kExtra = 2;      // an item's beginning and end, in units
+using Cursor = PagedCursor<kRows, kExtra>;
 
 template <int D>
 struct Cfg {
@@ -112,15 +114,16 @@ __device__ __forceinline__ void reg_dec() {
 struct Bars {
   unsigned long long full[8], empty[8];      // ring
   unsigned long long s[2], p[2], q[2], o[2], o_free[2];  // per tile
-  unsigned long long drain;
+  unsigned long long joined, drain;
 };
 
 // What the roles of a CTA share.
 struct Shared {
   PagedPlan plan;
   Bars bars;
-  PagedCursor<kRows> at[12];    // a warp's place, in memory: the softmax threads need their registers
-  PagedCursor<kRows> next[8];   // the softmax warps': the item whose Q is loaded next
+  Cursor start;
+  Cursor at[12], next[8];  // a warp's item, and the softmax warps' next one: in memory, their registers hold scores
+  float m[kTileRows], l[kTileRows];  // an item of one tile: the second group's statistics
   uint32_t tmem;
   int abort;
 };
@@ -129,54 +132,50 @@ struct Role {
   const PagedArgs& a;
   Shared& sh;
   uint32_t sq, ring;   // Q tiles, K and V stages
-  int units;           // of this CTA
   long long limit;
 
   __device__ __forceinline__ bool wait(unsigned long long& bar, unsigned parity, uint32_t bit) const {
     return mbar_wait_warp(smem_u32(&bar), parity, a.err, &sh.abort, bit, limit);
   }
   __device__ __forceinline__ bool aborted() const { return *(volatile int*)&sh.abort != 0; }
-  // units of the place's item that are this CTA's, with `left` units to go
-  static __device__ __forceinline__ int share(const PagedCursor<kRows>& c, int left) { return min(left, c.k.units - c.blk); }
-  // to the next item's first unit (a converged warp; left > 0 afterwards, or c stays)
-  __device__ __forceinline__ void next_item(PagedCursor<kRows>& c, int& left) const {
-    left -= share(c, left);
+  __device__ __forceinline__ int rows(const Cursor& c) const { return c.n * a.group - c.t * kRows; }
+  // dst = the item after c (a converged warp; both in shared memory)
+  __device__ __forceinline__ void next_item(Cursor& dst, const Cursor& c) const {
     __syncwarp();
-    if (left > 0 && (threadIdx.x & 31) == 0) {
-      c.blk = c.k.units - 1;
-      c.next(a, sh.plan);
+    if ((threadIdx.x & 31) == 0) {
+      Cursor k = c;
+      k.next_item(a, sh.plan);
+      dst = k;
     }
     __syncwarp();
   }
 };
 
-// K and V of every unit, in the order of their use: K0 V0 K1 V1 ...
+// K and V of every unit: K0 V0 K1 V1 ...
 template <int D>
 __device__ __forceinline__ void load_role(const Role& r, const CUtensorMap* tk, const CUtensorMap* tv) {
   using C = Cfg<D>;
   const PagedArgs& a = r.a;
   const int lane = threadIdx.x & 31;
-  PagedCursor<kRows> c = r.sh.at[threadIdx.x >> 5];
+  Cursor c = r.sh.start;
   const int pages = kUnitKeys >> a.page_log2;        // of a whole unit
   const int pg = lane / C::kHalves, half = lane % C::kHalves;
   const uint32_t box = 128u << a.page_log2;          // bytes: page_size rows of 128
   unsigned n = 0;                                    // stages filled
   auto entry = [&]() {
-    const int key = (c.k.blk0 + c.blk) * kUnitKeys + (pg << a.page_log2);
-    return pg < pages && key < c.k.hi ? page_of(a, c.b, key) : -1;
+    const int key = c.key0() + (pg << a.page_log2);
+    return !c.done() && pg < pages && key < c.k.hi ? page_of(a, c.b, key) : -1;
   };
   int page = entry();
   bool ok = true;
-  for (int left = r.units; left > 0 && ok; --left) {
-    const int key0 = (c.k.blk0 + c.blk) * kUnitKeys;
+  while (!c.done() && ok) {
+    const int key0 = c.key0();
     const int live = max(0, min(c.k.hi, key0 + kUnitKeys) - key0);
     const int need = (live + (1 << a.page_log2) - 1) >> a.page_log2;
     const bool mine = pg < need;
     const int row = mine ? pool_row(a, page_checked(a, page), c.h, 0) : 0;
-    if (left > 1) {
-      c.next(a, r.sh.plan);
-      page = entry();  // on its way while this unit waits for room
-    }
+    c.next(a, r.sh.plan);
+    page = entry();  // on its way while this unit waits for room
 #pragma unroll
     for (int kv = 0; kv < 2; ++kv) {
       const unsigned st = n % C::kStages;
@@ -202,28 +201,44 @@ __device__ __forceinline__ void mma_role(const Role& r, uint32_t tmem) {
   const PagedArgs& a = r.a;
   Bars& bars = r.sh.bars;
   const int lane = threadIdx.x & 31;
-  PagedCursor<kRows>& c = r.sh.at[threadIdx.x >> 5];
+  Cursor& c = r.sh.at[threadIdx.x >> 5];
   const bool leader = elect_one();
   constexpr uint32_t id_s = idesc_bf16_f32(kTileRows, kUnitKeys);
   constexpr uint32_t id_o = idesc_bf16_f32(kTileRows, D) | (1u << 16);  // B is MN-major
-  unsigned n = 0, sp[2] = {0, 0}, items[2] = {0, 0};
+  unsigned base = 0, sp[2] = {0, 0}, qs[2] = {0, 0}, os[2] = {0, 0};
   bool ok = true;
-  auto qk = [&](int tile, unsigned st) {
+  // stages of unit j of the item: K 2 j, V 2 j + 1 from base
+  auto full = [&](unsigned i) {
+    ok = ok && r.wait(bars.full[(base + i) % C::kStages], ((base + i) / C::kStages) & 1u, kErrTimeoutFull);
+    return ok;
+  };
+  auto free_stage = [&](unsigned i) {
+    if (leader) tc_commit(smem_u32(&bars.empty[(base + i) % C::kStages]));
+    __syncwarp();
+  };
+  auto qk = [&](int slot, int tile, unsigned i) {  // S of `slot` from the Q of `tile`
+    tc_fence_after();
     if (leader) {
-      const uint64_t qd = smem_desc_kmajor<64>(r.sq + tile * C::kTile), kd = smem_desc_kmajor<64>(r.ring + st * C::kTile);
+      const uint64_t qd = smem_desc_kmajor<64>(r.sq + tile * C::kTile);
+      const uint64_t kd = smem_desc_kmajor<64>(r.ring + ((base + i) % C::kStages) * C::kTile);
 #pragma unroll
       for (int kk = 0; kk < D / 16; ++kk) {
         const uint32_t at = ((kk >> 2) * C::kHalf + (kk & 3) * 32) >> 4;
-        mma_ss(tmem + tile * 128, qd + at, kd + at, id_s, kk > 0);
+        mma_ss(tmem + slot * 128, qd + at, kd + at, id_s, kk > 0);
       }
-      if (!a.fault) tc_commit(smem_u32(&bars.s[tile]));
+      if (!a.fault) tc_commit(smem_u32(&bars.s[slot]));
     }
     __syncwarp();
   };
-  auto pv = [&](int tile, unsigned st, int steps, bool first, bool last, bool fine) {
+  // O of `slot` += P V; fine: P has two parts
+  auto pv = [&](int slot, unsigned i, int steps, bool first, bool last, bool fine) {
+    if (first) ok = ok && r.wait(bars.o_free[slot], (os[slot]++ & 1u) ^ 1u, kErrTimeoutAcc);
+    ok = ok && r.wait(bars.p[slot], sp[slot]++ & 1u, kErrTimeoutAcc);
+    if (!ok) return;
+    tc_fence_after();
     if (leader) {
-      const uint64_t vd = smem_desc_mn(r.ring + st * C::kTile, C::kHalf);
-      const uint32_t d = tmem + C::kO + tile * D, p = tmem + tile * 128;
+      const uint64_t vd = smem_desc_mn(r.ring + ((base + i) % C::kStages) * C::kTile, C::kHalf);
+      const uint32_t d = tmem + C::kO + slot * D, p = tmem + slot * 128;
       if (steps == 8) {
 #pragma unroll
         for (int kk = 0; kk < 8; ++kk) mma_ts(d, p + kk * 8, vd + kk * 128, id_o, !(first && kk == 0));
@@ -232,61 +247,76 @@ __device__ __forceinline__ void mma_role(const Role& r, uint32_t tmem) {
       }
       if (fine)
         for (int kk = 0; kk < steps; ++kk) mma_ts(d, p + 64 + kk * 8, vd + kk * 128, id_o, 1u);
-      if (last) tc_commit(smem_u32(&bars.o[tile]));
+      if (last) tc_commit(smem_u32(&bars.o[slot]));
     }
     __syncwarp();
   };
-  auto free_stage = [&](unsigned st) {
-    if (leader) tc_commit(smem_u32(&bars.empty[st]));
-    __syncwarp();
-  };
-  auto full = [&](unsigned i) { return r.wait(bars.full[i % C::kStages], (i / C::kStages) & 1u, kErrTimeoutFull); };
-  for (int left = r.units; left > 0 && ok;) {
-    const int count = Role::share(c, left), first_key = (c.k.blk0 + c.blk) * kUnitKeys, hi = c.k.hi, len = c.len;
-    const bool two = c.n * a.group - c.t * kRows > kTileRows;
-    const int tiles = two ? 2 : 1;
-    for (int i = 0; i < tiles && ok; ++i) ok = r.wait(bars.q[i], items[i] & 1u, kErrTimeoutFull);
-    unsigned kst = n++;
-    if (!ok || !(ok = full(kst))) break;
-    tc_fence_after();
-    for (int i = 0; i < tiles; ++i) qk(i, kst % C::kStages);
-    free_stage(kst % C::kStages);
-    for (int j = 0; j < count && ok; ++j) {
-      const bool last = j + 1 == count;
-      const unsigned vst = n++;
-      if (!(ok = full(vst))) break;
-      const int key0 = first_key + j * kUnitKeys;
-      const int steps = (max(0, min(hi, key0 + kUnitKeys) - key0) + 15) >> 4;
+  while (!c.done() && ok) {
+    const int count = c.end - c.first, first_key = c.key0(), hi = c.k.hi, len = c.len;
+    const bool two = r.rows(c) > kTileRows;
+    // k-steps of unit j, whose values are in stage i
+    auto steps_of = [&](int j, unsigned i) {
+      const int key0 = first_key + j * kUnitKeys, steps = (max(0, min(hi, key0 + kUnitKeys) - key0) + 15) >> 4;
       if (key0 + steps * 16 > len) {
         // values past the sequence's end may be anything, and 0 * NaN is NaN: zero them
         const int from = max(0, len - key0), nz = steps * 16 - from;
-        for (int i = lane; i < nz * C::kHalves * 8; i += 32) {
-          const int row = from + i / (C::kHalves * 8), ch = i % (C::kHalves * 8);
-          sts_u4(r.ring + (vst % C::kStages) * C::kTile + (ch >> 3) * C::kHalf + row * 128 + (ch & 7) * 16,
+        for (int e = lane; e < nz * C::kHalves * 8; e += 32) {
+          const int row = from + e / (C::kHalves * 8), ch = e % (C::kHalves * 8);
+          sts_u4(r.ring + ((base + i) % C::kStages) * C::kTile + (ch >> 3) * C::kHalf + row * 128 + (ch & 7) * 16,
                  make_uint4(0u, 0u, 0u, 0u));
         }
         fence_proxy_async_smem();
         __syncwarp();
       }
-      for (int i = 0; i < tiles; ++i) {
-        if (j == 0) ok = r.wait(bars.o_free[i], (items[i] & 1u) ^ 1u, kErrTimeoutAcc);
-        ok = ok && r.wait(bars.p[i], sp[i] & 1u, kErrTimeoutAcc);
+      return steps;
+    };
+    ok = r.wait(bars.q[0], qs[0]++ & 1u, kErrTimeoutFull);
+    if (two) ok = ok && r.wait(bars.q[1], qs[1]++ & 1u, kErrTimeoutFull);
+    if (!ok || !full(0)) break;
+    qk(0, 0, 0);
+    if (two) {
+      // two tiles: both take every unit
+      qk(1, 1, 0);
+      free_stage(0);
+      for (int j = 0; j < count && full(2 * j + 1); ++j) {
+        const bool last = j + 1 == count;
+        const int steps = steps_of(j, 2 * j + 1);
+        pv(0, 2 * j + 1, steps, j == 0, last, false);
         if (!ok) break;
-        ++sp[i];
-        tc_fence_after();
-        pv(i, vst % C::kStages, steps, j == 0, last, !two);
-        if (!last && i == 0) {
-          kst = n++;
-          if (!(ok = full(kst))) break;
-          tc_fence_after();
+        if (!last) {
+          if (!full(2 * j + 2)) break;
+          qk(0, 0, 2 * j + 2);
         }
-        if (i == tiles - 1) free_stage(vst % C::kStages);
-        if (!last) qk(i, kst % C::kStages);
+        pv(1, 2 * j + 1, steps, j == 0, last, false);
+        if (!ok) break;
+        free_stage(2 * j + 1);
+        if (!last) {
+          qk(1, 1, 2 * j + 2);
+          free_stage(2 * j + 2);
+        }
       }
-      if (ok && !last) free_stage(kst % C::kStages);
+    } else {
+      // one tile: the units take turns
+      free_stage(0);
+      if (count > 1) {
+        if (!full(2)) break;
+        qk(1, 0, 2);
+        free_stage(2);
+      }
+      for (int j = 0; j < count && full(2 * j + 1); ++j) {
+        const int steps = steps_of(j, 2 * j + 1);
+        pv(j & 1, 2 * j + 1, steps, j < 2, j + 2 >= count, true);
+        if (!ok) break;
+        free_stage(2 * j + 1);
+        if (j + 2 < count) {
+          if (!full(2 * j + 4)) break;
+          qk(j & 1, 0, 2 * j + 4);
+          free_stage(2 * j + 4);
+        }
+      }
     }
-    for (int i = 0; i < tiles; ++i) ++items[i];
-    r.next_item(c, left);
+    base += 2 * count;
+    r.next_item(c, c);
   }
   if (r.aborted()) {  // the MMAs issued so far end before tensor memory is given back
     if (leader) tc_commit(smem_u32(&bars.drain));
@@ -301,195 +331,225 @@ __device__ __forceinline__ void softmax_role(const Role& r, uint32_t tmem) {
   using C = Cfg<D>;
   const PagedArgs& a = r.a;
   Bars& bars = r.sh.bars;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, tile = warp >> 2, row = threadIdx.x & 127;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, grp = warp >> 2, row = threadIdx.x & 127;
   const uint32_t lanes = (uint32_t)(warp & 3) << 21;  // the warp's 32 lanes of tensor memory
-  const uint32_t ts = tmem + lanes + tile * 128, to = tmem + lanes + C::kO + tile * D;
+  const uint32_t ts = tmem + lanes + grp * 128, to = tmem + lanes + C::kO + grp * D;
   const float sl2 = a.scale * 1.4426950408889634f, slack = kSlackLog2 / sl2;
-  PagedCursor<kRows>& c = r.sh.at[warp];
-  PagedCursor<kRows>& qc = r.sh.next[warp];
-  auto rows_of = [&](const PagedCursor<kRows>& k) { return k.n * a.group - k.t * kRows - tile * kTileRows; };
-  auto next_active = [&](PagedCursor<kRows>& k, int& left) {
-    do r.next_item(k, left); while (left > 0 && rows_of(k) <= 0);
-  };
-  // the rows of Q of an item, zero past its last row
-  auto load_q = [&]() {
-    const bool live = row < rows_of(qc);
-    const int at = live ? qc.t * kRows + tile * kTileRows + row : 0, tok = at / a.group, head = qc.h * a.group + at % a.group;
-    const __nv_bfloat16* p = a.q + (int64_t)(qc.q0 + tok) * a.ld_q + head * D;
-    const uint32_t dst = r.sq + tile * C::kTile;
+  Cursor& c = r.sh.at[warp];
+  Cursor& nx = r.sh.next[warp];
+  // this group's tile of Q of an item, if it has one: rows past the item's last are zero
+  auto load_q = [&](const Cursor& k) {
+    const int rows = r.rows(k) - grp * kTileRows;
+    if (k.done() || rows <= 0) return false;
+    const bool live = row < rows;
+    const int at = live ? k.t * kRows + grp * kTileRows + row : 0, tok = over_group(a, at);
+    const __nv_bfloat16* p = a.q + (int64_t)(k.q0 + tok) * a.ld_q + (k.h * a.group + at - tok * a.group) * D;
+    const uint32_t dst = r.sq + grp * C::kTile;
 #pragma unroll
     for (int i = 0; i < D / 8; ++i)
       cp_async_16(dst + (i >> 3) * C::kHalf + swz_offset<64>(row, i & 7), p + i * 8, live ? 16u : 0u);
     cp_async_commit();
+    return true;
   };
   auto q_ready = [&]() {
     cp_async_wait<0>();
     fence_proxy_async_smem();
     __syncwarp();
-    if (lane == 0) mbar_arrive(smem_u32(&bars.q[tile]));
+    if (lane == 0) mbar_arrive(smem_u32(&bars.q[grp]));
   };
-  int left = r.units, qleft = r.units;
-  if (rows_of(c) <= 0) {
-    next_active(c, left);
-    next_active(qc, qleft);
-  }
-  if (left > 0) {
-    load_q();
-    q_ready();
-  }
-  unsigned sn = 0, items = 0;
-  bool ok = true;
-  while (left > 0) {
-    const int count = Role::share(c, left), first_key = (c.k.blk0 + c.blk) * kUnitKeys;
-    const int rows = rows_of(c);
-    const bool fine = tile == 0 && rows <= kTileRows;  // an item of one tile
-    const bool live = row < rows;
+  if (load_q(c)) q_ready();
+  unsigned sn = 0, on = 0, joins = 0;
+  bool ok = true, second = false;  // second: not this CTA's first item
+  for (; !c.done(); second = true) {
+    r.next_item(nx, c);
+    const int rows = r.rows(c), count = c.end - c.first;
+    const bool two = rows > kTileRows;
+    // the group's rows and units: its own tile and all units, or the tile and every other unit
+    const int r0 = two ? grp * kTileRows : 0, j0 = two ? 0 : grp, dj = two ? 1 : 2;
+    const bool live = r0 + row < rows;
+    const bool idle = r0 + (warp & 3) * 32 >= rows;  // no row of the warp is the item's
+    const bool works = j0 < count;
     // keys [low, lim) that the row sees; a row past the item's last one never asks for masks
     int lim = 0x7FFFFFFF, low = 0;
     if (live) {
-      const int pos = c.len - c.n + (c.t * kRows + tile * kTileRows + row) / a.group;
-      lim = a.causal ? min(c.len, pos + 1) : c.len;
-      low = a.window > 0 ? max(0, pos - a.window + 1) : 0;
+      const int p = c.len - c.n + over_group(a, c.t * kRows + r0 + row);
+      lim = a.causal ? min(c.len, p + 1) : c.len;
+      low = a.window > 0 ? max(0, p - a.window + 1) : 0;
     }
+    const int first_key = c.key0();
+    bool loading = false;
+    if (!works) loading = load_q(nx);
     float m = -INFINITY, l = 0.f;
-    for (int j = 0; j < count; ++j) {
+    for (int j = j0; j < count; j += dj) {
       const int key0 = first_key + j * kUnitKeys;
-      if (!(ok = r.wait(bars.s[tile], sn & 1u, kErrTimeoutAcc))) break;
+      if (!(ok = r.wait(bars.s[grp], sn & 1u, kErrTimeoutAcc))) break;
       ++sn;
+      // every product with this group's tile of Q is done: the next item's rows (the other
+      // group may have the last unit of an item of one tile)
+      if (j + dj >= count && (two || grp == 1 || j + 1 == count)) loading = load_q(nx);
       tc_fence_after();
-      uint32_t s[4][32];
+      if (!idle) {
+        uint32_t s[4][32];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) tmem_ld32_nowait(ts + i * 32, s[i]);
+        for (int i = 0; i < 4; ++i) tmem_ld32_nowait(ts + i * 32, s[i]);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) tmem_wait_ld32(s[i]);
-      if (!__all_sync(0xffffffffu, key0 >= low && key0 + kUnitKeys <= lim)) {
-        const int from = low - key0, to_ = lim - key0;
+        for (int i = 0; i < 4; ++i) tmem_wait_ld32(s[i]);
+        if (!__all_sync(0xffffffffu, key0 >= low && key0 + kUnitKeys <= lim)) {
+          const int from = low - key0, to_ = lim - key0;
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+          for (int i = 0; i < 4; ++i)
 #pragma unroll
-          for (int k = 0; k < 32; ++k)
-            if (i * 32 + k < from || i * 32 + k >= to_) s[i][k] = 0xFF800000u;  // -infinity
+            for (int k = 0; k < 32; ++k)
+              if (i * 32 + k < from || i * 32 + k >= to_) s[i][k] = 0xFF800000u;  // -infinity
+        }
+        // (several maxima and sums side by side: one chain of 64 steps each is as long as all
+        // of the row's exponentials)
+        float mx4[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          mx4[i] = __uint_as_float(s[i][0]);
+#pragma unroll
+          for (int k = 1; k < 31; k += 2)
+            mx4[i] = fmaxf(mx4[i], fmaxf(__uint_as_float(s[i][k]), __uint_as_float(s[i][k + 1])));
+          mx4[i] = fmaxf(mx4[i], __uint_as_float(s[i][31]));
+        }
+        const float mx = fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3]));
+        const bool grows = mx > m + slack;
+        if (j == j0) {
+          m = mx;
+        } else if (__any_sync(0xffffffffu, grows)) {
+          // S of this unit is complete, so the product before it is: O stands still
+          const float f = !grows ? 1.f : (m == -INFINITY ? 0.f : ex2((m - mx) * sl2));
+          if (grows) m = mx;
+          l *= f;
+#pragma unroll 1
+          for (int i = 0; i < D / 16; ++i) {
+            float o[16];
+            uint32_t q[16];
+            tmem_ld16(to + i * 16, o);
+#pragma unroll
+            for (int k = 0; k < 16; ++k) q[k] = __float_as_uint(o[k] * f);
+            tmem_st16(to + i * 16, q);
+          }
+        }
+        const float nz = m == -INFINITY ? 0.f : -m * sl2;
+        const f2_t sc = f2(sl2, sl2), off = f2(nz, nz);
+        f2_t sum[4];
+        auto weigh = [&](auto two_parts) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            uint32_t p[16];
+#pragma unroll
+            for (int k = 0; k < 16; ++k) {
+              float x, y;
+              f2_split(ffma2(f2(__uint_as_float(s[i][2 * k]), __uint_as_float(s[i][2 * k + 1])), sc, off), x, y);
+              x = ex2(x);
+              y = ex2(y);
+              sum[k & 3] = i == 0 && k < 4 ? f2(x, y) : fadd2(sum[k & 3], f2(x, y));
+              s[i][2 * k] = __float_as_uint(x);
+              s[i][2 * k + 1] = __float_as_uint(y);
+              asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(p[k]) : "f"(y), "f"(x));
+            }
+            tmem_st16(ts + i * 16, p);  // (columns of scores that are in registers already)
+            if constexpr (decltype(two_parts)::value) {
+#pragma unroll
+              for (int k = 0; k < 16; ++k) {
+                const float lo = __uint_as_float(s[i][2 * k]) - __uint_as_float(p[k] << 16);
+                const float up = __uint_as_float(s[i][2 * k + 1]) - __uint_as_float(p[k] & 0xFFFF0000u);
+                asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(p[k]) : "f"(up), "f"(lo));
+              }
+              tmem_st16(ts + 64 + i * 16, p);
+            }
+          }
+        };
+        if (two)
+          weigh(BoolConst<false>());
+        else
+          weigh(BoolConst<true>());
+        float x, y;
+        f2_split(fadd2(fadd2(sum[0], sum[1]), fadd2(sum[2], sum[3])), x, y);
+        l += x + y;
+        tmem_wait_st();
       }
-      // (several maxima and sums side by side: one chain of 64 steps each is as long as all
-      // of the row's exponentials)
-      float mx4[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        mx4[i] = __uint_as_float(s[i][0]);
-#pragma unroll
-        for (int k = 1; k < 31; k += 2)
-          mx4[i] = fmaxf(mx4[i], fmaxf(__uint_as_float(s[i][k]), __uint_as_float(s[i][k + 1])));
-        mx4[i] = fmaxf(mx4[i], __uint_as_float(s[i][31]));
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&bars.p[grp]));
+    }
+    if (loading) q_ready();
+    if (works) ok = ok && r.wait(bars.o[grp], on++ & 1u, kErrTimeoutAcc);
+    if (!ok) break;
+    tc_fence_after();
+    const bool halves = !two && count > 1;  // two sums over every other unit
+    if (halves && grp == 1) {
+      // the first group adds this one's sums to its own
+      r.sh.m[row] = m;
+      r.sh.l[row] = l;
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&bars.joined));
+    } else if (works) {
+      float f0 = 1.f, f1 = 0.f;
+      loading = false;
+      if (halves) {
+        if (!(ok = r.wait(bars.joined, joins++ & 1u, kErrTimeoutAcc))) break;
+        tc_fence_after();
+        if (count % 2 == 0) loading = load_q(nx);
+        const float m1 = r.sh.m[row], l1 = r.sh.l[row], top = fmaxf(m, m1);
+        f0 = m == -INFINITY ? 0.f : ex2((m - top) * sl2);
+        f1 = m1 == -INFINITY ? 0.f : ex2((m1 - top) * sl2);
+        l = l * f0 + l1 * f1;
+        m = top;
       }
-      const float mx = fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3]));
-      const bool grows = mx > m + slack;
-      if (j == 0) {
-        m = mx;
-      } else if (__any_sync(0xffffffffu, grows)) {
-        // S of this unit is complete, so the product before it is: O stands still
-        const float f = !grows ? 1.f : (m == -INFINITY ? 0.f : ex2((m - mx) * sl2));
-        if (grows) m = mx;
-        l *= f;
+      const bool part = c.cut();
+      float* slot = a.ws + (size_t)(2 * blockIdx.x + (second ? 1 : 0)) * C::kSlotFloats;
+      const int at = r0 + row, of = live ? over_group(a, c.t * kRows + at) : 0;
+      const int64_t out = (int64_t)(c.q0 + of) * a.heads + c.h * a.group + (live ? c.t * kRows + at - of * a.group : 0);
+      const float inv = l > 0.f ? 1.f / l : 0.f;
+      if (!idle) {
 #pragma unroll 1
         for (int i = 0; i < D / 16; ++i) {
           float o[16];
-          uint32_t q[16];
           tmem_ld16(to + i * 16, o);
+          if (halves) {
+            float e[16];
+            tmem_ld16(to + D + i * 16, e);
 #pragma unroll
-          for (int k = 0; k < 16; ++k) q[k] = __float_as_uint(o[k] * f);
-          tmem_st16(to + i * 16, q);
+            for (int k = 0; k < 16; ++k) o[k] = o[k] * f0 + e[k] * f1;
+          }
+          if (!live) continue;
+          if (part) {
+            // a part of the item: sums, maximum and sum of weights as they are
+#pragma unroll
+            for (int k = 0; k < 16; k += 4)
+              *reinterpret_cast<float4*>(slot + (size_t)((i * 16 + k) / 4 * kRows + at) * 4) =
+                  make_float4(o[k], o[k + 1], o[k + 2], o[k + 3]);
+          } else {
+#pragma unroll
+            for (int k = 0; k < 16; k += 8) {
+              float f[8];
+#pragma unroll
+              for (int e = 0; e < 8; ++e) f[e] = l > 0.f ? o[k + e] * inv : 0.f;
+              *reinterpret_cast<uint4*>(a.y + out * D + i * 16 + k) = pack8(f);
+            }
+          }
+        }
+        if (part) {
+          slot[kRows * D + at] = m;
+          slot[kRows * D + kRows + at] = l;
+        } else if (live && a.lse) {
+          a.lse[out] = l > 0.f ? fmaf(m, a.scale, logf(l)) : -INFINITY;
         }
       }
-      const float nz = m == -INFINITY ? 0.f : -m * sl2;
-      const f2_t sc = f2(sl2, sl2), off = f2(nz, nz);
-      f2_t sum[4];
-      auto weigh = [&](auto two_parts) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          uint32_t p[16];
-#pragma unroll
-          for (int k = 0; k < 16; ++k) {
-            float x, y;
-            f2_split(ffma2(f2(__uint_as_float(s[i][2 * k]), __uint_as_float(s[i][2 * k + 1])), sc, off), x, y);
-            x = ex2(x);
-            y = ex2(y);
-            sum[k & 3] = i == 0 && k < 4 ? f2(x, y) : fadd2(sum[k & 3], f2(x, y));
-            s[i][2 * k] = __float_as_uint(x);
-            s[i][2 * k + 1] = __float_as_uint(y);
-            asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(p[k]) : "f"(y), "f"(x));
-          }
-          tmem_st16(ts + i * 16, p);  // (columns of scores that are in registers already)
-          if constexpr (decltype(two_parts)::value) {
-#pragma unroll
-            for (int k = 0; k < 16; ++k) {
-              const float lo = __uint_as_float(s[i][2 * k]) - __uint_as_float(p[k] << 16);
-              const float up = __uint_as_float(s[i][2 * k + 1]) - __uint_as_float(p[k] & 0xFFFF0000u);
-              asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(p[k]) : "f"(up), "f"(lo));
-            }
-            tmem_st16(ts + 64 + i * 16, p);
-          }
-        }
-      };
-      if (fine)
-        weigh(BoolConst<true>());
-      else
-        weigh(BoolConst<false>());
-      float x, y;
-      f2_split(fadd2(fadd2(sum[0], sum[1]), fadd2(sum[2], sum[3])), x, y);
-      l += x + y;
-      tmem_wait_st();
+      if (loading) q_ready();
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive(smem_u32(&bars.p[tile]));
-    }
-    if (!ok) break;
-    // every product with this item's Q is done: the next item's rows
-    next_active(qc, qleft);
-    if (qleft > 0) load_q();
-    ok = r.wait(bars.o[tile], items & 1u, kErrTimeoutAcc);
-    ++items;
-    if (qleft > 0) q_ready();
-    if (!ok) break;
-    tc_fence_after();
-    if (c.blk > 0 || count < c.k.units) {
-      // a part of the item: sums, maximum and sum of weights as they are
-      float* slot = a.ws + (size_t)(2 * blockIdx.x + (left < r.units ? 1 : 0)) * C::kSlotFloats;
-      const int at = tile * kTileRows + row;
-#pragma unroll 1
-      for (int i = 0; i < D / 16; ++i) {
-        float o[16];
-        tmem_ld16(to + i * 16, o);
-#pragma unroll
-        for (int k = 0; k < 16; k += 4)
-          *reinterpret_cast<float4*>(slot + (size_t)((i * 16 + k) / 4 * kRows + at) * 4) =
-              make_float4(o[k], o[k + 1], o[k + 2], o[k + 3]);
+      if (lane == 0) {
+        mbar_arrive(smem_u32(&bars.o_free[grp]));
+        if (halves) mbar_arrive(smem_u32(&bars.o_free[1]));
       }
-      slot[kRows * D + at] = m;
-      slot[kRows * D + kRows + at] = l;
-    } else {
-      const float inv = l > 0.f ? 1.f / l : 0.f;
-      const int of = c.t * kRows + tile * kTileRows + (live ? row : 0);
-      const int64_t at = (int64_t)(c.q0 + of / a.group) * a.heads + c.h * a.group + of % a.group;
-#pragma unroll 1
-      for (int i = 0; i < D / 16; ++i) {
-        float o[16];
-        tmem_ld16(to + i * 16, o);
-        if (live) {
-#pragma unroll
-          for (int k = 0; k < 16; k += 8) {
-            float f[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) f[e] = l > 0.f ? o[k + e] * inv : 0.f;
-            *reinterpret_cast<uint4*>(a.y + at * D + i * 16 + k) = pack8(f);
-          }
-        }
-      }
-      if (live && a.lse) a.lse[at] = l > 0.f ? fmaf(m, a.scale, logf(l)) : -INFINITY;
     }
-    tc_fence_before();
     __syncwarp();
-    if (lane == 0) mbar_arrive(smem_u32(&bars.o_free[tile]));
-    next_active(c, left);
+    if (lane == 0) c = nx;
+    __syncwarp();
   }
   cp_async_wait<0>();
 }
@@ -515,6 +575,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       mbar_init(smem_u32(&bars.o[i]), 1u);
       mbar_init(smem_u32(&bars.o_free[i]), 4u);
     }
+    mbar_init(smem_u32(&bars.joined), 4u);
     mbar_init(smem_u32(&bars.drain), 1u);
     fence_mbar_init();
     sh.abort = 0;
@@ -527,47 +588,44 @@ __global__ void __launch_bounds__(kThreads, 1)
   tc_fence_after();
   pdl_wait();
   pdl_trigger();
-  make_plan<kRows>(a, sh.plan);
+  make_plan<kRows, kExtra>(a, sh.plan);
   const unsigned long long total = sh.plan.total;
   const unsigned ctas = (unsigned)min((unsigned long long)gridDim.x, total);
-  JoinItem* join = reinterpret_cast<JoinItem*>(a.ws + (size_t)2 * gridDim.x * C::kSlotFloats);
-  int units = 0;
-  if (blockIdx.x < ctas) {
-    const unsigned long long u0 = cut_start(total, ctas, blockIdx.x);
-    units = (int)(cut_start(total, ctas, blockIdx.x + 1) - u0);
-    PagedCursor<kRows> c;
-    c.seek(a, sh.plan, u0);
-    if (lane == 0) {
-      sh.at[warp] = c;
-      if (warp < kSoftWarps) sh.next[warp] = c;
-    }
-    if (threadIdx.x == 0) {
+  const bool works = blockIdx.x < ctas;
+  if (warp == 0) {
+    JoinItem j{};
+    if (works) {
+      const unsigned long long u0 = cut_start(total, ctas, blockIdx.x), u1 = cut_start(total, ctas, blockIdx.x + 1);
+      Cursor c;
+      c.seek(a, sh.plan, u0, (int)(u1 - u0));
+      if (lane == 0) sh.start = c;
       // an item cut at this CTA's start is joined later; the first of its cuts speaks for it
-      const unsigned long long i0 = u0 - c.blk;
-      JoinItem j;
-      j.c0 = (int)cut_owner(total, ctas, i0);
-      j.c1 = (int)cut_owner(total, ctas, i0 + c.k.units - 1);
-      j.late = i0 > cut_start(total, ctas, j.c0);
-      j.q0 = c.q0;
-      j.t = c.t;
-      j.h = c.h;
-      j.rows = min(kRows, c.n * a.group - c.t * kRows);
-      j.valid = c.blk > 0 && j.c0 + 1 == (int)blockIdx.x;
-      join[blockIdx.x] = j;
+      if (c.first > 0) {
+        const PagedShares s = shares_of<kExtra>(total, ctas, u0 - c.pos, c.k.units);
+        j.c0 = (int)s.c0;
+        j.c1 = (int)s.c1;
+        j.late = s.late;
+        j.q0 = c.q0;
+        j.t = c.t;
+        j.h = c.h;
+        j.rows = min(kRows, c.n * a.group - c.t * kRows);
+        j.valid = s.c0 + 1 == blockIdx.x;
+      }
     }
-  } else if (threadIdx.x == 0) {
-    join[blockIdx.x].valid = 0;
+    if (lane == 0) reinterpret_cast<JoinItem*>(a.ws + (size_t)2 * gridDim.x * C::kSlotFloats)[blockIdx.x] = j;
   }
+  __syncthreads();
+  if (works && lane == 0) sh.at[warp] = sh.start;
   __syncwarp();
   const uint32_t sq = (smem_u32(smem_raw) + 1023u) & ~1023u;
-  const Role r{a, sh, sq, sq + 2 * C::kTile, units, a.wait_limit ? a.wait_limit : kWaitLimitCycles};
+  const Role r{a, sh, sq, sq + 2 * C::kTile, a.wait_limit ? a.wait_limit : kWaitLimitCycles};
   if (warp < kSoftWarps) {
     reg_inc<kManyRegs>();
-    if (units > 0) softmax_role<D>(r, sh.tmem);
+    if (works) softmax_role<D>(r, sh.tmem);
   } else {
     reg_dec<kFewRegs>();
-    if (units > 0 && warp == kMmaWarp) mma_role<D>(r, sh.tmem);
-    if (units > 0 && warp == kLoadWarp) load_role<D>(r, &tk, &tv);
+    if (works && warp == kMmaWarp) mma_role<D>(r, sh.tmem);
+    if (works && warp == kLoadWarp) load_role<D>(r, &tk, &tv);
   }
   tc_fence_before();
   __syncthreads();

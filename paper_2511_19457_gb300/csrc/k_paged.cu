@@ -24,7 +24,10 @@ constexpr int kRows = 16;     // rows of an item
 constexpr int kWarps = 8;
 constexpr int kThreads = 32 * kWarps;
 constexpr int kKeys = 16;     // a warp's keys of a unit
+constexpr int kExtra = 1;     // an item's beginning and end, in units
 static_assert(kKeys * kWarps == kUnitKeys, "unit");
+
+using Cursor = PagedCursor<kRows, kExtra>;
 
 template <int D>
 struct Cfg {
@@ -76,6 +79,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   constexpr int S = C::kStages;
   extern __shared__ uint8_t smem_raw[];
   __shared__ PagedPlan plan;
+  __shared__ Cursor s_start;
   __shared__ __align__(8) unsigned long long s_bar[kWarps][S];
   __shared__ float s_m[kWarps][kRows], s_l[kWarps][kRows];
   __shared__ uint32_t s_at[kWarps];
@@ -95,33 +99,35 @@ __global__ void __launch_bounds__(kThreads, 1)
   __syncthreads();
   pdl_wait();
   pdl_trigger();
-  make_plan<kRows>(a, plan);
+  make_plan<kRows, kExtra>(a, plan);
   const unsigned long long total = plan.total;
-  if (total == 0ull) return;
   const unsigned ctas = (unsigned)min((unsigned long long)gridDim.x, total);
   if (blockIdx.x >= ctas) return;
   const unsigned long long u0 = cut_start(total, ctas, blockIdx.x), u1 = cut_start(total, ctas, blockIdx.x + 1);
+  if (warp == 0) {
+    Cursor c;
+    c.seek(a, plan, u0, (int)(u1 - u0));
+    if (lane == 0) s_start = c;
+  }
+  __syncthreads();
 
   const long long limit = a.wait_limit ? a.wait_limit : kWaitLimitCycles;
-  PagedCursor<kRows> pc, cc;  // the next unit to fetch, and the one being used
-  cc.seek(a, plan, u0);
-  pc = cc;
+  Cursor pc = s_start, cc = pc;   // the next unit to fetch, and the one being used
   unsigned issued = 0, used = 0;  // stages filled and consumed
   bool dead = false;              // a wait ran out: no more loads or products
-  auto first_key = [&](const PagedCursor<kRows>& c) { return (c.k.blk0 + c.blk) * kUnitKeys + warp * kKeys; };
-  auto live = [&](const PagedCursor<kRows>& c) {
-    const int key = first_key(c);
+  auto live = [&](const Cursor& c) {
+    const int key = c.key0() + warp * kKeys;
     return key < c.k.hi && key + kKeys > c.k.lo;
   };
   int page = 0;  // of the next unit to fetch, loaded a step ahead
   auto look_up = [&]() {
-    if (live(pc)) page = page_of(a, pc.b, first_key(pc));
+    if (!pc.done() && live(pc)) page = page_of(a, pc.b, pc.key0() + warp * kKeys);
   };
-  auto fetch = [&](unsigned long long u) {  // unit u, where pc stands
-    if (u >= u1) return;
+  auto fetch = [&]() {
+    if (pc.done()) return;
     if (live(pc) && !dead) {
       if (lane == 0) {
-        const int row = pool_row(a, page_checked(a, page), pc.h, first_key(pc));
+        const int row = pool_row(a, page_checked(a, page), pc.h, pc.key0() + warp * kKeys);
         const uint32_t bar = smem_u32(&s_bar[warp][issued % S]), dst = ring + (issued % S) * C::kStageBytes;
         mbar_arrive_expect_tx(bar, C::kStageBytes);
 #pragma unroll
@@ -131,13 +137,11 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       ++issued;
     }
-    if (u + 1 < u1) {
-      pc.next(a, plan);
-      look_up();
-    }
+    pc.next(a, plan);
+    look_up();
   };
   look_up();
-  for (int i = 0; i < S - 1; ++i) fetch(u0 + i);
+  for (int i = 0; i < S - 1; ++i) fetch();
 
   uint32_t qa[D / 16][4];
   float o[D / 8][4], m0, m1, l0, l1;
@@ -148,8 +152,9 @@ __global__ void __launch_bounds__(kThreads, 1)
   const int krow = ((lane >> 4) << 3) + (lane & 7), kch = (lane >> 3) & 1;
   const int vrow = (((lane >> 3) & 1) << 3) + (lane & 7), vch = lane >> 4;
 
-  for (unsigned long long u = u0; u < u1; ++u) {
-    fetch(u + S - 1);
+  bool second = false;  // not this CTA's first item
+  for (; !cc.done(); cc.next(a, plan)) {
+    fetch();
     const int rows = cc.n * a.group - cc.t * kRows;  // rows of the item (16 at most count)
     if (fresh) {
       fresh = false;
@@ -163,7 +168,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         if (g + 8 * i < rows) {
-          const int row = cc.t * kRows + g + 8 * i, tok = row / a.group, head = cc.h * a.group + row % a.group;
+          const int row = cc.t * kRows + g + 8 * i, tok = over_group(a, row), head = cc.h * a.group + row - tok * a.group;
           const int pos = cc.len - cc.n + tok;
           p[i] = a.q + (int64_t)(cc.q0 + tok) * a.ld_q + head * D;
           lim[i] = a.causal ? min(cc.len, pos + 1) : cc.len;
@@ -187,7 +192,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       } else {
         ++used;
         any = true;
-        const int key0 = first_key(cc);
+        const int key0 = cc.key0() + warp * kKeys;
         // values past the sequence's end may be anything, and 0 * NaN is NaN: zero them
         if (key0 + kKeys > cc.len) {
           const int from = cc.len - key0;  // 1 to 15
@@ -265,7 +270,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         __syncwarp();  // the stage may be filled again
       }
     }
-    if (cc.blk + 1 == cc.k.units || u + 1 == u1) {
+    if (cc.blk + 1 == cc.end) {
       // the item, or this CTA's share of it, ends: join the warps
       const int valid = rows < kRows ? rows : kRows;
       l0 += __shfl_xor_sync(0xffffffffu, l0, 1);
@@ -313,12 +318,11 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
       }
       fence_proxy_async_smem();
-      const unsigned long long i0 = u - cc.blk, i1 = i0 + cc.k.units;  // the item's units
       bool write = true;
-      if (i0 < u0 || i1 > u1) {
+      if (cc.cut()) {
         // shared with other CTAs: leave the partial result; the last to arrive joins them
-        const unsigned c0 = cut_owner(total, ctas, i0), c1 = cut_owner(total, ctas, i1 - 1);
-        float* slot = a.ws + (size_t)(2 * blockIdx.x + (i0 > u0 ? 1 : 0)) * kSlotFloats<D>;
+        const PagedShares sh = shares_of<kExtra>(total, ctas, u1 - cc.left - cc.pos, cc.k.units);
+        float* slot = a.ws + (size_t)(2 * blockIdx.x + (second ? 1 : 0)) * kSlotFloats<D>;
         if (mine_out) {
           float4* d = reinterpret_cast<float4*>(slot + row * D + piece * 8);
           d[0] = make_float4(acc[0], acc[1], acc[2], acc[3]);
@@ -330,19 +334,19 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         __threadfence();
         __syncthreads();
-        if (threadIdx.x == 0) s_last = atomicAdd(&a.cnt[c0], 1u) == c1 - c0;
+        if (threadIdx.x == 0) s_last = atomicAdd(&a.cnt[sh.c0], 1u) == sh.c1 - sh.c0;
         __syncthreads();
         write = s_last != 0;
         if (write) {
           __threadfence();
-          if (threadIdx.x == 0) a.cnt[c0] = 0u;  // ready for the next call
+          if (threadIdx.x == 0) a.cnt[sh.c0] = 0u;  // ready for the next call
           if (mine_out) {
             mx = -INFINITY;
             ls = 0.f;
 #pragma unroll
             for (int k = 0; k < 8; ++k) acc[k] = 0.f;
-            for (unsigned c = c0; c <= c1; ++c) {
-              const float* p = a.ws + (size_t)(2 * c + (c == c0 && i0 > cut_start(total, ctas, c) ? 1 : 0)) * kSlotFloats<D>;
+            for (unsigned c = sh.c0; c <= sh.c1; ++c) {
+              const float* p = a.ws + (size_t)(2 * c + (c == sh.c0 && sh.late ? 1 : 0)) * kSlotFloats<D>;
               const float mw = __ldcg(p + kRows * D + row), lw = __ldcg(p + kRows * D + kRows + row);
               const float4 v0 = __ldcg(reinterpret_cast<const float4*>(p + row * D + piece * 8));
               const float4 v1 = __ldcg(reinterpret_cast<const float4*>(p + row * D + piece * 8 + 4));
@@ -359,9 +363,9 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
       }
       if (write && mine_out) {
-        const int r = cc.t * kRows + row;
-        const int64_t tok = cc.q0 + r / a.group;
-        const int head = cc.h * a.group + r % a.group;
+        const int r = cc.t * kRows + row, of = over_group(a, r);
+        const int64_t tok = cc.q0 + of;
+        const int head = cc.h * a.group + r - of * a.group;
         const float inv = ls > 0.f ? 1.f / ls : 0.f;
 #pragma unroll
         for (int k = 0; k < 8; ++k) acc[k] *= inv;
@@ -371,8 +375,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       __syncthreads();  // the free stages may be filled, s_m, s_l and s_at written again
       fresh = true;
+      second = true;
     }
-    if (u + 1 < u1) cc.next(a, plan);
   }
   // after a timeout: no copy is in flight into shared memory that is given back
   if (dead)

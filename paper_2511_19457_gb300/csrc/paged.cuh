@@ -2,11 +2,12 @@
 //
 // An item is one tile of RT query rows of one sequence and key head (row r of a
 // sequence: token r / group, query head key_head * group + r % group).  Its keys are
-// walked in units of 128.  The units of all items, in the order (sequence, key head,
-// tile), form one line that the CTAs cut into equal shares: every CTA loads as many
-// keys as any other, however ragged the batch, and at most its first and last item
-// are shared with other CTAs.  Lengths are on the device, so every CTA makes the plan
-// itself (a load per sequence and a scan; about a microsecond).
+// walked in units of 128; its cost is its units and EXTRA more for its beginning and
+// end.  The costs of all items, in the order (sequence, key head, tile), form one line
+// that the CTAs cut into equal shares: every CTA has as much to do as any other,
+// however ragged the batch, and at most its first and last item are shared with other
+// CTAs.  Lengths are on the device, so every CTA makes the plan itself (a load per
+// sequence and a scan).
 #pragma once
 
 #include "sparoa_kernels.h"
@@ -15,11 +16,11 @@ namespace sparoa {
 
 constexpr int kUnitKeys = 128;
 
-// The batch in shared memory: first row, new tokens, cached tokens and units per key
+// The batch in shared memory: first row, new tokens, cached tokens and cost per key
 // head of each sequence.
 struct PagedPlan {
   int q0[kPagedMaxBatch], n[kPagedMaxBatch], len[kPagedMaxBatch];
-  unsigned long long units[kPagedMaxBatch];
+  unsigned long long cost[kPagedMaxBatch];
   unsigned long long total;
 };
 
@@ -29,19 +30,25 @@ struct TileKeys {
   int lo, hi, blk0, units;
 };
 
+// row / group for rows below 2^31 (the host's multiplier, see PagedArgs)
+__device__ __forceinline__ int over_group(const PagedArgs& a, int row) {
+  return a.group == 1 ? row : (int)(__umulhi((unsigned)row, a.group_mul) >> a.group_shift);
+}
+
 template <int RT>
 __device__ __forceinline__ int tiles_of(int n, int group) {
-  return (int)(((long long)n * group + RT - 1) / RT);
+  return (n * group + RT - 1) / RT;  // (n * group is at most 2^30)
 }
 
 template <int RT>
 __device__ __forceinline__ TileKeys tile_keys(const PagedArgs& a, int n, int len, int t) {
   TileKeys k;
-  const int rows = n * a.group;
-  const int first = t * RT / a.group;
-  const int last = (min(rows, (t + 1) * RT) - 1) / a.group;
-  k.hi = a.causal ? max(0, min(len, len - n + last + 1)) : len;
-  k.lo = a.window > 0 ? max(0, len - n + first - a.window + 1) : 0;
+  k.hi = len;
+  if (a.causal) {
+    const int last = over_group(a, min(n * a.group, (t + 1) * RT) - 1);
+    k.hi = max(0, min(len, len - n + last + 1));
+  }
+  k.lo = a.window > 0 ? max(0, len - n + over_group(a, t * RT) - a.window + 1) : 0;
   k.blk0 = k.lo / kUnitKeys;
   k.units = max(1, (k.hi + kUnitKeys - 1) / kUnitKeys - k.blk0);
   return k;
@@ -50,7 +57,7 @@ __device__ __forceinline__ TileKeys tile_keys(const PagedArgs& a, int n, int len
 // Fills the plan (all threads of the CTA; ends with a block barrier).  What the lists
 // say is brought into the tensors' bounds; where it is not there already, the error
 // bit is set.
-template <int RT>
+template <int RT, int EXTRA>
 __device__ __forceinline__ void make_plan(const PagedArgs& a, PagedPlan& p) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
   if (threadIdx.x == 0) p.total = 0ull;
@@ -60,30 +67,30 @@ __device__ __forceinline__ void make_plan(const PagedArgs& a, PagedPlan& p) {
   unsigned long long sum = 0ull;
   for (int b = threadIdx.x; b < a.batch; b += blockDim.x) {
     long long q0 = a.q_start[b], n = (long long)a.q_start[b + 1] - q0, len = a.kv_len[b];
-    const bool bad = q0 < 0 || n < 0 || q0 + n > a.T || n * a.group > 0x3FFFFFFF || len < 0 || len > room;
-    if (bad) {
+    const bool bad_rows = q0 < 0 || n < 0 || q0 + n > a.T || n * a.group > 0x3FFFFFFF;
+    if (bad_rows || len < 0 || len > room) {
       atomicOr(a.err, kErrBadIndex);
-      n = q0 < 0 || n < 0 || q0 + n > a.T || n * a.group > 0x3FFFFFFF ? 0 : n;
+      if (bad_rows) n = 0;
       len = len < 0 ? 0 : min(len, room);
     }
     const int tiles = tiles_of<RT>((int)n, a.group);
     p.q0[b] = (int)q0;
     p.n[b] = (int)n;
     p.len[b] = (int)len;
-    p.units[b] = tiles == 1 ? (unsigned long long)tile_keys<RT>(a, (int)n, (int)len, 0).units : 0ull;
+    p.cost[b] = tiles == 1 ? (unsigned long long)(tile_keys<RT>(a, (int)n, (int)len, 0).units + EXTRA) : 0ull;
     many |= tiles > 1;
-    sum += p.units[b] * a.kv_heads;
+    sum += p.cost[b] * a.kv_heads;
   }
   if (__syncthreads_or(many)) {
     for (int b = warp; b < a.batch; b += warps) {
       const int n = p.n[b], len = p.len[b], tiles = tiles_of<RT>(n, a.group);
       if (tiles <= 1) continue;
       unsigned long long u = 0ull;
-      for (int t = lane; t < tiles; t += 32) u += (unsigned long long)tile_keys<RT>(a, n, len, t).units;
+      for (int t = lane; t < tiles; t += 32) u += (unsigned long long)(tile_keys<RT>(a, n, len, t).units + EXTRA);
 #pragma unroll
       for (int d = 16; d > 0; d >>= 1) u += __shfl_xor_sync(0xffffffffu, u, d);
       if (lane == 0) {
-        p.units[b] = u;
+        p.cost[b] = u;
         sum += u * a.kv_heads;
       }
     }
@@ -94,12 +101,20 @@ __device__ __forceinline__ void make_plan(const PagedArgs& a, PagedPlan& p) {
   __syncthreads();
 }
 
-// One place in the line of units, the same in all lanes of a warp.
-template <int RT>
+// A walk over one CTA's share of the line, the same in all lanes of a warp.
+template <int RT, int EXTRA>
 struct PagedCursor {
-  int b, h, t, tiles, blk;   // blk: unit within the item
+  int b, h, t, tiles;
   int q0, n, len;
   TileKeys k;
+  int pos, left;     // where the share enters the item's cost, and the share's cost from there
+  int first, end;    // the share's units of the item
+  int blk;           // unit, first to end - 1; at `end`: nothing left
+
+  __device__ __forceinline__ bool done() const { return blk >= end; }
+  __device__ __forceinline__ int key0() const { return (k.blk0 + blk) * kUnitKeys; }
+  // whether other CTAs have units of the item
+  __device__ __forceinline__ bool cut() const { return first > 0 || end < k.units; }
 
   __device__ __forceinline__ void load_seq(const PagedArgs& a, const PagedPlan& p) {
     q0 = p.q0[b];
@@ -107,13 +122,18 @@ struct PagedCursor {
     len = p.len[b];
     tiles = tiles_of<RT>(n, a.group);
   }
-  // to unit u < p.total (a converged warp)
-  __device__ __forceinline__ void seek(const PagedArgs& a, const PagedPlan& p, unsigned long long u) {
+  __device__ __forceinline__ void enter(const PagedArgs& a) {
+    k = tile_keys<RT>(a, n, len, t);
+    first = blk = max(0, pos - EXTRA);
+    end = min(k.units, pos + left - EXTRA);  // (below `first`: the share ends in the item's beginning)
+  }
+  // to position u < total of the line, `cost` of which are to be walked (a converged warp)
+  __device__ __forceinline__ void seek(const PagedArgs& a, const PagedPlan& p, unsigned long long u, int cost) {
     const int lane = threadIdx.x & 31;
-    unsigned long long before = 0ull;  // units of the sequences before b0
+    unsigned long long before = 0ull;  // cost of the sequences before b0
     int b0 = 0;
     for (;; b0 += 32) {
-      const unsigned long long mine = b0 + lane < a.batch ? p.units[b0 + lane] * a.kv_heads : 0ull;
+      const unsigned long long mine = b0 + lane < a.batch ? p.cost[b0 + lane] * a.kv_heads : 0ull;
       unsigned long long incl = mine;
 #pragma unroll
       for (int d = 1; d < 32; d <<= 1) {
@@ -130,57 +150,78 @@ struct PagedCursor {
       before += __shfl_sync(0xffffffffu, incl, 31);
     }
     load_seq(a, p);
-    const unsigned long long per = p.units[b];
+    const unsigned long long per = p.cost[b];
     unsigned long long rem = u - before;
     h = (int)(rem / per);
     rem -= h * per;
-    for (int t0 = 0;; t0 += 32) {
-      const unsigned mine = t0 + lane < tiles ? (unsigned)tile_keys<RT>(a, n, len, t0 + lane).units : 0u;
-      unsigned incl = mine;
+    t = 0;
+    if (tiles > 1) {
+      for (int t0 = 0;; t0 += 32) {
+        const unsigned mine = t0 + lane < tiles ? (unsigned)(tile_keys<RT>(a, n, len, t0 + lane).units + EXTRA) : 0u;
+        unsigned incl = mine;
 #pragma unroll
-      for (int d = 1; d < 32; d <<= 1) {
-        const unsigned o = __shfl_up_sync(0xffffffffu, incl, d);
-        if (lane >= d) incl += o;
+        for (int d = 1; d < 32; d <<= 1) {
+          const unsigned o = __shfl_up_sync(0xffffffffu, incl, d);
+          if (lane >= d) incl += o;
+        }
+        const unsigned hit = __ballot_sync(0xffffffffu, incl > rem);
+        if (hit || t0 + 32 >= tiles) {
+          const int l = hit ? __ffs(hit) - 1 : 31;
+          t = t0 + l;
+          rem -= __shfl_sync(0xffffffffu, incl - mine, l);
+          break;
+        }
+        rem -= __shfl_sync(0xffffffffu, incl, 31);
       }
-      const unsigned hit = __ballot_sync(0xffffffffu, incl > rem);
-      if (hit || t0 + 32 >= tiles) {
-        const int l = hit ? __ffs(hit) - 1 : 31;
-        t = t0 + l;
-        rem -= __shfl_sync(0xffffffffu, incl - mine, l);
-        break;
-      }
-      rem -= __shfl_sync(0xffffffffu, incl, 31);
     }
-    blk = (int)rem;
-    k = tile_keys<RT>(a, n, len, t);
+    pos = (int)rem;
+    left = cost;
+    enter(a);
   }
-  // to the next unit (not past the last)
-  __device__ __forceinline__ void next(const PagedArgs& a, const PagedPlan& p) {
-    if (++blk < k.units) return;
-    blk = 0;
+  // to the share's next item, if any (done() afterwards: none)
+  __device__ __forceinline__ void next_item(const PagedArgs& a, const PagedPlan& p) {
+    left -= k.units + EXTRA - pos;
+    if (left <= EXTRA) {
+      blk = end;
+      return;
+    }
     if (++t == tiles) {
       t = 0;
       if (++h == a.kv_heads) {
         h = 0;
-        do ++b; while (b < a.batch && p.units[b] == 0ull);
-        if (b >= a.batch) {  // past the end: stay on a valid place
-          b = a.batch - 1;
-          return;
-        }
+        do ++b; while (p.cost[b] == 0ull);  // (the line goes on: there is such a sequence)
         load_seq(a, p);
       }
     }
-    k = tile_keys<RT>(a, n, len, t);
+    pos = 0;
+    enter(a);
+  }
+  __device__ __forceinline__ void next(const PagedArgs& a, const PagedPlan& p) {
+    if (++blk >= end) next_item(a, p);
   }
 };
 
-// The line's cut: CTA c of `ctas` has units [c total / ctas, (c + 1) total / ctas).
+// The line's cut: CTA c of `ctas` has positions [c total / ctas, (c + 1) total / ctas).
 __device__ __forceinline__ unsigned long long cut_start(unsigned long long total, unsigned ctas, unsigned c) {
   return total * c / ctas;
 }
-// the CTA that has unit u
+// the CTA that has position u
 __device__ __forceinline__ unsigned cut_owner(unsigned long long total, unsigned ctas, unsigned long long u) {
   return (unsigned)(((u + 1) * ctas - 1) / total);
+}
+// The CTAs c0 to c1 that share an item of `units` units at position i0 of the line; late:
+// c0 has had another item before it.
+struct PagedShares {
+  unsigned c0, c1;
+  bool late;
+};
+template <int EXTRA>
+__device__ __forceinline__ PagedShares shares_of(unsigned long long total, unsigned ctas, unsigned long long i0, int units) {
+  PagedShares s;
+  s.c0 = cut_owner(total, ctas, i0 + EXTRA);  // (who has the item's first unit)
+  s.c1 = cut_owner(total, ctas, i0 + EXTRA + units - 1);
+  s.late = i0 > cut_start(total, ctas, s.c0);
+  return s;
 }
 
 // Page of key `key` of sequence b, brought into the pool's bounds.

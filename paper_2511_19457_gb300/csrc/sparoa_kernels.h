@@ -266,6 +266,7 @@ struct PagedArgs {
   const __nv_bfloat16* q = nullptr;
   int64_t ld_q = 0, T = 0;
   int heads = 0, kv_heads = 0, group = 0, D = 0;
+  uint32_t group_mul = 0, group_shift = 0;  // n / group = umulhi(n, mul) >> shift for group > 1, n < 2^31
   float scale = 1.f;
   int causal = 0, window = 0;
   const __nv_bfloat16 *k = nullptr, *v = nullptr;  // pools [pages][kv_heads][page][D]
