@@ -286,7 +286,7 @@ struct PagedArgs {
   int fault = 0;               // error-path tests: 1 withholds the chunk kernel's signals of its scores
 };
 constexpr int kPagedMaxBatch = 1024;
-constexpr int kPagedCounters = 512;
+constexpr int kPagedCounters = 256;  // and CTAs at most
 size_t paged_ws_bytes();
 cudaError_t launch_paged_attention(const PagedArgs& a, cudaStream_t s);
 // the kernel for chunks of tokens (k_chunk.cu)
