@@ -383,16 +383,22 @@ def sparoa_attention(ctx: Context, qkv, y, heads, y_occ=None):
 # ---------------------------------------------------------------------------
 # decoder operators: residual norm, rotary positions into a paged cache, attention over it
 # ---------------------------------------------------------------------------
+def _refuse(what):
+    raise SparoaError(ERR_INVALID_ARG, what)
+
+
 def _want(cond, what):
     if not cond:
-        raise SparoaError(ERR_INVALID_ARG, what)
+        _refuse(what)
 
 
 def _want_rows(t, dtypes, what):
     """t is a CUDA tensor of one of `dtypes` with contiguous storage."""
-    _want(t.is_cuda and t.dtype in dtypes and t.is_contiguous(), f"{what}: contiguous CUDA tensor of {dtypes} wanted")
+    if not (t.is_cuda and t.dtype in dtypes and t.is_contiguous()):
+        _refuse(f"{what}: contiguous CUDA tensor of {dtypes} wanted")
 
 
+_bf16, _f32 = torch.bfloat16, torch.float32
 _BF16S = (torch.bfloat16,)
 _FP32S = (torch.float32,)
 _I32S = (torch.int32,)
@@ -406,7 +412,9 @@ class Norm:
             if t is not None:
                 _want_rows(t, _FP32S, "norm parameter")
         self.weight, self.bias = weight, bias
-        self.size = {t.numel() for t in (weight, bias) if t is not None}
+        sizes = {t.numel() for t in (weight, bias) if t is not None}
+        _want(len(sizes) < 2, "norm parameters of different lengths")
+        self.C = sizes.pop() if sizes else 0
         self.desc = NormSpec({"none": NORM_NONE, "rms": NORM_RMS, "layer": NORM_LAYER}[kind], float(eps),
                              _ptr(weight), _ptr(bias))
         self.ref = _byref(self.desc)
@@ -421,28 +429,30 @@ def sparoa_add_norm(ctx: Context, x, h, r=None, y=None, post: Norm | None = None
                     scale=1.0, pre: Norm | None = None, y_occ=None):
     """r = x + scale gate N_post(h), y = N_pre(r) over the last dimension; x and r bf16 or
     fp32, h and y bf16; any of x, h (not both) and r, y may be None."""
-    lead = x if x is not None else h
-    _want(lead is not None, "add_norm: x or h")
-    C = lead.shape[-1]
-    R = _rows(lead.shape)
-    stream = x if x is not None else r
-    res = F32 if stream is not None and stream.dtype == torch.float32 else BF16
-    for t, dts in ((x, (torch.float32,) if res else _BF16S), (r, (torch.float32,) if res else _BF16S), (h, _BF16S),
-                   (y, _BF16S)):
-        if t is not None:
-            _want_rows(t, dts, "add_norm")
-            _want(t.numel() == R * C, "add_norm: tensors of different sizes")
-    for n in (post, pre):
-        _want(n is None or n.size <= {C}, "add_norm: norm parameters of another length")
-    rows_per_gate = int(rows_per_gate)
+    lead = h if x is None else x
+    if lead is None:
+        _refuse("add_norm: x or h")
+    shape = lead.shape
+    C = shape[-1]
+    R = lead.numel() // C if C else 0
+    stream = r if x is None else x
+    res = _f32 if stream is not None and stream.dtype is _f32 else _bf16
+    for t, dt in ((x, res), (r, res), (h, _bf16), (y, _bf16)):
+        if t is not None and not (t.dtype is dt and t.is_cuda and t.is_contiguous() and t.shape == shape):
+            _refuse("add_norm: contiguous CUDA tensors of one shape wanted: x and r of one type, h and y bf16")
+    if (post is not None and post.C not in (0, C)) or (pre is not None and pre.C not in (0, C)):
+        _refuse("add_norm: norm parameters of another length")
     if gate is not None:
         _want_rows(gate, _FP32S, "add_norm gate")
-        _want(rows_per_gate >= 0 and gate.numel() >= (C if not rows_per_gate else -(-R // rows_per_gate) * C),
-              "add_norm: gate rows")
+        if rows_per_gate < 0 or gate.numel() < (C if not rows_per_gate else -(-R // rows_per_gate) * C):
+            _refuse("add_norm: gate rows")
     ctx._bind()
-    ctx._check(_lib.sparoa_add_norm(ctx.h, _ptr(x), _ptr(h), R, C, res, None if post is None else post.ref, _ptr(gate),
-                                    rows_per_gate, float(scale), None if pre is None else pre.ref, _ptr(r), _ptr(y),
-                                    _occ(y_occ)))
+    st = _add_norm(ctx.h, None if x is None else x.data_ptr(), None if h is None else h.data_ptr(), R, C,
+                   F32 if res is _f32 else BF16, None if post is None else post.ref, _ptr(gate), rows_per_gate, scale,
+                   None if pre is None else pre.ref, None if r is None else r.data_ptr(),
+                   None if y is None else y.data_ptr(), _occ(y_occ))
+    if st:
+        ctx._check(st)
 
 
 class KVCache:
@@ -456,6 +466,7 @@ class KVCache:
         self.pages, self.kv_heads, self.page_size, self.head_dim = k.shape
         self.desc = KvCacheDesc(_ptr(k), _ptr(v), self.pages, self.page_size, self.kv_heads, self.head_dim, 0)
         self.ref = _byref(self.desc)
+        self.scale = self.head_dim ** -0.5
 
     @staticmethod
     def empty(pages, kv_heads, page_size, head_dim, device="cuda"):
@@ -505,30 +516,38 @@ class Rope:
         self.ref = _byref(self.desc)
 
 
-def _token_rows(t, T, width, what):
-    """Row length in elements of t [T, ...] whose rows hold `width` adjacent bf16 values."""
-    _want(t.is_cuda and t.dtype == torch.bfloat16 and t.dim() in (2, 3) and t.shape[0] == T, f"{what}: bf16 rows of {T} tokens")
-    inner = t.shape[1] if t.dim() == 2 else t.shape[1] * t.shape[2]
-    flat = t.shape[-1] <= 1 or t.stride(-1) == 1
-    flat = flat and (t.dim() == 2 or t.shape[1] <= 1 or t.stride(1) == t.shape[2])
-    _want(inner == width and flat, f"{what}: {width} adjacent values a row")
-    return t.stride(0) if T > 1 else max(t.stride(0), width)
+def _token_rows(t, T, what):
+    """(row length, values of a row) of t [T, width] or [T, heads, head_dim], bf16: rows may be
+    strided, the values of a row are adjacent."""
+    shape = t.shape
+    if not (t.dtype is _bf16 and t.is_cuda and 2 <= len(shape) <= 3 and shape[0] == T):
+        _refuse(f"{what}: bf16 rows of {T} tokens wanted")
+    width = shape[1] if len(shape) == 2 else shape[1] * shape[2]
+    if t.is_contiguous():
+        return width, width
+    st = t.stride()
+    if (shape[-1] > 1 and st[-1] != 1) or (len(shape) == 3 and shape[1] > 1 and st[1] != shape[2]):
+        _refuse(f"{what}: adjacent values in a row wanted")
+    return (st[0] if T > 1 else max(st[0], width)), width
 
 
 def sparoa_rope_append(ctx: Context, qkv, q_out, cache: KVCache, batch: PagedBatch, rope: Rope, positions=None):
     """Rotate the new tokens' queries (to q_out [T, heads, head_dim]) and keys (to the cache, with the
     values) from qkv [T, (heads + 2 kv_heads) head_dim]; rows may be strided."""
     T = qkv.shape[0]
-    width = q_out.numel() // T if T else q_out.shape[-1] * (q_out.shape[1] if q_out.dim() == 3 else 1)
-    heads = width // cache.head_dim
-    ld = _token_rows(qkv, T, width + 2 * cache.kv_heads * cache.head_dim, "rope_append qkv")
-    ldq = _token_rows(q_out, T, heads * cache.head_dim, "rope_append q_out")
+    ld, have = _token_rows(qkv, T, "rope_append qkv")
+    ldq, width = _token_rows(q_out, T, "rope_append q_out")
+    D = cache.head_dim
+    if width % D or have != width + 2 * cache.kv_heads * D:
+        _refuse("rope_append: qkv rows hold heads, key heads and value heads; q_out rows the heads")
     if positions is not None:
         _want_rows(positions, _I32S, "rope_append positions")
         _want(positions.numel() == T, "rope_append: a position per token")
     ctx._bind()
-    ctx._check(_lib.sparoa_rope_append(ctx.h, _ptr(qkv), ld, T, heads, rope.ref, _ptr(positions), cache.ref, batch.ref,
-                                       _ptr(q_out), ldq))
+    st = _rope_append(ctx.h, qkv.data_ptr(), ld, T, width // D, rope.ref, _ptr(positions), cache.ref, batch.ref,
+                      q_out.data_ptr(), ldq)
+    if st:
+        ctx._check(st)
 
 
 def sparoa_paged_attention(ctx: Context, q, y, cache: KVCache, batch: PagedBatch, scale=None, causal=True, window=0,
@@ -536,17 +555,21 @@ def sparoa_paged_attention(ctx: Context, q, y, cache: KVCache, batch: PagedBatch
     """y = softmax(scale q K^T) V of the new tokens over their cached sequences; q [T, heads, head_dim]
     (rows may be strided), y the same (contiguous), lse fp32 [T, heads] or None."""
     T, D = q.shape[0], cache.head_dim
-    heads = y.numel() // (T * D) if T else max(1, y.shape[-1] * (y.shape[1] if y.dim() == 3 else 1) // D)
-    ld = _token_rows(q, T, heads * D, "paged_attention q")
-    _want_rows(y, _BF16S, "paged_attention y")
-    _want(y.numel() == T * heads * D, "paged_attention: y")
+    ld, width = _token_rows(q, T, "paged_attention q")
+    if width % D or not (y.dtype is _bf16 and y.is_cuda and y.is_contiguous() and y.numel() == T * width):
+        _refuse("paged_attention: q rows of whole heads, y of q's size")
     if lse is not None:
         _want_rows(lse, _FP32S, "paged_attention lse")
-        _want(lse.numel() == T * heads, "paged_attention: lse")
+        _want(lse.numel() == T * (width // D), "paged_attention: lse")
     ctx._bind()
-    ctx._check(_lib.sparoa_paged_attention(ctx.h, _ptr(q), ld, T, heads, D ** -0.5 if scale is None else float(scale),
-                                           1 if causal else 0, int(window), cache.ref, batch.ref, _ptr(y), _ptr(lse),
-                                           _occ(y_occ)))
+    st = _paged_attention(ctx.h, q.data_ptr(), ld, T, width // D, cache.scale if scale is None else scale,
+                          1 if causal else 0, window, cache.ref, batch.ref, y.data_ptr(), _ptr(lse), _occ(y_occ))
+    if st:
+        ctx._check(st)
+
+
+_add_norm, _rope_append = _lib.sparoa_add_norm, _lib.sparoa_rope_append
+_paged_attention = _lib.sparoa_paged_attention
 
 
 def sparoa_gemm_noalloc(x, W, y, W_kn=None, bias=None, bn=None, eps=1e-5, act=ACT_NONE,
