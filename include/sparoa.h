@@ -419,8 +419,8 @@ typedef struct {
  *   y     bf16 input of the next block (nullable); may be h
  *   y_occ occupancy of y to write (nullable; needs y)
  * Tensors are contiguous and 16-byte aligned; but for r = x and y = h outputs
- * overlap nothing.  C % 8 == 0, C <= 16384.
- * Errors: INVALID_ARG, UNSUPPORTED (C > 16384), CUDA. */
+ * overlap nothing.  C % 8 == 0, C <= 16384, R < 2^31.
+ * Errors: INVALID_ARG, UNSUPPORTED (C, R), CUDA. */
 sparoa_status sparoa_add_norm(sparoa_ctx *ctx, const void *x, const void *h, int64_t R, int64_t C,
                               int32_t res_dtype, const sparoa_norm_spec *post, const float *gate,
                               int64_t rows_per_gate, float scale, const sparoa_norm_spec *pre,

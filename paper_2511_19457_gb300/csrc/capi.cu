@@ -1356,7 +1356,8 @@ sparoa_status sparoa_add_norm(sparoa_ctx* ctx, const void* x, const void* h, int
                               const sparoa_norm_spec* pre, void* r, void* y, const sparoa_occupancy* y_occ) {
   if (!ctx) return SPAROA_ERR_INVALID_ARG;
   if (R < 0 || C <= 0 || C % 8) return fail(ctx, SPAROA_ERR_INVALID_ARG, "add_norm: bad shape");
-  if (C > 16384) return fail(ctx, SPAROA_ERR_UNSUPPORTED, "add_norm: C <= 16384 only");
+  if (C > 16384 || R > 0x7FFFFFFF)
+    return fail(ctx, SPAROA_ERR_UNSUPPORTED, "add_norm: C <= 16384 and fewer than 2^31 rows only");
   if (res_dtype != SPAROA_BF16 && res_dtype != SPAROA_F32)
     return fail(ctx, SPAROA_ERR_INVALID_ARG, "add_norm: res_dtype");
   if (R > 0 && ((!x && !h) || (!r && !y))) return fail(ctx, SPAROA_ERR_INVALID_ARG, "add_norm: no input or no output");
@@ -1379,10 +1380,12 @@ sparoa_status sparoa_add_norm(sparoa_ctx* ctx, const void* x, const void* h, int
   a.post = to_dev(post);
   a.pre = to_dev(pre);
   a.gate = gate;
-  a.per = rows_per_gate;
+  a.per = (uint32_t)(rows_per_gate < R ? rows_per_gate : R);  // (one row of the gate for all, either way)
   a.scale = scale;
   a.r = r;
   a.y = static_cast<__nv_bfloat16*>(y);
+  a.err = ctx->d_err();
+  a.wait_limit = ctx->wait_limit;
   SP_CUDA(launch_add_norm(a, ctx->stream));
   if (y_occ) SP_TRY(run_stats(ctx, y, R, C, *y_occ));
   return SPAROA_OK;

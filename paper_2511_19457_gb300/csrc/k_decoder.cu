@@ -10,23 +10,24 @@ namespace {
 // ---------------------------------------------------------------------------
 // Residual step: r = x + scale g N_post(h), y = N_pre(r), rows of C values.
 //
-// Bound by bytes: h and x are read once, r and y written once.  A row is held in
-// registers between the reductions (8-value chunks, NCH a thread): by a warp where
-// C <= 1024, else by a CTA of its own.  Sums are fp32; a layer norm's variance is
-// the mean square of the deviations from the mean, not a difference of two sums.
-// y comes from the fp32 r, not from the r that is stored.
-template <typename RT>
-__device__ __forceinline__ void load8(const RT* p, float (&f)[8]);
-template <>
-__device__ __forceinline__ void load8<__nv_bfloat16>(const __nv_bfloat16* p, float (&f)[8]) {
-  unpack8(*reinterpret_cast<const uint4*>(p), f);
-}
-template <>
-__device__ __forceinline__ void load8<float>(const float* p, float (&f)[8]) {
+// Bound by bytes: h and x are read once, r and y written once.  A CTA takes every
+// gridDim-th row, 8 values of it a thread (16 of rows beyond 8192): rows are on their way
+// into shared memory by bulk copies, up to kNormStages of them, while one is in registers between
+// its reductions, and the norms' parameters, which are a thread's for all its rows, stay in
+// registers.  (Rows loaded into registers by the CTA that reduces them, without any ahead:
+// [8192, 4096] with both norms 102 us.)  Sums are fp32; a layer norm's variance is the mean
+// square of the deviations from the mean, not a difference of two sums.  y comes from the
+// fp32 r, not from the r that is stored.
+__device__ __forceinline__ void load8(const float* p, float (&f)[8]) {
   const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
   f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w;
   f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
 }
+// 8 values from shared memory
+__device__ __forceinline__ void read8(const __nv_bfloat16* p, float (&f)[8]) {
+  unpack8(*reinterpret_cast<const uint4*>(p), f);
+}
+__device__ __forceinline__ void read8(const float* p, float (&f)[8]) { load8(p, f); }
 __device__ __forceinline__ void store8(__nv_bfloat16* p, const float (&f)[8]) {
   *reinterpret_cast<uint4*>(p) = pack8(f);
 }
@@ -35,20 +36,51 @@ __device__ __forceinline__ void store8(float* p, const float (&f)[8]) {
   *reinterpret_cast<float4*>(p + 4) = make_float4(f[4], f[5], f[6], f[7]);
 }
 
-constexpr int kNormWarps = 4;  // warps of a CTA whose rows take a warp each
+constexpr int kNormStages = 3;
 
-template <typename RT, int NCH, bool WARP>
-__global__ void __launch_bounds__(WARP ? 32 * kNormWarps : 512) add_norm_kernel(const __grid_constant__ AddNormArgs a) {
+// A norm's parameters of a thread's 8 NCH columns: in registers, or read again for every
+// row (from L1) where there are too many.
+template <int NCH, bool KEEP>
+struct NormCols {
+  float w[KEEP ? NCH : 1][8], b[KEEP ? NCH : 1][8];
+  __device__ __forceinline__ void load(const NormDev& n, int i, int col, bool live) {
+    float (&ww)[8] = w[KEEP ? i : 0], (&bb)[8] = b[KEEP ? i : 0];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      ww[k] = 1.f;
+      bb[k] = 0.f;
+    }
+    if (live && n.weight) load8(n.weight + col, ww);
+    if (live && n.bias) load8(n.bias + col, bb);
+  }
+};
+
+template <typename RT, int NCH>
+__global__ void __launch_bounds__(1024, 1) add_norm_kernel(const __grid_constant__ AddNormArgs a) {
+  constexpr bool KEEP = NCH == 1;
+  extern __shared__ __align__(128) uint8_t norm_smem[];  // stages: a row of x, a row of h
   __shared__ float s_sum[2][32];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int T = WARP ? 32 : (int)blockDim.x, at = WARP ? lane : (int)threadIdx.x;
+  __shared__ __align__(8) unsigned long long s_full[kNormStages];
+  __shared__ int s_abort;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, T = (int)blockDim.x, at = (int)threadIdx.x;
   const int C = a.C, chunks = C / 8;
   const float inv_c = 1.f / (float)C;
+  const uint32_t xbytes = a.x ? (uint32_t)C * sizeof(RT) : 0u, hbytes = a.h ? (uint32_t)C * 2u : 0u;
+  const long long limit = a.wait_limit ? a.wait_limit : kWaitLimitCycles;
+  const unsigned S = (unsigned)a.stages;
+  if (at == 0) {
+    for (int i = 0; i < kNormStages; ++i) mbar_init(smem_u32(&s_full[i]), 1u);
+    fence_mbar_init();
+    s_abort = 0;
+  }
+  __syncthreads();
+  pdl_wait();
+  pdl_trigger();
   int slot = 0;
   auto sum = [&](float v) {
 #pragma unroll
     for (int d = 16; d > 0; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
-    if constexpr (!WARP) {
+    if (T > 32) {
       // (two slots in turn: a slot is written again only after another slot's barrier)
       if (lane == 0) s_sum[slot][warp] = v;
       __syncthreads();
@@ -59,9 +91,27 @@ __global__ void __launch_bounds__(WARP ? 32 * kNormWarps : 512) add_norm_kernel(
     }
     return v;
   };
+  unsigned fills = 0;
+  auto fill = [&](int64_t r) {  // by one thread: row r into the next stage
+    if (r >= a.R) return;
+    const unsigned n = fills++;
+    const uint32_t bar = smem_u32(&s_full[n % S]);
+    const uint32_t dst = smem_u32(norm_smem) + (n % S) * (xbytes + hbytes);
+    mbar_arrive_expect_tx(bar, xbytes + hbytes);
+    if (xbytes) bulk_load(dst, static_cast<const RT*>(a.x) + r * C, xbytes, bar);
+    if (hbytes) bulk_load(dst + xbytes, a.h + r * C, hbytes, bar);
+  };
+  const int64_t step = gridDim.x;
+  if (at == 0)
+    for (unsigned i = 0; i < S; ++i) fill(blockIdx.x + i * step);
+  NormCols<NCH, KEEP> post, pre;
+  if constexpr (KEEP) {
+    post.load(a.post, 0, at * 8, at < chunks);
+    pre.load(a.pre, 0, at * 8, at < chunks);
+  }
   float f[NCH][8];
-  // f = N(f); chunks past the row stay zero until the affine part, which they skip
-  auto normalise = [&](const NormDev& n) {
+  // f = N(f); columns past the row are zero, and stay zero until the affine part
+  auto normalise = [&](const NormDev& n, NormCols<NCH, KEEP>& p) {
     if (n.kind == 0) return;
     if (n.kind == 2) {
       float s = 0.f;
@@ -72,9 +122,8 @@ __global__ void __launch_bounds__(WARP ? 32 * kNormWarps : 512) add_norm_kernel(
       const float mean = sum(s) * inv_c;
 #pragma unroll
       for (int i = 0; i < NCH; ++i)
-        if (at + T * i < chunks)
 #pragma unroll
-          for (int k = 0; k < 8; ++k) f[i][k] -= mean;
+        for (int k = 0; k < 8; ++k) f[i][k] = at + T * i < chunks ? f[i][k] - mean : 0.f;
     }
     float q = 0.f;
 #pragma unroll
@@ -84,57 +133,57 @@ __global__ void __launch_bounds__(WARP ? 32 * kNormWarps : 512) add_norm_kernel(
     const float rs = rsqrtf(sum(q) * inv_c + n.eps);
 #pragma unroll
     for (int i = 0; i < NCH; ++i) {
-      const int c = at + T * i;
-      if (c >= chunks) continue;
-      float w[8], b[8];
-      if (n.weight) load8<float>(n.weight + c * 8, w);
-      if (n.bias) load8<float>(n.bias + c * 8, b);
+      if constexpr (!KEEP) p.load(n, i, (at + T * i) * 8, at + T * i < chunks);
 #pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        float v = f[i][k] * rs;
-        if (n.weight) v *= w[k];
-        if (n.bias) v += b[k];
-        f[i][k] = v;
-      }
+      for (int k = 0; k < 8; ++k) f[i][k] = fmaf(f[i][k] * rs, p.w[KEEP ? i : 0][k], p.b[KEEP ? i : 0][k]);
     }
   };
-  pdl_wait();
-  pdl_trigger();
-  const int64_t step = (int64_t)gridDim.x * (WARP ? kNormWarps : 1);
-  for (int64_t r = WARP ? (int64_t)blockIdx.x * kNormWarps + warp : (int64_t)blockIdx.x; r < a.R; r += step) {
-    const RT* xr = static_cast<const RT*>(a.x) + r * C;
-    float x[NCH][8];
+  bool ok = true;
+  unsigned n = 0;
+  for (int64_t r = blockIdx.x; r < a.R; r += step, ++n) {
+    const uint8_t* stage = norm_smem + (n % S) * (xbytes + hbytes);
+    float g[8], x[NCH][8];
+    const float* gr = a.gate ? a.gate + (a.per == 0u ? 0ll : (int64_t)((uint32_t)r / a.per) * C) : nullptr;
+#pragma unroll
+    for (int i = 0; i < NCH; ++i) {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        g[k] = 1.f;
+        f[i][k] = x[i][k] = 0.f;
+      }
+      if (KEEP && gr && at < chunks) load8(gr + at * 8, g);
+    }
+    ok = mbar_wait(smem_u32(&s_full[n % S]), (n / S) & 1u, a.err, &s_abort, kErrTimeoutFull, limit) && ok;
 #pragma unroll
     for (int i = 0; i < NCH; ++i) {
       const int c = at + T * i;
-#pragma unroll
-      for (int k = 0; k < 8; ++k) f[i][k] = x[i][k] = 0.f;
       if (c < chunks) {
-        if (a.h) load8<__nv_bfloat16>(a.h + r * C + c * 8, f[i]);
-        if (a.x) load8<RT>(xr + c * 8, x[i]);
+        if (xbytes) read8(reinterpret_cast<const RT*>(stage) + c * 8, x[i]);
+        if (hbytes) read8(reinterpret_cast<const __nv_bfloat16*>(stage + xbytes) + c * 8, f[i]);
       }
     }
-    normalise(a.post);
-    const float* gr = a.gate ? a.gate + (a.per ? r / a.per : 0) * C : nullptr;
-    RT* rr = static_cast<RT*>(a.r) + r * C;
+    __syncthreads();  // everyone has read the stage
+    if (at == 0 && ok) fill(r + S * step);
+    normalise(a.post, post);
 #pragma unroll
     for (int i = 0; i < NCH; ++i) {
       const int c = at + T * i;
-      if (c >= chunks) continue;
-      float g[8];
-      if (gr) load8<float>(gr + c * 8, g);
+      if (!KEEP && gr && c < chunks) load8(gr + c * 8, g);
 #pragma unroll
-      for (int k = 0; k < 8; ++k) f[i][k] = fmaf(f[i][k], gr ? a.scale * g[k] : a.scale, x[i][k]);
-      if (a.r) store8(rr + c * 8, f[i]);
+      for (int k = 0; k < 8; ++k) f[i][k] = c < chunks ? fmaf(f[i][k], a.scale * g[k], x[i][k]) : 0.f;
+      if (a.r && c < chunks && ok) store8(static_cast<RT*>(a.r) + r * C + c * 8, f[i]);
     }
     if (!a.y) continue;
-    normalise(a.pre);
+    normalise(a.pre, pre);
 #pragma unroll
     for (int i = 0; i < NCH; ++i) {
       const int c = at + T * i;
-      if (c < chunks) store8(a.y + r * C + c * 8, f[i]);
+      if (c < chunks && ok) store8(a.y + r * C + c * 8, f[i]);
     }
   }
+  // after a timeout: no copy is in flight into shared memory that is given back
+  if (!ok && at == 0)
+    for (unsigned i = fills > S ? fills - S : 0u; i < fills; ++i) mbar_drain(smem_u32(&s_full[i % S]), (i / S) & 1u, limit);
 }
 
 // ---------------------------------------------------------------------------
@@ -227,17 +276,25 @@ __global__ void __launch_bounds__(kRopeThreads) rope_append_kernel(const __grid_
 
 template <typename RT>
 cudaError_t launch_add_norm_t(const AddNormArgs& a, cudaStream_t s) {
-  const int chunks = a.C / 8;
-  const int64_t most = (int64_t)1 << 30;
-  auto go = [&](auto kernel, int threads, int64_t grid) {
-    return launch_kernel(kernel, dim3((unsigned)(grid < most ? grid : most)), dim3((unsigned)threads), 0, s, a);
+  const int chunks = a.C / 8, nch = chunks <= 1024 ? 1 : 2;
+  const int threads = ((chunks + nch - 1) / nch + 31) / 32 * 32;
+  const size_t row = (size_t)a.C * ((a.x ? sizeof(RT) : 0) + (a.h ? 2 : 0)), most = 220 << 10;
+  AddNormArgs args = a;
+  args.stages = most / row < (size_t)kNormStages ? (int)(most / row) : kNormStages;  // (16384 fp32 values and their h: 2)
+  const size_t smem = args.stages * row;
+  // CTAs that fit an SM at once: 64 registers a thread, 2048 threads, 32 CTAs, shared memory
+  int fit = 1024 / threads;
+  if (fit > 32) fit = 32;
+  const int by_smem = (int)(most / (smem + 2048));
+  if (fit > by_smem) fit = by_smem;
+  if (fit < 1) fit = 1;
+  const int64_t grid = (int64_t)fit * device_sm_count();
+  auto go = [&](auto kernel) {
+    const cudaError_t e = smem_optin(reinterpret_cast<const void*>(kernel), smem);
+    if (e != cudaSuccess) return e;
+    return launch_kernel(kernel, dim3((unsigned)(grid < a.R ? grid : a.R)), dim3((unsigned)threads), smem, s, args);
   };
-  const int64_t wgrid = (a.R + kNormWarps - 1) / kNormWarps;
-  if (chunks <= 32) return go(add_norm_kernel<RT, 1, true>, 32 * kNormWarps, wgrid);
-  if (chunks <= 64) return go(add_norm_kernel<RT, 2, true>, 32 * kNormWarps, wgrid);
-  if (chunks <= 128) return go(add_norm_kernel<RT, 4, true>, 32 * kNormWarps, wgrid);
-  if (chunks <= 1024) return go(add_norm_kernel<RT, 2, false>, ((chunks + 1) / 2 + 31) / 32 * 32, a.R);
-  return go(add_norm_kernel<RT, 4, false>, ((chunks + 3) / 4 + 31) / 32 * 32, a.R);
+  return nch == 1 ? go(add_norm_kernel<RT, 1>) : go(add_norm_kernel<RT, 2>);
 }
 
 }  // namespace

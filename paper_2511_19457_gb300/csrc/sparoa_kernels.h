@@ -229,15 +229,18 @@ struct NormDev {
 struct AddNormArgs {
   const void* x = nullptr;            // [R, C] or null, bf16 or fp32
   const __nv_bfloat16* h = nullptr;   // [R, C] or null
-  int64_t R = 0;
+  int64_t R = 0;                      // below 2^31
   int C = 0;                          // % 8 == 0, <= 16384
   int res_f32 = 0;
   NormDev post, pre;
   const float* gate = nullptr;        // [R / per][C], or [C] with per = 0
-  int64_t per = 0;
+  uint32_t per = 0;
   float scale = 1.f;
   void* r = nullptr;                  // nullable, the type of x
   __nv_bfloat16* y = nullptr;         // nullable
+  int stages = 0;                     // rows on their way at once (set by launch_add_norm)
+  uint32_t* err = nullptr;            // bounded waits: error bits
+  long long wait_limit = 0;
 };
 cudaError_t launch_add_norm(const AddNormArgs& a, cudaStream_t s);
 
