@@ -18,52 +18,67 @@ namespace {
 // [8192, 4096] with both norms 102 us.)  Sums are fp32; a layer norm's variance is the mean
 // square of the deviations from the mean, not a difference of two sums.  y comes from the
 // fp32 r, not from the r that is stored.
-__device__ __forceinline__ void load8(const float* p, float (&f)[8]) {
+// V values at p as floats, 4 or 8: 16 bytes or fewer at once
+__device__ __forceinline__ void load_v(const float* p, float (&f)[4]) {
+  const float4 a = *reinterpret_cast<const float4*>(p);
+  f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w;
+}
+__device__ __forceinline__ void load_v(const float* p, float (&f)[8]) {
   const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
   f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w;
   f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
 }
-// 8 values from shared memory
-__device__ __forceinline__ void read8(const __nv_bfloat16* p, float (&f)[8]) {
+__device__ __forceinline__ void load_v(const __nv_bfloat16* p, float (&f)[8]) {
   unpack8(*reinterpret_cast<const uint4*>(p), f);
 }
-__device__ __forceinline__ void read8(const float* p, float (&f)[8]) { load8(p, f); }
-__device__ __forceinline__ void store8(__nv_bfloat16* p, const float (&f)[8]) {
+__device__ __forceinline__ void load_v(const __nv_bfloat16* p, float (&f)[4]) {
+  const uint2 u = *reinterpret_cast<const uint2*>(p);
+  f[0] = __uint_as_float(u.x << 16);
+  f[1] = __uint_as_float(u.x & 0xFFFF0000u);
+  f[2] = __uint_as_float(u.y << 16);
+  f[3] = __uint_as_float(u.y & 0xFFFF0000u);
+}
+__device__ __forceinline__ void store_v(__nv_bfloat16* p, const float (&f)[8]) {
   *reinterpret_cast<uint4*>(p) = pack8(f);
 }
-__device__ __forceinline__ void store8(float* p, const float (&f)[8]) {
+__device__ __forceinline__ void store_v(__nv_bfloat16* p, const float (&f)[4]) {
+  *reinterpret_cast<uint2*>(p) = make_uint2(act_pack2<0>(f[0], f[1]), act_pack2<0>(f[2], f[3]));
+}
+__device__ __forceinline__ void store_v(float* p, const float (&f)[4]) {
   *reinterpret_cast<float4*>(p) = make_float4(f[0], f[1], f[2], f[3]);
-  *reinterpret_cast<float4*>(p + 4) = make_float4(f[4], f[5], f[6], f[7]);
 }
 
 constexpr int kNormStages = 3;
 
-// A norm's parameters of a thread's 8 NCH columns: in registers, or read again for every
-// row (from L1) where there are too many.
-template <int NCH, bool KEEP>
+// A norm's parameters of a thread's NCH pieces of V columns: in registers, or read again
+// for every row (from L1) where there are too many.
+template <int V, int NCH, bool KEEP>
 struct NormCols {
-  float w[KEEP ? NCH : 1][8], b[KEEP ? NCH : 1][8];
+  float w[KEEP ? NCH : 1][V], b[KEEP ? NCH : 1][V];
   __device__ __forceinline__ void load(const NormDev& n, int i, int col, bool live) {
-    float (&ww)[8] = w[KEEP ? i : 0], (&bb)[8] = b[KEEP ? i : 0];
+    float (&ww)[V] = w[KEEP ? i : 0], (&bb)[V] = b[KEEP ? i : 0];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
+    for (int k = 0; k < V; ++k) {
       ww[k] = 1.f;
       bb[k] = 0.f;
     }
-    if (live && n.weight) load8(n.weight + col, ww);
-    if (live && n.bias) load8(n.bias + col, bb);
+    if (live && n.weight) load_v(n.weight + col, ww);
+    if (live && n.bias) load_v(n.bias + col, bb);
   }
 };
 
-template <typename RT, int NCH>
+// VALUES a thread in pieces of 16 bytes of the residual stream, so that a warp's accesses
+// are whole lines (fp32 in pieces of 8 values, two halves of a sector in turn: 83 us).
+template <typename RT, int VALUES>
 __global__ void __launch_bounds__(1024, 1) add_norm_kernel(const __grid_constant__ AddNormArgs a) {
-  constexpr bool KEEP = NCH == 1;
+  constexpr int V = 16 / sizeof(RT), NCH = VALUES / V;
+  constexpr bool KEEP = VALUES == 8;
   extern __shared__ __align__(128) uint8_t norm_smem[];  // stages: a row of x, a row of h
   __shared__ float s_sum[2][32];
   __shared__ __align__(8) unsigned long long s_full[kNormStages];
   __shared__ int s_abort;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, T = (int)blockDim.x, at = (int)threadIdx.x;
-  const int C = a.C, chunks = C / 8;
+  const int C = a.C, chunks = C / V;
   const float inv_c = 1.f / (float)C;
   const uint32_t xbytes = a.x ? (uint32_t)C * sizeof(RT) : 0u, hbytes = a.h ? (uint32_t)C * 2u : 0u;
   const long long limit = a.wait_limit ? a.wait_limit : kWaitLimitCycles;
@@ -104,62 +119,65 @@ __global__ void __launch_bounds__(1024, 1) add_norm_kernel(const __grid_constant
   const int64_t step = gridDim.x;
   if (at == 0)
     for (unsigned i = 0; i < S; ++i) fill(blockIdx.x + i * step);
-  NormCols<NCH, KEEP> post, pre;
+  NormCols<V, NCH, KEEP> post, pre;
   if constexpr (KEEP) {
-    post.load(a.post, 0, at * 8, at < chunks);
-    pre.load(a.pre, 0, at * 8, at < chunks);
+#pragma unroll
+    for (int i = 0; i < NCH; ++i) {
+      post.load(a.post, i, (at + T * i) * V, at + T * i < chunks);
+      pre.load(a.pre, i, (at + T * i) * V, at + T * i < chunks);
+    }
   }
-  float f[NCH][8];
+  float f[NCH][V];
   // f = N(f); columns past the row are zero, and stay zero until the affine part
-  auto normalise = [&](const NormDev& n, NormCols<NCH, KEEP>& p) {
+  auto normalise = [&](const NormDev& n, NormCols<V, NCH, KEEP>& p) {
     if (n.kind == 0) return;
     if (n.kind == 2) {
       float s = 0.f;
 #pragma unroll
       for (int i = 0; i < NCH; ++i)
 #pragma unroll
-        for (int k = 0; k < 8; ++k) s += f[i][k];
+        for (int k = 0; k < V; ++k) s += f[i][k];
       const float mean = sum(s) * inv_c;
 #pragma unroll
       for (int i = 0; i < NCH; ++i)
 #pragma unroll
-        for (int k = 0; k < 8; ++k) f[i][k] = at + T * i < chunks ? f[i][k] - mean : 0.f;
+        for (int k = 0; k < V; ++k) f[i][k] = at + T * i < chunks ? f[i][k] - mean : 0.f;
     }
     float q = 0.f;
 #pragma unroll
     for (int i = 0; i < NCH; ++i)
 #pragma unroll
-      for (int k = 0; k < 8; ++k) q = fmaf(f[i][k], f[i][k], q);
+      for (int k = 0; k < V; ++k) q = fmaf(f[i][k], f[i][k], q);
     const float rs = rsqrtf(sum(q) * inv_c + n.eps);
 #pragma unroll
     for (int i = 0; i < NCH; ++i) {
-      if constexpr (!KEEP) p.load(n, i, (at + T * i) * 8, at + T * i < chunks);
+      if constexpr (!KEEP) p.load(n, i, (at + T * i) * V, at + T * i < chunks);
 #pragma unroll
-      for (int k = 0; k < 8; ++k) f[i][k] = fmaf(f[i][k] * rs, p.w[KEEP ? i : 0][k], p.b[KEEP ? i : 0][k]);
+      for (int k = 0; k < V; ++k) f[i][k] = fmaf(f[i][k] * rs, p.w[KEEP ? i : 0][k], p.b[KEEP ? i : 0][k]);
     }
   };
   bool ok = true;
   unsigned n = 0;
   for (int64_t r = blockIdx.x; r < a.R; r += step, ++n) {
     const uint8_t* stage = norm_smem + (n % S) * (xbytes + hbytes);
-    float g[8], x[NCH][8];
+    float g[KEEP ? NCH : 1][V], x[NCH][V];
     const float* gr = a.gate ? a.gate + (a.per == 0u ? 0ll : (int64_t)((uint32_t)r / a.per) * C) : nullptr;
 #pragma unroll
     for (int i = 0; i < NCH; ++i) {
 #pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        g[k] = 1.f;
+      for (int k = 0; k < V; ++k) {
+        g[KEEP ? i : 0][k] = 1.f;
         f[i][k] = x[i][k] = 0.f;
       }
-      if (KEEP && gr && at < chunks) load8(gr + at * 8, g);
+      if (KEEP && gr && at + T * i < chunks) load_v(gr + (at + T * i) * V, g[KEEP ? i : 0]);
     }
     ok = mbar_wait(smem_u32(&s_full[n % S]), (n / S) & 1u, a.err, &s_abort, kErrTimeoutFull, limit) && ok;
 #pragma unroll
     for (int i = 0; i < NCH; ++i) {
       const int c = at + T * i;
       if (c < chunks) {
-        if (xbytes) read8(reinterpret_cast<const RT*>(stage) + c * 8, x[i]);
-        if (hbytes) read8(reinterpret_cast<const __nv_bfloat16*>(stage + xbytes) + c * 8, f[i]);
+        if (xbytes) load_v(reinterpret_cast<const RT*>(stage) + c * V, x[i]);
+        if (hbytes) load_v(reinterpret_cast<const __nv_bfloat16*>(stage + xbytes) + c * V, f[i]);
       }
     }
     __syncthreads();  // everyone has read the stage
@@ -168,17 +186,17 @@ __global__ void __launch_bounds__(1024, 1) add_norm_kernel(const __grid_constant
 #pragma unroll
     for (int i = 0; i < NCH; ++i) {
       const int c = at + T * i;
-      if (!KEEP && gr && c < chunks) load8(gr + c * 8, g);
+      if (!KEEP && gr && c < chunks) load_v(gr + c * V, g[0]);
 #pragma unroll
-      for (int k = 0; k < 8; ++k) f[i][k] = c < chunks ? fmaf(f[i][k], a.scale * g[k], x[i][k]) : 0.f;
-      if (a.r && c < chunks && ok) store8(static_cast<RT*>(a.r) + r * C + c * 8, f[i]);
+      for (int k = 0; k < V; ++k) f[i][k] = c < chunks ? fmaf(f[i][k], a.scale * g[KEEP ? i : 0][k], x[i][k]) : 0.f;
+      if (a.r && c < chunks && ok) store_v(static_cast<RT*>(a.r) + r * C + c * V, f[i]);
     }
     if (!a.y) continue;
     normalise(a.pre, pre);
 #pragma unroll
     for (int i = 0; i < NCH; ++i) {
       const int c = at + T * i;
-      if (c < chunks && ok) store8(a.y + r * C + c * 8, f[i]);
+      if (c < chunks && ok) store_v(a.y + r * C + c * V, f[i]);
     }
   }
   // after a timeout: no copy is in flight into shared memory that is given back
@@ -276,8 +294,8 @@ __global__ void __launch_bounds__(kRopeThreads) rope_append_kernel(const __grid_
 
 template <typename RT>
 cudaError_t launch_add_norm_t(const AddNormArgs& a, cudaStream_t s) {
-  const int chunks = a.C / 8, nch = chunks <= 1024 ? 1 : 2;
-  const int threads = ((chunks + nch - 1) / nch + 31) / 32 * 32;
+  const int values = a.C <= 8192 ? 8 : 16;  // a thread
+  const int threads = ((a.C + values - 1) / values + 31) / 32 * 32;
   const size_t row = (size_t)a.C * ((a.x ? sizeof(RT) : 0) + (a.h ? 2 : 0)), most = 220 << 10;
   AddNormArgs args = a;
   args.stages = most / row < (size_t)kNormStages ? (int)(most / row) : kNormStages;  // (16384 fp32 values and their h: 2)
@@ -294,7 +312,7 @@ cudaError_t launch_add_norm_t(const AddNormArgs& a, cudaStream_t s) {
     if (e != cudaSuccess) return e;
     return launch_kernel(kernel, dim3((unsigned)(grid < a.R ? grid : a.R)), dim3((unsigned)threads), smem, s, args);
   };
-  return nch == 1 ? go(add_norm_kernel<RT, 1>) : go(add_norm_kernel<RT, 2>);
+  return values == 8 ? go(add_norm_kernel<RT, 8>) : go(add_norm_kernel<RT, 16>);
 }
 
 }  // namespace
