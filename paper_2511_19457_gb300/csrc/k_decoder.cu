@@ -11,67 +11,68 @@ namespace {
 // Residual step: r = x + scale g N_post(h), y = N_pre(r), rows of C values.
 //
 // Bound by bytes: h and x are read once, r and y written once.  A CTA takes every
-// gridDim-th row, 8 values of it a thread (16 of rows beyond 8192): rows are on their way
-// into shared memory by bulk copies, up to kNormStages of them, while one is in registers between
-// its reductions, and the norms' parameters, which are a thread's for all its rows, stay in
-// registers.  (Rows loaded into registers by the CTA that reduces them, without any ahead:
-// [8192, 4096] with both norms 102 us.)  Sums are fp32; a layer norm's variance is the mean
-// square of the deviations from the mean, not a difference of two sums.  y comes from the
-// fp32 r, not from the r that is stored.
-// V values at p as floats, 4 or 8: 16 bytes or fewer at once
-__device__ __forceinline__ void load_v(const float* p, float (&f)[4]) {
-  const float4 a = *reinterpret_cast<const float4*>(p);
-  f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w;
+// gridDim-th row, 8 to 32 values of it a thread.  While a row is in registers the next
+// ones are on their way into shared memory by bulk copies, `stages` of them.  What is left
+// above the bytes is instructions, hence packed fp32 pairs and two 16-byte pieces of the
+// stream a thread: [8192, 4096] bf16 with a norm before the next block 106 us without rows
+// ahead, 58 with 8 values a thread unpacked, 46 so (5.9 TB/s); 59 with 32 values a thread
+// and a warp per 1024, for want of warps.  Requesting parameters into L1 ahead of their
+// use made every size slower.
+// Sums are fp32; a layer norm's variance is the mean square of the deviations from the
+// mean, not a difference of two sums.  y comes from the fp32 r, not from the r that is
+// stored.
+// 16 bytes of a row or, with 4 values, 8 (bf16) as packed fp32 pairs; zeros unless `live`
+__device__ __forceinline__ f2_t pair_of(uint32_t u) {
+  return f2(__uint_as_float(u << 16), __uint_as_float(u & 0xFFFF0000u));
 }
-__device__ __forceinline__ void load_v(const float* p, float (&f)[8]) {
-  const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
-  f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w;
-  f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
+__device__ __forceinline__ void load_p(const float* p, bool live, f2_t (&f)[2]) {
+  const float4 a = live ? *reinterpret_cast<const float4*>(p) : make_float4(0.f, 0.f, 0.f, 0.f);
+  f[0] = f2(a.x, a.y);
+  f[1] = f2(a.z, a.w);
 }
-__device__ __forceinline__ void load_v(const __nv_bfloat16* p, float (&f)[8]) {
-  unpack8(*reinterpret_cast<const uint4*>(p), f);
+__device__ __forceinline__ void load_p(const float* p, bool live, f2_t (&f)[4]) {
+  f2_t a[2], b[2];
+  load_p(p, live, a);
+  load_p(p + 4, live, b);
+  f[0] = a[0]; f[1] = a[1]; f[2] = b[0]; f[3] = b[1];
 }
-__device__ __forceinline__ void load_v(const __nv_bfloat16* p, float (&f)[4]) {
-  const uint2 u = *reinterpret_cast<const uint2*>(p);
-  f[0] = __uint_as_float(u.x << 16);
-  f[1] = __uint_as_float(u.x & 0xFFFF0000u);
-  f[2] = __uint_as_float(u.y << 16);
-  f[3] = __uint_as_float(u.y & 0xFFFF0000u);
+__device__ __forceinline__ void load_p(const __nv_bfloat16* p, bool live, f2_t (&f)[4]) {
+  const uint4 u = live ? *reinterpret_cast<const uint4*>(p) : make_uint4(0u, 0u, 0u, 0u);
+  f[0] = pair_of(u.x); f[1] = pair_of(u.y); f[2] = pair_of(u.z); f[3] = pair_of(u.w);
 }
-__device__ __forceinline__ void store_v(__nv_bfloat16* p, const float (&f)[8]) {
-  *reinterpret_cast<uint4*>(p) = pack8(f);
+__device__ __forceinline__ void load_p(const __nv_bfloat16* p, bool live, f2_t (&f)[2]) {
+  const uint2 u = live ? *reinterpret_cast<const uint2*>(p) : make_uint2(0u, 0u);
+  f[0] = pair_of(u.x);
+  f[1] = pair_of(u.y);
 }
-__device__ __forceinline__ void store_v(__nv_bfloat16* p, const float (&f)[4]) {
-  *reinterpret_cast<uint2*>(p) = make_uint2(act_pack2<0>(f[0], f[1]), act_pack2<0>(f[2], f[3]));
+__device__ __forceinline__ uint32_t rounded(f2_t v) {
+  float lo, hi;
+  f2_split(v, lo, hi);
+  return act_pack2<0>(lo, hi);
 }
-__device__ __forceinline__ void store_v(float* p, const float (&f)[4]) {
-  *reinterpret_cast<float4*>(p) = make_float4(f[0], f[1], f[2], f[3]);
+__device__ __forceinline__ void store_p(__nv_bfloat16* p, const f2_t (&f)[4]) {
+  *reinterpret_cast<uint4*>(p) = make_uint4(rounded(f[0]), rounded(f[1]), rounded(f[2]), rounded(f[3]));
+}
+__device__ __forceinline__ void store_p(__nv_bfloat16* p, const f2_t (&f)[2]) {
+  *reinterpret_cast<uint2*>(p) = make_uint2(rounded(f[0]), rounded(f[1]));
+}
+__device__ __forceinline__ void store_p(float* p, const f2_t (&f)[2]) {
+  float4 v;
+  f2_split(f[0], v.x, v.y);
+  f2_split(f[1], v.z, v.w);
+  *reinterpret_cast<float4*>(p) = v;
 }
 
-constexpr int kNormStages = 3;
-
-// A norm's parameters of a thread's NCH pieces of V columns: in registers, or read again
-// for every row (from L1) where there are too many.
-template <int V, int NCH, bool KEEP>
-struct NormCols {
-  float w[KEEP ? NCH : 1][V], b[KEEP ? NCH : 1][V];
-  __device__ __forceinline__ void load(const NormDev& n, int i, int col, bool live) {
-    float (&ww)[V] = w[KEEP ? i : 0], (&bb)[V] = b[KEEP ? i : 0];
-#pragma unroll
-    for (int k = 0; k < V; ++k) {
-      ww[k] = 1.f;
-      bb[k] = 0.f;
-    }
-    if (live && n.weight) load_v(n.weight + col, ww);
-    if (live && n.bias) load_v(n.bias + col, bb);
-  }
-};
+template <int VALUES>
+constexpr int kNormThreads = VALUES == 8 ? 1024 : 512;  // at most
+constexpr int kNormStages = 4;  // at most
 
 // VALUES a thread in pieces of 16 bytes of the residual stream, so that a warp's accesses
-// are whole lines (fp32 in pieces of 8 values, two halves of a sector in turn: 83 us).
+// are whole lines (fp32 in pieces of 8 values, two halves of a sector in turn, was slower
+// by a sixth).
 template <typename RT, int VALUES>
-__global__ void __launch_bounds__(1024, 1) add_norm_kernel(const __grid_constant__ AddNormArgs a) {
-  constexpr int V = 16 / sizeof(RT), NCH = VALUES / V;
+__global__ void __launch_bounds__(kNormThreads<VALUES>, VALUES <= 16 ? 1024 / kNormThreads<VALUES> : 1) add_norm_kernel(const __grid_constant__ AddNormArgs a) {
+  constexpr int V = 16 / sizeof(RT), NCH = VALUES / V, P = V / 2;
   constexpr bool KEEP = VALUES == 8;
   extern __shared__ __align__(128) uint8_t norm_smem[];  // stages: a row of x, a row of h
   __shared__ float s_sum[2][32];
@@ -91,6 +92,19 @@ __global__ void __launch_bounds__(1024, 1) add_norm_kernel(const __grid_constant
   __syncthreads();
   pdl_wait();
   pdl_trigger();
+  const int64_t step = gridDim.x;
+  unsigned fills = 0;
+  auto fill = [&](int64_t r) {  // by one thread: row r into the next stage
+    if (r >= a.R) return;
+    const uint32_t bar = smem_u32(&s_full[fills % S]);
+    const uint32_t dst = smem_u32(norm_smem) + (fills % S) * (xbytes + hbytes);
+    ++fills;
+    mbar_arrive_expect_tx(bar, xbytes + hbytes);
+    if (xbytes) bulk_load(dst, static_cast<const RT*>(a.x) + r * C, xbytes, bar);
+    if (hbytes) bulk_load(dst + xbytes, a.h + r * C, hbytes, bar);
+  };
+  if (at == 0)
+    for (unsigned i = 0; i < S; ++i) fill(blockIdx.x + i * step);
   int slot = 0;
   auto sum = [&](float v) {
 #pragma unroll
@@ -106,97 +120,120 @@ __global__ void __launch_bounds__(1024, 1) add_norm_kernel(const __grid_constant
     }
     return v;
   };
-  unsigned fills = 0;
-  auto fill = [&](int64_t r) {  // by one thread: row r into the next stage
-    if (r >= a.R) return;
-    const unsigned n = fills++;
-    const uint32_t bar = smem_u32(&s_full[n % S]);
-    const uint32_t dst = smem_u32(norm_smem) + (n % S) * (xbytes + hbytes);
-    mbar_arrive_expect_tx(bar, xbytes + hbytes);
-    if (xbytes) bulk_load(dst, static_cast<const RT*>(a.x) + r * C, xbytes, bar);
-    if (hbytes) bulk_load(dst + xbytes, a.h + r * C, hbytes, bar);
+  // the norms' weights of the thread's columns: in registers, or read again for every row
+  // (from L1) where there are too many
+  f2_t post_w[KEEP ? NCH : 1][P], pre_w[KEEP ? NCH : 1][P];
+  auto keep = [&](const NormDev& n, f2_t (&w)[KEEP ? NCH : 1][P]) {
+#pragma unroll
+    for (int i = 0; i < (KEEP ? NCH : 1); ++i) {
+#pragma unroll
+      for (int k = 0; k < P; ++k) w[i][k] = f2(1.f, 1.f);
+      if (n.weight) load_p(n.weight + (at + T * i) * V, at + T * i < chunks, w[i]);
+    }
   };
-  const int64_t step = gridDim.x;
-  if (at == 0)
-    for (unsigned i = 0; i < S; ++i) fill(blockIdx.x + i * step);
-  NormCols<V, NCH, KEEP> post, pre;
   if constexpr (KEEP) {
-#pragma unroll
-    for (int i = 0; i < NCH; ++i) {
-      post.load(a.post, i, (at + T * i) * V, at + T * i < chunks);
-      pre.load(a.pre, i, (at + T * i) * V, at + T * i < chunks);
-    }
+    keep(a.post, post_w);
+    keep(a.pre, pre_w);
   }
-  float f[NCH][V];
+  f2_t f[NCH][P];
   // f = N(f); columns past the row are zero, and stay zero until the affine part
-  auto normalise = [&](const NormDev& n, NormCols<V, NCH, KEEP>& p) {
+  auto normalise = [&](const NormDev& n, f2_t (&nw)[KEEP ? NCH : 1][P]) {
     if (n.kind == 0) return;
+    float lo, hi;
     if (n.kind == 2) {
-      float s = 0.f;
+      f2_t s = f[0][0];
 #pragma unroll
       for (int i = 0; i < NCH; ++i)
 #pragma unroll
-        for (int k = 0; k < V; ++k) s += f[i][k];
-      const float mean = sum(s) * inv_c;
+        for (int k = 0; k < P; ++k)
+          if (i + k > 0) s = fadd2(s, f[i][k]);
+      f2_split(s, lo, hi);
+      const float mean = sum(lo + hi) * -inv_c;
 #pragma unroll
       for (int i = 0; i < NCH; ++i)
+        if (at + T * i < chunks)
 #pragma unroll
-        for (int k = 0; k < V; ++k) f[i][k] = at + T * i < chunks ? f[i][k] - mean : 0.f;
+          for (int k = 0; k < P; ++k) f[i][k] = fadd2(f[i][k], f2(mean, mean));
     }
-    float q = 0.f;
+    f2_t q = fmul2(f[0][0], f[0][0]);
 #pragma unroll
     for (int i = 0; i < NCH; ++i)
 #pragma unroll
-      for (int k = 0; k < V; ++k) q = fmaf(f[i][k], f[i][k], q);
-    const float rs = rsqrtf(sum(q) * inv_c + n.eps);
+      for (int k = 0; k < P; ++k)
+        if (i + k > 0) q = ffma2(f[i][k], f[i][k], q);
+    f2_split(q, lo, hi);
+    const float rs = rsqrtf(sum(lo + hi) * inv_c + n.eps);
 #pragma unroll
     for (int i = 0; i < NCH; ++i) {
-      if constexpr (!KEEP) p.load(n, i, (at + T * i) * V, at + T * i < chunks);
+      const int c = at + T * i;
+      const bool live = c < chunks;
+      f2_t w[P];
 #pragma unroll
-      for (int k = 0; k < V; ++k) f[i][k] = fmaf(f[i][k] * rs, p.w[KEEP ? i : 0][k], p.b[KEEP ? i : 0][k]);
+      for (int k = 0; k < P; ++k) {
+        f[i][k] = fmul2(f[i][k], f2(rs, rs));
+        if constexpr (KEEP) f[i][k] = fmul2(f[i][k], nw[i][k]);
+      }
+      if (!KEEP && n.weight) {
+        load_p(n.weight + c * V, live, w);
+#pragma unroll
+        for (int k = 0; k < P; ++k) f[i][k] = fmul2(f[i][k], w[k]);
+      }
+      if (n.bias) {
+        load_p(n.bias + c * V, live, w);
+#pragma unroll
+        for (int k = 0; k < P; ++k) f[i][k] = fadd2(f[i][k], w[k]);
+      }
     }
   };
   bool ok = true;
-  unsigned n = 0;
-  for (int64_t r = blockIdx.x; r < a.R; r += step, ++n) {
-    const uint8_t* stage = norm_smem + (n % S) * (xbytes + hbytes);
-    float g[KEEP ? NCH : 1][V], x[NCH][V];
-    const float* gr = a.gate ? a.gate + (a.per == 0u ? 0ll : (int64_t)((uint32_t)r / a.per) * C) : nullptr;
-#pragma unroll
-    for (int i = 0; i < NCH; ++i) {
-#pragma unroll
-      for (int k = 0; k < V; ++k) {
-        g[KEEP ? i : 0][k] = 1.f;
-        f[i][k] = x[i][k] = 0.f;
-      }
-      if (KEEP && gr && at + T * i < chunks) load_v(gr + (at + T * i) * V, g[KEEP ? i : 0]);
-    }
-    ok = mbar_wait(smem_u32(&s_full[n % S]), (n / S) & 1u, a.err, &s_abort, kErrTimeoutFull, limit) && ok;
+  unsigned st = 0, phase = 0;
+  const f2_t scale = f2(a.scale, a.scale);
+#pragma unroll 1
+  for (int64_t r = blockIdx.x; r < a.R; r += step) {
+    const uint8_t* stage = norm_smem + st * (xbytes + hbytes);
+    f2_t x[NCH][P];
+    ok = mbar_wait(smem_u32(&s_full[st]), phase, a.err, &s_abort, kErrTimeoutFull, limit) && ok;
 #pragma unroll
     for (int i = 0; i < NCH; ++i) {
       const int c = at + T * i;
-      if (c < chunks) {
-        if (xbytes) load_v(reinterpret_cast<const RT*>(stage) + c * V, x[i]);
-        if (hbytes) load_v(reinterpret_cast<const __nv_bfloat16*>(stage + xbytes) + c * V, f[i]);
-      }
+      load_p(reinterpret_cast<const RT*>(stage) + c * V, c < chunks && xbytes, x[i]);
+      load_p(reinterpret_cast<const __nv_bfloat16*>(stage + xbytes) + c * V, c < chunks && hbytes, f[i]);
     }
-    __syncthreads();  // everyone has read the stage
+    if (T > 32)
+      __syncthreads();  // everyone has read the stage
+    else
+      __syncwarp();
     if (at == 0 && ok) fill(r + S * step);
-    normalise(a.post, post);
+    if (++st == S) {
+      st = 0;
+      phase ^= 1u;
+    }
+    normalise(a.post, post_w);
+    if (a.gate) {
+      const float* gr = a.gate + (a.per == 0u ? 0ll : (int64_t)((uint32_t)r / a.per) * C);
+#pragma unroll
+      for (int i = 0; i < NCH; ++i) {
+        const int c = at + T * i;
+        f2_t g[P];
+        load_p(gr + c * V, c < chunks, g);
+#pragma unroll
+        for (int k = 0; k < P; ++k) f[i][k] = fmul2(f[i][k], g[k]);
+      }
+    }
+    const int64_t row = r * C;
 #pragma unroll
     for (int i = 0; i < NCH; ++i) {
       const int c = at + T * i;
-      if (!KEEP && gr && c < chunks) load_v(gr + c * V, g[0]);
 #pragma unroll
-      for (int k = 0; k < V; ++k) f[i][k] = c < chunks ? fmaf(f[i][k], a.scale * g[KEEP ? i : 0][k], x[i][k]) : 0.f;
-      if (a.r && c < chunks && ok) store_v(static_cast<RT*>(a.r) + r * C + c * V, f[i]);
+      for (int k = 0; k < P; ++k) f[i][k] = ffma2(f[i][k], scale, x[i][k]);
+      if (a.r && c < chunks && ok) store_p(static_cast<RT*>(a.r) + row + c * V, f[i]);
     }
     if (!a.y) continue;
-    normalise(a.pre, pre);
+    normalise(a.pre, pre_w);
 #pragma unroll
     for (int i = 0; i < NCH; ++i) {
       const int c = at + T * i;
-      if (c < chunks && ok) store_v(a.y + r * C + c * V, f[i]);
+      if (c < chunks && ok) store_p(a.y + row + c * V, f[i]);
     }
   }
   // after a timeout: no copy is in flight into shared memory that is given back
@@ -294,25 +331,33 @@ __global__ void __launch_bounds__(kRopeThreads) rope_append_kernel(const __grid_
 
 template <typename RT>
 cudaError_t launch_add_norm_t(const AddNormArgs& a, cudaStream_t s) {
-  const int values = a.C <= 8192 ? 8 : 16;  // a thread
+  // two 16-byte pieces of the stream a thread ([8192, 4096] bf16 46 us, one 48; fp32 75,
+  // four 78), one of a short bf16 row, whose weights then stay in registers ([6304, 768]
+  // 12.9 us, two 14.2), and four or eight where threads run out
+  const int values = a.C > 8192 ? 32 : sizeof(RT) == 2 && a.C > 1024 ? 16 : 8;
   const int threads = ((a.C + values - 1) / values + 31) / 32 * 32;
-  const size_t row = (size_t)a.C * ((a.x ? sizeof(RT) : 0) + (a.h ? 2 : 0)), most = 220 << 10;
-  AddNormArgs args = a;
-  args.stages = most / row < (size_t)kNormStages ? (int)(most / row) : kNormStages;  // (16384 fp32 values and their h: 2)
-  const size_t smem = args.stages * row;
-  // CTAs that fit an SM at once: 64 registers a thread, 2048 threads, 32 CTAs, shared memory
-  int fit = 1024 / threads;
+  // CTAs that fit an SM at once (64 or 128 registers a thread, two rows each in shared memory),
+  // and the rows that each has on its way
+  const size_t row = (size_t)a.C * ((a.x ? sizeof(RT) : 0) + (a.h ? 2 : 0)), most = 216 << 10;
+  int fit = (values <= 16 ? 1024 : 512) / threads;
   if (fit > 32) fit = 32;
-  const int by_smem = (int)(most / (smem + 2048));
+  const int by_smem = (int)(most / (2 * row + 1536));
   if (fit > by_smem) fit = by_smem;
   if (fit < 1) fit = 1;
+  AddNormArgs args = a;
+  args.stages = (int)((most / fit - 1536) / row);
+  if (args.stages > kNormStages) args.stages = kNormStages;
+  const size_t smem = args.stages * row;
   const int64_t grid = (int64_t)fit * device_sm_count();
   auto go = [&](auto kernel) {
     const cudaError_t e = smem_optin(reinterpret_cast<const void*>(kernel), smem);
     if (e != cudaSuccess) return e;
     return launch_kernel(kernel, dim3((unsigned)(grid < a.R ? grid : a.R)), dim3((unsigned)threads), smem, s, args);
   };
-  return values == 8 ? go(add_norm_kernel<RT, 8>) : go(add_norm_kernel<RT, 16>);
+  if (values == 32) return go(add_norm_kernel<RT, 32>);
+  if constexpr (sizeof(RT) == 2)
+    if (values == 16) return go(add_norm_kernel<RT, 16>);
+  return go(add_norm_kernel<RT, 8>);
 }
 
 }  // namespace
