@@ -35,6 +35,7 @@ constexpr int kSoftWarps = 8;
 constexpr int kMmaWarp = 8, kLoadWarp = 9;
 constexpr int kThreads = 384;  // 12 warps: the last two only fill the third group of four
 constexpr float kSlackLog2 = 8.f;
+constexpr int kOutBytes = 32 * 64;  // 32 rows of 32 values
 constexpr int kExtra = 2;      // an item's beginning and end, in units
 using Cursor = PagedCursor<kRows, kExtra>;
 
@@ -119,7 +120,7 @@ struct Bars {
 
 // What the roles of a CTA share.
 struct Shared {
-  PagedPlan plan;
+  PagedPlan<kSoftWarps * kOutBytes> plan;  // scratch: each softmax warp's block of the result on its way out
   Bars bars;
   Cursor start;
   Cursor at[12], next[8];  // a warp's item, and the softmax warps' next one: in memory, their registers hold scores
@@ -337,17 +338,22 @@ __device__ __forceinline__ void softmax_role(const Role& r, uint32_t tmem) {
   const float sl2 = a.scale * 1.4426950408889634f, slack = kSlackLog2 / sl2;
   Cursor& c = r.sh.at[warp];
   Cursor& nx = r.sh.next[warp];
-  // this group's tile of Q of an item, if it has one: rows past the item's last are zero
+  // the warp's 32 rows of this group's tile of Q of an item, if it has one; rows past the
+  // item's last are zero.  Lanes side by side take a row's chunks (a row a lane was 32 lines
+  // an instruction, and 4000 cycles of the load-store unit an item)
   auto load_q = [&](const Cursor& k) {
     const int rows = r.rows(k) - grp * kTileRows;
     if (k.done() || rows <= 0) return false;
-    const bool live = row < rows;
-    const int at = live ? k.t * kRows + grp * kTileRows + row : 0, tok = over_group(a, at);
-    const __nv_bfloat16* p = a.q + (int64_t)(k.q0 + tok) * a.ld_q + (k.h * a.group + at - tok * a.group) * D;
     const uint32_t dst = r.sq + grp * C::kTile;
-#pragma unroll
-    for (int i = 0; i < D / 8; ++i)
-      cp_async_16(dst + (i >> 3) * C::kHalf + swz_offset<64>(row, i & 7), p + i * 8, live ? 16u : 0u);
+    const __nv_bfloat16* base = a.q + (int64_t)k.q0 * a.ld_q + k.h * a.group * D;
+#pragma unroll 4
+    for (int i = 0; i < D / 8; ++i) {
+      const int e = i * 32 + lane, ch = e % (D / 8), rr = (warp & 3) * 32 + e / (D / 8);
+      const bool live = rr < rows;
+      const int at = live ? k.t * kRows + grp * kTileRows + rr : 0, tok = over_group(a, at);
+      cp_async_16(dst + (ch >> 3) * C::kHalf + swz_offset<64>(rr, ch & 7),
+                  base + tok * a.ld_q + (at - tok * a.group) * D + ch * 8, live ? 16u : 0u);
+    }
     cp_async_commit();
     return true;
   };
@@ -505,32 +511,54 @@ __device__ __forceinline__ void softmax_role(const Role& r, uint32_t tmem) {
       const int64_t out = (int64_t)(c.q0 + of) * a.heads + c.h * a.group + (live ? c.t * kRows + at - of * a.group : 0);
       const float inv = l > 0.f ? 1.f / l : 0.f;
       if (!idle) {
+        // the results leave 32 values of 32 rows at a time, by way of shared memory, so that
+        // four lanes write 64 bytes of a row
+        const uint32_t mine = smem_u32(r.sh.plan.scratch) + warp * kOutBytes;
+        int64_t to_row[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) to_row[i] = __shfl_sync(0xffffffffu, live ? out : -1ll, i * 8 + (lane >> 2));
 #pragma unroll 1
-        for (int i = 0; i < D / 16; ++i) {
-          float o[16];
-          tmem_ld16(to + i * 16, o);
-          if (halves) {
-            float e[16];
-            tmem_ld16(to + D + i * 16, e);
+        for (int i = 0; i < D / 32; ++i) {
+          uint4 w[4];
 #pragma unroll
-            for (int k = 0; k < 16; ++k) o[k] = o[k] * f0 + e[k] * f1;
-          }
-          if (!live) continue;
-          if (part) {
-            // a part of the item: sums, maximum and sum of weights as they are
+          for (int h = 0; h < 2; ++h) {
+            float o[16];
+            tmem_ld16(to + i * 32 + h * 16, o);
+            if (halves) {
+              float e[16];
+              tmem_ld16(to + D + i * 32 + h * 16, e);
 #pragma unroll
-            for (int k = 0; k < 16; k += 4)
-              *reinterpret_cast<float4*>(slot + (size_t)((i * 16 + k) / 4 * kRows + at) * 4) =
-                  make_float4(o[k], o[k + 1], o[k + 2], o[k + 3]);
-          } else {
+              for (int k = 0; k < 16; ++k) o[k] = o[k] * f0 + e[k] * f1;
+            }
+            if (part) {
+              // a part of the item: sums, maximum and sum of weights as they are
+              if (live)
+#pragma unroll
+                for (int k = 0; k < 16; k += 4)
+                  *reinterpret_cast<float4*>(slot + (size_t)((i * 32 + h * 16 + k) / 4 * kRows + at) * 4) =
+                      make_float4(o[k], o[k + 1], o[k + 2], o[k + 3]);
+              continue;
+            }
 #pragma unroll
             for (int k = 0; k < 16; k += 8) {
               float f[8];
 #pragma unroll
               for (int e = 0; e < 8; ++e) f[e] = l > 0.f ? o[k + e] * inv : 0.f;
-              *reinterpret_cast<uint4*>(a.y + out * D + i * 16 + k) = pack8(f);
+              w[h * 2 + k / 8] = make_uint4(act_pack2<0>(f[0], f[1]), act_pack2<0>(f[2], f[3]), act_pack2<0>(f[4], f[5]),
+                                            act_pack2<0>(f[6], f[7]));
             }
           }
+          if (part) continue;
+#pragma unroll
+          for (int k = 0; k < 4; ++k) sts_u4(mine + sw64_offset(lane, k), w[k]);
+          __syncwarp();
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const float4 v = lds_f4(mine + sw64_offset(k * 8 + (lane >> 2), lane & 3));
+            if (to_row[k] >= 0)
+              *reinterpret_cast<float4*>(a.y + to_row[k] * D + i * 32 + (lane & 3) * 8) = v;
+          }
+          __syncwarp();
         }
         if (part) {
           slot[kRows * D + at] = m;

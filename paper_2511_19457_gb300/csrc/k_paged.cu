@@ -78,7 +78,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   using C = Cfg<D>;
   constexpr int S = C::kStages;
   extern __shared__ uint8_t smem_raw[];
-  __shared__ PagedPlan plan;
+  __shared__ PagedPlan<> plan;
   __shared__ Cursor s_start;
   __shared__ __align__(8) unsigned long long s_bar[kWarps][S];
   __shared__ float s_m[kWarps][kRows], s_l[kWarps][kRows];

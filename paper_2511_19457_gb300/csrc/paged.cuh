@@ -16,12 +16,17 @@ namespace sparoa {
 
 constexpr int kUnitKeys = 128;
 
-// The batch in shared memory: first row, new tokens, cached tokens and cost per key
-// head of each sequence.
+// The batch in shared memory: first row, new tokens and cached tokens of each sequence,
+// and until the CTAs have found their shares its cost per key head (SCRATCH bytes to use
+// afterwards).
+template <int SCRATCH = 16>
 struct PagedPlan {
   int q0[kPagedMaxBatch], n[kPagedMaxBatch], len[kPagedMaxBatch];
-  unsigned long long cost[kPagedMaxBatch];
   unsigned long long total;
+  union alignas(16) {
+    unsigned long long cost[kPagedMaxBatch];
+    uint8_t scratch[SCRATCH];
+  };
 };
 
 // Keys [lo, hi) that some row of tile t may see; hi <= lo: none.  units >= 1, so that
@@ -57,8 +62,8 @@ __device__ __forceinline__ TileKeys tile_keys(const PagedArgs& a, int n, int len
 // Fills the plan (all threads of the CTA; ends with a block barrier).  What the lists
 // say is brought into the tensors' bounds; where it is not there already, the error
 // bit is set.
-template <int RT, int EXTRA>
-__device__ __forceinline__ void make_plan(const PagedArgs& a, PagedPlan& p) {
+template <int RT, int EXTRA, typename Plan>
+__device__ __forceinline__ void make_plan(const PagedArgs& a, Plan& p) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
   if (threadIdx.x == 0) p.total = 0ull;
   __syncthreads();
@@ -116,7 +121,8 @@ struct PagedCursor {
   // whether other CTAs have units of the item
   __device__ __forceinline__ bool cut() const { return first > 0 || end < k.units; }
 
-  __device__ __forceinline__ void load_seq(const PagedArgs& a, const PagedPlan& p) {
+  template <typename Plan>
+  __device__ __forceinline__ void load_seq(const PagedArgs& a, const Plan& p) {
     q0 = p.q0[b];
     n = p.n[b];
     len = p.len[b];
@@ -128,7 +134,8 @@ struct PagedCursor {
     end = min(k.units, pos + left - EXTRA);  // (below `first`: the share ends in the item's beginning)
   }
   // to position u < total of the line, `cost` of which are to be walked (a converged warp)
-  __device__ __forceinline__ void seek(const PagedArgs& a, const PagedPlan& p, unsigned long long u, int cost) {
+  template <typename Plan>
+  __device__ __forceinline__ void seek(const PagedArgs& a, const Plan& p, unsigned long long u, int cost) {
     const int lane = threadIdx.x & 31;
     unsigned long long before = 0ull;  // cost of the sequences before b0
     int b0 = 0;
@@ -179,7 +186,8 @@ struct PagedCursor {
     enter(a);
   }
   // to the share's next item, if any (done() afterwards: none)
-  __device__ __forceinline__ void next_item(const PagedArgs& a, const PagedPlan& p) {
+  template <typename Plan>
+  __device__ __forceinline__ void next_item(const PagedArgs& a, const Plan& p) {
     left -= k.units + EXTRA - pos;
     if (left <= EXTRA) {
       blk = end;
@@ -189,14 +197,15 @@ struct PagedCursor {
       t = 0;
       if (++h == a.kv_heads) {
         h = 0;
-        do ++b; while (p.cost[b] == 0ull);  // (the line goes on: there is such a sequence)
+        do ++b; while (p.n[b] == 0);  // (the line goes on: there is such a sequence)
         load_seq(a, p);
       }
     }
     pos = 0;
     enter(a);
   }
-  __device__ __forceinline__ void next(const PagedArgs& a, const PagedPlan& p) {
+  template <typename Plan>
+  __device__ __forceinline__ void next(const PagedArgs& a, const Plan& p) {
     if (++blk >= end) next_item(a, p);
   }
 };
