@@ -36,8 +36,15 @@ constexpr int kMmaWarp = 8, kLoadWarp = 9;
 constexpr int kThreads = 384;  // 12 warps: the last two only fill the third group of four
 constexpr float kSlackLog2 = 8.f;
 constexpr int kOutBytes = 32 * 64;  // 32 rows of 32 values
-constexpr int kExtra = 2;      // an item's beginning and end, in units
-using Cursor = PagedCursor<kRows, kExtra>;
+
+// Steps of about 0.55 us, fitted to the CTAs' times: a unit of one tile 1.1 us, of two
+// tiles 1.5, an item's beginning and end 4.4.  (A join is 6, but items left whole so that
+// there is none keep some CTAs twice as long: [4 x 1000 tokens, window 1024] 23 -> 37 us.)
+struct ChunkCut {
+  static constexpr int ROWS = kRows, EXTRA = 8, MIN_SHARE = 8, WHOLE_SHARE = 0, WHOLE_MORE = 0;
+  static __device__ __forceinline__ int weight(int rows) { return rows > kTileRows ? 3 : 2; }
+};
+using Cursor = PagedCursor<ChunkCut>;
 
 template <int D>
 struct Cfg {
@@ -52,7 +59,7 @@ struct Cfg {
 };
 
 struct JoinItem {
-  int c0, c1, late;  // CTAs that share the item; late: its first part is CTA c0's second
+  int c0, c1;  // CTAs that share the item
   int q0, t, h, rows, valid;
 };
 
@@ -365,8 +372,8 @@ __device__ __forceinline__ void softmax_role(const Role& r, uint32_t tmem) {
   };
   if (load_q(c)) q_ready();
   unsigned sn = 0, on = 0, joins = 0;
-  bool ok = true, second = false;  // second: not this CTA's first item
-  for (; !c.done(); second = true) {
+  bool ok = true;
+  while (!c.done()) {
     r.next_item(nx, c);
     const int rows = r.rows(c), count = c.end - c.first;
     const bool two = rows > kTileRows;
@@ -506,7 +513,7 @@ __device__ __forceinline__ void softmax_role(const Role& r, uint32_t tmem) {
         m = top;
       }
       const bool part = c.cut();
-      float* slot = a.ws + (size_t)(2 * blockIdx.x + (second ? 1 : 0)) * C::kSlotFloats;
+      float* slot = a.ws + (size_t)part_slot(blockIdx.x, c.first == 0) * C::kSlotFloats;
       const int at = r0 + row, of = live ? over_group(a, c.t * kRows + at) : 0;
       const int64_t out = (int64_t)(c.q0 + of) * a.heads + c.h * a.group + (live ? c.t * kRows + at - of * a.group : 0);
       const float inv = l > 0.f ? 1.f / l : 0.f;
@@ -616,23 +623,22 @@ __global__ void __launch_bounds__(kThreads, 1)
   tc_fence_after();
   pdl_wait();
   pdl_trigger();
-  make_plan<kRows, kExtra>(a, sh.plan);
+  make_plan<ChunkCut>(a, sh.plan);
   const unsigned long long total = sh.plan.total;
-  const unsigned ctas = (unsigned)min((unsigned long long)gridDim.x, total);
+  const unsigned ctas = cut_ctas<ChunkCut>(total);
   const bool works = blockIdx.x < ctas;
   if (warp == 0) {
     JoinItem j{};
     if (works) {
       const unsigned long long u0 = cut_start(total, ctas, blockIdx.x), u1 = cut_start(total, ctas, blockIdx.x + 1);
       Cursor c;
-      c.seek(a, sh.plan, u0, (int)(u1 - u0));
+      c.seek(a, sh.plan, ctas, u0, (int)(u1 - u0));
       if (lane == 0) sh.start = c;
       // an item cut at this CTA's start is joined later; the first of its cuts speaks for it
-      if (c.first > 0) {
-        const PagedShares s = shares_of<kExtra>(total, ctas, u0 - c.pos, c.k.units);
+      if (!c.done() && c.first > 0) {
+        const PagedShares s = shares_of(c, total, ctas, u1);
         j.c0 = (int)s.c0;
         j.c1 = (int)s.c1;
-        j.late = s.late;
         j.q0 = c.q0;
         j.t = c.t;
         j.h = c.h;
@@ -679,7 +685,7 @@ __global__ void __launch_bounds__(4 * D)
   const int r = blockIdx.y * 32 + lane, parts = j.c1 - j.c0 + 1;
   if (!j.valid || (int)blockIdx.y * 32 >= j.rows) return;
   const bool live = r < j.rows;
-  auto slot = [&](int c) { return a.ws + (size_t)(2 * (j.c0 + c) + (c == 0 && j.late ? 1 : 0)) * C::kSlotFloats; };
+  auto slot = [&](int c) { return a.ws + (size_t)part_slot(j.c0 + c, c == 0) * C::kSlotFloats; };
   const float sl2 = a.scale * 1.4426950408889634f;
   float l = 0.f, mx = -INFINITY;
   for (int c = warp; c < parts; c += D / 8) s_w[c][lane] = live ? slot(c)[kRows * D + r] : -INFINITY;

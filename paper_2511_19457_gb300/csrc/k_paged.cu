@@ -24,10 +24,16 @@ constexpr int kRows = 16;     // rows of an item
 constexpr int kWarps = 8;
 constexpr int kThreads = 32 * kWarps;
 constexpr int kKeys = 16;     // a warp's keys of a unit
-constexpr int kExtra = 1;     // an item's beginning and end, in units
+
+// An item's beginning and end take as long as a unit; joining parts of an item as eight
+// units of a CTA that has few.
+struct SmallCut {
+  static constexpr int ROWS = kRows, EXTRA = 1, MIN_SHARE = 2, WHOLE_SHARE = 8, WHOLE_MORE = 8;
+  static __device__ __forceinline__ int weight(int) { return 1; }
+};
 static_assert(kKeys * kWarps == kUnitKeys, "unit");
 
-using Cursor = PagedCursor<kRows, kExtra>;
+using Cursor = PagedCursor<SmallCut>;
 
 template <int D>
 struct Cfg {
@@ -99,14 +105,14 @@ __global__ void __launch_bounds__(kThreads, 1)
   __syncthreads();
   pdl_wait();
   pdl_trigger();
-  make_plan<kRows, kExtra>(a, plan);
+  make_plan<SmallCut>(a, plan);
   const unsigned long long total = plan.total;
-  const unsigned ctas = (unsigned)min((unsigned long long)gridDim.x, total);
+  const unsigned ctas = cut_ctas<SmallCut>(total);
   if (blockIdx.x >= ctas) return;
   const unsigned long long u0 = cut_start(total, ctas, blockIdx.x), u1 = cut_start(total, ctas, blockIdx.x + 1);
   if (warp == 0) {
     Cursor c;
-    c.seek(a, plan, u0, (int)(u1 - u0));
+    c.seek(a, plan, ctas, u0, (int)(u1 - u0));
     if (lane == 0) s_start = c;
   }
   __syncthreads();
@@ -152,7 +158,6 @@ __global__ void __launch_bounds__(kThreads, 1)
   const int krow = ((lane >> 4) << 3) + (lane & 7), kch = (lane >> 3) & 1;
   const int vrow = (((lane >> 3) & 1) << 3) + (lane & 7), vch = lane >> 4;
 
-  bool second = false;  // not this CTA's first item
   for (; !cc.done(); cc.next(a, plan)) {
     fetch();
     const int rows = cc.n * a.group - cc.t * kRows;  // rows of the item (16 at most count)
@@ -321,8 +326,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       bool write = true;
       if (cc.cut()) {
         // shared with other CTAs: leave the partial result; the last to arrive joins them
-        const PagedShares sh = shares_of<kExtra>(total, ctas, u1 - cc.left - cc.pos, cc.k.units);
-        float* slot = a.ws + (size_t)(2 * blockIdx.x + (second ? 1 : 0)) * kSlotFloats<D>;
+        const PagedShares sh = shares_of(cc, total, ctas, u1);
+        float* slot = a.ws + (size_t)part_slot(blockIdx.x, cc.first == 0) * kSlotFloats<D>;
         if (mine_out) {
           float4* d = reinterpret_cast<float4*>(slot + row * D + piece * 8);
           d[0] = make_float4(acc[0], acc[1], acc[2], acc[3]);
@@ -354,7 +359,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
               for (int i = 0; i < kParts; ++i) {
                 const unsigned ci = min(c + i, sh.c1);
-                const float* p = a.ws + (size_t)(2 * ci + (ci == sh.c0 && sh.late ? 1 : 0)) * kSlotFloats<D>;
+                const float* p = a.ws + (size_t)part_slot(ci, ci == sh.c0) * kSlotFloats<D>;
                 pm[i] = __ldcg(p + kRows * D + row);
                 pl[i] = __ldcg(p + kRows * D + kRows + row);
                 v[i] = __ldcg(reinterpret_cast<const float4*>(p + row * D + piece * 8));
@@ -388,7 +393,6 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       __syncthreads();  // the free stages may be filled, s_m, s_l and s_at written again
       fresh = true;
-      second = true;
     }
   }
   // after a timeout: no copy is in flight into shared memory that is given back

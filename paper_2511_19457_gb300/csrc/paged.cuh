@@ -1,13 +1,17 @@
 // Work plan of attention over a paged cache, shared by its kernels.
 //
-// An item is one tile of RT query rows of one sequence and key head (row r of a
+// An item is one tile of ROWS query rows of one sequence and key head (row r of a
 // sequence: token r / group, query head key_head * group + r % group).  Its keys are
-// walked in units of 128; its cost is its units and EXTRA more for its beginning and
-// end.  The costs of all items, in the order (sequence, key head, tile), form one line
-// that the CTAs cut into equal shares: every CTA has as much to do as any other,
-// however ragged the batch, and at most its first and last item are shared with other
-// CTAs.  Lengths are on the device, so every CTA makes the plan itself (a load per
-// sequence and a scan).
+// walked in units of 128; its cost is a weight for each and EXTRA for its beginning and
+// end, in steps that a kernel's Cut states as measured.  The costs of all items, in the
+// order (sequence, key head, tile), form one line that the CTAs cut into equal shares:
+// every CTA has as much to do as any other, however ragged the batch, and at most its
+// first and last item are shared with other CTAs.  Shares are MIN_SHARE at least, which is
+// no less than a unit, so that no CTA between two others of an item has none of it.  Where
+// the shares are shorter than
+// WHOLE_SHARE, an item not much longer than one is not cut but goes to the CTA in whose
+// share it begins: joining its parts would take longer than they do.  Lengths are on the
+// device, so every CTA makes the plan itself (a load per sequence and a scan).
 #pragma once
 
 #include "sparoa_kernels.h"
@@ -40,13 +44,14 @@ __device__ __forceinline__ int over_group(const PagedArgs& a, int row) {
   return a.group == 1 ? row : (int)(__umulhi((unsigned)row, a.group_mul) >> a.group_shift);
 }
 
-template <int RT>
+template <typename Cut>
 __device__ __forceinline__ int tiles_of(int n, int group) {
-  return (n * group + RT - 1) / RT;  // (n * group is at most 2^30)
+  return (n * group + Cut::ROWS - 1) / Cut::ROWS;  // (n * group is at most 2^30)
 }
 
-template <int RT>
+template <typename Cut>
 __device__ __forceinline__ TileKeys tile_keys(const PagedArgs& a, int n, int len, int t) {
+  constexpr int RT = Cut::ROWS;
   TileKeys k;
   k.hi = len;
   if (a.causal) {
@@ -59,10 +64,16 @@ __device__ __forceinline__ TileKeys tile_keys(const PagedArgs& a, int n, int len
   return k;
 }
 
+// Cost of tile t.
+template <typename Cut>
+__device__ __forceinline__ int tile_cost(const PagedArgs& a, int n, int len, int t) {
+  return tile_keys<Cut>(a, n, len, t).units * Cut::weight(n * a.group - t * Cut::ROWS) + Cut::EXTRA;
+}
+
 // Fills the plan (all threads of the CTA; ends with a block barrier).  What the lists
 // say is brought into the tensors' bounds; where it is not there already, the error
 // bit is set.
-template <int RT, int EXTRA, typename Plan>
+template <typename Cut, typename Plan>
 __device__ __forceinline__ void make_plan(const PagedArgs& a, Plan& p) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
   if (threadIdx.x == 0) p.total = 0ull;
@@ -78,20 +89,20 @@ __device__ __forceinline__ void make_plan(const PagedArgs& a, Plan& p) {
       if (bad_rows) n = 0;
       len = len < 0 ? 0 : min(len, room);
     }
-    const int tiles = tiles_of<RT>((int)n, a.group);
+    const int tiles = tiles_of<Cut>((int)n, a.group);
     p.q0[b] = (int)q0;
     p.n[b] = (int)n;
     p.len[b] = (int)len;
-    p.cost[b] = tiles == 1 ? (unsigned long long)(tile_keys<RT>(a, (int)n, (int)len, 0).units + EXTRA) : 0ull;
+    p.cost[b] = tiles == 1 ? (unsigned long long)tile_cost<Cut>(a, (int)n, (int)len, 0) : 0ull;
     many |= tiles > 1;
     sum += p.cost[b] * a.kv_heads;
   }
   if (__syncthreads_or(many)) {
     for (int b = warp; b < a.batch; b += warps) {
-      const int n = p.n[b], len = p.len[b], tiles = tiles_of<RT>(n, a.group);
+      const int n = p.n[b], len = p.len[b], tiles = tiles_of<Cut>(n, a.group);
       if (tiles <= 1) continue;
       unsigned long long u = 0ull;
-      for (int t = lane; t < tiles; t += 32) u += (unsigned long long)(tile_keys<RT>(a, n, len, t).units + EXTRA);
+      for (int t = lane; t < tiles; t += 32) u += (unsigned long long)tile_cost<Cut>(a, n, len, t);
 #pragma unroll
       for (int d = 16; d > 0; d >>= 1) u += __shfl_xor_sync(0xffffffffu, u, d);
       if (lane == 0) {
@@ -107,12 +118,14 @@ __device__ __forceinline__ void make_plan(const PagedArgs& a, Plan& p) {
 }
 
 // A walk over one CTA's share of the line, the same in all lanes of a warp.
-template <int RT, int EXTRA>
+template <typename Cut>
 struct PagedCursor {
   int b, h, t, tiles;
   int q0, n, len;
   TileKeys k;
+  int weight;        // of a unit of the item
   int pos, left;     // where the share enters the item's cost, and the share's cost from there
+  int whole;         // items of at most this cost are not cut
   int first, end;    // the share's units of the item
   int blk;           // unit, first to end - 1; at `end`: nothing left
 
@@ -126,16 +139,26 @@ struct PagedCursor {
     q0 = p.q0[b];
     n = p.n[b];
     len = p.len[b];
-    tiles = tiles_of<RT>(n, a.group);
+    tiles = tiles_of<Cut>(n, a.group);
   }
+  // a unit belongs to the share that has the first step of its cost
+  __device__ __forceinline__ int unit_at(int at) const { return max(0, at - Cut::EXTRA + weight - 1) / weight; }
   __device__ __forceinline__ void enter(const PagedArgs& a) {
-    k = tile_keys<RT>(a, n, len, t);
-    first = blk = max(0, pos - EXTRA);
-    end = min(k.units, pos + left - EXTRA);  // (below `first`: the share ends in the item's beginning)
+    k = tile_keys<Cut>(a, n, len, t);
+    weight = Cut::weight(n * a.group - t * Cut::ROWS);
+    if (cost() <= whole) {
+      first = pos == 0 ? 0 : k.units;
+      end = k.units;
+    } else {
+      first = unit_at(pos);
+      end = min(k.units, unit_at(pos + left));
+    }
+    blk = first;
   }
-  // to position u < total of the line, `cost` of which are to be walked (a converged warp)
+  __device__ __forceinline__ int cost() const { return k.units * weight + Cut::EXTRA; }
+  // to position u < total of the line, `steps` of which are to be walked (a converged warp)
   template <typename Plan>
-  __device__ __forceinline__ void seek(const PagedArgs& a, const Plan& p, unsigned long long u, int cost) {
+  __device__ __forceinline__ void seek(const PagedArgs& a, const Plan& p, unsigned ctas, unsigned long long u, int steps) {
     const int lane = threadIdx.x & 31;
     unsigned long long before = 0ull;  // cost of the sequences before b0
     int b0 = 0;
@@ -164,7 +187,7 @@ struct PagedCursor {
     t = 0;
     if (tiles > 1) {
       for (int t0 = 0;; t0 += 32) {
-        const unsigned mine = t0 + lane < tiles ? (unsigned)(tile_keys<RT>(a, n, len, t0 + lane).units + EXTRA) : 0u;
+        const unsigned mine = t0 + lane < tiles ? (unsigned)tile_cost<Cut>(a, n, len, t0 + lane) : 0u;
         unsigned incl = mine;
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
@@ -182,27 +205,32 @@ struct PagedCursor {
       }
     }
     pos = (int)rem;
-    left = cost;
+    left = steps;
+    whole = p.total < (unsigned long long)Cut::WHOLE_SHARE * ctas ? (int)(p.total / ctas) + Cut::WHOLE_MORE : 0;
     enter(a);
+    if (done()) next_item(a, p);
   }
-  // to the share's next item, if any (done() afterwards: none)
+  // to the share's next item that has units of it, if any (done() afterwards: none)
   template <typename Plan>
   __device__ __forceinline__ void next_item(const PagedArgs& a, const Plan& p) {
-    left -= k.units + EXTRA - pos;
-    if (left <= EXTRA) {
-      blk = end;
-      return;
-    }
-    if (++t == tiles) {
-      t = 0;
-      if (++h == a.kv_heads) {
-        h = 0;
-        do ++b; while (p.n[b] == 0);  // (the line goes on: there is such a sequence)
-        load_seq(a, p);
+    for (;;) {
+      left -= cost() - pos;
+      if (left <= 0) {
+        blk = end;
+        return;
       }
+      if (++t == tiles) {
+        t = 0;
+        if (++h == a.kv_heads) {
+          h = 0;
+          do ++b; while (p.n[b] == 0);  // (the line goes on: there is such a sequence)
+          load_seq(a, p);
+        }
+      }
+      pos = 0;
+      enter(a);
+      if (!done()) return;
     }
-    pos = 0;
-    enter(a);
   }
   template <typename Plan>
   __device__ __forceinline__ void next(const PagedArgs& a, const Plan& p) {
@@ -210,6 +238,11 @@ struct PagedCursor {
   }
 };
 
+// CTAs that get a share.
+template <typename Cut>
+__device__ __forceinline__ unsigned cut_ctas(unsigned long long total) {
+  return total < Cut::MIN_SHARE ? (unsigned)(total > 0) : (unsigned)min((unsigned long long)gridDim.x, total / Cut::MIN_SHARE);
+}
 // The line's cut: CTA c of `ctas` has positions [c total / ctas, (c + 1) total / ctas).
 __device__ __forceinline__ unsigned long long cut_start(unsigned long long total, unsigned ctas, unsigned c) {
   return total * c / ctas;
@@ -218,20 +251,23 @@ __device__ __forceinline__ unsigned long long cut_start(unsigned long long total
 __device__ __forceinline__ unsigned cut_owner(unsigned long long total, unsigned ctas, unsigned long long u) {
   return (unsigned)(((u + 1) * ctas - 1) / total);
 }
-// The CTAs c0 to c1 that share an item of `units` units at position i0 of the line; late:
-// c0 has had another item before it.
+// The CTAs that have the first and the last unit of the item of place c, whose share ends
+// at position `until`.
 struct PagedShares {
   unsigned c0, c1;
-  bool late;
 };
-template <int EXTRA>
-__device__ __forceinline__ PagedShares shares_of(unsigned long long total, unsigned ctas, unsigned long long i0, int units) {
+template <typename Cut>
+__device__ __forceinline__ PagedShares shares_of(const PagedCursor<Cut>& c, unsigned long long total, unsigned ctas,
+                                                 unsigned long long until) {
+  const unsigned long long first = until - c.left - c.pos + Cut::EXTRA;
   PagedShares s;
-  s.c0 = cut_owner(total, ctas, i0 + EXTRA);  // (who has the item's first unit)
-  s.c1 = cut_owner(total, ctas, i0 + EXTRA + units - 1);
-  s.late = i0 > cut_start(total, ctas, s.c0);
+  s.c0 = cut_owner(total, ctas, first);
+  s.c1 = cut_owner(total, ctas, first + (unsigned long long)(c.k.units - 1) * c.weight);
   return s;
 }
+// Where CTA c leaves its part of an item: a CTA has at most one part that another began
+// (its first item's end) and one that another ends (its last item's beginning).
+__device__ __forceinline__ unsigned part_slot(unsigned c, bool begins) { return 2u * c + (begins ? 1u : 0u); }
 
 // Page of key `key` of sequence b, brought into the pool's bounds.
 __device__ __forceinline__ int page_of(const PagedArgs& a, int b, int key) {
