@@ -25,10 +25,11 @@ constexpr int kWarps = 8;
 constexpr int kThreads = 32 * kWarps;
 constexpr int kKeys = 16;     // a warp's keys of a unit
 
-// An item's beginning and end take as long as a unit; joining parts of an item as eight
+// An item's beginning and end take as long as one unit to three (64 contexts of 500 to
+// 16000 tokens: 188 us with 1 and with 3, 185 with 2); joining parts of an item as eight
 // units of a CTA that has few.
 struct SmallCut {
-  static constexpr int ROWS = kRows, EXTRA = 1, MIN_SHARE = 2, WHOLE_SHARE = 8, WHOLE_MORE = 8;
+  static constexpr int ROWS = kRows, EXTRA = 2, MIN_SHARE = 2, WHOLE_SHARE = 8, WHOLE_MORE = 8;
   static __device__ __forceinline__ int weight(int) { return 1; }
 };
 static_assert(kKeys * kWarps == kUnitKeys, "unit");
@@ -348,7 +349,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (mine_out) {
             // kParts parts' loads are on their way at once (one after the other, 19 parts
             // of a sequence over the whole GPU took 15 us, now 4)
-            constexpr int kParts = 8;
+            constexpr int kParts = 10;
             mx = -INFINITY;
             ls = 0.f;
 #pragma unroll

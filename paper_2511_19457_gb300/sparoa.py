@@ -200,15 +200,19 @@ class Context:
         if st != OK:
             raise SparoaError(st, "sparoa_create")
         self.h = h
+        self._stream = None  # the stream that the context was last set to
 
     def _check(self, st):
         if st != OK:
             raise SparoaError(st, _lib.sparoa_last_error(self.h).decode())
 
     def _bind(self):
-        st = _set_stream(self.h, _raw_stream(self.device))
-        if st != OK:
-            self._check(st)
+        s = _raw_stream(self.device)
+        if s != self._stream:  # (0.4 us of host time a call otherwise)
+            st = _set_stream(self.h, s)
+            if st != OK:
+                self._check(st)
+            self._stream = s
 
     def close(self):
         if getattr(self, "h", None):
@@ -437,9 +441,11 @@ def sparoa_add_norm(ctx: Context, x, h, r=None, y=None, post: Norm | None = None
     R = lead.numel() // C if C else 0
     stream = r if x is None else x
     res = _f32 if stream is not None and stream.dtype is _f32 else _bf16
-    for t, dt in ((x, res), (r, res), (h, _bf16), (y, _bf16)):
-        if t is not None and not (t.dtype is dt and t.is_cuda and t.is_contiguous() and t.shape == shape):
-            _refuse("add_norm: contiguous CUDA tensors of one shape wanted: x and r of one type, h and y bf16")
+    if not ((x is None or (x.dtype is res and x.is_cuda and x.is_contiguous())) and
+            (h is None or (h.dtype is _bf16 and h.is_cuda and h.is_contiguous() and h.shape == shape)) and
+            (r is None or (r.dtype is res and r.is_cuda and r.is_contiguous() and r.shape == shape)) and
+            (y is None or (y.dtype is _bf16 and y.is_cuda and y.is_contiguous() and y.shape == shape))):
+        _refuse("add_norm: contiguous CUDA tensors of one shape wanted: x and r of one type, h and y bf16")
     if (post is not None and post.C not in (0, C)) or (pre is not None and pre.C not in (0, C)):
         _refuse("add_norm: norm parameters of another length")
     if gate is not None:
