@@ -32,7 +32,7 @@ namespace {
 constexpr int kRows = 256;     // rows of an item
 constexpr int kTileRows = 128;
 constexpr int kSoftWarps = 8;
-constexpr int kMmaWarp = 8, kLoadWarp = 9;
+constexpr int kMmaWarp = 8, kLoadWarp = 9, kJoinWarp = 10;
 constexpr int kThreads = 384;  // 12 warps: the last two only fill the third group of four
 constexpr float kSlackLog2 = 8.f;
 constexpr int kOutBytes = 32 * 64;  // 32 rows of 32 values
@@ -517,69 +517,81 @@ __device__ __forceinline__ void softmax_role(const Role& r, uint32_t tmem) {
       const int at = r0 + row, of = live ? over_group(a, c.t * kRows + at) : 0;
       const int64_t out = (int64_t)(c.q0 + of) * a.heads + c.h * a.group + (live ? c.t * kRows + at - of * a.group : 0);
       const float inv = l > 0.f ? 1.f / l : 0.f;
-      if (!idle) {
-        // the results leave 32 values of 32 rows at a time, by way of shared memory, so that
-        // four lanes write 64 bytes of a row
-        const uint32_t mine = smem_u32(r.sh.plan.scratch) + warp * kOutBytes;
-        int64_t to_row[4];
+      const uint32_t mine = smem_u32(r.sh.plan.scratch) + warp * kOutBytes;
+      int64_t to_row[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) to_row[i] = __shfl_sync(0xffffffffu, live ? out : -1ll, i * 8 + (lane >> 2));
-#pragma unroll 1
-        for (int i = 0; i < D / 32; ++i) {
-          uint4 w[4];
+      for (int i = 0; i < 4; ++i) to_row[i] = __shfl_sync(0xffffffffu, live ? out : -1ll, i * 8 + (lane >> 2));
+      // values [32 i, 32 i + 32) of the rows: to the workspace as they are (a part of the
+      // item), or divided, by way of shared memory, so that four lanes write 64 bytes of a row
+      auto put = [&](int i, const uint32_t (&o)[32]) {
+        if (part) {
+          if (live)
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            float o[16];
-            tmem_ld16(to + i * 32 + h * 16, o);
-            if (halves) {
-              float e[16];
-              tmem_ld16(to + D + i * 32 + h * 16, e);
-#pragma unroll
-              for (int k = 0; k < 16; ++k) o[k] = o[k] * f0 + e[k] * f1;
-            }
-            if (part) {
-              // a part of the item: sums, maximum and sum of weights as they are
-              if (live)
-#pragma unroll
-                for (int k = 0; k < 16; k += 4)
-                  *reinterpret_cast<float4*>(slot + (size_t)((i * 32 + h * 16 + k) / 4 * kRows + at) * 4) =
-                      make_float4(o[k], o[k + 1], o[k + 2], o[k + 3]);
-              continue;
-            }
-#pragma unroll
-            for (int k = 0; k < 16; k += 8) {
-              float f[8];
-#pragma unroll
-              for (int e = 0; e < 8; ++e) f[e] = l > 0.f ? o[k + e] * inv : 0.f;
-              w[h * 2 + k / 8] = make_uint4(act_pack2<0>(f[0], f[1]), act_pack2<0>(f[2], f[3]), act_pack2<0>(f[4], f[5]),
-                                            act_pack2<0>(f[6], f[7]));
-            }
-          }
-          if (part) continue;
-#pragma unroll
-          for (int k = 0; k < 4; ++k) sts_u4(mine + sw64_offset(lane, k), w[k]);
-          __syncwarp();
-#pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            const float4 v = lds_f4(mine + sw64_offset(k * 8 + (lane >> 2), lane & 3));
-            if (to_row[k] >= 0)
-              *reinterpret_cast<float4*>(a.y + to_row[k] * D + i * 32 + (lane & 3) * 8) = v;
-          }
-          __syncwarp();
+            for (int k = 0; k < 32; k += 4)
+              *reinterpret_cast<uint4*>(slot + (size_t)((i * 32 + k) / 4 * kRows + at) * 4) =
+                  make_uint4(o[k], o[k + 1], o[k + 2], o[k + 3]);
+          return;
         }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          uint32_t w[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float lo = __uint_as_float(o[k * 8 + 2 * e]) * inv, hi = __uint_as_float(o[k * 8 + 2 * e + 1]) * inv;
+            w[e] = l > 0.f ? act_pack2<0>(lo, hi) : 0u;
+          }
+          sts_u4(mine + sw64_offset(lane, k), make_uint4(w[0], w[1], w[2], w[3]));
+        }
+        __syncwarp();
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const float4 v = lds_f4(mine + sw64_offset(k * 8 + (lane >> 2), lane & 3));
+          if (to_row[k] >= 0) *reinterpret_cast<float4*>(a.y + to_row[k] * D + i * 32 + (lane & 3) * 8) = v;
+        }
+        __syncwarp();
+      };
+      auto give_back = [&]() {  // O has been read: the next item's products may begin
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) {
+          mbar_arrive(smem_u32(&bars.o_free[grp]));
+          if (halves) mbar_arrive(smem_u32(&bars.o_free[1]));
+        }
+      };
+      if (!halves && !idle) {
+        uint32_t o[D / 32][32];
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i) tmem_ld32_nowait(to + i * 32, o[i]);
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i) tmem_wait_ld32(o[i]);
+        give_back();
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i) put(i, o[i]);
+      } else {
+        if (!idle) {
+#pragma unroll 1
+          for (int i = 0; i < D / 32; ++i) {
+            uint32_t o[32], e[32];
+            tmem_ld32_nowait(to + i * 32, o);
+            tmem_ld32_nowait(to + D + i * 32, e);
+            tmem_wait_ld32(o);
+            tmem_wait_ld32(e);
+#pragma unroll
+            for (int k = 0; k < 32; ++k)
+              o[k] = __float_as_uint(__uint_as_float(o[k]) * f0 + __uint_as_float(e[k]) * f1);
+            put(i, o);
+          }
+        }
+        if (loading) q_ready();
+        give_back();
+      }
+      if (!idle) {
         if (part) {
           slot[kRows * D + at] = m;
           slot[kRows * D + kRows + at] = l;
         } else if (live && a.lse) {
           a.lse[out] = l > 0.f ? fmaf(m, a.scale, logf(l)) : -INFINITY;
         }
-      }
-      if (loading) q_ready();
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) {
-        mbar_arrive(smem_u32(&bars.o_free[grp]));
-        if (halves) mbar_arrive(smem_u32(&bars.o_free[1]));
       }
     }
     __syncwarp();
@@ -627,30 +639,32 @@ __global__ void __launch_bounds__(kThreads, 1)
   const unsigned long long total = sh.plan.total;
   const unsigned ctas = cut_ctas<ChunkCut>(total);
   const bool works = blockIdx.x < ctas;
-  if (warp == 0) {
-    JoinItem j{};
-    if (works) {
-      const unsigned long long u0 = cut_start(total, ctas, blockIdx.x), u1 = cut_start(total, ctas, blockIdx.x + 1);
-      Cursor c;
-      c.seek(a, sh.plan, ctas, u0, (int)(u1 - u0));
-      if (lane == 0) sh.start = c;
-      // an item cut at this CTA's start is joined later; the first of its cuts speaks for it
-      if (!c.done() && c.first > 0) {
-        const PagedShares s = shares_of(c, total, ctas, u1);
-        j.c0 = (int)s.c0;
-        j.c1 = (int)s.c1;
-        j.q0 = c.q0;
-        j.t = c.t;
-        j.h = c.h;
-        j.rows = min(kRows, c.n * a.group - c.t * kRows);
-        j.valid = s.c0 + 1 == blockIdx.x;
-      }
-    }
-    if (lane == 0) reinterpret_cast<JoinItem*>(a.ws + (size_t)2 * gridDim.x * C::kSlotFloats)[blockIdx.x] = j;
+  const unsigned long long u0 = works ? cut_start(total, ctas, blockIdx.x) : 0ull;
+  const unsigned long long u1 = works ? cut_start(total, ctas, blockIdx.x + 1) : 0ull;
+  if (warp == 0 && works) {
+    Cursor c;
+    c.seek(a, sh.plan, ctas, u0, (int)(u1 - u0));
+    if (lane == 0) sh.start = c;
   }
   __syncthreads();
   if (works && lane == 0) sh.at[warp] = sh.start;
   __syncwarp();
+  if (warp == kJoinWarp && lane == 0) {
+    // an item cut at this CTA's start is joined later; the first of its cuts speaks for it
+    JoinItem j{};
+    if (works && !sh.start.done() && sh.start.first > 0) {
+      const Cursor& c = sh.start;
+      const PagedShares s = shares_of(c, total, ctas, u1);
+      j.c0 = (int)s.c0;
+      j.c1 = (int)s.c1;
+      j.q0 = c.q0;
+      j.t = c.t;
+      j.h = c.h;
+      j.rows = min(kRows, c.n * a.group - c.t * kRows);
+      j.valid = s.c0 + 1 == blockIdx.x;
+    }
+    reinterpret_cast<JoinItem*>(a.ws + (size_t)2 * gridDim.x * C::kSlotFloats)[blockIdx.x] = j;
+  }
   const uint32_t sq = (smem_u32(smem_raw) + 1023u) & ~1023u;
   const Role r{a, sh, sq, sq + 2 * C::kTile, a.wait_limit ? a.wait_limit : kWaitLimitCycles};
   if (warp < kSoftWarps) {
@@ -668,16 +682,16 @@ __global__ void __launch_bounds__(kThreads, 1)
 }
 
 // Joins the parts of the items that several CTAs shared, in the order of their keys: a
-// block per cut and 32 rows, a warp per 8 columns and D / 8 warps.  Bound by latency: the
-// statistics of all parts are loaded at once, then their sums four parts at a time
-// (part after part, each waiting for the one before it, 10 parts took 15 us, now 4).
+// block per cut and 32 rows, a warp per 8 columns and D / 8 warps.  Bound by latency, so the
+// statistics of all parts and the sums of the first four are asked for at once, then four
+// parts at a time (part after part, each waiting for the one before it, 10 took 15 us).
 constexpr int kJoinParts = 4;
+constexpr int kCtas = 184;  // at most: the join keeps statistics of as many parts in shared memory
 template <int D>
 __global__ void __launch_bounds__(4 * D)
     paged_join_kernel(const __grid_constant__ PagedArgs a, int grid) {
   using C = Cfg<D>;
-  __shared__ float s_w[kPagedCounters][32];  // maxima, then weights of the parts
-  __shared__ float s_l[D / 8][32];
+  __shared__ float s_w[kCtas][32], s_l[kCtas][32];  // maxima and sums of weights of the parts
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   pdl_wait();
   pdl_trigger();
@@ -687,34 +701,36 @@ __global__ void __launch_bounds__(4 * D)
   const bool live = r < j.rows;
   auto slot = [&](int c) { return a.ws + (size_t)part_slot(j.c0 + c, c == 0) * C::kSlotFloats; };
   const float sl2 = a.scale * 1.4426950408889634f;
-  float l = 0.f, mx = -INFINITY;
-  for (int c = warp; c < parts; c += D / 8) s_w[c][lane] = live ? slot(c)[kRows * D + r] : -INFINITY;
-  __syncthreads();
-  for (int c = 0; c < parts; ++c) mx = fmaxf(mx, s_w[c][lane]);
-  __syncthreads();
+  float4 p[kJoinParts], q[kJoinParts];
+  auto fetch = [&](int c0) {
+#pragma unroll
+    for (int i = 0; i < kJoinParts; ++i) {
+      const float* from = slot(min(c0 + i, parts - 1)) + (size_t)(live ? r : 0) * 4;
+      p[i] = *reinterpret_cast<const float4*>(from + (size_t)(2 * warp) * kRows * 4);
+      q[i] = *reinterpret_cast<const float4*>(from + (size_t)(2 * warp + 1) * kRows * 4);
+    }
+  };
+  fetch(0);
   for (int c = warp; c < parts; c += D / 8) {
-    const float m = s_w[c][lane], w = m == -INFINITY ? 0.f : ex2((m - mx) * sl2);
-    s_w[c][lane] = w;
-    if (live) l = fmaf(w, slot(c)[kRows * D + kRows + r], l);
+    s_w[c][lane] = live ? slot(c)[kRows * D + r] : -INFINITY;
+    s_l[c][lane] = live ? slot(c)[kRows * D + kRows + r] : 0.f;
   }
-  s_l[warp][lane] = l;
   __syncthreads();
   if (!live) return;
-  l = 0.f;
-#pragma unroll
-  for (int i = 0; i < D / 8; ++i) l += s_l[i][lane];
+  float l = 0.f, mx = -INFINITY;
+  for (int c = 0; c < parts; ++c) mx = fmaxf(mx, s_w[c][lane]);
+  auto weight = [&](int c) {
+    const float m = s_w[c][lane];
+    return m == -INFINITY ? 0.f : ex2((m - mx) * sl2);
+  };
   float f[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
   for (int c0 = 0; c0 < parts; c0 += kJoinParts) {
-    float4 p[kJoinParts], q[kJoinParts];
+    if (c0 > 0) fetch(c0);
 #pragma unroll
     for (int i = 0; i < kJoinParts; ++i) {
-      const float* from = slot(min(c0 + i, parts - 1));
-      p[i] = *reinterpret_cast<const float4*>(from + (size_t)((2 * warp) * kRows + r) * 4);
-      q[i] = *reinterpret_cast<const float4*>(from + (size_t)((2 * warp + 1) * kRows + r) * 4);
-    }
-#pragma unroll
-    for (int i = 0; i < kJoinParts; ++i) {
-      const float w = c0 + i < parts ? s_w[c0 + i][lane] : 0.f;
+      if (c0 + i >= parts) break;
+      const float w = weight(c0 + i);
+      l = fmaf(w, s_l[c0 + i][lane], l);
       f[0] = fmaf(w, p[i].x, f[0]); f[1] = fmaf(w, p[i].y, f[1]); f[2] = fmaf(w, p[i].z, f[2]); f[3] = fmaf(w, p[i].w, f[3]);
       f[4] = fmaf(w, q[i].x, f[4]); f[5] = fmaf(w, q[i].y, f[5]); f[6] = fmaf(w, q[i].z, f[6]); f[7] = fmaf(w, q[i].w, f[7]);
     }
@@ -730,7 +746,7 @@ __global__ void __launch_bounds__(4 * D)
 
 int grid_of() {
   const int sms = device_sm_count();
-  return sms < kPagedCounters ? sms : kPagedCounters;
+  return sms < kCtas ? sms : kCtas;
 }
 
 template <int D>

@@ -349,7 +349,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (mine_out) {
             // kParts parts' loads are on their way at once (one after the other, 19 parts
             // of a sequence over the whole GPU took 15 us, now 4)
-            constexpr int kParts = 10;
+            constexpr int kParts = 8;
             mx = -INFINITY;
             ls = 0.f;
 #pragma unroll

@@ -436,16 +436,15 @@ def sparoa_add_norm(ctx: Context, x, h, r=None, y=None, post: Norm | None = None
     lead = h if x is None else x
     if lead is None:
         _refuse("add_norm: x or h")
-    shape = lead.shape
-    C = shape[-1]
-    R = lead.numel() // C if C else 0
+    C, n = lead.shape[-1], lead.numel()
+    R = n // C if C else 0
     stream = r if x is None else x
     res = _f32 if stream is not None and stream.dtype is _f32 else _bf16
     if not ((x is None or (x.dtype is res and x.is_cuda and x.is_contiguous())) and
-            (h is None or (h.dtype is _bf16 and h.is_cuda and h.is_contiguous() and h.shape == shape)) and
-            (r is None or (r.dtype is res and r.is_cuda and r.is_contiguous() and r.shape == shape)) and
-            (y is None or (y.dtype is _bf16 and y.is_cuda and y.is_contiguous() and y.shape == shape))):
-        _refuse("add_norm: contiguous CUDA tensors of one shape wanted: x and r of one type, h and y bf16")
+            (h is None or (h.dtype is _bf16 and h.is_cuda and h.is_contiguous() and h.numel() == n)) and
+            (r is None or (r.dtype is res and r.is_cuda and r.is_contiguous() and r.numel() == n)) and
+            (y is None or (y.dtype is _bf16 and y.is_cuda and y.is_contiguous() and y.numel() == n))):
+        _refuse("add_norm: contiguous CUDA tensors of one size wanted: x and r of one type, h and y bf16")
     if (post is not None and post.C not in (0, C)) or (pre is not None and pre.C not in (0, C)):
         _refuse("add_norm: norm parameters of another length")
     if gate is not None:
