@@ -1255,6 +1255,29 @@ def run_profile(args, rank, local_rank, world, peaks):
         x = act(401408, 64)
         oc = sp.OccupancyBuffer(401408, 64)
         call = lambda: sp.sparoa_op_stats(ctx, x, (401408, 64), occ=oc, host=False)
+    elif op == "add_norm":  # the residual step of 8192 tokens: bf16 stream, RMS norm before the next block
+        x, h = (torch.randn(8192, 4096, device=dev, generator=gen).to(torch.bfloat16) for _ in range(2))
+        r, y = torch.empty_like(x), torch.empty_like(h)
+        n = sp.norm("rms", torch.ones(4096, device=dev))
+        call = lambda: sp.sparoa_add_norm(ctx, x, h, r, y, pre=n)
+    elif op in ("rope_append", "paged_decode", "paged_chunk"):  # 32 query and 8 key heads of 128, pages of 64
+        new, kv = {"rope_append": ([8192], [8192]), "paged_decode": ([1] * 8, [16000] * 8),
+                   "paged_chunk": ([4000], [4000])}[op]
+        per = -(-max(kv) // 64)
+        cache = sp.KVCache(*(torch.randn(len(kv) * per, 8, 64, 128, device=dev, generator=gen).to(torch.bfloat16)
+                             for _ in range(2)))
+        ints = lambda v: torch.tensor(v, dtype=torch.int32, device=dev)
+        order = torch.randperm(len(kv) * per, device=dev, generator=gen).to(torch.int32)
+        batch = sp.PagedBatch(ints([sum(new[:i]) for i in range(len(new) + 1)]), ints(kv), order.view(len(kv), per),
+                              max_q=max(new))
+        q = torch.randn(sum(new), 32, 128, device=dev, generator=gen).to(torch.bfloat16)
+        if op == "rope_append":
+            qkv = torch.randn(sum(new), 48 * 128, device=dev, generator=gen).to(torch.bfloat16)
+            rope = sp.Rope(128)
+            call = lambda: sp.sparoa_rope_append(ctx, qkv, q, cache, batch, rope)
+        else:
+            y = torch.empty_like(q)
+            call = lambda: sp.sparoa_paged_attention(ctx, q, y, cache, batch)
     else:
         raise SystemExit(f"profile: unknown op {op}")
     t0 = time.perf_counter()
