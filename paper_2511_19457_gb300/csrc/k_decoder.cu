@@ -356,35 +356,42 @@ __global__ void __launch_bounds__(kRopeThreads) rope_append_kernel(const __grid_
   }
 }
 
-template <typename RT>
-cudaError_t launch_add_norm_t(const AddNormArgs& a, cudaStream_t s) {
-  // two 16-byte pieces of the stream a thread ([8192, 4096] bf16 46 us, one 48; fp32 75,
-  // four 78), one of a short bf16 row, whose weights then stay in registers ([6304, 768]
-  // 12.9 us, two 14.2), and four or eight where threads run out
-  const int values = a.C > 8192 ? 32 : sizeof(RT) == 2 && a.C > 1024 ? 16 : 8;
-  const int threads = ((a.C + values - 1) / values + 31) / 32 * 32;
-  // CTAs that fit an SM at once (64 or 128 registers a thread, two rows each in shared memory),
+template <typename RT, int VALUES>
+cudaError_t launch_add_norm_v(AddNormArgs a, cudaStream_t s) {
+  const void* kernel = reinterpret_cast<const void*>(add_norm_kernel<RT, VALUES>);
+  static const int regs = [&] {  // (the same on every device)
+    cudaFuncAttributes at;
+    return cudaFuncGetAttributes(&at, kernel) == cudaSuccess ? (at.numRegs + 7) / 8 * 8 : 128;
+  }();
+  const int threads = ((a.C + VALUES - 1) / VALUES + 31) / 32 * 32;
+  // CTAs that fit an SM at once (by their registers, with two rows each in shared memory),
   // and the rows that each has on its way
   const size_t row = (size_t)a.C * ((a.x ? sizeof(RT) : 0) + (a.h ? 2 : 0)), most = 216 << 10;
-  int fit = (values <= 16 ? 1024 : 512) / threads;
+  int fit = 65536 / (regs * threads);
+  if (fit > 2048 / threads) fit = 2048 / threads;
   if (fit > 32) fit = 32;
   const int by_smem = (int)(most / (2 * row + 1536));
   if (fit > by_smem) fit = by_smem;
   if (fit < 1) fit = 1;
-  AddNormArgs args = a;
-  args.stages = (int)((most / fit - 1536) / row);
-  if (args.stages > kNormStages) args.stages = kNormStages;
-  const size_t smem = args.stages * row;
+  a.stages = (int)((most / fit - 1536) / row);
+  if (a.stages > kNormStages) a.stages = kNormStages;
+  const size_t smem = a.stages * row;
   const int64_t grid = (int64_t)fit * device_sm_count();
-  auto go = [&](auto kernel) {
-    const cudaError_t e = smem_optin(reinterpret_cast<const void*>(kernel), smem);
-    if (e != cudaSuccess) return e;
-    return launch_kernel(kernel, dim3((unsigned)(grid < a.R ? grid : a.R)), dim3((unsigned)threads), smem, s, args);
-  };
-  if (values == 32) return go(add_norm_kernel<RT, 32>);
+  const cudaError_t e = smem_optin(kernel, smem);
+  if (e != cudaSuccess) return e;
+  return launch_kernel(add_norm_kernel<RT, VALUES>, dim3((unsigned)(grid < a.R ? grid : a.R)), dim3((unsigned)threads), smem,
+                       s, a);
+}
+
+// Two 16-byte pieces of the stream a thread ([8192, 4096] bf16 46 us, one 48; fp32 75, four
+// 78), one of a short bf16 row, whose weights then stay in registers ([6304, 768] 12.9 us,
+// two 14.2), and four or eight where threads run out.
+template <typename RT>
+cudaError_t launch_add_norm_t(const AddNormArgs& a, cudaStream_t s) {
+  if (a.C > 8192) return launch_add_norm_v<RT, 32>(a, s);
   if constexpr (sizeof(RT) == 2)
-    if (values == 16) return go(add_norm_kernel<RT, 16>);
-  return go(add_norm_kernel<RT, 8>);
+    if (a.C > 1024) return launch_add_norm_v<RT, 16>(a, s);
+  return launch_add_norm_v<RT, 8>(a, s);
 }
 
 }  // namespace
