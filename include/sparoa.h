@@ -445,7 +445,7 @@ typedef struct {
  * onwards of the call's tensors, and kv_len[b] tokens in the cache, the new ones
  * (its last n) included.  Its positions [i page_size, (i+1) page_size) are in page
  * table[b table_stride + i]; entries that no position below kv_len[b] needs are not
- * read.  Rows that belong to no sequence are left as they are. */
+ * read (those before a window may be).  Rows that belong to no sequence are left as they are. */
 typedef struct {
     const int32_t *q_start;  /* [batch + 1], not decreasing                   */
     const int32_t *kv_len;   /* [batch]                                       */
@@ -522,7 +522,8 @@ sparoa_status sparoa_rope_append(sparoa_ctx *ctx, const void *qkv, int64_t ld_qk
  *         the keys that a row sees (-infinity for none)
  *   y_occ occupancy of y to write (nullable); rows of no sequence count as they are
  * Splits long sequences over the GPU; partial results live in a workspace that the
- * context keeps for each stream it is used on.  A table entry outside [0, pages), or
+ * context keeps for each stream it is used on, of the last 16 (a graph goes on using
+ * that of the stream it was captured on).  A table entry outside [0, pages), or
  * a length past the table's row, is reported as INVALID_ARG by the next call that
  * synchronises, and the affected rows hold anything.
  * Errors: INVALID_ARG, UNSUPPORTED (head_dim, page_size, batch), CUDA, OOM, TIMEOUT. */

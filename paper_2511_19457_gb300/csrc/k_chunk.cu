@@ -516,7 +516,7 @@ __device__ __forceinline__ void softmax_role(const Role& r, uint32_t tmem) {
       float* slot = a.ws + (size_t)part_slot(blockIdx.x, c.first == 0) * C::kSlotFloats;
       const int at = r0 + row, of = live ? over_group(a, c.t * kRows + at) : 0;
       const int64_t out = (int64_t)(c.q0 + of) * a.heads + c.h * a.group + (live ? c.t * kRows + at - of * a.group : 0);
-      const float inv = l > 0.f ? 1.f / l : 0.f;
+      const float inv = l == 0.f ? 0.f : 1.f / l;  // (a sum of NaN stays one)
       const uint32_t mine = smem_u32(r.sh.plan.scratch) + warp * kOutBytes;
       int64_t to_row[4];
 #pragma unroll
@@ -538,7 +538,7 @@ __device__ __forceinline__ void softmax_role(const Role& r, uint32_t tmem) {
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const float lo = __uint_as_float(o[k * 8 + 2 * e]) * inv, hi = __uint_as_float(o[k * 8 + 2 * e + 1]) * inv;
-            w[e] = l > 0.f ? act_pack2<0>(lo, hi) : 0u;
+            w[e] = l == 0.f ? 0u : act_pack2<0>(lo, hi);
           }
           sts_u4(mine + sw64_offset(lane, k), make_uint4(w[0], w[1], w[2], w[3]));
         }
@@ -590,7 +590,7 @@ __device__ __forceinline__ void softmax_role(const Role& r, uint32_t tmem) {
           slot[kRows * D + at] = m;
           slot[kRows * D + kRows + at] = l;
         } else if (live && a.lse) {
-          a.lse[out] = l > 0.f ? fmaf(m, a.scale, logf(l)) : -INFINITY;
+          a.lse[out] = l == 0.f ? -INFINITY : fmaf(m, a.scale, logf(l));
         }
       }
     }
@@ -735,13 +735,13 @@ __global__ void __launch_bounds__(4 * D)
       f[4] = fmaf(w, q[i].x, f[4]); f[5] = fmaf(w, q[i].y, f[5]); f[6] = fmaf(w, q[i].z, f[6]); f[7] = fmaf(w, q[i].w, f[7]);
     }
   }
-  const float inv = l > 0.f ? 1.f / l : 0.f;
+  const float inv = l == 0.f ? 0.f : 1.f / l;  // (a sum of NaN stays one)
 #pragma unroll
   for (int k = 0; k < 8; ++k) f[k] *= inv;
   const int row = j.t * kRows + r, of = over_group(a, row);
   const int64_t at = (int64_t)(j.q0 + of) * a.heads + j.h * a.group + row - of * a.group;
   *reinterpret_cast<uint4*>(a.y + at * D + warp * 8) = pack8(f);
-  if (a.lse && warp == 0) a.lse[at] = l > 0.f ? fmaf(mx, a.scale, logf(l)) : -INFINITY;
+  if (a.lse && warp == 0) a.lse[at] = l == 0.f ? -INFINITY : fmaf(mx, a.scale, logf(l));
 }
 
 int grid_of() {

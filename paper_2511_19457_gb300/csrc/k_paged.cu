@@ -314,7 +314,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
         for (int w = 0; w < kWarps; ++w) {
           const float mw = s_m[w][row];
-          if (mw == -INFINITY) continue;  // saw no key: its sums may not be there
+          if (mw == -INFINITY && s_l[w][row] == 0.f) continue;  // saw no key: its sums may not be there
           const float f = ex2((mw - mx) * sl2);
           ls += f * s_l[w][row];
           const uint32_t at = s_at[w] + row * (D * 4) + ((piece ^ (row & 7)) << 5);
@@ -368,7 +368,7 @@ __global__ void __launch_bounds__(kThreads, 1)
               }
 #pragma unroll
               for (int i = 0; i < kParts; ++i) {
-                if (c + i > sh.c1 || pm[i] == -INFINITY) continue;
+                if (c + i > sh.c1 || (pm[i] == -INFINITY && pl[i] == 0.f)) continue;
                 const float nm = fmaxf(mx, pm[i]), f = mx == -INFINITY ? 0.f : ex2((mx - nm) * sl2), e = ex2((pm[i] - nm) * sl2);
                 mx = nm;
                 ls = ls * f + pl[i] * e;
@@ -385,12 +385,12 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int r = cc.t * kRows + row, of = over_group(a, r);
         const int64_t tok = cc.q0 + of;
         const int head = cc.h * a.group + r - of * a.group;
-        const float inv = ls > 0.f ? 1.f / ls : 0.f;
+        const float inv = ls == 0.f ? 0.f : 1.f / ls;  // (a sum of NaN stays one)
 #pragma unroll
         for (int k = 0; k < 8; ++k) acc[k] *= inv;
         *reinterpret_cast<uint4*>(a.y + (tok * a.heads + head) * D + piece * 8) = pack8(acc);
         if (a.lse && piece == 0)
-          a.lse[tok * a.heads + head] = ls > 0.f ? fmaf(mx, a.scale, logf(ls)) : -INFINITY;
+          a.lse[tok * a.heads + head] = ls == 0.f ? -INFINITY : fmaf(mx, a.scale, logf(ls));
       }
       __syncthreads();  // the free stages may be filled, s_m, s_l and s_at written again
       fresh = true;

@@ -377,6 +377,25 @@ def test_attention_large_scores(sp, ctx):
     _check_attn(sp, ctx, [1, 3], [300, 60], 4, 2, 64, 16, scale=20.0)
 
 
+@pytest.mark.parametrize("new,kv", [([2, 1], [700, 3000]), ([100, 40], [700, 3000]), ([3, 1], [20, 40])])
+def test_attention_nan_query(sp, ctx, new, kv):
+    """A query that is not a number gives results that are none, not zeros, and leaves other rows alone."""
+    cache, batch, k, v, table = _batch(sp, new, kv, 16, 2, 64, 8)
+    T = sum(new)
+    q = torch.randn(T, 4, 64, generator=_g(1)).to(torch.bfloat16)
+    q[1, 2, 5] = float("nan")
+    y = torch.empty(T, 4, 64, dtype=torch.bfloat16, device="cuda")
+    lse = torch.empty(T, 4, device="cuda")
+    sp.sparoa_paged_attention(ctx, q.cuda(), y, cache, batch, lse=lse)
+    ctx.sync()
+    assert torch.isnan(y[1, 2]).all() and torch.isnan(lse[1, 2])
+    q[1, 2, 5] = 0.0
+    want, wl, size = _attn64(q, k, v, table, new, kv, 16, 64 ** -0.5, True, 0)
+    keep = torch.ones(T, 4, dtype=torch.bool)
+    keep[1, 2] = False
+    _close(y[keep], want[keep], "rows beside it", extra=(2.0 ** -8 + 2.0 ** -12) * size[keep])
+
+
 def test_attention_leaves_other_rows(sp, ctx):
     """Rows past the last sequence's are not touched."""
     cache, batch, *_ = _batch(sp, [2, 1], [20, 40], 16, 2, 64, 8)
