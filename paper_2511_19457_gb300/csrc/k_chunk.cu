@@ -1,4 +1,6 @@
 // Attention of chunks of new tokens over a paged key/value cache on tcgen05.
+#include <cstring>
+
 #include "paged.cuh"
 
 namespace sparoa {
@@ -8,9 +10,9 @@ namespace {
 // ---------------------------------------------------------------------------
 // An item is 256 query rows: two tiles of 128, whose scores and sums live in tensor
 // memory side by side: S (128 x 128 fp32, later overwritten by the weights P in
-// bf16) and O (128 x D fp32) of each.  Ten warps: two groups of four for the softmax
+// bf16) and O (128 x D fp32) of each.  Eleven warps: two groups of four for the softmax
 // of a tile (a thread per row), one that issues the MMAs, one that loads K and V by
-// TMA, page by page, into a ring.
+// TMA, page by page, into a ring, and one that walks the items and loads their Q.
 //
 // Bound by the tensor cores and, as much, by the exponentials: 256 x 128 scores of a
 // unit are 2 x 2 x 128 x 128 x D MACs (1024 cycles at D = 128) and 32768 exponentials
@@ -32,8 +34,9 @@ namespace {
 constexpr int kRows = 256;     // rows of an item
 constexpr int kTileRows = 128;
 constexpr int kSoftWarps = 8;
-constexpr int kMmaWarp = 8, kLoadWarp = 9, kJoinWarp = 10;
-constexpr int kThreads = 384;  // 12 warps: the last two only fill the third group of four
+constexpr int kMmaWarp = 8, kLoadWarp = 9, kItemWarp = 10, kHelpWarp = 11;
+constexpr int kThreads = 384;
+constexpr int kItems = 4;      // items that the item warp is ahead, at most
 constexpr float kSlackLog2 = 8.f;
 constexpr int kOutBytes = 32 * 64;  // 32 rows of 32 values
 
@@ -121,6 +124,7 @@ __device__ __forceinline__ void reg_dec() {
 
 struct Bars {
   unsigned long long full[8], empty[8];      // ring
+  unsigned long long item[kItems], item_free[kItems], q_free[2];
   unsigned long long s[2], p[2], q[2], o[2], o_free[2];  // per tile
   unsigned long long joined, drain;
 };
@@ -130,7 +134,7 @@ struct Shared {
   PagedPlan<kSoftWarps * kOutBytes> plan;  // scratch: each softmax warp's block of the result on its way out
   Bars bars;
   Cursor start;
-  Cursor at[12], next[8];  // a warp's item, and the softmax warps' next one: in memory, their registers hold scores
+  Cursor items[kItems];
   float m[kTileRows], l[kTileRows];  // an item of one tile: the second group's statistics
   uint32_t tmem;
   int abort;
@@ -147,17 +151,83 @@ struct Role {
   }
   __device__ __forceinline__ bool aborted() const { return *(volatile int*)&sh.abort != 0; }
   __device__ __forceinline__ int rows(const Cursor& c) const { return c.n * a.group - c.t * kRows; }
-  // dst = the item after c (a converged warp; both in shared memory)
-  __device__ __forceinline__ void next_item(Cursor& dst, const Cursor& c) const {
+  // item n of the CTA's share; null after a timeout
+  __device__ __forceinline__ const Cursor* item(unsigned n) const {
+    return wait(sh.bars.item[n % kItems], (n / kItems) & 1u, kErrTimeoutFull) ? &sh.items[n % kItems] : nullptr;
+  }
+  __device__ __forceinline__ void item_done(unsigned n) const {
     __syncwarp();
-    if ((threadIdx.x & 31) == 0) {
-      Cursor k = c;
-      k.next_item(a, sh.plan);
-      dst = k;
-    }
-    __syncwarp();
+    if ((threadIdx.x & 31) == 0) mbar_arrive(smem_u32(&sh.bars.item_free[n % kItems]));
   }
 };
+
+// Whether the queries of a tile are a box [128 / group tokens][group heads][D] of q.
+__host__ __device__ __forceinline__ bool boxes_of_q(int group) { return kTileRows % group == 0; }
+
+// The share's items for the other warps, and their tiles of Q: by TMA, or row by row with
+// the help of one more warp where tiles do not begin and end with a token.  One warp that
+// does nothing else: in the softmax warps the same took 4000 cycles at every item, mostly
+// for its instructions, which the loops over units drive out of the caches.
+template <int D>
+__device__ __forceinline__ void item_role(const Role& r, const CUtensorMap* tq) {
+  using C = Cfg<D>;
+  const PagedArgs& a = r.a;
+  Bars& bars = r.sh.bars;
+  const int lane = threadIdx.x & 31;
+  const bool boxes = boxes_of_q(a.group), leads = (threadIdx.x >> 5) == kItemWarp;
+  Cursor c = r.sh.start;
+  unsigned used[2] = {0, 0};  // items of a tile
+  bool ok = true;
+  for (unsigned n = 0;; ++n) {
+    if (leads) {
+      if (!(ok = r.wait(bars.item_free[n % kItems], ((n / kItems) & 1u) ^ 1u, kErrTimeoutEmpty))) break;
+      if (lane == 0) {
+        r.sh.items[n % kItems] = c;
+        mbar_arrive(smem_u32(&bars.item[n % kItems]));
+      }
+      __syncwarp();
+    }
+    if (c.done()) break;
+    const int rows = r.rows(c);
+    for (int tile = 0; tile < (rows > kTileRows ? 2 : 1); ++tile) {
+      // every product with the tile before is done
+      if (!(ok = r.wait(bars.q_free[tile], (used[tile]++ & 1u) ^ 1u, kErrTimeoutEmpty))) break;
+      const uint32_t dst = r.sq + tile * C::kTile, bar = smem_u32(&bars.q[tile]);
+      const int first = c.t * kRows + tile * kTileRows;
+      if (boxes) {
+        // (rows past the item's last are other sequences' or zero: their results go nowhere)
+        if (lane == 0) {
+          mbar_arrive_expect_tx(bar, (uint32_t)C::kTile);
+#pragma unroll
+          for (int i = 0; i < C::kHalves; ++i)
+            tma_load_3d(dst + i * C::kHalf, tq, bar, i * 64, c.h * a.group, c.q0 + over_group(a, first));
+        }
+        __syncwarp();
+      } else {
+        const __nv_bfloat16* base = a.q + (int64_t)c.q0 * a.ld_q + c.h * a.group * D;
+#pragma unroll 2
+        for (int i = leads ? 0 : 1; i < kTileRows * D / 256; i += 2) {
+          const int e = i * 32 + lane, ch = e % (D / 8), rr = e / (D / 8);
+          const bool live = tile * kTileRows + rr < rows;
+          const int at = live ? first + rr : 0, tok = over_group(a, at);
+          cp_async_16(dst + (ch >> 3) * C::kHalf + swz_offset<64>(rr, ch & 7),
+                      base + tok * a.ld_q + (at - tok * a.group) * D + ch * 8, live ? 16u : 0u);
+        }
+        cp_async_commit();
+        cp_async_wait<0>();
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar);
+      }
+    }
+    if (!ok) break;
+    c.next_item(a, r.sh.plan);
+  }
+  // after a timeout: wait for the copies in flight into memory that is given back
+  if (boxes && r.aborted())
+    for (int tile = 0; tile < 2; ++tile)
+      if (used[tile] > 0) mbar_drain(smem_u32(&bars.q[tile]), (used[tile] - 1) & 1u, r.limit);
+}
 
 // K and V of every unit: K0 V0 K1 V1 ...
 template <int D>
@@ -209,7 +279,6 @@ __device__ __forceinline__ void mma_role(const Role& r, uint32_t tmem) {
   const PagedArgs& a = r.a;
   Bars& bars = r.sh.bars;
   const int lane = threadIdx.x & 31;
-  Cursor& c = r.sh.at[threadIdx.x >> 5];
   const bool leader = elect_one();
   constexpr uint32_t id_s = idesc_bf16_f32(kTileRows, kUnitKeys);
   constexpr uint32_t id_o = idesc_bf16_f32(kTileRows, D) | (1u << 16);  // B is MN-major
@@ -259,9 +328,16 @@ __device__ __forceinline__ void mma_role(const Role& r, uint32_t tmem) {
     }
     __syncwarp();
   };
-  while (!c.done() && ok) {
-    const int count = c.end - c.first, first_key = c.key0(), hi = c.k.hi, len = c.len;
-    const bool two = r.rows(c) > kTileRows;
+  auto free_q = [&](int tile) {
+    if (leader) tc_commit(smem_u32(&bars.q_free[tile]));
+    __syncwarp();
+  };
+  for (unsigned n = 0; ok; ++n) {
+    const Cursor* item = r.item(n);
+    if (!item || item->done()) break;
+    const int count = item->end - item->first, first_key = item->key0(), hi = item->k.hi, len = item->len;
+    const bool two = r.rows(*item) > kTileRows;
+    r.item_done(n);
     // k-steps of unit j, whose values are in stage i
     auto steps_of = [&](int j, unsigned i) {
       const int key0 = first_key + j * kUnitKeys, steps = (max(0, min(hi, key0 + kUnitKeys) - key0) + 15) >> 4;
@@ -286,6 +362,10 @@ __device__ __forceinline__ void mma_role(const Role& r, uint32_t tmem) {
       // two tiles: both take every unit
       qk(1, 1, 0);
       free_stage(0);
+      if (count == 1) {
+        free_q(0);
+        free_q(1);
+      }
       for (int j = 0; j < count && full(2 * j + 1); ++j) {
         const bool last = j + 1 == count;
         const int steps = steps_of(j, 2 * j + 1);
@@ -294,6 +374,7 @@ __device__ __forceinline__ void mma_role(const Role& r, uint32_t tmem) {
         if (!last) {
           if (!full(2 * j + 2)) break;
           qk(0, 0, 2 * j + 2);
+          if (j + 2 == count) free_q(0);
         }
         pv(1, 2 * j + 1, steps, j == 0, last, false);
         if (!ok) break;
@@ -301,6 +382,7 @@ __device__ __forceinline__ void mma_role(const Role& r, uint32_t tmem) {
         if (!last) {
           qk(1, 1, 2 * j + 2);
           free_stage(2 * j + 2);
+          if (j + 2 == count) free_q(1);
         }
       }
     } else {
@@ -311,6 +393,7 @@ __device__ __forceinline__ void mma_role(const Role& r, uint32_t tmem) {
         qk(1, 0, 2);
         free_stage(2);
       }
+      if (count <= 2) free_q(0);
       for (int j = 0; j < count && full(2 * j + 1); ++j) {
         const int steps = steps_of(j, 2 * j + 1);
         pv(j & 1, 2 * j + 1, steps, j < 2, j + 2 >= count, true);
@@ -320,11 +403,11 @@ __device__ __forceinline__ void mma_role(const Role& r, uint32_t tmem) {
           if (!full(2 * j + 4)) break;
           qk(j & 1, 0, 2 * j + 4);
           free_stage(2 * j + 4);
+          if (j + 3 == count) free_q(0);
         }
       }
     }
     base += 2 * count;
-    r.next_item(c, c);
   }
   if (r.aborted()) {  // the MMAs issued so far end before tensor memory is given back
     if (leader) tc_commit(smem_u32(&bars.drain));
@@ -343,38 +426,12 @@ __device__ __forceinline__ void softmax_role(const Role& r, uint32_t tmem) {
   const uint32_t lanes = (uint32_t)(warp & 3) << 21;  // the warp's 32 lanes of tensor memory
   const uint32_t ts = tmem + lanes + grp * 128, to = tmem + lanes + C::kO + grp * D;
   const float sl2 = a.scale * 1.4426950408889634f, slack = kSlackLog2 / sl2;
-  Cursor& c = r.sh.at[warp];
-  Cursor& nx = r.sh.next[warp];
-  // the warp's 32 rows of this group's tile of Q of an item, if it has one; rows past the
-  // item's last are zero.  Lanes side by side take a row's chunks (a row a lane was 32 lines
-  // an instruction, and 4000 cycles of the load-store unit an item)
-  auto load_q = [&](const Cursor& k) {
-    const int rows = r.rows(k) - grp * kTileRows;
-    if (k.done() || rows <= 0) return false;
-    const uint32_t dst = r.sq + grp * C::kTile;
-    const __nv_bfloat16* base = a.q + (int64_t)k.q0 * a.ld_q + k.h * a.group * D;
-#pragma unroll 4
-    for (int i = 0; i < D / 8; ++i) {
-      const int e = i * 32 + lane, ch = e % (D / 8), rr = (warp & 3) * 32 + e / (D / 8);
-      const bool live = rr < rows;
-      const int at = live ? k.t * kRows + grp * kTileRows + rr : 0, tok = over_group(a, at);
-      cp_async_16(dst + (ch >> 3) * C::kHalf + swz_offset<64>(rr, ch & 7),
-                  base + tok * a.ld_q + (at - tok * a.group) * D + ch * 8, live ? 16u : 0u);
-    }
-    cp_async_commit();
-    return true;
-  };
-  auto q_ready = [&]() {
-    cp_async_wait<0>();
-    fence_proxy_async_smem();
-    __syncwarp();
-    if (lane == 0) mbar_arrive(smem_u32(&bars.q[grp]));
-  };
-  if (load_q(c)) q_ready();
   unsigned sn = 0, on = 0, joins = 0;
   bool ok = true;
-  while (!c.done()) {
-    r.next_item(nx, c);
+  for (unsigned n = 0;; ++n) {
+    const Cursor* item = r.item(n);
+    if (!item || item->done()) break;
+    const Cursor& c = *item;
     const int rows = r.rows(c), count = c.end - c.first;
     const bool two = rows > kTileRows;
     // the group's rows and units: its own tile and all units, or the tile and every other unit
@@ -390,16 +447,11 @@ __device__ __forceinline__ void softmax_role(const Role& r, uint32_t tmem) {
       low = a.window > 0 ? max(0, p - a.window + 1) : 0;
     }
     const int first_key = c.key0();
-    bool loading = false;
-    if (!works) loading = load_q(nx);
     float m = -INFINITY, l = 0.f;
     for (int j = j0; j < count; j += dj) {
       const int key0 = first_key + j * kUnitKeys;
       if (!(ok = r.wait(bars.s[grp], sn & 1u, kErrTimeoutAcc))) break;
       ++sn;
-      // every product with this group's tile of Q is done: the next item's rows (the other
-      // group may have the last unit of an item of one tile)
-      if (j + dj >= count && (two || grp == 1 || j + 1 == count)) loading = load_q(nx);
       tc_fence_after();
       if (!idle) {
         uint32_t s[4][32];
@@ -488,7 +540,6 @@ __device__ __forceinline__ void softmax_role(const Role& r, uint32_t tmem) {
       __syncwarp();
       if (lane == 0) mbar_arrive(smem_u32(&bars.p[grp]));
     }
-    if (loading) q_ready();
     if (works) ok = ok && r.wait(bars.o[grp], on++ & 1u, kErrTimeoutAcc);
     if (!ok) break;
     tc_fence_after();
@@ -501,11 +552,9 @@ __device__ __forceinline__ void softmax_role(const Role& r, uint32_t tmem) {
       if (lane == 0) mbar_arrive(smem_u32(&bars.joined));
     } else if (works) {
       float f0 = 1.f, f1 = 0.f;
-      loading = false;
       if (halves) {
         if (!(ok = r.wait(bars.joined, joins++ & 1u, kErrTimeoutAcc))) break;
         tc_fence_after();
-        if (count % 2 == 0) loading = load_q(nx);
         const float m1 = r.sh.m[row], l1 = r.sh.l[row], top = fmaxf(m, m1);
         f0 = m == -INFINITY ? 0.f : ex2((m - top) * sl2);
         f1 = m1 == -INFINITY ? 0.f : ex2((m1 - top) * sl2);
@@ -582,7 +631,6 @@ __device__ __forceinline__ void softmax_role(const Role& r, uint32_t tmem) {
             put(i, o);
           }
         }
-        if (loading) q_ready();
         give_back();
       }
       if (!idle) {
@@ -594,17 +642,14 @@ __device__ __forceinline__ void softmax_role(const Role& r, uint32_t tmem) {
         }
       }
     }
-    __syncwarp();
-    if (lane == 0) c = nx;
-    __syncwarp();
+    r.item_done(n);
   }
-  cp_async_wait<0>();
 }
 
 template <int D>
 __global__ void __launch_bounds__(kThreads, 1)
     paged_chunk_kernel(const __grid_constant__ CUtensorMap tk, const __grid_constant__ CUtensorMap tv,
-                       const __grid_constant__ PagedArgs a) {
+                       const __grid_constant__ CUtensorMap tq, const __grid_constant__ PagedArgs a) {
   using C = Cfg<D>;
   extern __shared__ uint8_t smem_raw[];
   __shared__ __align__(8) Shared sh;
@@ -618,9 +663,14 @@ __global__ void __launch_bounds__(kThreads, 1)
     for (int i = 0; i < 2; ++i) {
       mbar_init(smem_u32(&bars.s[i]), 1u);
       mbar_init(smem_u32(&bars.p[i]), 4u);
-      mbar_init(smem_u32(&bars.q[i]), 4u);
+      mbar_init(smem_u32(&bars.q[i]), boxes_of_q(a.group) ? 1u : 2u);
+      mbar_init(smem_u32(&bars.q_free[i]), 1u);
       mbar_init(smem_u32(&bars.o[i]), 1u);
       mbar_init(smem_u32(&bars.o_free[i]), 4u);
+    }
+    for (int i = 0; i < kItems; ++i) {
+      mbar_init(smem_u32(&bars.item[i]), 1u);
+      mbar_init(smem_u32(&bars.item_free[i]), kSoftWarps + 1u);
     }
     mbar_init(smem_u32(&bars.joined), 4u);
     mbar_init(smem_u32(&bars.drain), 1u);
@@ -628,6 +678,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     sh.abort = 0;
     prefetch_tmap(&tk);
     prefetch_tmap(&tv);
+    prefetch_tmap(&tq);
   }
   if (warp == kMmaWarp) tmem_alloc(smem_u32(&sh.tmem), C::kCols);
   tc_fence_before();
@@ -647,9 +698,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     if (lane == 0) sh.start = c;
   }
   __syncthreads();
-  if (works && lane == 0) sh.at[warp] = sh.start;
-  __syncwarp();
-  if (warp == kJoinWarp && lane == 0) {
+  if (warp == kHelpWarp && lane == 0) {
     // an item cut at this CTA's start is joined later; the first of its cuts speaks for it
     JoinItem j{};
     if (works && !sh.start.done() && sh.start.first > 0) {
@@ -674,6 +723,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     reg_dec<kFewRegs>();
     if (works && warp == kMmaWarp) mma_role<D>(r, sh.tmem);
     if (works && warp == kLoadWarp) load_role<D>(r, &tk, &tv);
+    if (works && (warp == kItemWarp || (warp == kHelpWarp && !boxes_of_q(a.group)))) item_role<D>(r, &tq);
   }
   tc_fence_before();
   __syncthreads();
@@ -751,14 +801,18 @@ int grid_of() {
 
 template <int D>
 cudaError_t launch_chunk(const PagedArgs& a, cudaStream_t s) {
-  CUtensorMap tk, tv;
+  CUtensorMap tk, tv, tq;
   const uint64_t rows = (uint64_t)a.pages * a.kv_heads << a.page_log2;
   if (!make_tmap_2d(&tk, a.k, rows, D, 64, 1u << a.page_log2) || !make_tmap_2d(&tv, a.v, rows, D, 64, 1u << a.page_log2))
+    return cudaErrorInvalidValue;
+  memset(&tq, 0, sizeof(tq));
+  if (boxes_of_q(a.group) && !make_tmap_3d(&tq, a.q, D, (uint64_t)a.heads, (uint64_t)a.T, D, (uint64_t)a.ld_q, 64,
+                                           (uint32_t)a.group, (uint32_t)(kTileRows / a.group)))
     return cudaErrorInvalidValue;
   cudaError_t e = smem_optin(reinterpret_cast<const void*>(paged_chunk_kernel<D>), Cfg<D>::kSmem);
   if (e != cudaSuccess) return e;
   const int grid = grid_of();
-  e = launch_kernel(paged_chunk_kernel<D>, dim3(grid), dim3(kThreads), Cfg<D>::kSmem, s, tk, tv, a);
+  e = launch_kernel(paged_chunk_kernel<D>, dim3(grid), dim3(kThreads), Cfg<D>::kSmem, s, tk, tv, tq, a);
   if (e != cudaSuccess) return e;
   return launch_kernel(paged_join_kernel<D>, dim3(grid, kRows / 32), dim3(4 * D), 0, s, a, grid);
 }

@@ -131,11 +131,13 @@ struct IgemmArgs {
 cudaError_t launch_igemm(const IgemmArgs& a, cudaStream_t s);
 
 // bf16 tensor maps (k_igemm.cu): a [rows, cols] matrix with box {box_cols,
-// box_rows}; an NHWC tensor with box {box_c, bw, bh, bn} traversed with element
+// box_rows}; a [n2, n1, n0] tensor with strides in values; an NHWC tensor with box {box_c, bw, bh, bn} traversed with element
 // strides {1, stride, stride, 1}.  The swizzle is the box's inner extent, 64 or
 // 128 bytes.
 bool make_tmap_2d(CUtensorMap* m, const void* base, uint64_t rows, uint64_t cols, uint32_t box_cols,
                   uint32_t box_rows);
+bool make_tmap_3d(CUtensorMap* m, const void* base, uint64_t n0, uint64_t n1, uint64_t n2, uint64_t stride1,
+                  uint64_t stride2, uint32_t box0, uint32_t box1, uint32_t box2);
 bool make_tmap_nhwc(CUtensorMap* m, const void* base, int n, int h, int w, int c, int box_c, int bw, int bh,
                     int bn, int stride);
 
