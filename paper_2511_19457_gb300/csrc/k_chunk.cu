@@ -40,12 +40,13 @@ constexpr int kItems = 4;      // items that the item warp is ahead, at most
 constexpr float kSlackLog2 = 8.f;
 constexpr int kOutBytes = 32 * 64;  // 32 rows of 32 values
 
-// Steps of about 0.55 us, fitted to the CTAs' times: a unit of one tile 1.1 us, of two
-// tiles 1.5, an item's beginning and end 4.4.  (A join is 6, but items left whole so that
-// there is none keep some CTAs twice as long: [4 x 1000 tokens, window 1024] 23 -> 37 us.)
+// Steps of about 0.3 us, fitted to the CTAs' times: a unit of one tile 1.2 us, of two
+// tiles 1.5, an item's beginning and end 2.7 (7 and 12 steps were each slower on some of a
+// prompt, mixed chunks, drafts and windows).  A join is 4 us, but items left whole so that
+// there is none keep some CTAs twice as long: 4 x 1000 tokens, window 1024, 23 -> 37 us.
 struct ChunkCut {
-  static constexpr int ROWS = kRows, EXTRA = 8, MIN_SHARE = 8, WHOLE_SHARE = 0, WHOLE_MORE = 0;
-  static __device__ __forceinline__ int weight(int rows) { return rows > kTileRows ? 3 : 2; }
+  static constexpr int ROWS = kRows, EXTRA = 9, MIN_SHARE = 16, WHOLE_SHARE = 0, WHOLE_MORE = 0;
+  static __device__ __forceinline__ int weight(int rows) { return rows > kTileRows ? 5 : 4; }
 };
 using Cursor = PagedCursor<ChunkCut>;
 
@@ -599,39 +600,32 @@ __device__ __forceinline__ void softmax_role(const Role& r, uint32_t tmem) {
         }
         __syncwarp();
       };
-      auto give_back = [&]() {  // O has been read: the next item's products may begin
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) {
-          mbar_arrive(smem_u32(&bars.o_free[grp]));
-          if (halves) mbar_arrive(smem_u32(&bars.o_free[1]));
-        }
-      };
-      if (!halves && !idle) {
-        uint32_t o[D / 32][32];
-#pragma unroll
-        for (int i = 0; i < D / 32; ++i) tmem_ld32_nowait(to + i * 32, o[i]);
-#pragma unroll
-        for (int i = 0; i < D / 32; ++i) tmem_wait_ld32(o[i]);
-        give_back();
-#pragma unroll
-        for (int i = 0; i < D / 32; ++i) put(i, o[i]);
-      } else {
-        if (!idle) {
+      if (!idle) {
+        // (a loop, and 32 columns at a time: unrolled, its instructions are fetched for every
+        // item anew)
 #pragma unroll 1
-          for (int i = 0; i < D / 32; ++i) {
-            uint32_t o[32], e[32];
-            tmem_ld32_nowait(to + i * 32, o);
+        for (int i = 0; i < D / 32; ++i) {
+          uint32_t o[32];
+          tmem_ld32_nowait(to + i * 32, o);
+          if (halves) {
+            uint32_t e[32];
             tmem_ld32_nowait(to + D + i * 32, e);
             tmem_wait_ld32(o);
             tmem_wait_ld32(e);
 #pragma unroll
             for (int k = 0; k < 32; ++k)
               o[k] = __float_as_uint(__uint_as_float(o[k]) * f0 + __uint_as_float(e[k]) * f1);
-            put(i, o);
+          } else {
+            tmem_wait_ld32(o);
           }
+          put(i, o);
         }
-        give_back();
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) {  // O has been read: the next item's products may begin
+        mbar_arrive(smem_u32(&bars.o_free[grp]));
+        if (halves) mbar_arrive(smem_u32(&bars.o_free[1]));
       }
       if (!idle) {
         if (part) {

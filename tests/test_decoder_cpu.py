@@ -142,7 +142,7 @@ def test_cut_of_the_work():
         grid = rng.choice([1, 2, 7, 152])
         n, top = rng.randint(1, rng.choice([3, 50, 400])), rng.choice([1, 5, 100, 3000])
         _cut(2, 2, 8, 8, [(rng.randint(1, top), 1) for _ in range(n)], grid)            # few rows
-        _cut(8, 8, 0, 0, [(rng.randint(1, top), rng.choice([2, 3])) for _ in range(n)], grid)  # chunks
+        _cut(9, 16, 0, 0, [(rng.randint(1, top), rng.choice([4, 5])) for _ in range(n)], grid)  # chunks
 
 
 def test_group_multiplier():
