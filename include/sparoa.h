@@ -445,7 +445,8 @@ typedef struct {
  * onwards of the call's tensors, and kv_len[b] tokens in the cache, the new ones
  * (its last n) included.  Its positions [i page_size, (i+1) page_size) are in page
  * table[b table_stride + i]; entries that no position below kv_len[b] needs are not
- * read (those before a window may be).  Rows that belong to no sequence are left as they are. */
+ * read, nor are those of pages before the window of the sequence's first new token.
+ * Rows that belong to no sequence are left as they are. */
 typedef struct {
     const int32_t *q_start;  /* [batch + 1], not decreasing                   */
     const int32_t *kv_len;   /* [batch]                                       */

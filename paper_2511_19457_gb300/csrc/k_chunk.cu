@@ -1,4 +1,5 @@
 // Attention of chunks of new tokens over a paged key/value cache on tcgen05.
+#include <cfloat>
 #include <cstring>
 
 #include "paged.cuh"
@@ -14,10 +15,13 @@ namespace {
 // of a tile (a thread per row), one that issues the MMAs, one that loads K and V by
 // TMA, page by page, into a ring, and one that walks the items and loads their Q.
 //
-// Bound by the tensor cores and, as much, by the exponentials: 256 x 128 scores of a
-// unit are 2 x 2 x 128 x 128 x D MACs (1024 cycles at D = 128) and 32768 exponentials
-// (1024 cycles at 32 a cycle).  So the two tiles alternate: while the softmax works on
-// one, the tensor cores multiply for the other.
+// Bound by the tensor cores and, nearly as much, by the softmax: the 256 x 128 scores of a
+// unit are 2 x 2 x 128 x 128 x D MACs (2048 cycles at D = 128 and 4096 a cycle; Q K^T takes
+// a sixth more for its operands from shared memory) and 32768 exponentials (1024 cycles at
+// 32 a cycle) with as many maxima, sums and conversions.  So the two tiles alternate: while
+// the softmax works on one, the tensor cores multiply for the other.  A prompt of 8191
+// tokens, 32 heads over 8 of 128: 373 to 396 us, 1.39 PFLOP/s and more, at the card's power
+// limit; 327 without a softmax, 321 with an eighth of the products.
 //   S = Q K^T     both operands in shared memory, K-major, 128-byte swizzle
 //   O += P V      P from tensor memory, V from shared memory as it lies ([key][D], the
 //                 MN-major form of the B operand)
@@ -58,7 +62,7 @@ struct Cfg {
   static constexpr int kStages = D == 128 ? 4 : 8;
   static constexpr int kSmem = (2 + kStages) * kTile + 1024;
   static constexpr int kSlotFloats = kRows * (D + 2);   // a partial result: sums [D / 4][256][4], maxima, sums of weights
-  static constexpr uint32_t kCols = D == 128 ? 512 : 512;  // S, S, O, O: 256 + 2 D columns, a power of two
+  static constexpr uint32_t kCols = 512;                // S, S, O, O: 256 + 2 D columns, to a power of two
   static constexpr uint32_t kO = 256;                   // first column of O
 };
 
@@ -67,9 +71,6 @@ struct JoinItem {
   int q0, t, h, rows, valid;
 };
 
-__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t ad, uint64_t bd, uint32_t idesc, uint32_t acc) {
-  tc_mma_bf16(d, ad, bd, idesc, acc);
-}
 // A from tensor memory (a lane per row, two values a column)
 __device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t bd, uint32_t idesc, uint32_t acc) {
   asm volatile(
@@ -96,17 +97,6 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16
       " {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(taddr),
       "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
       "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
-      : "memory");
-}
-__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32]) {
-  asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0],"
-      " {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,"
-      "%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};" ::"r"(taddr),
-      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
-      "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]),
-      "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]),
-      "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
       : "memory");
 }
 
@@ -241,9 +231,11 @@ __device__ __forceinline__ void load_role(const Role& r, const CUtensorMap* tk, 
   const int pg = lane / C::kHalves, half = lane % C::kHalves;
   const uint32_t box = 128u << a.page_log2;          // bytes: page_size rows of 128
   unsigned n = 0;                                    // stages filled
+  // a page before all rows' windows may be gone: a box outside of the pool reads zeros
+  auto seen = [&](const Cursor& at, int key) { return key + (1 << a.page_log2) > at.k.lo; };
   auto entry = [&]() {
     const int key = c.key0() + (pg << a.page_log2);
-    return !c.done() && pg < pages && key < c.k.hi ? page_of(a, c.b, key) : -1;
+    return !c.done() && pg < pages && key < c.k.hi && seen(c, key) ? page_of(a, c.b, key) : -1;
   };
   int page = entry();
   bool ok = true;
@@ -252,7 +244,8 @@ __device__ __forceinline__ void load_role(const Role& r, const CUtensorMap* tk, 
     const int live = max(0, min(c.k.hi, key0 + kUnitKeys) - key0);
     const int need = (live + (1 << a.page_log2) - 1) >> a.page_log2;
     const bool mine = pg < need;
-    const int row = mine ? pool_row(a, page_checked(a, page), c.h, 0) : 0;
+    const bool there = mine && seen(c, key0 + (pg << a.page_log2));
+    const int row = there ? pool_row(a, page_checked(a, page), c.h, 0) : -kUnitKeys;
     c.next(a, r.sh.plan);
     page = entry();  // on its way while this unit waits for room
 #pragma unroll
@@ -302,7 +295,7 @@ __device__ __forceinline__ void mma_role(const Role& r, uint32_t tmem) {
 #pragma unroll
       for (int kk = 0; kk < D / 16; ++kk) {
         const uint32_t at = ((kk >> 2) * C::kHalf + (kk & 3) * 32) >> 4;
-        mma_ss(tmem + slot * 128, qd + at, kd + at, id_s, kk > 0);
+        tc_mma_bf16(tmem + slot * 128, qd + at, kd + at, id_s, kk > 0);
       }
       if (!a.fault) tc_commit(smem_u32(&bars.s[slot]));
     }
@@ -426,7 +419,7 @@ __device__ __forceinline__ void softmax_role(const Role& r, uint32_t tmem) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, grp = warp >> 2, row = threadIdx.x & 127;
   const uint32_t lanes = (uint32_t)(warp & 3) << 21;  // the warp's 32 lanes of tensor memory
   const uint32_t ts = tmem + lanes + grp * 128, to = tmem + lanes + C::kO + grp * D;
-  const float sl2 = a.scale * 1.4426950408889634f, slack = kSlackLog2 / sl2;
+  const float sl2 = a.scale * 1.4426950408889634f, slack = fminf(kSlackLog2 / sl2, FLT_MAX);
   unsigned sn = 0, on = 0, joins = 0;
   bool ok = true;
   for (unsigned n = 0;; ++n) {

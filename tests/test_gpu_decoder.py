@@ -427,6 +427,32 @@ def test_attention_reports_bad_lists(sp, ctx):
     call()
 
 
+@pytest.mark.parametrize("n", [1, 2, 40, 300])
+@pytest.mark.parametrize("page", [16, 32, 64, 128])
+def test_attention_pages_before_the_window(sp, ctx, n, page):
+    """Pages that every new token's window has left are not looked up: their entries may be anything."""
+    L, window, H, KH, D = 1000, 150, 4, 2, 64
+    cache, batch, k, v, table = _batch(sp, [n, n], [L, L - 3], page, KH, D, 17)
+    q = torch.randn(2 * n, H, D, generator=_g(18)).to(torch.bfloat16)
+    want, wl, size = _attn64(q, k, v, table, [n, n], [L, L - 3], page, D ** -0.5, True, window)
+    for b, kv in enumerate([L, L - 3]):
+        first = max(0, kv - n - window + 1)  # the oldest key that the first new token sees
+        batch.table[b, :first // page] = -1
+        assert first // page > 0
+    y = torch.empty(2 * n, H, D, dtype=torch.bfloat16, device="cuda")
+    lse = torch.empty(2 * n, H, device="cuda")
+    sp.sparoa_paged_attention(ctx, q.cuda(), y, cache, batch, window=window, lse=lse)
+    ctx.sync()
+    assert ((lse.double().cpu() - wl).abs() <= 2e-4).all()
+    _close(y, want, f"n {n} page {page}", extra=(2.0 ** -8 + 2.0 ** -12) * size)
+
+
+@pytest.mark.parametrize("new,kv", [([1], [300]), ([70, 3], [300, 500]), ([200], [400])])
+def test_attention_vanishing_scale(sp, ctx, new, kv):
+    """A scale so small that the slack of the running maximum passes the largest float: every key weighs the same."""
+    _check_attn(sp, ctx, new, kv, 4, 2, 64, 32, window=40, seed=4, scale=1e-38, p_round=2.0 ** -8)
+
+
 def test_attention_streams(sp, ctx):
     """Calls of one context on two streams at once: each has partial results of its own."""
     jobs = []
