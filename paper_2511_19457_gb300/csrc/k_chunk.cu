@@ -438,7 +438,7 @@ __device__ __forceinline__ void softmax_role(const Role& r, uint32_t tmem) {
     if (live) {
       const int p = c.len - c.n + over_group(a, c.t * kRows + r0 + row);
       lim = a.causal ? min(c.len, p + 1) : c.len;
-      low = a.window > 0 ? max(0, p - a.window + 1) : 0;
+      low = first_seen(a, p);
     }
     const int first_key = c.key0();
     float m = -INFINITY, l = 0.f;

@@ -178,7 +178,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           const int pos = cc.len - cc.n + tok;
           p[i] = a.q + (int64_t)(cc.q0 + tok) * a.ld_q + head * D;
           lim[i] = a.causal ? min(cc.len, pos + 1) : cc.len;
-          low[i] = a.window > 0 ? max(0, pos - a.window + 1) : 0;
+          low[i] = first_seen(a, pos);
         }
       }
       lim0 = lim[0]; lim1 = lim[1]; low0 = low[0]; low1 = low[1];

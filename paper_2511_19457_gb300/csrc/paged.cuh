@@ -49,6 +49,12 @@ __device__ __forceinline__ int tiles_of(int n, int group) {
   return (n * group + Cut::ROWS - 1) / Cut::ROWS;  // (n * group is at most 2^30)
 }
 
+// First key that the token at position p sees (no overflow: windows reach 2^31 - 1, and
+// tokens before the sequence's first position are negative).
+__device__ __forceinline__ int first_seen(const PagedArgs& a, int p) {
+  return a.window > 0 && p + 1 > a.window ? p + 1 - a.window : 0;
+}
+
 template <typename Cut>
 __device__ __forceinline__ TileKeys tile_keys(const PagedArgs& a, int n, int len, int t) {
   constexpr int RT = Cut::ROWS;
@@ -58,7 +64,7 @@ __device__ __forceinline__ TileKeys tile_keys(const PagedArgs& a, int n, int len
     const int last = over_group(a, min(n * a.group, (t + 1) * RT) - 1);
     k.hi = max(0, min(len, len - n + last + 1));
   }
-  k.lo = a.window > 0 ? max(0, len - n + over_group(a, t * RT) - a.window + 1) : 0;
+  k.lo = first_seen(a, len - n + over_group(a, t * RT));
   k.blk0 = k.lo / kUnitKeys;
   k.units = max(1, (k.hi + kUnitKeys - 1) / kUnitKeys - k.blk0);
   return k;

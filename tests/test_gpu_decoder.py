@@ -447,6 +447,14 @@ def test_attention_pages_before_the_window(sp, ctx, n, page):
     _close(y, want, f"n {n} page {page}", extra=(2.0 ** -8 + 2.0 ** -12) * size)
 
 
+@pytest.mark.parametrize("max_q", [1, 200])
+def test_attention_widest_window(sp, ctx, max_q):
+    """The widest window hides nothing, from tokens before their sequence's first position neither."""
+    for causal in (True, False):
+        _check_attn(sp, ctx, [7, 40, 2], [2, 20, 300], 4, 2, 64, 32, causal=causal, window=2 ** 31 - 1, seed=5, max_q=max_q,
+                    p_round=2.0 ** -8)
+
+
 @pytest.mark.parametrize("new,kv", [([1], [300]), ([70, 3], [300, 500]), ([200], [400])])
 def test_attention_vanishing_scale(sp, ctx, new, kv):
     """A scale so small that the slack of the running maximum passes the largest float: every key weighs the same."""
