@@ -10,7 +10,7 @@ namespace {
 // ---------------------------------------------------------------------------
 // Residual step: r = x + scale g N_post(h), y = N_pre(r), rows of C values.
 //
-// Bound by bytes: h and x are read once, r and y written once.  A CTA takes every
+// Bound by bytes: h and x are read once, r and y written once.  Of long rows a CTA takes every
 // gridDim-th row, 8 to 32 values of it a thread.  While a row is in registers the next
 // ones are on their way into shared memory by bulk copies, `stages` of them.  What is left
 // above the bytes is instructions, hence packed fp32 pairs and two 16-byte pieces of the
@@ -63,6 +63,112 @@ __device__ __forceinline__ void store_p(float* p, const f2_t (&f)[2]) {
   *reinterpret_cast<float4*>(p) = v;
 }
 
+// A row in registers, NCH 16-byte pieces of the stream a thread, the thread's T pieces apart.
+template <typename RT, int NCH>
+struct NormRow {
+  static constexpr int V = 16 / sizeof(RT), P = V / 2;
+  using Values = f2_t[NCH][P];
+
+  static __device__ __forceinline__ void load_weights(const NormDev& n, Values& w, int at, int T, int C) {
+#pragma unroll
+    for (int i = 0; i < NCH; ++i) {
+#pragma unroll
+      for (int k = 0; k < P; ++k) w[i][k] = f2(1.f, 1.f);
+      if (n.weight) load_p(n.weight + (at + T * i) * V, at + T * i < C / V, w[i]);
+    }
+  }
+  // f = N(f); columns past the row are zero, and stay zero until the affine part.  `kept`:
+  // the weights of the thread's columns, or null to read them (from L1).
+  template <typename Sum>
+  static __device__ __forceinline__ void normalise(const NormDev& n, Values& f, const Values* kept, int at, int T, int C,
+                                                   const Sum& sum) {
+    const int chunks = C / V;
+    const float inv_c = 1.f / (float)C;
+    if (n.kind == 0) return;
+    float lo, hi;
+    if (n.kind == 2) {
+      f2_t s = f[0][0];
+#pragma unroll
+      for (int i = 0; i < NCH; ++i)
+#pragma unroll
+        for (int k = 0; k < P; ++k)
+          if (i + k > 0) s = fadd2(s, f[i][k]);
+      f2_split(s, lo, hi);
+      const float mean = sum(lo + hi) * -inv_c;
+#pragma unroll
+      for (int i = 0; i < NCH; ++i)
+        if (at + T * i < chunks)
+#pragma unroll
+          for (int k = 0; k < P; ++k) f[i][k] = fadd2(f[i][k], f2(mean, mean));
+    }
+    f2_t q = fmul2(f[0][0], f[0][0]);
+#pragma unroll
+    for (int i = 0; i < NCH; ++i)
+#pragma unroll
+      for (int k = 0; k < P; ++k)
+        if (i + k > 0) q = ffma2(f[i][k], f[i][k], q);
+    f2_split(q, lo, hi);
+    const float rs = rsqrtf(sum(lo + hi) * inv_c + n.eps);
+#pragma unroll
+    for (int i = 0; i < NCH; ++i) {
+      const int c = at + T * i;
+      const bool live = c < chunks;
+      f2_t w[P];
+#pragma unroll
+      for (int k = 0; k < P; ++k) {
+        f[i][k] = fmul2(f[i][k], f2(rs, rs));
+        if (kept) f[i][k] = fmul2(f[i][k], (*kept)[i][k]);
+      }
+      if (!kept && n.weight) {
+        load_p(n.weight + c * V, live, w);
+#pragma unroll
+        for (int k = 0; k < P; ++k) f[i][k] = fmul2(f[i][k], w[k]);
+      }
+      if (n.bias) {
+        load_p(n.bias + c * V, live, w);
+#pragma unroll
+        for (int k = 0; k < P; ++k) f[i][k] = fadd2(f[i][k], w[k]);
+      }
+    }
+  }
+
+  // Row r from its x and h (in f) to r and y; `store`: whether they are written.
+  template <typename Sum>
+  static __device__ __forceinline__ void finish(const AddNormArgs& a, int64_t r, Values& f, const Values& x,
+                                                const Values* post_w, const Values* pre_w, int at, int T, bool store,
+                                                const Sum& sum) {
+    const int C = a.C, chunks = C / V;
+    normalise(a.post, f, post_w, at, T, C, sum);
+    if (a.gate) {
+      const float* gr = a.gate + (a.per == 0u ? 0ll : (int64_t)((uint32_t)r / a.per) * C);
+#pragma unroll
+      for (int i = 0; i < NCH; ++i) {
+        const int c = at + T * i;
+        f2_t g[P];
+        load_p(gr + c * V, c < chunks, g);
+#pragma unroll
+        for (int k = 0; k < P; ++k) f[i][k] = fmul2(f[i][k], g[k]);
+      }
+    }
+    const int64_t row = r * C;
+    const f2_t scale = f2(a.scale, a.scale);
+#pragma unroll
+    for (int i = 0; i < NCH; ++i) {
+      const int c = at + T * i;
+#pragma unroll
+      for (int k = 0; k < P; ++k) f[i][k] = ffma2(f[i][k], scale, x[i][k]);
+      if (a.r && c < chunks && store) store_p(static_cast<RT*>(a.r) + row + c * V, f[i]);
+    }
+    if (!a.y) return;
+    normalise(a.pre, f, pre_w, at, T, C, sum);
+#pragma unroll
+    for (int i = 0; i < NCH; ++i) {
+      const int c = at + T * i;
+      if (c < chunks && store) store_p(a.y + row + c * V, f[i]);
+    }
+  }
+};
+
 template <int VALUES>
 constexpr int kNormThreads = VALUES == 8 ? 1024 : 512;  // at most
 constexpr int kNormStages = 4;  // at most
@@ -73,6 +179,7 @@ constexpr int kNormStages = 4;  // at most
 template <typename RT, int VALUES>
 __global__ void __launch_bounds__(kNormThreads<VALUES>, VALUES <= 16 ? 1024 / kNormThreads<VALUES> : 1) add_norm_kernel(const __grid_constant__ AddNormArgs a) {
   constexpr int V = 16 / sizeof(RT), NCH = VALUES / V, P = V / 2;
+  using Row = NormRow<RT, NCH>;
   constexpr bool KEEP = VALUES == 8;
   extern __shared__ __align__(128) uint8_t norm_smem[];  // stages: a row of x, a row of h
   __shared__ float s_sum[2][32];
@@ -80,7 +187,6 @@ __global__ void __launch_bounds__(kNormThreads<VALUES>, VALUES <= 16 ? 1024 / kN
   __shared__ int s_abort;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, T = (int)blockDim.x, at = (int)threadIdx.x;
   const int C = a.C, chunks = C / V;
-  const float inv_c = 1.f / (float)C;
   const uint32_t xbytes = a.x ? (uint32_t)C * sizeof(RT) : 0u, hbytes = a.h ? (uint32_t)C * 2u : 0u;
   const long long limit = a.wait_limit ? a.wait_limit : kWaitLimitCycles;
   const unsigned S = (unsigned)a.stages;
@@ -122,76 +228,17 @@ __global__ void __launch_bounds__(kNormThreads<VALUES>, VALUES <= 16 ? 1024 / kN
   };
   // the norms' weights of the thread's columns: in registers, or read again for every row
   // (from L1) where there are too many
-  f2_t post_w[KEEP ? NCH : 1][P], pre_w[KEEP ? NCH : 1][P];
-  auto keep = [&](const NormDev& n, f2_t (&w)[KEEP ? NCH : 1][P]) {
-#pragma unroll
-    for (int i = 0; i < (KEEP ? NCH : 1); ++i) {
-#pragma unroll
-      for (int k = 0; k < P; ++k) w[i][k] = f2(1.f, 1.f);
-      if (n.weight) load_p(n.weight + (at + T * i) * V, at + T * i < chunks, w[i]);
-    }
-  };
+  typename Row::Values post_w, pre_w;
   if constexpr (KEEP) {
-    keep(a.post, post_w);
-    keep(a.pre, pre_w);
+    Row::load_weights(a.post, post_w, at, T, C);
+    Row::load_weights(a.pre, pre_w, at, T, C);
   }
-  f2_t f[NCH][P];
-  // f = N(f); columns past the row are zero, and stay zero until the affine part
-  auto normalise = [&](const NormDev& n, f2_t (&nw)[KEEP ? NCH : 1][P]) {
-    if (n.kind == 0) return;
-    float lo, hi;
-    if (n.kind == 2) {
-      f2_t s = f[0][0];
-#pragma unroll
-      for (int i = 0; i < NCH; ++i)
-#pragma unroll
-        for (int k = 0; k < P; ++k)
-          if (i + k > 0) s = fadd2(s, f[i][k]);
-      f2_split(s, lo, hi);
-      const float mean = sum(lo + hi) * -inv_c;
-#pragma unroll
-      for (int i = 0; i < NCH; ++i)
-        if (at + T * i < chunks)
-#pragma unroll
-          for (int k = 0; k < P; ++k) f[i][k] = fadd2(f[i][k], f2(mean, mean));
-    }
-    f2_t q = fmul2(f[0][0], f[0][0]);
-#pragma unroll
-    for (int i = 0; i < NCH; ++i)
-#pragma unroll
-      for (int k = 0; k < P; ++k)
-        if (i + k > 0) q = ffma2(f[i][k], f[i][k], q);
-    f2_split(q, lo, hi);
-    const float rs = rsqrtf(sum(lo + hi) * inv_c + n.eps);
-#pragma unroll
-    for (int i = 0; i < NCH; ++i) {
-      const int c = at + T * i;
-      const bool live = c < chunks;
-      f2_t w[P];
-#pragma unroll
-      for (int k = 0; k < P; ++k) {
-        f[i][k] = fmul2(f[i][k], f2(rs, rs));
-        if constexpr (KEEP) f[i][k] = fmul2(f[i][k], nw[i][k]);
-      }
-      if (!KEEP && n.weight) {
-        load_p(n.weight + c * V, live, w);
-#pragma unroll
-        for (int k = 0; k < P; ++k) f[i][k] = fmul2(f[i][k], w[k]);
-      }
-      if (n.bias) {
-        load_p(n.bias + c * V, live, w);
-#pragma unroll
-        for (int k = 0; k < P; ++k) f[i][k] = fadd2(f[i][k], w[k]);
-      }
-    }
-  };
   bool ok = true;
   unsigned st = 0, phase = 0;
-  const f2_t scale = f2(a.scale, a.scale);
 #pragma unroll 1
   for (int64_t r = blockIdx.x; r < a.R; r += step) {
     const uint8_t* stage = norm_smem + st * (xbytes + hbytes);
-    f2_t x[NCH][P];
+    typename Row::Values x, f;
     ok = mbar_wait(smem_u32(&s_full[st]), phase, a.err, &s_abort, kErrTimeoutFull, limit) && ok;
 #pragma unroll
     for (int i = 0; i < NCH; ++i) {
@@ -208,37 +255,43 @@ __global__ void __launch_bounds__(kNormThreads<VALUES>, VALUES <= 16 ? 1024 / kN
       st = 0;
       phase ^= 1u;
     }
-    normalise(a.post, post_w);
-    if (a.gate) {
-      const float* gr = a.gate + (a.per == 0u ? 0ll : (int64_t)((uint32_t)r / a.per) * C);
-#pragma unroll
-      for (int i = 0; i < NCH; ++i) {
-        const int c = at + T * i;
-        f2_t g[P];
-        load_p(gr + c * V, c < chunks, g);
-#pragma unroll
-        for (int k = 0; k < P; ++k) f[i][k] = fmul2(f[i][k], g[k]);
-      }
-    }
-    const int64_t row = r * C;
-#pragma unroll
-    for (int i = 0; i < NCH; ++i) {
-      const int c = at + T * i;
-#pragma unroll
-      for (int k = 0; k < P; ++k) f[i][k] = ffma2(f[i][k], scale, x[i][k]);
-      if (a.r && c < chunks && ok) store_p(static_cast<RT*>(a.r) + row + c * V, f[i]);
-    }
-    if (!a.y) continue;
-    normalise(a.pre, pre_w);
-#pragma unroll
-    for (int i = 0; i < NCH; ++i) {
-      const int c = at + T * i;
-      if (c < chunks && ok) store_p(a.y + row + c * V, f[i]);
-    }
+    Row::finish(a, r, f, x, KEEP ? &post_w : nullptr, KEEP ? &pre_w : nullptr, at, T, ok, sum);
   }
   // after a timeout: no copy is in flight into shared memory that is given back
   if (!ok && at == 0)
     for (unsigned i = fills > S ? fills - S : 0u; i < fills; ++i) mbar_drain(smem_u32(&s_full[i % S]), (i / S) & 1u, limit);
+}
+
+// Short rows: a warp for each, which needs no barrier and no shared memory, and a CTA for
+// every two or four (rows of 512 bytes: 5.8 us for 12000 with four, 6.6 with two).  The next
+// norm's weights are on their way with the row where a lane has 24 values of it ([6304, 768]
+// bf16 9.8 us so, 10.6 without; with 16 values 6.6 and 6.1, with 32 12.1 and 11.6: the
+// registers that they take cost warps).
+template <typename RT, int NCH>
+constexpr int kShortWarps = NCH * 16 / sizeof(RT) <= 8 ? 4 : 2;
+template <typename RT, int NCH>
+__global__ void __launch_bounds__(32 * kShortWarps<RT, NCH>) short_norm_kernel(const __grid_constant__ AddNormArgs a) {
+  using Row = NormRow<RT, NCH>;
+  const int lane = threadIdx.x & 31, C = a.C, chunks = C / Row::V;
+  const int64_t r = (int64_t)blockIdx.x * kShortWarps<RT, NCH> + (threadIdx.x >> 5);
+  pdl_wait();
+  pdl_trigger();
+  if (r >= a.R) return;
+  typename Row::Values x, f;
+#pragma unroll
+  for (int i = 0; i < NCH; ++i) {
+    const int c = lane + 32 * i;
+    load_p(static_cast<const RT*>(a.x) + r * C + c * Row::V, a.x && c < chunks, x[i]);
+    load_p(a.h + r * C + c * Row::V, a.h && c < chunks, f[i]);
+  }
+  typename Row::Values pre_w;
+  constexpr bool EARLY = NCH * Row::V == 24;
+  if constexpr (EARLY) Row::load_weights(a.pre, pre_w, lane, 32, C);
+  Row::finish(a, r, f, x, nullptr, EARLY ? &pre_w : nullptr, lane, 32, true, [](float v) {
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
+    return v;
+  });
 }
 
 // ---------------------------------------------------------------------------
@@ -383,11 +436,33 @@ cudaError_t launch_add_norm_v(AddNormArgs a, cudaStream_t s) {
                        s, a);
 }
 
-// Two 16-byte pieces of the stream a thread ([8192, 4096] bf16 46 us, one 48; fp32 75, four
-// 78), one of a short bf16 row, whose weights then stay in registers ([6304, 768] 12.9 us,
-// two 14.2), and four or eight where threads run out.
+template <typename RT, int NCH>
+cudaError_t launch_short_norm(const AddNormArgs& a, cudaStream_t s) {
+  constexpr int W = kShortWarps<RT, NCH>;
+  return launch_kernel(short_norm_kernel<RT, NCH>, dim3((unsigned)((a.R + W - 1) / W)), dim3(32 * W), 0, s, a);
+}
+
+// A warp a row where it has two 16-byte pieces of the stream a lane at most ([6304, 64] bf16
+// 2.4 us, by CTAs 5.3; [300, 512] 2.6 and 2.5) and, up to 1024 values, where there are 8 rows
+// an SM ([6304, 768] bf16 with a gate 9.9, 12.7; [2500, 768] fp32 5.6, 6.2; 1200 rows equal;
+// [300, 768] 3.1, 2.6: CTAs begin on a row with more loads), or 16 with more than 6 pieces
+// ([2500, 1024] fp32 7.8, 8.5; 1200 rows 6.0, 4.9).  Else by CTAs:
+// two pieces a thread ([8192, 4096] bf16 46 us, one 48; fp32 75, four 78), one of a bf16 row
+// of up to 1024 values, whose weights then stay in registers ([6304, 768] 12.9, two 14.2),
+// and four or eight where threads run out.
 template <typename RT>
 cudaError_t launch_add_norm_t(const AddNormArgs& a, cudaStream_t s) {
+  const int pieces = (a.C * (int)sizeof(RT) + 511) / 512;
+  if (pieces == 1) return launch_short_norm<RT, 1>(a, s);
+  if (pieces == 2) return launch_short_norm<RT, 2>(a, s);
+  if (a.C <= 1024 && a.R >= (pieces <= 6 ? 8ll : 16ll) * device_sm_count()) {
+    if constexpr (sizeof(RT) == 2)
+      return pieces == 3 ? launch_short_norm<RT, 3>(a, s) : launch_short_norm<RT, 4>(a, s);
+    else
+      return pieces <= 4   ? launch_short_norm<RT, 4>(a, s)
+             : pieces <= 6 ? launch_short_norm<RT, 6>(a, s)
+                           : launch_short_norm<RT, 8>(a, s);
+  }
   if (a.C > 8192) return launch_add_norm_v<RT, 32>(a, s);
   if constexpr (sizeof(RT) == 2)
     if (a.C > 1024) return launch_add_norm_v<RT, 16>(a, s);

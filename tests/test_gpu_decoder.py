@@ -96,6 +96,22 @@ def test_add_norm(sp, ctx, R, C, res, post, pre, gate):
     assert occ.to_host()["nnz"] == int((y != 0).sum())
 
 
+@pytest.mark.parametrize("R,C", [(1221, 200), (1301, 520), (2433, 600), (1217, 768), (1251, 1000), (1219, 1024), (2435, 1024), (1303, 1032)])
+@pytest.mark.parametrize("res", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("post,pre,gate", [("none", "layer", 197), ("rms", "rms", None), ("layer", "layer", 0)])
+def test_add_norm_many_rows(sp, ctx, R, C, res, post, pre, gate):
+    """More rows than CTAs are on the GPU at once, of lengths around those that a warp takes alone; in place too."""
+    test_add_norm(sp, ctx, R, C, res, post, pre, gate)
+    g = _g(R)
+    x = torch.randn(R, C, generator=g).to(res)
+    h = torch.randn(R, C, generator=g).to(torch.bfloat16)
+    w = _params("rms", C, 3)
+    xd, hd = x.cuda(), h.cuda()
+    sp.sparoa_add_norm(ctx, xd, hd, xd, hd, pre=sp.norm("rms", w[1].cuda()))
+    _close(xd, x.double() + h.double(), "r in place of x")
+    _close(hd, _norm64(x.double() + h.double(), w, 1e-6), "y in place of h")
+
+
 def test_add_norm_parts(sp, ctx):
     """No block output (a first norm), no stream before it, no output asked for, and results in place."""
     R, C = 37, 1000
