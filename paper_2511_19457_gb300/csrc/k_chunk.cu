@@ -35,6 +35,10 @@ namespace {
 // sum are only rescaled where the maximum has outgrown m by more than 2^8 in weight
 // (the weights, their sum and O hold that easily), which after a row's first units is
 // rare.  The end's O / sum is the same number.
+// Weights are 2^(s sl2 - z) in one FMA, z the scaled reference as rounded to fp32 (to a
+// quarter at scores of 2^24 / 8).  So everything that brings weights of two references together
+// (rescaling, the two groups' sums, the parts of an item) goes by the same z, and the log of the
+// sum takes back what the rounding added.
 constexpr int kRows = 256;     // rows of an item
 constexpr int kTileRows = 128;
 constexpr int kSoftWarps = 8;
@@ -65,6 +69,18 @@ struct Cfg {
   static constexpr uint32_t kCols = 512;                // S, S, O, O: 256 + 2 D columns, to a power of two
   static constexpr uint32_t kO = 256;                   // first column of O
 };
+
+__device__ __forceinline__ float scaled_ref(float m, float sl2) { return __fmul_rn(m, sl2); }
+// what weights by reference m are multiplied by to go by `top`
+__device__ __forceinline__ float to_ref(float m, float top, float sl2) {
+  return m == -INFINITY ? 0.f : ex2(scaled_ref(m, sl2) - scaled_ref(top, sl2));
+}
+// log of the sum of exp(scale s), of which l is by reference m
+__device__ __forceinline__ float log_sum(float m, float l, float scale, float sl2) {
+  if (l == 0.f) return -INFINITY;
+  const float added = fmaf(-m, sl2, scaled_ref(m, sl2));  // (exact)
+  return fmaf(m, scale, fmaf(added, 0.6931471805599453f, logf(l)));
+}
 
 struct JoinItem {
   int c0, c1;  // CTAs that share the item
@@ -478,7 +494,7 @@ __device__ __forceinline__ void softmax_role(const Role& r, uint32_t tmem) {
           m = mx;
         } else if (__any_sync(0xffffffffu, grows)) {
           // S of this unit is complete, so the product before it is: O stands still
-          const float f = !grows ? 1.f : (m == -INFINITY ? 0.f : ex2((m - mx) * sl2));
+          const float f = grows ? to_ref(m, mx, sl2) : 1.f;
           if (grows) m = mx;
           l *= f;
 #pragma unroll 1
@@ -491,7 +507,7 @@ __device__ __forceinline__ void softmax_role(const Role& r, uint32_t tmem) {
             tmem_st16(to + i * 16, q);
           }
         }
-        const float nz = m == -INFINITY ? 0.f : -m * sl2;
+        const float nz = m == -INFINITY ? 0.f : -scaled_ref(m, sl2);
         const f2_t sc = f2(sl2, sl2), off = f2(nz, nz);
         f2_t sum[4];
         auto weigh = [&](auto two_parts) {
@@ -550,8 +566,8 @@ __device__ __forceinline__ void softmax_role(const Role& r, uint32_t tmem) {
         if (!(ok = r.wait(bars.joined, joins++ & 1u, kErrTimeoutAcc))) break;
         tc_fence_after();
         const float m1 = r.sh.m[row], l1 = r.sh.l[row], top = fmaxf(m, m1);
-        f0 = m == -INFINITY ? 0.f : ex2((m - top) * sl2);
-        f1 = m1 == -INFINITY ? 0.f : ex2((m1 - top) * sl2);
+        f0 = to_ref(m, top, sl2);
+        f1 = to_ref(m1, top, sl2);
         l = l * f0 + l1 * f1;
         m = top;
       }
@@ -625,7 +641,7 @@ __device__ __forceinline__ void softmax_role(const Role& r, uint32_t tmem) {
           slot[kRows * D + at] = m;
           slot[kRows * D + kRows + at] = l;
         } else if (live && a.lse) {
-          a.lse[out] = l == 0.f ? -INFINITY : fmaf(m, a.scale, logf(l));
+          a.lse[out] = log_sum(m, l, a.scale, sl2);
         }
       }
     }
@@ -756,17 +772,13 @@ __global__ void __launch_bounds__(4 * D)
   if (!live) return;
   float l = 0.f, mx = -INFINITY;
   for (int c = 0; c < parts; ++c) mx = fmaxf(mx, s_w[c][lane]);
-  auto weight = [&](int c) {
-    const float m = s_w[c][lane];
-    return m == -INFINITY ? 0.f : ex2((m - mx) * sl2);
-  };
   float f[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
   for (int c0 = 0; c0 < parts; c0 += kJoinParts) {
     if (c0 > 0) fetch(c0);
 #pragma unroll
     for (int i = 0; i < kJoinParts; ++i) {
       if (c0 + i >= parts) break;
-      const float w = weight(c0 + i);
+      const float w = to_ref(s_w[c0 + i][lane], mx, sl2);
       l = fmaf(w, s_l[c0 + i][lane], l);
       f[0] = fmaf(w, p[i].x, f[0]); f[1] = fmaf(w, p[i].y, f[1]); f[2] = fmaf(w, p[i].z, f[2]); f[3] = fmaf(w, p[i].w, f[3]);
       f[4] = fmaf(w, q[i].x, f[4]); f[5] = fmaf(w, q[i].y, f[5]); f[6] = fmaf(w, q[i].z, f[6]); f[7] = fmaf(w, q[i].w, f[7]);
@@ -778,7 +790,7 @@ __global__ void __launch_bounds__(4 * D)
   const int row = j.t * kRows + r, of = over_group(a, row);
   const int64_t at = (int64_t)(j.q0 + of) * a.heads + j.h * a.group + row - of * a.group;
   *reinterpret_cast<uint4*>(a.y + at * D + warp * 8) = pack8(f);
-  if (a.lse && warp == 0) a.lse[at] = l == 0.f ? -INFINITY : fmaf(mx, a.scale, logf(l));
+  if (a.lse && warp == 0) a.lse[at] = log_sum(mx, l, a.scale, sl2);
 }
 
 int grid_of() {
