@@ -43,6 +43,27 @@ class Pages:
         self.held[seq] = pages + [self.free.pop() for _ in range(need)]
         self.length[seq] = length
 
+    def grow_all(self, seqs, new):
+        """Room for new[i] more tokens of each of seqs; raises, and changes nothing, if the cache is full."""
+        length: dict = {}
+        for s, n in zip(seqs, new):
+            length[s] = length.get(s, self.length.get(s, 0)) + n
+        need = sum(-(-n // self.page_size) - len(self.held.get(s, [])) for s, n in length.items())
+        if need > len(self.free):
+            raise RuntimeError(f"cache full: {need} pages wanted, {len(self.free)} free")
+        for s, n in zip(seqs, new):
+            self.grow(s, n)
+
+    def shrink_all(self, seqs, new):
+        """Takes back the grow_all of the same tokens, if nothing came after it."""
+        for s, n in zip(reversed(seqs), reversed(new)):
+            length, pages = self.length[s] - n, self.held[s]
+            keep = -(-length // self.page_size)
+            self.free += reversed(pages[keep:])
+            self.held[s], self.length[s] = pages[:keep], length
+            if not length:
+                self.release(s)
+
     def release(self, seq):
         """Takes a sequence's pages back, if it has any."""
         self.free += reversed(self.held.pop(seq, []))
@@ -86,9 +107,15 @@ class Decoder:
 
     def forward(self, tokens: torch.Tensor, seqs, new) -> torch.Tensor:
         """tokens int64 [T], new[i] of each of seqs one after the other, appended to their cached ones;
-        returns the logits [T, vocab] (fp32)."""
-        for s, n in zip(seqs, new):
-            self.pages.grow(s, n)
+        returns the logits [T, vocab] (fp32).  A step that raises changes no sequence's length."""
+        self.pages.grow_all(seqs, new)
+        try:
+            return self._forward(tokens, seqs, new)
+        except BaseException:
+            self.pages.shrink_all(seqs, new)  # (what was appended of this step is written over by the next)
+            raise
+
+    def _forward(self, tokens, seqs, new):
         ctx, T, dev = self.ctx, tokens.numel(), tokens.device
         batch = self.pages.batch(seqs, new, dev)
 
