@@ -145,7 +145,12 @@ class Decoder:
 
     def generate(self, prompts, steps: int, chunk: int = 256):
         """Greedy tokens after each prompt (lists of token numbers): prompts in chunks of at most
-        `chunk` tokens each, all sequences together, then one token of each at a time."""
+        `chunk` tokens each, all sequences together, then one token of each at a time.  No prompts:
+        no tokens; an empty prompt, which nothing can be said after, is refused."""
+        if not all(prompts):
+            raise ValueError("generate: a prompt without tokens")
+        if not prompts:
+            return []
         seqs = [object() for _ in prompts]
         try:
             return self._generate(seqs, prompts, steps, chunk)

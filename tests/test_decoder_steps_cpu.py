@@ -54,3 +54,13 @@ def test_grow_all_and_back():
     assert p.length == {"a": 41, "b": 16} and len(p.held["a"]) == 3 and len(p.free) == 4
     p.shrink_all(["a", "b", "a"], [30, 16, 1])
     assert _state(p) == before
+
+
+def test_prompts_without_tokens():
+    p = Pages(4, 16)
+    model = _decoder(p)
+    assert model.generate([], 3) == []
+    for prompts in ([[]], [[1, 2], []], [[], [1]]):
+        with pytest.raises(ValueError):
+            model.generate(prompts, 3)
+    assert len(p.free) == 4 and not p.held
