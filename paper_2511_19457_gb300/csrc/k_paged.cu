@@ -236,7 +236,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (__any_sync(0xffffffffu, grows)) {
           const float n0 = fmaxf(m0, x0), n1 = fmaxf(m1, x1);
           // (a row that has seen no key yet: nothing to rescale)
-          const float c0 = m0 == -INFINITY ? 0.f : ex2((m0 - n0) * sl2), c1 = m1 == -INFINITY ? 0.f : ex2((m1 - n1) * sl2);
+          const float c0 = m0 == -INFINITY ? 0.f : exp2f((m0 - n0) * sl2), c1 = m1 == -INFINITY ? 0.f : exp2f((m1 - n1) * sl2);
           m0 = n0;
           m1 = n1;
           l0 *= c0;
@@ -247,13 +247,14 @@ __global__ void __launch_bounds__(kThreads, 1)
             o[j][2] *= c1; o[j][3] *= c1;
           }
         }
+        // (exp2f: weights below the normal range count where their values are large)
         const float z0 = m0 == -INFINITY ? 0.f : m0, z1 = m1 == -INFINITY ? 0.f : m1;
 #pragma unroll
         for (int nt = 0; nt < 2; ++nt) {
-          s[nt][0] = ex2((s[nt][0] - z0) * sl2);
-          s[nt][1] = ex2((s[nt][1] - z0) * sl2);
-          s[nt][2] = ex2((s[nt][2] - z1) * sl2);
-          s[nt][3] = ex2((s[nt][3] - z1) * sl2);
+          s[nt][0] = exp2f((s[nt][0] - z0) * sl2);
+          s[nt][1] = exp2f((s[nt][1] - z0) * sl2);
+          s[nt][2] = exp2f((s[nt][2] - z1) * sl2);
+          s[nt][3] = exp2f((s[nt][3] - z1) * sl2);
           l0 += s[nt][0] + s[nt][1];
           l1 += s[nt][2] + s[nt][3];
         }
@@ -315,7 +316,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         for (int w = 0; w < kWarps; ++w) {
           const float mw = s_m[w][row];
           if (mw == -INFINITY && s_l[w][row] == 0.f) continue;  // saw no key: its sums may not be there
-          const float f = ex2((mw - mx) * sl2);
+          const float f = exp2f((mw - mx) * sl2);
           ls += f * s_l[w][row];
           const uint32_t at = s_at[w] + row * (D * 4) + ((piece ^ (row & 7)) << 5);
           const float4 p = lds_f4(at), q = lds_f4(at + 16);
@@ -369,7 +370,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
               for (int i = 0; i < kParts; ++i) {
                 if (c + i > sh.c1 || (pm[i] == -INFINITY && pl[i] == 0.f)) continue;
-                const float nm = fmaxf(mx, pm[i]), f = mx == -INFINITY ? 0.f : ex2((mx - nm) * sl2), e = ex2((pm[i] - nm) * sl2);
+                const float nm = fmaxf(mx, pm[i]), f = mx == -INFINITY ? 0.f : exp2f((mx - nm) * sl2), e = exp2f((pm[i] - nm) * sl2);
                 mx = nm;
                 ls = ls * f + pl[i] * e;
                 acc[0] = acc[0] * f + v[i].x * e; acc[1] = acc[1] * f + v[i].y * e;

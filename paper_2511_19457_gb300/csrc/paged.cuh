@@ -293,10 +293,4 @@ __device__ __forceinline__ int pool_row(const PagedArgs& a, int page, int h, int
   return (int)(((long long)page * a.kv_heads + h) << a.page_log2) + (key & ((1 << a.page_log2) - 1));
 }
 
-__device__ __forceinline__ float ex2(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-
 }  // namespace sparoa

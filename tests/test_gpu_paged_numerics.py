@@ -108,3 +108,24 @@ def test_scores_far_from_zero_that_grow(sp, ctx, n, H, max_q, D, unit):
     worst = ((y - want).abs() / (2.0 ** -8 * want.abs() + (2.0 ** -8 + 2.0 ** -12) * size)).max()
     assert worst <= 1, f"{worst:.2f} of the tolerance"
     assert ((lse - wl).abs() <= 2.0 ** -22 * wl.abs()).all()
+
+
+@pytest.mark.parametrize("n,H,max_q", FORMS)
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("small,large", [(0, 1), (1, 0), (0, 40), (100, 3), (0, 200), (200, 0), (0, 300), (300, 0), (5, 4000), (4000, 5)])
+def test_weights_below_the_normal_range(sp, ctx, n, H, max_q, D, small, large):
+    """Key `small` has a value of 2^125 and a weight of 2^-128.4 (key `large` scores 712 / 8 higher: in its
+    block of keys, another one, another unit or another CTA's): fp32 and bf16 hold such weights as subnormals,
+    and the output is 2^-3.4.  A weight that is rounded to bf16 there is a multiple of 2^-133: within
+    2^-134 / 2^-128.4 = 2.1 %; the result's own rounding is 2^-9."""
+    L = max(600, max(small, large) + 90)
+    q, k, v = torch.zeros(n, H, D), torch.zeros(L, 1, D), torch.zeros(L, 1, D)
+    q[..., 0] = 8.0
+    k[..., 0] = -1024.0
+    k[small, 0, 0], k[large, 0, 0] = 0.0, 89.0
+    v[small, 0, 0] = 2.0 ** 125
+    want, wl, _ = _plain(q, k, v, 0.125)
+    y, lse = _run(sp, ctx, q, k, v, 0.125, max_q)
+    assert want[0, 0, 0] > 0.09
+    assert (y[..., 0] / want[..., 0] - 1).abs().max() <= 0.021 + 2.0 ** -9
+    assert not y[..., 1:].any() and torch.allclose(lse, wl, rtol=1e-6)
