@@ -522,9 +522,11 @@ sparoa_status sparoa_rope_append(sparoa_ctx *ctx, const void *qkv, int64_t ld_qk
  *   lse   device fp32 [T][heads] (nullable): log of the sum of exp(scale q k) over
  *         the keys that a row sees (-infinity for none)
  *   y_occ occupancy of y to write (nullable); rows of no sequence count as they are
- * Splits long sequences over the GPU; partial results live in a workspace that the
- * context keeps for each stream it is used on, of the last 16 (a graph goes on using
- * that of the stream it was captured on).  A table entry outside [0, pages), or
+ * Splits long sequences over the GPU; partial results live in workspaces (3 to 42 MB)
+ * that the context keeps: one for each of the 16 streams that it was last used on, and
+ * one for each capture and stream of it, which is the graph's own on whichever stream it
+ * is replayed, until the graph and its executable forms are destroyed.  So calls on
+ * several streams and replays of several graphs may overlap.  A table entry outside [0, pages), or
  * a length past the table's row, is reported as INVALID_ARG by the next call that
  * synchronises, and the affected rows hold anything.
  * Errors: INVALID_ARG, UNSUPPORTED (head_dim, page_size, batch), CUDA, OOM, TIMEOUT. */

@@ -2,12 +2,14 @@
 // Declarations and documentation: include/sparoa.h.
 #include <cuda_runtime.h>
 
+#include <atomic>
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
 #include <cstring>
 #include <map>
 #include <mutex>
+#include <new>
 #include <string>
 #include <vector>
 
@@ -75,16 +77,30 @@ struct DevBuf {
   size_t bytes = 0;
 };
 
-// Paged attention's scratch, one for each stream that a context is used on: calls on
-// two streams may run at once.
+// What a slot and the graph that uses it share: whether the graph is gone.
+struct GraphHold {
+  std::atomic<int> owners{2};
+  std::atomic<bool> gone{false};
+  void drop() {
+    if (owners.fetch_sub(1) == 1) delete this;
+  }
+};
+
+// Paged attention's scratch: arrival counters (zero between calls), then partial results.  Calls
+// whose work may overlap must not share one.  So there is one for each stream that the context is
+// used on, the least recently used of which is given to a new stream when there are
+// kPagedSlots; and one for each stream of a capture, which stays its graph's whatever streams that is
+// replayed on, until the graph and its executable forms are gone.
 struct PagedSlot {
   cudaStream_t stream = nullptr;
-  bool taken = false;
+  uint64_t used = 0;               // number of the last call, 0: none
+  unsigned long long capture = 0;  // the capture's id
+  GraphHold* hold = nullptr;       // of a capture
+  PagedSlot* next = nullptr;
   DevBuf ws;
 };
 constexpr int kPagedSlots = 16;
-constexpr size_t kSmallBytes = 256;  // d_err(), d_path(), d_count()
-constexpr size_t kPagedCntBytes = sizeof(unsigned) * kPagedSlots * kPagedCounters;
+constexpr size_t kPagedCntBytes = sizeof(unsigned) * kPagedCounters;
 
 }  // namespace
 
@@ -92,13 +108,14 @@ struct sparoa_ctx {
   int device = 0;
   cudaStream_t stream = nullptr;
   std::string last_error;
-  DevBuf small;       // u32 error flag, i32 path slot, padding; paged attention's counters
+  DevBuf small;       // u32 error flag, i32 path slot, padding
   DevBuf occ;         // occupancy of inputs measured inside a call
   DevBuf pad_x, pad_w;
   DevBuf arena;       // sparoa_run_graph activations, occupancies, paths
   DevBuf splitk;      // split-K arrival counters (kept zero) + fp32 partial tiles
-  PagedSlot paged[kPagedSlots];
-  int paged_next = 0;  // the slot given to a new stream once all are taken
+  PagedSlot paged[kPagedSlots];        // by stream
+  PagedSlot* paged_graphs = nullptr;   // by capture
+  uint64_t paged_calls = 0;
   std::vector<sparoa_occupancy> graph_occ;
   int overlap = 1;    // programmatic dependent launch between consecutive kernels
   int64_t wait_limit = 0;  // SM cycles before a kernel's bounded wait gives up (0: default)
@@ -109,9 +126,6 @@ struct sparoa_ctx {
   int32_t* d_path() const { return reinterpret_cast<int32_t*>(reinterpret_cast<char*>(small.p) + 16); }
   // Eq. 1 count of an FC input that the fused small-FC kernel measures itself
   uint64_t* d_count() const { return reinterpret_cast<uint64_t*>(reinterpret_cast<char*>(small.p) + 32); }
-  unsigned* d_paged_cnt(int slot) const {
-    return reinterpret_cast<unsigned*>(reinterpret_cast<char*>(small.p) + kSmallBytes) + slot * kPagedCounters;
-  }
 };
 
 namespace {
@@ -646,13 +660,13 @@ sparoa_status sparoa_create(sparoa_ctx** out, int device, void* stream) {
   sparoa_ctx* ctx = new sparoa_ctx();
   ctx->device = device;
   ctx->stream = static_cast<cudaStream_t>(stream);
-  if (cudaMalloc(&ctx->small.p, kSmallBytes + kPagedCntBytes) != cudaSuccess) {
+  if (cudaMalloc(&ctx->small.p, 256) != cudaSuccess) {
     cudaGetLastError();
     delete ctx;
     return SPAROA_ERR_OOM;
   }
-  ctx->small.bytes = kSmallBytes + kPagedCntBytes;
-  if (cudaMemset(ctx->small.p, 0, ctx->small.bytes) != cudaSuccess) {
+  ctx->small.bytes = 256;
+  if (cudaMemset(ctx->small.p, 0, 256) != cudaSuccess) {
     cudaFree(ctx->small.p);
     delete ctx;
     return SPAROA_ERR_CUDA;
@@ -699,6 +713,12 @@ sparoa_status sparoa_destroy(sparoa_ctx* ctx) {
     if (b->p) cudaFree(b->p);
   for (PagedSlot& p : ctx->paged)
     if (p.ws.p) cudaFree(p.ws.p);
+  while (PagedSlot* p = ctx->paged_graphs) {
+    ctx->paged_graphs = p->next;
+    if (p->ws.p) cudaFree(p->ws.p);
+    if (p->hold) p->hold->drop();
+    delete p;
+  }
   if (ctx->ev_fork) cudaEventDestroy(ctx->ev_fork);
   if (ctx->ev_join) cudaEventDestroy(ctx->ev_join);
   if (ctx->aux) cudaStreamDestroy(ctx->aux);
@@ -1317,35 +1337,99 @@ int log2_of(int v) {
   return l;
 }
 
-// The scratch of the context's current stream.  A stream's first call may be under
-// capture: its buffer is then allocated in the relaxed mode (no work is enqueued).
-sparoa_status paged_slot(sparoa_ctx* ctx, int* out) {
-  for (int i = 0; i < kPagedSlots; ++i)
-    if (ctx->paged[i].taken && ctx->paged[i].stream == ctx->stream) {
-      *out = i;
+// Room for `bytes` of partial results, and counters that are zero.  The context's stream may be
+// under capture (nothing is enqueued on it).
+sparoa_status paged_room(sparoa_ctx* ctx, PagedSlot& p, size_t bytes) {
+  cudaStreamCaptureMode mode = cudaStreamCaptureModeRelaxed;
+  SP_CUDA(cudaThreadExchangeStreamCaptureMode(&mode));
+  sparoa_status st = ensure(ctx, p.ws, kPagedCntBytes + bytes);
+  if (st == SPAROA_OK) {
+    cudaStream_t s = nullptr;
+    cudaError_t e = cudaStreamCreateWithFlags(&s, cudaStreamNonBlocking);
+    if (e == cudaSuccess) e = cudaMemsetAsync(p.ws.p, 0, kPagedCntBytes, s);
+    if (e == cudaSuccess) e = cudaStreamSynchronize(s);
+    if (s) cudaStreamDestroy(s);
+    if (e != cudaSuccess) {
+      cudaGetLastError();
+      cudaFree(p.ws.p);
+      p.ws = DevBuf();
+      st = fail(ctx, SPAROA_ERR_CUDA, "paged_attention: counters: %s", cudaGetErrorString(e));
+    }
+  }
+  cudaThreadExchangeStreamCaptureMode(&mode);
+  return st;
+}
+
+void CUDART_CB graph_gone(void* p) {  // (on a thread of the driver's)
+  GraphHold* h = static_cast<GraphHold*>(p);
+  h->gone.store(true);
+  h->drop();
+}
+
+// The scratch of capture `id` into `graph` on the context's stream: what it has already, what a graph
+// that is gone has left, or more.
+sparoa_status paged_graph_slot(sparoa_ctx* ctx, unsigned long long id, cudaGraph_t graph, size_t bytes, PagedSlot** out) {
+  PagedSlot* left = nullptr;
+  for (PagedSlot* p = ctx->paged_graphs; p; p = p->next) {
+    if (p->ws.bytes < kPagedCntBytes + bytes) continue;
+    if (p->hold && !p->hold->gone.load()) {
+      if (p->capture != id || p->stream != ctx->stream) continue;
+      *out = p;
       return SPAROA_OK;
     }
-  int i = 0;
-  while (i < kPagedSlots && ctx->paged[i].taken) ++i;
-  if (i == kPagedSlots) {
+    if (!left || p->ws.bytes < left->ws.bytes) left = p;
+  }
+  if (!left) {
+    left = new (std::nothrow) PagedSlot;
+    if (!left) return fail(ctx, SPAROA_ERR_OOM, "paged_attention: no host memory");
+    left->next = ctx->paged_graphs;
+    ctx->paged_graphs = left;
+  }
+  if (left->hold) left->hold->drop();
+  left->hold = nullptr;
+  SP_TRY(paged_room(ctx, *left, bytes));
+  GraphHold* hold = new (std::nothrow) GraphHold;
+  if (!hold) return fail(ctx, SPAROA_ERR_OOM, "paged_attention: no host memory");
+  cudaUserObject_t object = nullptr;
+  cudaError_t e = cudaUserObjectCreate(&object, hold, graph_gone, 1, cudaUserObjectNoDestructorSync);
+  if (e != cudaSuccess) {
+    delete hold;
+    SP_CUDA(e);
+  }
+  left->hold = hold;
+  left->capture = id;
+  left->stream = ctx->stream;
+  e = cudaGraphRetainUserObject(graph, object, 1, cudaGraphUserObjectMove);
+  if (e != cudaSuccess) cudaUserObjectRelease(object, 1);  // (the slot is free again)
+  SP_CUDA(e);
+  *out = left;
+  return SPAROA_OK;
+}
+
+// The scratch of a call on the context's stream.
+sparoa_status paged_slot(sparoa_ctx* ctx, const PagedArgs& a, PagedSlot** out) {
+  if (ctx->stream != nullptr && ctx->stream != cudaStreamLegacy) {  // (those are never captured)
     cudaStreamCaptureStatus cap = cudaStreamCaptureStatusNone;
-    SP_CUDA(cudaStreamIsCapturing(ctx->stream, &cap));
-    if (cap != cudaStreamCaptureStatusNone)
-      return fail(ctx, SPAROA_ERR_UNSUPPORTED, "paged_attention: capture on more than %d streams of a context", kPagedSlots);
-    SP_CUDA(cudaDeviceSynchronize());  // the slot's last calls may be running
-    i = ctx->paged_next;
-    ctx->paged_next = (i + 1) % kPagedSlots;
+    unsigned long long id = 0;
+    cudaGraph_t graph = nullptr;
+    SP_CUDA(cudaStreamGetCaptureInfo(ctx->stream, &cap, &id, &graph, nullptr, nullptr, nullptr));
+    if (cap == cudaStreamCaptureStatusActive) return paged_graph_slot(ctx, id, graph, paged_ws_bytes(a), out);
   }
-  if (!ctx->paged[i].ws.p) {
-    cudaStreamCaptureMode mode = cudaStreamCaptureModeRelaxed;
-    SP_CUDA(cudaThreadExchangeStreamCaptureMode(&mode));
-    const sparoa_status st = ensure(ctx, ctx->paged[i].ws, paged_ws_bytes());
-    cudaThreadExchangeStreamCaptureMode(&mode);
-    SP_TRY(st);
+  PagedSlot* p = &ctx->paged[0];
+  for (PagedSlot& s : ctx->paged) {
+    if (s.used && s.stream == ctx->stream) {
+      p = &s;
+      break;
+    }
+    if (s.used < p->used) p = &s;
   }
-  ctx->paged[i].taken = true;
-  ctx->paged[i].stream = ctx->stream;
-  *out = i;
+  if (!p->used || p->stream != ctx->stream) {
+    if (p->used) SP_CUDA(cudaDeviceSynchronize());  // its last calls may be running
+    if (!p->ws.p) SP_TRY(paged_room(ctx, *p, paged_ws_bytes()));
+    p->stream = ctx->stream;
+  }
+  p->used = ++ctx->paged_calls;
+  *out = p;
   return SPAROA_OK;
 }
 
@@ -1473,8 +1557,6 @@ sparoa_status sparoa_paged_attention(sparoa_ctx* ctx, const void* q, int64_t ld_
   SP_TRY(check_occ(ctx, y_occ, T, heads * D, "paged_attention y_occ"));
   DeviceGuard g(ctx->device, ctx->overlap);
   if (T > 0) {
-    int slot = 0;
-    SP_TRY(paged_slot(ctx, &slot));
     PagedArgs a;
     a.q = static_cast<const __nv_bfloat16*>(q);
     a.ld_q = ld_q;
@@ -1504,8 +1586,10 @@ sparoa_status sparoa_paged_attention(sparoa_ctx* ctx, const void* q, int64_t ld_
     a.max_q = batch->max_q;
     a.y = static_cast<__nv_bfloat16*>(y);
     a.lse = lse;
-    a.ws = static_cast<float*>(ctx->paged[slot].ws.p);
-    a.cnt = ctx->d_paged_cnt(slot);
+    PagedSlot* slot = nullptr;
+    SP_TRY(paged_slot(ctx, a, &slot));
+    a.cnt = static_cast<unsigned*>(slot->ws.p);
+    a.ws = static_cast<float*>(slot->ws.p) + kPagedCounters;
     a.err = ctx->d_err();
     a.wait_limit = ctx->wait_limit;
     a.fault = ctx->fault == 1;

@@ -402,6 +402,14 @@ __global__ void __launch_bounds__(kThreads, 1)
     for (unsigned i = used; i < issued; ++i) mbar_drain(smem_u32(&s_bar[warp][i % S]), (i / S) & 1u, limit);
 }
 
+bool few_rows(const PagedArgs& a) { return (int64_t)a.max_q * a.group <= kRows; }
+
+int grid_of() {
+  const int sms = device_sm_count();
+  return sms < kPagedCounters ? sms : kPagedCounters;
+}
+size_t small_ws_bytes() { return (size_t)2 * kPagedCounters * kSlotFloats<128> * sizeof(float); }
+
 template <int D>
 cudaError_t launch_small(const PagedArgs& a, cudaStream_t s) {
   CUtensorMap tk, tv;
@@ -410,20 +418,19 @@ cudaError_t launch_small(const PagedArgs& a, cudaStream_t s) {
     return cudaErrorInvalidValue;
   const cudaError_t e = smem_optin(reinterpret_cast<const void*>(paged_small_kernel<D>), Cfg<D>::kSmem);
   if (e != cudaSuccess) return e;
-  const int sms = device_sm_count();
-  const int grid = sms < kPagedCounters ? sms : kPagedCounters;
-  return launch_kernel(paged_small_kernel<D>, dim3(grid), dim3(kThreads), Cfg<D>::kSmem, s, tk, tv, a);
+  return launch_kernel(paged_small_kernel<D>, dim3(grid_of()), dim3(kThreads), Cfg<D>::kSmem, s, tk, tv, a);
 }
 
 }  // namespace
 
 size_t paged_ws_bytes() {
-  const size_t small = (size_t)2 * kPagedCounters * kSlotFloats<128> * sizeof(float), chunk = paged_chunk_ws_bytes();
+  const size_t small = small_ws_bytes(), chunk = paged_chunk_ws_bytes();
   return small > chunk ? small : chunk;
 }
+size_t paged_ws_bytes(const PagedArgs& a) { return few_rows(a) ? small_ws_bytes() : paged_chunk_ws_bytes(); }
 
 cudaError_t launch_paged_attention(const PagedArgs& a, cudaStream_t s) {
-  if ((int64_t)a.max_q * a.group > kRows) return launch_paged_chunk(a, s);
+  if (!few_rows(a)) return launch_paged_chunk(a, s);
   return a.D == 128 ? launch_small<128>(a, s) : launch_small<64>(a, s);
 }
 

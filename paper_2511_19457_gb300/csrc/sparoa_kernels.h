@@ -292,7 +292,8 @@ struct PagedArgs {
 };
 constexpr int kPagedMaxBatch = 1024;
 constexpr int kPagedCounters = 256;  // and CTAs at most
-size_t paged_ws_bytes();
+size_t paged_ws_bytes();                    // at most
+size_t paged_ws_bytes(const PagedArgs& a);  // of one call
 cudaError_t launch_paged_attention(const PagedArgs& a, cudaStream_t s);
 // the kernel for chunks of tokens (k_chunk.cu)
 size_t paged_chunk_ws_bytes();
