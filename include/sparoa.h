@@ -500,8 +500,9 @@ sparoa_status sparoa_rope_turns(int32_t rot, double base, int32_t scaling, doubl
  *         its sequence); the place in the cache always goes by kv_len
  * Row lengths are multiples of 8 values, pointers 16-byte aligned.  A new token
  * before its sequence's first position (n > kv_len) is rotated but not cached.
- * An entry of the table outside [0, pages), or a position past the table's row, is
- * not written to and is reported as INVALID_ARG by the next call that synchronises.
+ * An entry of the table outside [0, pages) is not written to, nor are the pages of a
+ * sequence whose rows are outside [0, T) or decrease, or whose length is negative or past
+ * the table's row; each is reported as INVALID_ARG by the next call that synchronises.
  * Errors: INVALID_ARG, UNSUPPORTED (head_dim, page_size, batch), CUDA. */
 sparoa_status sparoa_rope_append(sparoa_ctx *ctx, const void *qkv, int64_t ld_qkv, int64_t T,
                                  int32_t heads, const sparoa_rope *rope, const int32_t *positions,

@@ -331,12 +331,20 @@ __global__ void __launch_bounds__(kRopeThreads) rope_append_kernel(const __grid_
   fetch(threadIdx.x);
   // the token's sequence: how many of them end at or before it
   int b = 0;
+  const int64_t room = (int64_t)a.max_pages << a.page_log2;
   for (int i0 = 0; i0 < a.batch; i0 += kRopeThreads) {
     const int i = i0 + (int)threadIdx.x;
-    b += __syncthreads_count(i < a.batch && (int64_t)a.q_start[i + 1] <= t);
+    const int64_t end = i < a.batch ? a.q_start[i + 1] : 0;
+    b += __syncthreads_count(i < a.batch && end <= t);
+  }
+  if (t == 0) {  // the first CTA looks the lists over
+    for (int i = threadIdx.x; i < a.batch; i += kRopeThreads) {
+      const int64_t begin = a.q_start[i], end = a.q_start[i + 1], len = a.kv_len[i];
+      if (begin < 0 || end < begin || end > a.T || len < 0 || len > room) atomicOr(a.err, kErrBadIndex);
+    }
   }
   if (b >= a.batch || t < a.q_start[0]) return;  // a row of no sequence
-  const int64_t place = (int64_t)a.kv_len[b] - a.q_start[b + 1] + t;
+  const int64_t begin = a.q_start[b], end = a.q_start[b + 1], len = a.kv_len[b], place = len - end + t;
   const uint64_t pos = (uint64_t)(a.positions ? (int64_t)a.positions[t] : place);
   for (int i = threadIdx.x; i < a.rot / 2; i += kRopeThreads) {
     const int32_t turn = (int32_t)((pos * a.turns[i]) >> 32);  // signed fraction of a turn, 2^-32
@@ -347,9 +355,10 @@ __global__ void __launch_bounds__(kRopeThreads) rope_append_kernel(const __grid_
   }
   // the page of the token's place; -1: not cached
   int64_t base = -1;
-  if (place >= 0) {
-    const int64_t col = place >> a.page_log2;
-    const int page = col < a.max_pages ? a.table[b * a.table_stride + col] : -1;
+  // (a sequence that its lists give rows it cannot have caches none of them: they would take the
+  // places of others)
+  if (place >= 0 && begin >= 0 && begin <= t && end > t && end <= a.T && len <= room) {
+    const int page = a.table[b * a.table_stride + (place >> a.page_log2)];
     if (page >= 0 && page < a.pages)
       base = (((int64_t)page * a.kv_heads) << a.page_log2) + (place & ((1 << a.page_log2) - 1));
     else if (threadIdx.x == 0)
