@@ -521,12 +521,14 @@ class Rope:
         self.ref = _byref(self.desc)
 
 
-def _token_rows(t, T, what):
-    """(row length, values of a row) of t [T, width] or [T, heads, head_dim], bf16: rows may be
+def _token_rows(t, T, D, what):
+    """(row length, values of a row) of t [T, width] or [T, heads, D], bf16: rows may be
     strided, the values of a row are adjacent."""
     shape = t.shape
     if not (t.dtype is _bf16 and t.is_cuda and 2 <= len(shape) <= 3 and shape[0] == T):
         _refuse(f"{what}: bf16 rows of {T} tokens wanted")
+    if len(shape) == 3 and shape[2] != D:
+        _refuse(f"{what}: heads of {shape[2]} values over a cache of {D}")
     width = shape[1] if len(shape) == 2 else shape[1] * shape[2]
     if t.is_contiguous():
         return width, width
@@ -540,9 +542,9 @@ def sparoa_rope_append(ctx: Context, qkv, q_out, cache: KVCache, batch: PagedBat
     """Rotate the new tokens' queries (to q_out [T, heads, head_dim]) and keys (to the cache, with the
     values) from qkv [T, (heads + 2 kv_heads) head_dim]; rows may be strided."""
     T = qkv.shape[0]
-    ld, have = _token_rows(qkv, T, "rope_append qkv")
-    ldq, width = _token_rows(q_out, T, "rope_append q_out")
     D = cache.head_dim
+    ld, have = _token_rows(qkv, T, D, "rope_append qkv")
+    ldq, width = _token_rows(q_out, T, D, "rope_append q_out")
     if width % D or have != width + 2 * cache.kv_heads * D:
         _refuse("rope_append: qkv rows hold heads, key heads and value heads; q_out rows the heads")
     if positions is not None:
@@ -560,7 +562,7 @@ def sparoa_paged_attention(ctx: Context, q, y, cache: KVCache, batch: PagedBatch
     """y = softmax(scale q K^T) V of the new tokens over their cached sequences; q [T, heads, head_dim]
     (rows may be strided), y the same (contiguous), lse fp32 [T, heads] or None."""
     T, D = q.shape[0], cache.head_dim
-    ld, width = _token_rows(q, T, "paged_attention q")
+    ld, width = _token_rows(q, T, D, "paged_attention q")
     if width % D or not (y.dtype is _bf16 and y.is_cuda and y.is_contiguous() and y.numel() == T * width):
         _refuse("paged_attention: q rows of whole heads, y of q's size")
     if lse is not None:

@@ -56,3 +56,23 @@ def test_rope_reports_bad_lists(sp, ctx, start, kv, T, bad):
     good = sp.PagedBatch(_ints([0, 2, 3]), _ints([40, 60]), table[:2].contiguous().cuda(), max_q=2)
     sp.sparoa_rope_append(ctx, x, q, cache, good, sp.Rope(64))
     ctx.sync()
+
+
+def test_heads_of_another_size(sp, ctx):
+    """Rows given as heads have heads of the cache's size; flat rows are cut into them."""
+    cache = sp.KVCache(*(torch.zeros(2, 2, 16, 64, dtype=torch.bfloat16, device="cuda") for _ in range(2)))
+    batch = sp.PagedBatch(_ints([0, 2]), _ints([20]), _ints([[0, 1]]), max_q=2)
+    new = lambda *shape: torch.zeros(*shape, dtype=torch.bfloat16, device="cuda")  # noqa: E731
+    rope = sp.Rope(64)
+    for q, y in ((new(2, 2, 128), new(2, 2, 128)), (new(2, 8, 32), new(2, 8, 32))):
+        with pytest.raises(sp.SparoaError):
+            sp.sparoa_paged_attention(ctx, q, y, cache, batch)
+    for qkv, q in ((new(2, 8, 64), new(2, 2, 128)), (new(2, 4, 128), new(2, 4, 64)), (new(2, 512), new(2, 8, 32))):
+        with pytest.raises(sp.SparoaError):
+            sp.sparoa_rope_append(ctx, qkv, q, cache, batch, rope)
+    for q in (new(2, 4, 64), new(2, 256)):
+        sp.sparoa_rope_append(ctx, new(2, 8, 64), q, cache, batch, rope)
+        sp.sparoa_rope_append(ctx, new(2, 512), q, cache, batch, rope)
+        sp.sparoa_paged_attention(ctx, q, new(2, 4, 64), cache, batch)
+        sp.sparoa_paged_attention(ctx, q, new(2, 256), cache, batch)
+    ctx.sync()
