@@ -129,3 +129,32 @@ def test_weights_below_the_normal_range(sp, ctx, n, H, max_q, D, small, large):
     assert want[0, 0, 0] > 0.09
     assert (y[..., 0] / want[..., 0] - 1).abs().max() <= 0.021 + 2.0 ** -9
     assert not y[..., 1:].any() and torch.allclose(lse, wl, rtol=1e-6)
+
+
+@pytest.mark.parametrize("n,H,max_q", [(1, 1, 1), (4, 4, 4), (2, 8, 2), (17, 1, 17), (4, 8, 4), (32, 4, 32), (40, 2, 1)])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("a,b,L", [(0, 1, 2), (3, 90, 100), (0, 130, 300), (5, 280, 300), (1, 4000, 5000)])
+def test_weights_of_few_rows_keep_16_bits(sp, ctx, n, H, max_q, D, a, b, L):
+    """Up to 128 rows per key head go into the product with their weights in two bf16 parts.  Two keys of
+    nearly one weight and opposite values: the result is the difference of the weights, small beside them,
+    so that its own rounding hides nothing.  Two parts leave 2^-16 of a weight, fp32 scores below 4 at most
+    128 2^-24 4 = 2^-15: 2^-14 of sum p |v| together with the result's 2^-8.  Weights of one part exceed that by far."""
+    g = _g(D + L + n)
+    q, k, v = torch.zeros(n, H, D), torch.zeros(L, 1, D), torch.zeros(L, 1, D)
+    q[..., 0] = 1 + 0.5 * torch.rand(n, H, generator=g)
+    q[..., 1] = 64.0
+    q = q.to(torch.bfloat16).float()
+    k[..., 1] = -64.0                       # keys without weight
+    k[a, 0, :2] = torch.tensor([2.0, 0.0])
+    k[b, 0, :2] = torch.tensor([1.75, 0.0])
+    v[a, 0], v[b, 0] = 1.0, -1.0
+    v[a, 0, 1], v[b, 0, 1] = 0.75, -0.625
+    scale = 0.125
+    want, wl, size = _plain(q, k, v, scale)
+    y, lse = _run(sp, ctx, q, k, v, scale, max_q)
+    tol = 2.0 ** -8 * want.abs() + 2.0 ** -14 * size
+    worst = ((y - want).abs() / tol).max()
+    assert worst <= 1, f"{worst:.2f} of the tolerance"
+    assert ((lse - wl).abs() <= 1e-5).all()
+
+
