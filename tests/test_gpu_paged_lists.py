@@ -76,3 +76,58 @@ def test_heads_of_another_size(sp, ctx):
         sp.sparoa_paged_attention(ctx, q, new(2, 4, 64), cache, batch)
         sp.sparoa_paged_attention(ctx, q, new(2, 256), cache, batch)
     ctx.sync()
+
+
+@pytest.mark.parametrize("B", [33, 40, 129, 300, 1024])
+@pytest.mark.parametrize("form", ["single", "ragged", "chunks"])
+def test_many_sequences(sp, ctx, B, form):
+    """Batches longer than a warp, than the CTAs' 128, 256 and 384 threads: every sequence's tokens are
+    rotated and cached at their places, and see their own cached tokens."""
+    H, KH, D, page = 4, 2, 64, 16
+    g = _g(B)
+    new = [1] * B if form == "single" else torch.randint(0, 4, (B,), generator=g).tolist()
+    if form == "chunks":
+        new[B // 2], new[-1] = 70, 33
+    kv = [n + int(t) for n, t in zip(new, torch.randint(0, 90, (B,), generator=g))]
+    kv[3] = 1500
+    T, width = sum(new), -(-max(kv) // page)
+    need = [-(-n // page) for n in kv]
+    order = torch.randperm(sum(need), generator=g)
+    table = torch.full((B, width), -1, dtype=torch.int32)
+    keys = [torch.randn(2, KH, n, D, generator=g).to(torch.bfloat16) for n in kv]
+    k, v = (torch.full((sum(need), KH, page, D), float("nan"), dtype=torch.bfloat16) for _ in range(2))
+    at = 0
+    for b, m in enumerate(need):
+        table[b, :m] = order[at:at + m].to(torch.int32)
+        for i in range(m):
+            e = min(page, kv[b] - i * page)
+            for pool, src in ((k, keys[b][0]), (v, keys[b][1])):
+                pool[order[at + i], :, :e] = src[:, i * page:i * page + e]
+        at += m
+    start = torch.tensor([0] + new).cumsum(0)
+    batch = sp.PagedBatch(start.to(torch.int32).cuda(), _ints(kv), table.cuda(), max_q=max(new))
+    # (no rotation: what is appended is the keys themselves, which are cached already, with other values)
+    cache = sp.KVCache(k.cuda(), v.cuda())
+    qkv = torch.empty(T, H + 2 * KH, D, dtype=torch.bfloat16)
+    qkv[:, :H] = torch.randn(T, H, D, generator=g).to(torch.bfloat16)
+    for b, n in enumerate(new):
+        rows = slice(int(start[b]), int(start[b]) + n)
+        keys[b][1, :, kv[b] - n:] = torch.randn(KH, n, D, generator=g).to(torch.bfloat16)
+        qkv[rows, H:H + KH] = keys[b][0, :, kv[b] - n:].transpose(0, 1)
+        qkv[rows, H + KH:] = keys[b][1, :, kv[b] - n:].transpose(0, 1)
+    q = torch.empty(T, H, D, dtype=torch.bfloat16, device="cuda")
+    y = torch.full((T, H, D), float("nan"), dtype=torch.bfloat16, device="cuda")
+    sp.sparoa_rope_append(ctx, qkv.view(T, -1).cuda(), q, cache, batch, sp.Rope(0))
+    sp.sparoa_paged_attention(ctx, q, y, cache, batch)
+    ctx.sync()
+    assert torch.equal(q.cpu(), qkv[:, :H])
+    y = y.double().cpu()
+    for b, n in enumerate(new):
+        for h in range(H):
+            rows = slice(int(start[b]), int(start[b]) + n)
+            s = qkv[rows, h].double() @ keys[b][0, h // 2].double().t() / D ** 0.5
+            keep = torch.arange(kv[b])[None] <= torch.arange(kv[b] - n, kv[b])[:, None]
+            p = torch.softmax(s.masked_fill(~keep, float("-inf")), -1)
+            val = keys[b][1, h // 2].double()
+            tol = 2.0 ** -8 * (p @ val).abs() + (2.0 ** -8 + 2.0 ** -12) * (p @ val.abs())
+            assert ((y[rows, h] - p @ val).abs() <= tol).all(), (b, n, kv[b], h)
