@@ -98,8 +98,7 @@ class Decoder:
         self.layers = [{"qkv": weight(width, dim), "o": weight(dim, heads * head_dim), "w1": weight(hidden, dim),
                         "w2": weight(dim, hidden), "n1": sp.norm("rms", gamma(1.0)), "n2": sp.norm("rms", gamma(1.0)),
                         "g1": gamma(0.5), "g2": gamma(0.5),
-                        "cache": sp.KVCache(*(torch.zeros(pages, kv_heads, page_size, head_dim, dtype=torch.bfloat16,
-                                                          device=device) for _ in range(2)))} for _ in range(layers)]
+                        "cache": sp.KVCache.empty(pages, kv_heads, page_size, head_dim, device)} for _ in range(layers)]
         self.last = sp.norm("rms", gamma(1.0))
         self.rope = rope or sp.Rope(head_dim, device=device)
         self.pages = Pages(pages, page_size)
