@@ -307,8 +307,10 @@ __global__ void __launch_bounds__(32 * kShortWarps<RT, NCH>) short_norm_kernel(c
 // bandwidth), and its first items are on their way while the place is looked up.
 // [8191 tokens, 48 heads of 128] 34 us so, 30 the bytes.
 constexpr int kRopeItems = 4;  // of a thread at once
+static_assert(kRopeThreads > 64, "a thread without an angle");
 __global__ void __launch_bounds__(kRopeThreads) rope_append_kernel(const __grid_constant__ RopeArgs a) {
   __shared__ __align__(16) float s_cos[64], s_sin[64];
+  __shared__ int64_t s_base;
   const int64_t t = blockIdx.x;
   const int D = a.D, sl = D == 128 ? 3 : 2, items = (a.heads + 2 * a.kv_heads) << sl;
   const int s = threadIdx.x & ((1 << sl) - 1);
@@ -344,7 +346,22 @@ __global__ void __launch_bounds__(kRopeThreads) rope_append_kernel(const __grid_
     }
   }
   if (b >= a.batch || t < a.q_start[0]) return;  // a row of no sequence
-  const int64_t begin = a.q_start[b], end = a.q_start[b + 1], len = a.kv_len[b], place = len - end + t;
+  const int64_t end = a.q_start[b + 1], len = a.kv_len[b], place = len - end + t;
+  // by a thread that has no angle to do: the row of the place's first key head, -1: not cached.
+  // A sequence that its lists give rows it cannot have caches none of them: they would take the
+  // places of others.
+  if (threadIdx.x == kRopeThreads - 1) {
+    int64_t base = -1;
+    const int64_t begin = a.q_start[b];
+    if (place >= 0 && begin >= 0 && begin <= t && end > t && end <= a.T && len <= room) {
+      const int page = a.table[b * a.table_stride + (place >> a.page_log2)];
+      if (page >= 0 && page < a.pages)
+        base = (((int64_t)page * a.kv_heads) << a.page_log2) + (place & ((1 << a.page_log2) - 1));
+      else
+        atomicOr(a.err, kErrBadIndex);
+    }
+    s_base = base;
+  }
   const uint64_t pos = (uint64_t)(a.positions ? (int64_t)a.positions[t] : place);
   for (int i = threadIdx.x; i < a.rot / 2; i += kRopeThreads) {
     const int32_t turn = (int32_t)((pos * a.turns[i]) >> 32);  // signed fraction of a turn, 2^-32
@@ -353,18 +370,8 @@ __global__ void __launch_bounds__(kRopeThreads) rope_append_kernel(const __grid_
     s_cos[i] = cs * a.scale;
     s_sin[i] = sn * a.scale;
   }
-  // the page of the token's place; -1: not cached
-  int64_t base = -1;
-  // (a sequence that its lists give rows it cannot have caches none of them: they would take the
-  // places of others)
-  if (place >= 0 && begin >= 0 && begin <= t && end > t && end <= a.T && len <= room) {
-    const int page = a.table[b * a.table_stride + (place >> a.page_log2)];
-    if (page >= 0 && page < a.pages)
-      base = (((int64_t)page * a.kv_heads) << a.page_log2) + (place & ((1 << a.page_log2) - 1));
-    else if (threadIdx.x == 0)
-      atomicOr(a.err, kErrBadIndex);
-  }
   __syncthreads();
+  const int64_t base = s_base;
   float cs[8], sn[8];
   if (turns) {
 #pragma unroll
