@@ -455,7 +455,8 @@ typedef struct {
     int32_t batch;           /* 1 to 1024                                     */
     int32_t max_pages;       /* entries of a row of the table                 */
     int32_t max_q;           /* new tokens of a sequence at most: chooses the
-                                kernel; any value gives right results          */
+                                kernel, and with it how probabilities are rounded
+                                (sparoa_paged_attention); any value is right  */
     int32_t reserved;
 } sparoa_paged_batch;
 
@@ -515,21 +516,24 @@ sparoa_status sparoa_rope_append(sparoa_ctx *ctx, const void *qkv, int64_t ld_qk
  *   y = softmax(scale Q K^T) V
  * in tensor cores with fp32 scores, softmax statistics and accumulation; for the
  * P V products the probabilities are rounded to bf16, or to two bf16 parts each
- * (16 bits) for a sequence of at most 128 rows per key head (n heads / kv_heads).  The token at position p sees
- * the keys j < kv_len with j <= p (causal) and j > p - window (window > 0).  A row
- * that sees no key is zero.
+ * (16 bits) for a sequence of at most 128 rows per key head (n heads / kv_heads), and
+ * for every sequence where max_q heads / kv_heads is 16 at most.  Probabilities below
+ * 2^-126 count, to 2^-134.  The fp32 sums of exp(scale (q k - m)) |v| before their
+ * division, with an m up to 8 log 2 / scale below a row's maximum, must be finite.
+ *   The token at position p sees the keys j < kv_len with j <= p (causal) and
+ * j > p - window (window > 0).  A row that sees no key is zero.
  *   q     bf16 [T][ld_q >= heads head_dim], ld_q % 8 == 0, 16-byte aligned
  *   y     bf16 [T][heads head_dim], 16-byte aligned
  *   lse   device fp32 [T][heads] (nullable): log of the sum of exp(scale q k) over
  *         the keys that a row sees (-infinity for none)
  *   y_occ occupancy of y to write (nullable); rows of no sequence count as they are
- * Splits long sequences over the GPU; partial results live in workspaces (3 to 42 MB)
+ * Splits long sequences over the GPU; partial results live in workspaces (5 to 41 MB)
  * that the context keeps: one for each of the 16 streams that it was last used on, and
  * one for each capture and stream of it, which is the graph's own on whichever stream it
  * is replayed, until the graph and its executable forms are destroyed.  So calls on
- * several streams and replays of several graphs may overlap.  A table entry outside [0, pages), or
- * a length past the table's row, is reported as INVALID_ARG by the next call that
- * synchronises, and the affected rows hold anything.
+ * several streams and replays of several graphs may overlap.  A table entry outside
+ * [0, pages), or a length past the table's row, is reported as INVALID_ARG by the next
+ * call that synchronises, and the affected rows hold anything.
  * Errors: INVALID_ARG, UNSUPPORTED (head_dim, page_size, batch), CUDA, OOM, TIMEOUT. */
 sparoa_status sparoa_paged_attention(sparoa_ctx *ctx, const void *q, int64_t ld_q, int64_t T,
                                      int32_t heads, float scale, int32_t causal, int32_t window,

@@ -11,9 +11,11 @@ namespace {
 // ---------------------------------------------------------------------------
 // An item is 256 query rows: two tiles of 128, whose scores and sums live in tensor
 // memory side by side: S (128 x 128 fp32, later overwritten by the weights P in
-// bf16) and O (128 x D fp32) of each.  Eleven warps: two groups of four for the softmax
+// bf16) and O (128 x D fp32) of each.  Twelve warps: two groups of four for the softmax
 // of a tile (a thread per row), one that issues the MMAs, one that loads K and V by
-// TMA, page by page, into a ring, and one that walks the items and loads their Q.
+// TMA, page by page, into a ring, one that walks the items and loads their Q, and one that
+// writes down for the second kernel which item was cut at the CTA's start and, where tiles of Q
+// are no boxes, loads half of their rows.
 //
 // Bound by the tensor cores and, nearly as much, by the softmax: the 256 x 128 scores of a
 // unit are 2 x 2 x 128 x 128 x D MACs (2048 cycles at D = 128 and 4096 a cycle; Q K^T takes
@@ -25,15 +27,21 @@ namespace {
 //   O += P V      P from tensor memory, V from shared memory as it lies ([key][D], the
 //                 MN-major form of the B operand)
 // An item of one tile is bound by the bytes of K and V, so there the weights are two
-// bf16 parts (the second in the columns of S that the first leaves free).
-// MMAs of one thread run in the order of their issue, so S of the next unit may be
-// issued behind the product that still reads P from the same columns, and S complete
-// means that the O before it is.
+// bf16 parts (the second in the columns of S that the first leaves free).  With two tiles they are
+// one part, since another would be half as many MACs again: the error of a prompt's results
+// against 64 bits is 2.1e-3 of their norm so, 1.6e-3 of it the results' own rounding.
+// S of the next unit is issued behind the product that still reads P from the same columns.
+// This rests on the one tensor pipe of an SM taking the MMAs of one thread, all of them of one
+// CTA and M = 128, in the order of their issue.  What is documented is that order for MMAs of one
+// shape and accumulator; these have two accumulators and, with D = 64, two values of N.  All 512
+// columns are in use, so P has no place of its own; waiting for the product's end before S is issued
+// makes a prompt of 8191 tokens 453 us instead of 421, with the same bits.  That O stands still once the
+// S after it is complete rests on the commit alone, which covers all MMAs issued before.
 //
 // The softmax keeps a reference m of each row instead of the exact maximum: O and the
 // sum are only rescaled where the maximum has outgrown m by more than 2^8 in weight
-// (the weights, their sum and O hold that easily), which after a row's first units is
-// rare.  The end's O / sum is the same number.
+// (weights and their sum hold that easily, and O for values up to 2^119 over the number of keys
+// that weigh), which after a row's first units is rare.  The end's O / sum is the same number.
 // Weights are 2^(s sl2 - z) in one FMA, z the scaled reference as rounded to fp32 (to a
 // quarter at scores of 2^24 / 8).  So everything that brings weights of two references together
 // (rescaling, the two groups' sums, the parts of an item) goes by the same z, and the log of the
@@ -47,7 +55,8 @@ constexpr int kItems = 4;      // items that the item warp is ahead, at most
 constexpr float kSlackLog2 = 8.f;
 constexpr int kOutBytes = 32 * 64;  // 32 rows of 32 values
 
-// Steps of about 0.3 us, fitted to the CTAs' times: a unit of one tile 1.2 us, of two
+// Steps of about 0.3 us, fitted to the CTAs' times as they were before weights below the normal
+// range were kept (6 % less for two tiles): a unit of one tile 1.2 us, of two
 // tiles 1.5, an item's beginning and end 2.7 (7 and 12 steps were each slower on some of a
 // prompt, mixed chunks, drafts and windows).  A join is 4 us, but items left whole so that
 // there is none keep some CTAs twice as long: 4 x 1000 tokens, window 1024, 23 -> 37 us.

@@ -305,7 +305,7 @@ __global__ void __launch_bounds__(32 * kShortWarps<RT, NCH>) short_norm_kernel(c
 // are the same 16 of every kRopeThreads / 8th (or / 4th) head, so their cosines and sines
 // are read from shared memory once (for every item again, in pairs: 70 % of the L1's
 // bandwidth), and its first items are on their way while the place is looked up.
-// [8191 tokens, 48 heads of 128] 34 us so, 30 the bytes.
+// [8191 tokens, 48 heads of 128] 33 us so, 30 the bytes.
 constexpr int kRopeItems = 4;  // of a thread at once
 static_assert(kRopeThreads > 64, "a thread without an angle");
 __global__ void __launch_bounds__(kRopeThreads) rope_append_kernel(const __grid_constant__ RopeArgs a) {

@@ -279,10 +279,11 @@ __device__ __forceinline__ PagedShares shares_of(const PagedCursor<Cut>& c, unsi
 // (its first item's end) and one that another ends (its last item's beginning).
 __device__ __forceinline__ unsigned part_slot(unsigned c, bool begins) { return 2u * c + (begins ? 1u : 0u); }
 
-// Page of key `key` of sequence b, brought into the pool's bounds.
+// The table's entry for key `key` of sequence b, as it is (loaded ahead of its use).
 __device__ __forceinline__ int page_of(const PagedArgs& a, int b, int key) {
   return a.table[b * a.table_stride + (key >> a.page_log2)];
 }
+// The page of an entry, brought into the pool's bounds.
 __device__ __forceinline__ int page_checked(const PagedArgs& a, int page) {
   if (page >= 0 && page < a.pages) return page;
   atomicOr(a.err, kErrBadIndex);
