@@ -309,7 +309,7 @@ def _prepare_own(s, c):
         return torch.empty(*shape, dtype=dtype, device="cuda")
 
     if kind == "w4":
-        s["w"] = sp.W4(s["codes"], s["scales"], s["zeros"])
+        s["w"] = sp.W4(s["ctx"], s["codes"], s["scales"], s["zeros"])
         s["y"] = empty(c["M"], c["N"], dtype=torch.float32 if c["out"] == "f32" else torch.bfloat16)
     elif kind == "logits":
         s["rules"] = sp.LogitRules(seen_start=s["seen_start"] if c["seen"] else None, seen=s["seen"] if c["seen"] else None,
