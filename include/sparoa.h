@@ -540,6 +540,112 @@ sparoa_status sparoa_paged_attention(sparoa_ctx *ctx, const void *q, int64_t ld_
                                      const sparoa_kv_cache *cache, const sparoa_paged_batch *batch,
                                      void *y, float *lse, const sparoa_occupancy *y_occ);
 
+/* ------------------------------------------------------------------------ */
+/* Operators of a decoder step that checks drafted tokens                     */
+/*                                                                            */
+/* A drafter proposes a tree of next tokens for each sequence; one step of the */
+/* decoder judges all of them.  Such a step has few rows: its products are     */
+/* bound by the weights' bytes (4 bits here), its attention by the cache's.     */
+/* ------------------------------------------------------------------------ */
+
+/* Weights of 4 bits, laid out once by sparoa_w4_pack:
+ *   W[n][k] = scale[n][k / group] * (code[n][k] - zero[n][k / group]). */
+typedef struct {
+    const void *packed;      /* device, sparoa_w4_bytes bytes, 16-byte aligned */
+    int64_t N, K;
+    int32_t group;           /* columns of a scale: 32, 64 or 128             */
+    int32_t zeros;           /* 1: packed with zero points; 0: all are 8      */
+} sparoa_w4;
+
+/* Bytes of packed weights [N, K]; 0 for sizes that sparoa_w4_pack refuses. */
+uint64_t sparoa_w4_bytes(int64_t N, int64_t K, int32_t group, int32_t zeros);
+
+/*
+ * Lay out 4-bit weights for sparoa_gemm_w4.
+ *   codes   device uint8 [N][K / 2]: column 2 i in the low half of byte i
+ *   scales  device bf16 [N][K / group]
+ *   zeros   device uint8 [N][K / group], 0 to 15 (the low four bits count), or NULL
+ *   packed  device, sparoa_w4_bytes(N, K, group, zeros != NULL) bytes
+ * N % 8 == 0, K % group == 0, group 32, 64 or 128, N and K <= 2^20; codes and packed 16-byte
+ * aligned.  Errors: INVALID_ARG, UNSUPPORTED (sizes), CUDA. */
+sparoa_status sparoa_w4_pack(sparoa_ctx *ctx, const void *codes, const void *scales,
+                             const void *zeros, int64_t N, int64_t K, int32_t group, void *packed);
+
+/*
+ * y[M, N] = epilogue( x[M, K] * W^T ) with 4-bit weights, for few rows: made for M up to 64
+ * (the weights are read once for every 64 rows).  Codes less their zeros are whole
+ * numbers, their products with x are summed in fp32 over a group, and the sum is
+ * multiplied by the scale: no weight is rounded.
+ *   x     bf16 [M][K], contiguous, 16-byte aligned; M <= 2^20
+ *   y     [M][N] SPAROA_BF16 or SPAROA_F32, 16-byte aligned; overlaps nothing but the
+ *         residual, which it may be
+ *   y_occ occupancy of y to write (nullable; bf16 y only)
+ * Errors: INVALID_ARG, UNSUPPORTED (sizes; y_occ with F32 output), CUDA, OOM, TIMEOUT. */
+sparoa_status sparoa_gemm_w4(sparoa_ctx *ctx, const void *x, int64_t M, const sparoa_w4 *w,
+                             const sparoa_epilogue *ep, void *y, int32_t y_dtype,
+                             const sparoa_occupancy *y_occ);
+
+/* Changes to the logits of a row r, in this order; what is NULL is left out.
+ * A token that is c > 0 times in the row's list seen[seen_start[r] .. seen_start[r + 1]):
+ *   z = (z > 0 ? z / repetition : z * repetition) - presence - frequency * c
+ * then every token: z = (z + bias) * (1 / temperature), and -infinity where the row's bit
+ * in `allowed` is 0.  Each operation is rounded to fp32. */
+typedef struct {
+    const int32_t *seen_start; /* device [R + 1], not decreasing, within [0, n_seen] */
+    const int32_t *seen;     /* device [n_seen] tokens; outside [0, V): no token */
+    int64_t n_seen;
+    const float *penalties;  /* device [R][4]: repetition, presence, frequency, temperature
+                                (repetition and temperature above 0)            */
+    const float *bias;       /* device [R][ld_bias], or one row with ld_bias 0  */
+    int64_t ld_bias;
+    const uint32_t *allowed; /* device [R][ld_allowed]: bit v % 32 of word v / 32 */
+    int64_t ld_allowed;
+} sparoa_logit_rules;
+
+/*
+ * Logits to tokens: the rules above over logits [R, V], in one pass.
+ *   logits  `dtype` (SPAROA_BF16 or SPAROA_F32) [R][ld >= V]
+ *   rules   NULL: none
+ *   y       device fp32 [R][ld_y >= V] (nullable): the changed logits; may be the
+ *           logits themselves (fp32, ld_y = ld), else overlaps no input
+ *   best    device int32 [R] (nullable): the lowest token whose z is largest; -1 where
+ *           none is above -infinity.  A z that is not a number is never the best
+ *   lse     device fp32 [R] (nullable): log of the sum of exp(z); -infinity where all
+ *           are, not a number where a z is not
+ * R < 2^27, V < 2^30.  A row whose list is not within [0, n_seen] counts as having none, and
+ * is reported as INVALID_ARG by the next call that synchronises.
+ * Errors: INVALID_ARG, UNSUPPORTED (R, V), CUDA. */
+sparoa_status sparoa_shape_logits(sparoa_ctx *ctx, const void *logits, int64_t ld, int64_t R,
+                                  int64_t V, int32_t dtype, const sparoa_logit_rules *rules,
+                                  float *y, int64_t ld_y, int32_t *best, float *lse);
+
+/*
+ * After a step over trees of drafted tokens: the path through each tree that the model's
+ * own choices confirm, and its keys and values in the places that follow one another.
+ * A sequence's new tokens (at most 64) are its tree: bit j of tree[row] says that new
+ * token j is an ancestor (bits at and above the token's own are ignored).  The path
+ * begins with token 0; after token i comes the lowest new token whose ancestors are
+ * those of i and i itself, and whose number is best[i] (a best below 0: none).
+ *   tokens  device int32 [T]: the new tokens' numbers
+ *   best    device int32 [T]: the model's choice after each (sparoa_shape_logits)
+ *   tree    device uint64 [T]
+ *   caches  host array of n_caches (at most 128) caches of one shape, a layer each, with
+ *           disjoint pools
+ *   path    device int32 [T]: a sequence's first rows hold its path's new tokens in
+ *           order, the others -1
+ *   count   device int32 [batch]: tokens of the path (0: no new tokens)
+ *   following  device int32 [batch]: the choice after the path's last token (-1: none)
+ *   new_len device int32 [batch]: tokens in the cache that stay; not kv_len itself
+ * The k-th token of the path moves to place kv_len - n + k; places at and after new_len
+ * hold anything afterwards.  Lists out of bounds, trees of more than 64 tokens and bad pages are
+ * reported as INVALID_ARG by the next call that synchronises; such a sequence (such a
+ * token) is left as it is.
+ * Errors: INVALID_ARG, UNSUPPORTED (head_dim, page_size, batch, n_caches), CUDA. */
+sparoa_status sparoa_tree_accept(sparoa_ctx *ctx, const int32_t *tokens, const int32_t *best,
+                                 const uint64_t *tree, int64_t T, const sparoa_kv_cache *caches,
+                                 int32_t n_caches, const sparoa_paged_batch *batch, int32_t *path,
+                                 int32_t *count, int32_t *following, int32_t *new_len);
+
 /*
  * Run a topologically ordered operator list (Sec. 4.1 layer execution order;
  * Sec. 5.1 operator-by-operator execution) on one GPU.  The input x is bf16

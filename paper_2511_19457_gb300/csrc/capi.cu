@@ -1600,6 +1600,170 @@ sparoa_status sparoa_paged_attention(sparoa_ctx* ctx, const void* q, int64_t ld_
 }
 
 // ---------------------------------------------------------------------------
+// operators of a step that checks drafted tokens
+// ---------------------------------------------------------------------------
+namespace {
+
+// nullptr, or what is wrong with the sizes of 4-bit weights
+const char* w4_sizes(int64_t N, int64_t K, int32_t group) {
+  if (group != 32 && group != 64 && group != 128) return "groups of 32, 64 or 128 columns only";
+  if (N <= 0 || K <= 0 || N % 8 || K % group) return "N must be a multiple of 8, K of the group";
+  if (N > (1 << 20) || K > (1 << 20)) return "N and K up to 2^20 only";
+  return nullptr;
+}
+
+}  // namespace
+
+uint64_t sparoa_w4_bytes(int64_t N, int64_t K, int32_t group, int32_t zeros) {
+  return w4_sizes(N, K, group) ? 0 : w4_packed_bytes(N, K, group, zeros != 0);
+}
+
+sparoa_status sparoa_w4_pack(sparoa_ctx* ctx, const void* codes, const void* scales, const void* zeros, int64_t N, int64_t K,
+                             int32_t group, void* packed) {
+  if (!ctx) return SPAROA_ERR_INVALID_ARG;
+  if (const char* what = w4_sizes(N, K, group))
+    return fail(ctx, N > 0 && K > 0 ? SPAROA_ERR_UNSUPPORTED : SPAROA_ERR_INVALID_ARG, "w4_pack: %s", what);
+  if (!codes || !scales || !packed || !aligned16(codes) || !aligned16(packed) || (reinterpret_cast<uintptr_t>(scales) & 1u))
+    return fail(ctx, SPAROA_ERR_INVALID_ARG, "w4_pack: NULL or misaligned tensor");
+  DeviceGuard g(ctx->device, ctx->overlap);
+  W4PackArgs a;
+  a.codes = static_cast<const uint8_t*>(codes);
+  a.scales = static_cast<const uint16_t*>(scales);
+  a.zeros = static_cast<const uint8_t*>(zeros);
+  a.N = (int)N;
+  a.K = (int)K;
+  a.group = group;
+  a.out = static_cast<uint8_t*>(packed);
+  SP_CUDA(launch_w4_pack(a, ctx->stream));
+  return SPAROA_OK;
+}
+
+sparoa_status sparoa_gemm_w4(sparoa_ctx* ctx, const void* x, int64_t M, const sparoa_w4* w, const sparoa_epilogue* ep, void* y,
+                             int32_t y_dtype, const sparoa_occupancy* y_occ) {
+  if (!ctx) return SPAROA_ERR_INVALID_ARG;
+  if (!w || M < 0) return fail(ctx, SPAROA_ERR_INVALID_ARG, "gemm_w4: no weights, or bad M");
+  if (const char* what = w4_sizes(w->N, w->K, w->group)) return fail(ctx, SPAROA_ERR_INVALID_ARG, "gemm_w4: %s", what);
+  if (M > (1 << 20)) return fail(ctx, SPAROA_ERR_UNSUPPORTED, "gemm_w4: M up to 2^20 only");
+  if (M > 0 && (!x || !w->packed || !y)) return fail(ctx, SPAROA_ERR_INVALID_ARG, "gemm_w4: NULL tensor");
+  if (!aligned16(x) || !aligned16(w->packed) || !aligned16(y))
+    return fail(ctx, SPAROA_ERR_INVALID_ARG, "gemm_w4: tensors must be 16-byte aligned");
+  if (y_dtype != SPAROA_BF16 && y_dtype != SPAROA_F32) return fail(ctx, SPAROA_ERR_INVALID_ARG, "gemm_w4: bad y_dtype");
+  if (y_occ && y_dtype != SPAROA_BF16) return fail(ctx, SPAROA_ERR_UNSUPPORTED, "gemm_w4: occupancy of an fp32 output");
+  SP_TRY(check_ep(ctx, ep));
+  SP_TRY(check_occ(ctx, y_occ, M, w->N, "gemm_w4 y_occ"));
+  DeviceGuard g(ctx->device, ctx->overlap);
+  if (M > 0) {
+    W4Args a;
+    a.x = static_cast<const __nv_bfloat16*>(x);
+    a.w = static_cast<const uint8_t*>(w->packed);
+    a.M = (int)M;
+    a.N = (int)w->N;
+    a.K = (int)w->K;
+    a.group = w->group;
+    a.zeros = w->zeros != 0;
+    a.ep = to_dev(ep);
+    a.y = y;
+    a.y_f32 = y_dtype == SPAROA_F32;
+    a.err = ctx->d_err();
+    a.wait_limit = ctx->wait_limit;
+    SP_CUDA(launch_w4(a, ctx->stream));
+  }
+  if (y_occ) SP_TRY(run_stats(ctx, y, M, w->N, *y_occ));
+  return SPAROA_OK;
+}
+
+sparoa_status sparoa_shape_logits(sparoa_ctx* ctx, const void* logits, int64_t ld, int64_t R, int64_t V, int32_t dtype,
+                                  const sparoa_logit_rules* rules, float* y, int64_t ld_y, int32_t* best, float* lse) {
+  if (!ctx) return SPAROA_ERR_INVALID_ARG;
+  if (R < 0 || V <= 0 || ld < V || (y && ld_y < V)) return fail(ctx, SPAROA_ERR_INVALID_ARG, "shape_logits: bad shape");
+  if (R >= (1 << 27) || V >= (1 << 30)) return fail(ctx, SPAROA_ERR_UNSUPPORTED, "shape_logits: too many rows or tokens");
+  if (dtype != SPAROA_BF16 && dtype != SPAROA_F32) return fail(ctx, SPAROA_ERR_INVALID_ARG, "shape_logits: bad dtype");
+  if (R > 0 && (!logits || (!y && !best && !lse))) return fail(ctx, SPAROA_ERR_INVALID_ARG, "shape_logits: no input or no output");
+  if (y && y == logits && (dtype != SPAROA_F32 || ld_y != ld))
+    return fail(ctx, SPAROA_ERR_INVALID_ARG, "shape_logits: in place, logits are fp32 with rows of one length");
+  const sparoa_logit_rules none = {};
+  const sparoa_logit_rules& u = rules ? *rules : none;
+  if (u.n_seen < 0 || u.n_seen > 0x7FFFFFFF || (u.seen_start && u.n_seen > 0 && !u.seen) || (!u.seen_start && u.n_seen > 0))
+    return fail(ctx, SPAROA_ERR_INVALID_ARG, "shape_logits: bad list of seen tokens");
+  if (u.bias && u.ld_bias != 0 && u.ld_bias < V) return fail(ctx, SPAROA_ERR_INVALID_ARG, "shape_logits: bias rows are short");
+  if (u.allowed && u.ld_allowed < (V + 31) / 32) return fail(ctx, SPAROA_ERR_INVALID_ARG, "shape_logits: mask rows are short");
+  const uintptr_t four = reinterpret_cast<uintptr_t>(u.seen_start) | reinterpret_cast<uintptr_t>(u.seen) |
+                         reinterpret_cast<uintptr_t>(u.penalties) | reinterpret_cast<uintptr_t>(u.bias) |
+                         reinterpret_cast<uintptr_t>(u.allowed) | reinterpret_cast<uintptr_t>(y) | reinterpret_cast<uintptr_t>(best) |
+                         reinterpret_cast<uintptr_t>(lse);
+  if ((four & 3u) || (reinterpret_cast<uintptr_t>(logits) & (dtype == SPAROA_F32 ? 3u : 1u)))
+    return fail(ctx, SPAROA_ERR_INVALID_ARG, "shape_logits: misaligned");
+  DeviceGuard g(ctx->device, ctx->overlap);
+  LogitArgs a;
+  a.x = logits;
+  a.ld_x = ld;
+  a.R = R;
+  a.x_bf16 = dtype == SPAROA_BF16;
+  a.V = (int)V;
+  a.seen_start = u.penalties ? u.seen_start : nullptr;  // (without penalties the lists change nothing)
+  a.seen = u.seen;
+  a.n_seen = u.n_seen;
+  a.penalties = u.penalties;
+  a.bias = u.bias;
+  a.ld_bias = u.ld_bias;
+  a.allowed = u.allowed;
+  a.ld_allowed = u.ld_allowed;
+  a.y = y;
+  a.ld_y = ld_y;
+  a.best = best;
+  a.lse = lse;
+  a.err = ctx->d_err();
+  SP_CUDA(launch_logits(a, ctx->stream));
+  return SPAROA_OK;
+}
+
+sparoa_status sparoa_tree_accept(sparoa_ctx* ctx, const int32_t* tokens, const int32_t* best, const uint64_t* tree, int64_t T,
+                                 const sparoa_kv_cache* caches, int32_t n_caches, const sparoa_paged_batch* batch,
+                                 int32_t* path, int32_t* count, int32_t* following, int32_t* new_len) {
+  if (!ctx) return SPAROA_ERR_INVALID_ARG;
+  if (n_caches <= 0 || !caches) return fail(ctx, SPAROA_ERR_INVALID_ARG, "tree_accept: no cache");
+  if (n_caches > kTreeCaches) return fail(ctx, SPAROA_ERR_UNSUPPORTED, "tree_accept: at most %d caches", kTreeCaches);
+  for (int i = 0; i < n_caches; ++i) {
+    SP_TRY(check_paged(ctx, caches + i, batch, T, caches[i].kv_heads, "tree_accept"));
+    if (caches[i].pages != caches->pages || caches[i].page_size != caches->page_size || caches[i].kv_heads != caches->kv_heads ||
+        caches[i].head_dim != caches->head_dim)
+      return fail(ctx, SPAROA_ERR_INVALID_ARG, "tree_accept: caches of different shapes");
+  }
+  if (batch->max_q > kTreeTokens) return fail(ctx, SPAROA_ERR_UNSUPPORTED, "tree_accept: trees of at most %d tokens", kTreeTokens);
+  if ((T > 0 && (!tokens || !best || !tree || !path)) || !count || !following || !new_len || new_len == batch->kv_len)
+    return fail(ctx, SPAROA_ERR_INVALID_ARG, "tree_accept: NULL list, or new_len is kv_len");
+  if (reinterpret_cast<uintptr_t>(tree) & 7u) return fail(ctx, SPAROA_ERR_INVALID_ARG, "tree_accept: misaligned");
+  DeviceGuard g(ctx->device, ctx->overlap);
+  TreeArgs a;
+  a.tokens = tokens;
+  a.best = best;
+  a.tree = tree;
+  a.T = T;
+  a.q_start = batch->q_start;
+  a.kv_len = batch->kv_len;
+  a.table = batch->table;
+  a.table_stride = batch->table_stride;
+  a.batch = batch->batch;
+  a.max_pages = batch->max_pages;
+  a.page_log2 = log2_of(caches->page_size);
+  a.kv_heads = caches->kv_heads;
+  a.D = caches->head_dim;
+  a.pages = caches->pages;
+  a.caches = n_caches;
+  for (int i = 0; i < n_caches; ++i) {
+    a.k[i] = caches[i].k;
+    a.v[i] = caches[i].v;
+  }
+  a.path = path;
+  a.count = count;
+  a.following = following;
+  a.new_len = new_len;
+  a.err = ctx->d_err();
+  SP_CUDA(launch_tree_accept(a, ctx->stream));
+  return SPAROA_OK;
+}
+
+// ---------------------------------------------------------------------------
 // graph walk
 // ---------------------------------------------------------------------------
 namespace {

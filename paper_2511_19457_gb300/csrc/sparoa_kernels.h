@@ -299,6 +299,72 @@ cudaError_t launch_paged_attention(const PagedArgs& a, cudaStream_t s);
 size_t paged_chunk_ws_bytes();
 cudaError_t launch_paged_chunk(const PagedArgs& a, cudaStream_t s);
 
+// Trees of drafted tokens, checked (k_tree.cu)
+constexpr int kTreeTokens = 64;     // new tokens of a sequence's tree at most
+constexpr int kTreeCaches = 128;    // layers at most
+struct TreeArgs {
+  const int32_t* tokens = nullptr;  // [T]
+  const int32_t* best = nullptr;    // [T]
+  const uint64_t* tree = nullptr;   // [T]
+  int64_t T = 0;
+  const int32_t* q_start = nullptr;
+  const int32_t* kv_len = nullptr;
+  const int32_t* table = nullptr;
+  int64_t table_stride = 0;
+  int batch = 0, max_pages = 0, page_log2 = 0, kv_heads = 0, D = 0, caches = 0;
+  int64_t pages = 0;
+  void* k[kTreeCaches];
+  void* v[kTreeCaches];
+  int32_t *path = nullptr, *count = nullptr, *following = nullptr, *new_len = nullptr;
+  uint32_t* err = nullptr;
+};
+cudaError_t launch_tree_accept(const TreeArgs& a, cudaStream_t s);
+
+// Logits to tokens (k_logits.cu)
+struct LogitArgs {
+  const void* x = nullptr;  // [R][ld_x]
+  int64_t ld_x = 0, R = 0;
+  int x_bf16 = 0, V = 0;
+  const int32_t* seen_start = nullptr;  // [R + 1] or null
+  const int32_t* seen = nullptr;
+  int64_t n_seen = 0;
+  const float* penalties = nullptr;  // [R][4] or null
+  const float* bias = nullptr;       // [..][ld_bias] or null; ld_bias 0: one row
+  int64_t ld_bias = 0;
+  const uint32_t* allowed = nullptr;  // [R][ld_allowed] or null
+  int64_t ld_allowed = 0;
+  float* y = nullptr;  // nullable
+  int64_t ld_y = 0;
+  int32_t* best = nullptr;
+  float* lse = nullptr;
+  uint32_t* err = nullptr;
+  int split = 1, chunk = 0;  // CTAs of a row, tokens of each at once (set by launch_logits)
+};
+cudaError_t launch_logits(const LogitArgs& a, cudaStream_t s);
+
+// Products with 4-bit weights (k_w4.cu)
+struct W4PackArgs {
+  const uint8_t* codes = nullptr;    // [N][K / 2]
+  const uint16_t* scales = nullptr;  // [N][K / group] bf16
+  const uint8_t* zeros = nullptr;    // [N][K / group] or null
+  int N = 0, K = 0, group = 0;
+  uint8_t* out = nullptr;
+};
+uint64_t w4_packed_bytes(int64_t N, int64_t K, int group, bool zeros);
+cudaError_t launch_w4_pack(const W4PackArgs& a, cudaStream_t s);
+struct W4Args {
+  const __nv_bfloat16* x = nullptr;  // [M][K]
+  const uint8_t* w = nullptr;        // packed
+  int M = 0, N = 0, K = 0, group = 0, zeros = 0;
+  EpiDev ep{};
+  void* y = nullptr;  // [M][N]
+  int y_f32 = 0;
+  uint32_t* err = nullptr;
+  long long wait_limit = 0;
+  int row_tiles = 0, tiles = 0, split = 1;  // tiles of rows and of columns, CTAs of a block's columns (set by launch_w4)
+};
+cudaError_t launch_w4(W4Args a, cudaStream_t s);
+
 // ----------------------------------------------------------------------------
 // Memory-bound kernels (128-row x 64-channel tiles, occupancy fused)
 // ----------------------------------------------------------------------------

@@ -87,6 +87,15 @@ class RopeDesc(ctypes.Structure):
     _fields_ = [("rot", _I32), ("layout", _I32), ("turns", _P), ("scale", ctypes.c_float), ("reserved", _I32)]
 
 
+class W4Desc(ctypes.Structure):
+    _fields_ = [("packed", _P), ("N", _I64), ("K", _I64), ("group", _I32), ("zeros", _I32)]
+
+
+class LogitRulesDesc(ctypes.Structure):
+    _fields_ = [("seen_start", _P), ("seen", _P), ("n_seen", _I64), ("penalties", _P), ("bias", _P), ("ld_bias", _I64),
+                ("allowed", _P), ("ld_allowed", _I64)]
+
+
 class Record(ctypes.Structure):
     _fields_ = [("stats", Stats), ("output", _P), ("out_shape", _I64 * 4),
                 ("out_occ", ctypes.POINTER(Occupancy))]
@@ -138,6 +147,13 @@ _sig("sparoa_rope_append", [_P, _P, _I64, _I64, _I32, ctypes.POINTER(RopeDesc), 
                             ctypes.POINTER(PagedBatchDesc), _P, _I64])
 _sig("sparoa_paged_attention", [_P, _P, _I64, _I64, _I32, ctypes.c_float, _I32, _I32, ctypes.POINTER(KvCacheDesc),
                                 ctypes.POINTER(PagedBatchDesc), _P, _P, ctypes.POINTER(Occupancy)])
+_lib.sparoa_w4_bytes.restype = ctypes.c_uint64
+_lib.sparoa_w4_bytes.argtypes = [_I64, _I64, _I32, _I32]
+_sig("sparoa_w4_pack", [_P, _P, _P, _P, _I64, _I64, _I32, _P])
+_sig("sparoa_gemm_w4", [_P, _P, _I64, ctypes.POINTER(W4Desc), ctypes.POINTER(Epilogue), _P, _I32, ctypes.POINTER(Occupancy)])
+_sig("sparoa_shape_logits", [_P, _P, _I64, _I64, _I64, _I32, ctypes.POINTER(LogitRulesDesc), _P, _I64, _P, _P])
+_sig("sparoa_tree_accept", [_P, _P, _P, _P, _I64, ctypes.POINTER(KvCacheDesc), _I32, ctypes.POINTER(PagedBatchDesc), _P, _P,
+                            _P, _P])
 _sig("sparoa_run_graph", [_P, ctypes.POINTER(Op), _I32, _P, _I64, _I64, _I64, _I64, _P,
                           ctypes.c_uint64, ctypes.POINTER(Record)])
 _sig("sparoa_gemm_noalloc", [_P, _P, _I64, _I64, _P, _P, _I64, ctypes.POINTER(Epilogue),
@@ -151,6 +167,7 @@ EXPORTED = ["sparoa_create", "sparoa_destroy", "sparoa_set_stream", "sparoa_set_
             "sparoa_maxpool2d", "sparoa_avgpool_global", "sparoa_bn_act", "sparoa_run_graph",
             "sparoa_graph_workspace", "sparoa_gemm_split", "sparoa_layernorm", "sparoa_attention",
             "sparoa_add_norm", "sparoa_rope_turns", "sparoa_rope_append", "sparoa_paged_attention",
+            "sparoa_w4_bytes", "sparoa_w4_pack", "sparoa_gemm_w4", "sparoa_shape_logits", "sparoa_tree_accept",
             "sparoa_gemm_noalloc"]
 
 
@@ -577,6 +594,170 @@ def sparoa_paged_attention(ctx: Context, q, y, cache: KVCache, batch: PagedBatch
 
 _add_norm, _rope_append = _lib.sparoa_add_norm, _lib.sparoa_rope_append
 _paged_attention = _lib.sparoa_paged_attention
+
+
+# ---------------------------------------------------------------------------
+# a step that checks drafted tokens: 4-bit products, logits to tokens, trees accepted
+# ---------------------------------------------------------------------------
+_U8S = (torch.uint8,)
+
+
+class W4:
+    """Weights [N, K] of 4 bits: codes uint8 [N, K / 2] (column 2 i in the low half of byte i), scales bf16
+    [N, K / group], zeros uint8 [N, K / group] or None (8).  Laid out for sparoa_gemm_w4 when it is made, on
+    the current torch stream; holds a copy of its own."""
+
+    def __init__(self, ctx: Context, codes, scales, zeros=None):
+        _want_rows(codes, _U8S, "W4 codes")
+        _want_rows(scales, _BF16S, "W4 scales")
+        _want(codes.dim() == 2 and scales.dim() == 2 and codes.shape[0] == scales.shape[0], "W4: codes and scales of N rows")
+        self.N, self.K = codes.shape[0], 2 * codes.shape[1]
+        groups = scales.shape[1]
+        _want(groups > 0 and self.K % groups == 0, "W4: a scale for every group of columns")
+        self.group = self.K // groups
+        if zeros is not None:
+            _want_rows(zeros, _U8S, "W4 zeros")
+            _want(zeros.shape == scales.shape, "W4: a zero for every scale")
+        for t in (scales, zeros):
+            _want(t is None or t.device == codes.device, "W4: tensors on one device")
+        nbytes = int(_lib.sparoa_w4_bytes(self.N, self.K, self.group, 0 if zeros is None else 1))
+        _want(nbytes > 0, f"W4: [{self.N}, {self.K}] in groups of {self.group}: N a multiple of 8, groups of 32, 64 or 128")
+        self.packed = torch.empty(nbytes, dtype=torch.uint8, device=codes.device)
+        sparoa_w4_pack(ctx, codes, scales, zeros, self.packed)
+        self.desc = W4Desc(_ptr(self.packed), self.N, self.K, self.group, 0 if zeros is None else 1)
+        self.ref = _byref(self.desc)
+
+    @staticmethod
+    def quantise(ctx: Context, weight, group=128, zeros=False) -> "W4":
+        """4-bit weights nearest to weight [N, K], by the range of each group (w4_quantise)."""
+        return W4(ctx, *w4_quantise(weight, group, zeros))
+
+
+def w4_quantise(weight, group=128, zeros=False):
+    """(codes, scales, zeros or None) of weight [N, K], as W4 takes them."""
+    N, K = weight.shape
+    w = weight.float().view(N, K // group, group)
+    lo, hi = w.amin(-1), w.amax(-1)
+    if zeros:
+        lo, hi = lo.clamp_max(0.0), hi.clamp_min(0.0)
+        scales = ((hi - lo) / 15.0).to(torch.bfloat16)
+    else:
+        scales = torch.maximum(lo / -8.0, hi / 7.0).to(torch.bfloat16)
+    step = scales.float()
+    step = torch.where(step > 0, step, 1.0)
+    zero = (-lo / step).round().clamp(0, 15) if zeros else torch.full_like(step, 8.0)
+    c = ((w / step[..., None]).round() + zero[..., None]).clamp(0, 15).to(torch.uint8).view(N, K)
+    return (c[:, 0::2] | c[:, 1::2] << 4).contiguous(), scales.contiguous(), zero.to(torch.uint8).contiguous() if zeros else None
+
+
+def sparoa_w4_pack(ctx: Context, codes, scales, zeros, packed):
+    """Lay out 4-bit weights (see W4) into packed, a uint8 tensor of sparoa_w4_bytes."""
+    N, K = codes.shape[0], 2 * codes.shape[1]
+    ctx._bind()
+    ctx._check(_lib.sparoa_w4_pack(ctx.h, _ptr(codes), _ptr(scales), _ptr(zeros), N, K, K // scales.shape[1], _ptr(packed)))
+
+
+def sparoa_gemm_w4(ctx: Context, x, w: W4, y, bias=None, bn=None, eps=1e-5, act=ACT_NONE, residual=None, y_occ=None):
+    """y[M, N] = epilogue(x[M, K] W^T) with 4-bit weights; x bf16, y bf16 or fp32."""
+    M = x.numel() // w.K
+    if not (x.is_cuda and x.dtype is _bf16 and x.is_contiguous() and x.shape[-1] == w.K):
+        _refuse(f"gemm_w4: contiguous bf16 rows of {w.K} wanted")
+    if not (y.is_cuda and y.dtype in (_bf16, _f32) and y.is_contiguous() and y.numel() == M * w.N):
+        _refuse(f"gemm_w4: contiguous bf16 or fp32 y of [{M}, {w.N}] wanted")
+    if bias is not None and not (bias.is_cuda and bias.dtype is _f32 and bias.is_contiguous() and bias.numel() == w.N):
+        _refuse("gemm_w4: bias fp32 [N]")
+    if bn is not None and not (bn.is_cuda and bn.dtype is _f32 and bn.is_contiguous() and bn.numel() == 4 * w.N):
+        _refuse("gemm_w4: bn fp32 [4, N]")
+    if residual is not None and not (residual.is_cuda and residual.dtype is _bf16 and residual.is_contiguous() and
+                                     residual.numel() == M * w.N):
+        _refuse("gemm_w4: residual bf16 of y's size")
+    ctx._bind()
+    st = _gemm_w4(ctx.h, x.data_ptr(), M, w.ref, _byref(_epi(bias, bn, eps, act, residual)), y.data_ptr(),
+                  F32 if y.dtype is _f32 else BF16, _occ(y_occ))
+    if st:
+        ctx._check(st)
+
+
+class LogitRules:
+    """Changes of sparoa_shape_logits to logits [R, V]; keeps its tensors alive.  seen_start int32 [R + 1] and
+    seen int32: the tokens that a row has seen; penalties fp32 [R, 4] (repetition, presence, frequency,
+    temperature); bias fp32 [V], [1, V] or [R, V]; allowed int32 [R, words >= V / 32], bit v % 32 of word v / 32."""
+
+    def __init__(self, seen_start=None, seen=None, penalties=None, bias=None, allowed=None):
+        _want((seen_start is None) == (seen is None), "LogitRules: seen_start and seen go together")
+        for t, types in ((seen_start, _I32S), (seen, _I32S), (penalties, _FP32S), (bias, _FP32S), (allowed, _I32S)):
+            if t is not None:
+                _want_rows(t, types, "LogitRules")
+        _want(penalties is None or (penalties.dim() == 2 and penalties.shape[1] == 4), "LogitRules: penalties [R, 4]")
+        _want(allowed is None or allowed.dim() == 2, "LogitRules: allowed [R, words]")
+        _want(bias is None or bias.dim() in (1, 2), "LogitRules: bias [V] or [R, V]")
+        self.keep = (seen_start, seen, penalties, bias, allowed)
+        self.bias_rows = 1 if bias is None or bias.dim() == 1 else bias.shape[0]
+        self.V = None if bias is None else bias.shape[-1]
+        # rows that the rules are for, where they say
+        self.R = {n for n in (None if seen_start is None else seen_start.numel() - 1, None if penalties is None else penalties.shape[0],
+                              None if allowed is None else allowed.shape[0], self.bias_rows if self.bias_rows != 1 else None)
+                  if n is not None}
+        self.words = None if allowed is None else allowed.shape[1]
+        self.desc = LogitRulesDesc(_ptr(seen_start), _ptr(seen), 0 if seen is None else seen.numel(), _ptr(penalties), _ptr(bias),
+                                   self.V if self.bias_rows != 1 else 0, _ptr(allowed), self.words or 0)
+        self.ref = _byref(self.desc)
+
+
+def _logit_rows(t, R, V, what):
+    """Row length of t [R, V], whose rows may be strided."""
+    if t.dim() != 2 or t.shape[0] != R or t.shape[1] != V or not t.is_cuda or (V > 1 and t.stride(1) != 1):
+        _refuse(f"{what}: CUDA rows of {V} adjacent values wanted")
+    return t.stride(0) if R > 1 else max(t.stride(0), V)
+
+
+def sparoa_shape_logits(ctx: Context, logits, rules: LogitRules | None = None, y=None, best=None, lse=None):
+    """The rules over logits [R, V] (bf16 or fp32): y fp32 [R, V] (may be the logits), best int32 [R], lse fp32
+    [R], each of them or None."""
+    R, V = logits.shape
+    ld = _logit_rows(logits, R, V, "shape_logits logits")
+    _want(logits.dtype in (_bf16, _f32), "shape_logits: bf16 or fp32 logits")
+    if y is not None:
+        _want(y.dtype is _f32, "shape_logits: y fp32")
+    ld_y = 0 if y is None else _logit_rows(y, R, V, "shape_logits y")
+    for t, types, what in ((best, _I32S, "shape_logits best"), (lse, _FP32S, "shape_logits lse")):
+        if t is not None:
+            _want_rows(t, types, what)
+            _want(t.numel() == R, f"{what}: a value per row")
+    if rules is not None:
+        # (one row of bias is for all)
+        if any(n != R for n in rules.R) or rules.V not in (None, V) or (rules.words is not None and rules.words * 32 < V):
+            _refuse("shape_logits: rules of other rows or tokens")
+    ctx._bind()
+    st = _shape_logits(ctx.h, logits.data_ptr(), ld, R, V, F32 if logits.dtype is _f32 else BF16, None if rules is None else rules.ref,
+                       _ptr(y), ld_y, _ptr(best), _ptr(lse))
+    if st:
+        ctx._check(st)
+
+
+def _tree_bits(tree, T, what):
+    if not (tree.is_cuda and tree.dtype is torch.int64 and tree.is_contiguous() and tree.numel() == T):
+        _refuse(f"{what}: ancestors int64 [{T}] wanted")
+
+
+def sparoa_tree_accept(ctx: Context, tokens, best, tree, caches, batch: PagedBatch, path, count, following, new_len):
+    """The path through each sequence's tree that the model's choices confirm; its keys and values move to the
+    places that follow one another in all caches.  tokens, best, path int32 [T], tree int64 [T] (ancestor
+    bits), count, following and new_len int32 [batch]."""
+    T, B = tokens.numel(), batch.kv_len.numel()
+    for t, n in ((tokens, T), (best, T), (path, T), (count, B), (following, B), (new_len, B)):
+        if not (t.is_cuda and t.dtype is torch.int32 and t.is_contiguous() and t.numel() == n):
+            _refuse("tree_accept: contiguous CUDA int32 lists of T or batch entries wanted")
+    _tree_bits(tree, T, "tree_accept")
+    descs = (KvCacheDesc * len(caches))(*[c.desc for c in caches])
+    ctx._bind()
+    st = _tree_accept(ctx.h, tokens.data_ptr(), best.data_ptr(), tree.data_ptr(), T, descs, len(caches), batch.ref,
+                      path.data_ptr(), count.data_ptr(), following.data_ptr(), new_len.data_ptr())
+    if st:
+        ctx._check(st)
+
+
+_gemm_w4, _shape_logits, _tree_accept = _lib.sparoa_gemm_w4, _lib.sparoa_shape_logits, _lib.sparoa_tree_accept
 
 
 def sparoa_gemm_noalloc(x, W, y, W_kn=None, bias=None, bn=None, eps=1e-5, act=ACT_NONE,
