@@ -548,6 +548,40 @@ sparoa_status sparoa_paged_attention(sparoa_ctx *ctx, const void *q, int64_t ld_
 /* bound by the weights' bytes (4 bits here), its attention by the cache's.     */
 /* ------------------------------------------------------------------------ */
 
+/* Rules for attention scores.  Positions count from the sequence's first token; a new
+ * token t has position p = kv_len - n + t and sees the key at position j if j <= p (causal)
+ * and j > p - window (window > 0).  What is NULL (0) is left out.
+ *   cap     > 0 (from 0.001): a score s = scale q k becomes cap tanh(s / cap)
+ *   slopes  device fp32 [heads]: then s - slopes[head] |p - j|
+ *   prefix  device int32 [batch]: with causal, keys j < prefix[b] are seen too, whatever
+ *           the token's position (a prompt's first part that all of it sees)
+ *   tree    device uint64 [T]: with causal, without prefix: a sequence's new tokens (at
+ *           most 64) are a tree, and bit i of tree[row] says that new token i is an
+ *           ancestor; bits at and above the token's own are ignored.  A token sees the
+ *           cached tokens before the new ones, its ancestors and itself, and its
+ *           position p is kv_len - n + its number of ancestors; an ancestor's is counted
+ *           likewise (sparoa_rope_append takes such positions) */
+typedef struct {
+    float cap;
+    int32_t reserved;
+    const float *slopes;
+    const int32_t *prefix;
+    const uint64_t *tree;
+} sparoa_score_rules;
+
+/*
+ * sparoa_paged_attention with score rules (NULL: none).  Everything said there holds,
+ * with scores taken after the rules; lse is of those.  A sequence with a tree of more than
+ * 64 tokens is reported as INVALID_ARG by the next call that synchronises, and its rows
+ * hold anything.
+ * Errors: as sparoa_paged_attention; INVALID_ARG also for a tree or prefix without causal, or
+ * both; UNSUPPORTED for max_q above 64 with a tree. */
+sparoa_status sparoa_ruled_attention(sparoa_ctx *ctx, const void *q, int64_t ld_q, int64_t T,
+                                     int32_t heads, float scale, int32_t causal, int32_t window,
+                                     const sparoa_score_rules *rules, const sparoa_kv_cache *cache,
+                                     const sparoa_paged_batch *batch, void *y, float *lse,
+                                     const sparoa_occupancy *y_occ);
+
 /* Weights of 4 bits, laid out once by sparoa_w4_pack:
  *   W[n][k] = scale[n][k / group] * (code[n][k] - zero[n][k / group]). */
 typedef struct {

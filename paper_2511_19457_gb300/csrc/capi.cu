@@ -1542,19 +1542,34 @@ sparoa_status sparoa_rope_append(sparoa_ctx* ctx, const void* qkv, int64_t ld_qk
   return SPAROA_OK;
 }
 
-sparoa_status sparoa_paged_attention(sparoa_ctx* ctx, const void* q, int64_t ld_q, int64_t T, int32_t heads, float scale,
-                                     int32_t causal, int32_t window, const sparoa_kv_cache* cache,
-                                     const sparoa_paged_batch* batch, void* y, float* lse,
-                                     const sparoa_occupancy* y_occ) {
-  if (!ctx) return SPAROA_ERR_INVALID_ARG;
-  SP_TRY(check_paged(ctx, cache, batch, T, heads, "paged_attention"));
+namespace {
+
+sparoa_status check_rules(sparoa_ctx* ctx, const sparoa_score_rules& u, int32_t causal, const sparoa_paged_batch* batch) {
+  if (!(u.cap >= 0.f) || !std::isfinite(u.cap)) return fail(ctx, SPAROA_ERR_INVALID_ARG, "ruled_attention: cap");
+  if (u.cap > 0.f && u.cap < 1e-3f) return fail(ctx, SPAROA_ERR_UNSUPPORTED, "ruled_attention: caps from 0.001 only");
+  if ((reinterpret_cast<uintptr_t>(u.tree) & 7u) || ((reinterpret_cast<uintptr_t>(u.slopes) | reinterpret_cast<uintptr_t>(u.prefix)) & 3u))
+    return fail(ctx, SPAROA_ERR_INVALID_ARG, "ruled_attention: misaligned rules");
+  if (!causal && (u.tree || u.prefix)) return fail(ctx, SPAROA_ERR_INVALID_ARG, "ruled_attention: a tree or prefix goes with causal");
+  if (u.tree && u.prefix) return fail(ctx, SPAROA_ERR_INVALID_ARG, "ruled_attention: a tree or a prefix");
+  if (u.tree && batch->max_q > kTreeTokens)
+    return fail(ctx, SPAROA_ERR_UNSUPPORTED, "ruled_attention: trees of at most %d tokens", kTreeTokens);
+  return SPAROA_OK;
+}
+
+// Attention over the cache, without score rules or with them.
+sparoa_status attend(sparoa_ctx* ctx, const void* q, int64_t ld_q, int64_t T, int32_t heads, float scale, int32_t causal,
+                     int32_t window, const sparoa_score_rules* rules, const sparoa_kv_cache* cache,
+                     const sparoa_paged_batch* batch, void* y, float* lse, const sparoa_occupancy* y_occ) {
+  const char* what = rules ? "ruled_attention" : "paged_attention";
+  SP_TRY(check_paged(ctx, cache, batch, T, heads, what));
+  if (rules) SP_TRY(check_rules(ctx, *rules, causal, batch));
   const int64_t D = cache->head_dim;
-  if (!(scale > 0.f) || !std::isfinite(scale)) return fail(ctx, SPAROA_ERR_INVALID_ARG, "paged_attention: scale");
-  if (window < 0) return fail(ctx, SPAROA_ERR_INVALID_ARG, "paged_attention: window");
-  if (ld_q < heads * D || ld_q % 8) return fail(ctx, SPAROA_ERR_INVALID_ARG, "paged_attention: bad row length");
+  if (!(scale > 0.f) || !std::isfinite(scale)) return fail(ctx, SPAROA_ERR_INVALID_ARG, "%s: scale", what);
+  if (window < 0) return fail(ctx, SPAROA_ERR_INVALID_ARG, "%s: window", what);
+  if (ld_q < heads * D || ld_q % 8) return fail(ctx, SPAROA_ERR_INVALID_ARG, "%s: bad row length", what);
   if (T > 0 && (!q || !y || !aligned16(q) || !aligned16(y)))
-    return fail(ctx, SPAROA_ERR_INVALID_ARG, "paged_attention: NULL or misaligned tensor");
-  SP_TRY(check_occ(ctx, y_occ, T, heads * D, "paged_attention y_occ"));
+    return fail(ctx, SPAROA_ERR_INVALID_ARG, "%s: NULL or misaligned tensor", what);
+  SP_TRY(check_occ(ctx, y_occ, T, heads * D, what));
   DeviceGuard g(ctx->device, ctx->overlap);
   if (T > 0) {
     PagedArgs a;
@@ -1586,6 +1601,13 @@ sparoa_status sparoa_paged_attention(sparoa_ctx* ctx, const void* q, int64_t ld_
     a.max_q = batch->max_q;
     a.y = static_cast<__nv_bfloat16*>(y);
     a.lse = lse;
+    if (rules) {
+      a.ruled = 1;
+      a.cap = rules->cap;
+      a.slopes = rules->slopes;
+      a.prefix = rules->prefix;
+      a.tree = rules->tree;
+    }
     PagedSlot* slot = nullptr;
     SP_TRY(paged_slot(ctx, a, &slot));
     a.cnt = static_cast<unsigned*>(slot->ws.p);
@@ -1597,6 +1619,25 @@ sparoa_status sparoa_paged_attention(sparoa_ctx* ctx, const void* q, int64_t ld_
   }
   if (y_occ) SP_TRY(run_stats(ctx, y, T, heads * D, *y_occ));
   return SPAROA_OK;
+}
+
+}  // namespace
+
+sparoa_status sparoa_paged_attention(sparoa_ctx* ctx, const void* q, int64_t ld_q, int64_t T, int32_t heads, float scale,
+                                     int32_t causal, int32_t window, const sparoa_kv_cache* cache,
+                                     const sparoa_paged_batch* batch, void* y, float* lse,
+                                     const sparoa_occupancy* y_occ) {
+  if (!ctx) return SPAROA_ERR_INVALID_ARG;
+  return attend(ctx, q, ld_q, T, heads, scale, causal, window, nullptr, cache, batch, y, lse, y_occ);
+}
+
+sparoa_status sparoa_ruled_attention(sparoa_ctx* ctx, const void* q, int64_t ld_q, int64_t T, int32_t heads, float scale,
+                                     int32_t causal, int32_t window, const sparoa_score_rules* rules,
+                                     const sparoa_kv_cache* cache, const sparoa_paged_batch* batch, void* y, float* lse,
+                                     const sparoa_occupancy* y_occ) {
+  if (!ctx) return SPAROA_ERR_INVALID_ARG;
+  const sparoa_score_rules none = {};
+  return attend(ctx, q, ld_q, T, heads, scale, causal, window, rules ? rules : &none, cache, batch, y, lse, y_occ);
 }
 
 // ---------------------------------------------------------------------------

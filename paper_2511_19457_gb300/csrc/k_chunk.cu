@@ -60,11 +60,14 @@ constexpr int kOutBytes = 32 * 64;  // 32 rows of 32 values
 // tiles 1.5, an item's beginning and end 2.7 (7 and 12 steps were each slower on some of a
 // prompt, mixed chunks, drafts and windows).  A join is 4 us, but items left whole so that
 // there is none keep some CTAs twice as long: 4 x 1000 tokens, window 1024, 23 -> 37 us.
+template <bool RULES>
 struct ChunkCut {
+  static constexpr bool RULED = RULES;
   static constexpr int ROWS = kRows, EXTRA = 9, MIN_SHARE = 16, WHOLE_SHARE = 0, WHOLE_MORE = 0;
   static __device__ __forceinline__ int weight(int rows) { return rows > kTileRows ? 5 : 4; }
 };
-using Cursor = PagedCursor<ChunkCut>;
+template <bool RULES>
+using Cursor = PagedCursor<ChunkCut<RULES>>;
 
 template <int D>
 struct Cfg {
@@ -151,7 +154,9 @@ struct Bars {
 };
 
 // What the roles of a CTA share.
+template <bool RULES>
 struct Shared {
+  using Cursor = sparoa::Cursor<RULES>;
   PagedPlan<kSoftWarps * kOutBytes> plan;  // scratch: each softmax warp's block of the result on its way out
   Bars bars;
   Cursor start;
@@ -161,9 +166,11 @@ struct Shared {
   int abort;
 };
 
+template <bool RULES>
 struct Role {
+  using Cursor = sparoa::Cursor<RULES>;
   const PagedArgs& a;
-  Shared& sh;
+  Shared<RULES>& sh;
   uint32_t sq, ring;   // Q tiles, K and V stages
   long long limit;
 
@@ -189,14 +196,14 @@ __host__ __device__ __forceinline__ bool boxes_of_q(int group) { return kTileRow
 // the help of one more warp where tiles do not begin and end with a token.  One warp that
 // does nothing else: in the softmax warps the same took 4000 cycles at every item, mostly
 // for its instructions, which the loops over units drive out of the caches.
-template <int D>
-__device__ __forceinline__ void item_role(const Role& r, const CUtensorMap* tq) {
+template <int D, bool RULES>
+__device__ __forceinline__ void item_role(const Role<RULES>& r, const CUtensorMap* tq) {
   using C = Cfg<D>;
   const PagedArgs& a = r.a;
   Bars& bars = r.sh.bars;
   const int lane = threadIdx.x & 31;
   const bool boxes = boxes_of_q(a.group), leads = (threadIdx.x >> 5) == kItemWarp;
-  Cursor c = r.sh.start;
+  Cursor<RULES> c = r.sh.start;
   unsigned used[2] = {0, 0};  // items of a tile
   bool ok = true;
   for (unsigned n = 0;; ++n) {
@@ -251,18 +258,18 @@ __device__ __forceinline__ void item_role(const Role& r, const CUtensorMap* tq) 
 }
 
 // K and V of every unit: K0 V0 K1 V1 ...
-template <int D>
-__device__ __forceinline__ void load_role(const Role& r, const CUtensorMap* tk, const CUtensorMap* tv) {
+template <int D, bool RULES>
+__device__ __forceinline__ void load_role(const Role<RULES>& r, const CUtensorMap* tk, const CUtensorMap* tv) {
   using C = Cfg<D>;
   const PagedArgs& a = r.a;
   const int lane = threadIdx.x & 31;
-  Cursor c = r.sh.start;
+  Cursor<RULES> c = r.sh.start;
   const int pages = kUnitKeys >> a.page_log2;        // of a whole unit
   const int pg = lane / C::kHalves, half = lane % C::kHalves;
   const uint32_t box = 128u << a.page_log2;          // bytes: page_size rows of 128
   unsigned n = 0;                                    // stages filled
   // a page before all rows' windows may be gone: a box outside of the pool reads zeros
-  auto seen = [&](const Cursor& at, int key) { return key + (1 << a.page_log2) > at.k.lo; };
+  auto seen = [&](const Cursor<RULES>& at, int key) { return key + (1 << a.page_log2) > at.k.lo; };
   auto entry = [&]() {
     const int key = c.key0() + (pg << a.page_log2);
     return !c.done() && pg < pages && key < c.k.hi && seen(c, key) ? page_of(a, c.b, key) : -1;
@@ -297,8 +304,8 @@ __device__ __forceinline__ void load_role(const Role& r, const CUtensorMap* tk, 
 }
 
 // The MMAs.
-template <int D>
-__device__ __forceinline__ void mma_role(const Role& r, uint32_t tmem) {
+template <int D, bool RULES>
+__device__ __forceinline__ void mma_role(const Role<RULES>& r, uint32_t tmem) {
   using C = Cfg<D>;
   const PagedArgs& a = r.a;
   Bars& bars = r.sh.bars;
@@ -357,7 +364,7 @@ __device__ __forceinline__ void mma_role(const Role& r, uint32_t tmem) {
     __syncwarp();
   };
   for (unsigned n = 0; ok; ++n) {
-    const Cursor* item = r.item(n);
+    const Cursor<RULES>* item = r.item(n);
     if (!item || item->done()) break;
     const int count = item->end - item->first, first_key = item->key0(), hi = item->k.hi, len = item->len;
     const bool two = r.rows(*item) > kTileRows;
@@ -440,22 +447,53 @@ __device__ __forceinline__ void mma_role(const Role& r, uint32_t tmem) {
   }
 }
 
+// A row's 128 scores of keys from key0 on, under its rules: scaled, capped, less slope times
+// distance (in a tree the distance of the drafted keys comes later).
+__device__ __forceinline__ void rule_scores(const PagedArgs& a, const RowRules& u, uint32_t (&s)[4][32], int key0) {
+  const float cap_log2 = a.cap > 0.f ? a.scale * 2.885390081777927f / a.cap : 0.f, far = (float)(u.pos - key0);
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int k = 0; k < 32; ++k) {
+      float t = __uint_as_float(s[i][k]);
+      t = a.cap > 0.f ? fmaf(-2.f * a.cap, rcp(1.f + exp2f(t * cap_log2)), a.cap) : t * a.scale;
+      if (a.slopes) t = fmaf(-u.slope, fabsf(far - (float)(i * 32 + k)), t);
+      s[i][k] = __float_as_uint(t);
+    }
+}
+
+// The masks of a tree's row, and for its ancestors the distance in the tree for the one in
+// the cache that was taken away.
+__device__ __forceinline__ void drafted_scores(const RowRules& u, uint32_t (&s)[4][32], int key0, int len) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int k = 0; k < 32; ++k) {
+      const int key = key0 + i * 32 + k;
+      if (key < len && u.drafted(key))
+        s[i][k] = __float_as_uint(fmaf(u.slope, fabsf((float)(u.pos - key)) - (float)u.above(key), __uint_as_float(s[i][k])));
+      else if (key < u.low || key >= u.lim)
+        s[i][k] = 0xFF800000u;
+    }
+}
+
 // The softmax: a thread per row of a tile.
-template <int D>
-__device__ __forceinline__ void softmax_role(const Role& r, uint32_t tmem) {
+template <int D, bool RULES>
+__device__ __forceinline__ void softmax_role(const Role<RULES>& r, uint32_t tmem) {
   using C = Cfg<D>;
   const PagedArgs& a = r.a;
   Bars& bars = r.sh.bars;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, grp = warp >> 2, row = threadIdx.x & 127;
   const uint32_t lanes = (uint32_t)(warp & 3) << 21;  // the warp's 32 lanes of tensor memory
   const uint32_t ts = tmem + lanes + grp * 128, to = tmem + lanes + C::kO + grp * D;
-  const float sl2 = a.scale * 1.4426950408889634f, slack = fminf(kSlackLog2 / sl2, FLT_MAX);
+  const float scale = RULES ? 1.f : a.scale;  // of the scores as they are weighed
+  const float sl2 = scale * 1.4426950408889634f, slack = fminf(kSlackLog2 / sl2, FLT_MAX);
   unsigned sn = 0, on = 0, joins = 0;
   bool ok = true;
   for (unsigned n = 0;; ++n) {
-    const Cursor* item = r.item(n);
+    const Cursor<RULES>* item = r.item(n);
     if (!item || item->done()) break;
-    const Cursor& c = *item;
+    const Cursor<RULES>& c = *item;
     const int rows = r.rows(c), count = c.end - c.first;
     const bool two = rows > kTileRows;
     // the group's rows and units: its own tile and all units, or the tile and every other unit
@@ -465,7 +503,16 @@ __device__ __forceinline__ void softmax_role(const Role& r, uint32_t tmem) {
     const bool works = j0 < count;
     // keys [low, lim) that the row sees; a row past the item's last one never asks for masks
     int lim = 0x7FFFFFFF, low = 0;
-    if (live) {
+    RowRules rule;
+    if constexpr (RULES) {
+      rule.none();
+      if (live) {
+        const int at = c.t * kRows + r0 + row, tok = over_group(a, at);
+        rule.load(a, c.q0, c.n, c.len, c.prefix, tok, c.h * a.group + at - tok * a.group);
+      }
+      low = rule.low;
+      lim = rule.lim;
+    } else if (live) {
       const int p = c.len - c.n + over_group(a, c.t * kRows + r0 + row);
       lim = a.causal ? min(c.len, p + 1) : c.len;
       low = first_seen(a, p);
@@ -483,13 +530,18 @@ __device__ __forceinline__ void softmax_role(const Role& r, uint32_t tmem) {
         for (int i = 0; i < 4; ++i) tmem_ld32_nowait(ts + i * 32, s[i]);
 #pragma unroll
         for (int i = 0; i < 4; ++i) tmem_wait_ld32(s[i]);
+        if constexpr (RULES) rule_scores(a, rule, s, key0);
         if (!__all_sync(0xffffffffu, key0 >= low && key0 + kUnitKeys <= lim)) {
-          const int from = low - key0, to_ = lim - key0;
+          if (RULES && a.tree) {
+            drafted_scores(rule, s, key0, c.len);
+          } else {
+            const int from = low - key0, to_ = lim - key0;
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
+            for (int i = 0; i < 4; ++i)
 #pragma unroll
-            for (int k = 0; k < 32; ++k)
-              if (i * 32 + k < from || i * 32 + k >= to_) s[i][k] = 0xFF800000u;  // -infinity
+              for (int k = 0; k < 32; ++k)
+                if (i * 32 + k < from || i * 32 + k >= to_) s[i][k] = 0xFF800000u;  // -infinity
+          }
         }
         // (several maxima and sums side by side: one chain of 64 steps each is as long as all
         // of the row's exponentials)
@@ -658,7 +710,7 @@ __device__ __forceinline__ void softmax_role(const Role& r, uint32_t tmem) {
           slot[kRows * D + at] = m;
           slot[kRows * D + kRows + at] = l;
         } else if (live && a.lse) {
-          a.lse[out] = log_sum(m, l, a.scale, sl2);
+          a.lse[out] = log_sum(m, l, scale, sl2);
         }
       }
     }
@@ -666,13 +718,13 @@ __device__ __forceinline__ void softmax_role(const Role& r, uint32_t tmem) {
   }
 }
 
-template <int D>
+template <int D, bool RULES>
 __global__ void __launch_bounds__(kThreads, 1)
     paged_chunk_kernel(const __grid_constant__ CUtensorMap tk, const __grid_constant__ CUtensorMap tv,
                        const __grid_constant__ CUtensorMap tq, const __grid_constant__ PagedArgs a) {
   using C = Cfg<D>;
   extern __shared__ uint8_t smem_raw[];
-  __shared__ __align__(8) Shared sh;
+  __shared__ __align__(8) Shared<RULES> sh;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   if (threadIdx.x == 0) {
     Bars& bars = sh.bars;
@@ -706,14 +758,14 @@ __global__ void __launch_bounds__(kThreads, 1)
   tc_fence_after();
   pdl_wait();
   pdl_trigger();
-  make_plan<ChunkCut>(a, sh.plan);
+  make_plan<ChunkCut<RULES>>(a, sh.plan);
   const unsigned long long total = sh.plan.total;
-  const unsigned ctas = cut_ctas<ChunkCut>(total);
+  const unsigned ctas = cut_ctas<ChunkCut<RULES>>(total);
   const bool works = blockIdx.x < ctas;
   const unsigned long long u0 = works ? cut_start(total, ctas, blockIdx.x) : 0ull;
   const unsigned long long u1 = works ? cut_start(total, ctas, blockIdx.x + 1) : 0ull;
   if (warp == 0 && works) {
-    Cursor c;
+    Cursor<RULES> c;
     c.seek(a, sh.plan, ctas, u0, (int)(u1 - u0));
     if (lane == 0) sh.start = c;
   }
@@ -722,7 +774,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     // an item cut at this CTA's start is joined later; the first of its cuts speaks for it
     JoinItem j{};
     if (works && !sh.start.done() && sh.start.first > 0) {
-      const Cursor& c = sh.start;
+      const Cursor<RULES>& c = sh.start;
       const PagedShares s = shares_of(c, total, ctas, u1);
       j.c0 = (int)s.c0;
       j.c1 = (int)s.c1;
@@ -735,15 +787,15 @@ __global__ void __launch_bounds__(kThreads, 1)
     reinterpret_cast<JoinItem*>(a.ws + (size_t)2 * gridDim.x * C::kSlotFloats)[blockIdx.x] = j;
   }
   const uint32_t sq = (smem_u32(smem_raw) + 1023u) & ~1023u;
-  const Role r{a, sh, sq, sq + 2 * C::kTile, a.wait_limit ? a.wait_limit : kWaitLimitCycles};
+  const Role<RULES> r{a, sh, sq, sq + 2 * C::kTile, a.wait_limit ? a.wait_limit : kWaitLimitCycles};
   if (warp < kSoftWarps) {
     reg_inc<kManyRegs>();
-    if (works) softmax_role<D>(r, sh.tmem);
+    if (works) softmax_role<D, RULES>(r, sh.tmem);
   } else {
     reg_dec<kFewRegs>();
-    if (works && warp == kMmaWarp) mma_role<D>(r, sh.tmem);
-    if (works && warp == kLoadWarp) load_role<D>(r, &tk, &tv);
-    if (works && (warp == kItemWarp || (warp == kHelpWarp && !boxes_of_q(a.group)))) item_role<D>(r, &tq);
+    if (works && warp == kMmaWarp) mma_role<D, RULES>(r, sh.tmem);
+    if (works && warp == kLoadWarp) load_role<D, RULES>(r, &tk, &tv);
+    if (works && (warp == kItemWarp || (warp == kHelpWarp && !boxes_of_q(a.group)))) item_role<D, RULES>(r, &tq);
   }
   tc_fence_before();
   __syncthreads();
@@ -815,8 +867,8 @@ int grid_of() {
   return sms < kCtas ? sms : kCtas;
 }
 
-template <int D>
-cudaError_t launch_chunk(const PagedArgs& a, cudaStream_t s) {
+template <int D, bool RULES>
+cudaError_t launch_chunk(PagedArgs a, cudaStream_t s) {
   CUtensorMap tk, tv, tq;
   const uint64_t rows = (uint64_t)a.pages * a.kv_heads << a.page_log2;
   if (!make_tmap_2d(&tk, a.k, rows, D, 64, 1u << a.page_log2) || !make_tmap_2d(&tv, a.v, rows, D, 64, 1u << a.page_log2))
@@ -825,11 +877,12 @@ cudaError_t launch_chunk(const PagedArgs& a, cudaStream_t s) {
   if (boxes_of_q(a.group) && !make_tmap_3d(&tq, a.q, D, (uint64_t)a.heads, (uint64_t)a.T, D, (uint64_t)a.ld_q, 64,
                                            (uint32_t)a.group, (uint32_t)(kTileRows / a.group)))
     return cudaErrorInvalidValue;
-  cudaError_t e = smem_optin(reinterpret_cast<const void*>(paged_chunk_kernel<D>), Cfg<D>::kSmem);
+  cudaError_t e = smem_optin(reinterpret_cast<const void*>(paged_chunk_kernel<D, RULES>), Cfg<D>::kSmem);
   if (e != cudaSuccess) return e;
   const int grid = grid_of();
-  e = launch_kernel(paged_chunk_kernel<D>, dim3(grid), dim3(kThreads), Cfg<D>::kSmem, s, tk, tv, tq, a);
+  e = launch_kernel(paged_chunk_kernel<D, RULES>, dim3(grid), dim3(kThreads), Cfg<D>::kSmem, s, tk, tv, tq, a);
   if (e != cudaSuccess) return e;
+  if (RULES) a.scale = 1.f;  // (the parts' maxima are scaled)
   return launch_kernel(paged_join_kernel<D>, dim3(grid, kRows / 32), dim3(4 * D), 0, s, a, grid);
 }
 
@@ -840,7 +893,8 @@ size_t paged_chunk_ws_bytes() {
 }
 
 cudaError_t launch_paged_chunk(const PagedArgs& a, cudaStream_t s) {
-  return a.D == 128 ? launch_chunk<128>(a, s) : launch_chunk<64>(a, s);
+  if (a.ruled) return a.D == 128 ? launch_chunk<128, true>(a, s) : launch_chunk<64, true>(a, s);
+  return a.D == 128 ? launch_chunk<128, false>(a, s) : launch_chunk<64, false>(a, s);
 }
 
 }  // namespace sparoa

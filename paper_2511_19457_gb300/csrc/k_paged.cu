@@ -28,13 +28,13 @@ constexpr int kKeys = 16;     // a warp's keys of a unit
 // An item's beginning and end take as long as one unit to three (64 contexts of 500 to
 // 16000 tokens: 188 us with 1 and with 3, 185 with 2); joining parts of an item as eight
 // units of a CTA that has few.
+template <bool RULES>
 struct SmallCut {
+  static constexpr bool RULED = RULES;
   static constexpr int ROWS = kRows, EXTRA = 2, MIN_SHARE = 2, WHOLE_SHARE = 8, WHOLE_MORE = 8;
   static __device__ __forceinline__ int weight(int) { return 1; }
 };
 static_assert(kKeys * kWarps == kUnitKeys, "unit");
-
-using Cursor = PagedCursor<SmallCut>;
 
 template <int D>
 struct Cfg {
@@ -78,11 +78,20 @@ __device__ __forceinline__ uint32_t rest2(uint32_t hi, float lo, float up) {
 template <int D>
 constexpr int kSlotFloats = kRows * (D + 2);
 
-template <int D>
+// A score under its row's rules, from q k scaled: capped, less slope times distance.  cap
+// tanh(t / cap) = cap - 2 cap / (1 + exp(2 t / cap)), off by a few 2^-24 of cap.
+__device__ __forceinline__ float ruled_score(float t, float cap, float two_over_cap_log2, float slope, float distance) {
+  if (cap > 0.f) t = fmaf(-2.f * cap, rcp(1.f + exp2f(t * two_over_cap_log2)), cap);
+  return fmaf(-slope, distance, t);
+}
+
+template <int D, bool RULES>
 __global__ void __launch_bounds__(kThreads, 1)
     paged_small_kernel(const __grid_constant__ CUtensorMap tk, const __grid_constant__ CUtensorMap tv,
                        const __grid_constant__ PagedArgs a) {
   using C = Cfg<D>;
+  using Cut = SmallCut<RULES>;
+  using Cursor = PagedCursor<Cut>;
   constexpr int S = C::kStages;
   extern __shared__ uint8_t smem_raw[];
   __shared__ PagedPlan<> plan;
@@ -106,9 +115,9 @@ __global__ void __launch_bounds__(kThreads, 1)
   __syncthreads();
   pdl_wait();
   pdl_trigger();
-  make_plan<SmallCut>(a, plan);
+  make_plan<Cut>(a, plan);
   const unsigned long long total = plan.total;
-  const unsigned ctas = cut_ctas<SmallCut>(total);
+  const unsigned ctas = cut_ctas<Cut>(total);
   if (blockIdx.x >= ctas) return;
   const unsigned long long u0 = cut_start(total, ctas, blockIdx.x), u1 = cut_start(total, ctas, blockIdx.x + 1);
   if (warp == 0) {
@@ -154,7 +163,10 @@ __global__ void __launch_bounds__(kThreads, 1)
   float o[D / 8][4], m0, m1, l0, l1;
   int lim0 = 0, lim1 = 0, low0 = 0, low1 = 0;  // keys that rows g and g + 8 see: [low, lim)
   bool fresh = true, any = false;
-  const float sl2 = a.scale * 1.4426950408889634f;
+  const float scale = RULES ? 1.f : a.scale;  // of the scores as they are weighed
+  const float sl2 = scale * 1.4426950408889634f;
+  const float cap_log2 = RULES && a.cap > 0.f ? 2.885390081777927f / a.cap : 0.f;
+  RowRules rule[2];
   // lane's rows within the ldmatrix blocks: K (n = key, k = value), V transposed
   const int krow = ((lane >> 4) << 3) + (lane & 7), kch = (lane >> 3) & 1;
   const int vrow = (((lane >> 3) & 1) << 3) + (lane & 7), vch = lane >> 4;
@@ -177,8 +189,14 @@ __global__ void __launch_bounds__(kThreads, 1)
           const int row = cc.t * kRows + g + 8 * i, tok = over_group(a, row), head = cc.h * a.group + row - tok * a.group;
           const int pos = cc.len - cc.n + tok;
           p[i] = a.q + (int64_t)(cc.q0 + tok) * a.ld_q + head * D;
-          lim[i] = a.causal ? min(cc.len, pos + 1) : cc.len;
-          low[i] = first_seen(a, pos);
+          if constexpr (RULES) {
+            rule[i].load(a, cc.q0, cc.n, cc.len, cc.prefix, tok, head);
+          } else {
+            lim[i] = a.causal ? min(cc.len, pos + 1) : cc.len;
+            low[i] = first_seen(a, pos);
+          }
+        } else if constexpr (RULES) {
+          rule[i].none();
         }
       }
       lim0 = lim[0]; lim1 = lim[1]; low0 = low[0]; low1 = low[1];
@@ -218,13 +236,30 @@ __global__ void __launch_bounds__(kThreads, 1)
           mma16816(s[0], qa[kk], r[0], r[1]);
           mma16816(s[1], qa[kk], r[2], r[3]);
         }
+        if constexpr (RULES) {
 #pragma unroll
-        for (int nt = 0; nt < 2; ++nt) {
-          const int key = key0 + nt * 8 + 2 * tq;
-          if (key < low0 || key >= lim0) s[nt][0] = -INFINITY;
-          if (key + 1 < low0 || key + 1 >= lim0) s[nt][1] = -INFINITY;
-          if (key < low1 || key >= lim1) s[nt][2] = -INFINITY;
-          if (key + 1 < low1 || key + 1 >= lim1) s[nt][3] = -INFINITY;
+          for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const RowRules& u = rule[e >> 1];
+              const int key = key0 + nt * 8 + 2 * tq + (e & 1);
+              bool seen = key >= u.low && key < u.lim;
+              int far = abs(u.pos - key);
+              if (a.tree && key >= u.base && key < cc.len && u.drafted(key)) {
+                seen = true;
+                far = u.above(key);
+              }
+              s[nt][e] = seen ? ruled_score(s[nt][e] * a.scale, a.cap, cap_log2, u.slope, (float)far) : -INFINITY;
+            }
+        } else {
+#pragma unroll
+          for (int nt = 0; nt < 2; ++nt) {
+            const int key = key0 + nt * 8 + 2 * tq;
+            if (key < low0 || key >= lim0) s[nt][0] = -INFINITY;
+            if (key + 1 < low0 || key + 1 >= lim0) s[nt][1] = -INFINITY;
+            if (key < low1 || key >= lim1) s[nt][2] = -INFINITY;
+            if (key + 1 < low1 || key + 1 >= lim1) s[nt][3] = -INFINITY;
+          }
         }
         float x0 = fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[1][0], s[1][1]));
         float x1 = fmaxf(fmaxf(s[0][2], s[0][3]), fmaxf(s[1][2], s[1][3]));
@@ -391,7 +426,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         for (int k = 0; k < 8; ++k) acc[k] *= inv;
         *reinterpret_cast<uint4*>(a.y + (tok * a.heads + head) * D + piece * 8) = pack8(acc);
         if (a.lse && piece == 0)
-          a.lse[tok * a.heads + head] = ls == 0.f ? -INFINITY : fmaf(mx, a.scale, logf(ls));
+          a.lse[tok * a.heads + head] = ls == 0.f ? -INFINITY : fmaf(mx, scale, logf(ls));
       }
       __syncthreads();  // the free stages may be filled, s_m, s_l and s_at written again
       fresh = true;
@@ -410,15 +445,15 @@ int grid_of() {
 }
 size_t small_ws_bytes() { return (size_t)2 * kPagedCounters * kSlotFloats<128> * sizeof(float); }
 
-template <int D>
+template <int D, bool RULES>
 cudaError_t launch_small(const PagedArgs& a, cudaStream_t s) {
   CUtensorMap tk, tv;
   const uint64_t rows = (uint64_t)a.pages * a.kv_heads << a.page_log2;
   if (!make_tmap_2d(&tk, a.k, rows, D, 64, kKeys) || !make_tmap_2d(&tv, a.v, rows, D, 64, kKeys))
     return cudaErrorInvalidValue;
-  const cudaError_t e = smem_optin(reinterpret_cast<const void*>(paged_small_kernel<D>), Cfg<D>::kSmem);
+  const cudaError_t e = smem_optin(reinterpret_cast<const void*>(paged_small_kernel<D, RULES>), Cfg<D>::kSmem);
   if (e != cudaSuccess) return e;
-  return launch_kernel(paged_small_kernel<D>, dim3(grid_of()), dim3(kThreads), Cfg<D>::kSmem, s, tk, tv, a);
+  return launch_kernel(paged_small_kernel<D, RULES>, dim3(grid_of()), dim3(kThreads), Cfg<D>::kSmem, s, tk, tv, a);
 }
 
 }  // namespace
@@ -431,7 +466,8 @@ size_t paged_ws_bytes(const PagedArgs& a) { return few_rows(a) ? small_ws_bytes(
 
 cudaError_t launch_paged_attention(const PagedArgs& a, cudaStream_t s) {
   if (!few_rows(a)) return launch_paged_chunk(a, s);
-  return a.D == 128 ? launch_small<128>(a, s) : launch_small<64>(a, s);
+  if (a.ruled) return a.D == 128 ? launch_small<128, true>(a, s) : launch_small<64, true>(a, s);
+  return a.D == 128 ? launch_small<128, false>(a, s) : launch_small<64, false>(a, s);
 }
 
 }  // namespace sparoa

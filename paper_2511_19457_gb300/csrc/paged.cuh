@@ -55,16 +55,25 @@ __device__ __forceinline__ int first_seen(const PagedArgs& a, int p) {
   return a.window > 0 && p + 1 > a.window ? p + 1 - a.window : 0;
 }
 
+// Keys that all new tokens of a sequence see (score rules; read again where it is wanted).
 template <typename Cut>
-__device__ __forceinline__ TileKeys tile_keys(const PagedArgs& a, int n, int len, int t) {
+__device__ __forceinline__ int prefix_of(const PagedArgs& a, int b) {
+  if constexpr (Cut::RULED) return a.prefix ? a.prefix[b] : 0;
+  return 0;
+}
+
+// `prefix`: of the sequence.  A tree's tokens are as deep as their branch, so none is
+// before its first one's position.
+template <typename Cut>
+__device__ __forceinline__ TileKeys tile_keys(const PagedArgs& a, int n, int len, int t, int prefix) {
   constexpr int RT = Cut::ROWS;
   TileKeys k;
   k.hi = len;
   if (a.causal) {
     const int last = over_group(a, min(n * a.group, (t + 1) * RT) - 1);
-    k.hi = max(0, min(len, len - n + last + 1));
+    k.hi = max(0, min(len, max(len - n + last + 1, prefix)));
   }
-  k.lo = first_seen(a, len - n + over_group(a, t * RT));
+  k.lo = first_seen(a, len - n + (Cut::RULED && a.tree ? 0 : over_group(a, t * RT)));
   k.blk0 = k.lo / kUnitKeys;
   k.units = max(1, (k.hi + kUnitKeys - 1) / kUnitKeys - k.blk0);
   return k;
@@ -72,8 +81,8 @@ __device__ __forceinline__ TileKeys tile_keys(const PagedArgs& a, int n, int len
 
 // Cost of tile t.
 template <typename Cut>
-__device__ __forceinline__ int tile_cost(const PagedArgs& a, int n, int len, int t) {
-  return tile_keys<Cut>(a, n, len, t).units * Cut::weight(n * a.group - t * Cut::ROWS) + Cut::EXTRA;
+__device__ __forceinline__ int tile_cost(const PagedArgs& a, int n, int len, int t, int prefix) {
+  return tile_keys<Cut>(a, n, len, t, prefix).units * Cut::weight(n * a.group - t * Cut::ROWS) + Cut::EXTRA;
 }
 
 // Fills the plan (all threads of the CTA; ends with a block barrier).  What the lists
@@ -89,7 +98,7 @@ __device__ __forceinline__ void make_plan(const PagedArgs& a, Plan& p) {
   unsigned long long sum = 0ull;
   for (int b = threadIdx.x; b < a.batch; b += blockDim.x) {
     long long q0 = a.q_start[b], n = (long long)a.q_start[b + 1] - q0, len = a.kv_len[b];
-    const bool bad_rows = q0 < 0 || n < 0 || q0 + n > a.T || n * a.group > 0x3FFFFFFF;
+    const bool bad_rows = q0 < 0 || n < 0 || q0 + n > a.T || n * a.group > 0x3FFFFFFF || (Cut::RULED && a.tree && n > kTreeTokens);
     if (bad_rows || len < 0 || len > room) {
       atomicOr(a.err, kErrBadIndex);
       if (bad_rows) n = 0;
@@ -99,16 +108,16 @@ __device__ __forceinline__ void make_plan(const PagedArgs& a, Plan& p) {
     p.q0[b] = (int)q0;
     p.n[b] = (int)n;
     p.len[b] = (int)len;
-    p.cost[b] = tiles == 1 ? (unsigned long long)tile_cost<Cut>(a, (int)n, (int)len, 0) : 0ull;
+    p.cost[b] = tiles == 1 ? (unsigned long long)tile_cost<Cut>(a, (int)n, (int)len, 0, prefix_of<Cut>(a, b)) : 0ull;
     many |= tiles > 1;
     sum += p.cost[b] * a.kv_heads;
   }
   if (__syncthreads_or(many)) {
     for (int b = warp; b < a.batch; b += warps) {
-      const int n = p.n[b], len = p.len[b], tiles = tiles_of<Cut>(n, a.group);
+      const int n = p.n[b], len = p.len[b], tiles = tiles_of<Cut>(n, a.group), prefix = prefix_of<Cut>(a, b);
       if (tiles <= 1) continue;
       unsigned long long u = 0ull;
-      for (int t = lane; t < tiles; t += 32) u += (unsigned long long)tile_cost<Cut>(a, n, len, t);
+      for (int t = lane; t < tiles; t += 32) u += (unsigned long long)tile_cost<Cut>(a, n, len, t, prefix);
 #pragma unroll
       for (int d = 16; d > 0; d >>= 1) u += __shfl_xor_sync(0xffffffffu, u, d);
       if (lane == 0) {
@@ -127,9 +136,19 @@ __device__ __forceinline__ void make_plan(const PagedArgs& a, Plan& p) {
 __device__ __forceinline__ unsigned long long quotient(unsigned long long a, unsigned long long b) {
   return (a >> 32) == 0ull && (b >> 32) == 0ull ? (unsigned)a / (unsigned)b : a / b;
 }
+// A cursor's part under score rules.
+template <bool RULED>
+struct CursorPrefix {
+  static constexpr int prefix = 0;
+};
+template <>
+struct CursorPrefix<true> {
+  int prefix;  // of the sequence
+};
 // A walk over one CTA's share of the line, the same in all lanes of a warp.
 template <typename Cut>
-struct PagedCursor {
+struct PagedCursor : CursorPrefix<Cut::RULED> {
+  using CursorPrefix<Cut::RULED>::prefix;
   int b, h, t, tiles;
   int q0, n, len;
   TileKeys k;
@@ -150,11 +169,12 @@ struct PagedCursor {
     n = p.n[b];
     len = p.len[b];
     tiles = tiles_of<Cut>(n, a.group);
+    if constexpr (Cut::RULED) prefix = prefix_of<Cut>(a, b);
   }
   // a unit belongs to the share that has the first step of its cost
   __device__ __forceinline__ int unit_at(int at) const { return max(0, at - Cut::EXTRA + weight - 1) / weight; }
   __device__ __forceinline__ void enter(const PagedArgs& a) {
-    k = tile_keys<Cut>(a, n, len, t);
+    k = tile_keys<Cut>(a, n, len, t, prefix);
     weight = Cut::weight(n * a.group - t * Cut::ROWS);
     if (cost() <= whole) {
       first = pos == 0 ? 0 : k.units;
@@ -197,7 +217,7 @@ struct PagedCursor {
     t = 0;
     if (tiles > 1) {
       for (int t0 = 0;; t0 += 32) {
-        const unsigned mine = t0 + lane < tiles ? (unsigned)tile_cost<Cut>(a, n, len, t0 + lane) : 0u;
+        const unsigned mine = t0 + lane < tiles ? (unsigned)tile_cost<Cut>(a, n, len, t0 + lane, prefix) : 0u;
         unsigned incl = mine;
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
@@ -278,6 +298,52 @@ __device__ __forceinline__ PagedShares shares_of(const PagedCursor<Cut>& c, unsi
 // Where CTA c leaves its part of an item: a CTA has at most one part that another began
 // (its first item's end) and one that another ends (its last item's beginning).
 __device__ __forceinline__ unsigned part_slot(unsigned c, bool begins) { return 2u * c + (begins ? 1u : 0u); }
+
+// 1 / x, to 2^-23
+__device__ __forceinline__ float rcp(float x) {
+  float y;
+  asm("rcp.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+// What a row sees and how its scores are changed, under score rules.
+struct RowRules {
+  int pos;                  // the token's position; its depth in a tree
+  int low, lim;             // keys [low, lim) are seen
+  int base;                 // and of the drafted keys from `base` on those in `tree`
+  unsigned long long tree;
+  float slope;
+
+  // of token `tok` of a sequence, query head `head`
+  __device__ __forceinline__ void load(const PagedArgs& a, int q0, int n, int len, int prefix, int tok, int head) {
+    base = len - n;
+    pos = base + tok;
+    tree = 0ull;
+    lim = a.causal ? min(len, max(pos + 1, prefix)) : len;
+    if (a.tree) {
+      // ancestors and the token itself (bits from its own on mean nothing)
+      const unsigned long long own = 1ull << tok;
+      tree = (a.tree[q0 + tok] & (own - 1ull)) | own;
+      const int deep = __popcll(tree);
+      pos = base + deep - 1;
+      lim = min(len, base);
+      if (a.window > 0 && a.window < deep)  // only the nearest
+        for (int i = deep - a.window; i > 0; --i) tree &= tree - 1ull;
+    }
+    low = first_seen(a, pos);
+    slope = a.slopes ? a.slopes[head] : 0.f;
+  }
+  // no row: sees what it likes, for its results go nowhere
+  __device__ __forceinline__ void none() {
+    pos = low = base = 0;
+    lim = 0x7FFFFFFF;
+    tree = 0ull;
+    slope = 0.f;
+  }
+  // whether drafted key `key` < len is the token's ancestor, and how far up
+  __device__ __forceinline__ bool drafted(int key) const { return key >= base && (tree >> (key - base)) & 1ull; }
+  __device__ __forceinline__ int above(int key) const { return __popcll(tree >> (key - base) >> 1); }
+};
 
 // The table's entry for key `key` of sequence b, as it is (loaded ahead of its use).
 __device__ __forceinline__ int page_of(const PagedArgs& a, int b, int key) {

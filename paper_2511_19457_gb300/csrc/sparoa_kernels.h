@@ -289,6 +289,12 @@ struct PagedArgs {
   uint32_t* err = nullptr;
   long long wait_limit = 0;
   int fault = 0;               // error-path tests: 1 withholds the chunk kernel's signals of its scores
+  // score rules
+  int ruled = 0;
+  float cap = 0.f;                   // above 0: scores s become cap tanh(s / cap)
+  const float* slopes = nullptr;     // [heads] or null: less slope times the distance
+  const int32_t* prefix = nullptr;   // [batch] or null
+  const uint64_t* tree = nullptr;    // [T] or null
 };
 constexpr int kPagedMaxBatch = 1024;
 constexpr int kPagedCounters = 256;  // and CTAs at most

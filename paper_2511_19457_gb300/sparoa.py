@@ -87,6 +87,10 @@ class RopeDesc(ctypes.Structure):
     _fields_ = [("rot", _I32), ("layout", _I32), ("turns", _P), ("scale", ctypes.c_float), ("reserved", _I32)]
 
 
+class ScoreRulesDesc(ctypes.Structure):
+    _fields_ = [("cap", ctypes.c_float), ("reserved", _I32), ("slopes", _P), ("prefix", _P), ("tree", _P)]
+
+
 class W4Desc(ctypes.Structure):
     _fields_ = [("packed", _P), ("N", _I64), ("K", _I64), ("group", _I32), ("zeros", _I32)]
 
@@ -147,6 +151,8 @@ _sig("sparoa_rope_append", [_P, _P, _I64, _I64, _I32, ctypes.POINTER(RopeDesc), 
                             ctypes.POINTER(PagedBatchDesc), _P, _I64])
 _sig("sparoa_paged_attention", [_P, _P, _I64, _I64, _I32, ctypes.c_float, _I32, _I32, ctypes.POINTER(KvCacheDesc),
                                 ctypes.POINTER(PagedBatchDesc), _P, _P, ctypes.POINTER(Occupancy)])
+_sig("sparoa_ruled_attention", [_P, _P, _I64, _I64, _I32, ctypes.c_float, _I32, _I32, ctypes.POINTER(ScoreRulesDesc),
+                                ctypes.POINTER(KvCacheDesc), ctypes.POINTER(PagedBatchDesc), _P, _P, ctypes.POINTER(Occupancy)])
 _lib.sparoa_w4_bytes.restype = ctypes.c_uint64
 _lib.sparoa_w4_bytes.argtypes = [_I64, _I64, _I32, _I32]
 _sig("sparoa_w4_pack", [_P, _P, _P, _P, _I64, _I64, _I32, _P])
@@ -167,7 +173,7 @@ EXPORTED = ["sparoa_create", "sparoa_destroy", "sparoa_set_stream", "sparoa_set_
             "sparoa_maxpool2d", "sparoa_avgpool_global", "sparoa_bn_act", "sparoa_run_graph",
             "sparoa_graph_workspace", "sparoa_gemm_split", "sparoa_layernorm", "sparoa_attention",
             "sparoa_add_norm", "sparoa_rope_turns", "sparoa_rope_append", "sparoa_paged_attention",
-            "sparoa_w4_bytes", "sparoa_w4_pack", "sparoa_gemm_w4", "sparoa_shape_logits", "sparoa_tree_accept",
+            "sparoa_ruled_attention", "sparoa_w4_bytes", "sparoa_w4_pack", "sparoa_gemm_w4", "sparoa_shape_logits", "sparoa_tree_accept",
             "sparoa_gemm_noalloc"]
 
 
@@ -574,26 +580,61 @@ def sparoa_rope_append(ctx: Context, qkv, q_out, cache: KVCache, batch: PagedBat
         ctx._check(st)
 
 
+def _attention_rows(q, y, cache, lse, what):
+    """Checks of q [T, heads, head_dim] and its results; (row length, T, heads)."""
+    T, D = q.shape[0], cache.head_dim
+    ld, width = _token_rows(q, T, D, what)
+    if width % D or not (y.dtype is _bf16 and y.is_cuda and y.is_contiguous() and y.numel() == T * width):
+        _refuse(f"{what}: q rows of whole heads, y of q's size")
+    if lse is not None:
+        _want_rows(lse, _FP32S, f"{what} lse")
+        _want(lse.numel() == T * (width // D), f"{what}: lse")
+    return ld, T, width // D
+
+
 def sparoa_paged_attention(ctx: Context, q, y, cache: KVCache, batch: PagedBatch, scale=None, causal=True, window=0,
                            lse=None, y_occ=None):
     """y = softmax(scale q K^T) V of the new tokens over their cached sequences; q [T, heads, head_dim]
     (rows may be strided), y the same (contiguous), lse fp32 [T, heads] or None."""
-    T, D = q.shape[0], cache.head_dim
-    ld, width = _token_rows(q, T, D, "paged_attention q")
-    if width % D or not (y.dtype is _bf16 and y.is_cuda and y.is_contiguous() and y.numel() == T * width):
-        _refuse("paged_attention: q rows of whole heads, y of q's size")
-    if lse is not None:
-        _want_rows(lse, _FP32S, "paged_attention lse")
-        _want(lse.numel() == T * (width // D), "paged_attention: lse")
+    ld, T, heads = _attention_rows(q, y, cache, lse, "paged_attention")
     ctx._bind()
-    st = _paged_attention(ctx.h, q.data_ptr(), ld, T, width // D, cache.scale if scale is None else scale,
+    st = _paged_attention(ctx.h, q.data_ptr(), ld, T, heads, cache.scale if scale is None else scale,
                           1 if causal else 0, window, cache.ref, batch.ref, y.data_ptr(), _ptr(lse), _occ(y_occ))
     if st:
         ctx._check(st)
 
 
+class ScoreRules:
+    """Rules of sparoa_ruled_attention; keeps its tensors alive.  cap: scores s become cap tanh(s / cap); slopes
+    fp32 [heads]: less slope |distance|; prefix int32 [batch]: keys that every new token sees; tree int64
+    [T]: bits of each new token's ancestors among its sequence's new tokens."""
+
+    def __init__(self, cap=0.0, slopes=None, prefix=None, tree=None):
+        for t, types in ((slopes, _FP32S), (prefix, _I32S), (tree, (torch.int64,))):
+            if t is not None:
+                _want_rows(t, types, "ScoreRules")
+        self.slopes, self.prefix, self.tree = slopes, prefix, tree
+        self.desc = ScoreRulesDesc(float(cap), 0, _ptr(slopes), _ptr(prefix), _ptr(tree))
+        self.ref = _byref(self.desc)
+
+
+def sparoa_ruled_attention(ctx: Context, q, y, cache: KVCache, batch: PagedBatch, rules: ScoreRules, scale=None, causal=True,
+                           window=0, lse=None, y_occ=None):
+    """sparoa_paged_attention with score rules: a cap, a bias by distance, a prefix, a tree of drafted tokens."""
+    ld, T, heads = _attention_rows(q, y, cache, lse, "ruled_attention")
+    for t, n, what in ((rules.slopes, heads, "a slope per head"), (rules.prefix, batch.kv_len.numel(), "a prefix per sequence"),
+                       (rules.tree, T, "ancestors of every new token")):
+        if t is not None and t.numel() != n:
+            _refuse(f"ruled_attention: {what} wanted")
+    ctx._bind()
+    st = _ruled_attention(ctx.h, q.data_ptr(), ld, T, heads, cache.scale if scale is None else scale, 1 if causal else 0, window,
+                          rules.ref, cache.ref, batch.ref, y.data_ptr(), _ptr(lse), _occ(y_occ))
+    if st:
+        ctx._check(st)
+
+
 _add_norm, _rope_append = _lib.sparoa_add_norm, _lib.sparoa_rope_append
-_paged_attention = _lib.sparoa_paged_attention
+_paged_attention, _ruled_attention = _lib.sparoa_paged_attention, _lib.sparoa_ruled_attention
 
 
 # ---------------------------------------------------------------------------
