@@ -1601,9 +1601,15 @@ sparoa_status attend(sparoa_ctx* ctx, const void* q, int64_t ld_q, int64_t T, in
     a.max_q = batch->max_q;
     a.y = static_cast<__nv_bfloat16*>(y);
     a.lse = lse;
+    a.unit = scale;
+    a.log2_unit = scale * 1.4426950408889634f;
     if (rules) {
       a.ruled = 1;
       a.cap = rules->cap;
+      if (rules->cap > 0.f || rules->slopes) {  // (changed scores are powers of 2: paged.cuh)
+        a.unit = 0.6931471805599453f;
+        a.log2_unit = 1.f;
+      }
       a.slopes = rules->slopes;
       a.prefix = rules->prefix;
       a.tree = rules->tree;

@@ -81,12 +81,6 @@ struct Cfg {
   static constexpr uint32_t kO = 256;                   // first column of O
 };
 
-// 2^x; results below the normal range are zero
-__device__ __forceinline__ float ex2_ftz(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
 __device__ __forceinline__ float scaled_ref(float m, float sl2) { return __fmul_rn(m, sl2); }
 // what weights by reference m are multiplied by to go by `top`
 __device__ __forceinline__ float to_ref(float m, float top, float sl2) {
@@ -447,19 +441,55 @@ __device__ __forceinline__ void mma_role(const Role<RULES>& r, uint32_t tmem) {
   }
 }
 
-// A row's 128 scores of keys from key0 on, under its rules: scaled, capped, less slope times
-// distance (in a tree the distance of the drafted keys comes later).
+// A row's 128 scores of keys from key0 on, under its rules (in a tree the distance of the
+// drafted keys is put right later).
 __device__ __forceinline__ void rule_scores(const PagedArgs& a, const RowRules& u, uint32_t (&s)[4][32], int key0) {
-  const float cap_log2 = a.cap > 0.f ? a.scale * 2.885390081777927f / a.cap : 0.f, far = (float)(u.pos - key0);
+  auto pair = [&](int i, int k) { return f2(__uint_as_float(s[i][k]), __uint_as_float(s[i][k + 1])); };
+  auto put = [&](int i, int k, f2_t v) {
+    float x, y;
+    f2_split(v, x, y);
+    s[i][k] = __float_as_uint(x);
+    s[i][k + 1] = __float_as_uint(y);
+  };
+  if (a.cap > 0.f) {
+    const CapConst cap(a);
+    float top[4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < 4; ++i) {
+      top[i] = fabsf(__uint_as_float(s[i][0]));
 #pragma unroll
-    for (int k = 0; k < 32; ++k) {
-      float t = __uint_as_float(s[i][k]);
-      t = a.cap > 0.f ? fmaf(-2.f * a.cap, rcp(1.f + exp2f(t * cap_log2)), a.cap) : t * a.scale;
-      if (a.slopes) t = fmaf(-u.slope, fabsf(far - (float)(i * 32 + k)), t);
-      s[i][k] = __float_as_uint(t);
+      for (int k = 1; k < 32; ++k) top[i] = fmaxf(top[i], fabsf(__uint_as_float(s[i][k])));
     }
+    if (__all_sync(0xffffffffu, fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * cap.k <= 0.5f)) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int k = 0; k < 32; k += 2) put(i, k, cap.near(pair(i, k)));
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int k = 0; k < 32; k += 2) put(i, k, cap.far(pair(i, k)));
+    }
+  }
+  if (a.slopes) {
+    const float far = (float)(u.pos - key0), one = a.cap > 0.f ? 1.f : a.scale * 1.4426950408889634f;
+    if (a.causal && !a.prefix) {
+      // (keys behind the token are masked: no distance is below zero)
+      const f2_t sl = f2(u.slope, u.slope), off = f2(-u.slope * far, -u.slope * far), o2 = f2(one, one);
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int k = 0; k < 32; k += 2)
+          put(i, k, ffma2(pair(i, k), o2, ffma2(f2((float)(i * 32 + k), (float)(i * 32 + k + 1)), sl, off)));
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int k = 0; k < 32; ++k)
+          s[i][k] = __float_as_uint(fmaf(-u.slope, fabsf(far - (float)(i * 32 + k)), __uint_as_float(s[i][k]) * one));
+    }
+  }
 }
 
 // The masks of a tree's row, and for its ancestors the distance in the tree for the one in
@@ -471,7 +501,7 @@ __device__ __forceinline__ void drafted_scores(const RowRules& u, uint32_t (&s)[
     for (int k = 0; k < 32; ++k) {
       const int key = key0 + i * 32 + k;
       if (key < len && u.drafted(key))
-        s[i][k] = __float_as_uint(fmaf(u.slope, fabsf((float)(u.pos - key)) - (float)u.above(key), __uint_as_float(s[i][k])));
+        s[i][k] = __float_as_uint(fmaf(u.slope, (float)(u.pos - key - u.above(key)), __uint_as_float(s[i][k])));
       else if (key < u.low || key >= u.lim)
         s[i][k] = 0xFF800000u;
     }
@@ -486,8 +516,7 @@ __device__ __forceinline__ void softmax_role(const Role<RULES>& r, uint32_t tmem
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, grp = warp >> 2, row = threadIdx.x & 127;
   const uint32_t lanes = (uint32_t)(warp & 3) << 21;  // the warp's 32 lanes of tensor memory
   const uint32_t ts = tmem + lanes + grp * 128, to = tmem + lanes + C::kO + grp * D;
-  const float scale = RULES ? 1.f : a.scale;  // of the scores as they are weighed
-  const float sl2 = scale * 1.4426950408889634f, slack = fminf(kSlackLog2 / sl2, FLT_MAX);
+  const float sl2 = a.log2_unit, slack = fminf(kSlackLog2 / sl2, FLT_MAX);
   unsigned sn = 0, on = 0, joins = 0;
   bool ok = true;
   for (unsigned n = 0;; ++n) {
@@ -710,7 +739,7 @@ __device__ __forceinline__ void softmax_role(const Role<RULES>& r, uint32_t tmem
           slot[kRows * D + at] = m;
           slot[kRows * D + kRows + at] = l;
         } else if (live && a.lse) {
-          a.lse[out] = log_sum(m, l, scale, sl2);
+          a.lse[out] = log_sum(m, l, a.unit, sl2);
         }
       }
     }
@@ -822,7 +851,7 @@ __global__ void __launch_bounds__(4 * D)
   if (!j.valid || (int)blockIdx.y * 32 >= j.rows) return;
   const bool live = r < j.rows;
   auto slot = [&](int c) { return a.ws + (size_t)part_slot(j.c0 + c, c == 0) * C::kSlotFloats; };
-  const float sl2 = a.scale * 1.4426950408889634f;
+  const float sl2 = a.log2_unit;
   float4 p[kJoinParts], q[kJoinParts];
   auto fetch = [&](int c0) {
 #pragma unroll
@@ -859,7 +888,7 @@ __global__ void __launch_bounds__(4 * D)
   const int row = j.t * kRows + r, of = over_group(a, row);
   const int64_t at = (int64_t)(j.q0 + of) * a.heads + j.h * a.group + row - of * a.group;
   *reinterpret_cast<uint4*>(a.y + at * D + warp * 8) = pack8(f);
-  if (a.lse && warp == 0) a.lse[at] = log_sum(mx, l, a.scale, sl2);
+  if (a.lse && warp == 0) a.lse[at] = log_sum(mx, l, a.unit, sl2);
 }
 
 int grid_of() {
@@ -868,7 +897,7 @@ int grid_of() {
 }
 
 template <int D, bool RULES>
-cudaError_t launch_chunk(PagedArgs a, cudaStream_t s) {
+cudaError_t launch_chunk(const PagedArgs& a, cudaStream_t s) {
   CUtensorMap tk, tv, tq;
   const uint64_t rows = (uint64_t)a.pages * a.kv_heads << a.page_log2;
   if (!make_tmap_2d(&tk, a.k, rows, D, 64, 1u << a.page_log2) || !make_tmap_2d(&tv, a.v, rows, D, 64, 1u << a.page_log2))
@@ -882,7 +911,6 @@ cudaError_t launch_chunk(PagedArgs a, cudaStream_t s) {
   const int grid = grid_of();
   e = launch_kernel(paged_chunk_kernel<D, RULES>, dim3(grid), dim3(kThreads), Cfg<D>::kSmem, s, tk, tv, tq, a);
   if (e != cudaSuccess) return e;
-  if (RULES) a.scale = 1.f;  // (the parts' maxima are scaled)
   return launch_kernel(paged_join_kernel<D>, dim3(grid, kRows / 32), dim3(4 * D), 0, s, a, grid);
 }
 

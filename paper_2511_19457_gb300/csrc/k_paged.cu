@@ -78,13 +78,6 @@ __device__ __forceinline__ uint32_t rest2(uint32_t hi, float lo, float up) {
 template <int D>
 constexpr int kSlotFloats = kRows * (D + 2);
 
-// A score under its row's rules, from q k scaled: capped, less slope times distance.  cap
-// tanh(t / cap) = cap - 2 cap / (1 + exp(2 t / cap)), off by a few 2^-24 of cap.
-__device__ __forceinline__ float ruled_score(float t, float cap, float two_over_cap_log2, float slope, float distance) {
-  if (cap > 0.f) t = fmaf(-2.f * cap, rcp(1.f + exp2f(t * two_over_cap_log2)), cap);
-  return fmaf(-slope, distance, t);
-}
-
 template <int D, bool RULES>
 __global__ void __launch_bounds__(kThreads, 1)
     paged_small_kernel(const __grid_constant__ CUtensorMap tk, const __grid_constant__ CUtensorMap tv,
@@ -163,10 +156,9 @@ __global__ void __launch_bounds__(kThreads, 1)
   float o[D / 8][4], m0, m1, l0, l1;
   int lim0 = 0, lim1 = 0, low0 = 0, low1 = 0;  // keys that rows g and g + 8 see: [low, lim)
   bool fresh = true, any = false;
-  const float scale = RULES ? 1.f : a.scale;  // of the scores as they are weighed
-  const float sl2 = scale * 1.4426950408889634f;
-  const float cap_log2 = RULES && a.cap > 0.f ? 2.885390081777927f / a.cap : 0.f;
+  const float sl2 = a.log2_unit;
   RowRules rule[2];
+  const CapConst cap(a);
   // lane's rows within the ldmatrix blocks: K (n = key, k = value), V transposed
   const int krow = ((lane >> 4) << 3) + (lane & 7), kch = (lane >> 3) & 1;
   const int vrow = (((lane >> 3) & 1) << 3) + (lane & 7), vch = lane >> 4;
@@ -237,19 +229,43 @@ __global__ void __launch_bounds__(kThreads, 1)
           mma16816(s[1], qa[kk], r[2], r[3]);
         }
         if constexpr (RULES) {
+          if (a.cap > 0.f) {
+            float top = 0.f;
+#pragma unroll
+            for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) top = fmaxf(top, fabsf(s[nt][e]));
+            const bool near = __all_sync(0xffffffffu, top * cap.k <= 0.5f);
+#pragma unroll
+            for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+              for (int e = 0; e < 4; e += 2) {
+                const f2_t v = f2(s[nt][e], s[nt][e + 1]);
+                f2_split(near ? cap.near(v) : cap.far(v), s[nt][e], s[nt][e + 1]);
+              }
+          }
+          if (a.slopes) {
+            const float far[2] = {(float)(rule[0].pos - key0), (float)(rule[1].pos - key0)};
+            const float one = a.cap > 0.f ? 1.f : a.scale * 1.4426950408889634f;
+#pragma unroll
+            for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                s[nt][e] = fmaf(-rule[e >> 1].slope, fabsf(far[e >> 1] - (float)(nt * 8 + 2 * tq + (e & 1))), s[nt][e] * one);
+          }
+          const bool drafts = a.tree && key0 + kKeys > rule[0].base;
 #pragma unroll
           for (int nt = 0; nt < 2; ++nt)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
               const RowRules& u = rule[e >> 1];
               const int key = key0 + nt * 8 + 2 * tq + (e & 1);
-              bool seen = key >= u.low && key < u.lim;
-              int far = abs(u.pos - key);
-              if (a.tree && key >= u.base && key < cc.len && u.drafted(key)) {
-                seen = true;
-                far = u.above(key);
+              if (drafts && key < cc.len && u.drafted(key)) {
+                // an ancestor: its distance in the tree for the one in the cache
+                if (a.slopes) s[nt][e] = fmaf(u.slope, fabsf((float)(u.pos - key)) - (float)u.above(key), s[nt][e]);
+              } else if (key < u.low || key >= u.lim) {
+                s[nt][e] = -INFINITY;
               }
-              s[nt][e] = seen ? ruled_score(s[nt][e] * a.scale, a.cap, cap_log2, u.slope, (float)far) : -INFINITY;
             }
         } else {
 #pragma unroll
@@ -426,7 +442,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         for (int k = 0; k < 8; ++k) acc[k] *= inv;
         *reinterpret_cast<uint4*>(a.y + (tok * a.heads + head) * D + piece * 8) = pack8(acc);
         if (a.lse && piece == 0)
-          a.lse[tok * a.heads + head] = ls == 0.f ? -INFINITY : fmaf(mx, scale, logf(ls));
+          a.lse[tok * a.heads + head] = ls == 0.f ? -INFINITY : fmaf(mx, a.unit, logf(ls));
       }
       __syncthreads();  // the free stages may be filled, s_m, s_l and s_at written again
       fresh = true;

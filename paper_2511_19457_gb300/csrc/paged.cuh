@@ -299,12 +299,49 @@ __device__ __forceinline__ PagedShares shares_of(const PagedCursor<Cut>& c, unsi
 // (its first item's end) and one that another ends (its last item's beginning).
 __device__ __forceinline__ unsigned part_slot(unsigned c, bool begins) { return 2u * c + (begins ? 1u : 0u); }
 
-// 1 / x, to 2^-23
-__device__ __forceinline__ float rcp(float x) {
+// 2^x; results below the normal range are zero
+__device__ __forceinline__ float ex2_ftz(float x) {
   float y;
-  asm("rcp.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
+// 1 / x, to 2^-23
+__device__ __forceinline__ float rcp_ftz(float x) {
+  float y;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+// Scores under a cap or with a bias are weighed as powers of 2: log2(e) (cap tanh(scale q k /
+// cap) - slope distance).  Where |t| <= 1/2, as it mostly is, tanh(t) = t p(t^2), p of
+// four coefficients fitted to the least error (1.3e-7), on packed pairs; else 1 - 2 / (1 +
+// exp(2 t)), off by a few 2^-24.
+struct CapConst {
+  float k, e, top;  // t = k q k, exp(2 t) = 2^(e q k), cap log2(e)
+  float p[4];
+  __device__ __forceinline__ explicit CapConst(const PagedArgs& a) {
+    k = a.cap > 0.f ? a.scale / a.cap : 0.f;
+    e = k * 2.885390081777927f;
+    top = a.cap * 1.4426950408889634f;
+    p[0] = 0.9999976761177359f * top;
+    p[1] = -0.33320654956697676f * top;
+    p[2] = 0.13145143396128597f * top;
+    p[3] = -0.04337242821643758f * top;
+  }
+  __device__ __forceinline__ f2_t near(f2_t s) const {
+    const f2_t t = fmul2(s, f2(k, k)), w = fmul2(t, t);
+    f2_t q = ffma2(w, f2(p[3], p[3]), f2(p[2], p[2]));
+    q = ffma2(w, q, f2(p[1], p[1]));
+    q = ffma2(w, q, f2(p[0], p[0]));
+    return fmul2(t, q);
+  }
+  __device__ __forceinline__ f2_t far(f2_t s) const {
+    float x, y;
+    f2_split(fmul2(s, f2(e, e)), x, y);
+    f2_split(fadd2(f2(ex2_ftz(x), ex2_ftz(y)), f2(1.f, 1.f)), x, y);
+    return ffma2(f2(rcp_ftz(x), rcp_ftz(y)), f2(-2.f * top, -2.f * top), f2(top, top));
+  }
+};
 
 // What a row sees and how its scores are changed, under score rules.
 struct RowRules {
@@ -312,7 +349,7 @@ struct RowRules {
   int low, lim;             // keys [low, lim) are seen
   int base;                 // and of the drafted keys from `base` on those in `tree`
   unsigned long long tree;
-  float slope;
+  float slope;              // times log2(e)
 
   // of token `tok` of a sequence, query head `head`
   __device__ __forceinline__ void load(const PagedArgs& a, int q0, int n, int len, int prefix, int tok, int head) {
@@ -331,7 +368,7 @@ struct RowRules {
         for (int i = deep - a.window; i > 0; --i) tree &= tree - 1ull;
     }
     low = first_seen(a, pos);
-    slope = a.slopes ? a.slopes[head] : 0.f;
+    slope = a.slopes ? a.slopes[head] * 1.4426950408889634f : 0.f;
   }
   // no row: sees what it likes, for its results go nowhere
   __device__ __forceinline__ void none() {

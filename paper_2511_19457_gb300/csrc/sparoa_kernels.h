@@ -289,6 +289,8 @@ struct PagedArgs {
   uint32_t* err = nullptr;
   long long wait_limit = 0;
   int fault = 0;               // error-path tests: 1 withholds the chunk kernel's signals of its scores
+  // what a score as it is weighed is worth: its weight is 2^(log2_unit s) = exp(unit s)
+  float unit = 1.f, log2_unit = 0.f;
   // score rules
   int ruled = 0;
   float cap = 0.f;                   // above 0: scores s become cap tanh(s / cap)
