@@ -1606,6 +1606,13 @@ sparoa_status attend(sparoa_ctx* ctx, const void* q, int64_t ld_q, int64_t T, in
     if (rules) {
       a.ruled = 1;
       a.cap = rules->cap;
+      a.score_log2 = scale * 1.4426950408889634f;
+      if (rules->cap > 0.f) {
+        // tanh(t) = t p(t^2) for |t| <= 1/2, four coefficients fitted to the least error (1.3e-7)
+        const double c[4] = {0.9999976761177359, -0.33320654956697676, 0.13145143396128597, -0.04337242821643758};
+        const double k = (double)scale / rules->cap;
+        for (int i = 0; i < 4; ++i) a.cap_near[i] = (float)(c[i] * std::pow(k, 2 * i) * scale * 1.4426950408889634);
+      }
       if (rules->cap > 0.f || rules->slopes) {  // (changed scores are powers of 2: paged.cuh)
         a.unit = 0.6931471805599453f;
         a.log2_unit = 1.f;

@@ -53,6 +53,10 @@ constexpr int kMmaWarp = 8, kLoadWarp = 9, kItemWarp = 10, kHelpWarp = 11;
 constexpr int kThreads = 384;
 constexpr int kItems = 4;      // items that the item warp is ahead, at most
 constexpr float kSlackLog2 = 8.f;
+// Under a cap, weights of scores that are small beside it lie within 2^-(1.5 cap log2(e)) of any
+// reference: normal numbers for caps up to this one.  With a bias, units whose scores are all this
+// far below their rows' references weigh nothing: zero in bf16, and far below the sums.
+constexpr float kDirectCap = 55.f, kGoneLog2 = 160.f;
 constexpr int kOutBytes = 32 * 64;  // 32 rows of 32 values
 
 // Steps of about 0.3 us, fitted to the CTAs' times as they were before weights below the normal
@@ -60,14 +64,14 @@ constexpr int kOutBytes = 32 * 64;  // 32 rows of 32 values
 // tiles 1.5, an item's beginning and end 2.7 (7 and 12 steps were each slower on some of a
 // prompt, mixed chunks, drafts and windows).  A join is 4 us, but items left whole so that
 // there is none keep some CTAs twice as long: 4 x 1000 tokens, window 1024, 23 -> 37 us.
-template <bool RULES>
+template <int WALK>
 struct ChunkCut {
-  static constexpr bool RULED = RULES;
+  static constexpr bool RULED = WALK != kPlainWalk, REVERSED = WALK == kReversedWalk;
   static constexpr int ROWS = kRows, EXTRA = 9, MIN_SHARE = 16, WHOLE_SHARE = 0, WHOLE_MORE = 0;
   static __device__ __forceinline__ int weight(int rows) { return rows > kTileRows ? 5 : 4; }
 };
-template <bool RULES>
-using Cursor = PagedCursor<ChunkCut<RULES>>;
+template <int WALK>
+using Cursor = PagedCursor<ChunkCut<WALK>>;
 
 template <int D>
 struct Cfg {
@@ -148,9 +152,9 @@ struct Bars {
 };
 
 // What the roles of a CTA share.
-template <bool RULES>
+template <int WALK>
 struct Shared {
-  using Cursor = sparoa::Cursor<RULES>;
+  using Cursor = sparoa::Cursor<WALK>;
   PagedPlan<kSoftWarps * kOutBytes> plan;  // scratch: each softmax warp's block of the result on its way out
   Bars bars;
   Cursor start;
@@ -160,11 +164,11 @@ struct Shared {
   int abort;
 };
 
-template <bool RULES>
+template <int WALK>
 struct Role {
-  using Cursor = sparoa::Cursor<RULES>;
+  using Cursor = sparoa::Cursor<WALK>;
   const PagedArgs& a;
-  Shared<RULES>& sh;
+  Shared<WALK>& sh;
   uint32_t sq, ring;   // Q tiles, K and V stages
   long long limit;
 
@@ -190,14 +194,14 @@ __host__ __device__ __forceinline__ bool boxes_of_q(int group) { return kTileRow
 // the help of one more warp where tiles do not begin and end with a token.  One warp that
 // does nothing else: in the softmax warps the same took 4000 cycles at every item, mostly
 // for its instructions, which the loops over units drive out of the caches.
-template <int D, bool RULES>
-__device__ __forceinline__ void item_role(const Role<RULES>& r, const CUtensorMap* tq) {
+template <int D, int WALK>
+__device__ __forceinline__ void item_role(const Role<WALK>& r, const CUtensorMap* tq) {
   using C = Cfg<D>;
   const PagedArgs& a = r.a;
   Bars& bars = r.sh.bars;
   const int lane = threadIdx.x & 31;
   const bool boxes = boxes_of_q(a.group), leads = (threadIdx.x >> 5) == kItemWarp;
-  Cursor<RULES> c = r.sh.start;
+  Cursor<WALK> c = r.sh.start;
   unsigned used[2] = {0, 0};  // items of a tile
   bool ok = true;
   for (unsigned n = 0;; ++n) {
@@ -252,18 +256,18 @@ __device__ __forceinline__ void item_role(const Role<RULES>& r, const CUtensorMa
 }
 
 // K and V of every unit: K0 V0 K1 V1 ...
-template <int D, bool RULES>
-__device__ __forceinline__ void load_role(const Role<RULES>& r, const CUtensorMap* tk, const CUtensorMap* tv) {
+template <int D, int WALK>
+__device__ __forceinline__ void load_role(const Role<WALK>& r, const CUtensorMap* tk, const CUtensorMap* tv) {
   using C = Cfg<D>;
   const PagedArgs& a = r.a;
   const int lane = threadIdx.x & 31;
-  Cursor<RULES> c = r.sh.start;
+  Cursor<WALK> c = r.sh.start;
   const int pages = kUnitKeys >> a.page_log2;        // of a whole unit
   const int pg = lane / C::kHalves, half = lane % C::kHalves;
   const uint32_t box = 128u << a.page_log2;          // bytes: page_size rows of 128
   unsigned n = 0;                                    // stages filled
   // a page before all rows' windows may be gone: a box outside of the pool reads zeros
-  auto seen = [&](const Cursor<RULES>& at, int key) { return key + (1 << a.page_log2) > at.k.lo; };
+  auto seen = [&](const Cursor<WALK>& at, int key) { return key + (1 << a.page_log2) > at.k.lo; };
   auto entry = [&]() {
     const int key = c.key0() + (pg << a.page_log2);
     return !c.done() && pg < pages && key < c.k.hi && seen(c, key) ? page_of(a, c.b, key) : -1;
@@ -298,8 +302,8 @@ __device__ __forceinline__ void load_role(const Role<RULES>& r, const CUtensorMa
 }
 
 // The MMAs.
-template <int D, bool RULES>
-__device__ __forceinline__ void mma_role(const Role<RULES>& r, uint32_t tmem) {
+template <int D, int WALK>
+__device__ __forceinline__ void mma_role(const Role<WALK>& r, uint32_t tmem) {
   using C = Cfg<D>;
   const PagedArgs& a = r.a;
   Bars& bars = r.sh.bars;
@@ -358,14 +362,14 @@ __device__ __forceinline__ void mma_role(const Role<RULES>& r, uint32_t tmem) {
     __syncwarp();
   };
   for (unsigned n = 0; ok; ++n) {
-    const Cursor<RULES>* item = r.item(n);
+    const Cursor<WALK>* item = r.item(n);
     if (!item || item->done()) break;
-    const int count = item->end - item->first, first_key = item->key0(), hi = item->k.hi, len = item->len;
+    const int count = item->end - item->first, first_key = item->key0(), step = Cursor<WALK>::kStep, hi = item->k.hi, len = item->len;
     const bool two = r.rows(*item) > kTileRows;
     r.item_done(n);
     // k-steps of unit j, whose values are in stage i
     auto steps_of = [&](int j, unsigned i) {
-      const int key0 = first_key + j * kUnitKeys, steps = (max(0, min(hi, key0 + kUnitKeys) - key0) + 15) >> 4;
+      const int key0 = first_key + j * step, steps = (max(0, min(hi, key0 + kUnitKeys) - key0) + 15) >> 4;
       if (key0 + steps * 16 > len) {
         // values past the sequence's end may be anything, and 0 * NaN is NaN: zero them
         const int from = max(0, len - key0), nz = steps * 16 - from;
@@ -441,76 +445,246 @@ __device__ __forceinline__ void mma_role(const Role<RULES>& r, uint32_t tmem) {
   }
 }
 
-// A row's 128 scores of keys from key0 on, under its rules (in a tree the distance of the
-// drafted keys is put right later).
+// A row's 128 scores of keys from key0 on: their largest in each 32 (several maxima side by
+// side: one chain of 64 steps is as long as all of the row's exponentials).
+__device__ __forceinline__ void maxima(const uint32_t (&s)[4][32], float (&mx)[4]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    mx[i] = __uint_as_float(s[i][0]);
+#pragma unroll
+    for (int k = 1; k < 31; k += 2) mx[i] = fmaxf(mx[i], fmaxf(__uint_as_float(s[i][k]), __uint_as_float(s[i][k + 1])));
+    mx[i] = fmaxf(mx[i], __uint_as_float(s[i][31]));
+  }
+}
+__device__ __forceinline__ float largest(const float (&mx)[4]) { return fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])); }
+
+__device__ __forceinline__ f2_t pair_at(const uint32_t (&s)[32], int k) { return f2(__uint_as_float(s[k]), __uint_as_float(s[k + 1])); }
+__device__ __forceinline__ void put_pair(uint32_t (&s)[32], int k, f2_t v) {
+  float x, y;
+  f2_split(v, x, y);
+  s[k] = __float_as_uint(x);
+  s[k + 1] = __float_as_uint(y);
+}
+
+// 32 scores less slope times distance; the first key's distance is `far`.
+__device__ __forceinline__ void bias_scores(const RowRules& u, uint32_t (&s)[32], float far, float one) {
+#pragma unroll
+  for (int k = 0; k < 32; ++k) s[k] = __float_as_uint(fmaf(-u.slope, fabsf(far - (float)k), __uint_as_float(s[k]) * one));
+}
+
+// -infinity for what the row does not see of 32 keys; with a bias in a tree, an ancestor's
+// distance there for the one in the cache.
+template <int RULES>
+__device__ __forceinline__ void mask_scores(const PagedArgs& a, const RowRules& u, uint32_t (&s)[32], int key0) {
+  const uint32_t w = u.template seen32<(RULES & kTree) != 0>(key0);
+  if ((RULES & kTree) && (RULES & kBias) && a.slopes && key0 + 32 > u.base) {
+#pragma unroll
+    for (int k = 0; k < 32; ++k)
+      if (key0 + k >= u.base && (w >> k & 1u))
+        s[k] = __float_as_uint(fmaf(u.slope, fabsf((float)(u.pos - key0 - k)) - (float)u.above(key0 + k), __uint_as_float(s[k])));
+  }
+#pragma unroll
+  for (int k = 0; k < 32; ++k)
+    if (!(w & (1u << k))) s[k] = 0xFF800000u;
+}
+
+template <int RULES>
+__device__ __forceinline__ void mask_unit(const PagedArgs& a, const RowRules& u, uint32_t (&s)[4][32], int key0) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) mask_scores<RULES>(a, u, s[i], key0 + i * 32);
+}
+
+// A unit's scores under their row's cap and bias.
+template <int RULES>
 __device__ __forceinline__ void rule_scores(const PagedArgs& a, const RowRules& u, uint32_t (&s)[4][32], int key0) {
-  auto pair = [&](int i, int k) { return f2(__uint_as_float(s[i][k]), __uint_as_float(s[i][k + 1])); };
-  auto put = [&](int i, int k, f2_t v) {
-    float x, y;
-    f2_split(v, x, y);
-    s[i][k] = __float_as_uint(x);
-    s[i][k + 1] = __float_as_uint(y);
-  };
-  if (a.cap > 0.f) {
-    const CapConst cap(a);
-    float top[4];
+  const bool caps = (RULES & kCap) && (!(RULES & kTree) || a.cap > 0.f);
+  if (caps) {
+    float size = 0.f;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      top[i] = fabsf(__uint_as_float(s[i][0]));
+    for (int i = 0; i < 4; ++i)
 #pragma unroll
-      for (int k = 1; k < 32; ++k) top[i] = fmaxf(top[i], fabsf(__uint_as_float(s[i][k])));
-    }
-    if (__all_sync(0xffffffffu, fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * cap.k <= 0.5f)) {
+      for (int k = 0; k < 32; ++k) size = fmaxf(size, fabsf(__uint_as_float(s[i][k])));
+    if (__all_sync(0xffffffffu, Capped(a).near(size))) {
 #pragma unroll
       for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int k = 0; k < 32; k += 2) put(i, k, cap.near(pair(i, k)));
+        for (int k = 0; k < 32; k += 2) put_pair(s[i], k, Capped(a).near(pair_at(s[i], k)));
     } else {
 #pragma unroll
       for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int k = 0; k < 32; k += 2) put(i, k, cap.far(pair(i, k)));
+        for (int k = 0; k < 32; k += 2) put_pair(s[i], k, Capped(a).far(pair_at(s[i], k)));
     }
   }
-  if (a.slopes) {
-    const float far = (float)(u.pos - key0), one = a.cap > 0.f ? 1.f : a.scale * 1.4426950408889634f;
-    if (a.causal && !a.prefix) {
-      // (keys behind the token are masked: no distance is below zero)
-      const f2_t sl = f2(u.slope, u.slope), off = f2(-u.slope * far, -u.slope * far), o2 = f2(one, one);
+  if ((RULES & kBias) && (!(RULES & kTree) || a.slopes)) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < 4; ++i) bias_scores(u, s[i], (float)(u.pos - key0 - i * 32), caps ? 1.f : a.score_log2);
+  }
+}
+
+// The weights 2^(2 (sc s + off)) of a unit's scores, to the columns of S that hold P; their
+// sums.  TWO_PARTS: two bf16 parts each.
+template <bool TWO_PARTS>
+__device__ __forceinline__ void weigh(uint32_t (&s)[4][32], uint32_t ts, f2_t sc, f2_t off, f2_t (&sum)[4]) {
+  float x, y;
 #pragma unroll
-        for (int k = 0; k < 32; k += 2)
-          put(i, k, ffma2(pair(i, k), o2, ffma2(f2((float)(i * 32 + k), (float)(i * 32 + k + 1)), sl, off)));
-    } else {
+  for (int i = 0; i < 4; ++i) {
+    uint32_t p[16];
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
+    for (int k = 0; k < 16; ++k) {
+      f2_split(ffma2(pair_at(s[i], 2 * k), sc, off), x, y);
+      const f2_t h = f2(ex2_ftz(x), ex2_ftz(y)), w = fmul2(h, h);
+      f2_split(w, x, y);
+      sum[k & 3] = i == 0 && k < 4 ? w : fadd2(sum[k & 3], w);
+      s[i][2 * k] = __float_as_uint(x);
+      s[i][2 * k + 1] = __float_as_uint(y);
+      asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(p[k]) : "f"(y), "f"(x));
+    }
+    tmem_st16(ts + i * 16, p);  // (columns of scores that are in registers already)
+    if constexpr (TWO_PARTS) {
 #pragma unroll
-        for (int k = 0; k < 32; ++k)
-          s[i][k] = __float_as_uint(fmaf(-u.slope, fabsf(far - (float)(i * 32 + k)), __uint_as_float(s[i][k]) * one));
+      for (int k = 0; k < 16; ++k) {
+        const float lo = __uint_as_float(s[i][2 * k]) - __uint_as_float(p[k] << 16);
+        const float up = __uint_as_float(s[i][2 * k + 1]) - __uint_as_float(p[k] & 0xFFFF0000u);
+        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(p[k]) : "f"(up), "f"(lo));
+      }
+      tmem_st16(ts + 64 + i * 16, p);
     }
   }
 }
 
-// The masks of a tree's row, and for its ancestors the distance in the tree for the one in
-// the cache that was taken away.
-__device__ __forceinline__ void drafted_scores(const RowRules& u, uint32_t (&s)[4][32], int key0, int len) {
+// A unit of two tiles under a cap or a bias: weights of one part, and their sum.  The scores are
+// walked twice, 32 at a time, read again from tensor memory: unrolled over all 128 the
+// instructions came too slowly (one of four issue slots was lost for want of them).
+//   direct   nothing is masked and the scores are small beside the cap: the first walk bounds the
+//            changed scores by the scores themselves, the second changes them on their way to
+//            their weights
+//   else     the first walk changes and masks them where they lie
+template <int RULES, typename Refer>
+__device__ __forceinline__ float changed_unit(const PagedArgs& a, const RowRules& u, uint32_t ts, int key0, bool whole, bool may_direct,
+                                              bool first, float m, const Refer& refer) {
+  const bool caps = (RULES & kCap) && (!(RULES & kTree) || a.cap > 0.f), slopes = (RULES & kBias) && (!(RULES & kTree) || a.slopes);
+  const float far = (float)(u.pos - key0);
+  float mx = -INFINITY;
+  bool near = true, direct = whole && may_direct;
+  const bool bounded = direct || (slopes && whole && a.causal && !a.prefix);  // no key is behind its token
+  uint32_t s[32];
+  if (caps || bounded) {
+    float bound = -INFINITY, size = 0.f;
+#pragma unroll 1
+    for (int i = 0; i < 4; ++i) {
+      tmem_ld32_nowait(ts + i * 32, s);
+      tmem_wait_ld32(s);
+      float t[4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
+      for (int k = 0; k < 4; ++k) {
+        auto of = [&](int at) { return caps ? fabsf(__uint_as_float(s[at])) : __uint_as_float(s[at]); };
+        t[k] = of(8 * k);
 #pragma unroll
-    for (int k = 0; k < 32; ++k) {
-      const int key = key0 + i * 32 + k;
-      if (key < len && u.drafted(key))
-        s[i][k] = __float_as_uint(fmaf(u.slope, (float)(u.pos - key - u.above(key)), __uint_as_float(s[i][k])));
-      else if (key < u.low || key >= u.lim)
-        s[i][k] = 0xFF800000u;
+        for (int e = 1; e < 7; e += 2) t[k] = fmaxf(t[k], fmaxf(of(8 * k + e), of(8 * k + e + 1)));
+        t[k] = fmaxf(t[k], of(8 * k + 7));
+      }
+      float top = largest(t);
+      size = fmaxf(size, top);
+      if (slopes) {
+        // (a slope may put the bound of 32 scores kSlackLog2 too high)
+        top = (caps ? Capped(a).near1(top) : top * a.score_log2) + u.slope * ((float)(i * 32) - far) + fmaxf(u.slope * 31.f, 0.f);
+        bound = fmaxf(bound, top);
+      }
     }
+    if (caps) near = __all_sync(0xffffffffu, Capped(a).near(size));
+    direct = direct && near;
+    mx = slopes ? bound : Capped(a).near1(size);
+    // too far away for any weight of the unit
+    if (slopes && bounded && near && !first && __all_sync(0xffffffffu, mx < m - kGoneLog2)) {
+      const uint32_t none[16] = {};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) tmem_st16(ts + i * 16, none);
+      return 0.f;
+    }
+  }
+  if (!direct) {
+    mx = -INFINITY;
+#pragma unroll 1
+    for (int i = 0; i < 4; ++i) {
+      tmem_ld32_nowait(ts + i * 32, s);
+      tmem_wait_ld32(s);
+      if (caps) {
+        if (near) {
+#pragma unroll
+          for (int k = 0; k < 32; k += 2) put_pair(s, k, Capped(a).near(pair_at(s, k)));
+        } else {
+#pragma unroll
+          for (int k = 0; k < 32; k += 2) put_pair(s, k, Capped(a).far(pair_at(s, k)));
+        }
+      }
+      if (slopes) bias_scores(u, s, far - (float)(i * 32), caps ? 1.f : a.score_log2);
+      if (!whole) mask_scores<RULES>(a, u, s, key0 + i * 32);
+      float t[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        t[k] = __uint_as_float(s[8 * k]);
+#pragma unroll
+        for (int e = 1; e < 8; ++e) t[k] = fmaxf(t[k], __uint_as_float(s[8 * k + e]));
+      }
+      mx = fmaxf(mx, largest(t));
+      uint32_t half[16];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+#pragma unroll
+        for (int k = 0; k < 16; ++k) half[k] = s[16 * h + k];
+        tmem_st16(ts + i * 32 + h * 16, half);
+      }
+    }
+    tmem_wait_st();
+  }
+  const float nz = refer(mx, first);
+  // half the changed scores less the reference, whose powers are squared (weigh); whole ones under a
+  // cap alone, whose weights are all normal numbers
+  constexpr float part = (RULES & kBias) != 0 ? 0.5f : 1.f;
+  const float sl = part * u.slope;
+  f2_t sum[4] = {f2(0.f, 0.f), f2(0.f, 0.f), f2(0.f, 0.f), f2(0.f, 0.f)};
+  float x, y;
+  auto walk = [&](auto changed) {
+#pragma unroll 1
+    for (int i = 0; i < 4; ++i) {
+      tmem_ld32_nowait(ts + i * 32, s);
+      // (the bias grows by a step from pair to pair: 15 roundings of a number that is small where it counts)
+      const float base = part * (nz - u.slope * (far - (float)(i * 32)));
+      f2_t o = (RULES & kBias) != 0 ? f2(base, base + sl) : f2(nz, nz);
+      uint32_t p[16];
+      tmem_wait_ld32(s);
+#pragma unroll
+      for (int k = 0; k < 16; ++k) {
+        const f2_t v = pair_at(s, 2 * k);
+        if constexpr (decltype(changed)::value) {
+          const f2_t f = (RULES & kCap) != 0 ? Capped(a).factor(v, part) : f2(part * a.score_log2, part * a.score_log2);
+          f2_split(ffma2(v, f, o), x, y);
+          if ((RULES & kBias) != 0) o = fadd2(o, f2(2.f * sl, 2.f * sl));
+        } else {
+          f2_split(ffma2(v, f2(0.5f, 0.5f), f2(0.5f * nz, 0.5f * nz)), x, y);
+        }
+        const f2_t h = f2(ex2_ftz(x), ex2_ftz(y)), w = decltype(changed)::value && part == 1.f ? h : fmul2(h, h);
+        f2_split(w, x, y);
+        sum[k & 3] = fadd2(sum[k & 3], w);
+        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(p[k]) : "f"(y), "f"(x));
+      }
+      tmem_st16(ts + i * 16, p);  // (columns of scores that were read already)
+    }
+  };
+  if (direct)
+    walk(BoolConst<true>());
+  else
+    walk(BoolConst<false>());
+  f2_split(fadd2(fadd2(sum[0], sum[1]), fadd2(sum[2], sum[3])), x, y);
+  return x + y;
 }
 
 // The softmax: a thread per row of a tile.
-template <int D, bool RULES>
-__device__ __forceinline__ void softmax_role(const Role<RULES>& r, uint32_t tmem) {
+template <int D, int RULES>
+__device__ __forceinline__ void softmax_role(const Role<walk_of(RULES)>& r, uint32_t tmem) {
   using C = Cfg<D>;
+  constexpr bool kChanges = (RULES & (kCap | kBias)) != 0;
   const PagedArgs& a = r.a;
   Bars& bars = r.sh.bars;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, grp = warp >> 2, row = threadIdx.x & 127;
@@ -520,9 +694,9 @@ __device__ __forceinline__ void softmax_role(const Role<RULES>& r, uint32_t tmem
   unsigned sn = 0, on = 0, joins = 0;
   bool ok = true;
   for (unsigned n = 0;; ++n) {
-    const Cursor<RULES>* item = r.item(n);
+    const Cursor<walk_of(RULES)>* item = r.item(n);
     if (!item || item->done()) break;
-    const Cursor<RULES>& c = *item;
+    const Cursor<walk_of(RULES)>& c = *item;
     const int rows = r.rows(c), count = c.end - c.first;
     const bool two = rows > kTileRows;
     // the group's rows and units: its own tile and all units, or the tile and every other unit
@@ -533,11 +707,11 @@ __device__ __forceinline__ void softmax_role(const Role<RULES>& r, uint32_t tmem
     // keys [low, lim) that the row sees; a row past the item's last one never asks for masks
     int lim = 0x7FFFFFFF, low = 0;
     RowRules rule;
-    if constexpr (RULES) {
-      rule.none();
+    rule.none();
+    if constexpr (RULES != kPlain) {
       if (live) {
         const int at = c.t * kRows + r0 + row, tok = over_group(a, at);
-        rule.load(a, c.q0, c.n, c.len, c.prefix, tok, c.h * a.group + at - tok * a.group);
+        rule.load<RULES>(a, c.q0, c.n, c.len, c.prefix, tok, c.h * a.group + at - tok * a.group);
       }
       low = rule.low;
       lim = rule.lim;
@@ -548,100 +722,113 @@ __device__ __forceinline__ void softmax_role(const Role<RULES>& r, uint32_t tmem
     }
     const int first_key = c.key0();
     float m = -INFINITY, l = 0.f;
+    // whether scores of whole units may be changed on their way to their weights.  The reference is
+    // then a bound of 32 keys' scores at a time, which a slope may put kSlackLog2 too high
+    const bool may_direct = kChanges && !(RULES & kTree) && (!(RULES & kCap) || a.cap <= kDirectCap) &&
+                            (!(RULES & kBias) || (__all_sync(0xffffffffu, fabsf(rule.slope) * 31.f <= kSlackLog2) && a.causal && !a.prefix));
     for (int j = j0; j < count; j += dj) {
-      const int key0 = first_key + j * kUnitKeys;
+      const int key0 = first_key + j * Cursor<walk_of(RULES)>::kStep;
       if (!(ok = r.wait(bars.s[grp], sn & 1u, kErrTimeoutAcc))) break;
       ++sn;
       tc_fence_after();
       if (!idle) {
-        uint32_t s[4][32];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) tmem_ld32_nowait(ts + i * 32, s[i]);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) tmem_wait_ld32(s[i]);
-        if constexpr (RULES) rule_scores(a, rule, s, key0);
-        if (!__all_sync(0xffffffffu, key0 >= low && key0 + kUnitKeys <= lim)) {
-          if (RULES && a.tree) {
-            drafted_scores(rule, s, key0, c.len);
-          } else {
-            const int from = low - key0, to_ = lim - key0;
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-              for (int k = 0; k < 32; ++k)
-                if (i * 32 + k < from || i * 32 + k >= to_) s[i][k] = 0xFF800000u;  // -infinity
-          }
-        }
-        // (several maxima and sums side by side: one chain of 64 steps each is as long as all
-        // of the row's exponentials)
-        float mx4[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          mx4[i] = __uint_as_float(s[i][0]);
-#pragma unroll
-          for (int k = 1; k < 31; k += 2)
-            mx4[i] = fmaxf(mx4[i], fmaxf(__uint_as_float(s[i][k]), __uint_as_float(s[i][k + 1])));
-          mx4[i] = fmaxf(mx4[i], __uint_as_float(s[i][31]));
-        }
-        const float mx = fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3]));
-        const bool grows = mx > m + slack;
-        if (j == j0) {
-          m = mx;
-        } else if (__any_sync(0xffffffffu, grows)) {
-          // S of this unit is complete, so the product before it is: O stands still
-          const float f = grows ? to_ref(m, mx, sl2) : 1.f;
-          if (grows) m = mx;
-          l *= f;
+        if constexpr (kChanges) {
+          const bool whole = __all_sync(0xffffffffu, key0 >= low && key0 + kUnitKeys <= lim);  // nothing is masked
+          // the reference that a unit whose largest score is mx goes by
+          auto refer = [&](float mx, bool first) {
+            const bool grows = mx > m + slack;
+            if (first) {
+              m = mx;
+            } else if (__any_sync(0xffffffffu, grows)) {
+              // S of this unit is complete, so the product before it is: O stands still
+              const float f = grows ? to_ref(m, mx, sl2) : 1.f;
+              if (grows) m = mx;
+              l *= f;
 #pragma unroll 1
-          for (int i = 0; i < D / 16; ++i) {
-            float o[16];
-            uint32_t q[16];
-            tmem_ld16(to + i * 16, o);
+              for (int i = 0; i < D / 16; ++i) {
+                float o[16];
+                uint32_t q[16];
+                tmem_ld16(to + i * 16, o);
 #pragma unroll
-            for (int k = 0; k < 16; ++k) q[k] = __float_as_uint(o[k] * f);
-            tmem_st16(to + i * 16, q);
-          }
-        }
-        const float nz = m == -INFINITY ? 0.f : -scaled_ref(m, sl2);
-        // A weight below the normal range counts where its value is large, and fp32 sums and
-        // bf16 weights hold it: 2^x is the square of 2^(x / 2), which is a normal number.  A prompt of
-        // 8191 tokens takes 397 us with such weights flushed to zero, 421 so, 477 with exp2f.
-        const f2_t sc = f2(0.5f * sl2, 0.5f * sl2), off = f2(0.5f * nz, 0.5f * nz);
-        f2_t sum[4];
-        auto weigh = [&](auto two_parts) {
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            uint32_t p[16];
-#pragma unroll
-            for (int k = 0; k < 16; ++k) {
-              float x, y;
-              f2_split(ffma2(f2(__uint_as_float(s[i][2 * k]), __uint_as_float(s[i][2 * k + 1])), sc, off), x, y);
-              const f2_t h = f2(ex2_ftz(x), ex2_ftz(y)), w = fmul2(h, h);
-              f2_split(w, x, y);
-              sum[k & 3] = i == 0 && k < 4 ? w : fadd2(sum[k & 3], w);
-              s[i][2 * k] = __float_as_uint(x);
-              s[i][2 * k + 1] = __float_as_uint(y);
-              asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(p[k]) : "f"(y), "f"(x));
-            }
-            tmem_st16(ts + i * 16, p);  // (columns of scores that are in registers already)
-            if constexpr (decltype(two_parts)::value) {
-#pragma unroll
-              for (int k = 0; k < 16; ++k) {
-                const float lo = __uint_as_float(s[i][2 * k]) - __uint_as_float(p[k] << 16);
-                const float up = __uint_as_float(s[i][2 * k + 1]) - __uint_as_float(p[k] & 0xFFFF0000u);
-                asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(p[k]) : "f"(up), "f"(lo));
+                for (int k = 0; k < 16; ++k) q[k] = __float_as_uint(o[k] * f);
+                tmem_st16(to + i * 16, q);
               }
-              tmem_st16(ts + 64 + i * 16, p);
+            }
+            return m == -INFINITY ? 0.f : -scaled_ref(m, sl2);
+          };
+          if (two) {
+            const float more = changed_unit<RULES>(a, rule, ts, key0, whole, may_direct, j == j0, m, refer);
+            l += more;  // (l may have been brought to another reference)
+          } else {
+            uint32_t s[4][32];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) tmem_ld32_nowait(ts + i * 32, s[i]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) tmem_wait_ld32(s[i]);
+            rule_scores<RULES>(a, rule, s, key0);
+            if (!whole) mask_unit<RULES>(a, rule, s, key0);
+            float mx[4];
+            maxima(s, mx);
+            const float nz = refer(largest(mx), j == j0);
+            f2_t sum[4];
+            weigh<true>(s, ts, f2(0.5f * sl2, 0.5f * sl2), f2(0.5f * nz, 0.5f * nz), sum);
+            float x, y;
+            f2_split(fadd2(fadd2(sum[0], sum[1]), fadd2(sum[2], sum[3])), x, y);
+            l += x + y;
+          }
+        } else {
+          uint32_t s[4][32];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) tmem_ld32_nowait(ts + i * 32, s[i]);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) tmem_wait_ld32(s[i]);
+          if (!__all_sync(0xffffffffu, key0 >= low && key0 + kUnitKeys <= lim)) {
+            if constexpr ((RULES & kTree) != 0) {
+              mask_unit<RULES>(a, rule, s, key0);
+            } else {
+              const int from = low - key0, to_ = lim - key0;
+#pragma unroll
+              for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int k = 0; k < 32; ++k)
+                  if (i * 32 + k < from || i * 32 + k >= to_) s[i][k] = 0xFF800000u;  // -infinity
             }
           }
-        };
-        if (two)
-          weigh(BoolConst<false>());
-        else
-          weigh(BoolConst<true>());
-        float x, y;
-        f2_split(fadd2(fadd2(sum[0], sum[1]), fadd2(sum[2], sum[3])), x, y);
-        l += x + y;
+          float mx4[4];
+          maxima(s, mx4);
+          const float mx = largest(mx4);
+          const bool grows = mx > m + slack;
+          if (j == j0) {
+            m = mx;
+          } else if (__any_sync(0xffffffffu, grows)) {
+            // S of this unit is complete, so the product before it is: O stands still
+            const float f = grows ? to_ref(m, mx, sl2) : 1.f;
+            if (grows) m = mx;
+            l *= f;
+#pragma unroll 1
+            for (int i = 0; i < D / 16; ++i) {
+              float o[16];
+              uint32_t q[16];
+              tmem_ld16(to + i * 16, o);
+#pragma unroll
+              for (int k = 0; k < 16; ++k) q[k] = __float_as_uint(o[k] * f);
+              tmem_st16(to + i * 16, q);
+            }
+          }
+          const float nz = m == -INFINITY ? 0.f : -scaled_ref(m, sl2);
+          // A weight below the normal range counts where its value is large, and fp32 sums and
+          // bf16 weights hold it: 2^x is the square of 2^(x / 2), which is a normal number.  A prompt of
+          // 8191 tokens takes 397 us with such weights flushed to zero, 421 so, 477 with exp2f.
+          const f2_t sc = f2(0.5f * sl2, 0.5f * sl2), off = f2(0.5f * nz, 0.5f * nz);
+          f2_t sum[4];
+          if (two)
+            weigh<false>(s, ts, sc, off, sum);
+          else
+            weigh<true>(s, ts, sc, off, sum);
+          float x, y;
+          f2_split(fadd2(fadd2(sum[0], sum[1]), fadd2(sum[2], sum[3])), x, y);
+          l += x + y;
+        }
         tmem_wait_st();
       }
       tc_fence_before();
@@ -747,13 +934,14 @@ __device__ __forceinline__ void softmax_role(const Role<RULES>& r, uint32_t tmem
   }
 }
 
-template <int D, bool RULES>
+template <int D, int RULES>
 __global__ void __launch_bounds__(kThreads, 1)
     paged_chunk_kernel(const __grid_constant__ CUtensorMap tk, const __grid_constant__ CUtensorMap tv,
                        const __grid_constant__ CUtensorMap tq, const __grid_constant__ PagedArgs a) {
   using C = Cfg<D>;
+  constexpr int WALK = walk_of(RULES);
   extern __shared__ uint8_t smem_raw[];
-  __shared__ __align__(8) Shared<RULES> sh;
+  __shared__ __align__(8) Shared<WALK> sh;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   if (threadIdx.x == 0) {
     Bars& bars = sh.bars;
@@ -787,14 +975,14 @@ __global__ void __launch_bounds__(kThreads, 1)
   tc_fence_after();
   pdl_wait();
   pdl_trigger();
-  make_plan<ChunkCut<RULES>>(a, sh.plan);
+  make_plan<ChunkCut<WALK>>(a, sh.plan);
   const unsigned long long total = sh.plan.total;
-  const unsigned ctas = cut_ctas<ChunkCut<RULES>>(total);
+  const unsigned ctas = cut_ctas<ChunkCut<WALK>>(total);
   const bool works = blockIdx.x < ctas;
   const unsigned long long u0 = works ? cut_start(total, ctas, blockIdx.x) : 0ull;
   const unsigned long long u1 = works ? cut_start(total, ctas, blockIdx.x + 1) : 0ull;
   if (warp == 0 && works) {
-    Cursor<RULES> c;
+    Cursor<WALK> c;
     c.seek(a, sh.plan, ctas, u0, (int)(u1 - u0));
     if (lane == 0) sh.start = c;
   }
@@ -803,7 +991,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     // an item cut at this CTA's start is joined later; the first of its cuts speaks for it
     JoinItem j{};
     if (works && !sh.start.done() && sh.start.first > 0) {
-      const Cursor<RULES>& c = sh.start;
+      const Cursor<WALK>& c = sh.start;
       const PagedShares s = shares_of(c, total, ctas, u1);
       j.c0 = (int)s.c0;
       j.c1 = (int)s.c1;
@@ -816,15 +1004,15 @@ __global__ void __launch_bounds__(kThreads, 1)
     reinterpret_cast<JoinItem*>(a.ws + (size_t)2 * gridDim.x * C::kSlotFloats)[blockIdx.x] = j;
   }
   const uint32_t sq = (smem_u32(smem_raw) + 1023u) & ~1023u;
-  const Role<RULES> r{a, sh, sq, sq + 2 * C::kTile, a.wait_limit ? a.wait_limit : kWaitLimitCycles};
+  const Role<WALK> r{a, sh, sq, sq + 2 * C::kTile, a.wait_limit ? a.wait_limit : kWaitLimitCycles};
   if (warp < kSoftWarps) {
     reg_inc<kManyRegs>();
     if (works) softmax_role<D, RULES>(r, sh.tmem);
   } else {
     reg_dec<kFewRegs>();
-    if (works && warp == kMmaWarp) mma_role<D, RULES>(r, sh.tmem);
-    if (works && warp == kLoadWarp) load_role<D, RULES>(r, &tk, &tv);
-    if (works && (warp == kItemWarp || (warp == kHelpWarp && !boxes_of_q(a.group)))) item_role<D, RULES>(r, &tq);
+    if (works && warp == kMmaWarp) mma_role<D, WALK>(r, sh.tmem);
+    if (works && warp == kLoadWarp) load_role<D, WALK>(r, &tk, &tv);
+    if (works && (warp == kItemWarp || (warp == kHelpWarp && !boxes_of_q(a.group)))) item_role<D, WALK>(r, &tq);
   }
   tc_fence_before();
   __syncthreads();
@@ -896,7 +1084,7 @@ int grid_of() {
   return sms < kCtas ? sms : kCtas;
 }
 
-template <int D, bool RULES>
+template <int D, int RULES>
 cudaError_t launch_chunk(const PagedArgs& a, cudaStream_t s) {
   CUtensorMap tk, tv, tq;
   const uint64_t rows = (uint64_t)a.pages * a.kv_heads << a.page_log2;
@@ -914,6 +1102,19 @@ cudaError_t launch_chunk(const PagedArgs& a, cudaStream_t s) {
   return launch_kernel(paged_join_kernel<D>, dim3(grid, kRows / 32), dim3(4 * D), 0, s, a, grid);
 }
 
+template <int D>
+cudaError_t launch_by_rules(const PagedArgs& a, cudaStream_t s) {
+  switch (rules_of(a)) {
+    case kPlain: return launch_chunk<D, kPlain>(a, s);
+    case kRuled: return launch_chunk<D, kRuled>(a, s);
+    case kRuled | kCap: return launch_chunk<D, kRuled | kCap>(a, s);
+    case kRuled | kBias: return launch_chunk<D, kRuled | kBias>(a, s);
+    case kRuled | kCap | kBias: return launch_chunk<D, kRuled | kCap | kBias>(a, s);
+    case kRuled | kTree: return launch_chunk<D, kRuled | kTree>(a, s);
+  }
+  return launch_chunk<D, kRuled | kCap | kBias | kTree>(a, s);
+}
+
 }  // namespace
 
 size_t paged_chunk_ws_bytes() {
@@ -921,8 +1122,7 @@ size_t paged_chunk_ws_bytes() {
 }
 
 cudaError_t launch_paged_chunk(const PagedArgs& a, cudaStream_t s) {
-  if (a.ruled) return a.D == 128 ? launch_chunk<128, true>(a, s) : launch_chunk<64, true>(a, s);
-  return a.D == 128 ? launch_chunk<128, false>(a, s) : launch_chunk<64, false>(a, s);
+  return a.D == 128 ? launch_by_rules<128>(a, s) : launch_by_rules<64>(a, s);
 }
 
 }  // namespace sparoa

@@ -28,9 +28,9 @@ constexpr int kKeys = 16;     // a warp's keys of a unit
 // An item's beginning and end take as long as one unit to three (64 contexts of 500 to
 // 16000 tokens: 188 us with 1 and with 3, 185 with 2); joining parts of an item as eight
 // units of a CTA that has few.
-template <bool RULES>
+template <int WALK>
 struct SmallCut {
-  static constexpr bool RULED = RULES;
+  static constexpr bool RULED = WALK != kPlainWalk, REVERSED = WALK == kReversedWalk;
   static constexpr int ROWS = kRows, EXTRA = 2, MIN_SHARE = 2, WHOLE_SHARE = 8, WHOLE_MORE = 8;
   static __device__ __forceinline__ int weight(int) { return 1; }
 };
@@ -78,12 +78,12 @@ __device__ __forceinline__ uint32_t rest2(uint32_t hi, float lo, float up) {
 template <int D>
 constexpr int kSlotFloats = kRows * (D + 2);
 
-template <int D, bool RULES>
+template <int D, int RULES>
 __global__ void __launch_bounds__(kThreads, 1)
     paged_small_kernel(const __grid_constant__ CUtensorMap tk, const __grid_constant__ CUtensorMap tv,
                        const __grid_constant__ PagedArgs a) {
   using C = Cfg<D>;
-  using Cut = SmallCut<RULES>;
+  using Cut = SmallCut<walk_of(RULES)>;
   using Cursor = PagedCursor<Cut>;
   constexpr int S = C::kStages;
   extern __shared__ uint8_t smem_raw[];
@@ -158,7 +158,6 @@ __global__ void __launch_bounds__(kThreads, 1)
   bool fresh = true, any = false;
   const float sl2 = a.log2_unit;
   RowRules rule[2];
-  const CapConst cap(a);
   // lane's rows within the ldmatrix blocks: K (n = key, k = value), V transposed
   const int krow = ((lane >> 4) << 3) + (lane & 7), kch = (lane >> 3) & 1;
   const int vrow = (((lane >> 3) & 1) << 3) + (lane & 7), vch = lane >> 4;
@@ -181,13 +180,13 @@ __global__ void __launch_bounds__(kThreads, 1)
           const int row = cc.t * kRows + g + 8 * i, tok = over_group(a, row), head = cc.h * a.group + row - tok * a.group;
           const int pos = cc.len - cc.n + tok;
           p[i] = a.q + (int64_t)(cc.q0 + tok) * a.ld_q + head * D;
-          if constexpr (RULES) {
-            rule[i].load(a, cc.q0, cc.n, cc.len, cc.prefix, tok, head);
+          if constexpr (RULES != kPlain) {
+            rule[i].load<RULES>(a, cc.q0, cc.n, cc.len, cc.prefix, tok, head);
           } else {
             lim[i] = a.causal ? min(cc.len, pos + 1) : cc.len;
             low[i] = first_seen(a, pos);
           }
-        } else if constexpr (RULES) {
+        } else if constexpr (RULES != kPlain) {
           rule[i].none();
         }
       }
@@ -228,45 +227,53 @@ __global__ void __launch_bounds__(kThreads, 1)
           mma16816(s[0], qa[kk], r[0], r[1]);
           mma16816(s[1], qa[kk], r[2], r[3]);
         }
-        if constexpr (RULES) {
-          if (a.cap > 0.f) {
+        if constexpr (RULES != kPlain) {
+          // (kernels for trees are for all that they may come with)
+          if ((RULES & kCap) && (!(RULES & kTree) || a.cap > 0.f)) {
+            const Capped cap(a);
             float top = 0.f;
 #pragma unroll
             for (int nt = 0; nt < 2; ++nt)
 #pragma unroll
               for (int e = 0; e < 4; ++e) top = fmaxf(top, fabsf(s[nt][e]));
-            const bool near = __all_sync(0xffffffffu, top * cap.k <= 0.5f);
+            if (__all_sync(0xffffffffu, cap.near(top))) {
 #pragma unroll
-            for (int nt = 0; nt < 2; ++nt)
+              for (int nt = 0; nt < 2; ++nt)
 #pragma unroll
-              for (int e = 0; e < 4; e += 2) {
-                const f2_t v = f2(s[nt][e], s[nt][e + 1]);
-                f2_split(near ? cap.near(v) : cap.far(v), s[nt][e], s[nt][e + 1]);
-              }
+                for (int e = 0; e < 4; e += 2) f2_split(cap.near(f2(s[nt][e], s[nt][e + 1])), s[nt][e], s[nt][e + 1]);
+            } else {
+#pragma unroll
+              for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+                for (int e = 0; e < 4; e += 2) f2_split(cap.far(f2(s[nt][e], s[nt][e + 1])), s[nt][e], s[nt][e + 1]);
+            }
           }
-          if (a.slopes) {
-            const float far[2] = {(float)(rule[0].pos - key0), (float)(rule[1].pos - key0)};
-            const float one = a.cap > 0.f ? 1.f : a.scale * 1.4426950408889634f;
+          if ((RULES & kBias) && (!(RULES & kTree) || a.slopes)) {
+            const float far[2] = {(float)(rule[0].pos - key0), (float)(rule[1].pos - key0)}, one = a.cap > 0.f ? 1.f : a.score_log2;
 #pragma unroll
             for (int nt = 0; nt < 2; ++nt)
 #pragma unroll
               for (int e = 0; e < 4; ++e)
                 s[nt][e] = fmaf(-rule[e >> 1].slope, fabsf(far[e >> 1] - (float)(nt * 8 + 2 * tq + (e & 1))), s[nt][e] * one);
           }
-          const bool drafts = a.tree && key0 + kKeys > rule[0].base;
+          const uint32_t seen[2] = {rule[0].seen32<(RULES & kTree) != 0>(key0), rule[1].seen32<(RULES & kTree) != 0>(key0)};
+          if ((RULES & kBias) && (RULES & kTree) && a.slopes && key0 + kKeys > rule[0].base) {
+            // ancestors: their distance in the tree for the one in the cache
+#pragma unroll
+            for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                const RowRules& u = rule[e >> 1];
+                const int key = key0 + nt * 8 + 2 * tq + (e & 1);
+                if (key >= u.base && key < cc.len)
+                  s[nt][e] = fmaf(u.slope, fabsf((float)(u.pos - key)) - (float)u.above(key), s[nt][e]);
+              }
+          }
 #pragma unroll
           for (int nt = 0; nt < 2; ++nt)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const RowRules& u = rule[e >> 1];
-              const int key = key0 + nt * 8 + 2 * tq + (e & 1);
-              if (drafts && key < cc.len && u.drafted(key)) {
-                // an ancestor: its distance in the tree for the one in the cache
-                if (a.slopes) s[nt][e] = fmaf(u.slope, fabsf((float)(u.pos - key)) - (float)u.above(key), s[nt][e]);
-              } else if (key < u.low || key >= u.lim) {
-                s[nt][e] = -INFINITY;
-              }
-            }
+            for (int e = 0; e < 4; ++e)
+              if (!(seen[e >> 1] >> (nt * 8 + 2 * tq + (e & 1)) & 1u)) s[nt][e] = -INFINITY;
         } else {
 #pragma unroll
           for (int nt = 0; nt < 2; ++nt) {
@@ -461,7 +468,7 @@ int grid_of() {
 }
 size_t small_ws_bytes() { return (size_t)2 * kPagedCounters * kSlotFloats<128> * sizeof(float); }
 
-template <int D, bool RULES>
+template <int D, int RULES>
 cudaError_t launch_small(const PagedArgs& a, cudaStream_t s) {
   CUtensorMap tk, tv;
   const uint64_t rows = (uint64_t)a.pages * a.kv_heads << a.page_log2;
@@ -472,7 +479,27 @@ cudaError_t launch_small(const PagedArgs& a, cudaStream_t s) {
   return launch_kernel(paged_small_kernel<D, RULES>, dim3(grid_of()), dim3(kThreads), Cfg<D>::kSmem, s, tk, tv, a);
 }
 
+template <int D>
+cudaError_t launch_by_rules(const PagedArgs& a, cudaStream_t s) {
+  switch (rules_of(a)) {
+    case kPlain: return launch_small<D, kPlain>(a, s);
+    case kRuled: return launch_small<D, kRuled>(a, s);
+    case kRuled | kCap: return launch_small<D, kRuled | kCap>(a, s);
+    case kRuled | kBias: return launch_small<D, kRuled | kBias>(a, s);
+    case kRuled | kCap | kBias: return launch_small<D, kRuled | kCap | kBias>(a, s);
+    case kRuled | kTree: return launch_small<D, kRuled | kTree>(a, s);
+  }
+  return launch_small<D, kRuled | kCap | kBias | kTree>(a, s);
+}
+
 }  // namespace
+
+int rules_of(const PagedArgs& a) {
+  if (!a.ruled) return kPlain;
+  const int changes = (a.cap > 0.f ? kCap : 0) | (a.slopes ? kBias : 0);
+  if (!a.tree) return kRuled | changes;
+  return kRuled | kTree | (changes ? kCap | kBias : 0);
+}
 
 size_t paged_ws_bytes() {
   const size_t small = small_ws_bytes(), chunk = paged_chunk_ws_bytes();
@@ -482,8 +509,7 @@ size_t paged_ws_bytes(const PagedArgs& a) { return few_rows(a) ? small_ws_bytes(
 
 cudaError_t launch_paged_attention(const PagedArgs& a, cudaStream_t s) {
   if (!few_rows(a)) return launch_paged_chunk(a, s);
-  if (a.ruled) return a.D == 128 ? launch_small<128, true>(a, s) : launch_small<64, true>(a, s);
-  return a.D == 128 ? launch_small<128, false>(a, s) : launch_small<64, false>(a, s);
+  return a.D == 128 ? launch_by_rules<128>(a, s) : launch_by_rules<64>(a, s);
 }
 
 }  // namespace sparoa

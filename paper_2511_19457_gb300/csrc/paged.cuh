@@ -158,8 +158,10 @@ struct PagedCursor : CursorPrefix<Cut::RULED> {
   int first, end;    // the share's units of the item
   int blk;           // unit, first to end - 1; at `end`: nothing left
 
+  static constexpr int kStep = Cut::REVERSED ? -kUnitKeys : kUnitKeys;  // keys from unit to unit
   __device__ __forceinline__ bool done() const { return blk >= end; }
-  __device__ __forceinline__ int key0() const { return (k.blk0 + blk) * kUnitKeys; }
+  // (with a bias the nearest keys come first, so that a row's reference is right from the start)
+  __device__ __forceinline__ int key0() const { return (k.blk0 + (Cut::REVERSED ? first + end - 1 - blk : blk)) * kUnitKeys; }
   // whether other CTAs have units of the item
   __device__ __forceinline__ bool cut() const { return first > 0 || end < k.units; }
 
@@ -312,34 +314,40 @@ __device__ __forceinline__ float rcp_ftz(float x) {
   return y;
 }
 
+// Rules that a kernel is made for: none, or kRuled (prefixes) and what else changes scores; a
+// tree alone, or with any of the others (which its kernel looks up).
+enum Rules : int { kPlain = 0, kCap = 1, kBias = 2, kTree = 4, kRuled = 8 };
+int rules_of(const PagedArgs& a);
+// what the walk over the work has to know of them
+enum Walk : int { kPlainWalk = 0, kRuledWalk = 1, kReversedWalk = 2 };
+__host__ __device__ constexpr int walk_of(int rules) { return rules == kPlain ? kPlainWalk : rules & kBias ? kReversedWalk : kRuledWalk; }
+
 // Scores under a cap or with a bias are weighed as powers of 2: log2(e) (cap tanh(scale q k /
-// cap) - slope distance).  Where |t| <= 1/2, as it mostly is, tanh(t) = t p(t^2), p of
-// four coefficients fitted to the least error (1.3e-7), on packed pairs; else 1 - 2 / (1 +
-// exp(2 t)), off by a few 2^-24.
-struct CapConst {
-  float k, e, top;  // t = k q k, exp(2 t) = 2^(e q k), cap log2(e)
-  float p[4];
-  __device__ __forceinline__ explicit CapConst(const PagedArgs& a) {
-    k = a.cap > 0.f ? a.scale / a.cap : 0.f;
-    e = k * 2.885390081777927f;
-    top = a.cap * 1.4426950408889634f;
-    p[0] = 0.9999976761177359f * top;
-    p[1] = -0.33320654956697676f * top;
-    p[2] = 0.13145143396128597f * top;
-    p[3] = -0.04337242821643758f * top;
+// cap) - slope distance).  Where |t| = |scale q k / cap| <= 1/2, as it mostly is, tanh(t) =
+// t p(t^2), on packed pairs; else 1 - 2 / (1 + exp(2 t)), off by a few 2^-24.
+struct Capped {
+  const PagedArgs& a;
+  float k;
+  __device__ __forceinline__ explicit Capped(const PagedArgs& args) : a(args), k(args.scale / args.cap) {}
+  // (p's coefficients hold powers of k: none of them counts and is flushed for such q k)
+  __device__ __forceinline__ bool near(float top) const { return top * k <= 0.5f && top <= 1024.f; }
+  __device__ __forceinline__ f2_t factor(f2_t s, float part) const {
+    const float c0 = a.cap_near[0] * part, c1 = a.cap_near[1] * part, c2 = a.cap_near[2] * part, c3 = a.cap_near[3] * part;
+    const f2_t w = fmul2(s, s);
+    return ffma2(w, ffma2(w, ffma2(w, f2(c3, c3), f2(c2, c2)), f2(c1, c1)), f2(c0, c0));
   }
-  __device__ __forceinline__ f2_t near(f2_t s) const {
-    const f2_t t = fmul2(s, f2(k, k)), w = fmul2(t, t);
-    f2_t q = ffma2(w, f2(p[3], p[3]), f2(p[2], p[2]));
-    q = ffma2(w, q, f2(p[1], p[1]));
-    q = ffma2(w, q, f2(p[0], p[0]));
-    return fmul2(t, q);
-  }
+  __device__ __forceinline__ f2_t near(f2_t s) const { return fmul2(s, factor(s, 1.f)); }
   __device__ __forceinline__ f2_t far(f2_t s) const {
+    const float e = k * 2.885390081777927f, top = a.cap * 1.4426950408889634f;
     float x, y;
     f2_split(fmul2(s, f2(e, e)), x, y);
     f2_split(fadd2(f2(ex2_ftz(x), ex2_ftz(y)), f2(1.f, 1.f)), x, y);
     return ffma2(f2(rcp_ftz(x), rcp_ftz(y)), f2(-2.f * top, -2.f * top), f2(top, top));
+  }
+  __device__ __forceinline__ float near1(float s) const {
+    float x, y;
+    f2_split(near(f2(s, s)), x, y);
+    return x;
   }
 };
 
@@ -352,12 +360,13 @@ struct RowRules {
   float slope;              // times log2(e)
 
   // of token `tok` of a sequence, query head `head`
+  template <int RULES>
   __device__ __forceinline__ void load(const PagedArgs& a, int q0, int n, int len, int prefix, int tok, int head) {
     base = len - n;
     pos = base + tok;
     tree = 0ull;
     lim = a.causal ? min(len, max(pos + 1, prefix)) : len;
-    if (a.tree) {
+    if constexpr ((RULES & kTree) != 0) {
       // ancestors and the token itself (bits from its own on mean nothing)
       const unsigned long long own = 1ull << tok;
       tree = (a.tree[q0 + tok] & (own - 1ull)) | own;
@@ -368,7 +377,7 @@ struct RowRules {
         for (int i = deep - a.window; i > 0; --i) tree &= tree - 1ull;
     }
     low = first_seen(a, pos);
-    slope = a.slopes ? a.slopes[head] * 1.4426950408889634f : 0.f;
+    slope = (RULES & kBias) && a.slopes ? a.slopes[head] * 1.4426950408889634f : 0.f;
   }
   // no row: sees what it likes, for its results go nowhere
   __device__ __forceinline__ void none() {
@@ -377,8 +386,17 @@ struct RowRules {
     tree = 0ull;
     slope = 0.f;
   }
-  // whether drafted key `key` < len is the token's ancestor, and how far up
-  __device__ __forceinline__ bool drafted(int key) const { return key >= base && (tree >> (key - base)) & 1ull; }
+  // bit i: key `key0` + i is seen (32 keys)
+  template <bool TREE>
+  __device__ __forceinline__ uint32_t seen32(int key0) const {
+    const int from = max(low - key0, 0), to = min(lim - key0, 32), at = base - key0;
+    uint32_t w = to > from ? (0xFFFFFFFFu >> (32 - to)) & (0xFFFFFFFFu << from) : 0u;
+    if constexpr (TREE) {
+      if (at > -64 && at < 32) w |= (uint32_t)(at >= 0 ? tree << at : tree >> -at);
+    }
+    return w;
+  }
+  // how far up an ancestor at key `key` is
   __device__ __forceinline__ int above(int key) const { return __popcll(tree >> (key - base) >> 1); }
 };
 
