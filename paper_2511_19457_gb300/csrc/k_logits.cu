@@ -17,9 +17,10 @@ namespace sparoa {
 
 namespace {
 
-constexpr int kThreads = 512;
-constexpr int kItems = 8;               // tokens of a thread at once
-constexpr int kMaxChunk = 48 * 1024;    // tokens counted at once, 4 bytes each
+constexpr int kThreads = 256;
+constexpr int kItems = 8;            // tokens of a thread at once
+constexpr int kStep = kItems * kThreads;
+constexpr int kMaxChunk = 80 << 10;  // tokens counted at once, two bytes each
 
 // The best token and the sum of exp(z - clamp(best)) of some tokens.
 struct Found {
@@ -29,7 +30,12 @@ struct Found {
 };
 // what sums go by: infinities would give differences that are no numbers
 __device__ __forceinline__ float ref_of(float top) { return fminf(fmaxf(top, -FLT_MAX), FLT_MAX); }
-__device__ __forceinline__ float weight(float z) { return exp2f(z * 1.4426950408889634f); }
+constexpr float kLog2e = 1.4426950408889634f;
+__device__ __forceinline__ float weight(float z) {
+  float w;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(w) : "f"(z * kLog2e));
+  return w;
+}
 __device__ __forceinline__ Found join(const Found& a, const Found& b) {
   Found f;
   const bool second = b.top > a.top || (b.top == a.top && b.token < a.token);
@@ -50,25 +56,115 @@ __device__ __forceinline__ Found from_lane(const Found& f, int d) {
 __device__ __forceinline__ float load_logit(const float* p) { return *p; }
 __device__ __forceinline__ float load_logit(const __nv_bfloat16* p) { return __bfloat162float(*p); }
 
-template <typename XT, bool SEEN>
-__global__ void __launch_bounds__(kThreads) logits_kernel(const __grid_constant__ LogitArgs a) {
-  extern __shared__ __align__(16) unsigned s_count[];  // [chunk]
+enum Parts : int { kSeen = 1, kBiased = 2, kMasked = 4, kStored = 8 };  // what a kernel does besides
+
+// A row's rules, and where a thread's tokens of the CTA's share are.
+template <typename XT>
+struct Share {
+  const XT* x;
+  const float* bias;
+  const uint32_t* allowed;
+  float* y;
+  const unsigned* count;  // two counts in each, or one (wide)
+  float rep, presence, frequency, inv;
+  int lo, len;
+  bool wide;
+};
+
+// kItems tokens of a thread, kThreads apart, from token v0 of the share on.  FULL: all are there.
+template <int PARTS, bool FULL, typename XT>
+struct Batch {
+  float z[kItems], b[kItems];
+  uint32_t open[kItems];
+
+  static __device__ __forceinline__ bool there(const Share<XT>& s, int v) { return FULL || v + (int)threadIdx.x < s.len; }
+  __device__ __forceinline__ void fetch(const Share<XT>& s, int v0) {
+#pragma unroll
+    for (int u = 0; u < kItems; ++u) {
+      const int v = v0 + u * kThreads;
+      z[u] = there(s, v) ? load_logit(s.x + v) : -INFINITY;
+      if ((PARTS & kBiased) != 0) b[u] = there(s, v) ? s.bias[v] : 0.f;
+      if ((PARTS & kMasked) != 0) open[u] = there(s, v) ? s.allowed[v >> 5] : 0u;
+    }
+  }
+  __device__ __forceinline__ void penalise(const Share<XT>& s, int v0) {
+    unsigned c[kItems], any = 0u;
+#pragma unroll
+    for (int u = 0; u < kItems; ++u) {
+      const int v = v0 + u * kThreads;
+      c[u] = !there(s, v) ? 0u : s.wide ? s.count[v + threadIdx.x] : reinterpret_cast<const uint16_t*>(s.count)[v + threadIdx.x];
+      any |= c[u];
+    }
+    if (!any) return;
+#pragma unroll
+    for (int u = 0; u < kItems; ++u)
+      if (c[u])
+        z[u] = __fsub_rn(__fsub_rn(z[u] > 0.f ? __fdiv_rn(z[u], s.rep) : __fmul_rn(z[u], s.rep), s.presence), __fmul_rn(s.frequency, (float)c[u]));
+  }
+  __device__ __forceinline__ void finish(const Share<XT>& s, int v0, Found& f) {
+    const uint32_t bit = 1u << (threadIdx.x & 31);
+    float top = -INFINITY;
+#pragma unroll
+    for (int u = 0; u < kItems; u += 2) {
+      f2_t p = f2(z[u], z[u + 1]);
+      if ((PARTS & kBiased) != 0) p = fadd2(p, f2(b[u], b[u + 1]));
+      f2_split(fmul2(p, f2(s.inv, s.inv)), z[u], z[u + 1]);
+    }
+#pragma unroll
+    for (int u = 0; u < kItems; ++u) {
+      const int v = v0 + u * kThreads;
+      if ((PARTS & kMasked) != 0) z[u] = open[u] & bit ? z[u] : -INFINITY;
+      if ((PARTS & kStored) != 0 && there(s, v)) s.y[v] = z[u];
+      top = fmaxf(top, z[u]);  // (a number that is none is never the largest)
+    }
+    if (top > f.top) {
+      const float ref = ref_of(top);
+      f.sum *= weight(ref_of(f.top) - ref);
+      f.top = top;
+#pragma unroll
+      for (int u = kItems - 1; u >= 0; --u)
+        if (z[u] == top) f.token = s.lo + v0 + u * kThreads + (int)threadIdx.x;
+    }
+    const float ref = -ref_of(f.top);
+    f2_t sum = f2(f.sum, 0.f);
+#pragma unroll
+    for (int u = 0; u < kItems; u += 2) {
+      float x, y;
+      f2_split(fmul2(fadd2(f2(z[u], z[u + 1]), f2(ref, ref)), f2(kLog2e, kLog2e)), x, y);
+      asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(x));
+      asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(y));
+      sum = fadd2(sum, f2(x, y));
+    }
+    float x, y;
+    f2_split(sum, x, y);
+    f.sum = x + y;
+  }
+};
+
+// Counts have 16 bits, which a list below 2^16 tokens cannot pass; the vocabulary of a row with a
+// longer one is walked in shares of half the size, with 32 bits.
+template <typename XT, int PARTS>
+__global__ void __launch_bounds__(kThreads, 4) logits_kernel(const __grid_constant__ LogitArgs a) {
+  extern __shared__ __align__(16) unsigned s_count[];
   __shared__ Found s_found[kThreads / 32], s_cta;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int rank = (int)(blockIdx.x % a.split);
   const int64_t r = blockIdx.x / a.split;
+  Share<XT> s;
+  s.rep = s.inv = 1.f;
+  s.presence = s.frequency = 0.f;
+  s.count = s_count;
   pdl_wait();
   pdl_trigger();
-  float rep = 1.f, presence = 0.f, frequency = 0.f, inv = 1.f;
   if (a.penalties) {
     const float* p = a.penalties + r * 4;
-    rep = p[0];
-    presence = p[1];
-    frequency = p[2];
-    inv = __frcp_rn(p[3]);
+    s.rep = p[0];
+    s.presence = p[1];
+    s.frequency = p[2];
+    s.inv = __frcp_rn(p[3]);
   }
   int64_t s0 = 0, s1 = 0;
-  if constexpr (SEEN) {
+  if constexpr ((PARTS & kSeen) != 0) {
     s0 = a.seen_start[r];
     s1 = a.seen_start[r + 1];
     if (s0 < 0 || s1 < s0 || s1 > a.n_seen) {
@@ -76,57 +172,46 @@ __global__ void __launch_bounds__(kThreads) logits_kernel(const __grid_constant_
       s0 = s1 = 0;
     }
   }
-  const XT* x = static_cast<const XT*>(a.x) + r * a.ld_x;
-  const float* bias = a.bias ? a.bias + r * a.ld_bias : nullptr;
-  const uint32_t* allowed = a.allowed ? a.allowed + r * a.ld_allowed : nullptr;
-  float* y = a.y ? a.y + r * a.ld_y : nullptr;
+  const bool seen = (PARTS & kSeen) && s1 > s0;
+  s.wide = seen && s1 - s0 > 65535;
+  const int chunk = s.wide ? a.chunk / 2 : a.chunk;
   Found f{-INFINITY, 0x7FFFFFFF, 0.f};
-  for (int64_t lo64 = (int64_t)rank * a.chunk; lo64 < a.V; lo64 += (int64_t)a.split * a.chunk) {
-    const int lo = (int)lo64, len = min(a.chunk, a.V - lo);
-    if constexpr (SEEN) {
-      if (s1 > s0) {
-        __syncthreads();  // (the counts before were read)
-        for (int i = threadIdx.x * 4; i < len; i += kThreads * 4) *reinterpret_cast<uint4*>(s_count + i) = make_uint4(0u, 0u, 0u, 0u);
-        __syncthreads();
-        for (int64_t i = s0 + threadIdx.x; i < s1; i += kThreads) {
-          const int64_t t = (int64_t)a.seen[i] - lo;  // (what is no token of the vocabulary counts nowhere)
-          if (t >= 0 && t < len) atomicAdd(s_count + t, 1u);
-        }
-        __syncthreads();
+  for (int64_t lo = (int64_t)rank * chunk; lo < a.V; lo += (int64_t)a.split * chunk) {
+    s.lo = (int)lo;
+    s.len = min(chunk, a.V - s.lo);
+    const int64_t at = lo + threadIdx.x;
+    s.x = static_cast<const XT*>(a.x) + r * a.ld_x + at;
+    if ((PARTS & kBiased) != 0) s.bias = a.bias + r * a.ld_bias + at;
+    if ((PARTS & kMasked) != 0) s.allowed = a.allowed + r * a.ld_allowed + (at >> 5);
+    if ((PARTS & kStored) != 0) s.y = a.y + r * a.ld_y + at;
+    if (seen) {
+      __syncthreads();  // (the counts before were read)
+      for (int i = threadIdx.x; i < (s.len + (s.wide ? 3 : 7)) / (s.wide ? 4 : 8); i += kThreads)
+        reinterpret_cast<uint4*>(s_count)[i] = make_uint4(0u, 0u, 0u, 0u);
+      __syncthreads();
+      // (eight loads of a thread are on their way at once)
+      for (int64_t i0 = s0 + threadIdx.x; i0 < s1; i0 += 8 * kThreads) {
+        int64_t t[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) t[k] = i0 + k * kThreads < s1 ? (int64_t)a.seen[i0 + k * kThreads] - lo : -1;
+#pragma unroll
+        for (int k = 0; k < 8; ++k)  // (what is no token of the vocabulary counts nowhere)
+          if (t[k] >= 0 && t[k] < s.len) atomicAdd(s_count + (s.wide ? t[k] : t[k] >> 1), !s.wide && (t[k] & 1) ? 0x10000u : 1u);
       }
+      __syncthreads();
     }
-    for (int v0 = 0; v0 < len; v0 += kItems * kThreads) {
-      float z[kItems], b[kItems];
-      uint32_t ok[kItems];
-#pragma unroll
-      for (int u = 0; u < kItems; ++u) {
-        const int v = v0 + u * kThreads + (int)threadIdx.x;
-        const bool there = v < len;
-        z[u] = there ? load_logit(x + lo + v) : 0.f;
-        b[u] = there && bias ? bias[lo + v] : 0.f;
-        ok[u] = there ? (allowed ? allowed[(lo + v) >> 5] >> lane : 1u) : 0u;
-      }
-      float top = f.top;
-#pragma unroll
-      for (int u = 0; u < kItems; ++u) {
-        const int v = v0 + u * kThreads + (int)threadIdx.x;
-        if constexpr (SEEN) {
-          const unsigned c = s1 > s0 && v < len ? s_count[v] : 0u;
-          if (c) z[u] = __fsub_rn(__fsub_rn(z[u] > 0.f ? __fdiv_rn(z[u], rep) : __fmul_rn(z[u], rep), presence), __fmul_rn(frequency, (float)c));
-        }
-        if (bias) z[u] = __fadd_rn(z[u], b[u]);
-        z[u] = ok[u] & 1u ? __fmul_rn(z[u], inv) : -INFINITY;
-        if (y && v < len) y[lo + v] = z[u];
-        if (z[u] > top) {
-          top = z[u];
-          f.token = lo + v;
-        }
-      }
-      const float ref = ref_of(top);
-      f.sum *= weight(ref_of(f.top) - ref);
-      f.top = top;
-#pragma unroll
-      for (int u = 0; u < kItems; ++u) f.sum += weight(z[u] - ref);
+    int v0 = 0;
+    for (; v0 + kStep <= s.len; v0 += kStep) {
+      Batch<PARTS, true, XT> batch;
+      batch.fetch(s, v0);
+      if (seen) batch.penalise(s, v0);
+      batch.finish(s, v0, f);
+    }
+    if (v0 < s.len) {
+      Batch<PARTS, false, XT> batch;
+      batch.fetch(s, v0);
+      if (seen) batch.penalise(s, v0);
+      batch.finish(s, v0, f);
     }
   }
 #pragma unroll
@@ -160,25 +245,36 @@ __global__ void __launch_bounds__(kThreads) logits_kernel(const __grid_constant_
   cluster_wait();
 }
 
-template <typename XT, bool SEEN>
+template <typename XT, int PARTS>
 cudaError_t launch_logits_t(LogitArgs a, cudaStream_t s) {
-  const int64_t want = 3ll * device_sm_count();
+  constexpr bool SEEN = (PARTS & kSeen) != 0;
+  // CTAs of a row until there are four an SM, each with two rounds of tokens at least, and until
+  // four CTAs' counts fit an SM
+  const int64_t want = 4ll * device_sm_count();
   a.split = 1;
-  while (a.split < 8 && (a.R * a.split < want || (SEEN && (a.V + a.split - 1) / a.split > 16384)) && a.V > a.split * 4096) a.split *= 2;
-  a.chunk = ((a.V + a.split - 1) / a.split + 31) / 32 * 32;
+  while (a.split < 8 && ((a.R * a.split * 2 <= want && a.V > a.split * 2 * kStep) || (SEEN && a.V > a.split * (24 << 10))))
+    a.split *= 2;
+  a.chunk = ((a.V + a.split - 1) / a.split + 63) / 64 * 64;
   if (SEEN && a.chunk > kMaxChunk) a.chunk = kMaxChunk;
-  const size_t smem = SEEN ? (size_t)a.chunk * sizeof(unsigned) : 0;
-  const cudaError_t e = smem_optin(reinterpret_cast<const void*>(logits_kernel<XT, SEEN>), smem);
+  const size_t smem = SEEN ? (size_t)a.chunk * 2 : 0;
+  const cudaError_t e = smem_optin(reinterpret_cast<const void*>(logits_kernel<XT, PARTS>), smem);
   if (e != cudaSuccess) return e;
-  return launch_cluster_kernel(logits_kernel<XT, SEEN>, dim3((unsigned)(a.R * a.split)), dim3(kThreads), (unsigned)a.split, smem, s, a);
+  return launch_cluster_kernel(logits_kernel<XT, PARTS>, dim3((unsigned)(a.R * a.split)), dim3(kThreads), (unsigned)a.split, smem, s, a);
+}
+
+template <typename XT, int PARTS = 0>
+cudaError_t launch_by_parts(int parts, const LogitArgs& a, cudaStream_t s) {
+  if (parts == PARTS) return launch_logits_t<XT, PARTS>(a, s);
+  if constexpr (PARTS < 15) return launch_by_parts<XT, PARTS + 1>(parts, a, s);
+  return cudaErrorInvalidValue;
 }
 
 }  // namespace
 
 cudaError_t launch_logits(const LogitArgs& a, cudaStream_t s) {
   if (a.R <= 0) return cudaSuccess;
-  if (a.x_bf16) return a.seen_start ? launch_logits_t<__nv_bfloat16, true>(a, s) : launch_logits_t<__nv_bfloat16, false>(a, s);
-  return a.seen_start ? launch_logits_t<float, true>(a, s) : launch_logits_t<float, false>(a, s);
+  const int parts = (a.seen_start ? kSeen : 0) | (a.bias ? kBiased : 0) | (a.allowed ? kMasked : 0) | (a.y ? kStored : 0);
+  return a.x_bf16 ? launch_by_parts<__nv_bfloat16>(parts, a, s) : launch_by_parts<float>(parts, a, s);
 }
 
 }  // namespace sparoa
