@@ -20,6 +20,7 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kItems = 8;            // tokens of a thread at once
 constexpr int kStep = kItems * kThreads;
+constexpr int kAhead = 16;           // tokens of the list that a thread loads at once
 constexpr int kMaxChunk = 80 << 10;  // tokens counted at once, two bytes each
 
 // The best token and the sum of exp(z - clamp(best)) of some tokens.
@@ -66,7 +67,9 @@ struct Share {
   const uint32_t* allowed;
   float* y;
   const unsigned* count;  // two counts in each, or one (wide)
-  float rep, presence, frequency, inv;
+  // inv_rep = 1 / rep rounded: a quotient q = z inv_rep, corrected by the rest z - q rep times
+  // inv_rep, is the rounded z / rep (Markstein, 1990)
+  float rep, inv_rep, presence, frequency, inv;
   int lo, len;
   bool wide;
 };
@@ -96,10 +99,15 @@ struct Batch {
       any |= c[u];
     }
     if (!any) return;
+    // without a branch for each (a division's own cost the share with most of the list's tokens
+    // as much again as its bytes)
 #pragma unroll
-    for (int u = 0; u < kItems; ++u)
-      if (c[u])
-        z[u] = __fsub_rn(__fsub_rn(z[u] > 0.f ? __fdiv_rn(z[u], s.rep) : __fmul_rn(z[u], s.rep), s.presence), __fmul_rn(s.frequency, (float)c[u]));
+    for (int u = 0; u < kItems; ++u) {
+      const float q = __fmul_rn(z[u], s.inv_rep), rest = fmaf(-q, s.rep, z[u]);
+      const float ratio = fabsf(q) < INFINITY ? fmaf(rest, s.inv_rep, q) : q;
+      const float less = __fsub_rn(__fsub_rn(z[u] > 0.f ? ratio : __fmul_rn(z[u], s.rep), s.presence), __fmul_rn(s.frequency, (float)c[u]));
+      z[u] = c[u] ? less : z[u];
+    }
   }
   __device__ __forceinline__ void finish(const Share<XT>& s, int v0, Found& f) {
     const uint32_t bit = 1u << (threadIdx.x & 31);
@@ -151,7 +159,7 @@ __global__ void __launch_bounds__(kThreads, 4) logits_kernel(const __grid_consta
   const int rank = (int)(blockIdx.x % a.split);
   const int64_t r = blockIdx.x / a.split;
   Share<XT> s;
-  s.rep = s.inv = 1.f;
+  s.rep = s.inv_rep = s.inv = 1.f;
   s.presence = s.frequency = 0.f;
   s.count = s_count;
   pdl_wait();
@@ -159,6 +167,7 @@ __global__ void __launch_bounds__(kThreads, 4) logits_kernel(const __grid_consta
   if (a.penalties) {
     const float* p = a.penalties + r * 4;
     s.rep = p[0];
+    s.inv_rep = __frcp_rn(p[0]);
     s.presence = p[1];
     s.frequency = p[2];
     s.inv = __frcp_rn(p[3]);
@@ -184,23 +193,27 @@ __global__ void __launch_bounds__(kThreads, 4) logits_kernel(const __grid_consta
     if ((PARTS & kBiased) != 0) s.bias = a.bias + r * a.ld_bias + at;
     if ((PARTS & kMasked) != 0) s.allowed = a.allowed + r * a.ld_allowed + (at >> 5);
     if ((PARTS & kStored) != 0) s.y = a.y + r * a.ld_y + at;
+    Batch<PARTS, false, XT> first;
     if (seen) {
-      __syncthreads();  // (the counts before were read)
+      first.fetch(s, 0);  // on its way while the tokens are counted
+      __syncthreads();    // (the counts before were read)
       for (int i = threadIdx.x; i < (s.len + (s.wide ? 3 : 7)) / (s.wide ? 4 : 8); i += kThreads)
         reinterpret_cast<uint4*>(s_count)[i] = make_uint4(0u, 0u, 0u, 0u);
       __syncthreads();
-      // (eight loads of a thread are on their way at once)
-      for (int64_t i0 = s0 + threadIdx.x; i0 < s1; i0 += 8 * kThreads) {
-        int64_t t[8];
+      // (kAhead loads of a thread are on their way at once; what is no token counts nowhere)
+      for (int64_t i0 = s0 + threadIdx.x; i0 < s1; i0 += kAhead * kThreads) {
+        unsigned t[kAhead];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) t[k] = i0 + k * kThreads < s1 ? (int64_t)a.seen[i0 + k * kThreads] - lo : -1;
+        for (int k = 0; k < kAhead; ++k) t[k] = i0 + k * kThreads < s1 ? (unsigned)a.seen[i0 + k * kThreads] - (unsigned)s.lo : 0xFFFFFFFFu;
 #pragma unroll
-        for (int k = 0; k < 8; ++k)  // (what is no token of the vocabulary counts nowhere)
-          if (t[k] >= 0 && t[k] < s.len) atomicAdd(s_count + (s.wide ? t[k] : t[k] >> 1), !s.wide && (t[k] & 1) ? 0x10000u : 1u);
+        for (int k = 0; k < kAhead; ++k)
+          if (t[k] < (unsigned)s.len) atomicAdd(s_count + (s.wide ? t[k] : t[k] >> 1), !s.wide && (t[k] & 1u) ? 0x10000u : 1u);
       }
       __syncthreads();
+      first.penalise(s, 0);
+      first.finish(s, 0, f);
     }
-    int v0 = 0;
+    int v0 = seen ? kStep : 0;
     for (; v0 + kStep <= s.len; v0 += kStep) {
       Batch<PARTS, true, XT> batch;
       batch.fetch(s, v0);

@@ -242,3 +242,20 @@ def test_refusals(sp, ctx):
             f()
             raise AssertionError(f"call {i} was taken")
     ctx.sync()
+
+
+def test_division_is_rounded_as_a_division(sp, ctx):
+    """z / repetition is the rounded quotient: the bits of the division of two fp32 numbers, for ordinary sizes;
+    infinities stay."""
+    V = 100000
+    g = torch.Generator().manual_seed(12)
+    x = torch.randn(4, V, generator=g).abs() * torch.tensor([[1.0], [1e-20], [1e20], [3.0]])
+    x[3, 7] = math.inf
+    rep = torch.tensor([1.1, 1.3, 0.7, 1.9999999])
+    pen = torch.stack([rep, torch.zeros(4), torch.zeros(4), torch.ones(4)], 1)
+    start = torch.arange(5, dtype=torch.int32) * V
+    seen = torch.arange(V, dtype=torch.int32).repeat(4)
+    y = torch.empty(4, V, device="cuda")
+    xd = x.cuda()
+    sp.sparoa_shape_logits(ctx, xd, sp.LogitRules(seen_start=start.cuda(), seen=seen.cuda(), penalties=pen.cuda()), y=y)
+    assert torch.equal(y, xd / rep.cuda()[:, None])
