@@ -25,6 +25,7 @@ thread_local bool t_pdl = true;
 struct DeviceFacts {
   int sms = 0;
   std::map<const void*, size_t> optin;
+  std::map<std::pair<const void*, int>, int> clusters;  // of a kernel and a cluster size: how many fit at once
 };
 std::mutex g_facts_mu;
 std::map<int, DeviceFacts> g_facts;
@@ -65,6 +66,32 @@ cudaError_t smem_optin(const void* func, size_t bytes) {
   if (e != cudaSuccess) return e;
   have = bytes;
   return cudaSuccess;
+}
+
+int cluster_fit(const void* func, int cluster, int threads, size_t smem) {
+  const int dev = current_device();
+  std::lock_guard<std::mutex> lock(g_facts_mu);
+  std::map<std::pair<const void*, int>, int>& known = g_facts[dev].clusters;
+  const auto at = known.find({func, cluster});
+  if (at != known.end()) return at->second;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)cluster);
+  cfg.blockDim = dim3((unsigned)threads);
+  cfg.dynamicSmemBytes = smem;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = (unsigned)cluster;
+  attr[0].val.clusterDim.y = 1;
+  attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  int n = 0;
+  if (cudaOccupancyMaxActiveClusters(&n, func, &cfg) != cudaSuccess) {
+    cudaGetLastError();
+    return 0;  // not remembered, so the next call asks again
+  }
+  known[{func, cluster}] = n;
+  return n;
 }
 }  // namespace sparoa
 
@@ -1720,6 +1747,7 @@ sparoa_status sparoa_gemm_w4(sparoa_ctx* ctx, const void* x, int64_t M, const sp
     a.y_f32 = y_dtype == SPAROA_F32;
     a.err = ctx->d_err();
     a.wait_limit = ctx->wait_limit;
+    a.fault = ctx->fault == 1;
     SP_CUDA(launch_w4(a, ctx->stream));
   }
   if (y_occ) SP_TRY(run_stats(ctx, y, M, w->N, *y_occ));

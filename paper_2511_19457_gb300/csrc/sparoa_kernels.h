@@ -55,6 +55,9 @@ cudaError_t launch_cluster_kernel(void (*kernel)(KArgs...), dim3 grid, dim3 bloc
   return cudaLaunchKernelEx(&cfg, kernel, static_cast<Args&&>(args)...);
 }
 
+// Clusters of `cluster` CTAs of `func` that the current device holds at once (asked once); 0: none.
+int cluster_fit(const void* func, int cluster, int threads, size_t smem);
+
 // Zero up to five word ranges (the fields of an occupancy block) in one launch.
 struct ClearArgs {
   uint32_t* p[5];
@@ -371,6 +374,7 @@ struct W4Args {
   int y_f32 = 0;
   uint32_t* err = nullptr;
   long long wait_limit = 0;
+  int fault = 0;  // error-path tests: 1 withholds the signals of the tcgen05 kernel's sums
   int row_tiles = 0, tiles = 0, split = 1;  // tiles of rows and of columns, CTAs of a block's columns (set by launch_w4)
 };
 cudaError_t launch_w4(W4Args a, cudaStream_t s);
