@@ -13,7 +13,13 @@ Per layer, on the new tokens of all sequences at once ([T, C] rows, sequence aft
 The residual stream is fp32, everything between operators bf16.  ``Pages`` hands out the cache's
 pages; a sequence holds its pages until it is freed.
 
-    python -m paper_2511_19457_gb300.decoder      # a few prompts in chunks, then tokens one by one
+With 4-bit weights (``group``) the products are sparoa_gemm_w4; with a cap of the scores or a bias by
+distance (``cap``, ``slopes``), and over trees of drafted tokens, the attention is sparoa_ruled_attention.
+Logits become tokens by sparoa_shape_logits.  ``check`` judges trees of drafted tokens in one step
+(sparoa_tree_accept keeps the path that the model's own choices confirm); ``generate`` takes the drafts from a
+function of the tokens so far.
+
+    python -m paper_2511_19457_gb300.decoder      # a few prompts in chunks, then tokens one by one and by drafts
 """
 from __future__ import annotations
 
@@ -64,6 +70,13 @@ class Pages:
             if not length:
                 self.release(s)
 
+    def cut(self, seq, length: int):
+        """Takes back what a sequence holds behind its first `length` tokens."""
+        pages = self.held[seq]
+        keep = -(-length // self.page_size)
+        self.free += reversed(pages[keep:])
+        self.held[seq], self.length[seq] = pages[:keep], length
+
     def release(self, seq):
         """Takes a sequence's pages back, if it has any."""
         self.free += reversed(self.held.pop(seq, []))
@@ -81,13 +94,31 @@ class Pages:
         return sp.PagedBatch(*lists, max_q=max(new))
 
 
+def ancestors(parents):
+    """Ancestor bits of a tree's tokens (its own among them) from each token's parent, -1 for none; parents
+    come first."""
+    if len(parents) > 64:
+        raise ValueError("a tree of more than 64 tokens")
+    bits: list = []
+    for i, p in enumerate(parents):
+        if not -1 <= p < i:
+            raise ValueError(f"parent {p} of token {i}")
+        bits.append((bits[p] if p >= 0 else 0) | 1 << i)
+    return bits
+
+
 class Decoder:
+    """cap: attention scores s become cap tanh(s / cap); slopes (fp32 [heads]): a bias by distance instead of rotary
+    positions; group: products with 4-bit weights, a scale for `group` columns."""
+
     def __init__(self, ctx: sp.Context, layers=2, dim=512, heads=8, kv_heads=2, head_dim=64, hidden=1024, vocab=1000,
-                 pages=256, page_size=64, rope: sp.Rope | None = None, seed=0, device="cuda"):
+                 pages=256, page_size=64, rope: sp.Rope | None = None, seed=0, device="cuda", cap=0.0, slopes=None,
+                 group: int | None = None):
         g = torch.Generator().manual_seed(seed)
 
         def weight(n, k):
-            return (torch.randn(n, k, generator=g) / math.sqrt(k)).to(torch.bfloat16).to(device)
+            w = (torch.randn(n, k, generator=g) / math.sqrt(k)).to(torch.bfloat16).to(device)
+            return w if group is None else sp.W4.quantise(ctx, w, group)
 
         def gamma(shift):
             return (shift + 0.1 * torch.randn(dim, generator=g)).to(device)
@@ -100,7 +131,8 @@ class Decoder:
                         "g1": gamma(0.5), "g2": gamma(0.5),
                         "cache": sp.KVCache.empty(pages, kv_heads, page_size, head_dim, device)} for _ in range(layers)]
         self.last = sp.norm("rms", gamma(1.0))
-        self.rope = rope or sp.Rope(head_dim, device=device)
+        self.rope = rope or sp.Rope(0 if slopes is not None else head_dim, device=device)
+        self.cap, self.slopes = cap, None if slopes is None else slopes.to(device)
         self.pages = Pages(pages, page_size)
         self.hidden = hidden
 
@@ -114,9 +146,49 @@ class Decoder:
             self.pages.shrink_all(seqs, new)  # (what was appended of this step is written over by the next)
             raise
 
+    def check(self, drafts, seqs):
+        """Judge drafted tokens.  drafts[i] = (tokens, parents) of seqs[i], the first token the last one that is
+        settled (and not in the cache yet), the others drafted behind their parents (parents[0] = -1).
+        Returns for each sequence its next tokens: the drafted ones that the model would have chosen itself
+        (greedily), and the one that it chooses after them.  The cache keeps what is settled."""
+        new = [len(t) for t, _ in drafts]
+        bits = [b for _, parents in drafts for b in ancestors(parents)]
+        if any(len(t) != len(p) or not t or p[0] != -1 for t, p in drafts):
+            raise ValueError("check: a tree begins with the last settled token and has a parent for each token")
+        dev = self.embed.device
+        flat = torch.tensor([t for tokens, _ in drafts for t in tokens], dtype=torch.int32).to(dev)
+        tree = torch.tensor([b - (1 << 64) if b >> 63 else b for b in bits], dtype=torch.int64).to(dev)
+        depth = [bin(b).count("1") - 1 for b in bits]
+        before = [self.pages.length.get(s, 0) for s in seqs]
+        self.pages.grow_all(seqs, new)
+        try:
+            at, positions = 0, []
+            for start, n in zip(before, new):
+                positions += [start + d for d in depth[at:at + n]]
+                at += n
+            batch = self.pages.batch(seqs, new, dev)
+            logits = self._layers(flat.long(), batch, tree, torch.tensor(positions, dtype=torch.int32).to(dev))
+            best, path = torch.empty_like(flat), torch.empty_like(flat)
+            sp.sparoa_shape_logits(self.ctx, logits, best=best)
+            count, following, length = (torch.empty(len(seqs), dtype=torch.int32, device=dev) for _ in range(3))
+            sp.sparoa_tree_accept(self.ctx, flat, best, tree, [w["cache"] for w in self.layers], batch, path, count, following, length)
+            self.ctx.sync()  # (reports device-side failures)
+            ways, counts, after, lengths = path.tolist(), count.tolist(), following.tolist(), length.tolist()
+        except BaseException:
+            self.pages.shrink_all(seqs, new)
+            raise
+        out, at = [], 0
+        for (tokens, _), s, n, c, f, L in zip(drafts, seqs, new, counts, after, lengths):
+            out.append([tokens[i] for i in ways[at + 1:at + c]] + [f])
+            self.pages.cut(s, L)
+            at += n
+        return out
+
     def _forward(self, tokens, seqs, new):
+        return self._layers(tokens, self.pages.batch(seqs, new, tokens.device))
+
+    def _layers(self, tokens, batch, tree=None, positions=None):
         ctx, T, dev = self.ctx, tokens.numel(), tokens.device
-        batch = self.pages.batch(seqs, new, dev)
 
         def rows(width, dtype=torch.bfloat16):
             return torch.empty(T, width, dtype=dtype, device=dev)
@@ -127,54 +199,130 @@ class Decoder:
         a = torch.empty_like(q)
         occ = sp.OccupancyBuffer(T, self.hidden, dev)
         dense = sp.thresholds(force_path=1)  # (norm and attention outputs have no zeros to skip)
+        rules = None
+        if tree is not None or self.cap or self.slopes is not None:
+            rules = sp.ScoreRules(cap=self.cap, slopes=self.slopes, tree=tree)
+
+        def product(x, w, y, **kw):
+            if isinstance(w, sp.W4):
+                sp.sparoa_gemm_w4(ctx, x, w, y, **kw)
+            else:
+                sp.sparoa_gemm(ctx, x, w, y, thr=dense, **kw)
+
         sp.sparoa_add_norm(ctx, x, None, None, y, pre=self.layers[0]["n1"])
         for i, w in enumerate(self.layers):
             after = self.layers[i + 1]["n1"] if i + 1 < len(self.layers) else self.last
-            sp.sparoa_gemm(ctx, y, w["qkv"], qkv, thr=dense)
-            sp.sparoa_rope_append(ctx, qkv, q, w["cache"], batch, self.rope)
-            sp.sparoa_paged_attention(ctx, q, a, w["cache"], batch)
-            sp.sparoa_gemm(ctx, a, w["o"], o, thr=dense)
+            product(y, w["qkv"], qkv)
+            sp.sparoa_rope_append(ctx, qkv, q, w["cache"], batch, self.rope, positions)
+            if rules is None:
+                sp.sparoa_paged_attention(ctx, q, a, w["cache"], batch)
+            else:
+                sp.sparoa_ruled_attention(ctx, q, a, w["cache"], batch, rules)
+            product(a, w["o"], o)
             sp.sparoa_add_norm(ctx, x, o, r, y, gate=w["g1"], pre=w["n2"])
-            sp.sparoa_gemm(ctx, y, w["w1"], h, act=sp.ACT_RELU, thr=dense, y_occ=occ)
-            sp.sparoa_gemm(ctx, h, w["w2"], o, x_occ=occ)
+            if isinstance(w["w2"], sp.W4):
+                product(y, w["w1"], h, act=sp.ACT_RELU)
+                product(h, w["w2"], o)
+            else:
+                product(y, w["w1"], h, act=sp.ACT_RELU, y_occ=occ)
+                sp.sparoa_gemm(ctx, h, w["w2"], o, x_occ=occ)
             sp.sparoa_add_norm(ctx, r, o, x, y, gate=w["g2"], pre=after)
         logits = rows(self.embed.shape[0], torch.float32)
         sp.sparoa_gemm(ctx, y, self.embed, logits, thr=dense)
         return logits
 
-    def generate(self, prompts, steps: int, chunk: int = 256):
+    def generate(self, prompts, steps: int, chunk: int = 256, draft=None, penalties=None, bias=None, allowed=None):
         """Greedy tokens after each prompt (lists of token numbers): prompts in chunks of at most
         `chunk` tokens each, all sequences together, then one token of each at a time.  No prompts:
-        no tokens; an empty prompt, which nothing can be said after, is refused."""
+        no tokens; an empty prompt, which nothing can be said after, is refused.
+          draft      a function of a sequence's tokens so far: (tokens, parents) that may come next, parents by
+                     their number among them, -1 behind the last token; they are judged together (check)
+          penalties  (repetition, presence, frequency, temperature) of every sequence
+          bias       fp32 [vocab] on the logits
+          allowed    a function of a sequence's tokens so far: int32 [words], bit v % 32 of word v / 32 for
+                     every token that may come next
+        Drafts go with none of the three others."""
         if not all(prompts):
             raise ValueError("generate: a prompt without tokens")
+        if draft is not None and not (penalties is None and bias is None and allowed is None):
+            raise ValueError("generate: drafts are judged by the logits as they are")
         if not prompts:
             return []
         seqs = [object() for _ in prompts]
         try:
-            return self._generate(seqs, prompts, steps, chunk)
+            return self._generate(seqs, prompts, steps, chunk, draft, penalties, bias, allowed)
         finally:
             for s in seqs:
                 self.pages.release(s)
 
-    def _generate(self, seqs, prompts, steps, chunk):
+    def _choose(self, logits, texts, penalties, bias, allowed):
+        """The best token of each row of logits behind its text."""
+        dev = logits.device
+        best = torch.empty(len(texts), dtype=torch.int32, device=dev)
+        rules = None
+        if not (penalties is None and bias is None and allowed is None):
+            lists, words, each = {}, None, None
+            if penalties is not None:
+                start = [0]
+                for t in texts:
+                    start.append(start[-1] + len(t))
+                lists = {"seen_start": torch.tensor(start, dtype=torch.int32).to(dev),
+                         "seen": torch.tensor([v for t in texts for v in t], dtype=torch.int32).to(dev)}
+                each = torch.tensor([penalties] * len(texts), dtype=torch.float32).to(dev)
+            if allowed is not None:
+                words = torch.stack([allowed(t) for t in texts]).to(dev)
+            rules = sp.LogitRules(penalties=each, bias=bias, allowed=words, **lists)
+        sp.sparoa_shape_logits(self.ctx, logits, rules, best=best)
+        out = best.tolist()
+        if min(out) < 0:
+            raise ValueError("generate: a sequence that no token may follow")
+        return out
+
+    def _generate(self, seqs, prompts, steps, chunk, draft, penalties, bias, allowed):
         dev = self.embed.device
         at = [0] * len(prompts)
         out: list = [[] for _ in prompts]
-        while any(a < len(p) for a, p in zip(at, prompts)) or len(out[0]) < steps:
+        while any(a < len(p) for a, p in zip(at, prompts)) or min(len(t) for t in out) < steps:
             todo = [(i, p[a:a + chunk]) for i, (a, p) in enumerate(zip(at, prompts)) if a < len(p)]
             if not todo:  # all prompts are in the cache
+                if draft is not None:
+                    self._check_drafts(seqs, prompts, out, steps, draft)
+                    continue
                 todo = [(i, [t[-1]]) for i, t in enumerate(out)]
             tokens = torch.tensor([t for _, part in todo for t in part]).to(dev)
             new = [len(part) for _, part in todo]
             logits = self.forward(tokens, [seqs[i] for i, _ in todo], new)
-            best = logits[torch.tensor(new).cumsum(0).to(dev) - 1].argmax(-1).tolist()
-            for (i, part), token in zip(todo, best):
+            ends = [(row, i) for row, (i, part) in zip(torch.tensor(new).cumsum(0).sub(1).tolist(), todo)
+                    if at[i] + len(part) >= len(prompts[i])]
+            for i, part in todo:
                 at[i] += len(part)
-                if at[i] >= len(prompts[i]):
+            if ends:
+                rows = logits if len(ends) == logits.shape[0] else logits[torch.tensor([r for r, _ in ends]).to(dev)]
+                texts = [prompts[i] + out[i] for _, i in ends]
+                for (_, i), token in zip(ends, self._choose(rows, texts, penalties, bias, allowed)):
                     out[i].append(token)
         self.ctx.sync()  # (reports device-side failures)
         return [t[:steps] for t in out]
+
+    def _check_drafts(self, seqs, prompts, out, steps, draft):
+        todo = [i for i, t in enumerate(out) if len(t) < steps]
+        drafts = []
+        for i in todo:
+            tokens, parents = draft(prompts[i] + out[i])
+            drafts.append(([out[i][-1]] + list(tokens), [-1] + [p + 1 for p in parents]))
+        for i, more in zip(todo, self.check(drafts, [seqs[i] for i in todo])):
+            out[i] += more
+
+
+def repeats(text, tokens=4, ways=2):
+    """Drafts from the text itself: what followed its last token the latest `ways` times, `tokens` each."""
+    out, parents = [], []
+    places = [i for i in range(len(text) - 2, -1, -1) if text[i] == text[-1]][:ways]
+    for i in places:
+        for k, t in enumerate(text[i + 1:i + 1 + tokens]):
+            parents.append(-1 if k == 0 else len(out) - 1)
+            out.append(t)
+    return out, parents
 
 
 def main():
@@ -184,6 +332,10 @@ def main():
     prompts = [torch.randint(0, 1000, (n,), generator=g).tolist() for n in (700, 1, 300, 64)]
     for p, t in zip(prompts, model.generate(prompts, 16)):
         print(f"{len(p)} tokens -> {t}")
+    for p, t in zip(prompts, model.generate(prompts, 16, draft=repeats)):
+        print(f"{len(p)} tokens, drafts -> {t}")
+    for p, t in zip(prompts, model.generate(prompts, 16, penalties=(1.0, 100.0, 0.0, 1.0))):
+        print(f"{len(p)} tokens, none twice -> {t}")
     ctx.close()
 
 
