@@ -1,8 +1,9 @@
 // Products of a few tokens' rows with weights of 4 bits: y = epilogue(x W^T),
 // W[n][k] = scale[n][k / group] (code[n][k] - zero[n][k / group]).
 //
-// Bound by the bytes of the weights, half a byte each and read once.  A CTA has 128 rows of W over
-// its share of the columns, 16 a warp; the rows' tiles of the same columns come in one copy (w4.cuh;
+// Bound by the bytes of the weights, half a byte each and read once, and nearly as much by the instructions
+// that make numbers of the codes (11 for 8 codes, 2 cycles each).  A CTA has 64, 96 or 128 rows of W over
+// its share of the columns, 16 a warp, as they fill the GPU best (w4_split); the rows' tiles of the same columns come in one copy (w4.cuh;
 // a copy for each took 44 cycles more of the copy unit, and there are eight), kStages of them on their way, with x beside
 // them by TMA.  A code becomes the bf16 number 128 + code
 // by one logic operation, 128 + zero is taken away, which is exact, and mma.sync m16n8k16 sums the
@@ -18,8 +19,7 @@ constexpr int kTileK = kW4TileK;
 constexpr int kWarps = 8;                             // of 16 rows each, a team: every other tile of columns
 constexpr int kTeams = 2;
 constexpr int kThreads = 32 * (kTeams * kWarps + 2);  // and a warp that loads codes, one that loads x
-constexpr int kRows = 16 * kWarps;
-constexpr int kPitch = kRows + 4;            // floats of a token's sums
+constexpr int kPitch = 16 * kWarps + 4;      // floats of a token's sums
 constexpr int kStages = 4;                   // of kTeams tiles of columns, on their way
 
 template <int NT>
@@ -56,7 +56,10 @@ __global__ void __launch_bounds__(kThreads, 1) w4_kernel(const __grid_constant__
   const int rank = (int)(blockIdx.x % a.split), block = (int)(blockIdx.x / a.split), tok0 = blockIdx.y * C::kTokens;
   const int tokens = min(C::kTokens, a.M - tok0);
   const int t0 = (int)((int64_t)rank * a.tiles / a.split), count = (int)((int64_t)(rank + 1) * a.tiles / a.split) - t0;
-  const int team = warp / kWarps, mine = warp % kWarps;  // (the loading warp: team kTeams)
+  // (as many warps as there are tiles of rows, the teams' one after the other: a scheduler has every
+  // fourth warp)
+  const int team = warp / a.block_tiles, mine = warp % a.block_tiles;
+  constexpr int kLoadWarp = kTeams * kWarps;
   const long long limit = a.wait_limit ? a.wait_limit : kWaitLimitCycles;
   if (threadIdx.x == 0) {
     for (int i = 0; i < kStages; ++i) {
@@ -74,22 +77,34 @@ __global__ void __launch_bounds__(kThreads, 1) w4_kernel(const __grid_constant__
 #pragma unroll
   for (int n = 0; n < NT; ++n) acc[n][0] = acc[n][1] = acc[n][2] = acc[n][3] = 0.f;
   const int stages = (count + kTeams - 1) / kTeams;
-  if (team == kTeams) {
+  const int first = block * a.block_tiles, rows = min(a.block_tiles, a.row_tiles - first);  // the CTA's tiles of rows
+  const int in_block = first % 8 ? 0 : min(8, a.row_tiles - first);                          // of the layout's block from there
+  if (warp >= kLoadWarp) {
     // (the copies of a stage take a warp 100 cycles each to give out: as few as there can be, by two warps)
-    const uint32_t bytes = (uint32_t)(min(8, a.row_tiles - block * 8) * tile);  // of the block's tiles of the same columns
-    const uint8_t* from = a.w + w4_tile_at(block * 8, t0, a.row_tiles, a.tiles) * tile;
     int s = 0;
     for (; s < stages; ++s) {
       const int st = s % kStages, t = s * kTeams, there = min(kTeams, count - t);
       if (!mbar_wait_warp(smem_u32(&s_empty[st]), (s / kStages + 1) & 1u, a.err, &s_abort, kErrTimeoutEmpty, limit)) break;
       if (lane == 0) {
         const uint32_t bar = smem_u32(&s_full[st]);
-        if (mine == 0) {
-          mbar_arrive_expect_tx(bar, there * bytes);
-          bulk_load(ring + st * kTeams * 8 * tile, from + (int64_t)t * bytes, there * bytes, bar);
+        if (warp == kLoadWarp) {
+          mbar_arrive_expect_tx(bar, (uint32_t)(there * rows * tile));
+          const uint32_t to = ring + st * kTeams * kWarps * tile;
+          if (rows == in_block) {  // whole blocks of the layout: tiles of columns side by side, too
+            bulk_load(to, a.w + w4_tile_at(first, t0 + t, a.row_tiles, a.tiles) * tile, (uint32_t)(there * rows * tile), bar);
+          } else {
+            const int head = min(rows, 8 - first % 8);  // rows up to the next block
+            for (int i = 0; i < there; ++i) {
+              bulk_load(to + i * rows * tile, a.w + w4_tile_at(first, t0 + t + i, a.row_tiles, a.tiles) * tile, (uint32_t)(head * tile), bar);
+              if (head < rows)
+                bulk_load(to + (i * rows + head) * tile, a.w + w4_tile_at(first + head, t0 + t + i, a.row_tiles, a.tiles) * tile,
+                          (uint32_t)((rows - head) * tile), bar);
+            }
+          }
         } else {
           mbar_arrive_expect_tx(bar, there * 2u * C::kHalf);
-          for (int i = 0; i < 2 * there; ++i) tma_load_2d(xring + (st * kTeams * 2 + i) * C::kHalf, &tx, bar, (t0 + t) * kTileK + i * 64, tok0);
+          for (int i = 0; i < 2 * there; ++i)
+            tma_load_2d(xring + (st * kTeams * 2 + i) * C::kHalf, &tx, bar, (t0 + t) * kTileK + i * 64, tok0);
         }
       }
       __syncwarp();
@@ -100,46 +115,46 @@ __global__ void __launch_bounds__(kThreads, 1) w4_kernel(const __grid_constant__
       for (int i = s > kStages ? s - kStages : 0; i < s; ++i) mbar_drain(smem_u32(&s_full[i % kStages]), (i / kStages) & 1u, limit);
   } else {
     const int token = (g >> 1) + (g & 1) * 4;
-    // (a warp without rows multiplies what its place in the ring holds: its results go nowhere)
-    const int rows8 = min(8, a.row_tiles - block * 8);
     for (int s = 0; s < stages; ++s) {
       const int st = s % kStages;
       if (!mbar_wait_warp(smem_u32(&s_full[st]), (s / kStages) & 1u, a.err, &s_abort, kErrTimeoutFull, limit)) break;
-      if (s * kTeams + team >= count) continue;  // (the last stage's other tiles)
-      const uint32_t x = xring + (st * kTeams + team) * 2 * C::kHalf, w = ring + (st * kTeams * 8 + team * rows8 + mine) * tile, meta = w + 1024 + g * 2;
-      const uint4 c0 = lds_u4(w + w4_piece(g, tq)), c1 = lds_u4(w + w4_piece(g + 8, tq));
+      if (team < kTeams && s * kTeams + team < count && mine < rows) {
+        const uint32_t x = xring + (st * kTeams + team) * 2 * C::kHalf, w = ring + (st * kTeams * kWarps + team * rows + mine) * tile;
+        const uint32_t meta = w + 1024 + g * 2;
+        const uint4 c0 = lds_u4(w + w4_piece(g, tq)), c1 = lds_u4(w + w4_piece(g + 8, tq));
 #pragma unroll
-      for (int gi = 0; gi < GROUPS; ++gi) {
-        float part[NT][4];
-        uint32_t z0 = 8u, z1 = 8u;
-        if (a.zeros) {
-          z0 = lds_u8(w + 1024 + GROUPS * 32 + gi * 16 + g);
-          z1 = lds_u8(w + 1024 + GROUPS * 32 + gi * 16 + g + 8);
-        }
-        z0 = w4_zero_pair(z0);
-        z1 = w4_zero_pair(z1);
+        for (int gi = 0; gi < GROUPS; ++gi) {
+          float part[NT][4];
+          uint32_t z0 = 8u, z1 = 8u;
+          if (a.zeros) {
+            z0 = lds_u8(w + 1024 + GROUPS * 32 + gi * 16 + g);
+            z1 = lds_u8(w + 1024 + GROUPS * 32 + gi * 16 + g + 8);
+          }
+          z0 = w4_zero_pair(z0);
+          z1 = w4_zero_pair(z1);
 #pragma unroll
-        for (int j = gi * 4 / GROUPS; j < (gi + 1) * 4 / GROUPS; ++j) {
-          const uint32_t w0 = j == 0 ? c0.x : j == 1 ? c0.y : j == 2 ? c0.z : c0.w, w1 = j == 0 ? c1.x : j == 1 ? c1.y : j == 2 ? c1.z : c1.w;
-          const uint32_t f0[4] = {w4_pair(w0, 0, z0), w4_pair(w1, 0, z1), w4_pair(w0, 1, z0), w4_pair(w1, 1, z1)};
-          const uint32_t f1[4] = {w4_pair(w0, 2, z0), w4_pair(w1, 2, z1), w4_pair(w0, 3, z0), w4_pair(w1, 3, z1)};
+          for (int j = gi * 4 / GROUPS; j < (gi + 1) * 4 / GROUPS; ++j) {
+            const uint32_t w0 = j == 0 ? c0.x : j == 1 ? c0.y : j == 2 ? c0.z : c0.w, w1 = j == 0 ? c1.x : j == 1 ? c1.y : j == 2 ? c1.z : c1.w;
+            const uint32_t f0[4] = {w4_pair(w0, 0, z0), w4_pair(w1, 0, z1), w4_pair(w0, 1, z0), w4_pair(w1, 1, z1)};
+            const uint32_t f1[4] = {w4_pair(w0, 2, z0), w4_pair(w1, 2, z1), w4_pair(w0, 3, z0), w4_pair(w1, 3, z1)};
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+              const uint4 v = lds_u4(x + (j >> 1) * C::kHalf + swz_offset<64>(n * 8 + token, (j & 1) * 4 + tq));
+              if (j == gi * 4 / GROUPS)
+                mma16816_first(part[n], f0, v.x, v.y);
+              else
+                mma16816(part[n], f0, v.x, v.y);
+              mma16816(part[n], f1, v.z, v.w);
+            }
+          }
+          const float s0 = __uint_as_float(lds_u16(meta + gi * 32) << 16), s1 = __uint_as_float(lds_u16(meta + gi * 32 + 16) << 16);
 #pragma unroll
           for (int n = 0; n < NT; ++n) {
-            const uint4 v = lds_u4(x + (j >> 1) * C::kHalf + swz_offset<64>(n * 8 + token, (j & 1) * 4 + tq));
-            if (j == gi * 4 / GROUPS)
-              mma16816_first(part[n], f0, v.x, v.y);
-            else
-              mma16816(part[n], f0, v.x, v.y);
-            mma16816(part[n], f1, v.z, v.w);
+            acc[n][0] = fmaf(s0, part[n][0], acc[n][0]);
+            acc[n][1] = fmaf(s0, part[n][1], acc[n][1]);
+            acc[n][2] = fmaf(s1, part[n][2], acc[n][2]);
+            acc[n][3] = fmaf(s1, part[n][3], acc[n][3]);
           }
-        }
-        const float s0 = __uint_as_float(lds_u16(meta + gi * 32) << 16), s1 = __uint_as_float(lds_u16(meta + gi * 32 + 16) << 16);
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-          acc[n][0] = fmaf(s0, part[n][0], acc[n][0]);
-          acc[n][1] = fmaf(s0, part[n][1], acc[n][1]);
-          acc[n][2] = fmaf(s1, part[n][2], acc[n][2]);
-          acc[n][3] = fmaf(s1, part[n][3], acc[n][3]);
         }
       }
       __syncwarp();
@@ -148,7 +163,7 @@ __global__ void __launch_bounds__(kThreads, 1) w4_kernel(const __grid_constant__
   }
   // the CTA's sums [tokens][rows], where x was (every copy has arrived)
   __syncthreads();
-  if (team < kTeams) {
+  if (warp < kLoadWarp && team < kTeams) {
 #pragma unroll
     for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -159,7 +174,7 @@ __global__ void __launch_bounds__(kThreads, 1) w4_kernel(const __grid_constant__
   }
   cluster_arrive();
   cluster_wait();
-  if (!*(volatile int*)&s_abort) w4_finish(a, xring, kPitch, kRows, block, rank, tok0, tokens, kTeams, C::kTokens);
+  if (!*(volatile int*)&s_abort) w4_finish(a, xring, kPitch, 16 * a.block_tiles, block, rank, tok0, tokens, kTeams, C::kTokens);
   cluster_arrive();  // the sums are read until here
   cluster_wait();
 }
@@ -198,8 +213,19 @@ cudaError_t launch_w4_t(W4Args a, cudaStream_t s) {
   if (e != cudaSuccess) return e;
   CUtensorMap tx;
   if (!make_tmap_2d(&tx, a.x, (uint64_t)a.M, (uint64_t)a.K, 64, C::kTokens)) return cudaErrorInvalidValue;
-  const int blocks = (a.N + kRows - 1) / kRows, toks = (a.M + C::kTokens - 1) / C::kTokens;
-  a.split = w4_split(kernel, (int64_t)blocks * toks, a.tiles, kThreads, smem);
+  // (rows that fill the GPU: 896 tiles of rows as 150 blocks of 6 instead of 112 of 8)
+  const int toks = (a.M + C::kTokens - 1) / C::kTokens;
+  W4Split best;
+  for (const int rows : {8, 6, 4}) {
+    const int64_t blocks = (int64_t)((a.row_tiles + rows - 1) / rows) * toks;
+    const W4Split s = w4_split(kernel, blocks, a.tiles, rows, kThreads, smem);
+    if (s.time < best.time) {
+      best = s;
+      a.block_tiles = rows;
+    }
+  }
+  a.split = best.split;
+  const int blocks = (a.row_tiles + a.block_tiles - 1) / a.block_tiles;
   return launch_cluster_kernel(kernel, dim3((unsigned)(blocks * a.split), (unsigned)toks), dim3(kThreads), (unsigned)a.split, smem, s, tx, a);
 }
 

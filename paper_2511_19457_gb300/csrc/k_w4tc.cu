@@ -270,7 +270,7 @@ cudaError_t launch_t(W4Args a, cudaStream_t s) {
   CUtensorMap tx;
   if (!make_tmap_2d(&tx, a.x, (uint64_t)a.M, (uint64_t)a.K, 64, NTOK)) return cudaErrorInvalidValue;
   const int blocks = (a.N + kRows - 1) / kRows, toks = (a.M + NTOK - 1) / NTOK;
-  a.split = w4_split(kernel, (int64_t)blocks * toks, a.tiles, kThreads, smem);
+  a.split = w4_split(kernel, (int64_t)blocks * toks, a.tiles, 8, kThreads, smem).split;
   return launch_cluster_kernel(kernel, dim3((unsigned)(blocks * a.split), (unsigned)toks), dim3(kThreads), (unsigned)a.split, smem, s, tx, a);
 }
 

@@ -375,7 +375,8 @@ struct W4Args {
   uint32_t* err = nullptr;
   long long wait_limit = 0;
   int fault = 0;  // error-path tests: 1 withholds the signals of the tcgen05 kernel's sums
-  int row_tiles = 0, tiles = 0, split = 1;  // tiles of rows and of columns, CTAs of a block's columns (set by launch_w4)
+  // tiles of rows and of columns, tiles of rows of a block, CTAs of its columns (set by launch_w4)
+  int row_tiles = 0, tiles = 0, block_tiles = 8, split = 1;
 };
 cudaError_t launch_w4(W4Args a, cudaStream_t s);
 
