@@ -1260,9 +1260,24 @@ def run_profile(args, rank, local_rank, world, peaks):
         r, y = torch.empty_like(x), torch.empty_like(h)
         n = sp.norm("rms", torch.ones(4096, device=dev))
         call = lambda: sp.sparoa_add_norm(ctx, x, h, r, y, pre=n)
-    elif op in ("rope_append", "paged_decode", "paged_chunk"):  # 32 query and 8 key heads of 128, pages of 64
-        new, kv = {"rope_append": ([8192], [8192]), "paged_decode": ([1] * 8, [16000] * 8),
-                   "paged_chunk": ([4000], [4000])}[op]
+    elif op in ("w4_16", "w4_64"):  # rows x 4096 x 14336 columns and rows of 4-bit weights, groups of 128
+        rows = int(op[3:])
+        codes = torch.randint(0, 256, (14336, 2048), device=dev, generator=gen, dtype=torch.uint8)
+        scales = torch.rand(14336, 32, device=dev, generator=gen).to(torch.bfloat16)
+        weights = sp.W4(ctx, codes, scales)
+        x = torch.randn(rows, 4096, device=dev, generator=gen).to(torch.bfloat16)
+        y = torch.empty(rows, 14336, dtype=torch.bfloat16, device=dev)
+        call = lambda: sp.sparoa_gemm_w4(ctx, x, weights, y)
+    elif op == "logits":  # [64, 128001] fp32, 3000 tokens seen a row, a mask
+        x = torch.randn(64, 128001, device=dev, generator=gen)
+        y, best, lse = torch.empty_like(x), torch.empty(64, dtype=torch.int32, device=dev), torch.empty(64, device=dev)
+        rules = sp.LogitRules(seen_start=torch.arange(65, dtype=torch.int32, device=dev) * 3000,
+                              seen=torch.randint(0, 128001, (64 * 3000,), device=dev, generator=gen, dtype=torch.int32),
+                              penalties=torch.tensor([[1.2, 0.1, 0.1, 0.8]] * 64, device=dev),
+                              allowed=torch.randint(-2 ** 31, 2 ** 31, (64, 4001), device=dev, generator=gen).int())
+        call = lambda: sp.sparoa_shape_logits(ctx, x, rules, y=y, best=best, lse=lse)
+    elif op in ("rope_append", "paged_decode", "paged_chunk", "capped_chunk", "distance_chunk"):  # 32 query and 8 key heads of 128, pages of 64
+        new, kv = {"rope_append": ([8192], [8192]), "paged_decode": ([1] * 8, [16000] * 8)}.get(op, ([4000], [4000]))
         per = -(-max(kv) // 64)
         cache = sp.KVCache(*(torch.randn(len(kv) * per, 8, 64, 128, device=dev, generator=gen).to(torch.bfloat16)
                              for _ in range(2)))
@@ -1277,7 +1292,12 @@ def run_profile(args, rank, local_rank, world, peaks):
             call = lambda: sp.sparoa_rope_append(ctx, qkv, q, cache, batch, rope)
         else:
             y = torch.empty_like(q)
-            call = lambda: sp.sparoa_paged_attention(ctx, q, y, cache, batch)
+            if op.startswith("paged"):
+                call = lambda: sp.sparoa_paged_attention(ctx, q, y, cache, batch)
+            else:
+                slopes = torch.exp2(-0.25 * torch.arange(1.0, 33.0, device=dev))
+                scores = sp.ScoreRules(cap=50.0) if op == "capped_chunk" else sp.ScoreRules(slopes=slopes)
+                call = lambda: sp.sparoa_ruled_attention(ctx, q, y, cache, batch, scores)
     else:
         raise SystemExit(f"profile: unknown op {op}")
     t0 = time.perf_counter()

@@ -552,7 +552,7 @@ sparoa_status sparoa_paged_attention(sparoa_ctx *ctx, const void *q, int64_t ld_
  * token t has position p = kv_len - n + t and sees the key at position j if j <= p (causal)
  * and j > p - window (window > 0).  What is NULL (0) is left out.
  *   cap     > 0 (from 0.001): a score s = scale q k becomes cap tanh(s / cap)
- *   slopes  device fp32 [heads]: then s - slopes[head] |p - j|
+ *   slopes  device fp32 [heads], finite: then s - slopes[head] |p - j|
  *   prefix  device int32 [batch]: with causal, keys j < prefix[b] are seen too, whatever
  *           the token's position (a prompt's first part that all of it sees)
  *   tree    device uint64 [T]: with causal, without prefix: a sequence's new tokens (at
@@ -571,7 +571,8 @@ typedef struct {
 
 /*
  * sparoa_paged_attention with score rules (NULL: none).  Everything said there holds,
- * with scores taken after the rules; lse is of those.  A sequence with a tree of more than
+ * with scores taken after the rules; lse is of those.  (With slopes, probabilities below
+ * 2^-60 of a row's largest may count as zero.)  A sequence with a tree of more than
  * 64 tokens is reported as INVALID_ARG by the next call that synchronises, and its rows
  * hold anything.
  * Errors: as sparoa_paged_attention; INVALID_ARG also for a tree or prefix without causal, or
@@ -629,7 +630,7 @@ typedef struct {
     const int32_t *seen;     /* device [n_seen] tokens; outside [0, V): no token */
     int64_t n_seen;
     const float *penalties;  /* device [R][4]: repetition, presence, frequency, temperature
-                                (repetition and temperature above 0)            */
+                                (finite, repetition and temperature above 0)    */
     const float *bias;       /* device [R][ld_bias], or one row with ld_bias 0  */
     int64_t ld_bias;
     const uint32_t *allowed; /* device [R][ld_allowed]: bit v % 32 of word v / 32 */
@@ -669,7 +670,8 @@ sparoa_status sparoa_shape_logits(sparoa_ctx *ctx, const void *logits, int64_t l
  *           order, the others -1
  *   count   device int32 [batch]: tokens of the path (0: no new tokens)
  *   following  device int32 [batch]: the choice after the path's last token (-1: none)
- *   new_len device int32 [batch]: tokens in the cache that stay; not kv_len itself
+ *   new_len device int32 [batch]: tokens in the cache that stay
+ * Outputs overlap no input, and no sequence's new places are another's.
  * The k-th token of the path moves to place kv_len - n + k; places at and after new_len
  * hold anything afterwards.  Lists out of bounds, trees of more than 64 tokens and bad pages are
  * reported as INVALID_ARG by the next call that synchronises; such a sequence (such a

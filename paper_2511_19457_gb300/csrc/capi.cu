@@ -1730,6 +1730,8 @@ sparoa_status sparoa_gemm_w4(sparoa_ctx* ctx, const void* x, int64_t M, const sp
     return fail(ctx, SPAROA_ERR_INVALID_ARG, "gemm_w4: tensors must be 16-byte aligned");
   if (y_dtype != SPAROA_BF16 && y_dtype != SPAROA_F32) return fail(ctx, SPAROA_ERR_INVALID_ARG, "gemm_w4: bad y_dtype");
   if (y_occ && y_dtype != SPAROA_BF16) return fail(ctx, SPAROA_ERR_UNSUPPORTED, "gemm_w4: occupancy of an fp32 output");
+  if (ep && ep->residual && ep->residual == y && y_dtype != SPAROA_BF16)
+    return fail(ctx, SPAROA_ERR_INVALID_ARG, "gemm_w4: an fp32 output in place of the residual");
   SP_TRY(check_ep(ctx, ep));
   SP_TRY(check_occ(ctx, y_occ, M, w->N, "gemm_w4 y_occ"));
   DeviceGuard g(ctx->device, ctx->overlap);
@@ -1811,9 +1813,14 @@ sparoa_status sparoa_tree_accept(sparoa_ctx* ctx, const int32_t* tokens, const i
         caches[i].head_dim != caches->head_dim)
       return fail(ctx, SPAROA_ERR_INVALID_ARG, "tree_accept: caches of different shapes");
   }
+  for (int i = 0; i < n_caches; ++i)
+    for (int j = 0; j <= i; ++j)
+      if (caches[i].k == caches[j].v || (j < i && (caches[i].k == caches[j].k || caches[i].v == caches[j].v || caches[i].v == caches[j].k)))
+        return fail(ctx, SPAROA_ERR_INVALID_ARG, "tree_accept: a pool twice");
   if (batch->max_q > kTreeTokens) return fail(ctx, SPAROA_ERR_UNSUPPORTED, "tree_accept: trees of at most %d tokens", kTreeTokens);
-  if ((T > 0 && (!tokens || !best || !tree || !path)) || !count || !following || !new_len || new_len == batch->kv_len)
-    return fail(ctx, SPAROA_ERR_INVALID_ARG, "tree_accept: NULL list, or new_len is kv_len");
+  if ((T > 0 && (!tokens || !best || !tree || !path)) || !count || !following || !new_len || new_len == batch->kv_len ||
+      (T > 0 && (path == tokens || path == best)))
+    return fail(ctx, SPAROA_ERR_INVALID_ARG, "tree_accept: NULL list, or a list in place of another");
   if (reinterpret_cast<uintptr_t>(tree) & 7u) return fail(ctx, SPAROA_ERR_INVALID_ARG, "tree_accept: misaligned");
   DeviceGuard g(ctx->device, ctx->overlap);
   TreeArgs a;

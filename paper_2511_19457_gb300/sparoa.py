@@ -425,7 +425,7 @@ def _want_rows(t, dtypes, what):
         _refuse(f"{what}: contiguous CUDA tensor of {dtypes} wanted")
 
 
-_bf16, _f32 = torch.bfloat16, torch.float32
+_bf16, _f32, _i32 = torch.bfloat16, torch.float32, torch.int32
 _BF16S = (torch.bfloat16,)
 _FP32S = (torch.float32,)
 _I32S = (torch.int32,)
@@ -712,8 +712,9 @@ def sparoa_gemm_w4(ctx: Context, x, w: W4, y, bias=None, bn=None, eps=1e-5, act=
     if residual is not None and not (residual.is_cuda and residual.dtype is _bf16 and residual.is_contiguous() and
                                      residual.numel() == M * w.N):
         _refuse("gemm_w4: residual bf16 of y's size")
+    plain = act == ACT_NONE and bias is None and bn is None and residual is None
     ctx._bind()
-    st = _gemm_w4(ctx.h, x.data_ptr(), M, w.ref, _byref(_epi(bias, bn, eps, act, residual)), y.data_ptr(),
+    st = _gemm_w4(ctx.h, x.data_ptr(), M, w.ref, None if plain else _byref(_epi(bias, bn, eps, act, residual)), y.data_ptr(),
                   F32 if y.dtype is _f32 else BF16, _occ(y_occ))
     if st:
         ctx._check(st)
@@ -755,6 +756,7 @@ def _logit_rows(t, R, V, what):
 def sparoa_shape_logits(ctx: Context, logits, rules: LogitRules | None = None, y=None, best=None, lse=None):
     """The rules over logits [R, V] (bf16 or fp32): y fp32 [R, V] (may be the logits), best int32 [R], lse fp32
     [R], each of them or None."""
+    _want(logits.dim() == 2, "shape_logits: logits [R, V]")
     R, V = logits.shape
     ld = _logit_rows(logits, R, V, "shape_logits logits")
     _want(logits.dtype in (_bf16, _f32), "shape_logits: bf16 or fp32 logits")
@@ -776,20 +778,18 @@ def sparoa_shape_logits(ctx: Context, logits, rules: LogitRules | None = None, y
         ctx._check(st)
 
 
-def _tree_bits(tree, T, what):
-    if not (tree.is_cuda and tree.dtype is torch.int64 and tree.is_contiguous() and tree.numel() == T):
-        _refuse(f"{what}: ancestors int64 [{T}] wanted")
-
-
 def sparoa_tree_accept(ctx: Context, tokens, best, tree, caches, batch: PagedBatch, path, count, following, new_len):
     """The path through each sequence's tree that the model's choices confirm; its keys and values move to the
     places that follow one another in all caches.  tokens, best, path int32 [T], tree int64 [T] (ancestor
     bits), count, following and new_len int32 [batch]."""
-    T, B = tokens.numel(), batch.kv_len.numel()
-    for t, n in ((tokens, T), (best, T), (path, T), (count, B), (following, B), (new_len, B)):
-        if not (t.is_cuda and t.dtype is torch.int32 and t.is_contiguous() and t.numel() == n):
-            _refuse("tree_accept: contiguous CUDA int32 lists of T or batch entries wanted")
-    _tree_bits(tree, T, "tree_accept")
+    T, B = tokens.numel(), batch.desc.batch
+    for t in (tokens, best, path, count, following, new_len):
+        if not (t.dtype is _i32 and t.is_cuda and t.is_contiguous()):
+            _refuse("tree_accept: contiguous CUDA int32 lists wanted")
+    if not (best.numel() == T == path.numel() and count.numel() == B == following.numel() == new_len.numel()):
+        _refuse("tree_accept: lists of T or batch entries wanted")
+    if not (tree.dtype is torch.int64 and tree.is_cuda and tree.is_contiguous() and tree.numel() == T):
+        _refuse("tree_accept: ancestors int64 [T] wanted")
     descs = (KvCacheDesc * len(caches))(*[c.desc for c in caches])
     ctx._bind()
     st = _tree_accept(ctx.h, tokens.data_ptr(), best.data_ptr(), tree.data_ptr(), T, descs, len(caches), batch.ref,

@@ -196,6 +196,40 @@ def test_long_contexts_are_split(sp, ctx):
     _run(sp, ctx, [1], [5000], 2, 1, 128, 64, slopes=True, window=3000, seed=3)
 
 
+def test_rows_of_no_sequence_are_left(sp, ctx):
+    for n in (2, 60):
+        cache, batch, *_ = _batch(sp, [n], [200], 32, 2, 64, 1)
+        start = batch.q_start + 3
+        batch = sp.PagedBatch(start, batch.kv_len, batch.table, n)
+        q = torch.randn(n + 8, 4, 64, generator=_g(2)).to(torch.bfloat16).cuda()
+        y, lse = torch.full_like(q, 9.0), torch.full((n + 8, 4), 9.0, device="cuda")
+        tree = torch.zeros(n + 8, dtype=torch.int64, device="cuda")
+        for rules in (sp.ScoreRules(cap=30.0), sp.ScoreRules(tree=tree)):
+            sp.sparoa_ruled_attention(ctx, q, y, cache, batch, rules, lse=lse)
+            ctx.sync()
+            for t in (y, lse):
+                assert (t[:3] == 9).all() and (t[n + 3:] == 9).all() and (t[3:n + 3] != 9).any()
+
+
+def test_far_keys_under_steep_slopes(sp, ctx):
+    """Keys whose bias is hundreds below the nearest ones' weigh nothing, and nothing of them is left in the
+    sums, whatever their values."""
+    for n in (1, 40, 300):
+        cache, batch, k, v, table = _batch(sp, [n], [1500], 64, 1, 64, 5)
+        slopes = torch.tensor([4.0, 0.3, 0.01])
+        q = torch.randn(n, 3, 64, generator=_g(6)).to(torch.bfloat16)
+        y, lse = torch.empty(n, 3, 64, dtype=torch.bfloat16, device="cuda"), torch.empty(n, 3, device="cuda")
+        sp.sparoa_ruled_attention(ctx, q.cuda(), y, cache, batch, sp.ScoreRules(slopes=slopes.cuda()), lse=lse)
+        some = sorted({0, n // 2, n - 1})
+        kk, vv = (torch.cat([pool[int(table[0, j]), 0] for j in range(24)])[:1500].double() for pool in (k, v))
+        for i in some:
+            p = 1500 - n + i
+            s = torch.einsum("hd,ld->hl", q[i].double(), kk[:p + 1]) / 8 - slopes.double()[:, None] * (p - torch.arange(p + 1))
+            w = torch.softmax(s, -1)
+            assert ((lse[i].double().cpu() - torch.logsumexp(s, -1)).abs() <= 2e-4).all()
+            _close(y[i], w @ vv[:p + 1], f"row {i} of {n}", extra=(2.0 ** -8 + 2.0 ** -12) * (w @ vv[:p + 1].abs()))
+
+
 def test_a_query_that_is_not_a_number(sp, ctx):
     """gives results that are none, its own only; under caps too."""
     for n in (2, 40):

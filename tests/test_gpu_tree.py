@@ -232,7 +232,10 @@ def test_refusals(sp, ctx):
         sp.sparoa_tree_accept(ctx, tokens, best, tree, caches, batch, path, count, following, length)
 
     bad = [{"tree": t.int()}, {"tree": t[:7]}, {"best": i(7)}, {"tokens": t}, {"count": i(3)}, {"length": batch.kv_len}, {"caches": ()},
-           {"caches": (cache, other)}, {"caches": (cache,) * 129}, {"batch": sp.PagedBatch(i(3), i(2), i(2, 4), max_q=65)}, {"path": i(16)[::2]}]
+           {"caches": (cache, other)}, {"caches": (cache,) * 129}, {"batch": sp.PagedBatch(i(3), i(2), i(2, 4), max_q=65)}, {"path": i(16)[::2]}, {"caches": (cache, cache)}, {"caches": (sp.KVCache(cache.k, cache.k),)},
+           {"caches": (cache, sp.KVCache(other.k[:4], cache.v))}]
+    same = i(8)
+    bad += [{"tokens": same, "path": same}, {"best": same, "path": same}]
     for kw in bad:
         with pytest.raises(sp.SparoaError):
             call(**kw)

@@ -210,6 +210,58 @@ def test_waits_end(sp):
     ctx.close()
 
 
+def test_a_missing_signal_is_reported(sp):
+    """The tensor cores' signal withheld: the wait for it gives up, the call is reported, and the next one works."""
+    ctx = sp.Context(0)
+    x, codes, scales, _ = _inputs(40, 1024, 256, 128, False)
+    w = sp.W4(ctx, codes.cuda(), scales.cuda())
+    y = torch.full((40, 256), 7.0, device="cuda")
+    ctx.sync()
+    ctx.set_wait_limit(20_000_000)
+    ctx.set_fault(1)
+    sp.sparoa_gemm_w4(ctx, x.cuda(), w, y)
+    with pytest.raises(sp.SparoaError) as e:
+        ctx.sync()
+    assert e.value.status == sp.ERR_TIMEOUT
+    assert (y == 7).all()  # (nothing is written without sums)
+    ctx.set_fault(0)
+    ctx.set_wait_limit(0)
+    sp.sparoa_gemm_w4(ctx, x.cuda(), w, y)
+    ctx.sync()
+    w64 = _weights64(codes, scales, None, 128)
+    _check(y, x.double() @ w64.t(), _bound(x, w64, 128), False, "after a missing signal")
+    ctx.close()
+
+
+@pytest.mark.parametrize("M", [5, 50])
+def test_two_streams_at_once(sp, ctx, M):
+    """Calls of one context on two streams whose work overlaps: nothing is shared between them."""
+    K, N = 2048, 4096
+    x, codes, scales, _ = _inputs(M, K, N, 64, False)
+    w = sp.W4(ctx, codes.cuda(), scales.cuda())
+    x2 = torch.randn(M, K, generator=torch.Generator().manual_seed(4)).to(torch.bfloat16)
+    jobs = [(v, v.cuda(), torch.empty(M, N, device="cuda"), torch.cuda.Stream()) for v in (x, x2)]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for _, v, y, st in jobs:
+            with torch.cuda.stream(st):
+                sp.sparoa_gemm_w4(ctx, v, w, y)
+    torch.cuda.synchronize()
+    w64 = _weights64(codes, scales, None, 64)
+    for v, _, y, _ in jobs:
+        _check(y, v.double() @ w64.t(), _bound(v, w64, 64), False, "streams")
+
+
+def test_rows_behind_are_left(sp, ctx):
+    """Results of fewer rows than a tile of tokens write nothing else."""
+    for M in (3, 20):
+        x, codes, scales, _ = _inputs(M, 256, 72, 32, False)
+        w = sp.W4(ctx, codes.cuda(), scales.cuda())
+        whole = torch.full((M + 4, 72), 9.0, device="cuda")
+        sp.sparoa_gemm_w4(ctx, x.cuda(), w, whole[:M])
+        assert (whole[M:] == 9).all() and (whole[:M] != 9).all()
+
+
 def test_refusals(sp, ctx):
     x, codes, scales, zero = (None if t is None else t.cuda() for t in _inputs(4, 256, 64, 64, True))
     w = sp.W4(ctx, codes, scales, zero)
