@@ -60,11 +60,12 @@ __global__ void __launch_bounds__(kThreads, 1) w4_kernel(const __grid_constant__
   // fourth warp)
   const int team = warp / a.block_tiles, mine = warp % a.block_tiles;
   constexpr int kLoadWarp = kTeams * kWarps;
+  const int first = block * a.block_tiles, rows = min(a.block_tiles, a.row_tiles - first);  // the CTA's tiles of rows
   const long long limit = a.wait_limit ? a.wait_limit : kWaitLimitCycles;
   if (threadIdx.x == 0) {
     for (int i = 0; i < kStages; ++i) {
       mbar_init(smem_u32(&s_full[i]), 2u);
-      mbar_init(smem_u32(&s_empty[i]), kTeams * kWarps);
+      mbar_init(smem_u32(&s_empty[i]), (uint32_t)(kTeams * rows));
     }
     fence_mbar_init();
     s_abort = 0;
@@ -77,51 +78,64 @@ __global__ void __launch_bounds__(kThreads, 1) w4_kernel(const __grid_constant__
 #pragma unroll
   for (int n = 0; n < NT; ++n) acc[n][0] = acc[n][1] = acc[n][2] = acc[n][3] = 0.f;
   const int stages = (count + kTeams - 1) / kTeams;
-  const int first = block * a.block_tiles, rows = min(a.block_tiles, a.row_tiles - first);  // the CTA's tiles of rows
   const int in_block = first % 8 ? 0 : min(8, a.row_tiles - first);                          // of the layout's block from there
   if (warp >= kLoadWarp) {
-    // (the copies of a stage take a warp 100 cycles each to give out: as few as there can be, by two warps)
-    int s = 0;
-    for (; s < stages; ++s) {
-      const int st = s % kStages, t = s * kTeams, there = min(kTeams, count - t);
-      if (!mbar_wait_warp(smem_u32(&s_empty[st]), (s / kStages + 1) & 1u, a.err, &s_abort, kErrTimeoutEmpty, limit)) break;
-      if (lane == 0) {
-        const uint32_t bar = smem_u32(&s_full[st]);
-        if (warp == kLoadWarp) {
-          mbar_arrive_expect_tx(bar, (uint32_t)(there * rows * tile));
-          const uint32_t to = ring + st * kTeams * kWarps * tile;
-          if (rows == in_block) {  // whole blocks of the layout: tiles of columns side by side, too
-            bulk_load(to, a.w + w4_tile_at(first, t0 + t, a.row_tiles, a.tiles) * tile, (uint32_t)(there * rows * tile), bar);
-          } else {
-            const int head = min(rows, 8 - first % 8);  // rows up to the next block
-            for (int i = 0; i < there; ++i) {
-              bulk_load(to + i * rows * tile, a.w + w4_tile_at(first, t0 + t + i, a.row_tiles, a.tiles) * tile, (uint32_t)(head * tile), bar);
-              if (head < rows)
-                bulk_load(to + (i * rows + head) * tile, a.w + w4_tile_at(first + head, t0 + t + i, a.row_tiles, a.tiles) * tile,
-                          (uint32_t)((rows - head) * tile), bar);
-            }
-          }
+    // A copy takes 200 cycles and more to give out, so there are as few as can be, by two warps: one has the
+    // first tile's codes (all tiles', where they lie side by side), the other x and the second tile's.  One
+    // lane of each, asleep while it waits.
+    if (lane == 0) {
+      const bool whole = rows == in_block, codes = warp == kLoadWarp;
+      const int head = min(rows, 8 - first % 8);  // rows up to the layout's next block
+      const uint32_t head_bytes = (uint32_t)(head * tile), tail_bytes = (uint32_t)((rows - head) * tile);
+      const int64_t step = (int64_t)min(8, a.row_tiles - first / 8 * 8) * tile, step2 = (int64_t)min(8, a.row_tiles - first - head) * tile;
+      const uint8_t* from = a.w + w4_tile_at(first, t0, a.row_tiles, a.tiles) * tile;
+      const uint8_t* from2 = head < rows ? a.w + w4_tile_at(first + head, t0, a.row_tiles, a.tiles) * tile : from;
+      int s = 0;
+      for (; s < stages; ++s, from += kTeams * step, from2 += kTeams * step2) {
+        const int st = s % kStages, t = s * kTeams, there = min(kTeams, count - t);
+        if (!mbar_wait(smem_u32(&s_empty[st]), (s / kStages + 1) & 1u, a.err, &s_abort, kErrTimeoutEmpty, limit)) break;
+        const uint32_t bar = smem_u32(&s_full[st]), to = ring + st * kTeams * kWarps * tile;
+        auto tile_codes = [&](int i) {
+          bulk_load(to + i * rows * tile, from + i * step, head_bytes, bar);
+          if (tail_bytes) bulk_load(to + i * rows * tile + head_bytes, from2 + i * step2, tail_bytes, bar);
+        };
+        if (codes) {
+          const uint32_t bytes = (uint32_t)((whole ? there : 1) * rows * tile);
+          mbar_arrive_expect_tx(bar, bytes);
+          if (whole)
+            bulk_load(to, from, bytes, bar);
+          else
+            tile_codes(0);
         } else {
-          mbar_arrive_expect_tx(bar, there * 2u * C::kHalf);
-          for (int i = 0; i < 2 * there; ++i)
-            tma_load_2d(xring + (st * kTeams * 2 + i) * C::kHalf, &tx, bar, (t0 + t) * kTileK + i * 64, tok0);
+          const bool second = !whole && there > 1;
+          const int boxes = a.x_boxed ? 2 * kTeams : 2 * there;  // of 64 columns
+          mbar_arrive_expect_tx(bar, (uint32_t)(boxes * C::kHalf + (second ? rows * tile : 0)));
+          const uint32_t xto = xring + st * kTeams * 2 * C::kHalf;
+          if (a.x_boxed)
+            tma_load_3d(xto, &tx, bar, 0, tok0, 2 * (t0 + t));
+          else
+            for (int i = 0; i < boxes; ++i) tma_load_2d(xto + i * C::kHalf, &tx, bar, (t0 + t) * kTileK + i * 64, tok0);
+          if (second) tile_codes(1);
         }
       }
-      __syncwarp();
+      // after a timeout: no copy is in flight into shared memory that is given back (where the other warp
+      // gave out none, this waits its limit)
+      if (*(volatile int*)&s_abort)
+        for (int i = s > kStages ? s - kStages : 0; i < s; ++i) mbar_drain(smem_u32(&s_full[i % kStages]), (i / kStages) & 1u, limit);
     }
-    // after a timeout: no copy is in flight into shared memory that is given back (where the other warp
-    // gave out none, this waits its limit)
-    if (*(volatile int*)&s_abort)
-      for (int i = s > kStages ? s - kStages : 0; i < s; ++i) mbar_drain(smem_u32(&s_full[i % kStages]), (i / kStages) & 1u, limit);
-  } else {
-    const int token = (g >> 1) + (g & 1) * 4;
+    __syncwarp();
+  } else if (team < kTeams && mine < rows) {
+    // byte of the lane's 16 of x in columns 0 to 31 of 64 (64 further, by the swizzle, in the others), and of
+    // its piece of row g
+    const uint32_t token = (g >> 1) + (g & 1) * 4, x_at = swz_offset<64>(token, tq), w_at = w4_piece(g, tq);
     for (int s = 0; s < stages; ++s) {
       const int st = s % kStages;
       if (!mbar_wait_warp(smem_u32(&s_full[st]), (s / kStages) & 1u, a.err, &s_abort, kErrTimeoutFull, limit)) break;
-      if (team < kTeams && s * kTeams + team < count && mine < rows) {
-        const uint32_t x = xring + (st * kTeams + team) * 2 * C::kHalf, w = ring + (st * kTeams * kWarps + team * rows + mine) * tile;
+      if (s * kTeams + team < count) {  // (but for the last stage's other tiles)
+        const uint32_t x = xring + (st * kTeams + team) * 2 * C::kHalf + x_at, x_odd = x ^ 64u;
+        const uint32_t w = ring + (st * kTeams * kWarps + team * rows + mine) * tile;
         const uint32_t meta = w + 1024 + g * 2;
-        const uint4 c0 = lds_u4(w + w4_piece(g, tq)), c1 = lds_u4(w + w4_piece(g + 8, tq));
+        const uint4 c0 = lds_u4(w + w_at), c1 = lds_u4(w + w_at + 512);
 #pragma unroll
         for (int gi = 0; gi < GROUPS; ++gi) {
           float part[NT][4];
@@ -139,7 +153,7 @@ __global__ void __launch_bounds__(kThreads, 1) w4_kernel(const __grid_constant__
             const uint32_t f1[4] = {w4_pair(w0, 2, z0), w4_pair(w1, 2, z1), w4_pair(w0, 3, z0), w4_pair(w1, 3, z1)};
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
-              const uint4 v = lds_u4(x + (j >> 1) * C::kHalf + swz_offset<64>(n * 8 + token, (j & 1) * 4 + tq));
+              const uint4 v = lds_u4((j & 1 ? x_odd : x) + (j >> 1) * C::kHalf + n * 1024);
               if (j == gi * 4 / GROUPS)
                 mma16816_first(part[n], f0, v.x, v.y);
               else
@@ -163,7 +177,7 @@ __global__ void __launch_bounds__(kThreads, 1) w4_kernel(const __grid_constant__
   }
   // the CTA's sums [tokens][rows], where x was (every copy has arrived)
   __syncthreads();
-  if (warp < kLoadWarp && team < kTeams) {
+  if (warp < kLoadWarp && team < kTeams && mine < rows) {
 #pragma unroll
     for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -212,7 +226,7 @@ cudaError_t launch_w4_t(W4Args a, cudaStream_t s) {
   const cudaError_t e = smem_optin(reinterpret_cast<const void*>(kernel), smem);
   if (e != cudaSuccess) return e;
   CUtensorMap tx;
-  if (!make_tmap_2d(&tx, a.x, (uint64_t)a.M, (uint64_t)a.K, 64, C::kTokens)) return cudaErrorInvalidValue;
+  if (!w4_x_map(&tx, &a, C::kTokens, 2 * kTeams)) return cudaErrorInvalidValue;
   // (rows that fill the GPU: 896 tiles of rows as 150 blocks of 6 instead of 112 of 8)
   const int toks = (a.M + C::kTokens - 1) / C::kTokens;
   W4Split best;
@@ -243,6 +257,12 @@ uint64_t w4_packed_bytes(int64_t N, int64_t K, int group, bool zeros) {
 cudaError_t launch_w4_pack(const W4PackArgs& a, cudaStream_t s) {
   const int64_t tiles = (int64_t)((a.N + 15) / 16) * ((a.K + kTileK - 1) / kTileK);
   return launch_kernel(w4_pack_kernel, dim3((unsigned)tiles), dim3(256), 0, s, a);
+}
+
+bool w4_x_map(CUtensorMap* m, W4Args* a, int tokens, int halves) {
+  a->x_boxed = a->K % 64 == 0;
+  if (!a->x_boxed) return make_tmap_2d(m, a->x, (uint64_t)a->M, (uint64_t)a->K, 64, (uint32_t)tokens);
+  return make_tmap_3d(m, a->x, 64, (uint64_t)a->M, (uint64_t)(a->K / 64), (uint64_t)a->K, 64, 64, (uint32_t)tokens, (uint32_t)halves);
 }
 
 cudaError_t launch_w4(W4Args a, cudaStream_t s) {

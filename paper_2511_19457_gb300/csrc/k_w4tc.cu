@@ -196,27 +196,31 @@ __global__ void __launch_bounds__(kThreads, 1) w4_tc_kernel(const __grid_constan
       const int mine = min(8, a.row_tiles - block * 8);  // tiles of rows that there are
       const uint32_t bytes = (uint32_t)(mine * tile);
       const uint8_t* from = a.w + w4_tile_at(block * 8, t0, a.row_tiles, a.tiles) * tile;
-      int t = 0;
-      for (; t < count; ++t, from += bytes) {
-        const int st = t % kStages;
-        if (!mbar_wait_warp(smem_u32(&bars.empty[st]), (t / kStages + 1) & 1u, a.err, &s_abort, kErrTimeoutEmpty, limit)) break;
-        const uint32_t bar = smem_u32(&bars.full[st]);
-        if (lane == 0) {
+      if (lane == 0) {  // (asleep while it waits)
+        int t = 0;
+        for (; t < count; ++t, from += bytes) {
+          const int st = t % kStages;
+          if (!mbar_wait(smem_u32(&bars.empty[st]), (t / kStages + 1) & 1u, a.err, &s_abort, kErrTimeoutEmpty, limit)) break;
+          const uint32_t bar = smem_u32(&bars.full[st]);
           if (warp == kLoadWarp) {
             mbar_arrive_expect_tx(bar, bytes);
             bulk_load(ring + st * 8 * tile, from, bytes, bar);
           } else {
             mbar_arrive_expect_tx(bar, 2u * C::kHalf);
-            tma_load_2d(xring + st * 2 * C::kHalf, &tx, bar, (t0 + t) * kTileK, tok0);
-            tma_load_2d(xring + (st * 2 + 1) * C::kHalf, &tx, bar, (t0 + t) * kTileK + 64, tok0);
+            if (a.x_boxed) {
+              tma_load_3d(xring + st * 2 * C::kHalf, &tx, bar, 0, tok0, 2 * (t0 + t));
+            } else {
+              tma_load_2d(xring + st * 2 * C::kHalf, &tx, bar, (t0 + t) * kTileK, tok0);
+              tma_load_2d(xring + (st * 2 + 1) * C::kHalf, &tx, bar, (t0 + t) * kTileK + 64, tok0);
+            }
           }
         }
-        __syncwarp();
+        // after a timeout: no copy is in flight into shared memory that is given back (the other warp's
+        // copies of a stage may be missing: then this waits its limit)
+        if (*(volatile int*)&s_abort)
+          for (int i = t > kStages ? t - kStages : 0; i < t; ++i) mbar_drain(smem_u32(&bars.full[i % kStages]), (i / kStages) & 1u, limit);
       }
-      // after a timeout: no copy is in flight into shared memory that is given back (the other warp's
-      // copies of a stage may be missing: then this waits its limit)
-      if (*(volatile int*)&s_abort && warp == kLoadWarp)
-        for (int i = t > kStages ? t - kStages : 0; i < t; ++i) mbar_drain(smem_u32(&bars.full[i % kStages]), (i / kStages) & 1u, limit);
+      __syncwarp();
     } else if (warp == kMmaWarp) {
       const bool leader = elect_one();
       constexpr uint32_t id = idesc_bf16_f32(kRows, NTOK);
@@ -268,7 +272,7 @@ cudaError_t launch_t(W4Args a, cudaStream_t s) {
   const cudaError_t e = smem_optin(reinterpret_cast<const void*>(kernel), smem);
   if (e != cudaSuccess) return e;
   CUtensorMap tx;
-  if (!make_tmap_2d(&tx, a.x, (uint64_t)a.M, (uint64_t)a.K, 64, NTOK)) return cudaErrorInvalidValue;
+  if (!w4_x_map(&tx, &a, NTOK, 2)) return cudaErrorInvalidValue;
   const int blocks = (a.N + kRows - 1) / kRows, toks = (a.M + NTOK - 1) / NTOK;
   a.split = w4_split(kernel, (int64_t)blocks * toks, a.tiles, 8, kThreads, smem).split;
   return launch_cluster_kernel(kernel, dim3((unsigned)(blocks * a.split), (unsigned)toks), dim3(kThreads), (unsigned)a.split, smem, s, tx, a);

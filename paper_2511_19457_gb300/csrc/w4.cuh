@@ -119,6 +119,9 @@ W4Split w4_split(void (*kernel)(KArgs...), int64_t blocks, int tiles, int weight
   }
   return best;
 }
+// x for TMA, in boxes of `tokens` rows: of 64 columns, or where a row is whole 64s (a->x_boxed) of
+// `halves` times 64 at once, which lie in shared memory as that many boxes would.
+bool w4_x_map(CUtensorMap* m, W4Args* a, int tokens, int halves);
 cudaError_t launch_w4_tc(const W4Args& a, cudaStream_t s);  // (k_w4tc.cu)
 
 }  // namespace sparoa
