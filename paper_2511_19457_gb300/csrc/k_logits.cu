@@ -8,7 +8,16 @@
 // out.  A row is a cluster's: every CTA counts the list's tokens of its share of the
 // vocabulary in shared memory, walks its logits once with a running maximum and sum, and
 // the first CTA joins what they found in the order of the tokens.  Lanes take neighbouring
-// tokens, so no row needs an alignment, and a word of the mask is a warp's.
+// tokens, so no row needs an alignment, and a word of the mask is a warp's (one lane loads
+// it for all).  The next kItems logits of a thread are on their way while these are worked
+// on, and go past the caches as what is not read again (22.3 -> 20.4 us at the size below).
+//
+// [64, 128001] fp32 with 3000 tokens seen a row, a bias and masks, all of it from memory:
+// 20.4 us, 3.3 TB/s (a plain copy of the size 11.7); 18.0 without lists, of which a CTA's
+// count is 2 us before its walk; 14 where the L2 has the logits.  In four CTAs an SM there
+// are two batches in flight at most: the rest is the walk's instructions, 25 a token.
+// Tried: the share into the L2 at first (24.1), 4 or 16 logits at once (23.6, 29.5), 512
+// threads (27.7), three CTAs an SM with more registers (29.9), no exponentials (20.1).
 #include <cfloat>
 
 #include "sparoa_kernels.h"
@@ -54,8 +63,8 @@ __device__ __forceinline__ Found from_lane(const Found& f, int d) {
   return o;
 }
 
-__device__ __forceinline__ float load_logit(const float* p) { return *p; }
-__device__ __forceinline__ float load_logit(const __nv_bfloat16* p) { return __bfloat162float(*p); }
+__device__ __forceinline__ float load_logit(const float* p) { return __ldcs(p); }
+__device__ __forceinline__ float load_logit(const __nv_bfloat16* p) { return __bfloat162float(__ldcs(p)); }
 
 enum Parts : int { kSeen = 1, kBiased = 2, kMasked = 4, kStored = 8 };  // what a kernel does besides
 
@@ -77,20 +86,27 @@ struct Share {
 // kItems tokens of a thread, kThreads apart, from token v0 of the share on.  FULL: all are there.
 template <int PARTS, bool FULL, typename XT>
 struct Batch {
-  float z[kItems], b[kItems];
-  uint32_t open[kItems];
+  float b[kItems];
+  uint32_t open;  // lane u: the word of token u
 
   static __device__ __forceinline__ bool there(const Share<XT>& s, int v) { return FULL || v + (int)threadIdx.x < s.len; }
-  __device__ __forceinline__ void fetch(const Share<XT>& s, int v0) {
+  static __device__ __forceinline__ void fetch(const Share<XT>& s, int v0, float (&z)[kItems]) {
 #pragma unroll
     for (int u = 0; u < kItems; ++u) {
       const int v = v0 + u * kThreads;
       z[u] = there(s, v) ? load_logit(s.x + v) : -INFINITY;
-      if ((PARTS & kBiased) != 0) b[u] = there(s, v) ? s.bias[v] : 0.f;
-      if ((PARTS & kMasked) != 0) open[u] = there(s, v) ? s.allowed[v >> 5] : 0u;
     }
   }
-  __device__ __forceinline__ void penalise(const Share<XT>& s, int v0) {
+  __device__ __forceinline__ void rules(const Share<XT>& s, int v0) {
+    const int lane = threadIdx.x & 31, v1 = v0 + lane * kThreads;
+    if ((PARTS & kMasked) != 0) open = lane < kItems && (FULL || v1 + (int)(threadIdx.x & ~31u) < s.len) ? s.allowed[v1 >> 5] : 0u;
+#pragma unroll
+    for (int u = 0; u < kItems; ++u) {
+      const int v = v0 + u * kThreads;
+      if ((PARTS & kBiased) != 0) b[u] = there(s, v) ? s.bias[v] : 0.f;
+    }
+  }
+  __device__ __forceinline__ void penalise(const Share<XT>& s, int v0, float (&z)[kItems]) {
     unsigned c[kItems], any = 0u;
 #pragma unroll
     for (int u = 0; u < kItems; ++u) {
@@ -109,7 +125,7 @@ struct Batch {
       z[u] = c[u] ? less : z[u];
     }
   }
-  __device__ __forceinline__ void finish(const Share<XT>& s, int v0, Found& f) {
+  __device__ __forceinline__ void finish(const Share<XT>& s, int v0, float (&z)[kItems], Found& f) {
     const uint32_t bit = 1u << (threadIdx.x & 31);
     float top = -INFINITY;
 #pragma unroll
@@ -121,7 +137,7 @@ struct Batch {
 #pragma unroll
     for (int u = 0; u < kItems; ++u) {
       const int v = v0 + u * kThreads;
-      if ((PARTS & kMasked) != 0) z[u] = open[u] & bit ? z[u] : -INFINITY;
+      if ((PARTS & kMasked) != 0) z[u] = __shfl_sync(0xffffffffu, open, u) & bit ? z[u] : -INFINITY;
       if ((PARTS & kStored) != 0 && there(s, v)) s.y[v] = z[u];
       top = fmaxf(top, z[u]);  // (a number that is none is never the largest)
     }
@@ -193,9 +209,9 @@ __global__ void __launch_bounds__(kThreads, 4) logits_kernel(const __grid_consta
     if ((PARTS & kBiased) != 0) s.bias = a.bias + r * a.ld_bias + at;
     if ((PARTS & kMasked) != 0) s.allowed = a.allowed + r * a.ld_allowed + (at >> 5);
     if ((PARTS & kStored) != 0) s.y = a.y + r * a.ld_y + at;
-    Batch<PARTS, false, XT> first;
+    float z[kItems];
+    Batch<PARTS, false, XT>::fetch(s, 0, z);  // on its way while the tokens are counted
     if (seen) {
-      first.fetch(s, 0);  // on its way while the tokens are counted
       __syncthreads();    // (the counts before were read)
       for (int i = threadIdx.x; i < (s.len + (s.wide ? 3 : 7)) / (s.wide ? 4 : 8); i += kThreads)
         reinterpret_cast<uint4*>(s_count)[i] = make_uint4(0u, 0u, 0u, 0u);
@@ -210,21 +226,26 @@ __global__ void __launch_bounds__(kThreads, 4) logits_kernel(const __grid_consta
           if (t[k] < (unsigned)s.len) atomicAdd(s_count + (s.wide ? t[k] : t[k] >> 1), !s.wide && (t[k] & 1u) ? 0x10000u : 1u);
       }
       __syncthreads();
-      first.penalise(s, 0);
-      first.finish(s, 0, f);
     }
-    int v0 = seen ? kStep : 0;
+    int v0 = 0;
     for (; v0 + kStep <= s.len; v0 += kStep) {
       Batch<PARTS, true, XT> batch;
-      batch.fetch(s, v0);
-      if (seen) batch.penalise(s, v0);
-      batch.finish(s, v0, f);
+      batch.rules(s, v0);
+      float next[kItems];
+      if (v0 + 2 * kStep <= s.len)
+        Batch<PARTS, true, XT>::fetch(s, v0 + kStep, next);
+      else
+        Batch<PARTS, false, XT>::fetch(s, v0 + kStep, next);
+      if (seen) batch.penalise(s, v0, z);
+      batch.finish(s, v0, z, f);
+#pragma unroll
+      for (int u = 0; u < kItems; ++u) z[u] = next[u];
     }
     if (v0 < s.len) {
       Batch<PARTS, false, XT> batch;
-      batch.fetch(s, v0);
-      if (seen) batch.penalise(s, v0);
-      batch.finish(s, v0, f);
+      batch.rules(s, v0);
+      if (seen) batch.penalise(s, v0, z);
+      batch.finish(s, v0, z, f);
     }
   }
 #pragma unroll
