@@ -458,6 +458,17 @@ __device__ __forceinline__ void maxima(const uint32_t (&s)[4][32], float (&mx)[4
 }
 __device__ __forceinline__ float largest(const float (&mx)[4]) { return fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])); }
 
+// The largest of three numbers (of their sizes), or none if one is none.
+template <bool SIZES>
+__device__ __forceinline__ float max3_nan(float a, float b, float c) {
+  float m;
+  if constexpr (SIZES)
+    asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(m) : "f"(a), "f"(b), "f"(c));
+  else
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(m) : "f"(a), "f"(b), "f"(c));
+  return m;
+}
+
 __device__ __forceinline__ f2_t pair_at(const uint32_t (&s)[32], int k) { return f2(__uint_as_float(s[k]), __uint_as_float(s[k + 1])); }
 __device__ __forceinline__ void put_pair(uint32_t (&s)[32], int k, f2_t v) {
   float x, y;
@@ -578,24 +589,23 @@ __device__ __forceinline__ float changed_unit(const PagedArgs& a, const RowRules
       float t[4];
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        auto of = [&](int at) { return caps ? fabsf(__uint_as_float(s[at])) : __uint_as_float(s[at]); };
-        t[k] = of(8 * k);
-#pragma unroll
-        for (int e = 1; e < 7; e += 2) t[k] = fmaxf(t[k], fmaxf(of(8 * k + e), of(8 * k + e + 1)));
-        t[k] = fmaxf(t[k], of(8 * k + 7));
+        auto at = [&](int e) { return __uint_as_float(s[8 * k + e]); };
+        auto more = [&](float x, int e, int f) { return caps ? max3_nan<true>(x, at(e), at(f)) : max3_nan<false>(x, at(e), at(f)); };
+        t[k] = more(more(more(more(at(0), 1, 2), 3, 4), 5, 6), 7, 7);
       }
-      float top = largest(t);
-      size = fmaxf(size, top);
+      float top = max3_nan<false>(max3_nan<false>(t[0], t[1], t[2]), t[3], t[3]);
+      size = max3_nan<false>(size, top, top);
       if (slopes) {
         // (a slope may put the bound of 32 scores kSlackLog2 too high)
         top = (caps ? Capped(a).near1(top) : top * a.score_log2) + u.slope * ((float)(i * 32) - far) + fmaxf(u.slope * 31.f, 0.f);
-        bound = fmaxf(bound, top);
+        bound = max3_nan<false>(bound, top, top);
       }
     }
     if (caps) near = __all_sync(0xffffffffu, Capped(a).near(size));
     direct = direct && near;
     mx = slopes ? bound : Capped(a).near1(size);
-    // too far away for any weight of the unit
+    // too far away for any weight of the unit (a score that is no number has one all the same, and is
+    // carried through the maxima for that)
     if (slopes && bounded && near && !first && __all_sync(0xffffffffu, mx < m - kGoneLog2)) {
       const uint32_t none[16] = {};
 #pragma unroll

@@ -381,8 +381,8 @@ struct RowRules {
   }
   // no row: sees what it likes, for its results go nowhere
   __device__ __forceinline__ void none() {
-    pos = low = base = 0;
-    lim = 0x7FFFFFFF;
+    pos = low = 0;
+    lim = base = 0x7FFFFFFF;
     tree = 0ull;
     slope = 0.f;
   }

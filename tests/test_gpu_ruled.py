@@ -242,6 +242,22 @@ def test_a_query_that_is_not_a_number(sp, ctx):
         assert bad[1, 2].all() and int(bad.sum()) == 64
 
 
+@pytest.mark.parametrize("n", [1, 40, 300])
+@pytest.mark.parametrize("cap", [0.0, 30.0, 200.0])
+def test_a_key_that_is_not_a_number(sp, ctx, n, cap):
+    """makes results none wherever it is seen, however far away: a bias does not hide it."""
+    cache, batch, k, v, table = _batch(sp, [n], [1500], 64, 1, 64, 5)
+    cache.k[int(table[0, 0]), 0, 9, 3] = float("nan")  # the key at position 9
+    q = torch.randn(n, 3, 64, generator=_g(6)).to(torch.bfloat16).cuda()
+    y, lse = torch.empty_like(q), torch.empty(n, 3, device="cuda")
+    slopes = torch.tensor([4.0, 0.3, 0.01], device="cuda")
+    for window in (0, 1400):
+        sp.sparoa_ruled_attention(ctx, q, y, cache, batch, sp.ScoreRules(cap=cap, slopes=slopes), window=window, lse=lse)
+        sees = torch.arange(1500 - n, 1500, device="cuda") < 9 + (window or 1500)
+        assert y[sees].isnan().all() and lse[sees].isnan().all()
+        assert y[~sees].isfinite().all() and lse[~sees].isfinite().all()
+
+
 def test_graph_follows_its_lists(sp):
     """Another tree, other lengths and queries than those captured."""
     c = sp.Context(0)
