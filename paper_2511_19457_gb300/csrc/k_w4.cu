@@ -3,12 +3,19 @@
 //
 // Bound by the bytes of the weights, half a byte each and read once, and nearly as much by the instructions
 // that make numbers of the codes (11 for 8 codes, 2 cycles each).  A CTA has 64, 96 or 128 rows of W over
-// its share of the columns, 16 a warp, as they fill the GPU best (w4_split); the rows' tiles of the same columns come in one copy (w4.cuh;
-// a copy for each took 44 cycles more of the copy unit, and there are eight), kStages of them on their way, with x beside
-// them by TMA.  A code becomes the bf16 number 128 + code
-// by one logic operation, 128 + zero is taken away, which is exact, and mma.sync m16n8k16 sums the
-// products with x in fp32 over a group; only that sum is multiplied by the scale.  So nothing is
-// rounded before the result but fp32 sums.
+// its share of the columns, 16 a warp, as they fill the GPU best (w4_split); a warp's teammate has the same
+// rows of every other tile of columns.  The rows' tiles of two tiles of columns come in one copy (w4.cuh; a
+// copy each took 44 cycles more of the copy unit, and there would be sixteen), kStages of them on their way,
+// with x beside them by TMA.  A code becomes the bf16 number 128 + code by one logic operation, 128 + zero is
+// taken away, which is exact, and mma.sync m16n8k16 sums the products with x in fp32 over a group; only that
+// sum is multiplied by the scale.  So nothing is rounded before the result but fp32 sums.
+//
+// 16 tokens x 4096 columns x 14336 rows, groups of 128, from memory: 14.7 us, 2.1 TB/s.  The copies alone
+// (no product, no numbers made of codes) 10.5, without the numbers of codes 13, without the products 15: half
+// of it is a launch, the first bytes' way and the cluster's sum (4.5 us for 2048 x 2048), and the rest waits
+// on issue slots (48 % busy) and the logic pipe (49 %).  Tried: weights straight from memory to registers,
+// without copies (slower), 24 warps of three teams (slower), shifts as multiplications (slower), the weights
+// into the L2 before the kernel before ends (16.4), no teams (24.6).
 #include "w4.cuh"
 
 namespace sparoa {
@@ -78,7 +85,7 @@ __global__ void __launch_bounds__(kThreads, 1) w4_kernel(const __grid_constant__
 #pragma unroll
   for (int n = 0; n < NT; ++n) acc[n][0] = acc[n][1] = acc[n][2] = acc[n][3] = 0.f;
   const int stages = (count + kTeams - 1) / kTeams;
-  const int in_block = first % 8 ? 0 : min(8, a.row_tiles - first);                          // of the layout's block from there
+  const int in_block = first % 8 ? 0 : min(8, a.row_tiles - first);  // of the layout's block from there
   if (warp >= kLoadWarp) {
     // A copy takes 200 cycles and more to give out, so there are as few as can be, by two warps: one has the
     // first tile's codes (all tiles', where they lie side by side), the other x and the second tile's.  One
@@ -268,8 +275,9 @@ bool w4_x_map(CUtensorMap* m, W4Args* a, int tokens, int halves) {
 cudaError_t launch_w4(W4Args a, cudaStream_t s) {
   a.row_tiles = (a.N + 15) / 16;
   a.tiles = (a.K + kTileK - 1) / kTileK;
-  // up to 16 tokens as columns of mma.sync (14336 x 4096, 16 tokens: 15.7 us, on tcgen05 15.9; one token
-  // x 2048 x 2048 4.5 and 5.0; groups of 32 16.6 and 21.1); 24 tokens 18.9 and 15.1, 64 38.5 and 17.3
+  // up to 16 tokens as columns of mma.sync: 16 tokens x 4096 x 14336 14.7 us, on tcgen05 17.8; x 14336 x 4096
+  // 15.8 and 16.2, x 2048 x 2048 5.2 and 5.9, in groups of 32 x 4096 x 14336 15.2 and 22.9; but 24 tokens 18.9
+  // and 15.1, 64 38.5 and 17.1
   if (a.M > 16) return launch_w4_tc(a, s);
   if (a.group == 128) return launch_w4_g<1>(a, s);
   return a.group == 64 ? launch_w4_g<2>(a, s) : launch_w4_g<4>(a, s);

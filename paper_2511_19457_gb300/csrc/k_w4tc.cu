@@ -1,14 +1,18 @@
-// Products with 4-bit weights on tcgen05.
+// Products with 4-bit weights on tcgen05, for more tokens than mma.sync takes in time.
 //
-// A CTA has 128 rows of W and up to 64 tokens.  Four warps make bf16 whole numbers of a tile of
-// columns' codes (a thread a row) and put them into tensor memory, where they are the A operand; x is the
-// B operand, by TMA in shared memory.  Another four take each group's sums out of tensor memory, and multiply
-// and add them in fp32 in registers (a thread a row).  Codes less zeros are exact, and only the fp32 sums of
-// a group are multiplied by its scale: nothing is rounded but fp32 sums.
+// A CTA has 128 rows of W and up to 64 tokens.  Eight warps, in two groups that take turns, make bf16 whole
+// numbers of a tile of columns' codes (a thread a row) and put them into tensor memory, where they are the A
+// operand; x is the B operand, by TMA in shared memory.  Another four take each group's sums out of tensor
+// memory, and multiply and add them in fp32 in registers (a thread a row).  Codes less zeros are exact, and
+// only the fp32 sums of a group are multiplied by its scale: nothing is rounded but fp32 sums.
 //
 // Bound by the bytes of the weights, read once for 64 tokens; beside them x comes from the L2 for every
-// block of rows.  On mma.sync 61 tokens x 14336 x 4096 cannot take less than 12.6 us (its products at 0.5 an
-// SM and cycle).
+// block of rows.  61 tokens x 14336 columns x 4096 rows, groups of 128, from memory: 17.3 us.  Its products
+// with A from tensor memory take 64 to 70 cycles each, whatever the number of tokens: 600 a tile of
+// 128 x 128, 28 tiles a CTA in clusters of 4, 9 us; the rest is the start, the first tile and the cluster's
+// sum.  On mma.sync the products alone cannot take less than 12.6 us (0.5 an SM and cycle), and with the codes'
+// instructions beside them took 38.5.  Tried: two CTAs an SM with half the tensor memory each (20.2), two
+// warps that issue products (no faster), the weights into the L2 before the kernel before ends (18.2).
 #include "w4.cuh"
 
 namespace sparoa {
@@ -156,27 +160,18 @@ __global__ void __launch_bounds__(kThreads, 1) w4_tc_kernel(const __grid_constan
         const float s = __uint_as_float(lds_u16(from + gi * 32) << 16);
         const f2_t scale = f2(s, s);
         tc_fence_after();
-        if constexpr (NTOK == 16) {
-          float v[16];
-          tmem_ld16(tmem + lanes + (n % kBufs) * NTOK, v);
-          tc_fence_before();
-          arrive(bars.d_free[n % kBufs]);
 #pragma unroll
-          for (int k = 0; k < 16; k += 2) acc[k / 2] = ffma2(f2(v[k], v[k + 1]), scale, acc[k / 2]);
-        } else {
-#pragma unroll
-          for (int c = 0; c < NTOK; c += 32) {
-            uint32_t v[32];
-            tmem_ld32_nowait(tmem + lanes + (n % kBufs) * NTOK + c, v);
-            tmem_wait_ld32(v);
-            if (c + 32 == NTOK) {
-              tc_fence_before();
-              arrive(bars.d_free[n % kBufs]);
-            }
-#pragma unroll
-            for (int k = 0; k < 32; k += 2)
-              acc[(c + k) / 2] = ffma2(f2(__uint_as_float(v[k]), __uint_as_float(v[k + 1])), scale, acc[(c + k) / 2]);
+        for (int c = 0; c < NTOK; c += 32) {
+          uint32_t v[32];
+          tmem_ld32_nowait(tmem + lanes + (n % kBufs) * NTOK + c, v);
+          tmem_wait_ld32(v);
+          if (c + 32 == NTOK) {
+            tc_fence_before();
+            arrive(bars.d_free[n % kBufs]);
           }
+#pragma unroll
+          for (int k = 0; k < 32; k += 2)
+            acc[(c + k) / 2] = ffma2(f2(__uint_as_float(v[k]), __uint_as_float(v[k + 1])), scale, acc[(c + k) / 2]);
         }
       }
       if (!ok) break;

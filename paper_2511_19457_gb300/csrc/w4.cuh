@@ -21,11 +21,6 @@ __device__ __forceinline__ uint4 lds_u4(uint32_t addr) {
   asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
   return v;
 }
-__device__ __forceinline__ uint2 lds_u2(uint32_t addr) {
-  uint2 v;
-  asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(addr) : "memory");
-  return v;
-}
 __device__ __forceinline__ uint32_t lds_u16(uint32_t addr) {
   uint16_t v;
   asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(addr) : "memory");
@@ -98,7 +93,7 @@ __device__ __forceinline__ void w4_finish(const W4Args& a, uint32_t part, int pi
 
 // CTAs (a cluster) that the columns of each of `blocks` blocks are split over, by the time that the rounds
 // of clusters take: a CTA's is its tiles, each of `weight` eighths, and kW4Start more for its beginning and
-// end (3 us of 0.3 each).  14336 columns, 32 blocks of 128 rows, one token: 1 CTA each 38.8 us, 2 21.4, 4 12.9, 8
+// end (3 us of 0.3 each).  14336 columns, 32 blocks of 128 rows, one token: 1 CTA each 38.8 us, 2 21.4, 4 13, 8
 // 24.0 (the GPU does not hold 32 clusters of 8 at once).
 constexpr int kW4Start = 10;
 struct W4Split {

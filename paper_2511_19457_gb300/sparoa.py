@@ -643,26 +643,30 @@ _paged_attention, _ruled_attention = _lib.sparoa_paged_attention, _lib.sparoa_ru
 _U8S = (torch.uint8,)
 
 
+def _w4_sizes(codes, scales, zeros):
+    """(N, K, group, packed bytes) of 4-bit weights as W4 takes them."""
+    _want_rows(codes, _U8S, "W4 codes")
+    _want_rows(scales, _BF16S, "W4 scales")
+    _want(codes.dim() == 2 and scales.dim() == 2 and codes.shape[0] == scales.shape[0], "W4: codes and scales of N rows")
+    N, K, groups = codes.shape[0], 2 * codes.shape[1], scales.shape[1]
+    _want(groups > 0 and K % groups == 0, "W4: a scale for every group of columns")
+    if zeros is not None:
+        _want_rows(zeros, _U8S, "W4 zeros")
+        _want(zeros.shape == scales.shape, "W4: a zero for every scale")
+    for t in (scales, zeros):
+        _want(t is None or t.device == codes.device, "W4: tensors on one device")
+    nbytes = int(_lib.sparoa_w4_bytes(N, K, K // groups, 0 if zeros is None else 1))
+    _want(nbytes > 0, f"W4: [{N}, {K}] in groups of {K // groups}: N a multiple of 8, groups of 32, 64 or 128")
+    return N, K, K // groups, nbytes
+
+
 class W4:
     """Weights [N, K] of 4 bits: codes uint8 [N, K / 2] (column 2 i in the low half of byte i), scales bf16
     [N, K / group], zeros uint8 [N, K / group] or None (8).  Laid out for sparoa_gemm_w4 when it is made, on
     the current torch stream; holds a copy of its own."""
 
     def __init__(self, ctx: Context, codes, scales, zeros=None):
-        _want_rows(codes, _U8S, "W4 codes")
-        _want_rows(scales, _BF16S, "W4 scales")
-        _want(codes.dim() == 2 and scales.dim() == 2 and codes.shape[0] == scales.shape[0], "W4: codes and scales of N rows")
-        self.N, self.K = codes.shape[0], 2 * codes.shape[1]
-        groups = scales.shape[1]
-        _want(groups > 0 and self.K % groups == 0, "W4: a scale for every group of columns")
-        self.group = self.K // groups
-        if zeros is not None:
-            _want_rows(zeros, _U8S, "W4 zeros")
-            _want(zeros.shape == scales.shape, "W4: a zero for every scale")
-        for t in (scales, zeros):
-            _want(t is None or t.device == codes.device, "W4: tensors on one device")
-        nbytes = int(_lib.sparoa_w4_bytes(self.N, self.K, self.group, 0 if zeros is None else 1))
-        _want(nbytes > 0, f"W4: [{self.N}, {self.K}] in groups of {self.group}: N a multiple of 8, groups of 32, 64 or 128")
+        self.N, self.K, self.group, nbytes = _w4_sizes(codes, scales, zeros)
         self.packed = torch.empty(nbytes, dtype=torch.uint8, device=codes.device)
         sparoa_w4_pack(ctx, codes, scales, zeros, self.packed)
         self.desc = W4Desc(_ptr(self.packed), self.N, self.K, self.group, 0 if zeros is None else 1)
@@ -692,10 +696,12 @@ def w4_quantise(weight, group=128, zeros=False):
 
 
 def sparoa_w4_pack(ctx: Context, codes, scales, zeros, packed):
-    """Lay out 4-bit weights (see W4) into packed, a uint8 tensor of sparoa_w4_bytes."""
-    N, K = codes.shape[0], 2 * codes.shape[1]
+    """Lay out 4-bit weights (see W4) into packed, uint8 of sparoa_w4_bytes."""
+    N, K, group, nbytes = _w4_sizes(codes, scales, zeros)
+    _want_rows(packed, _U8S, "w4_pack packed")
+    _want(packed.numel() == nbytes and packed.device == codes.device, f"w4_pack: packed of {nbytes} bytes beside the codes")
     ctx._bind()
-    ctx._check(_lib.sparoa_w4_pack(ctx.h, _ptr(codes), _ptr(scales), _ptr(zeros), N, K, K // scales.shape[1], _ptr(packed)))
+    ctx._check(_lib.sparoa_w4_pack(ctx.h, _ptr(codes), _ptr(scales), _ptr(zeros), N, K, group, _ptr(packed)))
 
 
 def sparoa_gemm_w4(ctx: Context, x, w: W4, y, bias=None, bn=None, eps=1e-5, act=ACT_NONE, residual=None, y_occ=None):

@@ -262,6 +262,19 @@ def test_rows_behind_are_left(sp, ctx):
         assert (whole[M:] == 9).all() and (whole[:M] != 9).all()
 
 
+def test_refusals_of_pack(sp, ctx):
+    _, codes, scales, zero = (None if t is None else t.cuda() for t in _inputs(4, 256, 64, 64, True))
+    packed = torch.empty(sp.W4(ctx, codes, scales, zero).packed.numel(), dtype=torch.uint8, device="cuda")
+    bad = [(codes, scales, zero, packed[16:]), (codes, scales, zero, packed.cpu()), (codes, scales, None, packed), (codes, scales[:, :0], None, packed),
+           (codes, scales, zero, packed.view(torch.int32)), (codes.int(), scales, zero, packed), (codes, scales, zero[:32], packed)]
+    for i, args in enumerate(bad):
+        with pytest.raises(sp.SparoaError):
+            sp.sparoa_w4_pack(ctx, *args)
+            raise AssertionError(f"call {i} was taken")
+    sp.sparoa_w4_pack(ctx, codes, scales, zero, packed)
+    assert torch.equal(packed, sp.W4(ctx, codes, scales, zero).packed)
+
+
 def test_refusals(sp, ctx):
     x, codes, scales, zero = (None if t is None else t.cuda() for t in _inputs(4, 256, 64, 64, True))
     w = sp.W4(ctx, codes, scales, zero)
