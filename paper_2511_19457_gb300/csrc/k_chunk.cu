@@ -593,12 +593,17 @@ __device__ __forceinline__ float changed_unit(const PagedArgs& a, const RowRules
         auto more = [&](float x, int e, int f) { return caps ? max3_nan<true>(x, at(e), at(f)) : max3_nan<false>(x, at(e), at(f)); };
         t[k] = more(more(more(more(at(0), 1, 2), 3, 4), 5, 6), 7, 7);
       }
-      float top = max3_nan<false>(max3_nan<false>(t[0], t[1], t[2]), t[3], t[3]);
-      size = max3_nan<false>(size, top, top);
+      size = max3_nan<false>(max3_nan<false>(size, t[0], t[1]), t[2], t[3]);
       if (slopes) {
-        // (a slope may put the bound of 32 scores kSlackLog2 too high)
-        top = (caps ? Capped(a).near1(top) : top * a.score_log2) + u.slope * ((float)(i * 32) - far) + fmaxf(u.slope * 31.f, 0.f);
-        bound = max3_nan<false>(bound, top, top);
+        // (a slope may put the bound of eight scores kSlackLog2 too high)
+        const float at0 = u.slope * ((float)(i * 32) - far) + fmaxf(u.slope * 7.f, 0.f);
+#pragma unroll
+        for (int k = 0; k < 4; k += 2) {
+          const f2_t top = f2(t[k], t[k + 1]), one = f2(a.score_log2, a.score_log2);
+          float x, y;
+          f2_split(ffma2(top, caps ? Capped(a).factor(top, 1.f) : one, f2(at0 + u.slope * (8.f * k), at0 + u.slope * (8.f * k + 8.f))), x, y);
+          bound = max3_nan<false>(bound, x, y);
+        }
       }
     }
     if (caps) near = __all_sync(0xffffffffu, Capped(a).near(size));
@@ -733,9 +738,9 @@ __device__ __forceinline__ void softmax_role(const Role<walk_of(RULES)>& r, uint
     const int first_key = c.key0();
     float m = -INFINITY, l = 0.f;
     // whether scores of whole units may be changed on their way to their weights.  The reference is
-    // then a bound of 32 keys' scores at a time, which a slope may put kSlackLog2 too high
+    // then a bound of eight keys' scores at a time, which a slope may put kSlackLog2 too high
     const bool may_direct = kChanges && !(RULES & kTree) && (!(RULES & kCap) || a.cap <= kDirectCap) &&
-                            (!(RULES & kBias) || (__all_sync(0xffffffffu, fabsf(rule.slope) * 31.f <= kSlackLog2) && a.causal && !a.prefix));
+                            (!(RULES & kBias) || (__all_sync(0xffffffffu, fabsf(rule.slope) * 7.f <= kSlackLog2) && a.causal && !a.prefix));
     for (int j = j0; j < count; j += dj) {
       const int key0 = first_key + j * Cursor<walk_of(RULES)>::kStep;
       if (!(ok = r.wait(bars.s[grp], sn & 1u, kErrTimeoutAcc))) break;
