@@ -14,8 +14,6 @@
 // device, so every CTA makes the plan itself (a load per sequence and a scan).
 #pragma once
 
-#include <type_traits>
-
 #include "sparoa_kernels.h"
 
 namespace sparoa {
@@ -175,11 +173,6 @@ struct PagedCursor : CursorPrefix<Cut::RULED> {
     tiles = tiles_of<Cut>(n, a.group);
     if constexpr (Cut::RULED) prefix = prefix_of<Cut>(a, b);
   }
-  // The order of items: a sequence's key heads, and their tiles.  With a bias a unit takes less time where
-  // the slope is steep (paged_chunk), and a share of one head's tiles would be all steep or none; so there the
-  // order is tiles, and their heads from both ends in turn.
-  static __device__ __forceinline__ int head_at(const PagedArgs& a, int place) { return place & 1 ? a.kv_heads - 1 - (place >> 1) : place >> 1; }
-  static __device__ __forceinline__ int place_of(const PagedArgs& a, int h) { return 2 * h < a.kv_heads + (a.kv_heads & 1) ? 2 * h : 2 * (a.kv_heads - 1 - h) + 1; }
   // a unit belongs to the share that has the first step of its cost
   __device__ __forceinline__ int unit_at(int at) const { return max(0, at - Cut::EXTRA + weight - 1) / weight; }
   __device__ __forceinline__ void enter(const PagedArgs& a) {
@@ -219,22 +212,18 @@ struct PagedCursor : CursorPrefix<Cut::RULED> {
       before += __shfl_sync(0xffffffffu, incl, 31);
     }
     load_seq(a, p);
-    // (a tile's, or all of a head's)
-    using Sum = std::conditional_t<Cut::REVERSED, unsigned long long, unsigned>;
+    const unsigned long long per = p.cost[b];
     unsigned long long rem = u - before;
-    if constexpr (!Cut::REVERSED) {
-      const unsigned long long per = p.cost[b];
-      h = (int)quotient(rem, per);
-      rem -= h * per;
-    }
+    h = (int)quotient(rem, per);
+    rem -= h * per;
     t = 0;
     if (tiles > 1) {
       for (int t0 = 0;; t0 += 32) {
-        const Sum mine = t0 + lane < tiles ? (Sum)tile_cost<Cut>(a, n, len, t0 + lane, prefix) * (Cut::REVERSED ? a.kv_heads : 1) : 0;
-        Sum incl = mine;
+        const unsigned mine = t0 + lane < tiles ? (unsigned)tile_cost<Cut>(a, n, len, t0 + lane, prefix) : 0u;
+        unsigned incl = mine;
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
-          const Sum o = __shfl_up_sync(0xffffffffu, incl, d);
+          const unsigned o = __shfl_up_sync(0xffffffffu, incl, d);
           if (lane >= d) incl += o;
         }
         const unsigned hit = __ballot_sync(0xffffffffu, incl > rem);
@@ -246,12 +235,6 @@ struct PagedCursor : CursorPrefix<Cut::RULED> {
         }
         rem -= __shfl_sync(0xffffffffu, incl, 31);
       }
-    }
-    if constexpr (Cut::REVERSED) {
-      const unsigned long long per = tile_cost<Cut>(a, n, len, t, prefix);
-      const int place = (int)quotient(rem, per);
-      rem -= place * per;
-      h = head_at(a, place);
     }
     pos = (int)rem;
     left = steps;
@@ -268,20 +251,13 @@ struct PagedCursor : CursorPrefix<Cut::RULED> {
         blk = end;
         return;
       }
-      bool over;  // the sequence is
-      if constexpr (Cut::REVERSED) {
-        const int place = place_of(a, h) + 1;
-        const bool last = place == a.kv_heads;
-        h = last ? 0 : head_at(a, place);
-        over = last && ++t == tiles;
-      } else {
-        over = ++t == tiles && ++h == a.kv_heads;
-        if (t == tiles) t = 0;
-      }
-      if (over) {
-        h = t = 0;
-        do ++b; while (p.n[b] == 0);  // (the line goes on: there is such a sequence)
-        load_seq(a, p);
+      if (++t == tiles) {
+        t = 0;
+        if (++h == a.kv_heads) {
+          h = 0;
+          do ++b; while (p.n[b] == 0);  // (the line goes on: there is such a sequence)
+          load_seq(a, p);
+        }
       }
       pos = 0;
       enter(a);
