@@ -568,9 +568,17 @@ __device__ __forceinline__ void weigh(uint32_t (&s)[4][32], uint32_t ts, f2_t sc
 // walked twice, 32 at a time, read again from tensor memory: unrolled over all 128 the
 // instructions came too slowly (one of four issue slots was lost for want of them).
 //   direct   nothing is masked and the scores are small beside the cap: the first walk bounds the
-//            changed scores by the scores themselves, the second changes them on their way to
-//            their weights
+//            changed scores by the scores themselves (under a bias, of eight keys at a time), the
+//            second changes them on their way to their weights
 //   else     the first walk changes and masks them where they lie
+// Bound, as without rules, by a unit's chain of softmax and products, the softmax being longer.  4095
+// tokens, 32 heads of 64, slopes 2^-0.25 to 2^-8: 130 us, 114 without a bias; all changed where they lie
+// 177, with bounds of 32 keys 140, with 128 scores unrolled 208, the next 32 scores asked for ahead 180.
+// 4 chunks of 1500 over 1600 to 4000, 16 heads over 8 of 128, window 2048, a prefix of 577, a cap of
+// 30: 105 us, 90 without cap and prefix; with exponentials for the cap and one walk 216, with the polynomial
+// and one walk 143.  Dropped: dearer and cheaper units in the plan's costs (far units at 4, 3 and 2 fifths:
+// 139, 138 and 148 us, since they take nearly as long as others), heads in turn instead of one after the
+// other (132.5).
 template <int RULES, typename Refer>
 __device__ __forceinline__ float changed_unit(const PagedArgs& a, const RowRules& u, uint32_t ts, int key0, bool whole, bool may_direct,
                                               bool first, float m, const Refer& refer) {

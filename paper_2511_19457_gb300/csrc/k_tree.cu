@@ -6,6 +6,9 @@
 // warp, two tokens a lane, a vote per step) and then moves its pieces of every kept token.
 // A kept token never moves up, and the path is walked in its order, so a place is written
 // only after what it held was read: a thread moves the same piece of all tokens.
+//
+// 64 trees of up to 25 tokens in four layers' caches, 8 key heads of 128: 3.8 us on the device,
+// one tree of 7 in two layers 2.5, of which a launch is 2; a call from Python takes 8.
 #include "sparoa_kernels.h"
 
 namespace sparoa {
