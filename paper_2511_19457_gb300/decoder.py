@@ -151,6 +151,8 @@ class Decoder:
         settled (and not in the cache yet), the others drafted behind their parents (parents[0] = -1).
         Returns for each sequence its next tokens: the drafted ones that the model would have chosen itself
         (greedily), and the one that it chooses after them.  The cache keeps what is settled."""
+        if len(drafts) != len(seqs) or len(set(seqs)) != len(seqs):
+            raise ValueError("check: a tree for each sequence, and no sequence twice")
         new = [len(t) for t, _ in drafts]
         bits = [b for _, parents in drafts for b in ancestors(parents)]
         if any(len(t) != len(p) or not t or p[0] != -1 for t, p in drafts):

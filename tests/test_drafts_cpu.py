@@ -109,6 +109,10 @@ def test_trees_that_are_none():
     for drafts in ([([], [])], [([1, 2], [-1])], [([1, 2], [0, 0])], [([1, 2], [-1, 1])], [(list(range(65)), [-1] + list(range(64)))]):
         with pytest.raises(ValueError):
             model.check(drafts, ["a"])
+    one = ([1], [-1])
+    for drafts, seqs in (([one, one], ["a", "a"]), ([one], ["a", "b"]), ([one, one], ["a"])):
+        with pytest.raises(ValueError):
+            model.check(drafts, seqs)
     with pytest.raises(ValueError):
         model.generate([[1]], 2, draft=repeats, penalties=(1.0, 0.0, 0.0, 1.0))
     assert len(model.pages.free) == 4 and not model.pages.held
