@@ -743,9 +743,11 @@ class LogitRules:
         self.bias_rows = 1 if bias is None or bias.dim() == 1 else bias.shape[0]
         self.V = None if bias is None else bias.shape[-1]
         # rows that the rules are for, where they say
-        self.R = {n for n in (None if seen_start is None else seen_start.numel() - 1, None if penalties is None else penalties.shape[0],
-                              None if allowed is None else allowed.shape[0], self.bias_rows if self.bias_rows != 1 else None)
-                  if n is not None}
+        rows = {n for n in (None if seen_start is None else seen_start.numel() - 1, None if penalties is None else penalties.shape[0],
+                            None if allowed is None else allowed.shape[0], self.bias_rows if self.bias_rows != 1 else None)
+                if n is not None}
+        _want(len(rows) <= 1, "LogitRules: lists, penalties, bias and masks of as many rows")
+        self.R = rows.pop() if rows else None
         self.words = None if allowed is None else allowed.shape[1]
         self.desc = LogitRulesDesc(_ptr(seen_start), _ptr(seen), 0 if seen is None else seen.numel(), _ptr(penalties), _ptr(bias),
                                    self.V if self.bias_rows != 1 else 0, _ptr(allowed), self.words or 0)
@@ -762,21 +764,22 @@ def _logit_rows(t, R, V, what):
 def sparoa_shape_logits(ctx: Context, logits, rules: LogitRules | None = None, y=None, best=None, lse=None):
     """The rules over logits [R, V] (bf16 or fp32): y fp32 [R, V] (may be the logits), best int32 [R], lse fp32
     [R], each of them or None."""
-    _want(logits.dim() == 2, "shape_logits: logits [R, V]")
+    if logits.dim() != 2 or logits.dtype not in (_bf16, _f32):
+        _refuse("shape_logits: bf16 or fp32 logits [R, V]")
     R, V = logits.shape
     ld = _logit_rows(logits, R, V, "shape_logits logits")
-    _want(logits.dtype in (_bf16, _f32), "shape_logits: bf16 or fp32 logits")
+    ld_y = 0
     if y is not None:
-        _want(y.dtype is _f32, "shape_logits: y fp32")
-    ld_y = 0 if y is None else _logit_rows(y, R, V, "shape_logits y")
-    for t, types, what in ((best, _I32S, "shape_logits best"), (lse, _FP32S, "shape_logits lse")):
-        if t is not None:
-            _want_rows(t, types, what)
-            _want(t.numel() == R, f"{what}: a value per row")
-    if rules is not None:
-        # (one row of bias is for all)
-        if any(n != R for n in rules.R) or rules.V not in (None, V) or (rules.words is not None and rules.words * 32 < V):
-            _refuse("shape_logits: rules of other rows or tokens")
+        if y.dtype is not _f32:
+            _refuse("shape_logits: y fp32")
+        ld_y = _logit_rows(y, R, V, "shape_logits y")
+    if best is not None and not (best.dtype is _i32 and best.is_cuda and best.is_contiguous() and best.numel() == R):
+        _refuse("shape_logits: best int32, a value per row")
+    if lse is not None and not (lse.dtype is _f32 and lse.is_cuda and lse.is_contiguous() and lse.numel() == R):
+        _refuse("shape_logits: lse fp32, a value per row")
+    # (one row of bias is for all)
+    if rules is not None and (rules.R not in (None, R) or rules.V not in (None, V) or (rules.words is not None and rules.words * 32 < V)):
+        _refuse("shape_logits: rules of other rows or tokens")
     ctx._bind()
     st = _shape_logits(ctx.h, logits.data_ptr(), ld, R, V, F32 if logits.dtype is _f32 else BF16, None if rules is None else rules.ref,
                        _ptr(y), ld_y, _ptr(best), _ptr(lse))
