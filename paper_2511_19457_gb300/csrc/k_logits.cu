@@ -165,6 +165,11 @@ struct Batch {
   }
 };
 
+// zero counts of `chunk` tokens, or of half as many that have 32 bits
+__device__ __forceinline__ void no_counts(unsigned* count, int chunk) {
+  for (int i = threadIdx.x; i < chunk / 8; i += kThreads) reinterpret_cast<uint4*>(count)[i] = make_uint4(0u, 0u, 0u, 0u);
+}
+
 // Counts have 16 bits, which a list below 2^16 tokens cannot pass; the vocabulary of a row with a
 // longer one is walked in shares of half the size, with 32 bits.
 template <typename XT, int PARTS>
@@ -178,6 +183,7 @@ __global__ void __launch_bounds__(kThreads, 4) logits_kernel(const __grid_consta
   s.rep = s.inv_rep = s.inv = 1.f;
   s.presence = s.frequency = 0.f;
   s.count = s_count;
+  if constexpr ((PARTS & kSeen) != 0) no_counts(s_count, a.chunk);
   pdl_wait();
   pdl_trigger();
   if (a.penalties) {
@@ -212,9 +218,10 @@ __global__ void __launch_bounds__(kThreads, 4) logits_kernel(const __grid_consta
     float z[kItems];
     Batch<PARTS, false, XT>::fetch(s, 0, z);  // on its way while the tokens are counted
     if (seen) {
-      __syncthreads();    // (the counts before were read)
-      for (int i = threadIdx.x; i < (s.len + (s.wide ? 3 : 7)) / (s.wide ? 4 : 8); i += kThreads)
-        reinterpret_cast<uint4*>(s_count)[i] = make_uint4(0u, 0u, 0u, 0u);
+      if (lo >= (int64_t)a.split * chunk) {  // (the first share's counts are zero already)
+        __syncthreads();                     // (the counts before were read)
+        no_counts(s_count, a.chunk);
+      }
       __syncthreads();
       // (kAhead loads of a thread are on their way at once; what is no token counts nowhere)
       for (int64_t i0 = s0 + threadIdx.x; i0 < s1; i0 += kAhead * kThreads) {
