@@ -1839,16 +1839,17 @@ sparoa_status sparoa_tree_accept(sparoa_ctx* ctx, const int32_t* tokens, const i
   a.D = caches->head_dim;
   a.pages = caches->pages;
   a.caches = n_caches;
+  void *k[kTreeCaches], *v[kTreeCaches];
   for (int i = 0; i < n_caches; ++i) {
-    a.k[i] = caches[i].k;
-    a.v[i] = caches[i].v;
+    k[i] = caches[i].k;
+    v[i] = caches[i].v;
   }
   a.path = path;
   a.count = count;
   a.following = following;
   a.new_len = new_len;
   a.err = ctx->d_err();
-  SP_CUDA(launch_tree_accept(a, ctx->stream));
+  SP_CUDA(launch_tree_accept(a, k, v, ctx->stream));
   return SPAROA_OK;
 }
 

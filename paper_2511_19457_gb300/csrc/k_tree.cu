@@ -7,8 +7,8 @@
 // A kept token never moves up, and the path is walked in its order, so a place is written
 // only after what it held was read: a thread moves the same piece of all tokens.
 //
-// 64 trees of up to 25 tokens in four layers' caches, 8 key heads of 128: 3.8 us on the device,
-// one tree of 7 in two layers 2.5, of which a launch is 2; a call from Python takes 8.
+// 64 trees of 25 tokens in four layers' caches, 8 key heads of 128: 3.6 us on the device,
+// one tree of 7 in two layers 2.5, of which a launch is 2; a call from Python takes 7.
 #include "sparoa_kernels.h"
 
 namespace sparoa {
@@ -18,7 +18,15 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kAhead = 8;  // tokens that a thread has on their way
 
-__global__ void __launch_bounds__(kThreads) tree_accept_kernel(const __grid_constant__ TreeArgs a) {
+// CACHES: pools that the arguments have room for.  Two KB of arguments take the host and the GPU a
+// microsecond and more of a call: with room for 8 caches 7.1 us, for 128 8.4 (two caches).
+template <int CACHES>
+struct Pools {
+  void *k[CACHES], *v[CACHES];
+};
+
+template <int CACHES>
+__global__ void __launch_bounds__(kThreads) tree_accept_kernel(const __grid_constant__ TreeArgs a, const __grid_constant__ Pools<CACHES> pools) {
   __shared__ int s_from[kTreeTokens], s_to[kTreeTokens];  // rows of the pool (key head 0), -1: not there
   __shared__ int s_path[kTreeTokens], s_best[kTreeTokens];
   __shared__ int s_count;
@@ -90,9 +98,9 @@ __global__ void __launch_bounds__(kThreads) tree_accept_kernel(const __grid_cons
     }
   }
   const int c = blockIdx.z * kThreads + threadIdx.x, pieces = a.D / 8, each = a.kv_heads * pieces;
-  if ((int)blockIdx.y >= a.caches || c >= 2 * each) return;
+  if (c >= 2 * each) return;
   const int head = c % each / pieces;
-  uint4* pool = reinterpret_cast<uint4*>(c < each ? a.k[blockIdx.y] : a.v[blockIdx.y]) +
+  uint4* pool = reinterpret_cast<uint4*>(c < each ? pools.k[blockIdx.y] : pools.v[blockIdx.y]) +
                 ((int64_t)head << a.page_log2) * pieces + c % pieces;
   for (int k0 = 0; k0 < count; k0 += kAhead) {
     uint4 u[kAhead];
@@ -105,12 +113,22 @@ __global__ void __launch_bounds__(kThreads) tree_accept_kernel(const __grid_cons
   }
 }
 
+template <int CACHES>
+cudaError_t launch(const TreeArgs& a, void* const* k, void* const* v, cudaStream_t s) {
+  Pools<CACHES> pools;
+  for (int i = 0; i < CACHES; ++i) {
+    pools.k[i] = i < a.caches ? k[i] : nullptr;
+    pools.v[i] = i < a.caches ? v[i] : nullptr;
+  }
+  const int parts = (2 * a.kv_heads * a.D / 8 + kThreads - 1) / kThreads;
+  return launch_kernel(tree_accept_kernel<CACHES>, dim3((unsigned)a.batch, (unsigned)a.caches, (unsigned)parts), dim3(kThreads), 0, s, a, pools);
+}
+
 }  // namespace
 
-cudaError_t launch_tree_accept(const TreeArgs& a, cudaStream_t s) {
-  const int parts = (2 * a.kv_heads * a.D / 8 + kThreads - 1) / kThreads;
-  return launch_kernel(tree_accept_kernel, dim3((unsigned)a.batch, (unsigned)(a.caches > 0 ? a.caches : 1), (unsigned)parts),
-                       dim3(kThreads), 0, s, a);
+cudaError_t launch_tree_accept(const TreeArgs& a, void* const* k, void* const* v, cudaStream_t s) {
+  if (a.caches <= 8) return launch<8>(a, k, v, s);
+  return a.caches <= 32 ? launch<32>(a, k, v, s) : launch<kTreeCaches>(a, k, v, s);
 }
 
 }  // namespace sparoa

@@ -326,12 +326,11 @@ struct TreeArgs {
   int64_t table_stride = 0;
   int batch = 0, max_pages = 0, page_log2 = 0, kv_heads = 0, D = 0, caches = 0;
   int64_t pages = 0;
-  void* k[kTreeCaches];
-  void* v[kTreeCaches];
   int32_t *path = nullptr, *count = nullptr, *following = nullptr, *new_len = nullptr;
   uint32_t* err = nullptr;
 };
-cudaError_t launch_tree_accept(const TreeArgs& a, cudaStream_t s);
+// k, v: host arrays of a.caches pools
+cudaError_t launch_tree_accept(const TreeArgs& a, void* const* k, void* const* v, cudaStream_t s);
 
 // Logits to tokens (k_logits.cu)
 struct LogitArgs {

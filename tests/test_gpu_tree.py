@@ -115,6 +115,12 @@ def test_paths(sp, ctx, seed, page, kv_heads, hd, layers):
     _same(c.run(sp, ctx), c.want())
 
 
+@pytest.mark.parametrize("layers", [8, 9, 32, 33, 128])
+def test_many_layers(sp, ctx, layers):
+    c = Case([5, 17, 1], [20, 30, 1], 16, 2, 64, layers, vocab=2, seed=layers)
+    _same(c.run(sp, ctx), c.want())
+
+
 def test_one_path_of_all(sp, ctx):
     """64 tokens that all follow one another (nothing moves), and a path that skips every other token."""
     c = Case([64, 64], [64, 100], vocab=1)
