@@ -607,8 +607,8 @@ sparoa_status sparoa_w4_pack(sparoa_ctx *ctx, const void *codes, const void *sca
                              const void *zeros, int64_t N, int64_t K, int32_t group, void *packed);
 
 /*
- * y[M, N] = epilogue( x[M, K] * W^T ) with 4-bit weights, for few rows: made for M up to 64
- * (the weights are read once for every 64 rows).  Codes less their zeros are whole
+ * y[M, N] = epilogue( x[M, K] * W^T ) with 4-bit weights, for few rows: made for M up to 128
+ * (the weights are read once for every 64 or 128 rows).  Codes less their zeros are whole
  * numbers, their products with x are summed in fp32 over a group, and the sum is
  * multiplied by the scale: no weight is rounded.
  *   x     bf16 [M][K], contiguous, 16-byte aligned; M <= 2^20

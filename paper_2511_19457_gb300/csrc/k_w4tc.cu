@@ -1,6 +1,6 @@
 // Products with 4-bit weights on tcgen05, for more tokens than mma.sync takes in time.
 //
-// A CTA has 128 rows of W and up to 64 tokens.  Eight warps, in two groups that take turns, make bf16 whole
+// A CTA has 128 rows of W and up to 64 tokens, or 128 where there are more (launch_g).  Eight warps, in two groups that take turns, make bf16 whole
 // numbers of a tile of columns' codes (a thread a row) and put them into tensor memory, where they are the A
 // operand; x is the B operand, by TMA in shared memory.  Another four take each group's sums out of tensor
 // memory, and multiply and add them in fp32 in registers (a thread a row).  Codes less zeros are exact, and
@@ -21,22 +21,26 @@ namespace {
 
 constexpr int kTileK = kW4TileK;
 constexpr int kRows = 128;
-constexpr int kStages = 8;  // tiles of columns on their way
-constexpr int kBufs = 4;    // of A and of sums in tensor memory
-constexpr int kCodeWarps = 8, kSumWarps = 4, kLoadWarp = 12, kXWarp = 13, kMmaWarp = 14;
-constexpr int kThreads = 480;
+constexpr int kBufs = 4;  // of A in tensor memory
+constexpr int kCodeWarps = 8;
 constexpr int kPitch = kRows + 4;  // floats of a token's sums
 constexpr uint32_t kCols = 512, kA = 256;
 
 template <int NTOK>
 struct Cfg {
+  static constexpr int kStages = NTOK > 64 ? 4 : 8;      // tiles of columns on their way
+  static constexpr int kSums = NTOK > 64 ? 2 : kBufs;    // of sums in tensor memory
+  static constexpr int kSumWarps = NTOK > 64 ? 8 : 4;    // four for 64 tokens
+  static constexpr int kLoadWarp = kCodeWarps + kSumWarps, kXWarp = kLoadWarp + 1, kMmaWarp = kLoadWarp + 2;
+  static constexpr int kThreads = 32 * (kMmaWarp + 1);
   static constexpr int kHalf = NTOK * 128;  // 64 columns of x
   static size_t smem(int tile) { return (size_t)kStages * (2 * kHalf + 8 * tile) + 1024; }
 };
 
+template <int NTOK>
 struct Bars {
-  unsigned long long full[kStages], empty[kStages];  // codes and x
-  unsigned long long a[kBufs], a_free[kBufs], d[kBufs], d_free[kBufs], drain;
+  unsigned long long full[Cfg<NTOK>::kStages], empty[Cfg<NTOK>::kStages];  // codes and x
+  unsigned long long a[kBufs], a_free[kBufs], d[Cfg<NTOK>::kSums], d_free[Cfg<NTOK>::kSums], drain;
 };
 
 __device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t bd, uint32_t idesc, uint32_t acc) {
@@ -57,10 +61,11 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16
 
 // GROUPS: of a tile's columns (128 / group)
 template <int GROUPS, int NTOK>
-__global__ void __launch_bounds__(kThreads, 1) w4_tc_kernel(const __grid_constant__ CUtensorMap tx, const __grid_constant__ W4Args a) {
+__global__ void __launch_bounds__(Cfg<NTOK>::kThreads, 1) w4_tc_kernel(const __grid_constant__ CUtensorMap tx, const __grid_constant__ W4Args a) {
   using C = Cfg<NTOK>;
+  constexpr int kStages = C::kStages, kSums = C::kSums, kSumWarps = C::kSumWarps, kLoadWarp = C::kLoadWarp, kXWarp = C::kXWarp, kMmaWarp = C::kMmaWarp;
   extern __shared__ uint8_t smem_raw[];
-  __shared__ __align__(8) Bars bars;
+  __shared__ __align__(8) Bars<NTOK> bars;
   __shared__ uint32_t s_tmem;
   __shared__ int s_abort;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -78,6 +83,8 @@ __global__ void __launch_bounds__(kThreads, 1) w4_tc_kernel(const __grid_constan
     for (int i = 0; i < kBufs; ++i) {
       mbar_init(smem_u32(&bars.a[i]), kCodeWarps / 2);
       mbar_init(smem_u32(&bars.a_free[i]), 1u);
+    }
+    for (int i = 0; i < kSums; ++i) {
       mbar_init(smem_u32(&bars.d[i]), 1u);
       mbar_init(smem_u32(&bars.d_free[i]), kSumWarps);
     }
@@ -145,32 +152,41 @@ __global__ void __launch_bounds__(kThreads, 1) w4_tc_kernel(const __grid_constan
       if (lane == 0) mbar_arrive(smem_u32(&bars.empty[st]));
     }
   } else if (warp < kCodeWarps + kSumWarps) {
-    const int row = threadIdx.x - 32 * kCodeWarps;
-    f2_t acc[NTOK / 2];
+    // a row a thread, and of 128 tokens half
+    constexpr int kMine = NTOK > 64 ? 64 : NTOK, kOnce = NTOK > 64 ? 16 : 32;
+    const int row = threadIdx.x & 127, col0 = kMine * ((warp - kCodeWarps) >> 2);
+    f2_t acc[kMine / 2];
 #pragma unroll
-    for (int i = 0; i < NTOK / 2; ++i) acc[i] = f2(0.f, 0.f);
+    for (int i = 0; i < kMine / 2; ++i) acc[i] = f2(0.f, 0.f);
     int n = 0;  // groups so far
     for (int t = 0; t < count; ++t) {
       const int st = t % kStages;
       bool ok = true;
       const uint32_t from = ring + (st * 8 + (row >> 4)) * tile + 1024 + (row & 15) * 2;
-#pragma unroll
+#pragma unroll(NTOK > 64 ? 1 : GROUPS)  // (four groups' registers would not do)
       for (int gi = 0; gi < GROUPS; ++gi, ++n) {
-        if (!(ok = ok && wait2(kErrTimeoutAcc, bars.d[n % kBufs], n / kBufs, bars.full[st], t / kStages))) break;
+        if (!(ok = ok && wait2(kErrTimeoutAcc, bars.d[n % kSums], n / kSums, bars.full[st], t / kStages))) break;
         const float s = __uint_as_float(lds_u16(from + gi * 32) << 16);
         const f2_t scale = f2(s, s);
         tc_fence_after();
 #pragma unroll
-        for (int c = 0; c < NTOK; c += 32) {
-          uint32_t v[32];
-          tmem_ld32_nowait(tmem + lanes + (n % kBufs) * NTOK + c, v);
-          tmem_wait_ld32(v);
-          if (c + 32 == NTOK) {
+        for (int c = 0; c < kMine; c += kOnce) {
+          uint32_t v[kOnce];
+          if constexpr (kOnce == 16) {
+            float w[16];
+            tmem_ld16(tmem + lanes + (n % kSums) * NTOK + col0 + c, w);
+#pragma unroll
+            for (int k = 0; k < 16; ++k) v[k] = __float_as_uint(w[k]);
+          } else {
+            tmem_ld32_nowait(tmem + lanes + (n % kSums) * NTOK + c, v);
+            tmem_wait_ld32(v);
+          }
+          if (c + kOnce == kMine) {
             tc_fence_before();
-            arrive(bars.d_free[n % kBufs]);
+            arrive(bars.d_free[n % kSums]);
           }
 #pragma unroll
-          for (int k = 0; k < 32; k += 2)
+          for (int k = 0; k < kOnce; k += 2)
             acc[(c + k) / 2] = ffma2(f2(__uint_as_float(v[k]), __uint_as_float(v[k + 1])), scale, acc[(c + k) / 2]);
         }
       }
@@ -180,11 +196,12 @@ __global__ void __launch_bounds__(kThreads, 1) w4_tc_kernel(const __grid_constan
     // the CTA's sums [tokens][rows], where x was: its last product is done
     static_assert(NTOK * kPitch * 4 <= kStages * 2 * C::kHalf, "sums over x alone");
 #pragma unroll
-    for (int i = 0; i < NTOK / 2; ++i) {
+    for (int i = 0; i < kMine / 2; ++i) {
       float x, y;
       f2_split(acc[i], x, y);
-      asm volatile("st.shared.f32 [%0], %1;" ::"r"(xring + (2 * i * kPitch + row) * 4), "f"(x) : "memory");
-      asm volatile("st.shared.f32 [%0], %1;" ::"r"(xring + ((2 * i + 1) * kPitch + row) * 4), "f"(y) : "memory");
+      const uint32_t to = xring + ((col0 + 2 * i) * kPitch + row) * 4;
+      asm volatile("st.shared.f32 [%0], %1;" ::"r"(to), "f"(x) : "memory");
+      asm volatile("st.shared.f32 [%0], %1;" ::"r"(to + kPitch * 4), "f"(y) : "memory");
     }
   } else {
     if (warp == kLoadWarp || warp == kXWarp) {
@@ -226,15 +243,15 @@ __global__ void __launch_bounds__(kThreads, 1) w4_tc_kernel(const __grid_constan
         const uint64_t xd = smem_desc_kmajor<64>(xring + st * 2 * C::kHalf);
 #pragma unroll
         for (int gi = 0; gi < GROUPS; ++gi, ++n) {
-          if (!(ok = ok && wait(kErrTimeoutAcc, bars.a[t % kBufs], t / kBufs, bars.d_free[n % kBufs], n / kBufs + 1, bars.full[st], t / kStages))) break;
+          if (!(ok = ok && wait(kErrTimeoutAcc, bars.a[t % kBufs], t / kBufs, bars.d_free[n % kSums], n / kSums + 1, bars.full[st], t / kStages))) break;
           tc_fence_after();
           if (leader) {
 #pragma unroll
             for (int k = 0; k < 8 / GROUPS; ++k) {
               const int kk = gi * (8 / GROUPS) + k;
-              mma_ts(tmem + (n % kBufs) * NTOK, tmem + kA + (t % kBufs) * 64 + kk * 8, xd + (((kk >> 2) * C::kHalf + (kk & 3) * 32) >> 4), id, k > 0);
+              mma_ts(tmem + (n % kSums) * NTOK, tmem + kA + (t % kBufs) * 64 + kk * 8, xd + (((kk >> 2) * C::kHalf + (kk & 3) * 32) >> 4), id, k > 0);
             }
-            if (!a.fault) tc_commit(smem_u32(&bars.d[n % kBufs]));
+            if (!a.fault) tc_commit(smem_u32(&bars.d[n % kSums]));
           }
           __syncwarp();
         }
@@ -260,22 +277,40 @@ __global__ void __launch_bounds__(kThreads, 1) w4_tc_kernel(const __grid_constan
   cluster_wait();
 }
 
+// The split of a's columns with NTOK tokens a CTA, and its time.  With 128 a tile takes half as long again
+// as with 64, and beginning and end two fifths.
 template <int GROUPS, int NTOK>
-cudaError_t launch_t(W4Args a, cudaStream_t s) {
+cudaError_t plan(const W4Args& a, W4Split* best) {
   const auto kernel = w4_tc_kernel<GROUPS, NTOK>;
   const size_t smem = Cfg<NTOK>::smem(w4_tile_bytes(GROUPS, true));
   const cudaError_t e = smem_optin(reinterpret_cast<const void*>(kernel), smem);
   if (e != cudaSuccess) return e;
+  const int64_t blocks = (int64_t)((a.N + kRows - 1) / kRows) * ((a.M + NTOK - 1) / NTOK);
+  *best = w4_split(kernel, blocks, a.tiles, NTOK > 64 ? 12 : 8, Cfg<NTOK>::kThreads, smem, NTOK > 64 ? 14 : kW4Start);
+  return cudaSuccess;
+}
+
+template <int GROUPS, int NTOK>
+cudaError_t launch_t(W4Args a, const W4Split& best, cudaStream_t s) {
   CUtensorMap tx;
   if (!w4_x_map(&tx, &a, NTOK, 2)) return cudaErrorInvalidValue;
   const int blocks = (a.N + kRows - 1) / kRows, toks = (a.M + NTOK - 1) / NTOK;
-  a.split = w4_split(kernel, (int64_t)blocks * toks, a.tiles, 8, kThreads, smem).split;
-  return launch_cluster_kernel(kernel, dim3((unsigned)(blocks * a.split), (unsigned)toks), dim3(kThreads), (unsigned)a.split, smem, s, tx, a);
+  a.split = best.split;
+  return launch_cluster_kernel(w4_tc_kernel<GROUPS, NTOK>, dim3((unsigned)(blocks * a.split), (unsigned)toks), dim3(Cfg<NTOK>::kThreads),
+                               (unsigned)a.split, Cfg<NTOK>::smem(w4_tile_bytes(GROUPS, true)), s, tx, a);
 }
 
+// Tokens a CTA: 32 or 64 where that is all, above it what takes less time by the plan.  4096 columns x 14336 rows,
+// 128 tokens: 64 a CTA 35.6 us, 128 23.5; 256 tokens 50.7 and 46, 512 100 and 67; but 4096 x 4096, 128 tokens 11.7 and
+// 12.9.
 template <int GROUPS>
 cudaError_t launch_g(const W4Args& a, cudaStream_t s) {
-  return a.M <= 32 ? launch_t<GROUPS, 32>(a, s) : launch_t<GROUPS, 64>(a, s);
+  W4Split best, wide;
+  cudaError_t e = a.M <= 32 ? plan<GROUPS, 32>(a, &best) : plan<GROUPS, 64>(a, &best);
+  if (e == cudaSuccess && a.M > 64) e = plan<GROUPS, 128>(a, &wide);
+  if (e != cudaSuccess) return e;
+  if (a.M <= 32) return launch_t<GROUPS, 32>(a, best, s);
+  return wide.time < best.time ? launch_t<GROUPS, 128>(a, wide, s) : launch_t<GROUPS, 64>(a, best, s);
 }
 
 }  // namespace

@@ -92,8 +92,8 @@ __device__ __forceinline__ void w4_finish(const W4Args& a, uint32_t part, int pi
 }
 
 // CTAs (a cluster) that the columns of each of `blocks` blocks are split over, by the time that the rounds
-// of clusters take: a CTA's is its tiles, each of `weight` eighths, and kW4Start more for its beginning and
-// end (3 us of 0.3 each).  14336 columns, 32 blocks of 128 rows, one token: 1 CTA each 38.8 us, 2 21.4, 4 13, 8
+// of clusters take: a CTA's is its tiles, each of `weight` eighths, and `start` more for its beginning and
+// end (kW4Start: 3 us of 0.3 each).  14336 columns, 32 blocks of 128 rows, one token: 1 CTA each 38.8 us, 2 21.4, 4 13, 8
 // 24.0 (the GPU does not hold 32 clusters of 8 at once).
 constexpr int kW4Start = 10;
 struct W4Split {
@@ -101,12 +101,12 @@ struct W4Split {
   int64_t time = INT64_MAX;
 };
 template <typename... KArgs>
-W4Split w4_split(void (*kernel)(KArgs...), int64_t blocks, int tiles, int weight, int threads, size_t smem) {
+W4Split w4_split(void (*kernel)(KArgs...), int64_t blocks, int tiles, int weight, int threads, size_t smem, int start = kW4Start) {
   W4Split best;
   for (int s = 1; s <= 8 && s <= tiles; s *= 2) {
     const int fit = cluster_fit(reinterpret_cast<const void*>(kernel), s, threads, smem);
     if (fit <= 0) continue;
-    const int64_t time = (blocks + fit - 1) / fit * ((tiles + s - 1) / s * weight + 8 * kW4Start);
+    const int64_t time = (blocks + fit - 1) / fit * ((tiles + s - 1) / s * weight + 8 * start);
     if (time < best.time) {
       best.time = time;
       best.split = s;

@@ -69,6 +69,12 @@ def test_rows(sp, ctx, M, group, zeros):
     _run(sp, ctx, M, 5 * 128 + group, 264, group, zeros, torch.float32)
 
 
+@pytest.mark.parametrize("M", [66, 127, 128, 129, 192, 300])
+@pytest.mark.parametrize("K,N,group,zeros", [(96, 24, 32, True), (1024, 2048, 64, False), (4096, 1000, 128, True), (640, 5000, 32, False)])
+def test_many_rows(sp, ctx, M, K, N, group, zeros):
+    _run(sp, ctx, M, K, N, group, zeros, torch.float32)
+
+
 @pytest.mark.parametrize("K,N,group", [(32, 8, 32), (64, 8, 64), (128, 16, 128), (160, 24, 32), (352, 128, 32), (384, 136, 128), (448, 1000, 64),
                                        (1024, 2048, 128), (2048, 520, 128), (4000, 72, 32), (16384, 64, 128), (256, 16384, 64), (8192, 1032, 32)])
 @pytest.mark.parametrize("M", [1, 5, 16, 40])
@@ -210,12 +216,13 @@ def test_waits_end(sp):
     ctx.close()
 
 
-def test_a_missing_signal_is_reported(sp):
+@pytest.mark.parametrize("M", [40, 128])
+def test_a_missing_signal_is_reported(sp, M):
     """The tensor cores' signal withheld: the wait for it gives up, the call is reported, and the next one works."""
     ctx = sp.Context(0)
-    x, codes, scales, _ = _inputs(40, 1024, 256, 128, False)
+    x, codes, scales, _ = _inputs(M, 1024, 256, 128, False)
     w = sp.W4(ctx, codes.cuda(), scales.cuda())
-    y = torch.full((40, 256), 7.0, device="cuda")
+    y = torch.full((M, 256), 7.0, device="cuda")
     ctx.sync()
     ctx.set_wait_limit(20_000_000)
     ctx.set_fault(1)
