@@ -336,7 +336,7 @@ def main():
         print(f"{len(p)} tokens -> {t}")
     for p, t in zip(prompts, model.generate(prompts, 16, draft=repeats)):
         print(f"{len(p)} tokens, drafts -> {t}")
-    for p, t in zip(prompts, model.generate(prompts, 16, penalties=(1.0, 100.0, 0.0, 1.0))):
+    for p, t in zip(prompts, model.generate(prompts, 16, penalties=(1.0, 1e4, 0.0, 1.0))):
         print(f"{len(p)} tokens, none twice -> {t}")
     ctx.close()
 
