@@ -2,6 +2,7 @@
 // Declarations and documentation: include/sparoa.h.
 #include <cuda_runtime.h>
 
+#include <algorithm>
 #include <atomic>
 #include <cmath>
 #include <cstdarg>
@@ -1637,8 +1638,10 @@ sparoa_status attend(sparoa_ctx* ctx, const void* q, int64_t ld_q, int64_t T, in
       if (rules->cap > 0.f) {
         // tanh(t) = t p(t^2) for |t| <= 1/2, four coefficients fitted to the least error (1.3e-7)
         const double c[4] = {0.9999976761177359, -0.33320654956697676, 0.13145143396128597, -0.04337242821643758};
-        const double k = (double)scale / rules->cap;
-        for (int i = 0; i < 4; ++i) a.cap_near[i] = (float)(c[i] * std::pow(k, 2 * i) * scale * 1.4426950408889634);
+        constexpr double most = 1.7e38;  // (twice that is finite)
+        a.cap_turn = (float)std::min((double)scale / rules->cap, most);
+        for (int i = 0; i < 4; ++i) a.cap_near[i] = (float)(c[i] * std::min(scale * 1.4426950408889634, most));
+        a.cap_log2 = (float)std::min(rules->cap * 1.4426950408889634, most);
       }
       if (rules->cap > 0.f || rules->slopes) {  // (changed scores are powers of 2: paged.cuh)
         a.unit = 0.6931471805599453f;

@@ -327,22 +327,22 @@ __host__ __device__ constexpr int walk_of(int rules) { return rules == kPlain ? 
 // t p(t^2), on packed pairs; else 1 - 2 / (1 + exp(2 t)), off by a few 2^-24.
 struct Capped {
   const PagedArgs& a;
-  float k;
-  __device__ __forceinline__ explicit Capped(const PagedArgs& args) : a(args), k(args.scale / args.cap) {}
-  // (p's coefficients hold powers of k: none of them counts and is flushed for such q k)
-  __device__ __forceinline__ bool near(float top) const { return top * k <= 0.5f && top <= 1024.f; }
+  __device__ __forceinline__ explicit Capped(const PagedArgs& args) : a(args) {}
+  __device__ __forceinline__ bool near(float top) const { return top * a.cap_turn <= 0.5f && top <= 1024.f; }
+  __device__ __forceinline__ f2_t turn(f2_t s) const { return fmul2(s, f2(a.cap_turn, a.cap_turn)); }
+  // what s is multiplied by (t goes into its square alone, so that no size of scale or cap leaves the range)
   __device__ __forceinline__ f2_t factor(f2_t s, float part) const {
     const float c0 = a.cap_near[0] * part, c1 = a.cap_near[1] * part, c2 = a.cap_near[2] * part, c3 = a.cap_near[3] * part;
-    const f2_t w = fmul2(s, s);
+    const f2_t t = turn(s), w = fmul2(t, t);
     return ffma2(w, ffma2(w, ffma2(w, f2(c3, c3), f2(c2, c2)), f2(c1, c1)), f2(c0, c0));
   }
   __device__ __forceinline__ f2_t near(f2_t s) const { return fmul2(s, factor(s, 1.f)); }
   __device__ __forceinline__ f2_t far(f2_t s) const {
-    const float e = k * 2.885390081777927f, top = a.cap * 1.4426950408889634f;
+    constexpr float e = 2.885390081777927f;
     float x, y;
-    f2_split(fmul2(s, f2(e, e)), x, y);
+    f2_split(fmul2(turn(s), f2(e, e)), x, y);
     f2_split(fadd2(f2(ex2_ftz(x), ex2_ftz(y)), f2(1.f, 1.f)), x, y);
-    return ffma2(f2(rcp_ftz(x), rcp_ftz(y)), f2(-2.f * top, -2.f * top), f2(top, top));
+    return ffma2(f2(rcp_ftz(x), rcp_ftz(y)), f2(-2.f * a.cap_log2, -2.f * a.cap_log2), f2(a.cap_log2, a.cap_log2));
   }
   __device__ __forceinline__ float near1(float s) const {
     float x, y;

@@ -1,0 +1,74 @@
+"""Capped attention scores on the GPU against 64 bits, over all that a cap and a scale may be: few rows, one tile of
+rows, two tiles.
+
+Tolerances.  A raw score q k is off by D 2^-24 of sum |q k|, which a cap passes on by its slope, 1 - tanh^2.  The
+capped score is off by 2^-20 of itself: the quotient's, the polynomial's, the tanh's and the product's roundings.  The
+log of the sum is off by the mean of its scores' errors, and a result by sum p |v - y| of them; half as much again
+is allowed for second orders.  Weights, their sums and the log take 2^-18 more, and probabilities rounded to
+one bf16 2^-8 of sum p |v|."""
+import math
+
+import pytest
+import torch
+
+from test_gpu_decoder import _batch, _close, _g, _seq
+
+pytestmark = pytest.mark.gpu
+
+ROWS = [(1, 300), (40, 500), (300, 700)]  # new and cached tokens; two rows of a key head a token
+
+
+@pytest.fixture(scope="module")
+def sp():
+    from paper_2511_19457_gb300 import sparoa
+    return sparoa
+
+
+@pytest.fixture(scope="module")
+def ctx(sp):
+    c = sp.Context(0)
+    yield c
+    c.sync()
+    c.close()
+
+
+def _check(sp, ctx, q, cache, batch, k, v, table, L, page, cap, scale, slopes=None):
+    """One sequence's new tokens q [n, H, D] behind L - n others."""
+    n, H, D = q.shape
+    rules = sp.ScoreRules(cap=cap, slopes=None if slopes is None else slopes.cuda())
+    y, lse = torch.full((n, H, D), float("nan"), dtype=torch.bfloat16, device="cuda"), torch.full((n, H), 5.0, device="cuda")
+    sp.sparoa_ruled_attention(ctx, q.cuda(), y, cache, batch, rules, scale=scale, lse=lse)
+    ctx.sync()
+    G = H // k.shape[1]
+    kk, vv = (_seq(t, table, 0, L, page).repeat_interleave(G, 0) for t in (k, v))
+    x = q.double().transpose(0, 1)
+    z = torch.tanh(x @ kk.transpose(1, 2) * scale / cap)
+    err = 2.0 ** -24 * D * scale * (x.abs() @ kk.abs().transpose(1, 2)) * (1 - z * z) + 2.0 ** -20 * (cap * z).abs()
+    s = cap * z
+    far = (torch.arange(L - n, L)[:, None] - torch.arange(L)[None]).double()
+    if slopes is not None:
+        s = s - slopes.double()[:, None, None] * far
+        err = err + 2.0 ** -21 * s.abs()
+    s = s.masked_fill(far < 0, -math.inf)
+    p = torch.softmax(s, -1)
+    want, size, off = p @ vv, p @ vv.abs(), 1.5 * (p * err)
+    tol = off.sum(-1) + 2.0 ** -18 + 2.0 ** -22 * torch.logsumexp(s, -1).abs()
+    got = lse.double().cpu().t()
+    assert ((got - torch.logsumexp(s, -1)).abs() <= tol).all(), f"lse off by {((got - torch.logsumexp(s, -1)).abs() - tol).max():.2e}"
+    extra = (2.0 ** -8 + 2.0 ** -17) * size + off @ vv.abs() + off.sum(-1)[..., None] * want.abs()
+    _close(y, want.transpose(0, 1), "y", extra=extra.transpose(0, 1))
+
+
+def _inputs(sp, n, L, seed, page=32, D=64, H=4, KH=2):
+    cache, batch, k, v, table = _batch(sp, [n], [L], page, KH, D, seed)
+    return torch.randn(n, H, D, generator=_g(seed + 1)), cache, batch, k, v, table
+
+
+@pytest.mark.parametrize("n,L", ROWS)
+@pytest.mark.parametrize("cap,scale", [(0.001, 1.4e3), (0.001, 1e6), (1.0, 1e8), (0.001, 2e38), (30.0, 1e-30)])
+def test_a_scale_of_any_size(sp, ctx, n, L, cap, scale):
+    """Scores that are zero (empty queries) beside a cap that others are far beyond."""
+    q, *rest = _inputs(sp, n, L, 11)
+    q[::3] = 0
+    q[:, 1] = 0
+    _check(sp, ctx, q.to(torch.bfloat16), *rest, L, 32, cap, scale)
