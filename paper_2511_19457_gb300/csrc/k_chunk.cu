@@ -477,6 +477,25 @@ __device__ __forceinline__ void put_pair(uint32_t (&s)[32], int k, f2_t v) {
   s[k + 1] = __float_as_uint(y);
 }
 
+// A row's 128 scores under their cap, where they lie.  (Large scores are rare: few instructions and
+// registers count here, not time.)
+__device__ __forceinline__ void cap_in_place(const Capped& cap, uint32_t ts) {
+#pragma unroll 1
+  for (int i = 0; i < 8; ++i) {
+    float v[16];
+    uint32_t c[16];
+    tmem_ld16(ts + i * 16, v);
+#pragma unroll
+    for (int k = 0; k < 16; k += 2) {
+      f2_split(cap.far(f2(v[k], v[k + 1])), v[k], v[k + 1]);
+      c[k] = __float_as_uint(v[k]);
+      c[k + 1] = __float_as_uint(v[k + 1]);
+    }
+    tmem_st16(ts + i * 16, c);
+  }
+  tmem_wait_st();
+}
+
 // 32 scores less slope times distance; the first key's distance is `far`.
 __device__ __forceinline__ void bias_scores(const RowRules& u, uint32_t (&s)[32], float far, float one) {
 #pragma unroll
@@ -505,9 +524,9 @@ __device__ __forceinline__ void mask_unit(const PagedArgs& a, const RowRules& u,
   for (int i = 0; i < 4; ++i) mask_scores<RULES>(a, u, s[i], key0 + i * 32);
 }
 
-// A unit's scores under their row's cap and bias.
+// A unit's scores, which are at `ts` too, under their row's cap and bias.
 template <int RULES>
-__device__ __forceinline__ void rule_scores(const PagedArgs& a, const RowRules& u, uint32_t (&s)[4][32], int key0) {
+__device__ __forceinline__ void rule_scores(const PagedArgs& a, const RowRules& u, uint32_t (&s)[4][32], uint32_t ts, int key0) {
   const bool caps = (RULES & kCap) && (!(RULES & kTree) || a.cap > 0.f);
   if (caps) {
     float size = 0.f;
@@ -521,10 +540,11 @@ __device__ __forceinline__ void rule_scores(const PagedArgs& a, const RowRules& 
 #pragma unroll
         for (int k = 0; k < 32; k += 2) put_pair(s[i], k, Capped(a).near(pair_at(s[i], k)));
     } else {
+      cap_in_place(Capped(a), ts);
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
+      for (int i = 0; i < 4; ++i) tmem_ld32_nowait(ts + i * 32, s[i]);
 #pragma unroll
-        for (int k = 0; k < 32; k += 2) put_pair(s[i], k, Capped(a).far(pair_at(s[i], k)));
+      for (int i = 0; i < 4; ++i) tmem_wait_ld32(s[i]);
     }
   }
   if ((RULES & kBias) && (!(RULES & kTree) || a.slopes)) {
@@ -628,19 +648,14 @@ __device__ __forceinline__ float changed_unit(const PagedArgs& a, const RowRules
   }
   if (!direct) {
     mx = -INFINITY;
+    if (caps && !near) cap_in_place(Capped(a), ts);
 #pragma unroll 1
     for (int i = 0; i < 4; ++i) {
       tmem_ld32_nowait(ts + i * 32, s);
       tmem_wait_ld32(s);
-      if (caps) {
-        if (near) {
+      if (caps && near)
 #pragma unroll
-          for (int k = 0; k < 32; k += 2) put_pair(s, k, Capped(a).near(pair_at(s, k)));
-        } else {
-#pragma unroll
-          for (int k = 0; k < 32; k += 2) put_pair(s, k, Capped(a).far(pair_at(s, k)));
-        }
-      }
+        for (int k = 0; k < 32; k += 2) put_pair(s, k, Capped(a).near(pair_at(s, k)));
       if (slopes) bias_scores(u, s, far - (float)(i * 32), caps ? 1.f : a.score_log2);
       if (!whole) mask_scores<RULES>(a, u, s, key0 + i * 32);
       float t[4];
@@ -788,7 +803,7 @@ __device__ __forceinline__ void softmax_role(const Role<walk_of(RULES)>& r, uint
             for (int i = 0; i < 4; ++i) tmem_ld32_nowait(ts + i * 32, s[i]);
 #pragma unroll
             for (int i = 0; i < 4; ++i) tmem_wait_ld32(s[i]);
-            rule_scores<RULES>(a, rule, s, key0);
+            rule_scores<RULES>(a, rule, s, ts, key0);
             if (!whole) mask_unit<RULES>(a, rule, s, key0);
             float mx[4];
             maxima(s, mx);

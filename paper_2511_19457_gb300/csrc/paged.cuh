@@ -324,11 +324,13 @@ __host__ __device__ constexpr int walk_of(int rules) { return rules == kPlain ? 
 
 // Scores under a cap or with a bias are weighed as powers of 2: log2(e) (cap tanh(scale q k /
 // cap) - slope distance).  Where |t| = |scale q k / cap| <= 1/2, as it mostly is, tanh(t) =
-// t p(t^2), on packed pairs; else 1 - 2 / (1 + exp(2 t)), off by a few 2^-24.
+// t p(t^2), on packed pairs; else 1 - 2 / (1 + exp(2 t)), off by a few 2^-24.  Which of them a
+// score goes by is its own affair: `near` is for scores that are all small, `far` for any, with
+// the same bits for a small one, so that a score's value does not depend on those beside it.
 struct Capped {
   const PagedArgs& a;
   __device__ __forceinline__ explicit Capped(const PagedArgs& args) : a(args) {}
-  __device__ __forceinline__ bool near(float top) const { return top * a.cap_turn <= 0.5f && top <= 1024.f; }
+  __device__ __forceinline__ bool near(float top) const { return top * a.cap_turn <= 0.5f; }
   __device__ __forceinline__ f2_t turn(f2_t s) const { return fmul2(s, f2(a.cap_turn, a.cap_turn)); }
   // what s is multiplied by (t goes into its square alone, so that no size of scale or cap leaves the range)
   __device__ __forceinline__ f2_t factor(f2_t s, float part) const {
@@ -339,10 +341,13 @@ struct Capped {
   __device__ __forceinline__ f2_t near(f2_t s) const { return fmul2(s, factor(s, 1.f)); }
   __device__ __forceinline__ f2_t far(f2_t s) const {
     constexpr float e = 2.885390081777927f;
-    float x, y;
-    f2_split(fmul2(turn(s), f2(e, e)), x, y);
+    float tx, ty, x, y, u, v;
+    f2_split(turn(s), tx, ty);
+    f2_split(fmul2(f2(tx, ty), f2(e, e)), x, y);
     f2_split(fadd2(f2(ex2_ftz(x), ex2_ftz(y)), f2(1.f, 1.f)), x, y);
-    return ffma2(f2(rcp_ftz(x), rcp_ftz(y)), f2(-2.f * a.cap_log2, -2.f * a.cap_log2), f2(a.cap_log2, a.cap_log2));
+    f2_split(ffma2(f2(rcp_ftz(x), rcp_ftz(y)), f2(-2.f * a.cap_log2, -2.f * a.cap_log2), f2(a.cap_log2, a.cap_log2)), x, y);
+    f2_split(near(s), u, v);
+    return f2(fabsf(tx) <= 0.5f ? u : x, fabsf(ty) <= 0.5f ? v : y);
   }
   __device__ __forceinline__ float near1(float s) const {
     float x, y;

@@ -72,3 +72,45 @@ def test_a_scale_of_any_size(sp, ctx, n, L, cap, scale):
     q[::3] = 0
     q[:, 1] = 0
     _check(sp, ctx, q.to(torch.bfloat16), *rest, L, 32, cap, scale)
+
+
+@pytest.mark.parametrize("n,L", ROWS)
+@pytest.mark.parametrize("cap", [1e3, 1e4, 1e6, 1e30, 3e38])
+def test_caps_far_above_the_scores(sp, ctx, n, L, cap):
+    """leave them as they are, products of more than 1024 too."""
+    q, *rest = _inputs(sp, n, L, 12)
+    _check(sp, ctx, (100 * q).to(torch.bfloat16), *rest, L, 32, cap, 0.01)
+
+
+@pytest.mark.parametrize("n,L", ROWS)
+@pytest.mark.parametrize("cap", [0.01, 2.0, 50.0, 54.0, 56.0, 1000.0])
+@pytest.mark.parametrize("biased", [False, True])
+def test_scores_small_and_large_in_turn(sp, ctx, n, L, cap, biased):
+    """Every other 128 keys are 40 times as large, and of those every fifth as small as the others."""
+    q, cache, batch, k, v, table = _inputs(sp, n, L, 13)
+    for j in range(L):
+        if j // 128 % 2 and j % 5:
+            k[int(table[0, j // 32]), :, j % 32] *= 40
+    cache.k.copy_(k)
+    slopes = torch.tensor([0.5, 0.1, 0.01, 0.0]) if biased else None
+    _check(sp, ctx, q.to(torch.bfloat16), cache, batch, k, v, table, L, 32, cap, 0.125, slopes)
+
+
+@pytest.mark.parametrize("n", [1, 40, 75, 300])
+@pytest.mark.parametrize("slopes", [False, True])
+@pytest.mark.parametrize("heads", [4, 6])
+def test_results_know_nothing_of_what_is_not_seen(sp, ctx, n, slopes, heads):
+    """The same bits whatever is in places that no token was written to, before the window and behind a token."""
+    outs = []
+    for fill in ("0", "nan", "inf", "30000"):
+        cache, batch, k, v, table = _batch(sp, [n], [700], 64, 2, 64, 14, fill=fill)
+        cache.k[int(table[0, 0])] = float(fill)  # before every token's window
+        q = torch.randn(n, heads, 64, generator=_g(15)).to(torch.bfloat16).cuda()
+        y, lse = torch.empty_like(q), torch.empty(n, heads, device="cuda")
+        rules = sp.ScoreRules(cap=30.0, slopes=torch.full((heads,), 0.02, device="cuda") if slopes else None)
+        sp.sparoa_ruled_attention(ctx, q, y, cache, batch, rules, window=300, lse=lse)
+        ctx.sync()
+        outs.append((y.clone(), lse.clone()))
+    assert outs[0][0].isfinite().all() and outs[0][1].isfinite().all()
+    for y, lse in outs[1:]:
+        assert torch.equal(y, outs[0][0]) and torch.equal(lse, outs[0][1])
