@@ -600,8 +600,8 @@ __device__ __forceinline__ void weigh(uint32_t (&s)[4][32], uint32_t ts, f2_t sc
 // 139, 138 and 148 us, since they take nearly as long as others), heads in turn instead of one after the
 // other (132.5).
 template <int RULES, typename Refer>
-__device__ __forceinline__ float changed_unit(const PagedArgs& a, const RowRules& u, uint32_t ts, int key0, bool whole, bool may_direct,
-                                              bool first, float m, const Refer& refer) {
+__device__ __forceinline__ float changed_unit(const PagedArgs& a, const RowRules& u, bool live, uint32_t ts, int key0, bool whole,
+                                              bool may_direct, bool first, float m, const Refer& refer) {
   const bool caps = (RULES & kCap) && (!(RULES & kTree) || a.cap > 0.f), slopes = (RULES & kBias) && (!(RULES & kTree) || a.slopes);
   const float far = (float)(u.pos - key0);
   float mx = -INFINITY;
@@ -634,12 +634,13 @@ __device__ __forceinline__ float changed_unit(const PagedArgs& a, const RowRules
         }
       }
     }
-    if (caps) near = __all_sync(0xffffffffu, Capped(a).near(size));
+    // (a row behind the item's last is another sequence's or none: it has no say)
+    if (caps) near = __all_sync(0xffffffffu, !live || Capped(a).near(size));
     direct = direct && near;
     mx = slopes ? bound : Capped(a).near1(size);
     // too far away for any weight of the unit (a score that is no number has one all the same, and is
     // carried through the maxima for that)
-    if (slopes && bounded && near && !first && __all_sync(0xffffffffu, mx < m - kGoneLog2)) {
+    if (slopes && bounded && near && !first && __all_sync(0xffffffffu, !live || mx < m - kGoneLog2)) {
       const uint32_t none[16] = {};
 #pragma unroll
       for (int i = 0; i < 4; ++i) tmem_st16(ts + i * 16, none);
@@ -795,7 +796,7 @@ __device__ __forceinline__ void softmax_role(const Role<walk_of(RULES)>& r, uint
             return m == -INFINITY ? 0.f : -scaled_ref(m, sl2);
           };
           if (two) {
-            const float more = changed_unit<RULES>(a, rule, ts, key0, whole, may_direct, j == j0, m, refer);
+            const float more = changed_unit<RULES>(a, rule, live, ts, key0, whole, may_direct, j == j0, m, refer);
             l += more;  // (l may have been brought to another reference)
           } else {
             uint32_t s[4][32];

@@ -114,3 +114,23 @@ def test_results_know_nothing_of_what_is_not_seen(sp, ctx, n, slopes, heads):
     assert outs[0][0].isfinite().all() and outs[0][1].isfinite().all()
     for y, lse in outs[1:]:
         assert torch.equal(y, outs[0][0]) and torch.equal(lse, outs[0][1])
+
+
+@pytest.mark.parametrize("n", [1, 40, 75, 300])
+@pytest.mark.parametrize("slopes", [False, True])
+def test_results_know_nothing_of_other_sequences(sp, ctx, n, slopes):
+    """The same bits whatever the next sequence asks for."""
+    outs = []
+    for loud in (0.0, 1.0, 1e4, float("nan")):
+        cache, batch, *_ = _batch(sp, [n, 70], [700, 300], 64, 2, 64, 16)
+        q = torch.randn(n + 70, 4, 64, generator=_g(17))
+        q[n:] *= loud
+        q = q.to(torch.bfloat16).cuda()
+        y, lse = torch.empty_like(q), torch.empty(n + 70, 4, device="cuda")
+        rules = sp.ScoreRules(cap=30.0, slopes=torch.full((4,), 0.02, device="cuda") if slopes else None)
+        sp.sparoa_ruled_attention(ctx, q, y, cache, batch, rules, lse=lse)
+        ctx.sync()
+        outs.append((y[:n].clone(), lse[:n].clone()))
+    assert outs[0][0].isfinite().all() and outs[0][1].isfinite().all()
+    for y, lse in outs[1:]:
+        assert torch.equal(y, outs[0][0]) and torch.equal(lse, outs[0][1])
