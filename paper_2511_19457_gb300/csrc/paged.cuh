@@ -323,14 +323,17 @@ enum Walk : int { kPlainWalk = 0, kRuledWalk = 1, kReversedWalk = 2 };
 __host__ __device__ constexpr int walk_of(int rules) { return rules == kPlain ? kPlainWalk : rules & kBias ? kReversedWalk : kRuledWalk; }
 
 // Scores under a cap or with a bias are weighed as powers of 2: log2(e) (cap tanh(scale q k /
-// cap) - slope distance).  Where |t| = |scale q k / cap| <= 1/2, as it mostly is, tanh(t) =
-// t p(t^2), on packed pairs; else 1 - 2 / (1 + exp(2 t)), off by a few 2^-24.  Which of them a
-// score goes by is its own affair: `near` is for scores that are all small, `far` for any, with
-// the same bits for a small one, so that a score's value does not depend on those beside it.
+// cap) - slope distance).  Where |t| = |scale q k / cap| <= 3/8, as it mostly is, tanh(t) =
+// t p(t^2), on packed pairs, off by 3 2^-24 of itself; else 1 - 2 / (1 + exp(2 |t|)) with t's
+// sign, off by 9 2^-24 of itself at most.  (To 1/2 p takes a coefficient more, and 4 chunks of 1500 as in
+// k_chunk.cu 117 us where they take 113.)  Which of them a score goes by is its own affair:
+// `near` is for scores that are all small, `far` for any, with the same bits for a small one,
+// so that a score's value does not depend on those beside it.
 struct Capped {
+  static constexpr float kNear = 0.375f;
   const PagedArgs& a;
   __device__ __forceinline__ explicit Capped(const PagedArgs& args) : a(args) {}
-  __device__ __forceinline__ bool near(float top) const { return top * a.cap_turn <= 0.5f; }
+  __device__ __forceinline__ bool near(float top) const { return top * a.cap_turn <= kNear; }
   __device__ __forceinline__ f2_t turn(f2_t s) const { return fmul2(s, f2(a.cap_turn, a.cap_turn)); }
   // what s is multiplied by (t goes into its square alone, so that no size of scale or cap leaves the range)
   __device__ __forceinline__ f2_t factor(f2_t s, float part) const {
@@ -343,11 +346,11 @@ struct Capped {
     constexpr float e = 2.885390081777927f;
     float tx, ty, x, y, u, v;
     f2_split(turn(s), tx, ty);
-    f2_split(fmul2(f2(tx, ty), f2(e, e)), x, y);
+    f2_split(fmul2(f2(fabsf(tx), fabsf(ty)), f2(e, e)), x, y);
     f2_split(fadd2(f2(ex2_ftz(x), ex2_ftz(y)), f2(1.f, 1.f)), x, y);
     f2_split(ffma2(f2(rcp_ftz(x), rcp_ftz(y)), f2(-2.f * a.cap_log2, -2.f * a.cap_log2), f2(a.cap_log2, a.cap_log2)), x, y);
     f2_split(near(s), u, v);
-    return f2(fabsf(tx) <= 0.5f ? u : x, fabsf(ty) <= 0.5f ? v : y);
+    return f2(fabsf(tx) <= kNear ? u : copysignf(x, tx), fabsf(ty) <= kNear ? v : copysignf(y, ty));
   }
   __device__ __forceinline__ float near1(float s) const {
     float x, y;

@@ -298,7 +298,7 @@ struct PagedArgs {
   int ruled = 0;
   float cap = 0.f;                   // above 0: scores s become cap tanh(s / cap)
   float cap_turn = 0.f;              // t = cap_turn s = scale s / cap
-  float cap_near[4] = {};            // log2(e) cap tanh(t) = s p(t^2) where |t| <= 1/2
+  float cap_near[4] = {};            // log2(e) cap tanh(t) = s p(t^2) where |t| <= 3/8
   float cap_log2 = 0.f;              // log2(e) cap
   float score_log2 = 0.f;            // scale log2(e)
   const float* slopes = nullptr;     // [heads] or null: less slope times the distance

@@ -134,3 +134,29 @@ def test_results_know_nothing_of_other_sequences(sp, ctx, n, slopes):
     assert outs[0][0].isfinite().all() and outs[0][1].isfinite().all()
     for y, lse in outs[1:]:
         assert torch.equal(y, outs[0][0]) and torch.equal(lse, outs[0][1])
+
+
+@pytest.mark.parametrize("n", [1, 40, 300])
+@pytest.mark.parametrize("cap", [0.01, 5.0, 50.0, 1e4, 1e30])
+def test_capped_scores_have_fp32_bits(sp, ctx, n, cap):
+    """A row's keys are all alike, so that the log of the sum is its score and the log of their number; off by
+    2^-21 of the score and by 2^-20 for the sum's weights (2^-22), the logs and their sum."""
+    H, D, L = 8, 64, 700
+    cache, batch, k, v, table = _batch(sp, [n], [L], 64, 1, D, 18)
+    k[:] = 0
+    k[..., 0] = 1
+    cache.k.copy_(k)
+    q = torch.zeros(n, H, D)
+    t = torch.exp(torch.rand(n, H, generator=_g(19)) * math.log(1e5) + math.log(1e-4)).clamp(max=10.0)
+    if n == 1:
+        t[0] = torch.tensor([1e-3, 0.01, 0.1, 0.3, 0.45, 0.55, 1.0, 3.0])
+    q[..., 0] = (t * min(cap, 1e30)).clamp(max=100.0) * torch.where(torch.arange(H) % 3 == 0, -1.0, 1.0)
+    q = q.to(torch.bfloat16)
+    y, lse = torch.empty(n, H, D, dtype=torch.bfloat16, device="cuda"), torch.empty(n, H, device="cuda")
+    sp.sparoa_ruled_attention(ctx, q.cuda(), y, cache, batch, sp.ScoreRules(cap=cap), scale=1.0, lse=lse)
+    ctx.sync()
+    score = cap * torch.tanh(q[..., 0].double() / cap)
+    keys = torch.arange(L - n + 1, L + 1).double().log()[:, None]
+    err = (lse.double().cpu() - score - keys).abs()
+    tol = 2.0 ** -21 * score.abs() + 2.0 ** -20 * (1 + keys)
+    assert (err <= tol).all(), f"off by {(err / tol).max():.2f} of what is allowed"
