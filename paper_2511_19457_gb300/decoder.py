@@ -150,7 +150,8 @@ class Decoder:
         """Judge drafted tokens.  drafts[i] = (tokens, parents) of seqs[i], the first token the last one that is
         settled (and not in the cache yet), the others drafted behind their parents (parents[0] = -1).
         Returns for each sequence its next tokens: the drafted ones that the model would have chosen itself
-        (greedily), and the one that it chooses after them.  The cache keeps what is settled."""
+        (greedily), and the one that it chooses after them.  The cache keeps what is settled.  Where the model
+        chooses nothing (no logit is a number above -infinity), that is an error, and the cache as it was."""
         if len(drafts) != len(seqs) or len(set(seqs)) != len(seqs):
             raise ValueError("check: a tree for each sequence, and no sequence twice")
         new = [len(t) for t, _ in drafts]
@@ -176,6 +177,8 @@ class Decoder:
             sp.sparoa_tree_accept(self.ctx, flat, best, tree, [w["cache"] for w in self.layers], batch, path, count, following, length)
             self.ctx.sync()  # (reports device-side failures)
             ways, counts, after, lengths = path.tolist(), count.tolist(), following.tolist(), length.tolist()
+            if min(after, default=0) < 0:
+                raise ValueError("check: a sequence that no token may follow")
         except BaseException:
             self.pages.shrink_all(seqs, new)
             raise
