@@ -137,8 +137,8 @@ class Decoder:
         self.hidden = hidden
 
     def forward(self, tokens: torch.Tensor, seqs, new) -> torch.Tensor:
-        """tokens int64 [T], new[i] of each of seqs one after the other, appended to their cached ones;
-        returns the logits [T, vocab] (fp32).  A step that raises changes no sequence's length."""
+        """tokens int64 [T], below the vocabulary's size (check and generate look, this does not), new[i] of
+        each of seqs one after the other, appended to their cached ones; returns the logits [T, vocab] (fp32).  A step that raises changes no sequence's length."""
         self.pages.grow_all(seqs, new)
         try:
             return self._forward(tokens, seqs, new)
@@ -158,6 +158,7 @@ class Decoder:
         bits = [b for _, parents in drafts for b in ancestors(parents)]
         if any(len(t) != len(p) or not t or p[0] != -1 for t, p in drafts):
             raise ValueError("check: a tree begins with the last settled token and has a parent for each token")
+        self._known(t for tokens, _ in drafts for t in tokens)
         dev = self.embed.device
         flat = torch.tensor([t for tokens, _ in drafts for t in tokens], dtype=torch.int32).to(dev)
         tree = torch.tensor([b - (1 << 64) if b >> 63 else b for b in bits], dtype=torch.int64).to(dev)
@@ -188,6 +189,12 @@ class Decoder:
             self.pages.cut(s, L)
             at += n
         return out
+
+    def _known(self, tokens):
+        """Raises for a token that has no embedding (its row would be looked up on the GPU all the same)."""
+        for t in tokens:
+            if not 0 <= t < self.embed.shape[0]:
+                raise ValueError(f"token {t} of {self.embed.shape[0]}")
 
     def _forward(self, tokens, seqs, new):
         return self._layers(tokens, self.pages.batch(seqs, new, tokens.device))
@@ -249,6 +256,7 @@ class Decoder:
         Drafts go with none of the three others."""
         if not all(prompts):
             raise ValueError("generate: a prompt without tokens")
+        self._known(t for p in prompts for t in p)
         if draft is not None and not (penalties is None and bias is None and allowed is None):
             raise ValueError("generate: drafts are judged by the logits as they are")
         if not prompts:

@@ -78,3 +78,18 @@ def test_a_choice_of_nothing_is_an_error(model):
     with pytest.raises(ValueError):
         model.generate([[1, 2], [3]], 12, draft=lambda text: ([(text[-1] + 1) % 10], [-1]))
     assert len(model.pages.free) == 3  # ("a" and "b" hold theirs)
+
+
+def test_tokens_outside_the_vocabulary(model):
+    """are refused on the host: the embedding's rows are looked up on the GPU."""
+    model.pages.grow("a", 15)
+    before = copy.deepcopy((sorted(model.pages.free), model.pages.held, model.pages.length))
+    for bad in (10, -1, 1 << 40):
+        for tokens, parents in (([1, bad], [-1, 0]), ([bad], [-1])):
+            with pytest.raises(ValueError):
+                model.check([(tokens, parents)], ["a"])
+        with pytest.raises(ValueError):
+            model.generate([[1], [2, bad, 3]], 2)
+        with pytest.raises(ValueError):
+            model.generate([[1], [2]], 4, draft=lambda text: ([bad], [-1]))
+    assert (sorted(model.pages.free), model.pages.held, model.pages.length) == before
