@@ -553,8 +553,9 @@ sparoa_status sparoa_paged_attention(sparoa_ctx *ctx, const void *q, int64_t ld_
  * and j > p - window (window > 0).  What is NULL (0) is left out.
  *   cap     > 0 (from 0.001): a score s = scale q k becomes cap tanh(s / cap)
  *   slopes  device fp32 [heads], finite: then s - slopes[head] |p - j|
- *   prefix  device int32 [batch]: with causal, keys j < prefix[b] are seen too, whatever
- *           the token's position (a prompt's first part that all of it sees)
+ *   prefix  device int32 [batch]: with causal, keys p < j < prefix[b] are seen too (a
+ *           prompt's first part, whose tokens all see each other); a window hides what is
+ *           behind it all the same
  *   tree    device uint64 [T]: with causal, without prefix: a sequence's new tokens (at
  *           most 64) are a tree, and bit i of tree[row] says that new token i is an
  *           ancestor; bits at and above the token's own are ignored.  A token sees the

@@ -606,8 +606,8 @@ def sparoa_paged_attention(ctx: Context, q, y, cache: KVCache, batch: PagedBatch
 
 class ScoreRules:
     """Rules of sparoa_ruled_attention; keeps its tensors alive.  cap: scores s become cap tanh(s / cap); slopes
-    fp32 [heads]: less slope |distance|; prefix int32 [batch]: keys that every new token sees; tree int64
-    [T]: bits of each new token's ancestors among its sequence's new tokens."""
+    fp32 [heads]: less slope |distance|; prefix int32 [batch]: keys that every new token sees, within its window;
+    tree int64 [T]: bits of each new token's ancestors among its sequence's new tokens."""
 
     def __init__(self, cap=0.0, slopes=None, prefix=None, tree=None):
         for t, types in ((slopes, _FP32S), (prefix, _I32S), (tree, (torch.int64,))):
