@@ -242,7 +242,8 @@ sparoa_status sparoa_last_path(sparoa_ctx *ctx, int32_t *path);
  * sparoa_set_fault: 1 = the tensor-core kernels' MMA issuer withholds its
  * signal for the first accumulator of each CTA until the code is set back to
  * 0, so that the epilogue's bounded wait runs out (no fault, trap or endless
- * loop on the GPU); 2 = the next workspace allocation of the context fails
+ * loop on the GPU; sparoa_gemm_w4 up to 16 rows: the signals that a stage of
+ * its loads is free); 2 = the next workspace allocation of the context fails
  * (SPAROA_ERR_OOM), once; 0 = off.
  * Errors: INVALID_ARG (ctx NULL, negative cycles, unknown code). */
 sparoa_status sparoa_set_wait_limit(sparoa_ctx *ctx, int64_t cycles);

@@ -179,7 +179,7 @@ __global__ void __launch_bounds__(kThreads, 1) w4_kernel(const __grid_constant__
         }
       }
       __syncwarp();
-      if (lane == 0) mbar_arrive(smem_u32(&s_empty[st]));
+      if (lane == 0 && !a.fault) mbar_arrive(smem_u32(&s_empty[st]));
     }
   }
   // the CTA's sums [tokens][rows], where x was (every copy has arrived)

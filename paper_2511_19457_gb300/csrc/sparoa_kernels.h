@@ -376,7 +376,7 @@ struct W4Args {
   uint32_t* err = nullptr;
   long long wait_limit = 0;
   int x_boxed = 0;  // x's tensor map is of whole stages (w4_x_map)
-  int fault = 0;  // error-path tests: 1 withholds the signals of the tcgen05 kernel's sums
+  int fault = 0;  // error-path tests: 1 withholds the signals of the tcgen05 kernel's sums, or the other's of free stages
   // tiles of rows and of columns, tiles of rows of a block, CTAs of its columns (set by launch_w4)
   int row_tiles = 0, tiles = 0, block_tiles = 8, split = 1;
 };
