@@ -1,4 +1,4 @@
-"""Products with 4-bit weights: the way out of a wait that runs out in the kernel for few rows."""
+"""Products with 4-bit weights: the way out of a wait that runs out in the kernel for few rows, and GELU behind both."""
 import pytest
 import torch
 
@@ -30,4 +30,23 @@ def test_a_missing_signal_is_reported(sp, M):  # noqa: F811
     ctx.sync()
     w64 = _weights64(codes, scales, None, 128)
     _check(y, x.double() @ w64.t(), _bound(x, w64, 128), False, "after a missing signal")
+    ctx.close()
+
+
+@pytest.mark.parametrize("M,out", [(3, torch.bfloat16), (37, torch.float32), (100, torch.bfloat16)])
+def test_gelu(sp, M, out):  # noqa: F811
+    """The tanh form, whose slope is 1.13 at most; the hardware's tanh is off by 2^-11 of itself, which is 2^-12 of |x|
+    here; as much again is allowed for the form's other roundings."""
+    ctx = sp.Context(0)
+    K, N, group = 512, 328, 64
+    x, codes, scales, zero = _inputs(M, K, N, group, True)
+    b = torch.randn(N, generator=torch.Generator().manual_seed(5))
+    w = sp.W4(ctx, codes.cuda(), scales.cuda(), zero.cuda())
+    y = torch.empty(M, N, dtype=out, device="cuda")
+    sp.sparoa_gemm_w4(ctx, x.cuda(), w, y, bias=b.cuda(), act=sp.ACT_GELU)
+    ctx.sync()
+    w64 = _weights64(codes, scales, zero, group)
+    z = x.double() @ w64.t() + b.double()
+    want = torch.nn.functional.gelu(z, approximate="tanh")
+    _check(y, want, 1.13 * (_bound(x, w64, group) + 2.0 ** -22 * z.abs()) + 2.0 ** -11 * z.abs(), out == torch.bfloat16, "gelu")
     ctx.close()
