@@ -175,7 +175,6 @@ struct Role {
   __device__ __forceinline__ bool wait(unsigned long long& bar, unsigned parity, uint32_t bit) const {
     return mbar_wait_warp(smem_u32(&bar), parity, a.err, &sh.abort, bit, limit);
   }
-  __device__ __forceinline__ bool aborted() const { return *(volatile int*)&sh.abort != 0; }
   __device__ __forceinline__ int rows(const Cursor& c) const { return c.n * a.group - c.t * kRows; }
   // item n of the CTA's share; null after a timeout
   __device__ __forceinline__ const Cursor* item(unsigned n) const {
@@ -249,8 +248,8 @@ __device__ __forceinline__ void item_role(const Role<WALK>& r, const CUtensorMap
     if (!ok) break;
     c.next_item(a, r.sh.plan);
   }
-  // after a timeout: wait for the copies in flight into memory that is given back
-  if (boxes && r.aborted())
+  // no copy is in flight into memory that is given back, whichever wait of the CTA ran out and when
+  if (boxes)
     for (int tile = 0; tile < 2; ++tile)
       if (used[tile] > 0) mbar_drain(smem_u32(&bars.q[tile]), (used[tile] - 1) & 1u, r.limit);
 }
@@ -295,10 +294,9 @@ __device__ __forceinline__ void load_role(const Role<WALK>& r, const CUtensorMap
       ++n;
     }
   }
-  // after a timeout: wait for the copies in flight into memory that is given back
-  if (r.aborted())
-    for (unsigned i = n > (unsigned)C::kStages ? n - C::kStages : 0u; i < n; ++i)
-      mbar_drain(smem_u32(&r.sh.bars.full[i % C::kStages]), (i / C::kStages) & 1u, r.limit);
+  // no copy is in flight into memory that is given back (as above)
+  for (unsigned i = n > (unsigned)C::kStages ? n - C::kStages : 0u; i < n; ++i)
+    mbar_drain(smem_u32(&r.sh.bars.full[i % C::kStages]), (i / C::kStages) & 1u, r.limit);
 }
 
 // The MMAs.
@@ -438,11 +436,10 @@ __device__ __forceinline__ void mma_role(const Role<WALK>& r, uint32_t tmem) {
     }
     base += 2 * count;
   }
-  if (r.aborted()) {  // the MMAs issued so far end before tensor memory is given back
-    if (leader) tc_commit(smem_u32(&bars.drain));
-    __syncwarp();
-    mbar_drain(smem_u32(&bars.drain), 0u, r.limit);
-  }
+  // the MMAs end before tensor memory is given back (waits for them may run out after this warp's)
+  if (leader) tc_commit(smem_u32(&bars.drain));
+  __syncwarp();
+  mbar_drain(smem_u32(&bars.drain), 0u, r.limit);
 }
 
 // A row's 128 scores of keys from key0 on: their largest in each 32 (several maxima side by

@@ -125,10 +125,9 @@ __global__ void __launch_bounds__(kThreads, 1) w4_kernel(const __grid_constant__
           if (second) tile_codes(1);
         }
       }
-      // after a timeout: no copy is in flight into shared memory that is given back (where the other warp
-      // gave out none, this waits its limit)
-      if (*(volatile int*)&s_abort)
-        for (int i = s > kStages ? s - kStages : 0; i < s; ++i) mbar_drain(smem_u32(&s_full[i % kStages]), (i / kStages) & 1u, limit);
+      // no copy is in flight into shared memory that is given back, whichever wait of the CTA ran out and
+      // when (where the other warp gave out none, this waits its limit)
+      for (int i = s > kStages ? s - kStages : 0; i < s; ++i) mbar_drain(smem_u32(&s_full[i % kStages]), (i / kStages) & 1u, limit);
     }
     __syncwarp();
   } else if (team < kTeams && mine < rows) {

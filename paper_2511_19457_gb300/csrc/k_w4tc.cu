@@ -227,10 +227,9 @@ __global__ void __launch_bounds__(Cfg<NTOK>::kThreads, 1) w4_tc_kernel(const __g
             }
           }
         }
-        // after a timeout: no copy is in flight into shared memory that is given back (the other warp's
-        // copies of a stage may be missing: then this waits its limit)
-        if (*(volatile int*)&s_abort)
-          for (int i = t > kStages ? t - kStages : 0; i < t; ++i) mbar_drain(smem_u32(&bars.full[i % kStages]), (i / kStages) & 1u, limit);
+        // no copy is in flight into shared memory that is given back, whichever wait of the CTA ran out and
+        // when (the other warp's copies of a stage may be missing: then this waits its limit)
+        for (int i = t > kStages ? t - kStages : 0; i < t; ++i) mbar_drain(smem_u32(&bars.full[i % kStages]), (i / kStages) & 1u, limit);
       }
       __syncwarp();
     } else if (warp == kMmaWarp) {
@@ -259,11 +258,10 @@ __global__ void __launch_bounds__(Cfg<NTOK>::kThreads, 1) w4_tc_kernel(const __g
         if (leader) tc_commit(smem_u32(&bars.a_free[t % kBufs]));
         __syncwarp();
       }
-      if (*(volatile int*)&s_abort) {  // the MMAs issued so far end before tensor memory is given back
-        if (leader) tc_commit(smem_u32(&bars.drain));
-        __syncwarp();
-        mbar_drain(smem_u32(&bars.drain), 0u, limit);
-      }
+      // the MMAs end before tensor memory is given back (waits for them may run out after this warp's)
+      if (leader) tc_commit(smem_u32(&bars.drain));
+      __syncwarp();
+      mbar_drain(smem_u32(&bars.drain), 0u, limit);
     }
   }
   tc_fence_before();

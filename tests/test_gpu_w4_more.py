@@ -50,3 +50,28 @@ def test_gelu(sp, M, out):  # noqa: F811
     want = torch.nn.functional.gelu(z, approximate="tanh")
     _check(y, want, 1.13 * (_bound(x, w64, group) + 2.0 ** -22 * z.abs()) + 2.0 ** -11 * z.abs(), out == torch.bfloat16, "gelu")
     ctx.close()
+
+
+@pytest.mark.parametrize("M", [4, 40, 128])
+def test_waits_of_a_cycle(sp, M):  # noqa: F811
+    """Waits that give up at once, wherever a call is: reported or not needed, call after call, and then results are
+    right."""
+    ctx = sp.Context(0)
+    x, codes, scales, _ = _inputs(M, 2048, 1024, 128, False)
+    w = sp.W4(ctx, codes.cuda(), scales.cuda())
+    y = torch.empty(M, 1024, device="cuda")
+    xd = x.cuda()
+    ctx.sync()
+    ctx.set_wait_limit(1)
+    for _ in range(10):
+        sp.sparoa_gemm_w4(ctx, xd, w, y)
+        try:
+            ctx.sync()
+        except sp.SparoaError as e:
+            assert e.status == sp.ERR_TIMEOUT
+    ctx.set_wait_limit(0)
+    sp.sparoa_gemm_w4(ctx, xd, w, y)
+    ctx.sync()
+    w64 = _weights64(codes, scales, None, 128)
+    _check(y, x.double() @ w64.t(), _bound(x, w64, 128), False, "after waits that gave up")
+    ctx.close()
