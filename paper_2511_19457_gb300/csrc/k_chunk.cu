@@ -493,32 +493,33 @@ __device__ __forceinline__ void cap_in_place(const Capped& cap, uint32_t ts) {
   tmem_wait_st();
 }
 
-// 32 scores less slope times distance; the first key's distance is `far`.
-__device__ __forceinline__ void bias_scores(const RowRules& u, uint32_t (&s)[32], float far, float one) {
-#pragma unroll
-  for (int k = 0; k < 32; ++k) s[k] = __float_as_uint(fmaf(-u.slope, fabsf(far - (float)k), __uint_as_float(s[k]) * one));
-}
-
-// -infinity for what the row does not see of 32 keys; with a bias in a tree, an ancestor's
-// distance there for the one in the cache.
+// 32 scores of keys from key0 on less slope times distance.
 template <int RULES>
-__device__ __forceinline__ void mask_scores(const PagedArgs& a, const RowRules& u, uint32_t (&s)[32], int key0) {
-  const uint32_t w = u.template seen32<(RULES & kTree) != 0>(key0);
-  if ((RULES & kTree) && (RULES & kBias) && a.slopes && key0 + 32 > u.base) {
+__device__ __forceinline__ void bias_scores(const RowRules& u, uint32_t (&s)[32], int key0, float one) {
+  const float far = (float)(u.pos - key0);
+  if ((RULES & kTree) && key0 + 32 > u.base) {
 #pragma unroll
     for (int k = 0; k < 32; ++k)
-      if (key0 + k >= u.base && (w >> k & 1u))
-        s[k] = __float_as_uint(fmaf(u.slope, fabsf((float)(u.pos - key0 - k)) - (float)u.above(key0 + k), __uint_as_float(s[k])));
+      s[k] = __float_as_uint(fmaf(-u.slope, u.distance(key0 + k, fabsf(far - (float)k)), __uint_as_float(s[k]) * one));
+  } else {
+#pragma unroll
+    for (int k = 0; k < 32; ++k) s[k] = __float_as_uint(fmaf(-u.slope, fabsf(far - (float)k), __uint_as_float(s[k]) * one));
   }
+}
+
+// -infinity for what the row does not see of 32 keys.
+template <int RULES>
+__device__ __forceinline__ void mask_scores(const RowRules& u, uint32_t (&s)[32], int key0) {
+  const uint32_t w = u.template seen32<(RULES & kTree) != 0>(key0);
 #pragma unroll
   for (int k = 0; k < 32; ++k)
     if (!(w & (1u << k))) s[k] = 0xFF800000u;
 }
 
 template <int RULES>
-__device__ __forceinline__ void mask_unit(const PagedArgs& a, const RowRules& u, uint32_t (&s)[4][32], int key0) {
+__device__ __forceinline__ void mask_unit(const RowRules& u, uint32_t (&s)[4][32], int key0) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) mask_scores<RULES>(a, u, s[i], key0 + i * 32);
+  for (int i = 0; i < 4; ++i) mask_scores<RULES>(u, s[i], key0 + i * 32);
 }
 
 // A unit's scores, which are at `ts` too, under their row's cap and bias.
@@ -546,7 +547,7 @@ __device__ __forceinline__ void rule_scores(const PagedArgs& a, const RowRules& 
   }
   if ((RULES & kBias) && (!(RULES & kTree) || a.slopes)) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) bias_scores(u, s[i], (float)(u.pos - key0 - i * 32), caps ? 1.f : a.score_log2);
+    for (int i = 0; i < 4; ++i) bias_scores<RULES>(u, s[i], key0 + i * 32, caps ? 1.f : a.score_log2);
   }
 }
 
@@ -654,8 +655,8 @@ __device__ __forceinline__ float changed_unit(const PagedArgs& a, const RowRules
       if (caps && near)
 #pragma unroll
         for (int k = 0; k < 32; k += 2) put_pair(s, k, Capped(a).near(pair_at(s, k)));
-      if (slopes) bias_scores(u, s, far - (float)(i * 32), caps ? 1.f : a.score_log2);
-      if (!whole) mask_scores<RULES>(a, u, s, key0 + i * 32);
+      if (slopes) bias_scores<RULES>(u, s, key0 + i * 32, caps ? 1.f : a.score_log2);
+      if (!whole) mask_scores<RULES>(u, s, key0 + i * 32);
       float t[4];
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
@@ -802,7 +803,7 @@ __device__ __forceinline__ void softmax_role(const Role<walk_of(RULES)>& r, uint
 #pragma unroll
             for (int i = 0; i < 4; ++i) tmem_wait_ld32(s[i]);
             rule_scores<RULES>(a, rule, s, ts, key0);
-            if (!whole) mask_unit<RULES>(a, rule, s, key0);
+            if (!whole) mask_unit<RULES>(rule, s, key0);
             float mx[4];
             maxima(s, mx);
             const float nz = refer(largest(mx), j == j0);
@@ -820,7 +821,7 @@ __device__ __forceinline__ void softmax_role(const Role<walk_of(RULES)>& r, uint
           for (int i = 0; i < 4; ++i) tmem_wait_ld32(s[i]);
           if (!__all_sync(0xffffffffu, key0 >= low && key0 + kUnitKeys <= lim)) {
             if constexpr ((RULES & kTree) != 0) {
-              mask_unit<RULES>(a, rule, s, key0);
+              mask_unit<RULES>(rule, s, key0);
             } else {
               const int from = low - key0, to_ = lim - key0;
 #pragma unroll

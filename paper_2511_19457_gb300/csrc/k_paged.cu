@@ -255,25 +255,19 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
           if ((RULES & kBias) && (!(RULES & kTree) || a.slopes)) {
             const float far[2] = {(float)(rule[0].pos - key0), (float)(rule[1].pos - key0)}, one = a.cap > 0.f ? 1.f : a.score_log2;
-#pragma unroll
-            for (int nt = 0; nt < 2; ++nt)
-#pragma unroll
-              for (int e = 0; e < 4; ++e)
-                s[nt][e] = fmaf(-rule[e >> 1].slope, fabsf(far[e >> 1] - (float)(nt * 8 + 2 * tq + (e & 1))), s[nt][e] * one);
-          }
-          const uint32_t seen[2] = {rule[0].seen32<(RULES & kTree) != 0>(key0), rule[1].seen32<(RULES & kTree) != 0>(key0)};
-          if ((RULES & kBias) && (RULES & kTree) && a.slopes && key0 + kKeys > rule[0].base) {
-            // ancestors: their distance in the tree for the one in the cache
+            const bool drafted = (RULES & kTree) && key0 + kKeys > rule[0].base;
 #pragma unroll
             for (int nt = 0; nt < 2; ++nt)
 #pragma unroll
               for (int e = 0; e < 4; ++e) {
                 const RowRules& u = rule[e >> 1];
-                const int key = key0 + nt * 8 + 2 * tq + (e & 1);
-                if (key >= u.base && key < cc.len)
-                  s[nt][e] = fmaf(u.slope, fabsf((float)(u.pos - key)) - (float)u.above(key), s[nt][e]);
+                const int k = nt * 8 + 2 * tq + (e & 1);
+                float d = fabsf(far[e >> 1] - (float)k);
+                if (drafted) d = u.distance(key0 + k, d);
+                s[nt][e] = fmaf(-u.slope, d, s[nt][e] * one);
               }
           }
+          const uint32_t seen[2] = {rule[0].seen32<(RULES & kTree) != 0>(key0), rule[1].seen32<(RULES & kTree) != 0>(key0)};
 #pragma unroll
           for (int nt = 0; nt < 2; ++nt)
 #pragma unroll

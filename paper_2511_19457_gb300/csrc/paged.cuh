@@ -404,8 +404,10 @@ struct RowRules {
     }
     return w;
   }
-  // how far up an ancestor at key `key` is
-  __device__ __forceinline__ int above(int key) const { return __popcll(tree >> (key - base) >> 1); }
+  // how far the key is that lies `there` away in the cache: an ancestor, as far as it is up
+  __device__ __forceinline__ float distance(int key, float there) const {
+    return key >= base && key - base < 64 ? (float)__popcll(tree >> (key - base) >> 1) : there;
+  }
 };
 
 // The table's entry for key `key` of sequence b, as it is (loaded ahead of its use).
