@@ -154,6 +154,8 @@ class Decoder:
         chooses nothing (no logit is a number above -infinity), that is an error, and the cache as it was."""
         if len(drafts) != len(seqs) or len(set(seqs)) != len(seqs):
             raise ValueError("check: a tree for each sequence, and no sequence twice")
+        if not drafts:
+            return []
         new = [len(t) for t, _ in drafts]
         bits = [b for _, parents in drafts for b in ancestors(parents)]
         if any(len(t) != len(p) or not t or p[0] != -1 for t, p in drafts):
@@ -248,7 +250,8 @@ class Decoder:
         `chunk` tokens each, all sequences together, then one token of each at a time.  No prompts:
         no tokens; an empty prompt, which nothing can be said after, is refused.
           draft      a function of a sequence's tokens so far: (tokens, parents) that may come next, parents by
-                     their number among them, -1 behind the last token; they are judged together (check)
+                     their number among them, -1 behind the last token; they are judged together (check), and
+                     hold pages of the cache until they are
           penalties  (repetition, presence, frequency, temperature) of every sequence
           bias       fp32 [vocab] on the logits
           allowed    a function of a sequence's tokens so far: int32 [words], bit v % 32 of word v / 32 for

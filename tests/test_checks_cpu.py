@@ -93,3 +93,7 @@ def test_tokens_outside_the_vocabulary(model):
         with pytest.raises(ValueError):
             model.generate([[1], [2]], 4, draft=lambda text: ([bad], [-1]))
     assert (sorted(model.pages.free), model.pages.held, model.pages.length) == before
+
+
+def test_nothing_to_check(model):
+    assert model.check([], []) == []
