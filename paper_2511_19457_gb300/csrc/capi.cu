@@ -1640,8 +1640,16 @@ sparoa_status attend(sparoa_ctx* ctx, const void* q, int64_t ld_q, int64_t T, in
         // roundings a score is off by 3 2^-24 of itself)
         const double c[4] = {1.0, -0.3333233349423876, 0.13289726199165688, -0.04848729234102447};
         constexpr double most = 1.7e38;  // (twice that is finite)
-        a.cap_turn = (float)std::min((double)scale / rules->cap, most);
-        for (int i = 0; i < 4; ++i) a.cap_near[i] = (float)(c[i] * std::min(scale * 1.4426950408889634, most));
+        const double turn = (double)scale / rules->cap, unit = std::min(scale * 1.4426950408889634, most);
+        bool fits = true;
+        for (int i = 0; i < 4; ++i) {
+          const double k = c[i] * unit * std::pow(turn, 2 * i);
+          fits = fits && std::fabs(k) > 1e-36 && std::fabs(k) < 1e36;
+          a.cap_near[i] = (float)(c[i] * unit);
+          a.cap_folded[i] = (float)std::max(-most, std::min(k, most));
+        }
+        a.cap_turn = (float)std::min(turn, most);
+        a.cap_small = fits ? (float)(0.375 / turn) : -1.f;
         a.cap_log2 = (float)std::min(rules->cap * 1.4426950408889634, most);
       }
       if (rules->cap > 0.f || rules->slopes) {  // (changed scores are powers of 2: paged.cuh)

@@ -325,32 +325,40 @@ __host__ __device__ constexpr int walk_of(int rules) { return rules == kPlain ? 
 // Scores under a cap or with a bias are weighed as powers of 2: log2(e) (cap tanh(scale q k /
 // cap) - slope distance).  Where |t| = |scale q k / cap| <= 3/8, as it mostly is, tanh(t) =
 // t p(t^2), on packed pairs, off by 3 2^-24 of itself; else 1 - 2 / (1 + exp(2 |t|)) with t's
-// sign, off by 9 2^-24 of itself at most.  (To 1/2 p takes a coefficient more, and 4 chunks of 1500 as in
-// k_chunk.cu 117 us where they take 113.)  Which of them a score goes by is its own affair:
-// `near` is for scores that are all small, `far` for any, with the same bits for a small one,
-// so that a score's value does not depend on those beside it.
+// sign, off by 9 2^-24 of itself at most.  (To 1/2 p takes a coefficient more.)  Which of them a
+// score goes by is its own affair: `near` is for scores that are all small, `far` for any, with
+// the same bits for a small one, so that a score's value does not depend on those beside it.
+// p's coefficients hold powers of scale / cap, which saves the product for t (4 chunks of 1500 as
+// in k_chunk.cu 113 us with it, 109 so; a prompt of 4000 163 and 156).  Where one of them leaves the
+// normal range, as for caps far above any score, no score counts as small, and `far` makes t.
 struct Capped {
-  static constexpr float kNear = 0.375f;
   const PagedArgs& a;
   __device__ __forceinline__ explicit Capped(const PagedArgs& args) : a(args) {}
-  __device__ __forceinline__ bool near(float top) const { return top * a.cap_turn <= kNear; }
-  __device__ __forceinline__ f2_t turn(f2_t s) const { return fmul2(s, f2(a.cap_turn, a.cap_turn)); }
-  // what s is multiplied by (t goes into its square alone, so that no size of scale or cap leaves the range)
-  __device__ __forceinline__ f2_t factor(f2_t s, float part) const {
-    const float c0 = a.cap_near[0] * part, c1 = a.cap_near[1] * part, c2 = a.cap_near[2] * part, c3 = a.cap_near[3] * part;
-    const f2_t t = turn(s), w = fmul2(t, t);
+  __device__ __forceinline__ bool near(float top) const { return top <= a.cap_small; }
+  static __device__ __forceinline__ f2_t poly(const float (&c)[4], f2_t w, float part) {
+    const float c0 = c[0] * part, c1 = c[1] * part, c2 = c[2] * part, c3 = c[3] * part;
     return ffma2(w, ffma2(w, ffma2(w, f2(c3, c3), f2(c2, c2)), f2(c1, c1)), f2(c0, c0));
   }
+  // what a small score is multiplied by
+  __device__ __forceinline__ f2_t factor(f2_t s, float part) const { return poly(a.cap_folded, fmul2(s, s), part); }
   __device__ __forceinline__ f2_t near(f2_t s) const { return fmul2(s, factor(s, 1.f)); }
   __device__ __forceinline__ f2_t far(f2_t s) const {
     constexpr float e = 2.885390081777927f;
+    const f2_t t = fmul2(s, f2(a.cap_turn, a.cap_turn));
     float tx, ty, x, y, u, v;
-    f2_split(turn(s), tx, ty);
+    f2_split(t, tx, ty);
     f2_split(fmul2(f2(fabsf(tx), fabsf(ty)), f2(e, e)), x, y);
     f2_split(fadd2(f2(ex2_ftz(x), ex2_ftz(y)), f2(1.f, 1.f)), x, y);
     f2_split(ffma2(f2(rcp_ftz(x), rcp_ftz(y)), f2(-2.f * a.cap_log2, -2.f * a.cap_log2), f2(a.cap_log2, a.cap_log2)), x, y);
-    f2_split(near(s), u, v);
-    return f2(fabsf(tx) <= kNear ? u : copysignf(x, tx), fabsf(ty) <= kNear ? v : copysignf(y, ty));
+    x = copysignf(x, tx);
+    y = copysignf(y, ty);
+    if (a.cap_small >= 0.f) {
+      f2_split(near(s), u, v);
+      f2_split(s, tx, ty);
+      return f2(fabsf(tx) <= a.cap_small ? u : x, fabsf(ty) <= a.cap_small ? v : y);
+    }
+    f2_split(fmul2(s, poly(a.cap_near, fmul2(t, t), 1.f)), u, v);  // (no power leaves the range here)
+    return f2(fabsf(tx) <= 0.375f ? u : x, fabsf(ty) <= 0.375f ? v : y);
   }
   __device__ __forceinline__ float near1(float s) const {
     float x, y;

@@ -299,6 +299,8 @@ struct PagedArgs {
   float cap = 0.f;                   // above 0: scores s become cap tanh(s / cap)
   float cap_turn = 0.f;              // t = cap_turn s = scale s / cap
   float cap_near[4] = {};            // log2(e) cap tanh(t) = s p(t^2) where |t| <= 3/8
+  float cap_folded[4] = {};          // the same by s^2: with powers of cap_turn
+  float cap_small = 0.f;             // s up to which those do; below 0 where a power leaves the normal range
   float cap_log2 = 0.f;              // log2(e) cap
   float score_log2 = 0.f;            // scale log2(e)
   const float* slopes = nullptr;     // [heads] or null: less slope times the distance
