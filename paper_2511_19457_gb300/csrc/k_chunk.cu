@@ -582,19 +582,23 @@ __device__ __forceinline__ void weigh(uint32_t (&s)[4][32], uint32_t ts, f2_t sc
   }
 }
 
-// A unit of two tiles under a cap or a bias: weights of one part, and their sum.  The scores are
+// A unit of two tiles under a cap or a bias: weights of one part, and their sum.  (One bf16 part, as
+// without rules: results are off by 1.9e-3 of their norm in the first case below and 2.3e-3 in the
+// second, of which their own rounding is 1.7e-3; a second part is half as many MACs again.)  The scores are
 // walked twice, 32 at a time, read again from tensor memory: unrolled over all 128 the
 // instructions came too slowly (one of four issue slots was lost for want of them).
 //   direct   nothing is masked and the scores are small beside the cap: the first walk bounds the
 //            changed scores by the scores themselves (under a bias, of eight keys at a time), the
 //            second changes them on their way to their weights
-//   else     the first walk changes and masks them where they lie
+//   else     the first walk changes and masks them where they lie, after a walk of its own for the cap of
+//            large ones (such scores in most units: 171 us where the second case below takes 109 from memory)
 // Bound, as without rules, by a unit's chain of softmax and products, the softmax being longer.  4095
 // tokens, 32 heads of 64, slopes 2^-0.25 to 2^-8: 130 us, 114 without a bias; all changed where they lie
 // 177, with bounds of 32 keys 140, with 128 scores unrolled 208, the next 32 scores asked for ahead 180.
 // 4 chunks of 1500 over 1600 to 4000, 16 heads over 8 of 128, window 2048, a prefix of 577, a cap of
-// 30: 105 us, 90 without cap and prefix; with exponentials for the cap and one walk 216, with the polynomial
-// and one walk 143.  Dropped: dearer and cheaper units in the plan's costs (far units at 4, 3 and 2 fifths:
+// 30: 104 us, 90 without cap and prefix; with exponentials for the cap and one walk 216, with the polynomial
+// and one walk 143, with a large score's tanh beside the small ones' in that walk 8 % more (spilled
+// registers).  Dropped: dearer and cheaper units in the plan's costs (far units at 4, 3 and 2 fifths:
 // 139, 138 and 148 us, since they take nearly as long as others), heads in turn instead of one after the
 // other (132.5).
 template <int RULES, typename Refer>

@@ -10,10 +10,10 @@
 // taken away, which is exact, and mma.sync m16n8k16 sums the products with x in fp32 over a group; only that
 // sum is multiplied by the scale.  So nothing is rounded before the result but fp32 sums.
 //
-// 16 tokens x 4096 columns x 14336 rows, groups of 128, from memory: 14.7 us, 2.1 TB/s.  The copies alone
-// (no product, no numbers made of codes) 10.5, without the numbers of codes 13, without the products 15: half
-// of it is a launch, the first bytes' way and the cluster's sum (4.5 us for 2048 x 2048), and the rest waits
-// on issue slots (48 % busy) and the logic pipe (49 %).  Tried: weights straight from memory to registers,
+// 16 tokens x 4096 columns x 14336 rows, groups of 128, from memory: 14.0 us, 2.2 TB/s.  The copies alone
+// (no product, no numbers made of codes) 10.5, without the numbers of codes 13: a third of it is a launch, the
+// first bytes' way and the cluster's sum (4.5 us for 2048 x 2048), and the rest waits on issue slots (46 %
+// busy) and the logic pipe (47 %).  Tried: weights straight from memory to registers,
 // without copies (slower), 24 warps of three teams (slower), shifts as multiplications (slower), the weights
 // into the L2 before the kernel before ends (16.4), no teams (24.6).
 #include "w4.cuh"
@@ -274,7 +274,7 @@ bool w4_x_map(CUtensorMap* m, W4Args* a, int tokens, int halves) {
 cudaError_t launch_w4(W4Args a, cudaStream_t s) {
   a.row_tiles = (a.N + 15) / 16;
   a.tiles = (a.K + kTileK - 1) / kTileK;
-  // up to 16 tokens as columns of mma.sync: 16 tokens x 4096 x 14336 14.7 us, on tcgen05 17.8; x 14336 x 4096
+  // up to 16 tokens as columns of mma.sync: 16 tokens x 4096 x 14336 14.0 us, on tcgen05 17.8; x 14336 x 4096
   // 15.8 and 16.2, x 2048 x 2048 5.2 and 5.9, in groups of 32 x 4096 x 14336 15.2 and 22.9; but 24 tokens 18.9
   // and 15.1, 64 38.5 and 17.1
   if (a.M > 16) return launch_w4_tc(a, s);

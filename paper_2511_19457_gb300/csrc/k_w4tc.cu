@@ -7,7 +7,7 @@
 // only the fp32 sums of a group are multiplied by its scale: nothing is rounded but fp32 sums.
 //
 // Bound by the bytes of the weights, read once for 64 tokens; beside them x comes from the L2 for every
-// block of rows.  61 tokens x 14336 columns x 4096 rows, groups of 128, from memory: 17.3 us.  Its products
+// block of rows.  61 tokens x 14336 columns x 4096 rows, groups of 128, from memory: 17.0 us.  Its products
 // with A from tensor memory take 64 to 70 cycles each, whatever the number of tokens: 600 a tile of
 // 128 x 128, 28 tiles a CTA in clusters of 4, 9 us; the rest is the start, the first tile and the cluster's
 // sum.  On mma.sync the products alone cannot take less than 12.6 us (0.5 an SM and cycle), and with the codes'

@@ -329,7 +329,7 @@ __host__ __device__ constexpr int walk_of(int rules) { return rules == kPlain ? 
 // score goes by is its own affair: `near` is for scores that are all small, `far` for any, with
 // the same bits for a small one, so that a score's value does not depend on those beside it.
 // p's coefficients hold powers of scale / cap, which saves the product for t (4 chunks of 1500 as
-// in k_chunk.cu 113 us with it, 109 so; a prompt of 4000 163 and 156).  Where one of them leaves the
+// in k_chunk.cu 107 us with it, 104 so).  Where one of them leaves the
 // normal range, as for caps far above any score, no score counts as small, and `far` makes t.
 struct Capped {
   const PagedArgs& a;
