@@ -138,7 +138,8 @@ class Decoder:
 
     def forward(self, tokens: torch.Tensor, seqs, new) -> torch.Tensor:
         """tokens int64 [T], below the vocabulary's size (check and generate look, this does not), new[i] of
-        each of seqs one after the other, appended to their cached ones; returns the logits [T, vocab] (fp32).  A step that raises changes no sequence's length."""
+        each of seqs one after the other, appended to their cached ones; returns the logits [T, vocab]
+        (fp32).  A step that raises changes no sequence's length."""
         self.pages.grow_all(seqs, new)
         try:
             return self._forward(tokens, seqs, new)
